@@ -32,9 +32,9 @@
  *    variable LMOP_INJECT_LAUNCH_FAILURE=<kernel name>:<n>, read by
  *    lmop_create, makes the n-th launch of that kernel on the ctx fail as a
  *    HIP launch error would, without launching it.
- *  - All calls are synchronous with respect to the host: when they return,
- *    their device work on the ctx stream has completed, also when they
- *    return an error.
+ *  - All calls but the operators at the end of this file are synchronous with
+ *    respect to the host: when they return, their device work on the ctx
+ *    stream has completed, also when they return an error.
  */
 #ifndef LMOP_H
 #define LMOP_H
@@ -360,6 +360,106 @@ typedef struct {
 lmop_status lmop_set_profiling(lmop_ctx* ctx, int32_t period);
 lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t max_entries,
                                   int32_t* n_entries);
+
+/* ------------------------------------------------------------------ operators
+ * The steps of a decoder layer with block-scaled FP8 linear maps and
+ * normalised queries and keys, on the caller's own tensors.  Row evaluation
+ * calls the same kernels for weights of format LMOP_W_FP8_BLOCK and after
+ * lmop_load_qk_norms.
+ *
+ * Unlike the calls above, an operator only queues its kernel on the ctx's
+ * stream and returns: the tensors must stay alive until the stream has passed
+ * it, work that writes them must be ordered before it, and a caller may
+ * capture it into a HIP graph (with profiling off).  It allocates nothing,
+ * uses no workspace and no state of the ctx other than what is said at each
+ * one, and leaves the calling thread's current device as it was.  The ctx
+ * needs no weights.  Tensors are device memory of the ctx's device; strides
+ * are in elements between rows; the elements of a row are adjacent; what
+ * lies between rows is not written.  An output may not overlap an input
+ * unless said.  A size of zero is a no-op.  Results do not depend on which
+ * other rows are in the call, bit for bit. */
+typedef enum { LMOP_F16 = 0, LMOP_BF16 = 1, LMOP_F32 = 2 } lmop_dtype;
+
+/* Features that share one scale. */
+#define LMOP_FP8_GROUP 128
+
+/* Quantises y = x, or y = silu(gate) * x (the middle of a SwiGLU MLP,
+ * computed in fp32), to OCP E4M3 codes with one fp32 scale per row and group
+ * of 128 features (the last group of a row may be shorter):
+ *   amax = max(|y| over the group, 2^-40), scale = amax / 448,
+ *   q = e4m3(y * (448 / amax)), rounded to nearest even.
+ * A group that holds an infinity or a NaN gets a NaN scale and NaN codes. */
+typedef struct {
+  const void* x;    /* [rows][cols] of dtype */
+  const void* gate; /* NULL, or [rows][cols] of dtype */
+  uint8_t* q;       /* [rows][cols] codes, 16-byte aligned; the bytes from cols up to the next
+                       multiple of 16 are set to zero */
+  float* scale;     /* [rows][ceil(cols / 128)] */
+  int64_t ldx, ldg; /* >= cols */
+  int64_t ldq;      /* >= cols, a multiple of 16 */
+  int64_t lds;      /* >= ceil(cols / 128) */
+  int32_t rows, cols;
+  int32_t dtype;    /* LMOP_F16, LMOP_BF16 or LMOP_F32 */
+} lmop_quantize_args;
+lmop_status lmop_quantize(lmop_ctx* ctx, const lmop_quantize_args* args);
+
+/* C = A B^T, or C = add + A B^T, of E4M3 codes with block scales:
+ *   C[i][j] = add[i][j] + sum over groups g of a_scale[i][g] * b_scale[j / 128][g]
+ *             * (sum over the features f of g of a[i][f] * b[j][f])
+ * The sums are held in fp32 and rounded to dtype once; the groups are added
+ * in order of g.  NaN codes give NaN. */
+typedef struct {
+  const uint8_t* a;     /* [m][k] codes (tokens), 16-byte aligned */
+  const float* a_scale; /* [m][ceil(k / 128)] */
+  const uint8_t* b;     /* [n][k] codes (a weight's rows), 16-byte aligned */
+  const float* b_scale; /* [ceil(n / 128)][ceil(k / 128)] */
+  const float* add;     /* NULL, or fp32 [m][n]; may be c itself if dtype is LMOP_F32 and
+                           ldadd == ldc */
+  void* c;              /* [m][n] of dtype */
+  int64_t lda, ldb;     /* >= k, multiples of 16, at most 2^23; the bytes of a row from k up to
+                           the next multiple of 16 are read and have no effect */
+  int64_t ldas, ldbs;   /* >= ceil(k / 128) */
+  int64_t ldadd, ldc;   /* >= n */
+  int32_t m, n, k;      /* k = 0: C = add, or zero */
+  int32_t dtype;        /* LMOP_F16, LMOP_BF16 or LMOP_F32 */
+} lmop_matmul_args;
+lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* args);
+
+/* How values are stored: a token's row [slot][n_kv_heads * head_dim], or
+ * transposed [n_kv_heads * head_dim][slot] (the layout of the library's own
+ * KV stores). */
+#define LMOP_V_ROWS 0
+#define LMOP_V_COLUMNS 1
+
+/* What lies between the Q, K, V projections and attention, for a batch of
+ * tokens: RMSNorm of every query and key head with a gain per dimension,
+ * rotate-half RoPE at the token's position, and the write of keys and values
+ * into a cache.  For each head x of q and k:
+ *   y = x / sqrt(mean(x^2) + rms_eps) * gain   (gain NULL: y = x)
+ *   out = y rotated by the angles pos * rope_theta^(-2 i / head_dim)
+ * in fp32, rounded once; v is copied.  The head counts, head_dim, rms_eps,
+ * rope_theta and max_seq are the ctx's.  A token at a position outside
+ * [0, max_seq) gets NaN queries and keys. */
+typedef struct {
+  const void *q, *k, *v; /* [n_tokens][n_heads * head_dim], [n_tokens][n_kv_heads * head_dim]
+                            twice; each may be NULL: then it has no output */
+  const float* q_gain;   /* NULL or fp32 [head_dim] */
+  const float* k_gain;   /* NULL or fp32 [head_dim] */
+  const int32_t* pos;    /* [n_tokens] */
+  const int32_t* slot;   /* NULL (token i's slot is i), or [n_tokens]: the slot of its key and
+                            value; outside [0, n_slots): neither is written.  Two tokens with
+                            one slot: either's key and value may stay */
+  void* q_out;           /* [n_tokens][n_heads * head_dim]; may be q itself */
+  void* k_out;           /* [n_slots][n_kv_heads * head_dim]; may be k itself without slots */
+  void* v_out;           /* LMOP_V_ROWS: [n_slots][n_kv_heads * head_dim];
+                            LMOP_V_COLUMNS: [n_kv_heads * head_dim][n_slots] */
+  int64_t ldq, ldk, ldv, ldqo, ldko; /* >= the row's length */
+  int64_t ldvo;                      /* >= the row's length; LMOP_V_COLUMNS: >= n_slots */
+  int32_t n_tokens, n_slots;
+  int32_t v_layout;      /* LMOP_V_ROWS or LMOP_V_COLUMNS */
+  int32_t dtype;         /* LMOP_F16 or LMOP_BF16, of all tensors */
+} lmop_qk_norm_rope_args;
+lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* args);
 
 #ifdef __cplusplus
 }

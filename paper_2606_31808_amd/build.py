@@ -15,7 +15,8 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "liblmop.so")
-SOURCES = ["gemm.hip", "attention.hip", "elementwise.hip", "lmop_api.cpp"]
+SOURCES = ["gemm.hip", "attention.hip", "elementwise.hip", "fp8_matmul.hip", "quantize.hip",
+           "qk_norm_rope.hip", "lmop_api.cpp"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

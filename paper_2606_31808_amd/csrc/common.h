@@ -8,6 +8,10 @@ typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16;
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 #define LMOP_DEVICE __device__ __forceinline__
 
@@ -16,6 +20,26 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 //   D: lane holds D[row 4g + r][col c], r = 0..3
 LMOP_DEVICE f32x4 mfma16x16x32(f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// v_mfma_f32_16x16x128_f8f6f4 of two E4M3 operands, accumulator zero: lane
+// 16g + c holds 32 features of row c of each operand (any 32 of the 128, the
+// same ones in both, a different set for each g); D as above.  Of the eight
+// products of a lane's 8 adjacent codes the instruction keeps the bits down
+// to 2^-13 of the largest one's leading bit (2^(sum of its two exponents))
+// and cuts the rest off; the sums of eights are added in fp32.  (Measured;
+// v_mfma_f32_16x16x32_fp8_fp8 does the same.)
+LMOP_DEVICE f32x4 mfma16x16x128_e4m3(i32x8 a, i32x8 b) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0,
+                                                          0, 0, 0);
+}
+
+// The 4 E4M3 codes of a word (byte 0 first) as fp16, exactly: every E4M3
+// value is an fp16 value, so a unit scale changes nothing.
+LMOP_DEVICE f16x4 fp8x4(uint32_t d) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, true);
+  return f16x4{a.x, a.y, b.x, b.y};
 }
 
 template <typename T>

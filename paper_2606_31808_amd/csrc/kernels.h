@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "lmop.h"
+
 namespace lmop {
 
 typedef uint16_t half_bits;  // fp16 storage as seen from host code
@@ -181,5 +183,19 @@ hipError_t launch_head_finalize(hipStream_t s, const float2* part, int n_chunks,
                                 const int32_t* allowed_tok, int R, HeadPick* out,
                                 const int32_t* row_state = nullptr,
                                 const uint8_t* state_mask = nullptr);
+
+// ---------------------------------------------------------------- block-scaled FP8 maps
+// The operators of include/lmop.h, with its argument structs: sizes above
+// zero, pointers and strides checked by the caller.
+hipError_t launch_quantize(hipStream_t s, const lmop_quantize_args& a);
+hipError_t launch_matmul_fp8(hipStream_t s, const lmop_matmul_args& a);
+struct QkArgs {
+  lmop_qk_norm_rope_args t;
+  int nq, nkv, hd;
+  float eps;
+  const float2* rope;  // [max_seq][hd/2] (cos, sin)
+  int max_seq;
+};
+hipError_t launch_qk_norm_rope(hipStream_t s, const QkArgs& a);
 
 }  // namespace lmop

@@ -39,7 +39,15 @@ LMOP_DEVICE void g2l16_m0(const void* sbase, uint32_t voff, uint32_t lds_addr) {
                : "memory");
 }
 
-// the same for the wave's first N lanes only; every lane must be active.  The
+// 4 bytes per lane from an address each: LDS at lds_addr + 4*lane
+LMOP_DEVICE void g2l4(const void* gaddr, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+               :
+               : "v"(gaddr), "s"(lds_addr)
+               : "memory");
+}
+
+// g2l16_m0 for the wave's first N lanes only; every lane must be active.  The
 // mask is set inside the asm, so the compiler sees no branch (a branch in a
 // pinned schedule lets it move the code around it)
 template <int N>

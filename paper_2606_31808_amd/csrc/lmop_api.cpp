@@ -43,6 +43,8 @@ constexpr size_t kDecodeGroupBytes = size_t(24) << 30;
 // KV store within the attention kernel's kMaxStoreSlots
 constexpr int kMaxSeq = 1 << 20;
 constexpr int kMaxBatchBudget = 1 << 21;
+// longest row of FP8 codes: a tile's row offsets fit 32 bits
+constexpr int64_t kMaxCodeRow = int64_t(1) << 23;
 
 int round_up(int x, int m) { return (x + m - 1) / m * m; }
 int64_t round_up64(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -1319,6 +1321,72 @@ lmop_status with_scratch(lmop_ctx* ctx, bool carve, char* base, size_t bytes, bo
   return st;
 }
 
+// ---------------------------------------------------------------- operator calls
+// An operator call up to its argument checks.
+lmop_status enter_operator(lmop_ctx* ctx, const void* args) {
+  if (!ctx) return LMOP_ERR_INVALID_ARG;
+  if (ctx->dead)
+    return fail(ctx, LMOP_ERR_DEVICE, "ctx is unusable after an earlier error (%s)",
+                ctx->err.c_str());
+  ctx->err.clear();
+  if (!args) return fail(ctx, LMOP_ERR_INVALID_ARG, "args is NULL");
+  return LMOP_OK;
+}
+
+// Queues one operator on the ctx's stream, with the ctx's device current for
+// the launch only.  Nothing here waits.
+template <typename F>
+lmop_status queue_operator(lmop_ctx* ctx, const char* name, double flops, double bytes,
+                                  F&& launch) {
+  if (ctx->host_only)
+    return fail(ctx, LMOP_ERR_UNSUPPORTED, "host-only ctx: arguments are valid, no device to run");
+  if (ctx->prof > 0) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    HIP_OK(ctx, hipStreamIsCapturing(ctx->stream, &cap));
+    if (cap != hipStreamCaptureStatusNone)
+      return fail(ctx, LMOP_ERR_STATE, "%s cannot be captured while profiling is on", name);
+  }
+  int before = -1;
+  HIP_OK(ctx, hipGetDevice(&before));
+  if (before != ctx->device) HIP_OK(ctx, hipSetDevice(ctx->device));
+  const lmop_status st = timed(ctx, name, flops, bytes, launch);
+  if (before != ctx->device) HIP_OK(ctx, hipSetDevice(before));
+  return st;
+}
+
+size_t dtype_bytes(int32_t dtype) { return dtype == LMOP_F32 ? 4 : 2; }
+
+// A tensor of rows of `len` elements of `esize` bytes, `ld` elements apart.
+lmop_status check_rows(lmop_ctx* c, const char* what, const void* p, int64_t len, int64_t ld,
+                              size_t esize, size_t align) {
+  if (!p) return fail(c, LMOP_ERR_INVALID_ARG, "%s is NULL", what);
+  if ((uintptr_t)p % align != 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "%s is not aligned to %zu bytes", what, align);
+  if (ld < len)
+    return fail(c, LMOP_ERR_INVALID_ARG, "%s: rows of %lld elements are %lld apart", what,
+                (long long)len, (long long)ld);
+  if (ld > (int64_t(1) << 40) / (int64_t)esize)
+    return fail(c, LMOP_ERR_UNSUPPORTED, "%s: rows %lld elements apart", what, (long long)ld);
+  return LMOP_OK;
+}
+
+// Rows of FP8 codes: read and written 16 bytes at a time.
+lmop_status check_codes(lmop_ctx* c, const char* what, const void* p, int64_t len,
+                               int64_t ld) {
+  LMOP_TRY(check_rows(c, what, p, len, ld, 1, 16));
+  if (ld % 16 != 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "%s: rows %lld bytes apart, not a multiple of 16", what,
+                (long long)ld);
+  if (ld > kMaxCodeRow)
+    return fail(c, LMOP_ERR_UNSUPPORTED, "%s: rows %lld bytes apart (at most %lld)", what,
+                (long long)ld, (long long)kMaxCodeRow);
+  return LMOP_OK;
+}
+
+int64_t fp8_groups(int64_t features) {
+  return (features + LMOP_FP8_GROUP - 1) / LMOP_FP8_GROUP;
+}
+
 }  // namespace
 
 // ====================================================================== ABI
@@ -2486,6 +2554,99 @@ lmop_status lmop_get_memory(const lmop_ctx* ctx, lmop_memory_stats* out) {
   out->workspace_bytes = ctx->user_ws_bytes;
   out->workspace_peak = ctx->user_ws_peak;
   return LMOP_OK;
+}
+
+// ---------------------------------------------------------------- operators
+lmop_status lmop_quantize(lmop_ctx* ctx, const lmop_quantize_args* a) {
+  LMOP_TRY(enter_operator(ctx, a));
+  if (a->rows < 0 || a->cols < 0)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "rows %d, cols %d", a->rows, a->cols);
+  if (a->dtype != LMOP_F16 && a->dtype != LMOP_BF16 && a->dtype != LMOP_F32)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
+  if (a->rows == 0 || a->cols == 0) return LMOP_OK;
+  const size_t es = dtype_bytes(a->dtype);
+  LMOP_TRY(check_rows(ctx, "x", a->x, a->cols, a->ldx, es, es));
+  if (a->gate) LMOP_TRY(check_rows(ctx, "gate", a->gate, a->cols, a->ldg, es, es));
+  LMOP_TRY(check_codes(ctx, "q", a->q, a->cols, a->ldq));
+  LMOP_TRY(check_rows(ctx, "scale", a->scale, fp8_groups(a->cols), a->lds, 4, 4));
+  const double e = (double)a->rows * a->cols;
+  return queue_operator(ctx, "quantize", e * (a->gate ? 10 : 4),
+                        e * (es * (a->gate ? 2 : 1) + 1) + 4.0 * a->rows * fp8_groups(a->cols),
+                        [&] { return launch_quantize(ctx->stream, *a); });
+}
+
+lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* a) {
+  LMOP_TRY(enter_operator(ctx, a));
+  if (a->m < 0 || a->n < 0 || a->k < 0)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "m %d, n %d, k %d", a->m, a->n, a->k);
+  if (a->dtype != LMOP_F16 && a->dtype != LMOP_BF16 && a->dtype != LMOP_F32)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
+  if (a->m == 0 || a->n == 0) return LMOP_OK;
+  if (a->k > 0) {
+    LMOP_TRY(check_codes(ctx, "a", a->a, a->k, a->lda));
+    LMOP_TRY(check_codes(ctx, "b", a->b, a->k, a->ldb));
+    LMOP_TRY(check_rows(ctx, "a_scale", a->a_scale, fp8_groups(a->k), a->ldas, 4, 4));
+    LMOP_TRY(check_rows(ctx, "b_scale", a->b_scale, fp8_groups(a->k), a->ldbs, 4, 4));
+  }
+  const size_t es = dtype_bytes(a->dtype);
+  LMOP_TRY(check_rows(ctx, "c", a->c, a->n, a->ldc, es, es));
+  if (a->add) {
+    LMOP_TRY(check_rows(ctx, "add", a->add, a->n, a->ldadd, 4, 4));
+    if ((const void*)a->add == a->c && (a->dtype != LMOP_F32 || a->ldadd != a->ldc))
+      return fail(ctx, LMOP_ERR_INVALID_ARG, "add is c, with another type or stride");
+  }
+  const double m = a->m, n = a->n, k = a->k;
+  return queue_operator(ctx, "matmul_fp8", 2 * m * n * k,
+                        m * k + n * k + m * n * (es + (a->add ? 4 : 0)),
+                        [&] { return launch_matmul_fp8(ctx->stream, *a); });
+}
+
+lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* a) {
+  LMOP_TRY(enter_operator(ctx, a));
+  const int64_t nqd = ctx->nq_dim, nkvd = ctx->nkv_dim;
+  if (a->n_tokens < 0 || a->n_slots < 0)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "n_tokens %d, n_slots %d", a->n_tokens, a->n_slots);
+  if (a->dtype != LMOP_F16 && a->dtype != LMOP_BF16)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "dtype %d (F16 or BF16)", a->dtype);
+  if (a->v_layout != LMOP_V_ROWS && a->v_layout != LMOP_V_COLUMNS)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown v_layout %d", a->v_layout);
+  if (a->n_tokens == 0 || (!a->q && !a->k && !a->v)) return LMOP_OK;
+  if ((a->k || a->v) && !a->slot && a->n_slots < a->n_tokens)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "%d tokens without slots, %d slots", a->n_tokens,
+                a->n_slots);
+  if ((a->q || a->k) && (!a->pos || (uintptr_t)a->pos % 4 != 0))
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "pos is NULL or misaligned");
+  if ((uintptr_t)a->slot % 4 != 0 || (uintptr_t)a->q_gain % 4 != 0 || (uintptr_t)a->k_gain % 4 != 0)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "slot or a gain is misaligned");
+  if (a->q) {
+    LMOP_TRY(check_rows(ctx, "q", a->q, nqd, a->ldq, 2, 2));
+    LMOP_TRY(check_rows(ctx, "q_out", a->q_out, nqd, a->ldqo, 2, 2));
+    if (a->q_out == a->q && a->ldqo != a->ldq)
+      return fail(ctx, LMOP_ERR_INVALID_ARG, "q_out is q, with another stride");
+  }
+  if (a->k) {
+    LMOP_TRY(check_rows(ctx, "k", a->k, nkvd, a->ldk, 2, 2));
+    LMOP_TRY(check_rows(ctx, "k_out", a->k_out, nkvd, a->ldko, 2, 2));
+    if (a->k_out == a->k && (a->ldko != a->ldk || a->slot))
+      return fail(ctx, LMOP_ERR_INVALID_ARG, "k_out is k, with slots or another stride");
+  }
+  if (a->v) {
+    LMOP_TRY(check_rows(ctx, "v", a->v, nkvd, a->ldv, 2, 2));
+    LMOP_TRY(check_rows(ctx, "v_out", a->v_out, a->v_layout == LMOP_V_ROWS ? nkvd : a->n_slots,
+                        a->ldvo, 2, 2));
+    if (a->v_out == a->v) return fail(ctx, LMOP_ERR_INVALID_ARG, "v_out is v");
+  }
+  const double e = (double)a->n_tokens * ((a->q ? nqd : 0) + (a->k ? nkvd : 0) + (a->v ? nkvd : 0));
+  QkArgs qa{};
+  qa.t = *a;
+  qa.nq = ctx->cfg.n_heads;
+  qa.nkv = ctx->cfg.n_kv_heads;
+  qa.hd = ctx->cfg.head_dim;
+  qa.eps = ctx->cfg.rms_eps;
+  qa.rope = ctx->rope_tab;
+  qa.max_seq = ctx->cfg.max_seq;
+  return queue_operator(ctx, "qk_norm_rope", 7 * e, 4 * e,
+                        [&] { return launch_qk_norm_rope(ctx->stream, qa); });
 }
 
 lmop_status lmop_set_profiling(lmop_ctx* ctx, int32_t period) {

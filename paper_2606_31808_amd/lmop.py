@@ -13,6 +13,7 @@ import os
 from typing import Optional, Sequence
 
 import numpy as np
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", "liblmop.so")
@@ -29,8 +30,12 @@ EXPORTED = (
     "lmop_create", "lmop_destroy", "lmop_last_error", "lmop_status_string", "lmop_load_weights",
     "lmop_set_prefix", "lmop_set_prefixes", "lmop_release_prefix", "lmop_prefix_length", "lmop_eval_rows",
     "lmop_dedup_rows", "lmop_set_profiling", "lmop_get_kernel_stats", "lmop_set_workspace",
-    "lmop_get_memory", "lmop_eval_rows_noalloc", "lmop_plan_rows",
+    "lmop_get_memory", "lmop_eval_rows_noalloc", "lmop_plan_rows", "lmop_quantize", "lmop_matmul",
+    "lmop_qk_norm_rope",
 )
+LMOP_F16, LMOP_BF16, LMOP_F32 = 0, 1, 2
+LMOP_FP8_GROUP = 128
+LMOP_V_ROWS, LMOP_V_COLUMNS = 0, 1
 # size of the static device array lmop_eval_rows_noalloc carves its scratch from
 LMOP_NOALLOC_SCRATCH_BYTES = 256 << 20
 
@@ -99,6 +104,29 @@ class lmop_kernel_stat(C.Structure):
                 ("total_ms", C.c_double), ("flops", C.c_double), ("bytes", C.c_double)]
 
 
+class lmop_quantize_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("gate", C.c_void_p), ("q", C.c_void_p), ("scale", C.c_void_p),
+                ("ldx", C.c_int64), ("ldg", C.c_int64), ("ldq", C.c_int64), ("lds", C.c_int64),
+                ("rows", C.c_int32), ("cols", C.c_int32), ("dtype", C.c_int32)]
+
+
+class lmop_matmul_args(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("a_scale", C.c_void_p), ("b", C.c_void_p),
+                ("b_scale", C.c_void_p), ("add", C.c_void_p), ("c", C.c_void_p),
+                ("lda", C.c_int64), ("ldb", C.c_int64), ("ldas", C.c_int64), ("ldbs", C.c_int64),
+                ("ldadd", C.c_int64), ("ldc", C.c_int64), ("m", C.c_int32), ("n", C.c_int32),
+                ("k", C.c_int32), ("dtype", C.c_int32)]
+
+
+class lmop_qk_norm_rope_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_gain", C.c_void_p),
+                ("k_gain", C.c_void_p), ("pos", C.c_void_p), ("slot", C.c_void_p),
+                ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("v_out", C.c_void_p),
+                ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldv", C.c_int64), ("ldqo", C.c_int64),
+                ("ldko", C.c_int64), ("ldvo", C.c_int64), ("n_tokens", C.c_int32),
+                ("n_slots", C.c_int32), ("v_layout", C.c_int32), ("dtype", C.c_int32)]
+
+
 RESULT_DTYPE = np.dtype([("value", "<i8"), ("logprob", "<f4"), ("logprob_full", "<f4"),
                          ("n_tokens", "<i4"), ("tokens", "<i4", (8,)), ("_pad", "<i4")])
 assert C.sizeof(lmop_result) == RESULT_DTYPE.itemsize
@@ -107,11 +135,10 @@ assert C.sizeof(lmop_result) == RESULT_DTYPE.itemsize
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2606_31808_amd.build`")
-    # torch ships its own HIP runtime under the same soname.  Loading it first
-    # makes the library bind to that one runtime: the streams and device
-    # pointers torch hands over are only valid there, and a second runtime
-    # loaded beside it finds no devices.
-    import torch  # noqa: F401
+    # torch (imported above) ships its own HIP runtime under the same soname.
+    # Loading it first makes the library bind to that one runtime: the streams
+    # and device pointers torch hands over are only valid there, and a second
+    # runtime loaded beside it finds no devices.
     lib = C.CDLL(LIB_PATH)
     vp, i32, st = C.c_void_p, C.c_int32, C.c_int
     sig = {
@@ -142,6 +169,9 @@ def _load():
         "lmop_set_profiling": (st, [vp, i32]),
         "lmop_get_kernel_stats": (st, [vp, C.POINTER(lmop_kernel_stat), i32,
                                        C.POINTER(C.c_int32)]),
+        "lmop_quantize": (st, [vp, C.POINTER(lmop_quantize_args)]),
+        "lmop_matmul": (st, [vp, C.POINTER(lmop_matmul_args)]),
+        "lmop_qk_norm_rope": (st, [vp, C.POINTER(lmop_qk_norm_rope_args)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -395,6 +425,123 @@ def lmop_get_kernel_stats(ctx):
             for i in range(n.value)}
 
 
+# ---------------------------------------------------------------- operators
+# Tensors here are torch tensors: inputs of rows with adjacent elements at any
+# row stride, outputs given or allocated by the Context methods below.
+_DTYPES = {torch.float16: LMOP_F16, torch.bfloat16: LMOP_BF16, torch.float32: LMOP_F32}
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _up(x: int, to: int) -> int:
+    return (x + to - 1) // to * to
+
+
+def _mat(t, what: str, rows: int, cols: int, dtypes, least: int = 0):
+    """(address, row stride) of a [rows][cols] tensor; a single row's stride does
+    not matter and counts as `least` (or the row's length)."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected ({rows}, {cols})")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what}: dtype {t.dtype}")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{what}: the elements of a row are not adjacent")
+    return t.data_ptr(), ld if rows > 1 else max(least, cols)
+
+
+def _codes(t, what: str, rows: int, cols: int):
+    """_mat of FP8 codes, whose rows are read to the next multiple of 16 bytes."""
+    most = _up(cols, 16)
+    p, ld = _mat(t, what, rows, cols, _CODES, most)
+    if most != cols and rows > 0 and (t.storage_offset() + (rows - 1) * ld + most >
+                                      t.untyped_storage().nbytes()):
+        raise ValueError(f"{what}: the last row's storage ends before {most} bytes")
+    return p, ld
+
+
+def _vec(t, what: str, n: int, dtype):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: expected {n} adjacent elements of {dtype}")
+    return t.data_ptr()
+
+
+def lmop_quantize(ctx, x, q, scale, gate=None) -> None:
+    """E4M3 codes q and scales of x, or of silu(gate) * x."""
+    rows, cols = x.shape
+    groups = (cols + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP
+    px, ldx = _mat(x, "x", rows, cols, _DTYPES)
+    pg, ldg = (None, 0) if gate is None else _mat(gate, "gate", rows, cols, (x.dtype,))
+    pq, ldq = _codes(q, "q", rows, cols)
+    ps, lds = _mat(scale, "scale", rows, groups, (torch.float32,))
+    a = lmop_quantize_args(px, pg, pq, ps, ldx, ldg, ldq, lds, rows, cols, _DTYPES[x.dtype])
+    st = _lib.lmop_quantize(ctx, C.byref(a))
+    if st:
+        _check(st, ctx)
+
+
+def lmop_matmul(ctx, a, a_scale, b, b_scale, c, add=None) -> None:
+    """c = a b^T (+ add) of E4M3 codes: scales per row and 128 features of a, per
+    128 x 128 block of b."""
+    (m, k), n = a.shape, b.shape[0]
+    groups = (k + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP
+    pa, lda = _codes(a, "a", m, k)
+    pb, ldb = _codes(b, "b", n, k)
+    f32 = (torch.float32,)
+    psa, ldas = _mat(a_scale, "a_scale", m, groups, f32)
+    psb, ldbs = _mat(b_scale, "b_scale", (n + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP, groups, f32)
+    pc, ldc = _mat(c, "c", m, n, _DTYPES)
+    pd, ldadd = (None, 0) if add is None else _mat(add, "add", m, n, f32)
+    s = lmop_matmul_args(pa, psa, pb, psb, pd, pc, lda, ldb, ldas, ldbs, ldadd, ldc, m, n, k,
+                         _DTYPES[c.dtype])
+    st = _lib.lmop_matmul(ctx, C.byref(s))
+    if st:
+        _check(st, ctx)
+
+
+def lmop_qk_norm_rope(ctx, shape, n_tokens, q=None, k=None, v=None, pos=None, q_gain=None,
+                      k_gain=None, slot=None, q_out=None, k_out=None, v_out=None,
+                      v_columns: bool = False) -> None:
+    """Per-head RMSNorm, RoPE and cache write of n_tokens tokens; shape is the
+    ctx's (n_heads, n_kv_heads, head_dim)."""
+    nq, nkv, hd = shape
+    first = next((t for t in (q, k, v) if t is not None), None)
+    if first is None:
+        raise ValueError("q, k and v are all None")
+    dt = (first.dtype,)
+    if first.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"dtype {first.dtype}: float16 or bfloat16")
+    n_slots = None
+    if k is not None and k_out is not None:
+        n_slots = k_out.shape[0]
+    if v is not None and v_out is not None:
+        ns = v_out.shape[1 if v_columns else 0]
+        if n_slots not in (None, ns):
+            raise ValueError(f"k_out has {n_slots} slots, v_out {ns}")
+        n_slots = ns
+    n_slots = n_slots or 0
+
+    def mat(t, what, rows, cols):
+        return (None, 0) if t is None else _mat(t, what, rows, cols, dt)
+
+    pq, ldq = mat(q, "q", n_tokens, nq * hd)
+    pk, ldk = mat(k, "k", n_tokens, nkv * hd)
+    pv, ldv = mat(v, "v", n_tokens, nkv * hd)
+    pqo, ldqo = mat(q_out if q is not None else None, "q_out", n_tokens, nq * hd)
+    pko, ldko = mat(k_out if k is not None else None, "k_out", n_slots, nkv * hd)
+    pvo, ldvo = mat(v_out if v is not None else None, "v_out",
+                    *((nkv * hd, n_slots) if v_columns else (n_slots, nkv * hd)))
+    a = lmop_qk_norm_rope_args(
+        pq, pk, pv, _vec(q_gain, "q_gain", hd, torch.float32),
+        _vec(k_gain, "k_gain", hd, torch.float32), _vec(pos, "pos", n_tokens, torch.int32),
+        _vec(slot, "slot", n_tokens, torch.int32), pqo, pko, pvo, ldq, ldk, ldv, ldqo, ldko, ldvo,
+        n_tokens, n_slots, LMOP_V_COLUMNS if v_columns else LMOP_V_ROWS, _DTYPES[first.dtype])
+    st = _lib.lmop_qk_norm_rope(ctx, C.byref(a))
+    if st:
+        _check(st, ctx)
+
+
 # ---------------------------------------------------------------- convenience
 def config_from_shape(shape, max_seq: int = 0) -> lmop_config:
     return lmop_config(shape.n_layers, shape.d_model, shape.n_heads, shape.n_kv_heads,
@@ -411,6 +558,10 @@ class Context:
         if n_layers is not None:
             cfg.n_layers = n_layers
         self.vocab = shape.vocab
+        self.heads = (cfg.n_heads, cfg.n_kv_heads, cfg.head_dim)
+        # where the operators' tensors live, and the torch stream they are ordered on
+        self.device = torch.device("cuda", device) if device >= 0 else torch.device("cpu")
+        self.stream = int(stream or 0)
         self.ctx = lmop_create(cfg, device, stream)
 
     def close(self):
@@ -463,3 +614,52 @@ class Context:
 
     def kernel_stats(self):
         return lmop_get_kernel_stats(self.ctx)
+
+    # -- operators: they queue work on the ctx's stream and return
+    def _ready(self, *tensors):
+        """The tensors are on the ctx's device, and torch's current stream is the
+        ctx's: a ctx made without a stream has one that the null stream orders."""
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"a tensor is on {t.device}, the ctx on {self.device}")
+        if (self.device.type == "cuda" and
+                torch.cuda.current_stream(self.device).cuda_stream != self.stream):
+            raise ValueError("torch's current stream is not the ctx's stream: make the Context "
+                             "with stream=..., or call under torch.cuda.stream(...)")
+
+    def quantize(self, x, gate=None, out=None):
+        """E4M3 codes [rows, cols] (torch.float8_e4m3fn, rows a multiple of 16 bytes
+        apart) and float32 scales [rows, ceil(cols / 128)] of x, or of
+        silu(gate) * x.  out: (codes, scales) to write into."""
+        if out is None:
+            rows, cols = x.shape
+            q = torch.empty((rows, _up(cols, 16)), dtype=torch.float8_e4m3fn, device=x.device)
+            if q.shape[1] != cols:
+                q = q[:, :cols]
+            out = q, torch.empty((rows, (cols + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP),
+                                 dtype=torch.float32, device=x.device)
+        self._ready(x, gate, *out)
+        lmop_quantize(self.ctx, x, out[0], out[1], gate)
+        return out
+
+    def matmul(self, a, a_scale, b, b_scale, dtype=torch.float16, add=None, out=None):
+        """a b^T (+ add) of E4M3 codes a [m, k], b [n, k] with block scales."""
+        if out is None:
+            out = torch.empty((a.shape[0], b.shape[0]), dtype=dtype, device=a.device)
+        self._ready(a, a_scale, b, b_scale, add, out)
+        lmop_matmul(self.ctx, a, a_scale, b, b_scale, out, add)
+        return out
+
+    def qk_norm_rope(self, q=None, k=None, v=None, *, pos, q_gain=None, k_gain=None, slot=None,
+                     q_out=None, k_out=None, v_out=None, v_columns=False):
+        """Normalises (where a gain is given) and rotates queries and keys, and writes
+        keys and values by slot into k_out, v_out.  Returns the queries (q_out,
+        or a new tensor; None without q)."""
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if (k is None) != (k_out is None) or (v is None) != (v_out is None):
+            raise ValueError("k needs k_out, v needs v_out")
+        self._ready(q, k, v, pos, q_gain, k_gain, slot, q_out, k_out, v_out)
+        lmop_qk_norm_rope(self.ctx, self.heads, pos.shape[0], q, k, v, pos, q_gain, k_gain, slot,
+                          q_out, k_out, v_out, v_columns)
+        return q_out
