@@ -46,3 +46,14 @@ template <typename T>
 LMOP_DEVICE T shfl_xor(T v, int mask) {
   return __shfl_xor(v, mask, 64);
 }
+
+// The value of the lane that the DPP control CTRL names (every lane active).
+// Within 8 lanes 0xB1, 0x4E and 0x141 in turn reduce over lanes 1, 2 and 4 apart.
+template <int CTRL>
+LMOP_DEVICE uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+template <int CTRL>
+LMOP_DEVICE float dpp(float x) {
+  return __uint_as_float(dpp<CTRL>(__float_as_uint(x)));
+}

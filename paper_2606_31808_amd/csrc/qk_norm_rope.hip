@@ -1,5 +1,11 @@
 // RMSNorm of every query and key head, rotate-half RoPE and the write of keys
 // and values into a cache, in one pass over a batch of tokens.
+//
+// Bound by memory: each element is read and written once.  A head is held by
+// hd / 16 lanes, lane j with dimensions 8j .. 8j+7 and the same of the upper
+// half, so that both members of every rotation pair are in one lane and the
+// sum of squares takes two or three exchanges between lanes, without LDS.  A
+// wave takes 64 / (hd / 16) heads of a token at a time.
 #include "common.h"
 #include "kernels.h"
 
@@ -7,72 +13,222 @@ namespace lmop {
 
 namespace {
 
-// One wave per (token, head): the pair (i, i + hd/2) in lane i.  Heads are
-// numbered queries, keys, values.
+constexpr int kWaves = 4;       // of a workgroup
+constexpr int kValueTokens = 64;  // of a workgroup that transposes values
+constexpr int kValueDims = 64;
+
 template <typename T>
-__global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs a) {
+using Run = T __attribute__((ext_vector_type(8)));
+
+template <typename T, bool VEC>
+LMOP_DEVICE Run<T> load_run(const T* p) {
+  if constexpr (VEC) {
+    return *(const Run<T>*)p;
+  } else {
+    Run<T> v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p[i];
+    return v;
+  }
+}
+template <typename T, bool VEC>
+LMOP_DEVICE void store_run(T* p, Run<T> v) {
+  if constexpr (VEC) {
+    *(Run<T>*)p = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = v[i];
+  }
+}
+
+// One workgroup: kValueTokens tokens x kValueDims dimensions of one value
+// head, transposed through LDS.  Tokens in consecutive slots (a prompt's) are
+// written 16 bytes of a dimension's row at a time where the slots reach a
+// multiple of 8; other tokens one value each, the lanes along the slots.
+template <typename T, int HD>
+LMOP_DEVICE void value_columns(const QkArgs& a, int block, bool vec_in, bool vec_out,
+                               uint16_t (*tile)[kValueDims + 2]) {
   const lmop_qk_norm_rope_args& p = a.t;
-  const int lane = threadIdx.x & 63, half = a.hd / 2;
-  const int heads = a.nq + 2 * a.nkv;
-  const size_t task = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (task >= (size_t)p.n_tokens * heads) return;
-  const size_t t = task / heads;
-  int h = (int)(task % heads);
-  const int sec = h < a.nq ? 0 : h < a.nq + a.nkv ? 1 : 2;
-  h -= sec == 0 ? 0 : sec == 1 ? a.nq : a.nq + a.nkv;
-  const T* in = sec == 0 ? (const T*)p.q : sec == 1 ? (const T*)p.k : (const T*)p.v;
-  if (in == nullptr) return;
-  in += t * (sec == 0 ? p.ldq : sec == 1 ? p.ldk : p.ldv) + h * a.hd;
-  const int slot = sec == 0 ? 0 : p.slot ? p.slot[t] : (int)t;
-  if (sec > 0 && (slot < 0 || slot >= p.n_slots)) return;
-  const bool on = lane < half;
-  const T r1 = on ? in[lane] : (T)0.f, r2 = on ? in[lane + half] : (T)0.f;
-  if (sec == 2) {
-    if (!on) return;
-    T* o = (T*)p.v_out;
-    if (p.v_layout == LMOP_V_ROWS) {
-      o += (size_t)slot * p.ldvo + h * a.hd;
-      o[lane] = r1;
-      o[lane + half] = r2;
-    } else {
-      o += (size_t)(h * a.hd + lane) * p.ldvo + slot;
-      o[0] = r1;
-      o[(size_t)half * p.ldvo] = r2;
+  constexpr int DT = HD / kValueDims;
+  const int per_tile = a.nkv * DT;
+  const int t0 = block / per_tile * kValueTokens, d0 = block % per_tile * kValueDims;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int n = p.n_tokens - t0 < kValueTokens ? p.n_tokens - t0 : kValueTokens;
+  const T* v = (const T*)p.v + d0;
+#pragma unroll
+  for (int i = 0; i < kValueTokens * kValueDims / 8 / (64 * kWaves); ++i) {
+    const int t = (tid >> 3) + i * 8 * kWaves, d = (tid & 7) * 8;
+    if (t < n) {
+      const T* src = v + (size_t)(t0 + t) * p.ldv + d;
+      const Run<T> r = vec_in ? load_run<T, true>(src) : load_run<T, false>(src);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const T x = r[j];  // of the vector's element itself the cast takes element 0
+        tile[t][d + j] = __builtin_bit_cast(uint16_t, x);
+      }
     }
+  }
+  const int tl = lane < n ? t0 + lane : t0 + n - 1;
+  const int slot = p.slot ? p.slot[tl] : tl;
+  const int s0 = __shfl(slot, 0, 64);
+  const bool here = slot >= 0 && slot < p.n_slots;
+  const bool run = __all(here && (lane >= n || slot == s0 + lane));
+  __syncthreads();
+  uint16_t* out = (uint16_t*)p.v_out + (size_t)d0 * p.ldvo;
+  if (run && vec_out) {
+    // chunk j: slots first + 8j .. +7
+    const int first = s0 & ~7, chunks = (s0 - first + n + 7) / 8;
+    for (int i = tid; i < chunks * kValueDims; i += 64 * kWaves) {
+      const int d = i / chunks, j = i - d * chunks;
+      const int t = first + 8 * j - s0;
+      uint16_t* o = out + (size_t)d * p.ldvo + first + 8 * j;
+      if (t >= 0 && t + 8 <= n) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          w[q] = tile[t + 2 * q][d] | (uint32_t)tile[t + 2 * q + 1][d] << 16;
+        *(uint4*)o = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (t + q >= 0 && t + q < n) o[q] = tile[t + q][d];
+      }
+    }
+  } else if (lane < n && here) {
+    for (int d = tid >> 6; d < kValueDims; d += kWaves) out[(size_t)d * p.ldvo + slot] = tile[lane][d];
+  }
+}
+
+// Blocks below value_blocks transpose values; a wave of the others takes
+// `chunks` head chunks of a token, from chunk task % splits * chunks on, and
+// goes on with every `waves`-th (token, chunk range).  Heads are numbered
+// queries, keys, and (LMOP_V_ROWS) values.
+template <typename T, int HD, bool VEC>
+__global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const QkArgs a, int value_blocks,
+                                                                   bool vec_v, int chunks,
+                                                                   int splits) {
+  constexpr int LPH = HD / 16;   // lanes of a head
+  constexpr int HPW = 64 / LPH;  // heads of a chunk
+  const lmop_qk_norm_rope_args& p = a.t;
+  if ((int)blockIdx.x < value_blocks) {
+    __shared__ uint16_t tile[kValueTokens][kValueDims + 2];
+    value_columns<T, HD>(a, blockIdx.x, VEC, vec_v, tile);
     return;
   }
-  float x1 = (float)r1, x2 = (float)r2;
-  const float* gain = sec == 0 ? p.q_gain : p.k_gain;
-  if (gain) {
-    float ss = x1 * x1 + x2 * x2;
+  const int lane = threadIdx.x & 63;
+  const int wave =
+      __builtin_amdgcn_readfirstlane((blockIdx.x - value_blocks) * kWaves + (threadIdx.x >> 6));
+  const int waves = (int)(gridDim.x - value_blocks) * kWaves;
+  const int d = lane % LPH * 8;
+  const int heads = a.nq + a.nkv + (p.v && p.v_layout == LMOP_V_ROWS ? a.nkv : 0);
+  const long tasks = (long)p.n_tokens * splits;
+  for (long task = wave; task < tasks; task += waves) {
+    const int t = (int)(task / splits), c0 = (int)(task % splits) * chunks;
+    const int pos = p.pos ? p.pos[t] : 0;
+    const int slot = p.slot ? p.slot[t] : t;
+    const bool here = slot >= 0 && slot < p.n_slots;
+    // the angles of this lane's dimensions, for all the heads
+    float cs[8], sn[8];
+    if (pos >= 0 && pos < a.max_seq) {
+      const float4* r = (const float4*)(a.rope + (size_t)pos * (HD / 2) + d);
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) ss += shfl_xor(ss, o);
-    const float r = 1.0f / sqrtf(ss / (float)a.hd + a.eps);
-    if (on) {
-      x1 = x1 * r * gain[lane];
-      x2 = x2 * r * gain[lane + half];
+      for (int i = 0; i < 4; ++i) {
+        const float4 w = r[i];
+        cs[2 * i] = w.x, sn[2 * i] = w.y, cs[2 * i + 1] = w.z, sn[2 * i + 1] = w.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) cs[i] = sn[i] = NAN;
+    }
+    for (int c = c0; c < c0 + chunks; ++c) {
+      const int h = c * HPW + lane / LPH;
+      const int sec = h < a.nq ? 0 : h < a.nq + a.nkv ? 1 : 2;
+      const int hs = h - (sec == 0 ? 0 : sec == 1 ? a.nq : a.nq + a.nkv);
+      const T* in = sec == 0 ? (const T*)p.q + t * p.ldq
+                    : sec == 1 ? (const T*)p.k + t * p.ldk
+                               : (const T*)p.v + t * p.ldv;
+      T* out = sec == 0 ? (T*)p.q_out + t * p.ldqo
+               : sec == 1 ? (T*)p.k_out + slot * p.ldko
+                          : (T*)p.v_out + slot * p.ldvo;
+      const bool on = h < heads && (sec == 0 ? p.q != nullptr
+                                             : here && (sec == 2 || p.k != nullptr));
+      in += hs * HD + d;
+      out += hs * HD + d;
+      Run<T> r1 = {}, r2 = {};
+      if (on) {
+        r1 = load_run<T, VEC>(in);
+        r2 = load_run<T, VEC>(in + HD / 2);
+      }
+      if (sec < 2) {
+        float x1[8], x2[8], ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x1[i] = (float)r1[i], x2[i] = (float)r2[i];
+          ss = __builtin_fmaf(x1[i], x1[i], ss);
+          ss = __builtin_fmaf(x2[i], x2[i], ss);
+        }
+        ss += dpp<0xB1>(ss);
+        ss += dpp<0x4E>(ss);
+        if constexpr (LPH == 8) ss += dpp<0x141>(ss);
+        const float* gain = sec == 0 ? p.q_gain : p.k_gain;
+        if (gain) {
+          const float rn = __builtin_amdgcn_rsqf(ss * (1.0f / HD) + a.eps);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x1[i] = x1[i] * rn * gain[d + i];
+            x2[i] = x2[i] * rn * gain[HD / 2 + d + i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          r1[i] = (T)(x1[i] * cs[i] - x2[i] * sn[i]);
+          r2[i] = (T)(x1[i] * sn[i] + x2[i] * cs[i]);
+        }
+      }
+      if (on) {
+        store_run<T, VEC>(out, r1);
+        store_run<T, VEC>(out + HD / 2, r2);
+      }
     }
   }
-  if (!on) return;
-  const int pos = p.pos[t];
-  float2 cs = make_float2(NAN, NAN);
-  if (pos >= 0 && pos < a.max_seq) cs = a.rope[(size_t)pos * half + lane];
-  T* o = sec == 0 ? (T*)p.q_out + t * p.ldqo : (T*)p.k_out + (size_t)slot * p.ldko;
-  o += h * a.hd;
-  o[lane] = (T)(x1 * cs.x - x2 * cs.y);
-  o[lane + half] = (T)(x1 * cs.y + x2 * cs.x);
+}
+
+// whether rows start on 16-byte boundaries (absent tensors count as aligned)
+bool aligned16(const void* p, int64_t ld) { return !p || ((uintptr_t)p % 16 == 0 && ld % 8 == 0); }
+
+template <typename T, int HD>
+hipError_t launch(hipStream_t s, const QkArgs& a) {
+  const lmop_qk_norm_rope_args& p = a.t;
+  const bool columns = p.v && p.v_layout == LMOP_V_COLUMNS;
+  const bool vec_v = columns && aligned16(p.v_out, p.ldvo);
+  const bool vec = aligned16(p.q, p.ldq) && aligned16(p.k, p.ldk) && aligned16(p.v, p.ldv) &&
+                   aligned16(p.q ? p.q_out : nullptr, p.ldqo) &&
+                   aligned16(p.k ? p.k_out : nullptr, p.ldko) &&
+                   aligned16(p.v && !columns ? p.v_out : nullptr, p.ldvo);
+  const long value_blocks = columns ? (long)((p.n_tokens + kValueTokens - 1) / kValueTokens) *
+                                          a.nkv * (HD / kValueDims)
+                                    : 0;
+  const int heads = a.nq + a.nkv + (p.v && !columns ? a.nkv : 0);
+  const int all = (heads + 64 / (HD / 16) - 1) / (64 / (HD / 16));
+  // few tokens: a wave per chunk of heads, to spread them over the chip;
+  // many: a wave keeps a token's angles for all its heads
+  const int chunks = (long)p.n_tokens * all <= 4096 ? 1 : all, splits = all / chunks;
+  const long want = ((long)p.n_tokens * splits + kWaves - 1) / kWaves;
+  const long blocks = (!p.q && !p.k && (columns || !p.v)) ? 0 : want < 65536 ? want : 65536;
+  if (value_blocks + blocks > 0x7fffffff) return hipErrorInvalidValue;
+  auto* k = vec ? qk_norm_rope_kernel<T, HD, true> : qk_norm_rope_kernel<T, HD, false>;
+  hipLaunchKernelGGL(k, dim3((unsigned)(value_blocks + blocks)), dim3(64 * kWaves), 0, s, a,
+                     (int)value_blocks, vec_v, chunks, splits);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_qk_norm_rope(hipStream_t s, const QkArgs& a) {
-  const size_t blocks = ((size_t)a.t.n_tokens * (a.nq + 2 * a.nkv) + 3) / 4;
-  if (blocks > 0x7fffffffu) return hipErrorInvalidValue;
-  if (a.t.dtype == LMOP_F16)
-    hipLaunchKernelGGL(qk_norm_rope_kernel<f16>, dim3((unsigned)blocks), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(qk_norm_rope_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, s, a);
-  return hipGetLastError();
+  const bool wide = a.hd == 128;
+  if (!wide && a.hd != 64) return hipErrorInvalidValue;
+  if (a.t.dtype == LMOP_F16) return wide ? launch<f16, 128>(s, a) : launch<f16, 64>(s, a);
+  return wide ? launch<bf16, 128>(s, a) : launch<bf16, 64>(s, a);
 }
 
 }  // namespace lmop

@@ -1,7 +1,15 @@
 // E4M3 quantisation with one scale per row and group of 128 features, of x or
 // of silu(gate) * x (the operand of the block-scaled FP8 products).
+//
+// Bound by memory: every input is read once, held in registers between the
+// maximum and the codes, and every code written once.  Eight lanes hold a
+// group, two runs of 8 features each (64 features apart, so that the lanes'
+// 16-byte loads lie side by side); the maximum takes three exchanges between
+// lanes, without LDS.
 #include "common.h"
 #include "kernels.h"
+
+#include <type_traits>
 
 namespace lmop {
 
@@ -10,58 +18,106 @@ namespace {
 constexpr float kE4m3Max = 448.0f;
 constexpr float kAmaxMin = 0x1p-40f;
 
-// One half-wave of 32 lanes per group, four features a lane.
 template <typename T>
-__global__ __launch_bounds__(256) void quantize_kernel(const lmop_quantize_args p, int groups) {
-  const size_t task = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (task >= (size_t)p.rows * groups) return;
-  const size_t row = task / groups;
-  const int g = (int)(task % groups), lane = threadIdx.x & 31;
-  const T* x = (const T*)p.x + row * p.ldx;
-  const T* gt = p.gate ? (const T*)p.gate + row * p.ldg : nullptr;
-  float y[4], amax = kAmaxMin;
-  bool bad = false;
+using Run = T __attribute__((ext_vector_type(8)));
+
+// features f .. f+7 of a row, zero from cols on
+template <typename T, bool VEC>
+LMOP_DEVICE void load_run(const T* row, int f, int cols, float (&y)[8]) {
+  if (VEC && f + 8 <= cols) {
+    const Run<T> v = *(const Run<T>*)(row + f);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int f = g * LMOP_FP8_GROUP + lane * 4 + i;
-    y[i] = f < p.cols ? (float)x[f] : 0.f;
-    if (gt && f < p.cols) {
-      const float z = (float)gt[f];
-      y[i] *= z / (1.0f + expf(-z));
+    for (int i = 0; i < 8; ++i) y[i] = (float)v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = f + i < cols ? (float)row[f + i] : 0.f;
+  }
+}
+
+LMOP_DEVICE uint32_t max_u32(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+template <typename T, bool VEC, bool GATE>
+__global__ __launch_bounds__(256) void quantize_kernel(const lmop_quantize_args p, uint32_t groups,
+                                                       uint32_t tasks) {
+  const uint32_t task = blockIdx.x * 32u + (threadIdx.x >> 3);
+  // lanes past the last task repeat it up to the stores: every lane takes part
+  // in the exchanges
+  const uint32_t at = task < tasks ? task : tasks - 1;
+  const uint32_t row = at / groups, g = at - row * groups;
+  const int lane = threadIdx.x & 7, f0 = (int)g * LMOP_FP8_GROUP + lane * 8;
+  float y[2][8];
+  const T* x = (const T*)p.x + (size_t)row * p.ldx;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) load_run<T, VEC>(x, f0 + 64 * h, p.cols, y[h]);
+  if constexpr (GATE) {
+    const T* gt = (const T*)p.gate + (size_t)row * p.ldg;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float z[8];
+      load_run<T, VEC>(gt, f0 + 64 * h, p.cols, z);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        y[h][i] *= z[i] * __builtin_amdgcn_rcpf(1.0f + __expf(-z[i]));
     }
-    amax = fmaxf(amax, fabsf(y[i]));
-    bad |= !(fabsf(y[i]) < INFINITY);
   }
+  // the magnitudes' bits order like the magnitudes, with infinity and then
+  // NaN above every finite one
+  uint32_t top = __float_as_uint(kAmaxMin);
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) {
-    amax = fmaxf(amax, shfl_xor(amax, o));
-    bad |= shfl_xor((int)bad, o) != 0;
-  }
-  if (bad) amax = NAN;
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max_u32(top, __float_as_uint(y[h][i]) & 0x7FFFFFFFu);
+  top = max_u32(top, dpp<0xB1>(top));
+  top = max_u32(top, dpp<0x4E>(top));
+  top = max_u32(top, dpp<0x141>(top));
+  const float amax = top < 0x7F800000u ? __uint_as_float(top) : NAN;
   const float inv = kE4m3Max / amax;
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inv, y[1] * inv, 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, w, true);
-  const int f = g * LMOP_FP8_GROUP + lane * 4;
-  uint32_t code = (uint32_t)w;
-  if (f + 4 > p.cols) code = f < p.cols ? code & ((1u << (8 * (p.cols - f))) - 1) : 0u;
-  if (f < (p.cols + 15) / 16 * 16) *(uint32_t*)(p.q + row * p.ldq + f) = code;
-  if (lane == 0) p.scale[row * p.lds + g] = amax / kE4m3Max;
+  if (task >= tasks) return;
+  uint8_t* q = p.q + (size_t)row * p.ldq;
+  const int up = (p.cols + 15) / 16 * 16;  // codes of features from cols on are zero
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int f = f0 + 64 * h;
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float* v = &y[h][4 * i];
+      int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+      c = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, c, true);
+      w[i] = (uint32_t)c;
+      const int n = p.cols - f - 4 * i;  // a NaN group's codes end there too
+      if (n < 4) w[i] = n > 0 ? w[i] & ((1u << (8 * n)) - 1) : 0u;
+    }
+    if (f < up) *(uint2*)(q + f) = make_uint2(w[0], w[1]);
+  }
+  if (lane == 0) p.scale[(size_t)row * p.lds + g] = amax / kE4m3Max;
+}
+
+// whether rows start on 16-byte boundaries
+bool aligned16(const void* p, int64_t ld, size_t esize) {
+  return (uintptr_t)p % 16 == 0 && (size_t)ld * esize % 16 == 0;
+}
+
+template <typename T>
+hipError_t launch(hipStream_t s, const lmop_quantize_args& a) {
+  const size_t groups = ((size_t)a.cols + LMOP_FP8_GROUP - 1) / LMOP_FP8_GROUP;
+  const size_t tasks = a.rows * groups;
+  if (tasks > 0xFFFFFFE0u) return hipErrorInvalidValue;
+  const bool vec =
+      aligned16(a.x, a.ldx, sizeof(T)) && (!a.gate || aligned16(a.gate, a.ldg, sizeof(T)));
+  auto* k = vec ? (a.gate ? quantize_kernel<T, true, true> : quantize_kernel<T, true, false>)
+                : (a.gate ? quantize_kernel<T, false, true> : quantize_kernel<T, false, false>);
+  hipLaunchKernelGGL(k, dim3((unsigned)((tasks + 31) / 32)), dim3(256), 0, s, a, (uint32_t)groups,
+                     (uint32_t)tasks);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_quantize(hipStream_t s, const lmop_quantize_args& a) {
-  const int groups = (a.cols + LMOP_FP8_GROUP - 1) / LMOP_FP8_GROUP;
-  const size_t blocks = ((size_t)a.rows * groups + 7) / 8;
-  if (blocks > 0x7fffffffu) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks);
-  if (a.dtype == LMOP_F16)
-    hipLaunchKernelGGL(quantize_kernel<f16>, grid, dim3(256), 0, s, a, groups);
-  else if (a.dtype == LMOP_BF16)
-    hipLaunchKernelGGL(quantize_kernel<bf16>, grid, dim3(256), 0, s, a, groups);
-  else
-    hipLaunchKernelGGL(quantize_kernel<float>, grid, dim3(256), 0, s, a, groups);
-  return hipGetLastError();
+  if (a.dtype == LMOP_F16) return launch<f16>(s, a);
+  if (a.dtype == LMOP_BF16) return launch<bf16>(s, a);
+  return launch<float>(s, a);
 }
 
 }  // namespace lmop
