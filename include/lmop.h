@@ -377,7 +377,8 @@ lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t 
  * are in elements between rows; the elements of a row are adjacent; what
  * lies between rows is not written.  An output may not overlap an input
  * unless said.  A size of zero is a no-op.  Results do not depend on which
- * other rows are in the call, bit for bit. */
+ * other rows are in the call, bit for bit.  A call is limited to 2^30 tiles of
+ * 16 x 16 results, groups, or heads. */
 typedef enum { LMOP_F16 = 0, LMOP_BF16 = 1, LMOP_F32 = 2 } lmop_dtype;
 
 /* Features that share one scale. */
@@ -407,7 +408,10 @@ lmop_status lmop_quantize(lmop_ctx* ctx, const lmop_quantize_args* args);
  *   C[i][j] = add[i][j] + sum over groups g of a_scale[i][g] * b_scale[j / 128][g]
  *             * (sum over the features f of g of a[i][f] * b[j][f])
  * The sums are held in fp32 and rounded to dtype once; the groups are added
- * in order of g.  NaN codes give NaN. */
+ * in order of g.  For fp16 and bf16 results the inner sum runs on the 8-bit
+ * matrix instruction, which cuts a product's bits below 2^-13 of the largest
+ * of its 8 neighbours (2e-5 of a result's usual size, less than a tenth of its
+ * rounding); for fp32 results every product is whole.  NaN codes give NaN. */
 typedef struct {
   const uint8_t* a;     /* [m][k] codes (tokens), 16-byte aligned */
   const float* a_scale; /* [m][ceil(k / 128)] */
@@ -418,7 +422,7 @@ typedef struct {
   void* c;              /* [m][n] of dtype */
   int64_t lda, ldb;     /* >= k, multiples of 16, at most 2^23; the bytes of a row from k up to
                            the next multiple of 16 are read and have no effect */
-  int64_t ldas, ldbs;   /* >= ceil(k / 128) */
+  int64_t ldas, ldbs;   /* >= ceil(k / 128); ldas at most 2^21 */
   int64_t ldadd, ldc;   /* >= n */
   int32_t m, n, k;      /* k = 0: C = add, or zero */
   int32_t dtype;        /* LMOP_F16, LMOP_BF16 or LMOP_F32 */

@@ -19,6 +19,7 @@
 //   fp32: the codes converted to fp16, exactly, and four MFMAs 16x16x32,
 //     which keep every product whole and add in fp32.
 #include "common.h"
+#include "fp8_tiles.h"
 #include "kernels.h"
 #include "lds_dma.h"
 
@@ -42,7 +43,7 @@ LMOP_DEVICE uint4 keep_bytes(uint4 v, int valid) {
 }
 
 // A lane's 32 codes of one row and group: lane 16g + c holds features
-// 32g .. 32g+31 of row c.
+// 16g .. 16g+15 and 64+16g .. 64+16g+15 of row c.
 struct Codes {
   uint4 w[2];
 };
@@ -50,9 +51,10 @@ struct Halves {
   f16x8 h[4];
 };
 
+// `valid` features left from the lane's first one on
 LMOP_DEVICE void keep_valid(Codes& c, int valid) {
   c.w[0] = keep_bytes(c.w[0], valid);
-  c.w[1] = keep_bytes(c.w[1], valid - 16);
+  c.w[1] = keep_bytes(c.w[1], valid - 64);
 }
 
 // the operand of `dot`: the codes themselves, or their fp16 values
@@ -126,15 +128,20 @@ LMOP_DEVICE void store4(const lmop_matmul_args& p, bool vec, int m, int n, f32x4
 template <int MT, int NT, int WM, int WN, int OCC>
 struct Tile {
   static constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, NW = WM * WN;
-  static constexpr int STAGE = (BM + BN) * 128 + BM * 4;
-  static constexpr int NS_FIT = 160 * 1024 / OCC / STAGE;
-  static constexpr int NS = NS_FIT < 4 ? NS_FIT : 4;
+  static constexpr int STAGE = (BM + BN) * 128;
+  // the tokens' scales of the groups 4q .. 4q+3, for SBUF q in turn
+  static constexpr int SCALES = BM * 16;
+  static constexpr int NS_FIT = (160 * 1024 / OCC - 3 * SCALES) / STAGE;
+  static constexpr int NS = NS_FIT < 8 ? NS_FIT : 8;
+  static constexpr int SBUF = (NS + 2) / 4 + 1;  // from the stage in use to the last in flight
   static_assert(NS >= 2, "a stage in use and one in flight");
-  static_assert(BM % 64 == 0 && (BM + BN) % (8 * NW) == 0, "whole loads");
+  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole loads");
   static_assert(GROUP % (16 * NT) == 0, "a wave's columns lie in one block of B");
-  static constexpr int CODE_LOADS = (BM + BN) / 8 / NW;  // of a wave and stage
-  static constexpr int LOADS = CODE_LOADS + 1;           // and the scales
-  static constexpr int LDS = NS * STAGE;
+  // a wave's loads per stage, 8 rows each
+  static constexpr int A_LOADS = BM / 8 / NW, B_LOADS = BN / 8 / NW;
+  static constexpr int LOADS = A_LOADS + B_LOADS;
+  static constexpr int LDS = NS * STAGE + SBUF * SCALES;
+  static_assert((NS - 2) * LOADS < 63, "the loads waited for fit the counter");
 };
 
 constexpr int GM = 4;  // token tiles per L2 group
@@ -160,37 +167,54 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
   const int m0 = (grp * GM + within % gsz) * BM, n0 = within / gsz * BN;
 
   const int kr = (p.k + 15) / 16 * 16, kb_n = (p.k + GROUP - 1) / GROUP;
-  const bool ragged = p.k % GROUP != 0;
 
-  // Load i of a wave: 8 rows of the stage (tokens first).  Rows past the
-  // matrix repeat its last one; chunks past a row's end repeat its last one
-  // and are cleared after they are read.
+  // A wave's loads take rows 8 * (wave + NW * n) .. +7 of the tile's tokens,
+  // then of its columns.  Rows past the matrix repeat its last one; chunks past
+  // a row's end repeat its last one and are cleared after they are read.
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
   const uint8_t* abase = p.a + (size_t)m0 * p.lda;
   const uint8_t* bbase = p.b + (size_t)n0 * p.ldb;
-  uint32_t rowoff[C::CODE_LOADS];
-  const int chunk = ((lane & 7) ^ (lane >> 3)) * 16;
+  const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb;
+  const uint32_t row0 = (uint32_t)(wave * 8 + (lane >> 3));
+  const uint32_t a_first = row0 * lda, b_first = row0 * ldb;
+  const uint32_t a_last = (uint32_t)(p.m - 1 - m0 < BM ? p.m - 1 - m0 : BM) * lda;
+  const uint32_t b_last = (uint32_t)(p.n - 1 - n0 < BN ? p.n - 1 - n0 : BN) * ldb;
+  const uint32_t chunk = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16u;
+  // A wave loads the scales of SROWS tokens, 16 at a time: lane 4r + q the
+  // scale of token r and group 4 * (kb / 4) + q ([token][4] in LDS).
+  constexpr int SROWS = BM / NW, SLOADS = (SROWS + 15) / 16;
+  const uint32_t scl0 = lds0 + NS * C::STAGE + (uint32_t)(wave * SROWS) * 16u;
+  const float* sbase = p.a_scale + (size_t)m0 * p.ldas;
+  uint32_t srow[SLOADS];
 #pragma unroll
-  for (int i = 0; i < C::CODE_LOADS; ++i) {
-    const int r = (wave + NW * i) * 8 + (lane >> 3);
-    const int ra = m0 + r < p.m ? r : p.m - 1 - m0;
-    const int rb = n0 + r - BM < p.n ? r - BM : p.n - 1 - n0;
-    rowoff[i] = (wave + NW * i) * 8 < BM ? (uint32_t)ra * (uint32_t)p.lda
-                                         : (uint32_t)rb * (uint32_t)p.ldb;
+  for (int i = 0; i < SLOADS; ++i) {
+    const int r = wave * SROWS + 16 * i + (lane >> 2);
+    srow[i] = (uint32_t)(r < p.m - 1 - m0 ? r : p.m - 1 - m0) * (uint32_t)p.ldas;
   }
-  const int srow = (wave * 64) % BM + lane;
-  const float* sa = p.a_scale + (size_t)(m0 + srow < p.m ? m0 + srow : p.m - 1) * p.ldas;
-  auto issue = [&](int kb) {
-    const uint32_t st = lds0 + (uint32_t)(kb % NS * C::STAGE);
-    const bool last = ragged && kb == kb_n - 1;
-    const int o = last && kb * GROUP + chunk > kr - 16 ? kr - 16 - kb * GROUP : chunk;
+  auto issue_scales = [&](int kb) {
+    const int q = kb + (lane & 3) < kb_n ? kb + (lane & 3) : kb_n - 1;
+    const uint32_t to = scl0 + (uint32_t)((kb >> 2) % C::SBUF * C::SCALES);
+    const uint64_t on = SROWS >= 16 ? ~0ull : (1ull << (4 * (SROWS % 16))) - 1;
 #pragma unroll
-    for (int i = 0; i < C::CODE_LOADS; ++i) {
-      const int q = wave + NW * i;
-      g2l16_m0((q * 8 < BM ? abase : bbase) + (size_t)kb * GROUP, rowoff[i] + (uint32_t)o,
-               st + (uint32_t)q * 1024u);
+    for (int i = 0; i < SLOADS; ++i)
+      g2l4_m0_mask(sbase, (srow[i] + (uint32_t)q) * 4u, to + 256u * i, kb % 4 == 0 ? on : 0ull);
+  };
+  // Instruction n of the loads of stage kb, into its slot; past the last stage
+  // the loads repeat that one, so that every stage is as many loads.
+  auto issue_one = [&](int n, int kb) {
+    const uint32_t st = lds0 + (uint32_t)(kb % NS * C::STAGE);
+    kb = kb < kb_n ? kb : kb_n - 1;
+    const uint32_t end = (uint32_t)(kr - 16 - kb * GROUP), at = chunk < end ? chunk : end;
+    if (n < C::A_LOADS) {
+      const uint32_t r = a_first + (uint32_t)(NW * 8 * n) * lda;
+      g2l16_m0(abase + (size_t)kb * GROUP, (r < a_last ? r : a_last) + at,
+               st + (uint32_t)(wave + NW * n) * 1024u);
+    } else {
+      const int i = n - C::A_LOADS;
+      const uint32_t r = b_first + (uint32_t)(NW * 8 * i) * ldb;
+      g2l16_m0(bbase + (size_t)kb * GROUP, (r < b_last ? r : b_last) + at,
+               st + (uint32_t)(BM * 128 + (wave + NW * i) * 1024));
     }
-    g2l4(sa + kb, st + (uint32_t)((BM + BN) * 128 + (wave * 64) % BM * 4));
   };
 
   f32x4 acc[MT][NT];
@@ -201,53 +225,110 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
   const int nblk = n0 + wn * NT * 16 < p.n ? (n0 + wn * NT * 16) / GROUP : (p.n - 1) / GROUP;
   const float* sb = p.b_scale + (size_t)nblk * p.ldbs;
 
-  auto step = [&](int kb, auto tail) {
-    const char* st = smem + kb % NS * C::STAGE;
-    const int valid = p.k - kb * GROUP - 32 * g;
-    auto frag = [&](int row) {
-      Codes x;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        x.w[i] = *(const uint4*)(st + row * 128 + (((2 * g + i) ^ (c & 7)) * 16));
-      if constexpr (decltype(tail)::value) keep_valid(x, valid);
-      return operand<F32>(x);
-    };
-    const float sbk = sb[kb];
-    Operand<F32> b[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) b[j] = frag(BM + (wn * NT + j) * 16 + c);
-    f32x4 d[2][NT];
-    float s[2];
-#pragma unroll
-    for (int i = 0; i <= MT; ++i) {
-      // the tile before is added while this one is multiplied
-      if (i < MT) {
-        const int row = (wm * MT + i) * 16 + c;
-        const Operand<F32> a = frag(row);
-        s[i & 1] = *(const float*)(st + (BM + BN) * 128 + row * 4) * sbk;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) d[i & 1][j] = dot(b[j], a);
-      }
-      if (i > 0)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) add_scaled(acc[i - 1][j], d[(i - 1) & 1][j], s[(i - 1) & 1]);
-    }
+  // this lane's chunks of its rows within a stage: 16 bytes at g and g + 4, so
+  // that no two of the 16 lanes that LDS serves at once share a bank (chunks 2g
+  // and 2g + 1 conflict in pairs)
+  const int off0 = (g ^ (c & 7)) * 16, off1 = ((g + 4) ^ (c & 7)) * 16;
+  const int arow = (wm * MT * 16 + c) * 128, brow = (BM + wn * NT * 16 + c) * 128;
+  auto codes = [&](int kb, int row, int i) {
+    const char* st = smem + kb % NS * C::STAGE + row;
+    Codes x;
+    x.w[0] = *(const uint4*)(st + off0 + i * 2048);
+    x.w[1] = *(const uint4*)(st + off1 + i * 2048);
+    return x;
+  };
+  auto frag = [&](int kb, int row, int i) { return operand<F32>(codes(kb, row, i)); };
+  auto scale = [&](int kb, int i) {
+    return *(const float*)(smem + NS * C::STAGE + (kb >> 2) % C::SBUF * C::SCALES + kb % 4 * 4 +
+                           (wm * MT * 16 + c) * 16 + i * 256);
   };
 
-  for (int kb = 0; kb < NS - 1 && kb < kb_n; ++kb) issue(kb);
-  for (int kb = 0; kb < kb_n; ++kb) {
-    // stage kb has landed for every wave, and every wave is done with the
-    // stage before it, which the next loads refill
-    if (kb + NS - 2 < kb_n)
-      wait_vmcnt_lgkm0<(NS - 2) * C::LOADS>();
-    else
-      wait_vmcnt_lgkm0<0>();
+  // One whole group.  In phase i the tile row i is multiplied while row i - 1
+  // is added to the sums, row i + 1 is read, and a share of a later stage's
+  // loads is issued (waves that issue all of theirs at once hold each other up
+  // while the matrix cores run dry).  No branch: one would let the compiler
+  // move the additions behind it.
+  constexpr int PER = (C::LOADS + MT - 1) / MT < 2 ? 2 : (C::LOADS + MT - 1) / MT;
+  auto stage = [&](int kb, float sbk) {
+    // the stage has landed for every wave, and every wave is done with the one
+    // before it, which the loads below refill (the later stages' scales are not
+    // counted: a smaller count waits for more)
+    wait_vmcnt_lgkm0<(NS - 2) * C::LOADS>();
     barrier();
-    if (kb + NS - 1 < kb_n) issue(kb + NS - 1);
-    if (ragged && kb == kb_n - 1)
-      step(kb, std::true_type{});
-    else
-      step(kb, std::false_type{});
+    Operand<F32> b[NT], a[2];
+    f32x4 d[2][NT];
+    float s[2], sc = 0.f;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) b[j] = frag(kb, brow, j);
+    a[0] = frag(kb, arow, 0);
+    s[0] = scale(kb, 0);
+#pragma unroll
+    for (int i = 0; i <= MT; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i == 0) issue_scales(kb + NS - 1);
+#pragma unroll
+      for (int n = i * PER; n < (i + 1) * PER && n < C::LOADS; ++n) issue_one(n, kb + NS - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const float sc_before = sc;
+      if (i < MT) sc = s[i & 1] * sbk;
+      if (i + 1 < MT) {
+        a[(i + 1) & 1] = frag(kb, arow, i + 1);
+        s[(i + 1) & 1] = scale(kb, i + 1);
+      }
+      if (i < MT)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) d[i & 1][j] = dot(b[j], a[i & 1]);
+      if (i > 0)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) add_scaled(acc[i - 1][j], d[(i - 1) & 1][j], sc_before);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x008, F32 ? 4 : 1, 0);  // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);            // LDS read
+        __builtin_amdgcn_sched_group_barrier(0x002, F32 ? 8 : 5, 0);  // VALU
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+#pragma unroll
+  for (int kb = 0; kb < NS - 1; ++kb) {
+    issue_scales(kb);
+#pragma unroll
+    for (int n = 0; n < C::LOADS; ++n) issue_one(n, kb);
+  }
+  const int full = p.k / GROUP;
+  // 64 groups at a time: their scales of the wave's columns, one a lane
+  for (int k0 = 0; k0 < full; k0 += 64) {
+    float sb_64 = sb[k0 + lane < kb_n ? k0 + lane : kb_n - 1];
+    // waited for here: in the loop the wait would be for the stages in flight too
+    asm volatile("" : "+v"(sb_64));
+    const int end = full < k0 + 64 ? full : k0 + 64;
+    for (int kb = k0; kb < end; ++kb)
+      stage(kb, __uint_as_float(
+                    __builtin_amdgcn_readlane(__float_as_uint(sb_64), kb - k0)));
+  }
+  // the loads end before the workgroup does
+  wait_vmcnt_lgkm0<0>();
+  if (full < kb_n) {
+    // the last features, less than a group: their stage is the last one loaded
+    barrier();
+    const int valid = p.k - full * GROUP - 16 * g;
+    auto masked = [&](int row, int i) {
+      Codes x = codes(full, row, i);
+      keep_valid(x, valid);
+      return operand<F32>(x);
+    };
+    Operand<F32> b[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) b[j] = masked(brow, j);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const Operand<F32> a = masked(arow, i);
+      const float sc = scale(full, i) * sb[full];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) add_scaled(acc[i][j], dot(b[j], a), sc);
+    }
   }
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -258,36 +339,38 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
 
 // ---------------------------------------------------------------- few tokens
 // 16*MT tokens x 16 columns by 8 waves, each with its own groups: wave w
-// multiplies groups w, w + 8, ... straight from memory, U at a time, and
+// multiplies groups w, w + 8, ... straight from memory, U of them a round, and
 // leaves the products in LDS, where the threads (one or more outputs each)
 // add them in the order of the groups.  A weight of few rows is then spread
-// over the chip along K, with U * 2 KB of it in flight per wave.
+// over the chip along K.  The operands of two rounds are in flight or in
+// registers (4 * U * (1 + MT) KB a wave).
 template <typename T, int MT, int U>
-__global__ __launch_bounds__(512, 2) void matmul_few_kernel(const lmop_matmul_args p, bool vec) {
+__global__ __launch_bounds__(512, 2) void matmul_few_kernel(const lmop_matmul_args p) {
   constexpr bool F32 = std::is_same_v<T, float>;
   constexpr int NW = 8, CH = NW * U;       // groups of a round
   constexpr int OUT = 256 * MT;            // outputs of the workgroup
   constexpr int PER = (OUT + 511) / 512;   // of a thread
   __shared__ __attribute__((aligned(16))) float prod[2][CH][OUT];
-  __shared__ float scl[2][CH][16 * MT];
+  __shared__ float scl[2][CH][16 * MT + 1];
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tn = (p.n + 15) / 16;
   const int m0 = (int)(blockIdx.x / tn) * 16 * MT, n0 = (int)(blockIdx.x % tn) * 16;
   const int kr = (p.k + 15) / 16 * 16, kb_n = (p.k + GROUP - 1) / GROUP;
   const uint8_t* brow = p.b + (size_t)(n0 + c < p.n ? n0 + c : p.n - 1) * p.ldb;
-  const float* sb = p.b_scale + (size_t)(n0 / GROUP) * p.ldbs;
   const uint8_t* arow[MT];
-  const float* sarow[MT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = m0 + 16 * i + c < p.m ? m0 + 16 * i + c : p.m - 1;
-    arow[i] = p.a + (size_t)m * p.lda;
-    sarow[i] = p.a_scale + (size_t)m * p.ldas;
-  }
-  Codes b[U], a[U][MT];
-  float s[U][MT];
-  auto load = [&](int round) {
+  for (int i = 0; i < MT; ++i)
+    arow[i] = p.a + (size_t)(m0 + 16 * i + c < p.m ? m0 + 16 * i + c : p.m - 1) * p.lda;
+  // a round's scales: thread t brings group t % CH of token t / CH
+  const int st = (int)threadIdx.x / CH, sq = (int)threadIdx.x % CH;
+  static_assert(16 * MT * CH <= 512, "a thread brings one scale of a round");
+  const float* sa = p.a_scale + (size_t)(m0 + st < p.m ? m0 + st : p.m - 1) * p.ldas;
+  const float* sb = p.b_scale + (size_t)(n0 / GROUP) * p.ldbs;
+  Codes b[2][U], a[2][U][MT];
+  float sak[2], sbk[2];
+  auto load = [&](int round, auto set) {
+    constexpr int S = decltype(set)::value;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       // groups past the last repeat it; their products are not used
@@ -295,53 +378,67 @@ __global__ __launch_bounds__(512, 2) void matmul_few_kernel(const lmop_matmul_ar
       if (kb >= kb_n) kb = kb_n - 1;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        int o = kb * GROUP + 32 * g + 16 * h;
+        int o = kb * GROUP + 16 * g + 64 * h;
         if (o > kr - 16) o = kr - 16;
-        b[u].w[h] = *(const uint4*)(brow + o);
+        b[S][u].w[h] = *(const uint4*)(brow + o);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[u][i].w[h] = *(const uint4*)(arow[i] + o);
+        for (int i = 0; i < MT; ++i) a[S][u][i].w[h] = *(const uint4*)(arow[i] + o);
       }
-      const float sbk = sb[kb];
-#pragma unroll
-      for (int i = 0; i < MT; ++i) s[u][i] = sarow[i][kb] * sbk;
     }
+    const int kb = round * CH + sq < kb_n ? round * CH + sq : kb_n - 1;
+    sak[S] = sa[kb];
+    sbk[S] = sb[kb];
   };
   float acc[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.f;
   const int rounds = (kb_n + CH - 1) / CH;
-  load(0);
-  for (int rd = 0; rd < rounds; ++rd) {
-    auto& pr = prod[rd & 1];
-    auto& sc = scl[rd & 1];
+  auto round = [&](int rd, auto set) {
+    constexpr int S = decltype(set)::value;
+    auto& pr = prod[S];
+    auto& sc = scl[S];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int q = u * NW + wave, kb = rd * CH + q;
-      const int valid = p.k - kb * GROUP - 32 * g;
+      const int valid = p.k - kb * GROUP - 16 * g;
       if (kb == kb_n - 1) {
-        keep_valid(b[u], valid);
+        keep_valid(b[S][u], valid);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) keep_valid(a[u][i], valid);
+        for (int i = 0; i < MT; ++i) keep_valid(a[S][u][i], valid);
       }
-      const Operand<F32> bo = operand<F32>(b[u]);
+      const Operand<F32> bo = operand<F32>(b[S][u]);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        *(f32x4*)&pr[q][256 * i + 4 * lane] = dot(bo, operand<F32>(a[u][i]));
-        if (g == 0) sc[q][16 * i + c] = s[u][i];
+        *(f32x4*)&pr[q][256 * i + 4 * lane] = dot(bo, operand<F32>(a[S][u][i]));
       }
     }
-    if (rd + 1 < rounds) load(rd + 1);
+    if (st < 16 * MT) sc[sq][st] = sak[S] * sbk[S];
+    if (rd + 2 < rounds) load(rd + 2, set);
     // a round's products are added between this barrier and the next, while
     // the next round's go to the other buffer
-    __syncthreads();
+    wait_vmcnt_lgkm0<63>();
+    barrier();
     const int live = kb_n - rd * CH < CH ? kb_n - rd * CH : CH;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int o = (int)threadIdx.x + 512 * i;
-      if (o < OUT)
-        for (int q = 0; q < live; ++q)
-          acc[i] = __builtin_fmaf(pr[q][o], sc[q][(o >> 8) * 16 + ((o >> 2) & 15)], acc[i]);
+      if (o < OUT) {
+        if (live == CH) {
+#pragma unroll 8
+          for (int q = 0; q < CH; ++q)
+            acc[i] = __builtin_fmaf(pr[q][o], sc[q][(o >> 8) * 16 + ((o >> 2) & 15)], acc[i]);
+        } else {
+          for (int q = 0; q < live; ++q)
+            acc[i] = __builtin_fmaf(pr[q][o], sc[q][(o >> 8) * 16 + ((o >> 2) & 15)], acc[i]);
+        }
+      }
     }
+  };
+  load(0, std::integral_constant<int, 0>{});
+  if (rounds > 1) load(1, std::integral_constant<int, 1>{});
+  for (int rd = 0; rd < rounds; rd += 2) {
+    round(rd, std::integral_constant<int, 0>{});
+    if (rd + 1 < rounds) round(rd + 1, std::integral_constant<int, 1>{});
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -364,12 +461,13 @@ __global__ __launch_bounds__(256) void matmul_empty_kernel(const lmop_matmul_arg
   ((T*)p.c)[m * p.ldc + n] = (T)(p.add ? p.add[m * p.ldadd + n] : 0.f);
 }
 
-template <typename T, int MT, int NT, int WM, int WN, int OCC>
+template <typename T, int TILE>
 hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
-  using C = Tile<MT, NT, WM, WN, OCC>;
+  constexpr Fp8Tile t = kFp8Tiles[TILE];
+  using C = Tile<t.mt, t.nt, t.wm, t.wn, t.occ>;
   const size_t tiles = (size_t)((a.m + C::BM - 1) / C::BM) * ((a.n + C::BN - 1) / C::BN);
   if (tiles > 0x3fffffffu) return hipErrorInvalidValue;
-  auto* k = matmul_tile_kernel<T, MT, NT, WM, WN, OCC>;
+  auto* k = matmul_tile_kernel<T, t.mt, t.nt, t.wm, t.wn, t.occ>;
   static const hipError_t raised = hipFuncSetAttribute(
       (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
   if (raised != hipSuccess) return raised;
@@ -381,8 +479,7 @@ template <typename T, int MT, int U>
 hipError_t launch_few(hipStream_t s, const lmop_matmul_args& a) {
   const size_t tiles = (size_t)((a.m + 16 * MT - 1) / (16 * MT)) * ((a.n + 15) / 16);
   if (tiles > 0x7fffffffu) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((matmul_few_kernel<T, MT, U>), dim3((unsigned)tiles), dim3(512), 0, s, a,
-                     aligned4<T>(a));
+  hipLaunchKernelGGL((matmul_few_kernel<T, MT, U>), dim3((unsigned)tiles), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
@@ -394,9 +491,17 @@ hipError_t launch(hipStream_t s, const lmop_matmul_args& a) {
     hipLaunchKernelGGL(matmul_empty_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  if (a.m <= 16) return launch_few<T, 1, 4>(s, a);
-  if (a.m <= 128) return launch_few<T, 2, 2>(s, a);
-  return launch_tile<T, 4, 4, 2, 2, 2>(s, a);
+  switch (pick_fp8_kernel(std::is_same_v<T, float>, a.m, a.n, a.k)) {
+    case 0:
+      if constexpr (!std::is_same_v<T, float>) return launch_tile<T, 0>(s, a);
+      return hipErrorInvalidValue;  // not offered
+    case 1: return launch_tile<T, 1>(s, a);
+    case 2: return launch_tile<T, 2>(s, a);
+    case 3: return launch_tile<T, 3>(s, a);
+    case 4: return launch_tile<T, 4>(s, a);
+    case kFp8Few16: return launch_few<T, 1, 2>(s, a);
+    default: return launch_few<T, 2, 1>(s, a);
+  }
 }
 
 }  // namespace

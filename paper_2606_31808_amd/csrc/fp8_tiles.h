@@ -1,0 +1,68 @@
+// The block-scaled FP8 product's kernels and the rule that picks one; plain
+// C++, so that the host can check which call takes which.
+#pragma once
+#include <algorithm>
+
+namespace lmop {
+
+// A tile of 16*mt*wm tokens x 16*nt*wn columns by wm x wn waves, occ
+// workgroups a CU; us per group of 128 features with one workgroup on a CU and
+// with occ of them (same card, weights from memory), for 16-bit results and
+// for fp32 ones (0: not offered).  few: 16*mt tokens x 16 columns by 8 waves
+// that share K.
+struct Fp8Tile {
+  int mt, nt, wm, wn, occ;
+  float one[2], all[2];
+  constexpr int bm() const { return 16 * mt * wm; }
+  constexpr int bn() const { return 16 * nt * wn; }
+};
+constexpr Fp8Tile kFp8Tiles[] = {
+    {8, 4, 2, 4, 1, {1.90f, 0.f}, {2.00f, 0.f}},  // 256 x 256
+    {4, 4, 2, 4, 1, {1.12f, 2.05f}, {1.20f, 2.05f}},  // 128 x 256
+    {2, 4, 2, 2, 2, {0.55f, 0.85f}, {0.80f, 1.25f}},  // 64 x 128
+    {2, 2, 2, 2, 2, {0.38f, 0.57f}, {0.65f, 0.87f}},  // 64 x 64
+    {2, 1, 1, 4, 2, {0.29f, 0.46f}, {0.45f, 0.61f}},  // 32 x 64
+};
+constexpr int kNumFp8Tiles = sizeof(kFp8Tiles) / sizeof(kFp8Tiles[0]);
+// the picks after the tiles: up to 16 tokens, up to 32 tokens
+constexpr int kFp8Few16 = kNumFp8Tiles, kFp8Few32 = kNumFp8Tiles + 1;
+constexpr int kNumFp8Kernels = kNumFp8Tiles + 2;
+
+// Estimated us.  Tiles: rounds over the 256 CUs, at least the time in which
+// the weight comes from memory (4.4 TB/s), and 3 us around them.  Few tokens:
+// 4 us and a time per tile and group that grows with the tokens (their codes
+// are read again for every 16 columns).  Measured, us, few against the best tile:
+//   1 token:   n 6144 k 4096: 8.5 / 12.4, n 4096 k 14336: 12.9 / 33, n 28672 k 4096: 22.7 / 26.8
+//   16 tokens: 11.7 / 11.8, 18.6 / 32.3, 35.6 / 26.6
+//   24 tokens: 14.6 / 12.1, 23.8 / 32.6, 44.2 / 27.9;  n 2048 k 2048: 5.1 / 7.1
+//   64 tokens (two rounds of few): 22.3 / 12.3, 46.6 / 32.8
+// and of the tiles, 16-bit results (fp32): 512 x 4096, k 4096: 32 x 64 26, 64 x 64 21
+// (28), 64 x 128 19 (30), 128 x 256 35 (61), 256 x 256 60; 2047 x 4096, k 4096: 64 x 128 58
+// (81), 128 x 256 42 (66), 256 x 256 62; 16384 x 28672, k 4096: 128 x 256 2181, 256 x 256 1830.
+inline float fp8_cost(int kernel, bool f32, int m, int n, int k) {
+  const float groups = (k + 127) / 128;
+  if (kernel >= kNumFp8Tiles) {
+    const bool wide = kernel == kFp8Few32;
+    if (m > (wide ? 32 : 16)) return 1e30f;
+    const float per = wide ? 0.62e-3f + 0.014e-3f * std::max(m - 16, 0) : 0.32e-3f + 0.02e-3f * (m - 1);
+    return 4.f + per * (float)((n + 15) / 16) * groups;
+  }
+  const Fp8Tile& t = kFp8Tiles[kernel];
+  if (t.all[f32] == 0.f) return 1e30f;
+  const long tiles = (long)((m + t.bm() - 1) / t.bm()) * ((n + t.bn() - 1) / t.bn());
+  const long round = 256L * t.occ, full = tiles / round, rem = tiles % round;
+  const float rounds =
+      full * t.all[f32] + (rem == 0 ? 0.f : rem <= 256 ? t.one[f32] : t.all[f32]);
+  return 3.f + std::max(groups * rounds, (float)n * (float)k / 4.4e6f);
+}
+
+// The kernel with the least estimated time, the smaller tile of two that wait
+// for the same memory.  Every kernel gives the same bits.
+inline int pick_fp8_kernel(bool f32, int m, int n, int k) {
+  int best = kNumFp8Kernels - 1;
+  for (int i = best - 1; i >= 0; --i)
+    if (fp8_cost(i, f32, m, n, k) < fp8_cost(best, f32, m, n, k)) best = i;
+  return best;
+}
+
+}  // namespace lmop

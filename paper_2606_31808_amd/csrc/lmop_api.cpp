@@ -45,6 +45,10 @@ constexpr int kMaxSeq = 1 << 20;
 constexpr int kMaxBatchBudget = 1 << 21;
 // longest row of FP8 codes: a tile's row offsets fit 32 bits
 constexpr int64_t kMaxCodeRow = int64_t(1) << 23;
+constexpr int64_t kMaxScaleRow = int64_t(1) << 21;  // and of the tokens' scales
+// the most 16 x 16 tiles, groups or heads of one operator call: grid and index
+// arithmetic stay within 31 bits
+constexpr uint64_t kMaxTasks = uint64_t(1) << 30;
 
 int round_up(int x, int m) { return (x + m - 1) / m * m; }
 int64_t round_up64(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -2569,6 +2573,8 @@ lmop_status lmop_quantize(lmop_ctx* ctx, const lmop_quantize_args* a) {
   if (a->gate) LMOP_TRY(check_rows(ctx, "gate", a->gate, a->cols, a->ldg, es, es));
   LMOP_TRY(check_codes(ctx, "q", a->q, a->cols, a->ldq));
   LMOP_TRY(check_rows(ctx, "scale", a->scale, fp8_groups(a->cols), a->lds, 4, 4));
+  if ((uint64_t)a->rows * fp8_groups(a->cols) > kMaxTasks)
+    return fail(ctx, LMOP_ERR_UNSUPPORTED, "%d x %d is too large for one call", a->rows, a->cols);
   const double e = (double)a->rows * a->cols;
   return queue_operator(ctx, "quantize", e * (a->gate ? 10 : 4),
                         e * (es * (a->gate ? 2 : 1) + 1) + 4.0 * a->rows * fp8_groups(a->cols),
@@ -2582,11 +2588,16 @@ lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* a) {
   if (a->dtype != LMOP_F16 && a->dtype != LMOP_BF16 && a->dtype != LMOP_F32)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
   if (a->m == 0 || a->n == 0) return LMOP_OK;
+  if ((uint64_t)((a->m + 15ll) / 16) * ((a->n + 15ll) / 16) > kMaxTasks)
+    return fail(ctx, LMOP_ERR_UNSUPPORTED, "%d x %d is too large for one call", a->m, a->n);
   if (a->k > 0) {
     LMOP_TRY(check_codes(ctx, "a", a->a, a->k, a->lda));
     LMOP_TRY(check_codes(ctx, "b", a->b, a->k, a->ldb));
     LMOP_TRY(check_rows(ctx, "a_scale", a->a_scale, fp8_groups(a->k), a->ldas, 4, 4));
     LMOP_TRY(check_rows(ctx, "b_scale", a->b_scale, fp8_groups(a->k), a->ldbs, 4, 4));
+    if (a->ldas > kMaxScaleRow)
+      return fail(ctx, LMOP_ERR_UNSUPPORTED, "a_scale: rows %lld apart (at most %lld)",
+                  (long long)a->ldas, (long long)kMaxScaleRow);
   }
   const size_t es = dtype_bytes(a->dtype);
   LMOP_TRY(check_rows(ctx, "c", a->c, a->n, a->ldc, es, es));
@@ -2611,6 +2622,8 @@ lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* a) {
   if (a->v_layout != LMOP_V_ROWS && a->v_layout != LMOP_V_COLUMNS)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown v_layout %d", a->v_layout);
   if (a->n_tokens == 0 || (!a->q && !a->k && !a->v)) return LMOP_OK;
+  if ((uint64_t)a->n_tokens * (ctx->cfg.n_heads + 2ll * ctx->cfg.n_kv_heads) > kMaxTasks)
+    return fail(ctx, LMOP_ERR_UNSUPPORTED, "%d tokens are too many for one call", a->n_tokens);
   if ((a->k || a->v) && !a->slot && a->n_slots < a->n_tokens)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "%d tokens without slots, %d slots", a->n_tokens,
                 a->n_slots);

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -169,9 +170,9 @@ def _load():
         "lmop_set_profiling": (st, [vp, i32]),
         "lmop_get_kernel_stats": (st, [vp, C.POINTER(lmop_kernel_stat), i32,
                                        C.POINTER(C.c_int32)]),
-        "lmop_quantize": (st, [vp, C.POINTER(lmop_quantize_args)]),
-        "lmop_matmul": (st, [vp, C.POINTER(lmop_matmul_args)]),
-        "lmop_qk_norm_rope": (st, [vp, C.POINTER(lmop_qk_norm_rope_args)]),
+        "lmop_quantize": (st, [vp, vp]),
+        "lmop_matmul": (st, [vp, vp]),
+        "lmop_qk_norm_rope": (st, [vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -427,56 +428,80 @@ def lmop_get_kernel_stats(ctx):
 
 # ---------------------------------------------------------------- operators
 # Tensors here are torch tensors: inputs of rows with adjacent elements at any
-# row stride, outputs given or allocated by the Context methods below.
+# row stride, outputs given or allocated by the Context methods below.  A call
+# on one token takes the GPU 2 to 4 us, so these functions are kept short: the
+# argument structs are packed with `struct`, which takes a quarter of the time
+# of filling a ctypes structure (whose fields are checked against the formats
+# below when the module loads).
 _DTYPES = {torch.float16: LMOP_F16, torch.bfloat16: LMOP_BF16, torch.float32: LMOP_F32}
-_CODES = (torch.float8_e4m3fn, torch.uint8)
+_CODES = {torch.float8_e4m3fn: 0, torch.uint8: 0}
+_F32 = {torch.float32: LMOP_F32}
+_PACK = {}
+for _name, _fmt, _struct in (("quantize", "4P4q3i4x", lmop_quantize_args),
+                             ("matmul", "6P6q4i", lmop_matmul_args),
+                             ("qk_norm_rope", "10P6q4i", lmop_qk_norm_rope_args)):
+    assert struct.calcsize(_fmt) == C.sizeof(_struct)
+    _PACK[_name] = struct.Struct(_fmt).pack
 
 
-def _up(x: int, to: int) -> int:
-    return (x + to - 1) // to * to
-
-
-def _mat(t, what: str, rows: int, cols: int, dtypes, least: int = 0):
-    """(address, row stride) of a [rows][cols] tensor; a single row's stride does
-    not matter and counts as `least` (or the row's length)."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+def _bad(t, what: str, rows: int, cols: int, dtypes, dev: int):
+    """Raises what is wrong with a tensor."""
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}, the ctx on device {dev}")
+    if tuple(t.shape) != (rows, cols):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, expected ({rows}, {cols})")
     if t.dtype not in dtypes:
         raise ValueError(f"{what}: dtype {t.dtype}")
+    raise ValueError(f"{what}: the elements of a row are not adjacent")
+
+
+def _ld(t, what: str, rows: int, cols: int, dtypes, dev: int, least: int = 0) -> int:
+    """The row stride of a [rows][cols] tensor; a single row's does not matter and
+    counts as its length, or `least`."""
+    if t.get_device() != dev or t.shape != (rows, cols) or t.dtype not in dtypes:
+        _bad(t, what, rows, cols, dtypes, dev)
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
-        raise ValueError(f"{what}: the elements of a row are not adjacent")
-    return t.data_ptr(), ld if rows > 1 else max(least, cols)
+        _bad(t, what, rows, cols, dtypes, dev)
+    return ld if rows > 1 else max(least, cols)
 
 
-def _codes(t, what: str, rows: int, cols: int):
-    """_mat of FP8 codes, whose rows are read to the next multiple of 16 bytes."""
-    most = _up(cols, 16)
-    p, ld = _mat(t, what, rows, cols, _CODES, most)
+def _ld_codes(t, what: str, rows: int, cols: int, dev: int) -> int:
+    """_ld of FP8 codes, whose rows are read to the next multiple of 16 bytes."""
+    most = (cols + 15) & -16
+    ld = _ld(t, what, rows, cols, _CODES, dev, most)
     if most != cols and rows > 0 and (t.storage_offset() + (rows - 1) * ld + most >
                                       t.untyped_storage().nbytes()):
         raise ValueError(f"{what}: the last row's storage ends before {most} bytes")
-    return p, ld
+    return ld
 
 
-def _vec(t, what: str, n: int, dtype):
+def _current_stream(dev: int) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _vec(t, what: str, n: int, dtype, dev: int) -> int:
     if t is None:
-        return None
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{what}: expected {n} adjacent elements of {dtype}")
+        return 0
+    if (t.get_device() != dev or t.shape != (n,) or t.dtype != dtype or
+            (n > 1 and t.stride(0) != 1)):
+        raise ValueError(f"{what}: expected {n} adjacent elements of {dtype} on device {dev}")
     return t.data_ptr()
 
 
 def lmop_quantize(ctx, x, q, scale, gate=None) -> None:
     """E4M3 codes q and scales of x, or of silu(gate) * x."""
     rows, cols = x.shape
-    groups = (cols + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP
-    px, ldx = _mat(x, "x", rows, cols, _DTYPES)
-    pg, ldg = (None, 0) if gate is None else _mat(gate, "gate", rows, cols, (x.dtype,))
-    pq, ldq = _codes(q, "q", rows, cols)
-    ps, lds = _mat(scale, "scale", rows, groups, (torch.float32,))
-    a = lmop_quantize_args(px, pg, pq, ps, ldx, ldg, ldq, lds, rows, cols, _DTYPES[x.dtype])
-    st = _lib.lmop_quantize(ctx, C.byref(a))
+    dt, dev = x.dtype, x.get_device()
+    ldx = _ld(x, "x", rows, cols, _DTYPES, dev)
+    pg = ldg = 0
+    if gate is not None:
+        ldg = _ld(gate, "gate", rows, cols, (dt,), dev)
+        pg = gate.data_ptr()
+    st = _lib.lmop_quantize(ctx, _PACK["quantize"](
+        x.data_ptr(), pg, q.data_ptr(), scale.data_ptr(), ldx, ldg,
+        _ld_codes(q, "q", rows, cols, dev), _ld(scale, "scale", rows, (cols + 127) >> 7, _F32, dev),
+        rows, cols, _DTYPES[dt]))
     if st:
         _check(st, ctx)
 
@@ -484,60 +509,62 @@ def lmop_quantize(ctx, x, q, scale, gate=None) -> None:
 def lmop_matmul(ctx, a, a_scale, b, b_scale, c, add=None) -> None:
     """c = a b^T (+ add) of E4M3 codes: scales per row and 128 features of a, per
     128 x 128 block of b."""
-    (m, k), n = a.shape, b.shape[0]
-    groups = (k + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP
-    pa, lda = _codes(a, "a", m, k)
-    pb, ldb = _codes(b, "b", n, k)
-    f32 = (torch.float32,)
-    psa, ldas = _mat(a_scale, "a_scale", m, groups, f32)
-    psb, ldbs = _mat(b_scale, "b_scale", (n + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP, groups, f32)
-    pc, ldc = _mat(c, "c", m, n, _DTYPES)
-    pd, ldadd = (None, 0) if add is None else _mat(add, "add", m, n, f32)
-    s = lmop_matmul_args(pa, psa, pb, psb, pd, pc, lda, ldb, ldas, ldbs, ldadd, ldc, m, n, k,
-                         _DTYPES[c.dtype])
-    st = _lib.lmop_matmul(ctx, C.byref(s))
+    (m, k), n, dev = a.shape, b.shape[0], a.get_device()
+    groups = (k + 127) >> 7
+    pd = ldadd = 0
+    if add is not None:
+        ldadd = _ld(add, "add", m, n, _F32, dev)
+        pd = add.data_ptr()
+    ldc = _ld(c, "c", m, n, _DTYPES, dev)
+    st = _lib.lmop_matmul(ctx, _PACK["matmul"](
+        a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), pd, c.data_ptr(),
+        _ld_codes(a, "a", m, k, dev), _ld_codes(b, "b", n, k, dev),
+        _ld(a_scale, "a_scale", m, groups, _F32, dev),
+        _ld(b_scale, "b_scale", (n + 127) >> 7, groups, _F32, dev), ldadd, ldc, m, n, k,
+        _DTYPES[c.dtype]))
     if st:
         _check(st, ctx)
 
 
-def lmop_qk_norm_rope(ctx, shape, n_tokens, q=None, k=None, v=None, pos=None, q_gain=None,
+def lmop_qk_norm_rope(ctx, heads, n_tokens, q=None, k=None, v=None, pos=None, q_gain=None,
                       k_gain=None, slot=None, q_out=None, k_out=None, v_out=None,
                       v_columns: bool = False) -> None:
-    """Per-head RMSNorm, RoPE and cache write of n_tokens tokens; shape is the
+    """Per-head RMSNorm, RoPE and cache write of n_tokens tokens; heads is the
     ctx's (n_heads, n_kv_heads, head_dim)."""
-    nq, nkv, hd = shape
-    first = next((t for t in (q, k, v) if t is not None), None)
+    first = q if q is not None else k if k is not None else v
     if first is None:
         raise ValueError("q, k and v are all None")
-    dt = (first.dtype,)
-    if first.dtype not in (torch.float16, torch.bfloat16):
-        raise ValueError(f"dtype {first.dtype}: float16 or bfloat16")
-    n_slots = None
-    if k is not None and k_out is not None:
+    nq, nkv, hd = heads
+    nq *= hd
+    nkv *= hd
+    dev, dt = first.get_device(), first.dtype
+    if dt not in _DTYPES or dt is torch.float32:
+        raise ValueError(f"dtype {dt}: float16 or bfloat16")
+    own = (dt,)
+    n_slots = 0
+    if v is not None:
+        n_slots = v_out.shape[1 if v_columns else 0]
+    if k is not None:
+        if v is not None and n_slots != k_out.shape[0]:
+            raise ValueError(f"k_out has {k_out.shape[0]} slots, v_out {n_slots}")
         n_slots = k_out.shape[0]
-    if v is not None and v_out is not None:
-        ns = v_out.shape[1 if v_columns else 0]
-        if n_slots not in (None, ns):
-            raise ValueError(f"k_out has {n_slots} slots, v_out {ns}")
-        n_slots = ns
-    n_slots = n_slots or 0
-
-    def mat(t, what, rows, cols):
-        return (None, 0) if t is None else _mat(t, what, rows, cols, dt)
-
-    pq, ldq = mat(q, "q", n_tokens, nq * hd)
-    pk, ldk = mat(k, "k", n_tokens, nkv * hd)
-    pv, ldv = mat(v, "v", n_tokens, nkv * hd)
-    pqo, ldqo = mat(q_out if q is not None else None, "q_out", n_tokens, nq * hd)
-    pko, ldko = mat(k_out if k is not None else None, "k_out", n_slots, nkv * hd)
-    pvo, ldvo = mat(v_out if v is not None else None, "v_out",
-                    *((nkv * hd, n_slots) if v_columns else (n_slots, nkv * hd)))
-    a = lmop_qk_norm_rope_args(
-        pq, pk, pv, _vec(q_gain, "q_gain", hd, torch.float32),
-        _vec(k_gain, "k_gain", hd, torch.float32), _vec(pos, "pos", n_tokens, torch.int32),
-        _vec(slot, "slot", n_tokens, torch.int32), pqo, pko, pvo, ldq, ldk, ldv, ldqo, ldko, ldvo,
-        n_tokens, n_slots, LMOP_V_COLUMNS if v_columns else LMOP_V_ROWS, _DTYPES[first.dtype])
-    st = _lib.lmop_qk_norm_rope(ctx, C.byref(a))
+    pq = pk = pv = pqo = pko = pvo = ldq = ldk = ldv = ldqo = ldko = ldvo = 0
+    if q is not None:
+        ldq, ldqo = _ld(q, "q", n_tokens, nq, own, dev), _ld(q_out, "q_out", n_tokens, nq, own, dev)
+        pq, pqo = q.data_ptr(), q_out.data_ptr()
+    if k is not None:
+        ldk, ldko = _ld(k, "k", n_tokens, nkv, own, dev), _ld(k_out, "k_out", n_slots, nkv, own, dev)
+        pk, pko = k.data_ptr(), k_out.data_ptr()
+    if v is not None:
+        ldv = _ld(v, "v", n_tokens, nkv, own, dev)
+        ldvo = (_ld(v_out, "v_out", nkv, n_slots, own, dev) if v_columns
+                else _ld(v_out, "v_out", n_slots, nkv, own, dev))
+        pv, pvo = v.data_ptr(), v_out.data_ptr()
+    st = _lib.lmop_qk_norm_rope(ctx, _PACK["qk_norm_rope"](
+        pq, pk, pv, _vec(q_gain, "q_gain", hd, torch.float32, dev),
+        _vec(k_gain, "k_gain", hd, torch.float32, dev), _vec(pos, "pos", n_tokens, torch.int32, dev),
+        _vec(slot, "slot", n_tokens, torch.int32, dev), pqo, pko, pvo, ldq, ldk, ldv, ldqo, ldko,
+        ldvo, n_tokens, n_slots, LMOP_V_COLUMNS if v_columns else LMOP_V_ROWS, _DTYPES[dt]))
     if st:
         _check(st, ctx)
 
@@ -559,8 +586,9 @@ class Context:
             cfg.n_layers = n_layers
         self.vocab = shape.vocab
         self.heads = (cfg.n_heads, cfg.n_kv_heads, cfg.head_dim)
-        # where the operators' tensors live, and the torch stream they are ordered on
-        self.device = torch.device("cuda", device) if device >= 0 else torch.device("cpu")
+        # where the operators' tensors live (-1: the host), and the torch stream
+        # they are ordered on
+        self.device = max(int(device), -1)
         self.stream = int(stream or 0)
         self.ctx = lmop_create(cfg, device, stream)
 
@@ -616,14 +644,13 @@ class Context:
         return lmop_get_kernel_stats(self.ctx)
 
     # -- operators: they queue work on the ctx's stream and return
-    def _ready(self, *tensors):
-        """The tensors are on the ctx's device, and torch's current stream is the
-        ctx's: a ctx made without a stream has one that the null stream orders."""
-        for t in tensors:
-            if t is not None and t.device != self.device:
-                raise ValueError(f"a tensor is on {t.device}, the ctx on {self.device}")
-        if (self.device.type == "cuda" and
-                torch.cuda.current_stream(self.device).cuda_stream != self.stream):
+    def _here(self, t):
+        """The ctx's device, which t has to be on, and torch's current stream has to be
+        the ctx's (a ctx made without a stream has one that the null stream orders)."""
+        dev = self.device
+        if t.get_device() != dev or (dev < 0 and not t.is_cpu):
+            raise ValueError(f"a tensor is on {t.device}, the ctx on device {dev}")
+        if dev >= 0 and _current_stream(dev) != self.stream:
             raise ValueError("torch's current stream is not the ctx's stream: make the Context "
                              "with stream=..., or call under torch.cuda.stream(...)")
 
@@ -631,22 +658,22 @@ class Context:
         """E4M3 codes [rows, cols] (torch.float8_e4m3fn, rows a multiple of 16 bytes
         apart) and float32 scales [rows, ceil(cols / 128)] of x, or of
         silu(gate) * x.  out: (codes, scales) to write into."""
+        self._here(x)
         if out is None:
             rows, cols = x.shape
-            q = torch.empty((rows, _up(cols, 16)), dtype=torch.float8_e4m3fn, device=x.device)
-            if q.shape[1] != cols:
+            most = (cols + 15) & -16
+            q = torch.empty((rows, most), dtype=torch.float8_e4m3fn, device=x.device)
+            if most != cols:
                 q = q[:, :cols]
-            out = q, torch.empty((rows, (cols + LMOP_FP8_GROUP - 1) // LMOP_FP8_GROUP),
-                                 dtype=torch.float32, device=x.device)
-        self._ready(x, gate, *out)
+            out = q, torch.empty((rows, (cols + 127) >> 7), dtype=torch.float32, device=x.device)
         lmop_quantize(self.ctx, x, out[0], out[1], gate)
         return out
 
     def matmul(self, a, a_scale, b, b_scale, dtype=torch.float16, add=None, out=None):
         """a b^T (+ add) of E4M3 codes a [m, k], b [n, k] with block scales."""
+        self._here(a)
         if out is None:
             out = torch.empty((a.shape[0], b.shape[0]), dtype=dtype, device=a.device)
-        self._ready(a, a_scale, b, b_scale, add, out)
         lmop_matmul(self.ctx, a, a_scale, b, b_scale, out, add)
         return out
 
@@ -655,11 +682,11 @@ class Context:
         """Normalises (where a gain is given) and rotates queries and keys, and writes
         keys and values by slot into k_out, v_out.  Returns the queries (q_out,
         or a new tensor; None without q)."""
+        self._here(pos)
         if q is not None and q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if (k is None) != (k_out is None) or (v is None) != (v_out is None):
             raise ValueError("k needs k_out, v needs v_out")
-        self._ready(q, k, v, pos, q_gain, k_gain, slot, q_out, k_out, v_out)
         lmop_qk_norm_rope(self.ctx, self.heads, pos.shape[0], q, k, v, pos, q_gain, k_gain, slot,
                           q_out, k_out, v_out, v_columns)
         return q_out

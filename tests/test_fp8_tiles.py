@@ -1,0 +1,91 @@
+"""The block-scaled FP8 product's rule on the host: the sizes that the GPU tests
+run take every kernel it offers, and it is never far from the fastest one."""
+import ctypes as C
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2606_31808_amd import build
+from tests import test_gpu_operators as gpu
+
+SRC = """
+#include "fp8_tiles.h"
+extern "C" int pick(int f32, int m, int n, int k) { return lmop::pick_fp8_kernel(f32, m, n, k); }
+extern "C" int kernels() { return lmop::kNumFp8Kernels; }
+"""
+
+
+@pytest.fixture(scope="module")
+def rule(tmp_path_factory):
+    if not shutil.which("g++"):
+        pytest.skip("no g++")
+    d = tmp_path_factory.mktemp("rule")
+    (d / "r.cpp").write_text(SRC)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{build.CSRC}",
+                    str(d / "r.cpp"), "-o", str(d / "r.so")], check=True)
+    return C.CDLL(str(d / "r.so"))
+
+
+@pytest.mark.parametrize("f32", [0, 1])
+def test_gpu_sizes_take_every_kernel(rule, f32):
+    taken = {rule.pick(f32, m, n, k) for m, n, k in gpu.SIZES + gpu.LARGE}
+    assert taken == set(range(f32, rule.kernels()))  # the largest tile is for 16-bit results
+
+
+# us by kernel: 0 256x256, 1 128x256, 2 64x128, 3 64x64, 4 32x64, 5 and 6 few tokens
+MEASURED = [
+    (0, 1, 6144, 4096, {3: 12.4, 5: 8.5, 6: 10.2}),
+    (0, 16, 6144, 4096, {3: 12.9, 4: 11.8, 5: 11.7, 6: 12.7}),
+    (0, 24, 6144, 4096, {3: 13.1, 4: 12.1, 6: 14.6}),
+    (0, 64, 6144, 4096, {2: 20.3, 3: 14.6, 4: 12.3}),
+    (0, 256, 6144, 4096, {2: 19.9, 3: 21.9, 4: 26.1}),
+    (0, 1, 4096, 14336, {3: 35.8, 5: 12.9, 6: 15.5}),
+    (0, 16, 4096, 14336, {3: 37.7, 4: 32.3, 5: 18.6, 6: 20.0}),
+    (1, 24, 4096, 14336, {3: 61.7, 4: 51.0, 6: 24.5}),
+    (0, 128, 4096, 14336, {2: 59.9, 3: 42.3, 4: 32.8}),
+    (0, 256, 4096, 14336, {2: 58.7, 3: 42.8, 4: 50.8}),
+    (0, 1, 28672, 4096, {3: 26.8, 5: 22.7, 6: 29.5}),
+    (0, 16, 28672, 4096, {2: 28.6, 3: 27.2, 4: 26.6, 5: 35.6}),
+    (0, 128, 28672, 4096, {2: 41.2, 3: 46.6, 4: 57.8}),
+    (0, 24, 2048, 2048, {3: 7.2, 4: 7.0, 6: 5.1}),
+    (0, 512, 4096, 4096, {0: 60.1, 1: 35.5, 2: 19.4, 3: 21.2}),
+    (1, 512, 4096, 4096, {1: 61.4, 2: 30.2, 3: 27.9}),
+    (0, 2047, 4096, 4096, {0: 62.5, 1: 41.7, 2: 57.6, 3: 72.7}),
+    (1, 2047, 4096, 4096, {1: 65.9, 2: 81.4, 3: 98.7}),
+    (0, 4093, 16384, 2048, {0: 159.2, 1: 195.5, 2: 224.8}),
+    (0, 16384, 28672, 4096, {0: 1829.9, 1: 2180.9, 2: 2646.3}),
+]
+
+
+@pytest.mark.parametrize("f32,m,n,k,us", MEASURED)
+def test_pick_is_near_the_fastest(rule, f32, m, n, k, us):
+    pick = rule.pick(f32, m, n, k)
+    assert pick in us, pick
+    assert us[pick] <= 1.1 * min(us.values())
+
+
+def test_rule_is_defined_at_the_limits(rule):
+    for f32 in (0, 1):
+        for m, n, k in ((1, 1, 1), (2 ** 30, 16, 1), (16, 2 ** 30, 1), (1, 1, 2 ** 23),
+                        (2 ** 19, 2 ** 19, 2 ** 23)):
+            assert f32 <= rule.pick(f32, m, n, k) < rule.kernels()
+
+
+def test_helpers_keep_the_wait_state(tmp_path):
+    """The masked 4-byte load has an instruction between its write of M0 and the load."""
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("no hipcc")
+    src, out = tmp_path / "p.hip", tmp_path / "p.s"
+    src.write_text('#include "lds_dma.h"\nusing namespace lmop;\nextern "C" __global__ void probe('
+                   "const char* a, unsigned off, unsigned lds, unsigned long m) {\n"
+                   "  g2l4_m0_mask(a, off * threadIdx.x, lds, m);\n}\n")
+    subprocess.run([build.HIPCC, *build.FLAGS, "-x", "hip", "--offload-device-only", "-S", str(src),
+                    "-o", str(out)], check=True, capture_output=True)
+    lines = [l.split(";")[0].strip() for l in out.read_text().splitlines()]
+    lines = [l for l in lines if l and not l.startswith(".")]
+    at = next(i for i, l in enumerate(lines) if l.startswith("global_load_lds_dword "))
+    assert re.match(r"s_\w+ m0,", lines[at - 2]) and not re.match(r"s_\w+ m0,", lines[at - 1])
+    assert lines[at + 1].startswith("s_mov_b64 exec, -1")

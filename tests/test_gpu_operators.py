@@ -168,21 +168,34 @@ def _scales(rows, cols, seed, pad=1):
 
 
 def _ref_matmul(a, sa, b, sb):
-    """(A B^T, sum of magnitudes) in 64 bits."""
+    """(A B^T, sum of magnitudes, sum over eights of features of the largest product's
+    bound) in 64 bits."""
     f = torch.arange(a.shape[1], device=a.device) // G
     r = torch.arange(b.shape[0], device=a.device) // G
     A = a.float().double() * sa.double()[:, f]
-    B = (b.float().double() * sb.double()[r][:, f]).t().contiguous()
-    return A @ B, A.abs() @ B.abs()
+    B = b.float().double() * sb.double()[r][:, f]
+
+    def eights(x):
+        x = torch.nn.functional.pad(x.abs(), (0, -x.shape[1] % 8))
+        return x.view(x.shape[0], -1, 8).amax(-1)
+
+    return (A @ B.t().contiguous(), A.abs() @ B.abs().t().contiguous(),
+            eights(A) @ eights(B).t().contiguous())
 
 
 def _check_product(c, a, sa, b, sb, add=None):
-    ref, mag = _ref_matmul(a, sa, b, sb)
+    ref, mag, most = _ref_matmul(a, sa, b, sb)
     k = a.shape[1]
     if add is not None:
         ref, mag = ref + add.double(), mag + add.double().abs()
     # 128 terms of a group, the groups' fma chain, the scales' product, the addition
     tol = (G + -(-k // G) + 4) * 2.0 ** -23 * mag
+    if c.dtype != torch.float32:
+        # The 8-bit matrix instruction cuts off what lies below 2^-13 of the leading
+        # bit of the largest of eight neighbouring products: less than 2^-13 of
+        # that product (at most the product of the eights' largest values) from
+        # each of the other seven.
+        tol = tol + 7 * 2.0 ** -13 * most
     tol = tol + torch.finfo(c.dtype).eps / 2 * (ref.abs() + tol) + torch.finfo(c.dtype).tiny
     d = (c.double() - ref).abs()
     assert torch.all(d <= tol), f"off by {(d / tol).max():.3g} of the tolerance"
@@ -194,8 +207,13 @@ SIZES = [(1, 1, 1), (1, 16, 128), (2, 17, 15), (16, 64, 688), (17, 65, 129), (64
          (100, 16, 256), (520, 520, 272), (1000, 48, 128), (31, 4100, 384)]
 
 
+# where the larger tiles are the fastest
+LARGE = [(2047, 4096, 1000), (300, 2050, 1100), (257, 4099, 700), (2500, 7001, 200),
+         (3001, 5103, 1300), (4097, 6145, 130), (1001, 1103, 8448)]
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
-@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("m,n,k", SIZES + LARGE)
 def test_matmul(ctx, dtype, m, n, k):
     print("matmul", dtype, m, n, k, flush=True)
     a, b = _codes(m, k, 1), _codes(n, k, 2, pad=0)
@@ -209,15 +227,17 @@ def test_matmul(ctx, dtype, m, n, k):
     assert torch.all(wide[:, n:] == 9)
 
 
-@pytest.mark.parametrize("n,k", [(200, 688), (1040, 1300), (5000, 256)])
-def test_matmul_rows_do_not_depend_on_the_batch(ctx, n, k):
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("n,k", [(200, 688), (1040, 1300), (5000, 256), (4100, 4096)])
+def test_matmul_rows_do_not_depend_on_the_batch(ctx, n, k, dtype):
     """Any number of tokens gives a token the same bits: in any kernel and tile."""
-    M = 1100
+    M = 2700
     a, b = _codes(M, k, 11), _codes(n, k, 12)
     sa, sb = _scales(M, -(-k // G), 13), _scales(-(-n // G), -(-k // G), 14)
-    whole = ctx.matmul(a, sa, b, sb, dtype=torch.float32)
-    for m in (1, 2, 9, 16, 17, 32, 33, 48, 64, 65, 100, 128, 129, 200, 256, 257, 400, 513, 1024):
-        part = ctx.matmul(a[M - m:], sa[M - m:], b, sb, dtype=torch.float32)
+    whole = ctx.matmul(a, sa, b, sb, dtype=DT[dtype])
+    for m in (1, 2, 9, 16, 17, 32, 33, 48, 64, 65, 100, 128, 129, 200, 256, 257, 400, 513, 1024,
+              2100):
+        part = ctx.matmul(a[M - m:], sa[M - m:], b, sb, dtype=DT[dtype])
         assert torch.equal(part, whole[M - m:]), m
 
 

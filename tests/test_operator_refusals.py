@@ -57,6 +57,7 @@ INV, UNS, OK = L.LMOP_ERR_INVALID_ARG, L.LMOP_ERR_UNSUPPORTED, L.LMOP_OK
     (dict(ldx=299), INV), (dict(ldx=0), INV), (dict(ldx=-300), INV),
     (dict(ldq=300), INV), (dict(ldq=288), INV), (dict(ldq=320), UNS), (dict(lds=2), INV),
     (dict(ldq=(1 << 23) + 16), UNS),
+    (dict(rows=2 ** 31 - 1), UNS),
     (dict(gate=P, ldg=300), UNS), (dict(gate=P, ldg=10), INV), (dict(gate=P + 1, ldg=300), INV),
 ])
 def test_quantize(ctx, change, status):
@@ -73,6 +74,7 @@ def test_quantize(ctx, change, status):
     (dict(a=P + 8), INV), (dict(b=P + 1), INV), (dict(a_scale=P + 1), INV), (dict(c=P + 1), INV),
     (dict(lda=300), INV), (dict(ldb=288), INV), (dict(ldas=2), INV), (dict(ldbs=2), INV),
     (dict(ldc=199), INV), (dict(lda=(1 << 23) + 16), UNS), (dict(ldb=1 << 23), UNS),
+    (dict(ldas=(1 << 21) + 1), UNS), (dict(m=2 ** 31 - 1, n=2 ** 31 - 1, ldc=2 ** 31), UNS),
     (dict(add=2 * P, ldadd=200), UNS), (dict(add=2 * P, ldadd=199), INV),
     (dict(add=2 * P + 2, ldadd=200), INV),
     (dict(add=P, ldadd=200), INV),                       # c in place, fp16
@@ -92,6 +94,7 @@ def test_matmul(ctx, change, status):
     (dict(pos=None), INV), (dict(pos=P + 1), INV), (dict(slot=P + 2), INV),
     (dict(q_gain=P + 1), INV), (dict(k_gain=P + 2), INV), (dict(q_gain=P, k_gain=P), UNS),
     (dict(dtype=L.LMOP_F32), INV), (dict(dtype=L.LMOP_BF16), UNS), (dict(v_layout=2), INV),
+    (dict(n_tokens=2 ** 31 - 1, n_slots=2 ** 31 - 1), UNS),
     (dict(n_slots=6), INV), (dict(n_slots=6, slot=P), UNS),
     (dict(q_out=None), INV), (dict(k_out=None), INV), (dict(v_out=None), INV),
     (dict(ldq=255), INV), (dict(ldk=255), INV), (dict(ldv=255), INV), (dict(ldqo=255), INV),
