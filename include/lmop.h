@@ -368,7 +368,7 @@ lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t 
  * lmop_load_qk_norms.
  *
  * Unlike the calls above, an operator only queues its kernel on the ctx's
- * stream and returns: the tensors must stay alive until the stream has passed
+ * stream (the null stream for a ctx made without one) and returns: the tensors must stay alive until the stream has passed
  * it, work that writes them must be ordered before it, and a caller may
  * capture it into a HIP graph (with profiling off).  It allocates nothing,
  * uses no workspace and no state of the ctx other than what is said at each

@@ -381,13 +381,14 @@ hipEvent_t take_event(lmop_ctx* c) {
 }
 
 template <typename F>
-lmop_status timed(lmop_ctx* c, const char* name, double flops, double bytes, F&& launch) {
+lmop_status timed_on(lmop_ctx* c, hipStream_t stream, const char* name, double flops, double bytes,
+                     F&& launch) {
   hipEvent_t a = nullptr, b = nullptr;
   if (c->prof > 0 && c->stats[name].launches++ % c->prof == 0) {
     a = take_event(c);
     b = take_event(c);
     if (a && b) {
-      HIP_OK(c, hipEventRecord(a, c->stream));
+      HIP_OK(c, hipEventRecord(a, stream));
     } else {
       if (a) c->ev_free.push_back(a);
       if (b) c->ev_free.push_back(b);
@@ -400,10 +401,15 @@ lmop_status timed(lmop_ctx* c, const char* name, double flops, double bytes, F&&
   if (e != hipSuccess) return fail(c, LMOP_ERR_DEVICE, "launch of %s failed: %s", name,
                                    hipGetErrorString(e));
   if (a && b) {
-    HIP_OK(c, hipEventRecord(b, c->stream));
+    HIP_OK(c, hipEventRecord(b, stream));
     c->spans.push_back(Span{name, a, b, flops, bytes});
   }
   return LMOP_OK;
+}
+
+template <typename F>
+lmop_status timed(lmop_ctx* c, const char* name, double flops, double bytes, F&& launch) {
+  return timed_on(c, c->stream, name, flops, bytes, launch);
 }
 
 lmop_status resolve_spans(lmop_ctx* c) {
@@ -1337,23 +1343,28 @@ lmop_status enter_operator(lmop_ctx* ctx, const void* args) {
   return LMOP_OK;
 }
 
-// Queues one operator on the ctx's stream, with the ctx's device current for
-// the launch only.  Nothing here waits.
+// Queues one operator, with the ctx's device current for the launch only.
+// Nothing here waits.  A ctx made without a stream queues it on the null
+// stream: its own stream is ordered with that one, but not with another such
+// ctx's, while memory that a caller frees and allocates again on the null
+// stream (torch's allocator) passes from one ctx to the other.
 template <typename F>
 lmop_status queue_operator(lmop_ctx* ctx, const char* name, double flops, double bytes,
                                   F&& launch) {
   if (ctx->host_only)
     return fail(ctx, LMOP_ERR_UNSUPPORTED, "host-only ctx: arguments are valid, no device to run");
-  if (ctx->prof > 0) {
+  const hipStream_t stream = ctx->own_stream ? nullptr : ctx->stream;
+  if (ctx->prof > 0 && stream) {
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-    HIP_OK(ctx, hipStreamIsCapturing(ctx->stream, &cap));
+    HIP_OK(ctx, hipStreamIsCapturing(stream, &cap));
     if (cap != hipStreamCaptureStatusNone)
       return fail(ctx, LMOP_ERR_STATE, "%s cannot be captured while profiling is on", name);
   }
   int before = -1;
   HIP_OK(ctx, hipGetDevice(&before));
   if (before != ctx->device) HIP_OK(ctx, hipSetDevice(ctx->device));
-  const lmop_status st = timed(ctx, name, flops, bytes, launch);
+  const lmop_status st =
+      timed_on(ctx, stream, name, flops, bytes, [&] { return launch(stream); });
   if (before != ctx->device) HIP_OK(ctx, hipSetDevice(before));
   return st;
 }
@@ -1534,6 +1545,8 @@ void lmop_destroy(lmop_ctx* ctx) {
   if (!ctx->host_only) {
     (void)hipSetDevice(ctx->device);
     if (ctx->stream) (void)hipStreamSynchronize(ctx->stream);
+    // operators of a ctx with a stream of its own
+    if (ctx->own_stream) (void)hipStreamSynchronize(nullptr);
   }
   for (lmop_prefix* p : ctx->prefixes) {
     destroy_prefix_storage(p);
@@ -2578,7 +2591,7 @@ lmop_status lmop_quantize(lmop_ctx* ctx, const lmop_quantize_args* a) {
   const double e = (double)a->rows * a->cols;
   return queue_operator(ctx, "quantize", e * (a->gate ? 10 : 4),
                         e * (es * (a->gate ? 2 : 1) + 1) + 4.0 * a->rows * fp8_groups(a->cols),
-                        [&] { return launch_quantize(ctx->stream, *a); });
+                        [&](hipStream_t s) { return launch_quantize(s, *a); });
 }
 
 lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* a) {
@@ -2609,7 +2622,7 @@ lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* a) {
   const double m = a->m, n = a->n, k = a->k;
   return queue_operator(ctx, "matmul_fp8", 2 * m * n * k,
                         m * k + n * k + m * n * (es + (a->add ? 4 : 0)),
-                        [&] { return launch_matmul_fp8(ctx->stream, *a); });
+                        [&](hipStream_t s) { return launch_matmul_fp8(s, *a); });
 }
 
 lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* a) {
@@ -2659,7 +2672,7 @@ lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* a) {
   qa.rope = ctx->rope_tab;
   qa.max_seq = ctx->cfg.max_seq;
   return queue_operator(ctx, "qk_norm_rope", 7 * e, 4 * e,
-                        [&] { return launch_qk_norm_rope(ctx->stream, qa); });
+                        [&](hipStream_t s) { return launch_qk_norm_rope(s, qa); });
 }
 
 lmop_status lmop_set_profiling(lmop_ctx* ctx, int32_t period) {

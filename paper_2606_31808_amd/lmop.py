@@ -643,10 +643,11 @@ class Context:
     def kernel_stats(self):
         return lmop_get_kernel_stats(self.ctx)
 
-    # -- operators: they queue work on the ctx's stream and return
+    # -- operators: they queue work on the ctx's stream (made without one: on the
+    # null stream) and return
     def _here(self, t):
-        """The ctx's device, which t has to be on, and torch's current stream has to be
-        the ctx's (a ctx made without a stream has one that the null stream orders)."""
+        """t has to be on the ctx's device, and torch's current stream has to be the one
+        that the operators run on: the ctx's, or without one the null stream."""
         dev = self.device
         if t.get_device() != dev or (dev < 0 and not t.is_cpu):
             raise ValueError(f"a tensor is on {t.device}, the ctx on device {dev}")

@@ -554,6 +554,25 @@ def test_two_contexts_at_once(L):
             assert torch.equal(c, alone[i])
 
 
+def test_two_contexts_without_streams(L):
+    """Outputs that are freed at once, so that the two ctxs' calls write the same memory in turn."""
+    ctxs = [_ctx(L, 4, 2, 64) for _ in range(2)]
+    m, n, k = 512, 4096, 4096
+    inputs = [(_codes(m, k, i), _scales(m, k // G, i), _codes(n, k, 9 + i), _scales(n // G, k // G, i))
+              for i in range(2)]
+    alone = []
+    for i in range(2):
+        alone.append(ctxs[i].matmul(*inputs[i]).clone())
+        torch.cuda.synchronize()
+    for _ in range(20):
+        ctxs[0].matmul(*inputs[0])
+        ctxs[1].matmul(*inputs[1])
+        c = ctxs[0].matmul(*inputs[0])
+        torch.cuda.synchronize()
+        assert torch.equal(c, alone[0])
+        del c
+
+
 def test_profiled(L):
     ctx = _ctx(L)
     ctx.set_profiling(1)
