@@ -84,6 +84,7 @@ const char* lmop_status_string(lmop_status s);
 /* Formats of the linear maps' weights (lmop_weights.format). */
 #define LMOP_W_INT4_G32 0u /* W4A16: int4 codes, one fp16 scale per 32 input features (Sec. 3.2) */
 #define LMOP_W_FP8_E4M3 1u /* FP8 checkpoints: OCP E4M3 codes, one fp32 scale per output row   */
+#define LMOP_W_FP8_BLOCK 2 /* FP8 checkpoints with block scales, activations in FP8 too         */
 
 /* One linear map y = x W^T with W [n][k].
  * LMOP_W_INT4_G32:
@@ -95,7 +96,14 @@ const char* lmop_status_string(lmop_status s);
  *   qweight uint8 [n][k]: OCP FP8 E4M3 codes (the "fn" variant: largest 448,
  *     no infinities; NaN codes are not allowed);
  *   scales  fp32 [n]: W[r][j] = e4m3(q[r][j]) * scales[r].
- * Activations stay fp16 in both (weight-only quantisation). */
+ * Activations stay fp16 in both (weight-only quantisation).
+ * LMOP_W_FP8_BLOCK:
+ *   qweight uint8 [n][k]: OCP FP8 E4M3 codes, no NaN codes;
+ *   scales  fp32 [ceil(n/128)][ceil(k/128)]:
+ *     W[r][j] = e4m3(q[r][j]) * scales[r/128][j/128].
+ * Every map's input, fp16 per token, is quantised as lmop_quantize does (one
+ * scale per 128 features; w_down's is silu(gate) * up of the fp16 gate and
+ * up) and multiplied as lmop_matmul does. */
 typedef struct {
   const uint8_t* qweight;
   const void* scales;
@@ -119,13 +127,21 @@ typedef struct {
   const lmop_layer* layers;      /* host array [n_layers] (always host memory) */
   int32_t n_layers;
   int32_t on_device; /* 0: the tensor pointers are host memory; 1: device memory on the ctx's device */
-  int32_t format;    /* LMOP_W_INT4_G32 or LMOP_W_FP8_E4M3, for all seven maps of every layer */
+  int32_t format;    /* LMOP_W_INT4_G32, _FP8_E4M3 or _FP8_BLOCK, for all seven maps of every layer */
 } lmop_weights;
 
 /* Copies the weights to the device and repacks them into the kernels'
  * tiled layout (fusing q/k/v and gate/up).  May be called again to replace
  * the weights; existing prefixes are then invalid and are released. */
 lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w);
+
+/* Decoders that normalise queries and keys: RMSNorm (rms_eps) of every query
+ * and key head before the rotation, with a gain per dimension.  q_gain,
+ * k_gain: fp32 [n_layers][head_dim], host memory or (on_device) device memory;
+ * both NULL: no norms, as after lmop_load_weights.  Any weight format.
+ * Existing prefixes are then invalid and are released. */
+lmop_status lmop_load_qk_norms(lmop_ctx* ctx, const float* q_gain, const float* k_gain,
+                               int32_t on_device);
 
 /* Computes and keeps the keys/values of a shared prompt prefix (the
  * instruction part of the LLMMap prompt, Appendix "Prompts").  parent ==

@@ -21,9 +21,13 @@ describe the model; its shape is a Llama-style decoder:
               x += (silu(h2 Wg^T) * (h2 Wu^T)) Wd^T
   z = RMSNorm(x_last) * g_final  W_lm^T
 
-Weights are W4A16 (Sec. 3.2, Table "tab:models"): each linear matrix is
-int4 with one fp16 scale per 32 input features; the oracle multiplies the
-stored code by the stored scale, which is exact in fp32 and fp64.
+Queries and keys are RMS-normalised per head before the rotation where a layer
+has q_norm and k_norm.  Weights are W4A16 (Sec. 3.2, Table "tab:models"): each
+linear matrix is int4 with one fp16 scale per 32 input features; the oracle multiplies the
+stored code by the stored scale, which is exact in fp32 and fp64.  FP8 weights
+come with a scale per row, or with one per 128 x 128 block; with block scales
+every map's input is quantised to FP8 as well (quantize_rows) and the values
+between the maps are fp16, as the checkpoints' runtime format has them.
 
 Precision: float64 by default; float32 on request (the large shapes, where
 fp64 would double the CPU time).  The constrained step and the integer
@@ -119,6 +123,34 @@ def dequant_fp8(codes: np.ndarray, scales: np.ndarray, dtype=np.float64) -> np.n
     assert codes.ndim == 2 and scales.shape == (codes.shape[0],)
     out = decode_e4m3(codes) * scales[:, None]
     return out.astype(dtype)
+
+
+def dequant_fp8_block(codes: np.ndarray, scales: np.ndarray, dtype=np.float64) -> np.ndarray:
+    """W'[n, j] = e4m3(q[n, j]) * s[n // 128, j // 128] (FP8 weights with block scales)."""
+    codes = np.asarray(codes)
+    n, k = codes.shape
+    s = np.asarray(scales, dtype=np.float64)[np.arange(n) // 128][:, np.arange(k) // 128]
+    return (decode_e4m3(codes) * s).astype(dtype)
+
+
+def round_e4m3(y: np.ndarray) -> np.ndarray:
+    """The E4M3 value nearest to y, ties to the even one; |y| at most 448 (more is 448)."""
+    y = np.asarray(y, dtype=np.float64)
+    e = np.floor(np.log2(np.maximum(np.abs(y), 2.0 ** -6)))
+    step = np.exp2(np.maximum(e, -6.0) - 3)
+    return np.clip(np.rint(y / step) * step, -448.0, 448.0)
+
+
+def quantize_rows(x: np.ndarray) -> np.ndarray:
+    """The values of x [T][K] after FP8 quantisation with one scale per row and 128
+    features: s = max(|x| over the group, 2^-40) / 448, value = s * e4m3(x / s)."""
+    t, k = x.shape
+    groups = -(-k // 128)
+    p = np.zeros((t, groups * 128))
+    p[:, :k] = x
+    g = p.reshape(t, groups, 128)
+    s = np.maximum(np.abs(g).max(-1, keepdims=True), 2.0 ** -40) / 448.0
+    return (round_e4m3(g / s) * s).reshape(t, -1)[:, :k].astype(x.dtype)
 
 
 def rms_norm(x: np.ndarray, gamma: np.ndarray, eps: float) -> np.ndarray:
@@ -283,6 +315,7 @@ class OracleLM:
         self.lm_head = _np(weights.lm_head)
         self.final_norm = _np(weights.final_norm)
         self.layers = []
+        self.qk_norms = []  # per layer (query gain, key gain), None without
         for l in weights.layers:
             mats = {}
             for name in ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down"):
@@ -290,6 +323,8 @@ class OracleLM:
                 mats[name] = (_np(m.qweight), _np(m.scales), int(m.n), int(m.k),
                               getattr(m, "fmt", "int4_g32"))
             self.layers.append((_np(l.attn_norm), _np(l.mlp_norm), mats))
+            norms = [getattr(l, n, None) for n in ("q_norm", "k_norm")]
+            self.qk_norms.append([None if g is None else _np(g) for g in norms])
         n_params = sum(m[2] * m[3] for _, _, mats in self.layers for m in mats.values())
         if cache_dequant is None:
             cache_dequant = n_params * self.dtype.itemsize < (4 << 30)
@@ -302,6 +337,7 @@ class OracleLM:
             return self._cache[l]
         g1, g2, mats = self.layers[l]
         w = {name: (dequant_fp8(q, s, self.dtype) if fmt == "fp8_e4m3"
+                    else dequant_fp8_block(q, s, self.dtype) if fmt == "fp8_block"
                     else dequant(q, s, k, self.dtype))
              for name, (q, s, n, k, fmt) in mats.items()}
         out = (g1, g2, w)
@@ -314,6 +350,35 @@ class OracleLM:
             self._head = self.lm_head.astype(self.dtype)
         return self._head
 
+    # -- linear maps ------------------------------------------------------
+    def _block(self, l: int) -> bool:
+        return self.layers[l][2]["wq"][4] == "fp8_block"
+
+    def _half(self, l: int, x: np.ndarray) -> np.ndarray:
+        """With block-scaled maps the values between the maps are fp16."""
+        return x.astype(np.float16).astype(x.dtype) if self._block(l) else x
+
+    def _input(self, l: int, x: np.ndarray) -> np.ndarray:
+        """A map's input: with block-scaled maps fp16, then quantised to FP8."""
+        return quantize_rows(self._half(l, x)) if self._block(l) else x
+
+    def _qkv(self, l: int, h: np.ndarray, w, pos: np.ndarray):
+        """Queries and keys (normalised where the layer has norms, rotated), values."""
+        sh, T = self.shape, len(h)
+        h = self._input(l, h)
+        q = self._half(l, h @ w["wq"].T).reshape(T, sh.n_heads, sh.head_dim)
+        k = self._half(l, h @ w["wk"].T).reshape(T, sh.n_kv_heads, sh.head_dim)
+        v = self._half(l, h @ w["wv"].T).reshape(T, sh.n_kv_heads, sh.head_dim)
+        gq, gk = self.qk_norms[l]
+        if gq is not None:
+            q, k = rms_norm(q, gq, sh.rms_eps), rms_norm(k, gk, sh.rms_eps)
+        return rope(q, pos, sh.rope_theta), rope(k, pos, sh.rope_theta), v
+
+    def _mlp(self, l: int, h: np.ndarray, w) -> np.ndarray:
+        h = self._input(l, h)
+        y = silu(self._half(l, h @ w["w_gate"].T)) * self._half(l, h @ w["w_up"].T)
+        return (quantize_rows(y) if self._block(l) else y) @ w["w_down"].T
+
     # -- plain full forward over one sequence (the definition) ----------
     def forward_sequence(self, tokens: Sequence[int]) -> np.ndarray:
         """Final-layer hidden states [T][d] of one sequence at positions 0..T-1."""
@@ -325,15 +390,11 @@ class OracleLM:
         for l in range(len(self.layers)):
             g1, g2, w = self.layer_weights(l)
             h = rms_norm(x, g1, sh.rms_eps)
-            q = (h @ w["wq"].T).reshape(T, sh.n_heads, sh.head_dim)
-            k = (h @ w["wk"].T).reshape(T, sh.n_kv_heads, sh.head_dim)
-            v = (h @ w["wv"].T).reshape(T, sh.n_kv_heads, sh.head_dim)
-            q = rope(q, pos, sh.rope_theta)
-            k = rope(k, pos, sh.rope_theta)
+            q, k, v = self._qkv(l, h, w, pos)
             o = attention(q, k, v, pos + 1)
-            x = x + o.reshape(T, -1) @ w["wo"].T
+            x = x + self._input(l, o.reshape(T, -1)) @ w["wo"].T
             h2 = rms_norm(x, g2, sh.rms_eps)
-            x = x + (silu(h2 @ w["w_gate"].T) * (h2 @ w["w_up"].T)) @ w["w_down"].T
+            x = x + self._mlp(l, h2, w)
         return x
 
     def logits(self, x_last: np.ndarray) -> np.ndarray:
@@ -361,9 +422,7 @@ class OracleLM:
         for l in range(len(self.layers)):
             g1, g2, w = self.layer_weights(l)
             h = rms_norm(x, g1, sh.rms_eps)
-            q = rope((h @ w["wq"].T).reshape(T, sh.n_heads, sh.head_dim), pos, sh.rope_theta)
-            k = rope((h @ w["wk"].T).reshape(T, sh.n_kv_heads, sh.head_dim), pos, sh.rope_theta)
-            v = (h @ w["wv"].T).reshape(T, sh.n_kv_heads, sh.head_dim)
+            q, k, v = self._qkv(l, h, w, pos)
             for i, nd in enumerate(nodes):
                 nd.k.append(k[cuts[i]:cuts[i + 1]])
                 nd.v.append(v[cuts[i]:cuts[i + 1]])
@@ -375,9 +434,9 @@ class OracleLM:
                 past = nd.start
                 o[cuts[i]:cuts[i + 1]] = attention(q[cuts[i]:cuts[i + 1]], kk, vv,
                                                    past + np.arange(nd.n) + 1)
-            x = x + o.reshape(T, -1) @ w["wo"].T
+            x = x + self._input(l, o.reshape(T, -1)) @ w["wo"].T
             h2 = rms_norm(x, g2, sh.rms_eps)
-            x = x + (silu(h2 @ w["w_gate"].T) * (h2 @ w["w_up"].T)) @ w["w_down"].T
+            x = x + self._mlp(l, h2, w)
         for i, nd in enumerate(nodes):
             nd.x_last = x[cuts[i + 1] - 1].copy()
 

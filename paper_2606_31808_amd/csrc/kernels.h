@@ -195,6 +195,7 @@ struct QkArgs {
   float eps;
   const float2* rope;  // [max_seq][hd/2] (cos, sin)
   int max_seq;
+  bool k_in_slots;     // token t's key is at row slot[t] of t.k (in place: t.k == t.k_out)
 };
 hipError_t launch_qk_norm_rope(hipStream_t s, const QkArgs& a);
 

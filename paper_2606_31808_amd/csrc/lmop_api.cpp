@@ -58,10 +58,25 @@ int64_t round_up64(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 // once (bind_static_scratch) and passes that address to the kernels.
 static __device__ __align__(256) char scratch[kNoAllocScratchBytes];
 
+// A linear map with block-scaled FP8 weights: rows of codes, ld bytes apart
+// (zero past the k-th), and a scale per 128 x 128 block.  Of several source
+// maps in one, each starts at a multiple of 128 rows; the rows between are zero.
+struct BlockW {
+  uint8_t* q = nullptr;
+  float* s = nullptr;
+  int n = 0, k = 0;
+  int64_t ld = 0, lds = 0;
+};
+
 struct LayerW {
   float* attn_norm = nullptr;
   float* mlp_norm = nullptr;
   PackedW qkv, o, gu, down;
+  // LMOP_W_FP8_BLOCK: instead of the packed maps
+  BlockW bqkv, bo, bgu, bdown;
+  // query and key norms of this layer, or NULL (part of the ctx's qk_gain)
+  const float* q_gain = nullptr;
+  const float* k_gain = nullptr;
 };
 
 struct Stat {
@@ -133,6 +148,10 @@ struct lmop_ctx {
   std::vector<LayerW> layers;
   std::vector<void*> weight_allocs;
   float2* rope_tab = nullptr;
+  // lmop_load_qk_norms: the layers' gains, and a rotation by nothing for the
+  // QKV epilogue of the packed formats (the norms come before the rotation)
+  float* qk_gain = nullptr;
+  float2* no_rope = nullptr;
 
   // library-allocated scratch: named grow-only buffers
   std::map<std::string, std::pair<void*, size_t>> ws;
@@ -612,6 +631,52 @@ void free_weights(lmop_ctx* c) {
   c->layers.clear();
   c->emb = c->head = nullptr;
   c->final_norm = nullptr;
+  (void)dev_free(c, c->qk_gain);
+  (void)dev_free(c, c->no_rope);
+  c->qk_gain = nullptr;
+  c->no_rope = nullptr;
+}
+
+bool block_format(const lmop_ctx* c) { return c->wfmt == LMOP_W_FP8_BLOCK; }
+// columns of a fused block-scaled map: every part starts at a block
+int blocks_of(int n) { return (n + 127) / 128; }
+int qkv_width(const lmop_ctx* c) {
+  return 128 * (blocks_of(c->nq_dim) + 2 * blocks_of(c->nkv_dim));
+}
+int gu_width(const lmop_ctx* c) { return 256 * blocks_of(c->cfg.d_ff); }
+
+// Copies block-scaled source maps (the same k) into one.
+lmop_status load_blocks(lmop_ctx* c, const lmop_qmat* const* srcs, int n_src, bool on_device,
+                        BlockW* out) {
+  BlockW w;
+  w.k = srcs[0]->k;
+  w.ld = round_up(w.k, 16);
+  w.lds = blocks_of(w.k);
+  for (int i = 0; i < n_src; ++i) w.n += 128 * blocks_of(srcs[i]->n);
+  if (n_src == 1) w.n = srcs[0]->n;
+  void *q = nullptr, *sc = nullptr;
+  const size_t bytes = (size_t)w.n * w.ld, sbytes = (size_t)blocks_of(w.n) * w.lds * 4;
+  LMOP_TRY(dev_alloc(c, &q, bytes));
+  c->weight_allocs.push_back(q);
+  LMOP_TRY(dev_alloc(c, &sc, sbytes));
+  c->weight_allocs.push_back(sc);
+  HIP_OK(c, launch_fill_u32(c->stream, q, bytes / 4, 0u));
+  const hipMemcpyKind kind = on_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice;
+  size_t row = 0, block = 0;
+  for (int i = 0; i < n_src; ++i) {
+    const lmop_qmat& m = *srcs[i];
+    const size_t nb = blocks_of(m.n);
+    HIP_OK(c, hipMemcpy2DAsync((uint8_t*)q + row * w.ld, w.ld, m.qweight, m.k, m.k, m.n, kind,
+                               c->stream));
+    HIP_OK(c, hipMemcpyAsync((float*)sc + block * w.lds, m.scales, nb * w.lds * 4, kind,
+                             c->stream));
+    row += 128 * nb;
+    block += nb;
+  }
+  w.q = (uint8_t*)q;
+  w.s = (float*)sc;
+  *out = w;
+  return LMOP_OK;
 }
 
 // Packs up to three source matrices (rows = output columns) into one tiled
@@ -750,10 +815,12 @@ hipError_t launch_gemm_packed(const lmop_ctx* c, GemmArgs& ga, const PackedW& W,
 const char* gemm_name(const lmop_ctx* c, const char* proj, bool decode = false) {
   static thread_local std::string n;
   n = std::string(decode ? "decode_" : "") +
-      (c->wfmt == LMOP_W_FP8_E4M3 ? "gemm_w8a16_" : "gemm_w4a16_") + proj;
+      (block_format(c) ? "matmul_fp8_"
+       : c->wfmt == LMOP_W_FP8_E4M3 ? "gemm_w8a16_" : "gemm_w4a16_") + proj;
   return n.c_str();
 }
 double weight_bytes(const lmop_ctx* c, double n, double k) {
+  if (block_format(c)) return n * k * (1 + 4.0 / (128 * 128));
   return c->wfmt == LMOP_W_FP8_E4M3 ? n * k + n * 4 : n * k * 0.5625;
 }
 
@@ -809,7 +876,15 @@ std::vector<std::pair<const char*, size_t>> scratch_items(const lmop_ctx* c, con
   add("h", T * d * 2);
   add("q", T * c->nq_dim * 2);
   add("att", T * c->nq_dim * 2);
-  add("act", T * c->f64 * 2);
+  if (block_format(c)) {
+    // the widest operand of a map, quantised, and the widest fused result
+    const size_t k = std::max({(size_t)c->cfg.d_model, (size_t)c->nq_dim, (size_t)c->cfg.d_ff});
+    add("codes", T * ((k + 15) / 16 * 16));
+    add("code_scales", T * blocks_of((int)k) * 4);
+    add("wide", T * std::max(qkv_width(c), gu_width(c)) * 2);
+  } else {
+    add("act", T * c->f64 * 2);
+  }
   add("xlast", n.last * d * 4);
   add("own_kv", n.own_kv);
   if (n.head_rows > 0) {
@@ -1011,8 +1086,9 @@ constexpr int kQuerySplitTokens = 256;
 // computes Q and attention for those only.  Their normalised rows wait in
 // "act", which a narrow MLP (d_ff below d_model * n_last / T) makes too small;
 // such a pass takes the whole projection rather than more scratch.
+// Block-scaled maps do not split (their QKV result is one tensor).
 bool query_split(const lmop_ctx* c, int T, int n_last) {
-  return n_last > 0 && T - n_last >= kQuerySplitTokens &&
+  return !block_format(c) && n_last > 0 && T - n_last >= kQuerySplitTokens &&
          (size_t)n_last * c->cfg.d_model <= (size_t)T * c->f64;
 }
 
@@ -1028,7 +1104,74 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
   LMOP_TRY(ws_get(c, "h", (size_t)T * d, &h));
   LMOP_TRY(ws_get(c, "q", (size_t)T * c->nq_dim, &q));
   LMOP_TRY(ws_get(c, "att", (size_t)T * c->nq_dim, &att));
-  LMOP_TRY(ws_get(c, "act", (size_t)T * c->f64, &act));
+  const bool blocks = block_format(c);
+  uint8_t* codes = nullptr;
+  float* code_scales = nullptr;
+  uint16_t* wide = nullptr;
+  if (blocks) {
+    const size_t k = std::max({d, c->nq_dim, cf.d_ff});
+    LMOP_TRY(ws_get(c, "codes", (size_t)T * ((k + 15) / 16 * 16), &codes));
+    LMOP_TRY(ws_get(c, "code_scales", (size_t)T * blocks_of((int)k), &code_scales));
+    LMOP_TRY(ws_get(c, "wide", (size_t)T * std::max(qkv_width(c), gu_width(c)), &wide));
+  } else {
+    LMOP_TRY(ws_get(c, "act", (size_t)T * c->f64, &act));
+  }
+  // Block-scaled maps: rows of fp16 (or silu(gate) * x of them) to codes, and
+  // codes through a map, the result fp16 in `wide` or added to the fp32 rows `x32`.
+  auto quantize = [&](const uint16_t* in, int64_t ld, const uint16_t* gate, int rows, int cols) {
+    lmop_quantize_args a{};
+    a.x = in;
+    a.gate = gate;
+    a.q = codes;
+    a.scale = code_scales;
+    a.ldx = a.ldg = ld;
+    a.ldq = round_up(cols, 16);
+    a.lds = blocks_of(cols);
+    a.rows = rows;
+    a.cols = cols;
+    a.dtype = LMOP_F16;
+    const double e = (double)rows * cols;
+    return timed(c, b.decode ? "decode_quantize" : "quantize", e * (gate ? 10 : 4),
+                 e * (gate ? 5 : 3), [&] { return launch_quantize(c->stream, a); });
+  };
+  auto block_map = [&](const char* name, const BlockW& W, int rows, float* x32) {
+    lmop_matmul_args a{};
+    a.a = codes;
+    a.a_scale = code_scales;
+    a.b = W.q;
+    a.b_scale = W.s;
+    a.add = x32;
+    a.c = x32 ? (void*)x32 : (void*)wide;
+    a.lda = a.ldb = W.ld;
+    a.ldas = a.ldbs = W.lds;
+    a.ldadd = a.ldc = W.n;
+    a.m = rows;
+    a.n = W.n;
+    a.k = W.k;
+    a.dtype = x32 ? LMOP_F32 : LMOP_F16;
+    return timed(c, gemm_name(c, name, b.decode), 2.0 * rows * W.n * W.k,
+                 (double)rows * W.k + weight_bytes(c, W.n, W.k) + (double)rows * W.n * (x32 ? 8 : 2),
+                 [&] { return launch_matmul_fp8(c->stream, a); });
+  };
+  // norms (where loaded) and rotation of queries and keys; args: what the
+  // tensors are
+  auto norm_rope = [&](const LayerW& L, QkArgs a) {
+    a.t.q_gain = L.q_gain;
+    a.t.k_gain = L.k_gain;
+    a.t.n_slots = b.own_cap;
+    a.t.v_layout = LMOP_V_COLUMNS;
+    a.t.dtype = LMOP_F16;
+    a.nq = cf.n_heads;
+    a.nkv = cf.n_kv_heads;
+    a.hd = hd;
+    a.eps = cf.rms_eps;
+    a.rope = c->rope_tab;
+    a.max_seq = cf.max_seq;
+    const double e = (double)a.t.n_tokens * ((a.t.q ? c->nq_dim : 0) + (a.t.k ? c->nkv_dim : 0) +
+                                             (a.t.v ? c->nkv_dim : 0));
+    return timed(c, b.decode ? "decode_qk_norm_rope" : "qk_norm_rope", 7 * e, 4 * e,
+                 [&] { return launch_qk_norm_rope(c->stream, a); });
+  };
 
   LMOP_TRY(timed(c, "embed", 0, (double)T * d * 6, [&] {
     return launch_embed(c->stream, b.tok, T, c->emb, d, x);
@@ -1066,7 +1209,8 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
       ga.K = L.qkv.kp;
       ga.pos = pos;
       ga.slot = b.slot;
-      ga.rope = c->rope_tab;
+      // query and key norms come before the rotation, in a pass of their own
+      ga.rope = L.q_gain ? c->no_rope : c->rope_tab;
       ga.qout = q;
       ga.kc = kc;
       ga.vt = vt;
@@ -1083,7 +1227,26 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
       return timed(c, gemm_name(c, "qkv", b.decode), flops, bytes,
                    [&] { return launch_gemm_packed(c, ga, L.qkv, EPI_QKV, c0); });
     };
-    if (split_q) {
+    if (blocks) {
+      LMOP_TRY(quantize(h, d, nullptr, T, d));
+      LMOP_TRY(block_map("qkv", L.bqkv, T, nullptr));
+      const int wq = 128 * blocks_of(c->nq_dim), wkv = 128 * blocks_of(c->nkv_dim);
+      QkArgs a{};
+      a.t.q = wide;
+      a.t.k = wide + wq;
+      a.t.v = wide + wq + wkv;
+      a.t.ldq = a.t.ldk = a.t.ldv = L.bqkv.n;
+      a.t.q_out = q;
+      a.t.ldqo = c->nq_dim;
+      a.t.k_out = kc;
+      a.t.ldko = c->nkv_dim;
+      a.t.v_out = vt;
+      a.t.ldvo = b.own_cap;
+      a.t.pos = b.pos;
+      a.t.slot = b.slot;
+      a.t.n_tokens = T;
+      LMOP_TRY(norm_rope(L, a));
+    } else if (split_q) {
       // from the last multiple of 256 columns: where Q does not end at one, the
       // few Q columns before K are written here too, and again by the next launch
       LMOP_TRY(qkv(h, T, b.pos, c->nq_dim / 256 * 256, L.qkv.n));
@@ -1093,6 +1256,23 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
       LMOP_TRY(qkv(act, M, b.pos_last, 0, c->nq_dim));
     } else {
       LMOP_TRY(qkv(h, T, b.pos, 0, L.qkv.n));
+    }
+    if (!blocks && L.q_gain) {
+      // in place: the queries that were computed, every token's key in its slot
+      QkArgs a{};
+      a.t.q = a.t.q_out = q;
+      a.t.ldq = a.t.ldqo = c->nq_dim;
+      a.t.n_tokens = split_q ? M : T;
+      a.t.pos = split_q ? b.pos_last : b.pos;
+      LMOP_TRY(norm_rope(L, a));
+      QkArgs k{};
+      k.t.k = k.t.k_out = kc;
+      k.t.ldk = k.t.ldko = c->nkv_dim;
+      k.t.n_tokens = T;
+      k.t.pos = b.pos;
+      k.t.slot = b.slot;
+      k.k_in_slots = true;
+      LMOP_TRY(norm_rope(L, k));
     }
     AttnArgs aa{};
     aa.q = q;
@@ -1140,10 +1320,22 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
       return timed(c, gemm_name(c, name, b.decode), flops, bytes,
                    [&] { return launch_gemm_packed(c, ga, W, epi); });
     };
-    LMOP_TRY(gemm2("o", ar, c->nq_dim, L.o, EPI_ADD_F32, nullptr, 0, d));
+    if (blocks) {
+      LMOP_TRY(quantize(ar, c->nq_dim, nullptr, M, c->nq_dim));
+      LMOP_TRY(block_map("o", L.bo, M, xr));
+    } else {
+      LMOP_TRY(gemm2("o", ar, c->nq_dim, L.o, EPI_ADD_F32, nullptr, 0, d));
+    }
     LMOP_TRY(timed(c, b.decode ? "decode_rmsnorm" : "rmsnorm", 0, (double)M * d * 6, [&] {
       return launch_rmsnorm(c->stream, xr, d, nullptr, M, L.mlp_norm, d, cf.rms_eps, h, d);
     }));
+    if (blocks) {
+      LMOP_TRY(quantize(h, d, nullptr, M, d));
+      LMOP_TRY(block_map("gateup", L.bgu, M, nullptr));
+      LMOP_TRY(quantize(wide + gu_width(c) / 2, L.bgu.n, wide, M, cf.d_ff));
+      LMOP_TRY(block_map("down", L.bdown, M, xr));
+      continue;
+    }
     LMOP_TRY(gemm2("gateup", h, d, L.gu, EPI_SWIGLU, act, c->f64, c->f64));
     LMOP_TRY(gemm2("down", act, c->f64, L.down, EPI_ADD_F32, nullptr, 0, d));
   }
@@ -1598,7 +1790,8 @@ lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w) {
                 cf.n_layers);
   if (!w->tok_embedding || !w->lm_head || !w->final_norm || (cf.n_layers > 0 && !w->layers))
     return fail(ctx, LMOP_ERR_INVALID_ARG, "NULL embedding, head, final norm or layer array");
-  if (w->format != (int32_t)LMOP_W_INT4_G32 && w->format != (int32_t)LMOP_W_FP8_E4M3)
+  if (w->format != (int32_t)LMOP_W_INT4_G32 && w->format != (int32_t)LMOP_W_FP8_E4M3 &&
+      w->format != (int32_t)LMOP_W_FP8_BLOCK)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown weight format %d", w->format);
   const int d = cf.d_model, nq = ctx->nq_dim, nkv = ctx->nkv_dim, F = cf.d_ff;
   for (int l = 0; l < cf.n_layers; ++l) {
@@ -1616,6 +1809,7 @@ lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w) {
   if (ctx->host_only) {
     release_all_prefixes(ctx);
     ctx->generation++;
+    ctx->wfmt = (uint32_t)w->format;
     ctx->loaded = true;
     return LMOP_OK;
   }
@@ -1661,6 +1855,15 @@ lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w) {
     D.attn_norm = (float*)p;
     LMOP_TRY(upload(ctx, L.mlp_norm, (size_t)d * 4, od, &p));
     D.mlp_norm = (float*)p;
+    if (block_format(ctx)) {
+      const lmop_qmat *qkv[3] = {&L.wq, &L.wk, &L.wv}, *gu[2] = {&L.w_gate, &L.w_up};
+      const lmop_qmat *o = &L.wo, *down = &L.w_down;
+      LMOP_TRY(load_blocks(ctx, qkv, 3, od, &D.bqkv));
+      LMOP_TRY(load_blocks(ctx, &o, 1, od, &D.bo));
+      LMOP_TRY(load_blocks(ctx, gu, 2, od, &D.bgu));
+      LMOP_TRY(load_blocks(ctx, &down, 1, od, &D.bdown));
+      continue;
+    }
     {  // fused q | k | v; q and k columns ordered so rotation pairs share a lane
       const lmop_qmat* s[3] = {&L.wq, &L.wk, &L.wv};
       std::vector<int32_t> m(round_up(ctx->qkv_n, 256), -1);
@@ -1705,6 +1908,44 @@ lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w) {
   }
   LMOP_TRY(sync(ctx));
   ctx->loaded = true;
+  return LMOP_OK;
+}
+
+lmop_status lmop_load_qk_norms(lmop_ctx* ctx, const float* q_gain, const float* k_gain,
+                               int32_t on_device) {
+  LMOP_TRY(enter(ctx));
+  if (!ctx->loaded) return fail(ctx, LMOP_ERR_STATE, "lmop_load_weights has not succeeded");
+  if ((q_gain == nullptr) != (k_gain == nullptr))
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "query and key norms come together");
+  const lmop_config& cf = ctx->cfg;
+  if (!ctx->host_only) HIP_OK(ctx, hipStreamSynchronize(ctx->stream));
+  release_all_prefixes(ctx);
+  ctx->generation++;
+  if (ctx->host_only) return LMOP_OK;
+  for (LayerW& L : ctx->layers) L.q_gain = L.k_gain = nullptr;
+  if (!q_gain || cf.n_layers == 0) return LMOP_OK;
+  const size_t n = (size_t)cf.n_layers * cf.head_dim;
+  void* p = nullptr;
+  if (!ctx->qk_gain) {
+    LMOP_TRY(dev_alloc(ctx, &p, 2 * n * 4));
+    ctx->qk_gain = (float*)p;
+  }
+  if (!ctx->no_rope && !block_format(ctx)) {
+    const std::vector<float2> one((size_t)cf.max_seq * (cf.head_dim / 2), make_float2(1.f, 0.f));
+    LMOP_TRY(dev_alloc(ctx, &p, one.size() * sizeof(float2)));
+    ctx->no_rope = (float2*)p;
+    HIP_OK(ctx, hipMemcpyAsync(p, one.data(), one.size() * sizeof(float2), hipMemcpyHostToDevice,
+                               ctx->stream));
+    HIP_OK(ctx, hipStreamSynchronize(ctx->stream));
+  }
+  const hipMemcpyKind kind = on_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice;
+  HIP_OK(ctx, hipMemcpyAsync(ctx->qk_gain, q_gain, n * 4, kind, ctx->stream));
+  HIP_OK(ctx, hipMemcpyAsync(ctx->qk_gain + n, k_gain, n * 4, kind, ctx->stream));
+  LMOP_TRY(sync(ctx));
+  for (int l = 0; l < cf.n_layers; ++l) {
+    ctx->layers[l].q_gain = ctx->qk_gain + (size_t)l * cf.head_dim;
+    ctx->layers[l].k_gain = ctx->qk_gain + n + (size_t)l * cf.head_dim;
+  }
   return LMOP_OK;
 }
 

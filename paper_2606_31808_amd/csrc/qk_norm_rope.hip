@@ -145,7 +145,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const QkArgs 
       const int sec = h < a.nq ? 0 : h < a.nq + a.nkv ? 1 : 2;
       const int hs = h - (sec == 0 ? 0 : sec == 1 ? a.nq : a.nq + a.nkv);
       const T* in = sec == 0 ? (const T*)p.q + t * p.ldq
-                    : sec == 1 ? (const T*)p.k + t * p.ldk
+                    : sec == 1 ? (const T*)p.k + (a.k_in_slots ? slot : t) * p.ldk
                                : (const T*)p.v + t * p.ldv;
       T* out = sec == 0 ? (T*)p.q_out + t * p.ldqo
                : sec == 1 ? (T*)p.k_out + slot * p.ldko

@@ -22,8 +22,9 @@ LIB_PATH = os.path.join(_HERE, "_lib", "liblmop.so")
 LMOP_OK, LMOP_ERR_INVALID_ARG, LMOP_ERR_STATE, LMOP_ERR_OOM, LMOP_ERR_DEVICE, \
     LMOP_ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 LMOP_BOOL, LMOP_ENUM, LMOP_INT, LMOP_AUTOMATON = 0, 1, 2, 3
-LMOP_W_INT4_G32, LMOP_W_FP8_E4M3 = 0, 1
-_WEIGHT_FORMATS = {"int4_g32": LMOP_W_INT4_G32, "fp8_e4m3": LMOP_W_FP8_E4M3}
+LMOP_W_INT4_G32, LMOP_W_FP8_E4M3, LMOP_W_FP8_BLOCK = 0, 1, 2
+_WEIGHT_FORMATS = {"int4_g32": LMOP_W_INT4_G32, "fp8_e4m3": LMOP_W_FP8_E4M3,
+                   "fp8_block": LMOP_W_FP8_BLOCK}
 LMOP_NO_DEDUP = 1
 LMOP_HEAD_RESTRICTED = 2
 
@@ -32,7 +33,7 @@ EXPORTED = (
     "lmop_set_prefix", "lmop_set_prefixes", "lmop_release_prefix", "lmop_prefix_length", "lmop_eval_rows",
     "lmop_dedup_rows", "lmop_set_profiling", "lmop_get_kernel_stats", "lmop_set_workspace",
     "lmop_get_memory", "lmop_eval_rows_noalloc", "lmop_plan_rows", "lmop_quantize", "lmop_matmul",
-    "lmop_qk_norm_rope",
+    "lmop_qk_norm_rope", "lmop_load_qk_norms",
 )
 LMOP_F16, LMOP_BF16, LMOP_F32 = 0, 1, 2
 LMOP_FP8_GROUP = 128
@@ -170,6 +171,7 @@ def _load():
         "lmop_set_profiling": (st, [vp, i32]),
         "lmop_get_kernel_stats": (st, [vp, C.POINTER(lmop_kernel_stat), i32,
                                        C.POINTER(C.c_int32)]),
+        "lmop_load_qk_norms": (st, [vp, vp, vp, i32]),
         "lmop_quantize": (st, [vp, vp]),
         "lmop_matmul": (st, [vp, vp]),
         "lmop_qk_norm_rope": (st, [vp, vp]),
@@ -234,7 +236,8 @@ def _tensor_ptr(t, keep):
 def lmop_load_weights(ctx, weights) -> None:
     """weights: object with tok_embedding, lm_head (fp16 [V][d]), final_norm, layers[...]
     (attn_norm, mlp_norm, wq .. w_down each with qweight/scales/n/k and a format name
-    `fmt`, "int4_g32" (default) or "fp8_e4m3"), all on one device."""
+    `fmt`, "int4_g32" (default), "fp8_e4m3" or "fp8_block"), all on one device.  Layers
+    with q_norm and k_norm (fp32 [head_dim]) have these loaded too."""
     keep = []
     where = set()
 
@@ -262,6 +265,27 @@ def lmop_load_weights(ctx, weights) -> None:
         raise ValueError("weights must all be on the host or all on the device")
     w.on_device = 1 if where.pop() else 0
     _check(_lib.lmop_load_weights(ctx, C.byref(w)), ctx)
+    norms = [(getattr(l, "q_norm", None), getattr(l, "k_norm", None)) for l in weights.layers]
+    if any(n is not None for pair in norms for n in pair):
+        if any(n is None for pair in norms for n in pair):
+            raise ValueError("query and key norms: in every layer, or in none")
+        lmop_load_qk_norms(ctx, *(torch.stack([torch.as_tensor(pair[i]) for pair in norms])
+                                  for i in (0, 1)))
+
+
+def lmop_load_qk_norms(ctx, q_gain=None, k_gain=None) -> None:
+    """Query and key norms, fp32 [n_layers, head_dim] (both None: no norms)."""
+    keep, where, at = [], set(), []
+    for g in (q_gain, k_gain):
+        if g is None:
+            at.append(None)
+            continue
+        a, dev = _tensor_ptr(torch.as_tensor(g, dtype=torch.float32), keep)
+        at.append(a)
+        where.add(dev)
+    if len(where) > 1:
+        raise ValueError("query and key norms must both be on the host or on the device")
+    _check(_lib.lmop_load_qk_norms(ctx, at[0], at[1], 1 if where == {True} else 0), ctx)
 
 
 def lmop_set_prefix(ctx, tokens, parent=None):
@@ -586,6 +610,7 @@ class Context:
             cfg.n_layers = n_layers
         self.vocab = shape.vocab
         self.heads = (cfg.n_heads, cfg.n_kv_heads, cfg.head_dim)
+        self.n_layers = cfg.n_layers
         # where the operators' tensors live (-1: the host), and the torch stream
         # they are ordered on
         self.device = max(int(device), -1)
@@ -605,6 +630,13 @@ class Context:
 
     def load_weights(self, weights):
         lmop_load_weights(self.ctx, weights)
+
+    def load_qk_norms(self, q_gain=None, k_gain=None):
+        for g in (q_gain, k_gain):
+            if g is not None and tuple(g.shape) != (self.n_layers, self.heads[2]):
+                raise ValueError(f"a norm of shape {tuple(g.shape)}, expected "
+                                 f"({self.n_layers}, {self.heads[2]})")
+        lmop_load_qk_norms(self.ctx, q_gain, k_gain)
 
     def set_prefix(self, tokens, parent=None):
         return lmop_set_prefix(self.ctx, tokens, parent)

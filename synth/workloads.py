@@ -59,8 +59,9 @@ SHAPES = {
 
 @dataclasses.dataclass
 class QMat:
-    qweight: torch.Tensor  # int4_g32: uint8 [N][Kp/2]; fp8_e4m3: uint8 codes [N][K]
-    scales: torch.Tensor   # int4_g32: float16 [N][Kp/32]; fp8_e4m3: float32 [N]
+    qweight: torch.Tensor  # int4_g32: uint8 [N][Kp/2]; fp8_e4m3, fp8_block: uint8 codes [N][K]
+    scales: torch.Tensor   # int4_g32: float16 [N][Kp/32]; fp8_e4m3: float32 [N];
+                           # fp8_block: float32 [ceil(N/128)][ceil(K/128)]
     n: int
     k: int
     fmt: str = "int4_g32"
@@ -77,6 +78,8 @@ class Layer:
     w_gate: QMat
     w_up: QMat
     w_down: QMat
+    q_norm: Optional[torch.Tensor] = None  # float32 [head_dim]
+    k_norm: Optional[torch.Tensor] = None
 
 
 @dataclasses.dataclass
@@ -90,8 +93,11 @@ class Weights:
     def to(self, device) -> "Weights":
         def qm(m: QMat) -> QMat:
             return QMat(m.qweight.to(device), m.scales.to(device), m.n, m.k, m.fmt)
+        def opt(t):
+            return None if t is None else t.to(device)
         layers = [Layer(l.attn_norm.to(device), l.mlp_norm.to(device), qm(l.wq), qm(l.wk),
-                        qm(l.wv), qm(l.wo), qm(l.w_gate), qm(l.w_up), qm(l.w_down))
+                        qm(l.wv), qm(l.wo), qm(l.w_gate), qm(l.w_up), qm(l.w_down),
+                        opt(l.q_norm), opt(l.k_norm))
                   for l in self.layers]
         return Weights(self.shape, self.tok_embedding.to(device), self.lm_head.to(device),
                        self.final_norm.to(device), layers)
@@ -142,10 +148,28 @@ def quantize_fp8_e4m3(w: torch.Tensor):
     return q.view(torch.uint8).contiguous(), s.float().contiguous()
 
 
+def quantize_fp8_block(w: torch.Tensor):
+    """FP8 (OCP e4m3) with one fp32 scale per block of 128 x 128.
+
+    Input generation: s = max|w| / 448 per block (1 if that is 0), q = e4m3(w / s
+    clamped to +-448).  Returns (codes uint8 [N][K], scales float32
+    [ceil(N/128)][ceil(K/128)])."""
+    n, k = w.shape
+    p = torch.nn.functional.pad(w, (0, -k % 128, 0, -n % 128))
+    b = p.reshape(p.shape[0] // 128, 128, p.shape[1] // 128, 128)
+    s = b.abs().amax((1, 3)) / 448.0
+    s = torch.where(s == 0, torch.ones_like(s), s)
+    q = (b / s[:, None, :, None]).clamp_(-448.0, 448.0).reshape(p.shape)[:n, :k]
+    return q.to(torch.float8_e4m3fn).view(torch.uint8).contiguous(), s.float().contiguous()
+
+
 def make_weights(shape: ModelShape, seed: int = 1234, device="cpu", std: float = 0.02,
-                 n_layers: Optional[int] = None, fmt: str = "int4_g32") -> Weights:
+                 n_layers: Optional[int] = None, fmt: str = "int4_g32",
+                 qk_norm: bool = False) -> Weights:
     """Random-init weights of `shape`, linear layers quantised to int4 g32
-    (fmt "int4_g32") or to FP8 e4m3 with per-channel scales ("fp8_e4m3").
+    (fmt "int4_g32"), to FP8 e4m3 with per-channel scales ("fp8_e4m3") or with
+    128 x 128 block scales ("fp8_block"); qk_norm adds query and key norms,
+    gains 1 + N(0, 0.2).
 
     Each tensor has its own stream keyed by (seed, shape, layer, tensor), so a
     model with fewer layers is a prefix of the full one.
@@ -160,6 +184,8 @@ def make_weights(shape: ModelShape, seed: int = 1234, device="cpu", std: float =
         w = _normal((n, k), std, _seed(seed, sid, layer, tid), dev)
         if fmt == "fp8_e4m3":
             qw, sc = quantize_fp8_e4m3(w)
+        elif fmt == "fp8_block":
+            qw, sc = quantize_fp8_block(w)
         else:
             qw, sc = quantize_int4_g32(w)
         del w
@@ -174,7 +200,9 @@ def make_weights(shape: ModelShape, seed: int = 1234, device="cpu", std: float =
             attn_norm=ones.clone(), mlp_norm=ones.clone(),
             wq=qmat(l, 0, nq, d), wk=qmat(l, 1, nkv, d), wv=qmat(l, 2, nkv, d),
             wo=qmat(l, 3, d, nq), w_gate=qmat(l, 4, f, d), w_up=qmat(l, 5, f, d),
-            w_down=qmat(l, 6, d, f)))
+            w_down=qmat(l, 6, d, f),
+            **({n: 1 + _normal((hd,), 0.2, _seed(seed, sid, l, t), dev)
+                for n, t in (("q_norm", 7), ("k_norm", 8))} if qk_norm else {})))
     return Weights(shape, emb, head, ones.clone(), layers)
 
 

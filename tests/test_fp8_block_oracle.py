@@ -1,0 +1,130 @@
+"""The oracle's block-scaled FP8 maps and query/key norms against brute force, and
+the host checks of the calls that load them."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import OracleLM
+from oracle.lmop_oracle import (KIND_ENUM, dequant_fp8_block, quantize_rows, rms_norm, round_e4m3)
+from paper_2606_31808_amd import lmop as L
+from synth import SHAPES, ModelShape, make_weights, quantize_fp8_block
+
+TINY = SHAPES["tiny"]
+MICRO = ModelShape("micro", 2, 64, 4, 2, 16, 96, 64, 1e4)
+
+
+def test_round_e4m3_matches_torch():
+    y = torch.cat([torch.linspace(-448, 448, 20001, dtype=torch.float64),
+                   torch.logspace(-12, 2, 4001, base=2, dtype=torch.float64),
+                   torch.tensor([0.0, 2.0 ** -10, 3 * 2.0 ** -10, 17.0, 19.0, -17.0], dtype=torch.float64)])
+    y = y.float()
+    want = y.to(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(round_e4m3(y.double().numpy()), want)
+
+
+def test_quantize_rows_by_hand():
+    x = np.zeros((2, 200))
+    x[0, :128] = np.arange(128) - 64.0
+    x[0, 128:] = 1e-3
+    x[1, 130] = -7.0
+    got = quantize_rows(x)
+    for r in range(2):
+        for g in (slice(0, 128), slice(128, 200)):
+            s = max(np.abs(x[r, g]).max(), 2.0 ** -40) / 448
+            want = torch.from_numpy((x[r, g] / s).astype(np.float32)).to(torch.float8_e4m3fn).double()
+            assert np.allclose(got[r, g], want.numpy() * s, rtol=1e-12, atol=0)
+    # a step of E4M3 is an eighth of a power of two: half of it off at most
+    assert np.all(np.abs(got - x) <= np.abs(x) / 16 + 1e-12 + 64 / 448 * 2.0 ** -10)
+
+
+def test_block_weights():
+    w = torch.randn(200, 300, generator=torch.Generator().manual_seed(1))
+    w[:128, 128:256] = 0
+    q, s = quantize_fp8_block(w)
+    assert q.shape == (200, 300) and s.shape == (2, 3) and s[0, 1] == 1
+    deq = dequant_fp8_block(q.numpy(), s.numpy())
+    for i in range(2):
+        for j in range(3):
+            b = (slice(128 * i, 128 * i + 128), slice(128 * j, 128 * j + 128))
+            v = q[b].view(torch.float8_e4m3fn).double().numpy() * float(s[i, j])
+            assert np.array_equal(deq[b], v)
+            assert np.abs(deq[b] - w[b].double().numpy()).max() <= float(w[b].abs().max()) / 16 + 1e-12
+
+
+@pytest.mark.parametrize("fmt,norm", [("fp8_block", False), ("fp8_block", True), ("int4_g32", True)])
+def test_model_prefix_cached_equals_full_forward(fmt, norm):
+    w = make_weights(MICRO, seed=13, fmt=fmt, qk_norm=norm)
+    orc = OracleLM(w, MICRO)
+    rng = np.random.default_rng(17)
+    prefix = rng.integers(0, MICRO.vocab, size=9)
+    rows = [rng.integers(0, MICRO.vocab, size=n) for n in (1, 7, 3)]
+    res = orc.eval_rows(prefix, rows, KIND_ENUM, np.array([3, 50, 7]), keep_logits=True)
+    for r in range(3):
+        z = orc.logits(orc.forward_sequence(np.concatenate([prefix, rows[r]]))[-1])[0]
+        assert np.allclose(res["logits"][r][0], z, atol=1e-11)
+
+
+def test_norms_are_taken_per_head_before_the_rotation():
+    """Doubling a query projection changes nothing behind its norm; a gain scales it."""
+    w = make_weights(MICRO, seed=3, qk_norm=True)
+    orc = OracleLM(w, MICRO)
+    h = np.random.default_rng(1).normal(size=(5, 64))
+    _, _, ws = orc.layer_weights(0)
+    pos = np.arange(5)
+    q, k, _ = orc._qkv(0, h, ws, pos)
+    q2, _, _ = orc._qkv(0, h, {**ws, "wq": 1000 * ws["wq"]}, pos)
+    assert np.allclose(q, q2, rtol=1e-3)
+    raw = (h @ ws["wk"].T).reshape(5, 2, 16)
+    want = rms_norm(raw, w.layers[0].k_norm.numpy(), MICRO.rms_eps)
+    assert np.allclose(np.linalg.norm(k, axis=-1), np.linalg.norm(want, axis=-1))
+
+
+def _expect(status, fn, *a, **k):
+    with pytest.raises(L.LmopError) as ei:
+        fn(*a, **k)
+    assert ei.value.status == status
+
+
+def test_loading_on_a_host_ctx():
+    ctx = L.Context(TINY, device=-1)
+    g = torch.ones(TINY.n_layers, TINY.head_dim)
+    _expect(L.LMOP_ERR_STATE, ctx.load_qk_norms, g, g)
+    w = make_weights(TINY, seed=5, fmt="fp8_block", qk_norm=True)
+    ctx.load_weights(w)
+    _expect(L.LMOP_ERR_INVALID_ARG, ctx.load_qk_norms, g, None)
+    with pytest.raises(ValueError):
+        ctx.load_qk_norms(g[:, :32], g)
+    # norms change what a prefix's keys are: prefixes are released
+    pre = ctx.set_prefix([1, 2, 3])
+    ctx.load_qk_norms(g, g)
+    _expect(L.LMOP_ERR_INVALID_ARG, ctx.release_prefix, pre)
+    ctx.load_qk_norms()
+    w.layers[1].q_norm = None
+    with pytest.raises(ValueError):
+        ctx.load_weights(w)
+    bad = make_weights(TINY, seed=5, fmt="fp8_block")
+    bad.layers[0] = dataclasses.replace(bad.layers[0], wo=bad.layers[0].w_up)
+    _expect(L.LMOP_ERR_INVALID_ARG, ctx.load_weights, bad)
+    bad.layers[0] = dataclasses.replace(bad.layers[0], wo=dataclasses.replace(
+        bad.layers[1].wo, fmt="int4_g32"))
+    with pytest.raises(ValueError):
+        ctx.load_weights(bad)
+
+
+@pytest.mark.parametrize("rows,dec", [(1, 1), (40, 1), (40, 4)])
+def test_plan_covers_block_scaled_passes(rows, dec):
+    """The scratch of a plan holds the operand codes and the widest result of a pass."""
+    ctx = L.Context(TINY, device=-1)
+    ctx.load_weights(make_weights(TINY, seed=5, fmt="fp8_block"))
+    n = 20
+    kw = dict(kind=L.LMOP_INT, allowed=list(range(10)), eos=11, max_tokens=dec) if dec > 1 else \
+        dict(kind=L.LMOP_BOOL, allowed=[3, 4])
+    toks = np.arange(rows * n) % TINY.vocab
+    pl = ctx.plan_rows(toks, np.arange(rows + 1) * n, no_dedup=True, **kw)
+    T = min(rows * n, pl["max_batch_tokens"])
+    wide = 256 * -(-TINY.d_ff // 128)
+    need = T * (TINY.d_model * 6 + TINY.n_heads * TINY.head_dim * 4 + 2 * wide + 688 + 4 * 6)
+    assert pl["scratch_bytes"] >= need
+    assert 0 < pl["min_workspace_bytes"] <= pl["scratch_bytes"]

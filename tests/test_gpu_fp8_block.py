@@ -1,0 +1,299 @@
+"""Row evaluation with block-scaled FP8 maps, and with query and key norms, against
+the oracle and against itself: the same bits in every batching, workspace and
+allocation mode.
+
+Tolerance.  Query and key norms in the weight-only formats: tests/parity.py.  With
+block scales every map's input is quantised to 3 fraction bits, and a value
+that lies near the middle of two codes falls to the one or the other by the last
+bit of what was computed before it, so two correct evaluations drift apart
+(the oracle in 32 and in 64 bits: 0.10 sigma at most on the tiny filter).  The
+bound is the oracle's own drift: the quantisers' inputs are fp16 in the library,
+off by up to 2^-11 by rounding alone; the oracle is evaluated again with its
+quantisers' inputs off by up to that (two draws), and the library may be twice
+as far from the oracle as these are, at most and in the root mean square.
+
+One layer on single tokens without a prefix (attention over one key is its
+value) separates a wrong step from the drift, row by row.  A 16-bit map's result
+is off by 2.2e-5 of its size (the 8-bit matrix instructions' cut), which
+turns its rounding to fp16 in about 2.2e-5 / 2^-10.5 = 3% of the values; the
+value moves by 2^-10.5, and a code, 2^-3.5 apart from the next, falls the other way
+in about 2^-7 of those: 2.5e-4 per quantised value.  With 720 to 1340 values behind
+a map in a row, 0.2 to 0.35 codes fall the other way, so 70 to 80% of the rows have
+none and are as near as fp16 has it (values of the last norm off by 2^-11
+at most, some 2^-12 of the logits' spread in the root mean square, 5 times that at
+the largest of 2048: 0.0013 sigma); one code of step 2^-3 among 256 values moves
+the logits by some 0.01 to 0.1 sigma.  More than half of the rows have to
+be within 0.005 sigma, and all within twice the oracle's drift."""
+import dataclasses
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import OracleLM
+from oracle.lmop_oracle import KIND_AUTOMATON, KIND_BOOL, KIND_INT
+from synth import SHAPES, ModelShape, make_weights, make_workload
+from tests.parity import assert_automaton, assert_typed, compare
+
+pytestmark = pytest.mark.gpu
+TINY = SHAPES["tiny"]
+
+
+def _log(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2606_31808_amd import lmop
+    return lmop
+
+
+class _Nudged(OracleLM):
+    """The oracle with the inputs of its quantisers off by up to 2^-11."""
+
+    def __init__(self, seed, *a, **k):
+        super().__init__(*a, **k)
+        self.rng = np.random.default_rng(seed)
+
+    def _half(self, l, x):
+        return super()._half(l, x * (1 + self.rng.uniform(-1, 1, x.shape) * 2.0 ** -11))
+
+
+def _near(w, shape, run, out, dbg, label, dtype=np.float64):
+    """run(oracle, **kw) evaluates the rows of `out`, whose logits are dbg."""
+    n = [int(x) for x in out["n_tokens"]]
+    forced = [out["tokens"][r][: n[r]] for r in range(len(n))]
+
+    def logits(orc):
+        ref = run(orc, keep_logits=True, forced=forced)
+        return np.concatenate([np.stack(z) for z in ref["logits"]]), ref
+
+    z, _ = logits(OracleLM(w, shape, dtype=dtype))
+    got = np.concatenate([dbg[r][: n[r]] for r in range(len(n))])
+    drift = [np.abs(logits(_Nudged(s, w, shape, dtype=dtype))[0] - z) for s in (1, 2)]
+    most, rms = max(d.max() for d in drift), max(np.sqrt((d ** 2).mean()) for d in drift)
+    off = np.abs(got - z)
+    _log(label, f"off by {off.max() / z.std():.3f} sigma (rms {np.sqrt((off ** 2).mean()) / z.std():.4f}), "
+         f"the oracle drifts {most / z.std():.3f} (rms {rms / z.std():.4f})")
+    assert np.isfinite(got).all()
+    assert off.max() <= 2 * most and np.sqrt((off ** 2).mean()) <= 2 * rms
+    # the chosen values, where no drift can turn them
+    free = run(OracleLM(w, shape, dtype=dtype))
+    sure = free["margin"] > 4 * most
+    assert np.array_equal(out["value"][sure], np.asarray(free["value"])[sure])
+
+
+def _ctx(L, w, shape=TINY):
+    ctx = L.Context(shape, device=0, stream=torch.cuda.current_stream().cuda_stream)
+    ctx.load_weights(w)
+    return ctx
+
+
+def _run(ctx, wl, pre, **kw):
+    return ctx.eval_rows(wl.tokens, wl.offsets, wl.kind, wl.type_spec, eos=wl.eos,
+                         max_tokens=wl.max_tokens, prefix=pre, debug_logits=True, **kw)
+
+
+CASES = [("fp8_block", False), ("fp8_block", True), ("int4_g32", True), ("fp8_e4m3", True)]
+
+
+@pytest.mark.parametrize("fmt,norm", CASES)
+def test_filter_and_batching(L, fmt, norm):
+    w = make_weights(TINY, seed=1234, fmt=fmt, qk_norm=norm)
+    ctx = _ctx(L, w)
+    wl = make_workload("filter_tiny")
+    pre = ctx.set_prefix(wl.prefix)
+    _log("filter", fmt, norm)
+    out, dbg = _run(ctx, wl, pre)
+    if fmt == "fp8_block":
+        _near(w, TINY, lambda o, **k: o.eval_workload(wl, **k), out, dbg, "filter")
+    else:
+        ref = OracleLM(w, TINY).eval_workload(wl, keep_logits=True)
+        _log(compare(ref, out, dbg, f"{fmt} {norm}"))
+    assert_typed(out, wl.kind, len(wl.allowed), wl.allowed)
+    for kw in (dict(max_batch_tokens=50), dict(max_batch_tokens=400), dict(no_alloc=True)):
+        o2, d2 = _run(ctx, wl, pre, **kw)
+        assert o2.tobytes() == out.tobytes() and np.array_equal(d2, dbg)
+    # weights that are on the device already
+    ctx2 = _ctx(L, w.to("cuda"))
+    o3, d3 = _run(ctx2, wl, ctx2.set_prefix(wl.prefix))
+    assert o3.tobytes() == out.tobytes() and np.array_equal(d3, dbg)
+
+
+@pytest.mark.parametrize("hd,nq,nkv,d,d_ff", [(64, 4, 4, 256, 688), (128, 6, 2, 320, 700),
+                                              (64, 3, 1, 192, 333)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_one_layer_on_single_tokens(L, norm, hd, nq, nkv, d, d_ff):
+    shape = dataclasses.replace(TINY, n_layers=1, d_model=d, n_heads=nq, n_kv_heads=nkv,
+                                head_dim=hd, d_ff=d_ff)
+    w = make_weights(shape, seed=1234, fmt="fp8_block", qk_norm=norm)
+    toks = np.random.default_rng(2).choice(shape.vocab, 40, replace=False)
+    allowed = np.array([3, 9], dtype=np.int32)
+    out, dbg = _ctx(L, w, shape).eval_rows(toks, np.arange(41), KIND_BOOL, allowed, debug_logits=True)
+    run = lambda o, **k: o.eval_rows(None, [[t] for t in toks], KIND_BOOL, allowed, **k)  # noqa: E731
+    _near(w, shape, run, out, dbg, "one layer")
+    z = np.stack([s[0] for s in run(OracleLM(w, shape), keep_logits=True)["logits"]])
+    off = np.abs(dbg[:, 0] - z).max(1) / z.std()
+    assert np.median(off) <= 0.005, np.sort(off)
+
+
+@pytest.mark.parametrize("fmt,norm", CASES[:3])
+def test_decode_and_children(L, fmt, norm):
+    """Integers and an option trie (several steps), a child prefix per row, a batch
+    whose rows have no tokens of their own."""
+    w = make_weights(TINY, seed=77, fmt=fmt, qk_norm=norm)
+    orc, ctx = OracleLM(w, TINY), _ctx(L, w)
+    wl = make_workload("filter_tiny", n_rows=20)
+    pre = ctx.set_prefix(wl.prefix)
+    rng = np.random.default_rng(8)
+    digits = rng.choice(TINY.vocab, 10, replace=False).astype(np.int32)
+    eos = int(next(t for t in range(TINY.vocab) if t not in digits))
+    rows = [wl.suffix(r) for r in range(20)]
+    offs = np.concatenate([[0], np.cumsum([len(r) for r in rows])])
+    _log("integers", fmt, norm)
+    kw = dict(eos=eos, max_tokens=3)
+    oi, di = ctx.eval_rows(np.concatenate(rows), offs, KIND_INT, digits, prefix=pre,
+                           debug_logits=True, **kw)
+    if fmt == "fp8_block":
+        _near(w, TINY, lambda o, **k: o.eval_rows(wl.prefix, rows, KIND_INT, digits, **kw, **k),
+              oi, di, "integers")
+    else:
+        ri = orc.eval_rows(wl.prefix, rows, KIND_INT, digits, keep_logits=True, **kw)
+        fi = orc.eval_rows(wl.prefix, rows, KIND_INT, digits, keep_logits=True,
+                           forced=[oi["tokens"][r][: oi["n_tokens"][r]] for r in range(20)], **kw)
+        _log(compare(ri, oi, di, "int", orc_forced=fi))
+    o1, _ = ctx.eval_rows(np.concatenate(rows), offs, KIND_INT, digits, prefix=pre,
+                          max_batch_tokens=64, **kw)
+    assert o1.tobytes() == oi.tobytes()
+
+    _log("options", fmt, norm)
+    wo = make_workload("options_tiny", n_rows=12)
+    po = ctx.set_prefix(wo.prefix)
+    oo, _ = _run(ctx, wo, po)
+    assert_automaton(oo, wo.automaton, eos=wo.eos, max_tokens=wo.max_tokens)
+
+    _log("children", fmt, norm)
+    kids_t = [wl.suffix(5)[:9], wl.suffix(6)[:17]]
+    kids = ctx.set_prefixes(kids_t, parent=pre)
+    alone = ctx.set_prefix(kids_t[1], parent=pre)
+    allowed = np.array([3, 50], dtype=np.int32)
+    rc = [0, 1, 0, 1, 1]
+    sufs = [rows[0], rows[1], rows[2][:0], rows[3], rows[4][:1]]
+    co = np.concatenate([[0], np.cumsum([len(r) for r in sufs])])
+    args = (np.concatenate(sufs), co, KIND_BOOL, allowed)
+    out, dbg = ctx.eval_rows(*args, row_prefix=[kids[i] for i in rc], debug_logits=True)
+    run = lambda o, **k: o.eval_rows(wl.prefix, sufs, KIND_BOOL, allowed, children=kids_t,  # noqa: E731
+                                     row_child=rc, **k)
+    if fmt == "fp8_block":
+        _near(w, TINY, run, out, dbg, "children")
+    else:
+        _log(compare(run(orc, keep_logits=True), out, dbg, "children"))
+    o2, _ = ctx.eval_rows(*args, row_prefix=[[kids[0], alone][i] for i in rc], debug_logits=True)
+    assert o2.tobytes() == out.tobytes()
+
+
+# head size 128, grouped heads, widths that are no multiple of 128 (and an odd
+# MLP), a last layer whose queries are split off in the packed formats
+ODD = [dataclasses.replace(TINY, n_layers=2, d_model=320, n_heads=6, n_kv_heads=2, head_dim=128,
+                           d_ff=700, vocab=1000),
+       dataclasses.replace(TINY, n_layers=1, d_model=192, n_heads=3, n_kv_heads=1, head_dim=64,
+                           d_ff=333, vocab=600)]
+
+
+@pytest.mark.parametrize("fmt,norm", CASES)
+@pytest.mark.parametrize("shape", ODD, ids=["hd128", "hd64"])
+def test_odd_shapes(L, shape, fmt, norm):
+    w = make_weights(shape, seed=4, fmt=fmt, qk_norm=norm)
+    ctx, orc = _ctx(L, w, shape), OracleLM(w, shape)
+    rng = np.random.default_rng(3)
+    prefix = rng.integers(0, shape.vocab, 70)
+    rows = [rng.integers(0, shape.vocab, n) for n in (400, 1, 33, 64, 3)]
+    offs = np.concatenate([[0], np.cumsum([len(r) for r in rows])])
+    allowed = np.array([5, 9], dtype=np.int32)
+    pre = ctx.set_prefix(prefix)
+    _log("odd", shape.d_model, fmt, norm)
+    args = (np.concatenate(rows), offs, KIND_BOOL, allowed)
+    out, dbg = ctx.eval_rows(*args, prefix=pre, debug_logits=True)
+    if fmt == "fp8_block":
+        _near(w, shape, lambda o, **k: o.eval_rows(prefix, rows, KIND_BOOL, allowed, **k), out, dbg,
+              "odd")
+    else:
+        ref = orc.eval_rows(prefix, rows, KIND_BOOL, allowed, keep_logits=True)
+        _log(compare(ref, out, dbg, "odd"))
+    for i in range(len(rows)):
+        one, d1 = ctx.eval_rows(rows[i], [0, len(rows[i])], KIND_BOOL, allowed, prefix=pre,
+                                debug_logits=True)
+        assert one.tobytes() == out[i:i + 1].tobytes() and np.array_equal(d1[0], dbg[i])
+
+
+def test_min_workspace_and_memory(L):
+    """A workspace of the planned smallest size gives the same bits; one byte less is refused."""
+    w = make_weights(TINY, seed=1234, fmt="fp8_block", qk_norm=True)
+    ctx = _ctx(L, w)
+    wl = make_workload("filter_tiny", n_rows=30)
+    pre = ctx.set_prefix(wl.prefix)
+    out, _ = _run(ctx, wl, pre)
+    need = ctx.plan_rows(wl.tokens, wl.offsets, wl.kind, wl.type_spec, prefix=pre,
+                         debug_logits=True)["min_workspace_bytes"]
+    buf = torch.full((need + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    at = -buf.data_ptr() % 256
+    ctx.set_workspace(buf.data_ptr() + at, need)
+    o2, _ = _run(ctx, wl, pre)
+    assert o2.tobytes() == out.tobytes()
+    ctx.set_workspace(buf.data_ptr() + at, need - 1)
+    with pytest.raises(L.LmopError) as ei:
+        _run(ctx, wl, pre)
+    assert ei.value.status == L.LMOP_ERR_OOM
+    ctx.set_workspace(0, 0)
+
+
+def test_norms_come_and_go(L):
+    """Norms loaded later, replaced and removed: the bits of a fresh ctx each time."""
+    wl = make_workload("filter_tiny", n_rows=10)
+    w0 = make_weights(TINY, seed=9)
+    w1 = make_weights(TINY, seed=9, qk_norm=True)
+    gains = [torch.stack([getattr(l, n) for l in w1.layers]) for n in ("q_norm", "k_norm")]
+
+    def fresh(w):
+        ctx = _ctx(L, w)
+        return _run(ctx, wl, ctx.set_prefix(wl.prefix))[0].tobytes()
+
+    ctx = _ctx(L, w0)
+    run = lambda: _run(ctx, wl, ctx.set_prefix(wl.prefix))[0].tobytes()  # noqa: E731
+    plain, normed = fresh(w0), fresh(w1)
+    assert plain != normed
+    assert run() == plain
+    ctx.load_qk_norms(*gains)
+    assert run() == normed
+    ctx.load_qk_norms(gains[0].cuda() * 2, gains[1].cuda())
+    assert run() not in (plain, normed)
+    ctx.load_qk_norms()
+    assert run() == plain
+    ctx.load_qk_norms(*gains)
+    ctx.load_weights(w0)  # loading weights drops the norms
+    assert run() == plain
+
+
+def test_1b_widths(L):
+    """Two layers of the 1B widths: the larger tiles of the product in the path."""
+    shape = dataclasses.replace(SHAPES["1b"], n_layers=2, vocab=4096)
+    w = make_weights(shape, seed=6, fmt="fp8_block", qk_norm=True)
+    ctx = _ctx(L, w.to("cuda"), shape)
+    rng = np.random.default_rng(5)
+    prefix = rng.integers(0, shape.vocab, 40)
+    rows = [rng.integers(0, shape.vocab, n) for n in rng.integers(8, 90, 60)]
+    offs = np.concatenate([[0], np.cumsum([len(r) for r in rows])])
+    allowed = np.array([5, 9, 77], dtype=np.int32)
+    pre = ctx.set_prefix(prefix)
+    _log("1b widths")
+    out, dbg = ctx.eval_rows(np.concatenate(rows), offs, 1, allowed, prefix=pre, debug_logits=True)
+    few, d2 = ctx.eval_rows(np.concatenate(rows), offs, 1, allowed, prefix=pre, debug_logits=True,
+                            max_batch_tokens=200)
+    assert few.tobytes() == out.tobytes() and np.array_equal(dbg, d2)
+    _near(w, shape, lambda o, **k: o.eval_rows(prefix, rows[:6], 1, allowed, **k), out[:6], dbg[:6],
+          "1b widths", dtype=np.float32)
