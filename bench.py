@@ -42,10 +42,12 @@ def log(*a):
 
 
 def gemm_roofline(stats, recorded=""):
-    """Dominant kernel family: the weight GEMMs (all four projections), W4A16
-    or, with FP8 weights, W8A16.  recorded: see recorded_workload."""
-    fp8 = any(n.startswith("gemm_w8a16") for n in stats)
-    fam = "gemm_w8a16" if fp8 else "gemm_w4a16"
+    """Dominant kernel family: the weight GEMMs (all four projections), W4A16;
+    with FP8 weights, W8A16; with block-scaled FP8 weights the FP8 products
+    (qkv and gate/up on 8-bit, o and down on fp16 matrix instructions, all
+    priced against the fp16 peak).  recorded: see recorded_workload."""
+    fam = next((f for f in ("gemm_w8a16", "matmul_fp8") if any(n.startswith(f) for n in stats)),
+               "gemm_w4a16")
     names = [n for n in stats if n.startswith(fam)]
     ms = sum(stats[n]["ms"] for n in names)
     fl = sum(stats[n]["flops"] for n in names)
@@ -56,7 +58,7 @@ def gemm_roofline(stats, recorded=""):
     algo_bytes = sum(stats[n]["bytes"] for n in names) / timed
     return {"bound": "mfma", "kernel": f"{fam} (qkv, o, gate/up, down)", "achieved": ach,
             "peak": PEAK_F16_TFLOPS, "unit": "TFLOP/s", "frac": ach / PEAK_F16_TFLOPS,
-            "traffic": None if fp8 else measured_traffic(TRAFFIC_FILE, recorded),
+            "traffic": None if fam != "gemm_w4a16" else measured_traffic(TRAFFIC_FILE, recorded),
             "algorithmic_bytes_per_launch": algo_bytes,
             "launches": sum(stats[n]["launches"] for n in names), "timed_launches": timed,
             "avg_launch_ms": ms / timed, "flops_per_launch": fl / timed}
@@ -461,7 +463,7 @@ def main():
     ap.add_argument("--limit", type=int, default=0,
                     help="LIMIT k early exit: stop once k rows have value --limit-value")
     ap.add_argument("--limit-value", type=int, default=1)
-    ap.add_argument("--weights", default="int4_g32", choices=["int4_g32", "fp8_e4m3"],
+    ap.add_argument("--weights", default="int4_g32", choices=["int4_g32", "fp8_e4m3", "fp8_block"],
                     help="weight format of the linear maps")
     ap.add_argument("--cascade", action="store_true",
                     help="cascade filtering: a bool predicate first, the workload on its survivors")
@@ -615,7 +617,8 @@ def main():
     value = rows / (ms_step * 1e-3)
     rep, n_unique = L.lmop_dedup_rows(wl.tokens, wl.offsets,
                                       None if wl.row_child is None else wl.row_child)
-    wdesc = "int4-g32" if args.weights == "int4_g32" else "fp8-e4m3 per-channel"
+    wdesc = {"int4_g32": "int4-g32", "fp8_e4m3": "fp8-e4m3 per-channel",
+             "fp8_block": "fp8-e4m3 128x128-block"}[args.weights]
     res = {
         "metric": "rows/sec, 8B-shape W4 LM filter (10k rows); MFMA util %, HBM GB/s",
         "value": value, "unit": "rows/s", "n_gpus": 1, "steps": args.steps,

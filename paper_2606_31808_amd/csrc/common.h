@@ -34,14 +34,6 @@ LMOP_DEVICE f32x4 mfma16x16x128_e4m3(i32x8 a, i32x8 b) {
                                                           0, 0, 0);
 }
 
-// The 4 E4M3 codes of a word (byte 0 first) as fp16, exactly: every E4M3
-// value is an fp16 value, so a unit scale changes nothing.
-LMOP_DEVICE f16x4 fp8x4(uint32_t d) {
-  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, false);
-  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, true);
-  return f16x4{a.x, a.y, b.x, b.y};
-}
-
 template <typename T>
 LMOP_DEVICE T shfl_xor(T v, int mask) {
   return __shfl_xor(v, mask, 64);

@@ -22,6 +22,7 @@
 #include "fp8_tiles.h"
 #include "kernels.h"
 #include "lds_dma.h"
+#include "lds_dma4.h"
 
 #include <type_traits>
 
@@ -30,6 +31,14 @@ namespace lmop {
 namespace {
 
 constexpr int GROUP = LMOP_FP8_GROUP;
+
+// The 4 codes of a word (byte 0 first) as fp16, exactly: every E4M3 value is an
+// fp16 value, so a unit scale changes nothing.
+LMOP_DEVICE f16x4 halves_of(uint32_t d) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, true);
+  return f16x4{a.x, a.y, b.x, b.y};
+}
 
 // bytes of a 16-byte chunk from `valid` on become zero (+0.0)
 LMOP_DEVICE uint4 keep_bytes(uint4 v, int valid) {
@@ -67,7 +76,7 @@ LMOP_DEVICE Operand<F32> operand(const Codes& c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint4 w = c.w[i >> 1];
-      const f16x4 lo = fp8x4(i & 1 ? w.z : w.x), hi = fp8x4(i & 1 ? w.w : w.y);
+      const f16x4 lo = halves_of(i & 1 ? w.z : w.x), hi = halves_of(i & 1 ? w.w : w.y);
       r.h[i] = f16x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
     }
     return r;

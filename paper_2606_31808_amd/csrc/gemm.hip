@@ -110,6 +110,14 @@ LMOP_DEVICE void dequant_step(uint32_t w, int half, f16x2 s2, uint32_t mask, uin
   }
 }
 
+// The 4 E4M3 codes of a word (byte 0 first) as fp16, exactly: every E4M3
+// value is an fp16 value, so a unit scale changes nothing.
+LMOP_DEVICE f16x4 fp8x4(uint32_t d) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.0f, true);
+  return f16x4{a.x, a.y, b.x, b.y};
+}
+
 // fp16 of a product that has first been rounded to fp32: without the empty
 // asm the compiler turns some of these into one instruction that rounds once,
 // in some tile shapes and not in others

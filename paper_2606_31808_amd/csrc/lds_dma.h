@@ -39,21 +39,7 @@ LMOP_DEVICE void g2l16_m0(const void* sbase, uint32_t voff, uint32_t lds_addr) {
                : "memory");
 }
 
-// 4 bytes per lane, LDS at lds_addr + 4*lane, for the lanes of a wave-uniform
-// mask (none: no load); every lane must be active
-LMOP_DEVICE void g2l4_m0_mask(const void* sbase, uint32_t voff, uint32_t lds_addr, uint64_t mask) {
-  // (the compiler may compute a uniform mask in vector registers)
-  mask = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(mask >> 32)) << 32 |
-         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)mask);
-  asm volatile(
-      "s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dword %0, %1\n\t"
-      "s_mov_b64 exec, -1"
-      :
-      : "v"(voff), "s"(sbase), "s"(lds_addr), "s"(mask)
-      : "memory");
-}
-
-// g2l16_m0 for the wave's first N lanes only; every lane must be active.  The
+// the same for the wave's first N lanes only; every lane must be active.  The
 // mask is set inside the asm, so the compiler sees no branch (a branch in a
 // pinned schedule lets it move the code around it)
 template <int N>

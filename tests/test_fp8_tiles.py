@@ -79,7 +79,7 @@ def test_helpers_keep_the_wait_state(tmp_path):
     if not os.path.exists(build.HIPCC):
         pytest.skip("no hipcc")
     src, out = tmp_path / "p.hip", tmp_path / "p.s"
-    src.write_text('#include "lds_dma.h"\nusing namespace lmop;\nextern "C" __global__ void probe('
+    src.write_text('#include "lds_dma4.h"\nusing namespace lmop;\nextern "C" __global__ void probe('
                    "const char* a, unsigned off, unsigned lds, unsigned long m) {\n"
                    "  g2l4_m0_mask(a, off * threadIdx.x, lds, m);\n}\n")
     subprocess.run([build.HIPCC, *build.FLAGS, "-x", "hip", "--offload-device-only", "-S", str(src),
