@@ -66,6 +66,13 @@ LMOP_DEVICE void keep_valid(Codes& c, int valid) {
   c.w[1] = keep_bytes(c.w[1], valid - 64);
 }
 
+// 8 of a lane's 32 codes as fp16
+LMOP_DEVICE f16x8 quarter(const Codes& c, int i) {
+  const uint4 w = c.w[i >> 1];
+  const f16x4 lo = halves_of(i & 1 ? w.z : w.x), hi = halves_of(i & 1 ? w.w : w.y);
+  return f16x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+}
+
 // the operand of `dot`: the codes themselves, or their fp16 values
 template <bool F32>
 using Operand = std::conditional_t<F32, Halves, Codes>;
@@ -74,11 +81,7 @@ LMOP_DEVICE Operand<F32> operand(const Codes& c) {
   if constexpr (F32) {
     Halves r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 w = c.w[i >> 1];
-      const f16x4 lo = halves_of(i & 1 ? w.z : w.x), hi = halves_of(i & 1 ? w.w : w.y);
-      r.h[i] = f16x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    }
+    for (int i = 0; i < 4; ++i) r.h[i] = quarter(c, i);
     return r;
   } else {
     return c;
@@ -252,70 +255,152 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
                            (wm * MT * 16 + c) * 16 + i * 256);
   };
 
-  // One whole group.  In phase i the tile row i is multiplied while row i - 1
-  // is added to the sums, row i + 1 is read, and a share of a later stage's
-  // loads is issued (waves that issue all of theirs at once hold each other up
-  // while the matrix cores run dry).  No branch: one would let the compiler
-  // move the additions behind it.
-  constexpr int PER = (C::LOADS + MT - 1) / MT < 2 ? 2 : (C::LOADS + MT - 1) / MT;
-  auto stage = [&](int kb, float sbk) {
-    // the stage has landed for every wave, and every wave is done with the one
-    // before it, which the loads below refill (the later stages' scales are not
-    // counted: a smaller count waits for more)
-    wait_vmcnt_lgkm0<(NS - 2) * C::LOADS>();
-    barrier();
-    Operand<F32> b[NT], a[2];
+  // 64 groups at a time: their scales of the wave's columns, one a lane
+  const int full = p.k / GROUP;
+  auto groups = [&](auto& stage) {
+    for (int k0 = 0; k0 < full; k0 += 64) {
+      float sb_64 = sb[k0 + lane < kb_n ? k0 + lane : kb_n - 1];
+      // waited for here: in the loop the wait would be for the stages in flight too
+      asm volatile("" : "+v"(sb_64));
+      const int end = full < k0 + 64 ? full : k0 + 64;
+      for (int kb = k0; kb < end; ++kb)
+        stage(kb, __uint_as_float(
+                      __builtin_amdgcn_readlane(__float_as_uint(sb_64), kb - k0)));
+    }
+  };
+  if constexpr (F32) {
+    // fp32: the codes' conversions take the vector units as long as the products
+    // take the matrix cores, so each has to run beside the other.  In phase i the
+    // tile row i is multiplied, a quarter of the group at a time, while row i - 1
+    // is added to the sums and row i + 1 is read and converted; the last phase
+    // begins with the barrier, reads the next group's first row and columns, and
+    // puts a converted quarter of the columns in the place of the one just used
+    // up.  16384 x 4096, k 14336: 1592 us, 1642 with the columns converted at a
+    // group's start; 512 x 4096, k 4096 on a workgroup a CU: 54.4, 60.9.
+    static_assert(MT % 2 == 0, "rows alternate between two buffers across groups");
+    constexpr int PER = (C::LOADS + MT - 1) / MT;
+    Halves b[NT], a[2];
     f32x4 d[2][NT];
     float s[2], sc = 0.f;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) b[j] = frag(kb, brow, j);
-    a[0] = frag(kb, arow, 0);
-    s[0] = scale(kb, 0);
+    for (int j = 0; j < NT; ++j) d[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto stage = [&](int kb, float sbk) {
 #pragma unroll
-    for (int i = 0; i <= MT; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
-      if (i == 0) issue_scales(kb + NS - 1);
+      for (int i = 0; i < MT; ++i) {
+        const bool last = i == MT - 1;
+        __builtin_amdgcn_sched_barrier(0);
+        if (last) {
+          // the next stage has landed for every wave, and every wave has read
+          // this one, whose slot the loads below refill (the later stages'
+          // scales are not counted: a smaller count waits for more)
+          wait_vmcnt_lgkm0<(NS - 2) * C::LOADS>();
+          barrier();
+          issue_scales(kb + NS);
+        }
+        const int share = (i + 1) % MT;
 #pragma unroll
-      for (int n = i * PER; n < (i + 1) * PER && n < C::LOADS; ++n) issue_one(n, kb + NS - 1);
-      __builtin_amdgcn_sched_barrier(0);
-      const float sc_before = sc;
-      if (i < MT) sc = s[i & 1] * sbk;
-      if (i + 1 < MT) {
-        a[(i + 1) & 1] = frag(kb, arow, i + 1);
-        s[(i + 1) & 1] = scale(kb, i + 1);
+        for (int n = share * PER; n < (share + 1) * PER && n < C::LOADS; ++n)
+          issue_one(n, last ? kb + NS : kb + NS - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const float sc_before = sc;
+        sc = s[i & 1] * sbk;
+        const int next = last ? kb + 1 : kb, row = last ? 0 : i + 1;
+        const Codes ac = codes(next, arow, row);
+        s[(i + 1) & 1] = scale(next, row);
+        Codes bc[NT];
+        if (last)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) bc[j] = codes(next, brow, j);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            d[i & 1][j] = mfma16x16x32(b[j].h[h], a[i & 1].h[h],
+                                       h ? d[i & 1][j] : f32x4{0.f, 0.f, 0.f, 0.f});
+          a[(i + 1) & 1].h[h] = quarter(ac, h);
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            if (j % 4 == h) add_scaled(acc[(i + MT - 1) % MT][j], d[(i + 1) & 1][j], sc_before);
+          if (last)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j].h[h] = quarter(bc[j], h);
+        }
       }
-      if (i < MT)
+      __builtin_amdgcn_sched_barrier(0);
+    };
 #pragma unroll
-        for (int j = 0; j < NT; ++j) d[i & 1][j] = dot(b[j], a[i & 1]);
-      if (i > 0)
+    for (int kb = 0; kb < NS; ++kb) {
+      issue_scales(kb);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) add_scaled(acc[i - 1][j], d[(i - 1) & 1][j], sc_before);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        __builtin_amdgcn_sched_group_barrier(0x008, F32 ? 4 : 1, 0);  // MFMA
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);            // LDS read
-        __builtin_amdgcn_sched_group_barrier(0x002, F32 ? 8 : 5, 0);  // VALU
-      }
+      for (int n = 0; n < (kb < NS - 1 ? C::LOADS : PER); ++n) issue_one(n, kb);
     }
-    __builtin_amdgcn_sched_barrier(0);
-  };
+    wait_vmcnt_lgkm0<(NS - 2) * C::LOADS>();
+    barrier();
+#pragma unroll
+    for (int j = 0; j < NT; ++j) b[j] = frag(0, brow, j);
+    a[0] = frag(0, arow, 0);
+    s[0] = scale(0, 0);
+    groups(stage);
+    if (full > 0)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) add_scaled(acc[MT - 1][j], d[(MT - 1) & 1][j], sc);
+  } else {
+    // 16-bit results, one whole group.  In phase i the tile row i is multiplied while row i - 1
+    // is added to the sums, row i + 1 is read, and a share of a later stage's
+    // loads is issued (waves that issue all of theirs at once hold each other up
+    // while the matrix cores run dry).  No branch: one would let the compiler
+    // move the additions behind it.
+    constexpr int PER = (C::LOADS + MT - 1) / MT < 2 ? 2 : (C::LOADS + MT - 1) / MT;
+    auto stage = [&](int kb, float sbk) {
+      // the stage has landed for every wave, and every wave is done with the one
+      // before it, which the loads below refill (the later stages' scales are not
+      // counted: a smaller count waits for more)
+      wait_vmcnt_lgkm0<(NS - 2) * C::LOADS>();
+      barrier();
+      Codes b[NT], a[2];
+      f32x4 d[2][NT];
+      float s[2], sc = 0.f;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) b[j] = codes(kb, brow, j);
+      a[0] = codes(kb, arow, 0);
+      s[0] = scale(kb, 0);
+#pragma unroll
+      for (int i = 0; i <= MT; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (i == 0) issue_scales(kb + NS - 1);
+#pragma unroll
+        for (int n = i * PER; n < (i + 1) * PER && n < C::LOADS; ++n) issue_one(n, kb + NS - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const float sc_before = sc;
+        if (i < MT) sc = s[i & 1] * sbk;
+        if (i + 1 < MT) {
+          a[(i + 1) & 1] = codes(kb, arow, i + 1);
+          s[(i + 1) & 1] = scale(kb, i + 1);
+        }
+        if (i < MT)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) d[i & 1][j] = dot(b[j], a[i & 1]);
+        if (i > 0)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) add_scaled(acc[i - 1][j], d[(i - 1) & 1][j], sc_before);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+          __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);  // VALU
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+
 
 #pragma unroll
-  for (int kb = 0; kb < NS - 1; ++kb) {
-    issue_scales(kb);
+    for (int kb = 0; kb < NS - 1; ++kb) {
+      issue_scales(kb);
 #pragma unroll
-    for (int n = 0; n < C::LOADS; ++n) issue_one(n, kb);
-  }
-  const int full = p.k / GROUP;
-  // 64 groups at a time: their scales of the wave's columns, one a lane
-  for (int k0 = 0; k0 < full; k0 += 64) {
-    float sb_64 = sb[k0 + lane < kb_n ? k0 + lane : kb_n - 1];
-    // waited for here: in the loop the wait would be for the stages in flight too
-    asm volatile("" : "+v"(sb_64));
-    const int end = full < k0 + 64 ? full : k0 + 64;
-    for (int kb = k0; kb < end; ++kb)
-      stage(kb, __uint_as_float(
-                    __builtin_amdgcn_readlane(__float_as_uint(sb_64), kb - k0)));
+      for (int n = 0; n < C::LOADS; ++n) issue_one(n, kb);
+    }
+    groups(stage);
   }
   // the loads end before the workgroup does
   wait_vmcnt_lgkm0<0>();

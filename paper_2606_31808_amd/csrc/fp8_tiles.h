@@ -18,10 +18,10 @@ struct Fp8Tile {
 };
 constexpr Fp8Tile kFp8Tiles[] = {
     {8, 4, 2, 4, 1, {1.90f, 0.f}, {2.00f, 0.f}},  // 256 x 256
-    {4, 4, 2, 4, 1, {1.12f, 2.05f}, {1.20f, 2.05f}},  // 128 x 256
-    {2, 4, 2, 2, 2, {0.55f, 0.85f}, {0.80f, 1.25f}},  // 64 x 128
-    {2, 2, 2, 2, 2, {0.38f, 0.57f}, {0.65f, 0.87f}},  // 64 x 64
-    {2, 1, 1, 4, 2, {0.29f, 0.46f}, {0.45f, 0.61f}},  // 32 x 64
+    {4, 4, 2, 4, 1, {1.12f, 1.80f}, {1.20f, 1.80f}},  // 128 x 256
+    {2, 4, 2, 2, 2, {0.55f, 0.77f}, {0.80f, 1.20f}},  // 64 x 128
+    {2, 2, 2, 2, 2, {0.38f, 0.49f}, {0.65f, 0.78f}},  // 64 x 64
+    {2, 1, 1, 4, 2, {0.29f, 0.45f}, {0.45f, 0.64f}},  // 32 x 64
 };
 constexpr int kNumFp8Tiles = sizeof(kFp8Tiles) / sizeof(kFp8Tiles[0]);
 // the picks after the tiles: up to 16 tokens, up to 32 tokens
@@ -36,9 +36,12 @@ constexpr int kNumFp8Kernels = kNumFp8Tiles + 2;
 //   16 tokens: 11.7 / 11.8, 18.6 / 32.3, 35.6 / 26.6
 //   24 tokens: 14.6 / 12.1, 23.8 / 32.6, 44.2 / 27.9;  n 2048 k 2048: 5.1 / 7.1
 //   64 tokens (two rounds of few): 22.3 / 12.3, 46.6 / 32.8
-// and of the tiles, 16-bit results (fp32): 512 x 4096, k 4096: 32 x 64 26, 64 x 64 21
-// (28), 64 x 128 19 (30), 128 x 256 35 (61), 256 x 256 60; 2047 x 4096, k 4096: 64 x 128 58
-// (81), 128 x 256 42 (66), 256 x 256 62; 16384 x 28672, k 4096: 128 x 256 2181, 256 x 256 1830.
+// and of the tiles, 16-bit results (fp32): 256 x 4096, k 4096: 32 x 64 17.1 (24.0), 64 x 64
+// 14.5 (18.4), 64 x 128 19.2 (26.6); 512 x 4096, k 4096: 32 x 64 31.7 (43.9), 64 x 64 20.8
+// (27.3), 64 x 128 19.6 (27.4), 128 x 256 35.4 (54.2), 256 x 256 60.0; 2047 x 4096, k 4096: 64 x 64
+// 71.9 (95.8), 64 x 128 57.0 (81.0), 128 x 256 40.8 (62.5), 256 x 256 62.3; 16384 x 4096, k 14336:
+// 64 x 128 1266 (1926), 128 x 256 932 (1526), 256 x 256 791; 16384 x 28672, k 4096: 128 x 256
+// 2187, 256 x 256 1790.
 inline float fp8_cost(int kernel, bool f32, int m, int n, int k) {
   const float groups = (k + 127) / 128;
   if (kernel >= kNumFp8Tiles) {

@@ -44,7 +44,7 @@ MEASURED = [
     (0, 256, 6144, 4096, {2: 19.9, 3: 21.9, 4: 26.1}),
     (0, 1, 4096, 14336, {3: 35.8, 5: 12.9, 6: 15.5}),
     (0, 16, 4096, 14336, {3: 37.7, 4: 32.3, 5: 18.6, 6: 20.0}),
-    (1, 24, 4096, 14336, {3: 61.7, 4: 51.0, 6: 24.5}),
+    (1, 24, 4096, 14336, {3: 53.2, 4: 49.8, 6: 24.5}),
     (0, 128, 4096, 14336, {2: 59.9, 3: 42.3, 4: 32.8}),
     (0, 256, 4096, 14336, {2: 58.7, 3: 42.8, 4: 50.8}),
     (0, 1, 28672, 4096, {3: 26.8, 5: 22.7, 6: 29.5}),
@@ -52,9 +52,11 @@ MEASURED = [
     (0, 128, 28672, 4096, {2: 41.2, 3: 46.6, 4: 57.8}),
     (0, 24, 2048, 2048, {3: 7.2, 4: 7.0, 6: 5.1}),
     (0, 512, 4096, 4096, {0: 60.1, 1: 35.5, 2: 19.4, 3: 21.2}),
-    (1, 512, 4096, 4096, {1: 61.4, 2: 30.2, 3: 27.9}),
+    (1, 256, 4096, 4096, {1: 53.4, 2: 26.6, 3: 18.4, 4: 24.0}),
+    (1, 512, 4096, 4096, {1: 54.2, 2: 27.4, 3: 27.3, 4: 43.9}),
     (0, 2047, 4096, 4096, {0: 62.5, 1: 41.7, 2: 57.6, 3: 72.7}),
-    (1, 2047, 4096, 4096, {1: 65.9, 2: 81.4, 3: 98.7}),
+    (1, 2047, 4096, 4096, {1: 62.5, 2: 81.0, 3: 95.8}),
+    (1, 16384, 4096, 14336, {1: 1526.0, 2: 1926.0, 3: 2363.0}),
     (0, 4093, 16384, 2048, {0: 159.2, 1: 195.5, 2: 224.8}),
     (0, 16384, 28672, 4096, {0: 1829.9, 1: 2180.9, 2: 2646.3}),
 ]
