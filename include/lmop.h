@@ -127,7 +127,7 @@ typedef struct {
   const lmop_layer* layers;      /* host array [n_layers] (always host memory) */
   int32_t n_layers;
   int32_t on_device; /* 0: the tensor pointers are host memory; 1: device memory on the ctx's device */
-  int32_t format;    /* LMOP_W_INT4_G32, _FP8_E4M3 or _FP8_BLOCK, for all seven maps of every layer */
+  int32_t format;    /* LMOP_W_INT4_G32, _FP8_E4M3 or _FP8_BLOCK, for all maps of every layer */
 } lmop_weights;
 
 /* Copies the weights to the device and repacks them into the kernels'
@@ -384,9 +384,10 @@ lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t 
  * lmop_load_qk_norms.
  *
  * Unlike the calls above, an operator only queues its kernel on the ctx's
- * stream (the null stream for a ctx made without one) and returns: the tensors must stay alive until the stream has passed
- * it, work that writes them must be ordered before it, and a caller may
- * capture it into a HIP graph (with profiling off).  It allocates nothing,
+ * stream (the null stream for a ctx made without one) and returns: the
+ * tensors must stay alive until the stream has passed it, work that writes
+ * them must be ordered before it, and a caller may capture it into a HIP
+ * graph (a ctx with a stream, profiling off).  It allocates nothing,
  * uses no workspace and no state of the ctx other than what is said at each
  * one, and leaves the calling thread's current device as it was.  The ctx
  * needs no weights.  Tensors are device memory of the ctx's device; strides

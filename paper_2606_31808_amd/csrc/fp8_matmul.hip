@@ -24,6 +24,7 @@
 #include "lds_dma.h"
 #include "lds_dma4.h"
 
+#include <atomic>
 #include <type_traits>
 
 namespace lmop {
@@ -562,9 +563,16 @@ hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
   const size_t tiles = (size_t)((a.m + C::BM - 1) / C::BM) * ((a.n + C::BN - 1) / C::BN);
   if (tiles > 0x3fffffffu) return hipErrorInvalidValue;
   auto* k = matmul_tile_kernel<T, t.mt, t.nt, t.wm, t.wn, t.occ>;
-  static const hipError_t raised = hipFuncSetAttribute(
-      (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
-  if (raised != hipSuccess) return raised;
+  // more than 64 KB of LDS: asked for once on each device
+  static std::atomic<uint64_t> raised{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (e == hipSuccess && !(raised.load(std::memory_order_acquire) & bit)) {
+    e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+    if (e == hipSuccess) raised.fetch_or(bit, std::memory_order_release);
+  }
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k, dim3((unsigned)tiles), dim3(64 * C::NW), C::LDS, s, a, aligned4<T>(a));
   return hipGetLastError();
 }

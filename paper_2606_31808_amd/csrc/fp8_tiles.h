@@ -47,7 +47,8 @@ inline float fp8_cost(int kernel, bool f32, int m, int n, int k) {
   if (kernel >= kNumFp8Tiles) {
     const bool wide = kernel == kFp8Few32;
     if (m > (wide ? 32 : 16)) return 1e30f;
-    const float per = wide ? 0.62e-3f + 0.014e-3f * std::max(m - 16, 0) : 0.32e-3f + 0.02e-3f * (m - 1);
+    const float per = wide ? 0.62e-3f + 0.014e-3f * std::max(m - 16, 0)
+                           : 0.32e-3f + 0.02e-3f * (m - 1);
     return 4.f + per * (float)((n + 15) / 16) * groups;
   }
   const Fp8Tile& t = kFp8Tiles[kernel];
