@@ -109,12 +109,17 @@ LMOP_DEVICE void add_scaled(f32x4& acc, f32x4 d, float s) {
   for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(d[r], s, acc[r]);
 }
 
-// Whether rows of C (and add) take the 4-column accesses of store4.
+// Whether rows of C (and add) take accesses of w columns.
 template <typename T>
-bool aligned4(const lmop_matmul_args& p) {
-  return (uintptr_t)p.c % (4 * sizeof(T)) == 0 && p.ldc % 4 == 0 &&
+bool aligned(const lmop_matmul_args& p, int w) {
+  return (uintptr_t)p.c % (w * sizeof(T)) == 0 && p.ldc % w == 0 &&
          (!p.add || ((uintptr_t)p.add % 16 == 0 && p.ldadd % 4 == 0));
 }
+
+// How a tile goes to memory: value by value, 4 columns at a time from the
+// registers (store4), or the wave's rows of 128 bytes and more through LDS,
+// 16 bytes a lane (store_rows).
+enum Store { kValues, kFour, kRows };
 
 // columns n .. n+3 of token m
 template <typename T>
@@ -130,6 +135,49 @@ LMOP_DEVICE void store4(const lmop_matmul_args& p, bool vec, int m, int n, f32x4
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (n + r < p.n) c[r] = (T)(add ? add[r] + v[r] : v[r]);
+  }
+}
+
+// 16 tokens x NT * 16 columns of the wave from token m, column n on, through
+// its 16 * ROW bytes of LDS at `mine`: the lanes of a store hold whole rows.
+// With one workgroup on a CU nothing hides the stores.  16384 x 28672 of fp16, k
+// 4096: 1824 us with store4's 32 bytes a row, 1720 with these 128, 1645 streamed
+// (STREAM: past the caches), 1535 without any stores; fp32, 16384 x 4096, k 4096:
+// 468 (64 bytes a row), 467 (256), 457, 427.
+template <typename T, int NT>
+struct Rows {
+  static constexpr int BYTES = 16 * NT * (int)sizeof(T), CHUNKS = BYTES / 16;
+  static constexpr int ROW = BYTES + 16;  // rows 16 bytes apart in the banks
+  static constexpr bool ON = BYTES >= 128;
+};
+template <typename T, int NT, bool STREAM>
+LMOP_DEVICE void store_rows(const lmop_matmul_args& p, char* mine, int m, int n,
+                            const f32x4 (&v)[NT]) {
+  using R = Rows<T, NT>;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  constexpr int W = 16 / sizeof(T);
+  typedef T Chunk __attribute__((ext_vector_type(W)));
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  // the wave's earlier reads of these bytes are done
+  wait_vmcnt_lgkm0<63>();
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+    *(T4*)(mine + c * R::ROW + (16 * j + 4 * g) * (int)sizeof(T)) =
+        T4{(T)v[j][0], (T)v[j][1], (T)v[j][2], (T)v[j][3]};
+  wait_vmcnt_lgkm0<63>();
+#pragma unroll
+  for (int q = 0; q < 16 * R::CHUNKS / 64; ++q) {
+    const int r = (q * 64 + lane) / R::CHUNKS, x = (q * 64 + lane) % R::CHUNKS;
+    if (m + r < p.m) {
+      Chunk w = *(const Chunk*)(mine + r * R::ROW + 16 * x);
+      if constexpr (std::is_same_v<T, float>)
+        if (p.add) w = *(const Chunk*)(p.add + (size_t)(m + r) * p.ldadd + n + W * x) + w;
+      Chunk* to = (Chunk*)((T*)p.c + (size_t)(m + r) * p.ldc + n + W * x);
+      if constexpr (STREAM)
+        __builtin_nontemporal_store(w, to);
+      else
+        *to = w;
+    }
   }
 }
 
@@ -159,9 +207,9 @@ struct Tile {
 
 constexpr int GM = 4;  // token tiles per L2 group
 
-template <typename T, int MT, int NT, int WM, int WN, int OCC>
+template <typename T, int MT, int NT, int WM, int WN, int OCC, bool STREAM>
 __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void matmul_tile_kernel(
-    const lmop_matmul_args p, bool vec) {
+    const lmop_matmul_args p, Store how) {
   using C = Tile<MT, NT, WM, WN, OCC>;
   constexpr bool F32 = std::is_same_v<T, float>;
   constexpr int BM = C::BM, BN = C::BN, NW = C::NW, NS = C::NS;
@@ -425,11 +473,25 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
       for (int j = 0; j < NT; ++j) add_scaled(acc[i][j], dot(b[j], a), sc);
     }
   }
+  const int n = n0 + wn * NT * 16;
+  if constexpr (Rows<T, NT>::ON) {
+    static_assert(NW * 16 * Rows<T, NT>::ROW <= C::LDS, "the ring's LDS serves again");
+    if (how == kRows) {
+      barrier();  // every wave has read the last stage
+      if (n + NT * 16 <= p.n) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          store_rows<T, NT, STREAM>(p, smem + wave * 16 * Rows<T, NT>::ROW,
+                                    m0 + (wm * MT + i) * 16, n, acc[i]);
+        return;
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j)
-      store4<T>(p, vec, m0 + (wm * MT + i) * 16 + c, n0 + (wn * NT + j) * 16 + 4 * g, acc[i][j]);
+      store4<T>(p, how != kValues, m0 + (wm * MT + i) * 16 + c, n + 16 * j + 4 * g, acc[i][j]);
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -556,13 +618,19 @@ __global__ __launch_bounds__(256) void matmul_empty_kernel(const lmop_matmul_arg
   ((T*)p.c)[m * p.ldc + n] = (T)(p.add ? p.add[m * p.ldadd + n] : 0.f);
 }
 
-template <typename T, int TILE>
-hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
+// Results that the caches (256 MB at last) cannot keep until they are read are
+// streamed past them.  fp16 [m][28672], k 4096, and the quantisation that
+// reads it, us, streamed against not: 59 MB 131 / 129, 117 MB 257 / 260, 235 MB 484 /
+// 490, 940 MB 1910 / 1976.
+constexpr double kStreamBytes = 1e8;
+
+template <typename T, int TILE, bool STREAM>
+hipError_t launch_tile_kernel(hipStream_t s, const lmop_matmul_args& a, Store how) {
   constexpr Fp8Tile t = kFp8Tiles[TILE];
   using C = Tile<t.mt, t.nt, t.wm, t.wn, t.occ>;
   const size_t tiles = (size_t)((a.m + C::BM - 1) / C::BM) * ((a.n + C::BN - 1) / C::BN);
   if (tiles > 0x3fffffffu) return hipErrorInvalidValue;
-  auto* k = matmul_tile_kernel<T, t.mt, t.nt, t.wm, t.wn, t.occ>;
+  auto* k = matmul_tile_kernel<T, t.mt, t.nt, t.wm, t.wn, t.occ, STREAM>;
   // more than 64 KB of LDS: asked for once on each device
   static std::atomic<uint64_t> raised{0};
   int dev = 0;
@@ -573,8 +641,21 @@ hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
     if (e == hipSuccess) raised.fetch_or(bit, std::memory_order_release);
   }
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k, dim3((unsigned)tiles), dim3(64 * C::NW), C::LDS, s, a, aligned4<T>(a));
+  hipLaunchKernelGGL(k, dim3((unsigned)tiles), dim3(64 * C::NW), C::LDS, s, a, how);
   return hipGetLastError();
+}
+
+template <typename T, int TILE>
+hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
+  constexpr Fp8Tile t = kFp8Tiles[TILE];
+  // a 16-bit result with `add` reads 16 bytes of it for 8 it writes: store4
+  const bool rows = aligned<T>(a, 16 / sizeof(T)) && (std::is_same_v<T, float> || !a.add);
+  const Store how = rows ? kRows : aligned<T>(a, 4) ? kFour : kValues;
+  if constexpr (t.occ == 1) {  // the large tiles, which such results take
+    if (rows && (double)a.m * a.n * sizeof(T) > kStreamBytes)
+      return launch_tile_kernel<T, TILE, true>(s, a, how);
+  }
+  return launch_tile_kernel<T, TILE, false>(s, a, how);
 }
 
 template <typename T, int MT, int U>

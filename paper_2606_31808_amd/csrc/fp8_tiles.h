@@ -17,8 +17,8 @@ struct Fp8Tile {
   constexpr int bn() const { return 16 * nt * wn; }
 };
 constexpr Fp8Tile kFp8Tiles[] = {
-    {8, 4, 2, 4, 1, {1.90f, 0.f}, {2.00f, 0.f}},  // 256 x 256
-    {4, 4, 2, 4, 1, {1.12f, 1.80f}, {1.20f, 1.80f}},  // 128 x 256
+    {8, 4, 2, 4, 1, {1.75f, 0.f}, {1.85f, 0.f}},  // 256 x 256
+    {4, 4, 2, 4, 1, {1.08f, 1.78f}, {1.10f, 1.78f}},  // 128 x 256
     {2, 4, 2, 2, 2, {0.55f, 0.77f}, {0.80f, 1.20f}},  // 64 x 128
     {2, 2, 2, 2, 2, {0.38f, 0.49f}, {0.65f, 0.78f}},  // 64 x 64
     {2, 1, 1, 4, 2, {0.29f, 0.45f}, {0.45f, 0.64f}},  // 32 x 64
@@ -40,8 +40,8 @@ constexpr int kNumFp8Kernels = kNumFp8Tiles + 2;
 // 14.5 (18.4), 64 x 128 19.2 (26.6); 512 x 4096, k 4096: 32 x 64 31.7 (43.9), 64 x 64 20.8
 // (27.3), 64 x 128 19.6 (27.4), 128 x 256 35.4 (54.2), 256 x 256 60.0; 2047 x 4096, k 4096: 64 x 64
 // 71.9 (95.8), 64 x 128 57.0 (81.0), 128 x 256 40.8 (62.5), 256 x 256 62.3; 16384 x 4096, k 14336:
-// 64 x 128 1266 (1926), 128 x 256 932 (1526), 256 x 256 791; 16384 x 28672, k 4096: 128 x 256
-// 2187, 256 x 256 1790.
+// 64 x 128 1266 (1926), 128 x 256 902 (1526), 256 x 256 772; 16384 x 28672, k 4096: 128 x 256
+// 1868, 256 x 256 1645.
 inline float fp8_cost(int kernel, bool f32, int m, int n, int k) {
   const float groups = (k + 127) / 128;
   if (kernel >= kNumFp8Tiles) {

@@ -57,8 +57,9 @@ MEASURED = [
     (0, 2047, 4096, 4096, {0: 62.5, 1: 41.7, 2: 57.6, 3: 72.7}),
     (1, 2047, 4096, 4096, {1: 62.5, 2: 81.0, 3: 95.8}),
     (1, 16384, 4096, 14336, {1: 1526.0, 2: 1926.0, 3: 2363.0}),
-    (0, 4093, 16384, 2048, {0: 159.2, 1: 195.5, 2: 224.8}),
-    (0, 16384, 28672, 4096, {0: 1829.9, 1: 2180.9, 2: 2646.3}),
+    (0, 4096, 16384, 2048, {0: 123.0, 1: 146.0}),
+    (0, 16384, 4096, 14336, {0: 772.0, 1: 902.0, 2: 1266.0}),
+    (0, 16384, 28672, 4096, {0: 1645.0, 1: 1868.0, 2: 2600.8}),
 ]
 
 

@@ -241,6 +241,31 @@ def test_matmul_rows_do_not_depend_on_the_batch(ctx, n, k, dtype):
         assert torch.equal(part, whole[M - m:]), m
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("m,n,pad", [(4099, 16400, 8), (7001, 9000, 0), (300, 4100, 4)])
+def test_matmul_large_results_are_written_once(ctx, dtype, m, n, pad):
+    """Results too large for the caches are the rows of small calls, and nothing beside them
+    is written."""
+    print("large", dtype, m, n, flush=True)
+    k = 144
+    a, b = _codes(m, k, 1), _codes(n, k, 2, pad=0)
+    sa, sb = _scales(m, -(-k // G), 3), _scales(-(-n // G), -(-k // G), 4, pad=0)
+    wide = torch.full((m + 1, n + pad), 9.0, dtype=DT[dtype], device="cuda")
+    c = wide[:m, :n]
+    ctx.matmul(a, sa, b, sb, out=c)
+    for r in (0, 37, m - 20):
+        assert torch.equal(c[r:r + 20], ctx.matmul(a[r:r + 20], sa[r:r + 20], b, sb, dtype=DT[dtype]))
+    _check_product(c[-40:], a[-40:], sa[-40:], b, sb)
+    assert torch.all(wide[:m, n:] == 9) and torch.all(wide[m] == 9)
+    if dtype == "f32":
+        base = torch.randn(m, n, generator=_gen(5)).cuda()
+        want = base + c
+        wide[:m, :n] = base
+        ctx.matmul(a, sa, b, sb, add=c, out=c)
+        assert torch.equal(c, want)
+        assert torch.all(wide[:m, n:] == 9) and torch.all(wide[m] == 9)
+
+
 def test_matmul_columns_do_not_depend_on_the_weight(ctx):
     """A weight's first rows alone give the same bits."""
     m, n, k = 70, 2000, 1040
