@@ -109,74 +109,73 @@ LMOP_DEVICE void add_scaled(f32x4& acc, f32x4 d, float s) {
   for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(d[r], s, acc[r]);
 }
 
-// Whether rows of C (and add) take accesses of w columns.
-template <typename T>
-bool aligned(const lmop_matmul_args& p, int w) {
-  return (uintptr_t)p.c % (w * sizeof(T)) == 0 && p.ldc % w == 0 &&
-         (!p.add || ((uintptr_t)p.add % 16 == 0 && p.ldadd % 4 == 0));
-}
-
-// How a tile goes to memory: value by value, 4 columns at a time from the
-// registers (store4), or the wave's rows of 128 bytes and more through LDS,
-// 16 bytes a lane (store_rows).
-enum Store { kValues, kFour, kRows };
-
-// columns n .. n+3 of token m
-template <typename T>
-LMOP_DEVICE void store4(const lmop_matmul_args& p, bool vec, int m, int n, f32x4 v) {
-  typedef T T4 __attribute__((ext_vector_type(4)));
-  if (m >= p.m) return;
-  T* c = (T*)p.c + (size_t)m * p.ldc + n;
-  const float* add = p.add ? p.add + (size_t)m * p.ldadd + n : nullptr;
-  if (vec && n + 4 <= p.n) {
-    if (add) v = *(const f32x4*)add + v;
-    *(T4*)c = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (n + r < p.n) c[r] = (T)(add ? add[r] + v[r] : v[r]);
-  }
-}
-
-// 16 tokens x NT * 16 columns of the wave from token m, column n on, through
-// its 16 * ROW bytes of LDS at `mine`: the lanes of a store hold whole rows.
-// With one workgroup on a CU nothing hides the stores.  16384 x 28672 of fp16, k
-// 4096: 1824 us with store4's 32 bytes a row, 1720 with these 128, 1645 streamed
+// ---------------------------------------------------------------- results to memory
+// 16 tokens x NT * 16 columns of a wave from token m, column n on go through
+// its LDS at `mine`, so that the lanes of a store hold whole rows; a lane's
+// accesses to memory need the alignment of one value only.  With one workgroup
+// on a CU nothing hides the stores.  16384 x 28672 of fp16, k 4096: 1824 us with the
+// 4 columns that a lane has (32 bytes a row), 1720 with rows of 128 bytes, 1645 streamed
 // (STREAM: past the caches), 1535 without any stores; fp32, 16384 x 4096, k 4096:
 // 468 (64 bytes a row), 467 (256), 457, 427.
-template <typename T, int NT>
+template <int NT>
 struct Rows {
-  static constexpr int BYTES = 16 * NT * (int)sizeof(T), CHUNKS = BYTES / 16;
-  static constexpr int ROW = BYTES + 16;  // rows 16 bytes apart in the banks
-  static constexpr bool ON = BYTES >= 128;
+  static constexpr int COLS = 16 * NT;
+  static constexpr int PITCH = 4 * COLS + 16;  // bytes of a row of fp32; 16 apart in the banks
+  static constexpr int LDS = 16 * PITCH;       // of a wave
 };
+
+// every column is in the matrix, and 16-bit results have no `add`: 16 bytes a lane
 template <typename T, int NT, bool STREAM>
 LMOP_DEVICE void store_rows(const lmop_matmul_args& p, char* mine, int m, int n,
                             const f32x4 (&v)[NT]) {
-  using R = Rows<T, NT>;
+  using R = Rows<NT>;
+  constexpr int W = 16 / sizeof(T), CHUNKS = R::COLS / W;
+  constexpr int PITCH = R::COLS * (int)sizeof(T) + 16;
   typedef T T4 __attribute__((ext_vector_type(4)));
-  constexpr int W = 16 / sizeof(T);
   typedef T Chunk __attribute__((ext_vector_type(W)));
+  typedef Chunk Any __attribute__((aligned(sizeof(T))));
+  typedef f32x4 Any4 __attribute__((aligned(4)));
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   // the wave's earlier reads of these bytes are done
   wait_vmcnt_lgkm0<63>();
 #pragma unroll
   for (int j = 0; j < NT; ++j)
-    *(T4*)(mine + c * R::ROW + (16 * j + 4 * g) * (int)sizeof(T)) =
+    *(T4*)(mine + c * PITCH + (16 * j + 4 * g) * (int)sizeof(T)) =
         T4{(T)v[j][0], (T)v[j][1], (T)v[j][2], (T)v[j][3]};
   wait_vmcnt_lgkm0<63>();
 #pragma unroll
-  for (int q = 0; q < 16 * R::CHUNKS / 64; ++q) {
-    const int r = (q * 64 + lane) / R::CHUNKS, x = (q * 64 + lane) % R::CHUNKS;
-    if (m + r < p.m) {
-      Chunk w = *(const Chunk*)(mine + r * R::ROW + 16 * x);
+  for (int q = 0; q < (16 * CHUNKS + 63) / 64; ++q) {
+    const int r = (q * 64 + lane) / CHUNKS, x = (q * 64 + lane) % CHUNKS;
+    if (r < 16 && m + r < p.m) {
+      Chunk w = *(const Chunk*)(mine + r * PITCH + 16 * x);
       if constexpr (std::is_same_v<T, float>)
-        if (p.add) w = *(const Chunk*)(p.add + (size_t)(m + r) * p.ldadd + n + W * x) + w;
-      Chunk* to = (Chunk*)((T*)p.c + (size_t)(m + r) * p.ldc + n + W * x);
+        if (p.add) w = *(const Any4*)(p.add + (size_t)(m + r) * p.ldadd + n + W * x) + w;
+      T* to = (T*)p.c + (size_t)(m + r) * p.ldc + n + W * x;
       if constexpr (STREAM)
-        __builtin_nontemporal_store(w, to);
+        __builtin_nontemporal_store(w, (Any*)to);
       else
-        *to = w;
+        *(Any*)to = w;
+    }
+  }
+}
+
+// any columns: a value a lane
+template <typename T, int NT>
+LMOP_DEVICE void store_values(const lmop_matmul_args& p, char* mine, int m, int n,
+                              const f32x4 (&v)[NT]) {
+  using R = Rows<NT>;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  wait_vmcnt_lgkm0<63>();
+#pragma unroll
+  for (int j = 0; j < NT; ++j) *(f32x4*)(mine + c * R::PITCH + (16 * j + 4 * g) * 4) = v[j];
+  wait_vmcnt_lgkm0<63>();
+#pragma unroll
+  for (int q = 0; q < 16 * R::COLS / 64; ++q) {
+    const int r = (q * 64 + lane) / R::COLS, x = (q * 64 + lane) % R::COLS;
+    if (m + r < p.m && n + x < p.n) {
+      float w = *(const float*)(mine + r * R::PITCH + 4 * x);
+      if (p.add) w = p.add[(size_t)(m + r) * p.ldadd + n + x] + w;
+      ((T*)p.c)[(size_t)(m + r) * p.ldc + n + x] = (T)w;
     }
   }
 }
@@ -209,7 +208,7 @@ constexpr int GM = 4;  // token tiles per L2 group
 
 template <typename T, int MT, int NT, int WM, int WN, int OCC, bool STREAM>
 __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void matmul_tile_kernel(
-    const lmop_matmul_args p, Store how) {
+    const lmop_matmul_args p) {
   using C = Tile<MT, NT, WM, WN, OCC>;
   constexpr bool F32 = std::is_same_v<T, float>;
   constexpr int BM = C::BM, BN = C::BN, NW = C::NW, NS = C::NS;
@@ -473,25 +472,18 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
       for (int j = 0; j < NT; ++j) add_scaled(acc[i][j], dot(b[j], a), sc);
     }
   }
+  static_assert(NW * Rows<NT>::LDS <= C::LDS, "the ring's LDS serves again");
+  barrier();  // every wave has read the last stage
+  char* mine = smem + wave * Rows<NT>::LDS;
   const int n = n0 + wn * NT * 16;
-  if constexpr (Rows<T, NT>::ON) {
-    static_assert(NW * 16 * Rows<T, NT>::ROW <= C::LDS, "the ring's LDS serves again");
-    if (how == kRows) {
-      barrier();  // every wave has read the last stage
-      if (n + NT * 16 <= p.n) {
+  if (n + NT * 16 <= p.n && (F32 || !p.add)) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-          store_rows<T, NT, STREAM>(p, smem + wave * 16 * Rows<T, NT>::ROW,
-                                    m0 + (wm * MT + i) * 16, n, acc[i]);
-        return;
-      }
-    }
+    for (int i = 0; i < MT; ++i)
+      store_rows<T, NT, STREAM>(p, mine, m0 + (wm * MT + i) * 16, n, acc[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) store_values<T, NT>(p, mine, m0 + (wm * MT + i) * 16, n, acc[i]);
   }
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-      store4<T>(p, how != kValues, m0 + (wm * MT + i) * 16 + c, n + 16 * j + 4 * g, acc[i][j]);
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -625,7 +617,7 @@ __global__ __launch_bounds__(256) void matmul_empty_kernel(const lmop_matmul_arg
 constexpr double kStreamBytes = 1e8;
 
 template <typename T, int TILE, bool STREAM>
-hipError_t launch_tile_kernel(hipStream_t s, const lmop_matmul_args& a, Store how) {
+hipError_t launch_tile_kernel(hipStream_t s, const lmop_matmul_args& a) {
   constexpr Fp8Tile t = kFp8Tiles[TILE];
   using C = Tile<t.mt, t.nt, t.wm, t.wn, t.occ>;
   const size_t tiles = (size_t)((a.m + C::BM - 1) / C::BM) * ((a.n + C::BN - 1) / C::BN);
@@ -641,21 +633,17 @@ hipError_t launch_tile_kernel(hipStream_t s, const lmop_matmul_args& a, Store ho
     if (e == hipSuccess) raised.fetch_or(bit, std::memory_order_release);
   }
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k, dim3((unsigned)tiles), dim3(64 * C::NW), C::LDS, s, a, how);
+  hipLaunchKernelGGL(k, dim3((unsigned)tiles), dim3(64 * C::NW), C::LDS, s, a);
   return hipGetLastError();
 }
 
 template <typename T, int TILE>
 hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
   constexpr Fp8Tile t = kFp8Tiles[TILE];
-  // a 16-bit result with `add` reads 16 bytes of it for 8 it writes: store4
-  const bool rows = aligned<T>(a, 16 / sizeof(T)) && (std::is_same_v<T, float> || !a.add);
-  const Store how = rows ? kRows : aligned<T>(a, 4) ? kFour : kValues;
   if constexpr (t.occ == 1) {  // the large tiles, which such results take
-    if (rows && (double)a.m * a.n * sizeof(T) > kStreamBytes)
-      return launch_tile_kernel<T, TILE, true>(s, a, how);
+    if ((double)a.m * a.n * sizeof(T) > kStreamBytes) return launch_tile_kernel<T, TILE, true>(s, a);
   }
-  return launch_tile_kernel<T, TILE, false>(s, a, how);
+  return launch_tile_kernel<T, TILE, false>(s, a);
 }
 
 template <typename T, int MT, int U>

@@ -17,37 +17,17 @@ constexpr int kWaves = 4;       // of a workgroup
 constexpr int kValueTokens = 64;  // of a workgroup that transposes values
 constexpr int kValueDims = 64;
 
+// 16 bytes, at the alignment of one value
 template <typename T>
-using Run = T __attribute__((ext_vector_type(8)));
-
-template <typename T, bool VEC>
-LMOP_DEVICE Run<T> load_run(const T* p) {
-  if constexpr (VEC) {
-    return *(const Run<T>*)p;
-  } else {
-    Run<T> v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p[i];
-    return v;
-  }
-}
-template <typename T, bool VEC>
-LMOP_DEVICE void store_run(T* p, Run<T> v) {
-  if constexpr (VEC) {
-    *(Run<T>*)p = v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = v[i];
-  }
-}
+using Run = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
 
 // One workgroup: kValueTokens tokens x kValueDims dimensions of one value
 // head, transposed through LDS.  Tokens in consecutive slots (a prompt's) are
 // written 16 bytes of a dimension's row at a time where the slots reach a
 // multiple of 8; other tokens one value each, the lanes along the slots.
 template <typename T, int HD>
-LMOP_DEVICE void value_columns(const QkArgs& a, int block, bool vec_in, bool vec_out,
-                               uint16_t (*tile)[kValueDims + 2]) {
+LMOP_DEVICE void value_columns(const QkArgs& a, int block, uint16_t (*tile)[kValueDims + 2]) {
   const lmop_qk_norm_rope_args& p = a.t;
   constexpr int DT = HD / kValueDims;
   const int per_tile = a.nkv * DT;
@@ -60,7 +40,7 @@ LMOP_DEVICE void value_columns(const QkArgs& a, int block, bool vec_in, bool vec
     const int t = (tid >> 3) + i * 8 * kWaves, d = (tid & 7) * 8;
     if (t < n) {
       const T* src = v + (size_t)(t0 + t) * p.ldv + d;
-      const Run<T> r = vec_in ? load_run<T, true>(src) : load_run<T, false>(src);
+      const Run<T> r = *(const Run<T>*)src;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const T x = r[j];  // of the vector's element itself the cast takes element 0
@@ -75,7 +55,7 @@ LMOP_DEVICE void value_columns(const QkArgs& a, int block, bool vec_in, bool vec
   const bool run = __all(here && (lane >= n || slot == s0 + lane));
   __syncthreads();
   uint16_t* out = (uint16_t*)p.v_out + (size_t)d0 * p.ldvo;
-  if (run && vec_out) {
+  if (run) {
     // chunk j: slots first + 8j .. +7
     const int first = s0 & ~7, chunks = (s0 - first + n + 7) / 8;
     for (int i = tid; i < chunks * kValueDims; i += 64 * kWaves) {
@@ -87,7 +67,7 @@ LMOP_DEVICE void value_columns(const QkArgs& a, int block, bool vec_in, bool vec
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           w[q] = tile[t + 2 * q][d] | (uint32_t)tile[t + 2 * q + 1][d] << 16;
-        *(uint4*)o = make_uint4(w[0], w[1], w[2], w[3]);
+        *(Words*)o = Words{w[0], w[1], w[2], w[3]};
       } else {
 #pragma unroll
         for (int q = 0; q < 8; ++q)
@@ -103,16 +83,15 @@ LMOP_DEVICE void value_columns(const QkArgs& a, int block, bool vec_in, bool vec
 // `chunks` head chunks of a token, from chunk task % splits * chunks on, and
 // goes on with every `waves`-th (token, chunk range).  Heads are numbered
 // queries, keys, and (LMOP_V_ROWS) values.
-template <typename T, int HD, bool VEC>
+template <typename T, int HD>
 __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const QkArgs a, int value_blocks,
-                                                                   bool vec_v, int chunks,
-                                                                   int splits) {
+                                                                   int chunks, int splits) {
   constexpr int LPH = HD / 16;   // lanes of a head
   constexpr int HPW = 64 / LPH;  // heads of a chunk
   const lmop_qk_norm_rope_args& p = a.t;
   if ((int)blockIdx.x < value_blocks) {
     __shared__ uint16_t tile[kValueTokens][kValueDims + 2];
-    value_columns<T, HD>(a, blockIdx.x, VEC, vec_v, tile);
+    value_columns<T, HD>(a, blockIdx.x, tile);
     return;
   }
   const int lane = threadIdx.x & 63;
@@ -156,8 +135,8 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const QkArgs 
       out += hs * HD + d;
       Run<T> r1 = {}, r2 = {};
       if (on) {
-        r1 = load_run<T, VEC>(in);
-        r2 = load_run<T, VEC>(in + HD / 2);
+        r1 = *(const Run<T>*)in;
+        r2 = *(const Run<T>*)(in + HD / 2);
       }
       if (sec < 2) {
         float x1[8], x2[8], ss = 0.f;
@@ -186,25 +165,17 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const QkArgs 
         }
       }
       if (on) {
-        store_run<T, VEC>(out, r1);
-        store_run<T, VEC>(out + HD / 2, r2);
+        *(Run<T>*)out = r1;
+        *(Run<T>*)(out + HD / 2) = r2;
       }
     }
   }
 }
 
-// whether rows start on 16-byte boundaries (absent tensors count as aligned)
-bool aligned16(const void* p, int64_t ld) { return !p || ((uintptr_t)p % 16 == 0 && ld % 8 == 0); }
-
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const QkArgs& a) {
   const lmop_qk_norm_rope_args& p = a.t;
   const bool columns = p.v && p.v_layout == LMOP_V_COLUMNS;
-  const bool vec_v = columns && aligned16(p.v_out, p.ldvo);
-  const bool vec = aligned16(p.q, p.ldq) && aligned16(p.k, p.ldk) && aligned16(p.v, p.ldv) &&
-                   aligned16(p.q ? p.q_out : nullptr, p.ldqo) &&
-                   aligned16(p.k ? p.k_out : nullptr, p.ldko) &&
-                   aligned16(p.v && !columns ? p.v_out : nullptr, p.ldvo);
   const long value_blocks = columns ? (long)((p.n_tokens + kValueTokens - 1) / kValueTokens) *
                                           a.nkv * (HD / kValueDims)
                                     : 0;
@@ -216,9 +187,8 @@ hipError_t launch(hipStream_t s, const QkArgs& a) {
   const long want = ((long)p.n_tokens * splits + kWaves - 1) / kWaves;
   const long blocks = (!p.q && !p.k && (columns || !p.v)) ? 0 : want < 65536 ? want : 65536;
   if (value_blocks + blocks > 0x7fffffff) return hipErrorInvalidValue;
-  auto* k = vec ? qk_norm_rope_kernel<T, HD, true> : qk_norm_rope_kernel<T, HD, false>;
-  hipLaunchKernelGGL(k, dim3((unsigned)(value_blocks + blocks)), dim3(64 * kWaves), 0, s, a,
-                     (int)value_blocks, vec_v, chunks, splits);
+  hipLaunchKernelGGL((qk_norm_rope_kernel<T, HD>), dim3((unsigned)(value_blocks + blocks)),
+                     dim3(64 * kWaves), 0, s, a, (int)value_blocks, chunks, splits);
   return hipGetLastError();
 }
 

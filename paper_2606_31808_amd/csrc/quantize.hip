@@ -18,13 +18,14 @@ namespace {
 constexpr float kE4m3Max = 448.0f;
 constexpr float kAmaxMin = 0x1p-40f;
 
+// 8 features in accesses of 16 bytes, at the alignment of one
 template <typename T>
-using Run = T __attribute__((ext_vector_type(8)));
+using Run = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));
 
 // features f .. f+7 of a row, zero from cols on
-template <typename T, bool VEC>
+template <typename T>
 LMOP_DEVICE void load_run(const T* row, int f, int cols, float (&y)[8]) {
-  if (VEC && f + 8 <= cols) {
+  if (f + 8 <= cols) {
     const Run<T> v = *(const Run<T>*)(row + f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = (float)v[i];
@@ -36,7 +37,7 @@ LMOP_DEVICE void load_run(const T* row, int f, int cols, float (&y)[8]) {
 
 LMOP_DEVICE uint32_t max_u32(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-template <typename T, bool VEC, bool GATE>
+template <typename T, bool GATE>
 __global__ __launch_bounds__(256) void quantize_kernel(const lmop_quantize_args p, uint32_t groups,
                                                        uint32_t tasks) {
   const uint32_t task = blockIdx.x * 32u + (threadIdx.x >> 3);
@@ -48,13 +49,13 @@ __global__ __launch_bounds__(256) void quantize_kernel(const lmop_quantize_args 
   float y[2][8];
   const T* x = (const T*)p.x + (size_t)row * p.ldx;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) load_run<T, VEC>(x, f0 + 64 * h, p.cols, y[h]);
+  for (int h = 0; h < 2; ++h) load_run<T>(x, f0 + 64 * h, p.cols, y[h]);
   if constexpr (GATE) {
     const T* gt = (const T*)p.gate + (size_t)row * p.ldg;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float z[8];
-      load_run<T, VEC>(gt, f0 + 64 * h, p.cols, z);
+      load_run<T>(gt, f0 + 64 * h, p.cols, z);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         y[h][i] *= z[i] * __builtin_amdgcn_rcpf(1.0f + __expf(-z[i]));
@@ -93,20 +94,12 @@ __global__ __launch_bounds__(256) void quantize_kernel(const lmop_quantize_args 
   if (lane == 0) p.scale[(size_t)row * p.lds + g] = amax / kE4m3Max;
 }
 
-// whether rows start on 16-byte boundaries
-bool aligned16(const void* p, int64_t ld, size_t esize) {
-  return (uintptr_t)p % 16 == 0 && (size_t)ld * esize % 16 == 0;
-}
-
 template <typename T>
 hipError_t launch(hipStream_t s, const lmop_quantize_args& a) {
   const size_t groups = ((size_t)a.cols + LMOP_FP8_GROUP - 1) / LMOP_FP8_GROUP;
   const size_t tasks = a.rows * groups;
   if (tasks > 0xFFFFFFE0u) return hipErrorInvalidValue;
-  const bool vec =
-      aligned16(a.x, a.ldx, sizeof(T)) && (!a.gate || aligned16(a.gate, a.ldg, sizeof(T)));
-  auto* k = vec ? (a.gate ? quantize_kernel<T, true, true> : quantize_kernel<T, true, false>)
-                : (a.gate ? quantize_kernel<T, false, true> : quantize_kernel<T, false, false>);
+  auto* k = a.gate ? quantize_kernel<T, true> : quantize_kernel<T, false>;
   hipLaunchKernelGGL(k, dim3((unsigned)((tasks + 31) / 32)), dim3(256), 0, s, a, (uint32_t)groups,
                      (uint32_t)tasks);
   return hipGetLastError();
