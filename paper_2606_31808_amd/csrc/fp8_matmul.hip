@@ -181,6 +181,12 @@ LMOP_DEVICE void store_values(const lmop_matmul_args& p, char* mine, int m, int 
 }
 
 // ---------------------------------------------------------------- tiles through LDS
+// Bound by the matrix cores, LDS and the vector units together: a group of 256 x 256
+// takes the matrix cores 2048 cycles, LDS 2048 (192 KB read, 64 KB filled, 128 B a cycle) and
+// each SIMD some 1800 cycles of issue, and they overlap in part: 16384 x 28672, k 4096
+// runs at 2340 TFLOP/s (fp16 results; 2508 without its stores, 52% of the MFMA peak at the
+// clock of the run), 16384 x 4096, k 14336 at 2490; with fp32 results, whose codes become
+// fp16, at 1260.
 // A workgroup of WM x WN waves computes 16*MT*WM tokens x 16*NT*WN columns; a
 // wave MT x NT tiles of 16 x 16.  One ring stage is one group of the tile's
 // rows: 128 bytes a row, 16-byte chunks XOR-swizzled by row, and the tokens'
@@ -492,7 +498,10 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
 // leaves the products in LDS, where the threads (one or more outputs each)
 // add them in the order of the groups.  A weight of few rows is then spread
 // over the chip along K.  The operands of two rounds are in flight or in
-// registers (4 * U * (1 + MT) KB a wave).
+// registers (4 * U * (1 + MT) KB a wave).  Bound by memory for one token (n 28672, k 4096: 117 MB
+// in 22.6 us, 5.2 TB/s; n 4096, k 14336: 13.9, 4.2), for more by L2, from which every 16
+// columns read the tokens' codes again (16 tokens 19.0, 24 tokens 24.2); twice the loads
+// in flight, or 16 waves, take as long.
 template <typename T, int MT, int U>
 __global__ __launch_bounds__(512, 2) void matmul_few_kernel(const lmop_matmul_args p) {
   constexpr bool F32 = std::is_same_v<T, float>;
