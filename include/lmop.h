@@ -103,7 +103,8 @@ const char* lmop_status_string(lmop_status s);
  *     W[r][j] = e4m3(q[r][j]) * scales[r/128][j/128].
  * Every map's input, fp16 per token, is quantised as lmop_quantize does (one
  * scale per 128 features; w_down's is silu(gate) * up of the fp16 gate and
- * up) and multiplied as lmop_matmul does. */
+ * up) and multiplied as lmop_matmul does (fp16 results, and fast fp32 ones
+ * added to the residual). */
 typedef struct {
   const uint8_t* qweight;
   const void* scales;
@@ -428,7 +429,8 @@ lmop_status lmop_quantize(lmop_ctx* ctx, const lmop_quantize_args* args);
  * in order of g.  For fp16 and bf16 results the inner sum runs on the 8-bit
  * matrix instruction, which cuts a product's bits below 2^-13 of the largest
  * of its 8 neighbours (2e-5 of a result's usual size, less than a tenth of its
- * rounding); for fp32 results every product is whole.  NaN codes give NaN. */
+ * rounding); for fp32 results every product is whole, unless `fast` asks for
+ * the 8-bit instruction there too.  NaN codes give NaN. */
 typedef struct {
   const uint8_t* a;     /* [m][k] codes (tokens), 16-byte aligned */
   const float* a_scale; /* [m][ceil(k / 128)] */
@@ -443,6 +445,7 @@ typedef struct {
   int64_t ldadd, ldc;   /* >= n */
   int32_t m, n, k;      /* k = 0: C = add, or zero */
   int32_t dtype;        /* LMOP_F16, LMOP_BF16 or LMOP_F32 */
+  int32_t fast;         /* 1: products cut in fp32 results too, at up to twice the rate; else 0 */
 } lmop_matmul_args;
 lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* args);
 

@@ -7,8 +7,8 @@ namespace lmop {
 
 // A tile of 16*mt*wm tokens x 16*nt*wn columns by wm x wn waves, occ
 // workgroups a CU; us per group of 128 features with one workgroup on a CU and
-// with occ of them (same card, weights from memory), for 16-bit results and
-// for fp32 ones (0: not offered).  few: 16*mt tokens x 16 columns by 8 waves
+// with occ of them (same card, weights from memory), on the 8-bit instruction and
+// with whole products (0: not offered).  few: 16*mt tokens x 16 columns by 8 waves
 // that share K.
 struct Fp8Tile {
   int mt, nt, wm, wn, occ;
@@ -42,7 +42,7 @@ constexpr int kNumFp8Kernels = kNumFp8Tiles + 2;
 // 71.9 (95.8), 64 x 128 57.0 (81.0), 128 x 256 40.8 (62.5), 256 x 256 62.3; 16384 x 4096, k 14336:
 // 64 x 128 1266 (1926), 128 x 256 902 (1526), 256 x 256 772; 16384 x 28672, k 4096: 128 x 256
 // 1868, 256 x 256 1645.
-inline float fp8_cost(int kernel, bool f32, int m, int n, int k) {
+inline float fp8_cost(int kernel, bool whole, int m, int n, int k) {
   const float groups = (k + 127) / 128;
   if (kernel >= kNumFp8Tiles) {
     const bool wide = kernel == kFp8Few32;
@@ -52,20 +52,20 @@ inline float fp8_cost(int kernel, bool f32, int m, int n, int k) {
     return 4.f + per * (float)((n + 15) / 16) * groups;
   }
   const Fp8Tile& t = kFp8Tiles[kernel];
-  if (t.all[f32] == 0.f) return 1e30f;
+  if (t.all[whole] == 0.f) return 1e30f;
   const long tiles = (long)((m + t.bm() - 1) / t.bm()) * ((n + t.bn() - 1) / t.bn());
   const long round = 256L * t.occ, full = tiles / round, rem = tiles % round;
   const float rounds =
-      full * t.all[f32] + (rem == 0 ? 0.f : rem <= 256 ? t.one[f32] : t.all[f32]);
+      full * t.all[whole] + (rem == 0 ? 0.f : rem <= 256 ? t.one[whole] : t.all[whole]);
   return 3.f + std::max(groups * rounds, (float)n * (float)k / 4.4e6f);
 }
 
 // The kernel with the least estimated time, the smaller tile of two that wait
 // for the same memory.  Every kernel gives the same bits.
-inline int pick_fp8_kernel(bool f32, int m, int n, int k) {
+inline int pick_fp8_kernel(bool whole, int m, int n, int k) {
   int best = kNumFp8Kernels - 1;
   for (int i = best - 1; i >= 0; --i)
-    if (fp8_cost(i, f32, m, n, k) < fp8_cost(best, f32, m, n, k)) best = i;
+    if (fp8_cost(i, whole, m, n, k) < fp8_cost(best, whole, m, n, k)) best = i;
   return best;
 }
 

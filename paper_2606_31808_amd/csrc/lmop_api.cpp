@@ -1149,6 +1149,8 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
     a.n = W.n;
     a.k = W.k;
     a.dtype = x32 ? LMOP_F32 : LMOP_F16;
+    // 2e-5 of a map's result against the 2e-2 that quantising its input costs
+    a.fast = x32 != nullptr;
     return timed(c, gemm_name(c, name, b.decode), 2.0 * rows * W.n * W.k,
                  (double)rows * W.k + weight_bytes(c, W.n, W.k) + (double)rows * W.n * (x32 ? 8 : 2),
                  [&] { return launch_matmul_fp8(c->stream, a); });
@@ -2841,6 +2843,8 @@ lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* a) {
     return fail(ctx, LMOP_ERR_INVALID_ARG, "m %d, n %d, k %d", a->m, a->n, a->k);
   if (a->dtype != LMOP_F16 && a->dtype != LMOP_BF16 && a->dtype != LMOP_F32)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
+  if (a->fast != 0 && a->fast != 1)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "fast is %d (0 or 1)", a->fast);
   if (a->m == 0 || a->n == 0) return LMOP_OK;
   if ((uint64_t)((a->m + 15ll) / 16) * ((a->n + 15ll) / 16) > kMaxTasks)
     return fail(ctx, LMOP_ERR_UNSUPPORTED, "%d x %d is too large for one call", a->m, a->n);

@@ -117,7 +117,7 @@ class lmop_matmul_args(C.Structure):
                 ("b_scale", C.c_void_p), ("add", C.c_void_p), ("c", C.c_void_p),
                 ("lda", C.c_int64), ("ldb", C.c_int64), ("ldas", C.c_int64), ("ldbs", C.c_int64),
                 ("ldadd", C.c_int64), ("ldc", C.c_int64), ("m", C.c_int32), ("n", C.c_int32),
-                ("k", C.c_int32), ("dtype", C.c_int32)]
+                ("k", C.c_int32), ("dtype", C.c_int32), ("fast", C.c_int32)]
 
 
 class lmop_qk_norm_rope_args(C.Structure):
@@ -462,7 +462,7 @@ _CODES = {torch.float8_e4m3fn: 0, torch.uint8: 0}
 _F32 = {torch.float32: LMOP_F32}
 _PACK = {}
 for _name, _fmt, _struct in (("quantize", "4P4q3i4x", lmop_quantize_args),
-                             ("matmul", "6P6q4i", lmop_matmul_args),
+                             ("matmul", "6P6q5i4x", lmop_matmul_args),
                              ("qk_norm_rope", "10P6q4i", lmop_qk_norm_rope_args)):
     assert struct.calcsize(_fmt) == C.sizeof(_struct)
     _PACK[_name] = struct.Struct(_fmt).pack
@@ -534,9 +534,9 @@ def lmop_quantize(ctx, x, q, scale, gate=None) -> None:
         _check(st, ctx)
 
 
-def lmop_matmul(ctx, a, a_scale, b, b_scale, c, add=None) -> None:
+def lmop_matmul(ctx, a, a_scale, b, b_scale, c, add=None, fast: bool = False) -> None:
     """c = a b^T (+ add) of E4M3 codes: scales per row and 128 features of a, per
-    128 x 128 block of b."""
+    128 x 128 block of b.  fast: float32 results on the 8-bit instruction."""
     (m, k), n, dev = a.shape, b.shape[0], a.get_device()
     groups = (k + 127) >> 7
     pd = ldadd = 0
@@ -549,7 +549,7 @@ def lmop_matmul(ctx, a, a_scale, b, b_scale, c, add=None) -> None:
         _ld_codes(a, "a", m, k, dev), _ld_codes(b, "b", n, k, dev),
         _ld(a_scale, "a_scale", m, groups, _F32, dev),
         _ld(b_scale, "b_scale", (n + 127) >> 7, groups, _F32, dev), ldadd, ldc, m, n, k,
-        _DTYPES[c.dtype]))
+        _DTYPES[c.dtype], fast))
     if st:
         _check(st, ctx)
 
@@ -706,12 +706,13 @@ class Context:
         lmop_quantize(self.ctx, x, out[0], out[1], gate)
         return out
 
-    def matmul(self, a, a_scale, b, b_scale, dtype=torch.float16, add=None, out=None):
-        """a b^T (+ add) of E4M3 codes a [m, k], b [n, k] with block scales."""
+    def matmul(self, a, a_scale, b, b_scale, dtype=torch.float16, add=None, out=None, fast=False):
+        """a b^T (+ add) of E4M3 codes a [m, k], b [n, k] with block scales.  A float32
+        result keeps every product whole, or (fast) has them cut as 16-bit ones do."""
         self._here(a)
         if out is None:
             out = torch.empty((a.shape[0], b.shape[0]), dtype=dtype, device=a.device)
-        lmop_matmul(self.ctx, a, a_scale, b, b_scale, out, add)
+        lmop_matmul(self.ctx, a, a_scale, b, b_scale, out, add, fast)
         return out
 
     def qk_norm_rope(self, q=None, k=None, v=None, *, pos, q_gain=None, k_gain=None, slot=None,

@@ -183,14 +183,14 @@ def _ref_matmul(a, sa, b, sb):
             eights(A) @ eights(B).t().contiguous())
 
 
-def _check_product(c, a, sa, b, sb, add=None):
+def _check_product(c, a, sa, b, sb, add=None, fast=False):
     ref, mag, most = _ref_matmul(a, sa, b, sb)
     k = a.shape[1]
     if add is not None:
         ref, mag = ref + add.double(), mag + add.double().abs()
     # 128 terms of a group, the groups' fma chain, the scales' product, the addition
     tol = (G + -(-k // G) + 4) * 2.0 ** -23 * mag
-    if c.dtype != torch.float32:
+    if c.dtype != torch.float32 or fast:
         # The 8-bit matrix instruction cuts off what lies below 2^-13 of the leading
         # bit of the largest of eight neighbouring products: less than 2^-13 of
         # that product (at most the product of the eights' largest values) from
@@ -225,6 +225,22 @@ def test_matmul(ctx, dtype, m, n, k):
     ctx.matmul(a, sa, b, sb, add=add, out=wide[:, :n])
     _check_product(wide[:, :n], a, sa, b, sb, add)
     assert torch.all(wide[:, n:] == 9)
+
+
+@pytest.mark.parametrize("m,n,k", SIZES + LARGE)
+def test_matmul_fast(ctx, m, n, k):
+    print("fast", m, n, k, flush=True)
+    a, b = _codes(m, k, 1), _codes(n, k, 2, pad=0)
+    sa, sb = _scales(m, -(-k // G), 3), _scales(-(-n // G), -(-k // G), 4, pad=0)
+    c = ctx.matmul(a, sa, b, sb, dtype=torch.float32, fast=True)
+    _check_product(c, a, sa, b, sb, fast=True)
+    # what the 16-bit results round
+    assert torch.equal(c.half(), ctx.matmul(a, sa, b, sb, fast=True))
+    assert torch.equal(c.bfloat16(), ctx.matmul(a, sa, b, sb, dtype=torch.bfloat16))
+    add = torch.randn(m, n, generator=_gen(5)).cuda()
+    want = add + c
+    ctx.matmul(a, sa, b, sb, add=add, out=add, fast=True)
+    assert torch.equal(add, want)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])

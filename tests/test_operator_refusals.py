@@ -68,7 +68,7 @@ def test_quantize(ctx, change, status):
     ({}, UNS),
     (dict(m=0), OK), (dict(n=0), OK), (dict(m=-1), INV), (dict(n=-1), INV), (dict(k=-1), INV),
     (dict(k=0, a=None, b=None, a_scale=None, b_scale=None), UNS),
-    (dict(dtype=5), INV),
+    (dict(dtype=5), INV), (dict(fast=1), UNS), (dict(fast=2), INV), (dict(fast=-1), INV),
     (dict(a=None), INV), (dict(b=None), INV), (dict(a_scale=None), INV), (dict(b_scale=None), INV),
     (dict(c=None), INV),
     (dict(a=P + 8), INV), (dict(b=P + 1), INV), (dict(a_scale=P + 1), INV), (dict(c=P + 1), INV),
