@@ -191,8 +191,8 @@ LMOP_DEVICE void store_values(const lmop_matmul_args& p, char* mine, int m, int 
 // Bound by the matrix cores, LDS and the vector units together: a group of 256 x 256
 // takes the matrix cores 2048 cycles, LDS 2048 (192 KB read, 64 KB filled, 128 B a cycle) and
 // each SIMD some 1800 cycles of issue, and they overlap in part: 16384 x 28672, k 4096
-// runs at 2340 TFLOP/s (fp16 results; 2508 without its stores, 52% of the MFMA peak at the
-// clock of the run), 16384 x 4096, k 14336 at 2490; with fp32 results, whose codes become
+// runs at 2340 TFLOP/s (fp16 results; the matrix cores busy 57% of the cycles, 2508 without
+// its stores), 16384 x 4096, k 14336 at 2490; with whole products, whose codes become
 // fp16, at 1260.
 // A workgroup of WM x WN waves computes 16*MT*WM tokens x 16*NT*WN columns; a
 // wave MT x NT tiles of 16 x 16.  One ring stage is one group of the tile's
