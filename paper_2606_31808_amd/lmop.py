@@ -233,11 +233,26 @@ def _tensor_ptr(t, keep):
     return a.ctypes.data, False
 
 
+def _qk_norms(weights, head_dim: Optional[int] = None):
+    """The layers' query and key norms, [n_layers, head_dim] each; None without."""
+    norms = [(getattr(l, "q_norm", None), getattr(l, "k_norm", None)) for l in weights.layers]
+    if all(n is None for pair in norms for n in pair):
+        return None
+    if any(n is None for pair in norms for n in pair):
+        raise ValueError("query and key norms: in every layer, or in none")
+    norms = [[torch.as_tensor(n).detach().cpu().float() for n in pair] for pair in norms]
+    for n in (n for pair in norms for n in pair):
+        if tuple(n.shape) != (head_dim or norms[0][0].numel(),):
+            raise ValueError(f"a query or key norm of shape {tuple(n.shape)}")
+    return [torch.stack([pair[i] for pair in norms]) for i in (0, 1)]
+
+
 def lmop_load_weights(ctx, weights) -> None:
     """weights: object with tok_embedding, lm_head (fp16 [V][d]), final_norm, layers[...]
     (attn_norm, mlp_norm, wq .. w_down each with qweight/scales/n/k and a format name
     `fmt`, "int4_g32" (default), "fp8_e4m3" or "fp8_block"), all on one device.  Layers
     with q_norm and k_norm (fp32 [head_dim]) have these loaded too."""
+    norms = _qk_norms(weights)
     keep = []
     where = set()
 
@@ -265,27 +280,18 @@ def lmop_load_weights(ctx, weights) -> None:
         raise ValueError("weights must all be on the host or all on the device")
     w.on_device = 1 if where.pop() else 0
     _check(_lib.lmop_load_weights(ctx, C.byref(w)), ctx)
-    norms = [(getattr(l, "q_norm", None), getattr(l, "k_norm", None)) for l in weights.layers]
-    if any(n is not None for pair in norms for n in pair):
-        if any(n is None for pair in norms for n in pair):
-            raise ValueError("query and key norms: in every layer, or in none")
-        lmop_load_qk_norms(ctx, *(torch.stack([torch.as_tensor(pair[i]) for pair in norms])
-                                  for i in (0, 1)))
+    if norms is not None:
+        lmop_load_qk_norms(ctx, *norms)
 
 
 def lmop_load_qk_norms(ctx, q_gain=None, k_gain=None) -> None:
-    """Query and key norms, fp32 [n_layers, head_dim] (both None: no norms)."""
-    keep, where, at = [], set(), []
-    for g in (q_gain, k_gain):
-        if g is None:
-            at.append(None)
-            continue
-        a, dev = _tensor_ptr(torch.as_tensor(g, dtype=torch.float32), keep)
-        at.append(a)
-        where.add(dev)
-    if len(where) > 1:
-        raise ValueError("query and key norms must both be on the host or on the device")
-    _check(_lib.lmop_load_qk_norms(ctx, at[0], at[1], 1 if where == {True} else 0), ctx)
+    """Query and key norms, [n_layers, head_dim] (both None: no norms)."""
+    # few values, from the host: a copy or conversion on torch's current stream is
+    # not ordered with the ctx's
+    keep = [None if g is None else torch.as_tensor(g).detach().cpu().float().contiguous()
+            for g in (q_gain, k_gain)]
+    _check(_lib.lmop_load_qk_norms(ctx, *(None if g is None else g.data_ptr() for g in keep), 0),
+           ctx)
 
 
 def lmop_set_prefix(ctx, tokens, parent=None):
@@ -633,6 +639,7 @@ class Context:
             pass
 
     def load_weights(self, weights):
+        _qk_norms(weights, self.heads[2])  # refused before anything is loaded
         lmop_load_weights(self.ctx, weights)
 
     def load_qk_norms(self, q_gain=None, k_gain=None):

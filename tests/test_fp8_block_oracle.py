@@ -113,6 +113,20 @@ def test_loading_on_a_host_ctx():
         ctx.load_weights(bad)
 
 
+@pytest.mark.parametrize("which,n", [("q_norm", 32), ("k_norm", 128), ("k_norm", 1)])
+def test_norms_of_another_length_load_nothing(which, n):
+    w = make_weights(TINY, seed=5, fmt="fp8_block", qk_norm=True)
+    setattr(w.layers[1], which, torch.ones(n))
+    ctx = L.Context(TINY, device=-1)
+    with pytest.raises(ValueError):
+        ctx.load_weights(w)
+    _expect(L.LMOP_ERR_STATE, ctx.load_qk_norms)
+    for l in w.layers:
+        l.q_norm = l.k_norm = torch.ones(n)
+    with pytest.raises(ValueError):
+        ctx.load_weights(w)
+
+
 @pytest.mark.parametrize("rows,dec", [(1, 1), (40, 1), (40, 4)])
 def test_plan_covers_block_scaled_passes(rows, dec):
     """The scratch of a plan holds the operand codes and the widest result of a pass."""
