@@ -48,17 +48,6 @@ LMOP_DEVICE f16x4 halves_of(uint32_t d) {
   return f16x4{a.x, a.y, b.x, b.y};
 }
 
-// bytes of a 16-byte chunk from `valid` on become zero (+0.0)
-LMOP_DEVICE uint4 keep_bytes(uint4 v, int valid) {
-  uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = valid - 4 * i;
-    w[i] = n >= 4 ? w[i] : n <= 0 ? 0u : w[i] & ((1u << (8 * n)) - 1);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 // A lane's 32 codes of one row and group: lane 16g + c holds features
 // 16g .. 16g+15 and 64+16g .. 64+16g+15 of row c.
 struct Codes {
@@ -68,10 +57,30 @@ struct Halves {
   f16x8 h[4];
 };
 
-// `valid` features left from the lane's first one on
-LMOP_DEVICE void keep_valid(Codes& c, int valid) {
-  c.w[0] = keep_bytes(c.w[0], valid);
-  c.w[1] = keep_bytes(c.w[1], valid - 64);
+// What is left of a lane's codes where `valid` features are left from its first
+// one on: the bytes from there on become zero (+0.0).
+struct Left {
+  uint4 w[2];
+};
+LMOP_DEVICE Left left_of(int valid) {
+  Left l;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = valid - 64 * h - 4 * i;
+      w[i] = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+    }
+    l.w[h] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return l;
+}
+LMOP_DEVICE void keep(Codes& c, const Left& l) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    c.w[h] = make_uint4(c.w[h].x & l.w[h].x, c.w[h].y & l.w[h].y, c.w[h].z & l.w[h].z,
+                        c.w[h].w & l.w[h].w);
 }
 
 // 8 of a lane's 32 codes as fp16
@@ -131,17 +140,38 @@ struct Rows {
   static constexpr int LDS = 16 * PITCH;       // of a wave
 };
 
-// every column is in the matrix, and 16-bit results have no `add`: 16 bytes a lane
-template <typename T, int NT, bool STREAM>
-LMOP_DEVICE void store_rows(const lmop_matmul_args& p, char* mine, int m, int n,
-                            const f32x4 (&v)[NT]) {
-  using R = Rows<NT>;
-  constexpr int W = 16 / sizeof(T), CHUNKS = R::COLS / W;
-  constexpr int PITCH = R::COLS * (int)sizeof(T) + 16;
-  typedef T T4 __attribute__((ext_vector_type(4)));
+// What a lane stores of 16 rows where every column is in the matrix: Q chunks of
+// 16 bytes, chunk q of row at(q) / CHUNKS.
+template <typename T, int NT>
+struct Chunks {
+  static constexpr int W = 16 / sizeof(T), CHUNKS = Rows<NT>::COLS / W, Q = (16 * CHUNKS + 63) / 64;
   typedef T Chunk __attribute__((ext_vector_type(W)));
   typedef Chunk Any __attribute__((aligned(sizeof(T))));
-  typedef f32x4 Any4 __attribute__((aligned(4)));
+  static LMOP_DEVICE int at(int q) { return q * 64 + (threadIdx.x & 63); }
+};
+
+// the chunks of `add` (fp32); rows past the matrix repeat its last one, so that
+// the loads of 16 rows are in flight together
+template <int NT>
+LMOP_DEVICE void load_add(const lmop_matmul_args& p, int m, int n,
+                          typename Chunks<float, NT>::Chunk (&v)[Chunks<float, NT>::Q]) {
+  using R = Chunks<float, NT>;
+#pragma unroll
+  for (int q = 0; q < R::Q; ++q) {
+    const int r = m + R::at(q) / R::CHUNKS, x = R::at(q) % R::CHUNKS;
+    v[q] = *(const typename R::Any*)(p.add + (size_t)(r < p.m ? r : p.m - 1) * p.ldadd + n +
+                                     R::W * x);
+  }
+}
+
+// every column is in the matrix, and 16-bit results have no `add`
+template <typename T, int NT, bool STREAM>
+LMOP_DEVICE void store_rows(const lmop_matmul_args& p, char* mine, int m, int n,
+                            const f32x4 (&v)[NT],
+                            const typename Chunks<T, NT>::Chunk (&add)[Chunks<T, NT>::Q]) {
+  using R = Chunks<T, NT>;
+  constexpr int PITCH = Rows<NT>::COLS * (int)sizeof(T) + 16;
+  typedef T T4 __attribute__((ext_vector_type(4)));
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   // the wave's earlier reads of these bytes are done
   wait_vmcnt_lgkm0<63>();
@@ -151,38 +181,47 @@ LMOP_DEVICE void store_rows(const lmop_matmul_args& p, char* mine, int m, int n,
         T4{(T)v[j][0], (T)v[j][1], (T)v[j][2], (T)v[j][3]};
   wait_vmcnt_lgkm0<63>();
 #pragma unroll
-  for (int q = 0; q < (16 * CHUNKS + 63) / 64; ++q) {
-    const int r = (q * 64 + lane) / CHUNKS, x = (q * 64 + lane) % CHUNKS;
+  for (int q = 0; q < R::Q; ++q) {
+    const int r = R::at(q) / R::CHUNKS, x = R::at(q) % R::CHUNKS;
     if (r < 16 && m + r < p.m) {
-      Chunk w = *(const Chunk*)(mine + r * PITCH + 16 * x);
+      typename R::Chunk w = *(const typename R::Chunk*)(mine + r * PITCH + 16 * x);
       if constexpr (std::is_same_v<T, float>)
-        if (p.add) w = *(const Any4*)(p.add + (size_t)(m + r) * p.ldadd + n + W * x) + w;
-      T* to = (T*)p.c + (size_t)(m + r) * p.ldc + n + W * x;
+        if (p.add) w = add[q] + w;
+      T* to = (T*)p.c + (size_t)(m + r) * p.ldc + n + R::W * x;
       if constexpr (STREAM)
-        __builtin_nontemporal_store(w, (Any*)to);
+        __builtin_nontemporal_store(w, (typename R::Any*)to);
       else
-        *(Any*)to = w;
+        *(typename R::Any*)to = w;
     }
   }
 }
 
-// any columns: a value a lane
+// any columns: a value a lane, the loads of 8 rounds in flight together
 template <typename T, int NT>
 LMOP_DEVICE void store_values(const lmop_matmul_args& p, char* mine, int m, int n,
                               const f32x4 (&v)[NT]) {
   using R = Rows<NT>;
+  constexpr int ROUNDS = 16 * R::COLS / 64, U = ROUNDS < 8 ? ROUNDS : 8;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   wait_vmcnt_lgkm0<63>();
 #pragma unroll
   for (int j = 0; j < NT; ++j) *(f32x4*)(mine + c * R::PITCH + (16 * j + 4 * g) * 4) = v[j];
   wait_vmcnt_lgkm0<63>();
 #pragma unroll
-  for (int q = 0; q < 16 * R::COLS / 64; ++q) {
-    const int r = (q * 64 + lane) / R::COLS, x = (q * 64 + lane) % R::COLS;
-    if (m + r < p.m && n + x < p.n) {
+  for (int q0 = 0; q0 < ROUNDS; q0 += U) {
+    float add[U];
+    if (p.add)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = (q0 + u) * 64 + lane, r = m + at / R::COLS, x = n + at % R::COLS;
+        add[u] = p.add[(size_t)(r < p.m ? r : p.m - 1) * p.ldadd + (x < p.n ? x : p.n - 1)];
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = (q0 + u) * 64 + lane, r = at / R::COLS, x = at % R::COLS;
       float w = *(const float*)(mine + r * R::PITCH + 4 * x);
-      if (p.add) w = p.add[(size_t)(m + r) * p.ldadd + n + x] + w;
-      ((T*)p.c)[(size_t)(m + r) * p.ldc + n + x] = (T)w;
+      if (p.add) w = add[u] + w;
+      if (m + r < p.m && n + x < p.n) ((T*)p.c)[(size_t)(m + r) * p.ldc + n + x] = (T)w;
     }
   }
 }
@@ -469,10 +508,11 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
   if (full < kb_n) {
     // the last features, less than a group: their stage is the last one loaded
     barrier();
-    const int valid = p.k - full * GROUP - 16 * g;
+    const Left left = left_of(p.k - full * GROUP - 16 * g);
+    const float sb_last = sb[full];
     auto masked = [&](int row, int i) {
       Codes x = codes(full, row, i);
-      keep_valid(x, valid);
+      keep(x, left);
       return operand<WHOLE>(x);
     };
     Operand<WHOLE> b[NT];
@@ -481,7 +521,7 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const Operand<WHOLE> a = masked(arow, i);
-      const float sc = scale(full, i) * sb[full];
+      const float sc = scale(full, i) * sb_last;
 #pragma unroll
       for (int j = 0; j < NT; ++j) add_scaled(acc[i][j], dot(b[j], a), sc);
     }
@@ -491,9 +531,17 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
   char* mine = smem + wave * Rows<NT>::LDS;
   const int n = n0 + wn * NT * 16;
   if (n + NT * 16 <= p.n && (std::is_same_v<T, float> || !p.add)) {
+    // the next 16 rows of `add` are on their way while these are stored
+    typename Chunks<T, NT>::Chunk add[2][Chunks<T, NT>::Q];
+    const int m = m0 + wm * MT * 16;
+    if constexpr (std::is_same_v<T, float>)
+      if (p.add) load_add<NT>(p, m, n, add[0]);
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-      store_rows<T, NT, STREAM>(p, mine, m0 + (wm * MT + i) * 16, n, acc[i]);
+    for (int i = 0; i < MT; ++i) {
+      if constexpr (std::is_same_v<T, float>)
+        if (p.add && i + 1 < MT) load_add<NT>(p, m + (i + 1) * 16, n, add[(i + 1) & 1]);
+      store_rows<T, NT, STREAM>(p, mine, m + i * 16, n, acc[i], add[i & 1]);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < MT; ++i) store_values<T, NT>(p, mine, m0 + (wm * MT + i) * 16, n, acc[i]);
@@ -567,11 +615,11 @@ __global__ __launch_bounds__(512, 2) void matmul_few_kernel(const lmop_matmul_ar
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int q = u * NW + wave, kb = rd * CH + q;
-      const int valid = p.k - kb * GROUP - 16 * g;
       if (kb == kb_n - 1) {
-        keep_valid(b[S][u], valid);
+        const Left left = left_of(p.k - kb * GROUP - 16 * g);
+        keep(b[S][u], left);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) keep_valid(a[S][u][i], valid);
+        for (int i = 0; i < MT; ++i) keep(a[S][u][i], left);
       }
       const Operand<WHOLE> bo = operand<WHOLE>(b[S][u]);
 #pragma unroll
@@ -631,7 +679,9 @@ __global__ __launch_bounds__(256) void matmul_empty_kernel(const lmop_matmul_arg
 // Results that the caches (256 MB at last) cannot keep until they are read are
 // streamed past them.  fp16 [m][28672], k 4096, and the quantisation that
 // reads it, us, streamed against not: 59 MB 131 / 129, 117 MB 257 / 260, 235 MB 484 /
-// 490, 940 MB 1910 / 1976.
+// 490, 940 MB 1910 / 1976.  Rows have to start at 64 bytes: two waves' stores
+// share the memory's words otherwise (16282 x 5533, k 359: 116 / 76; 16282 x 5536 of fp32: 125 /
+// 140).
 constexpr double kStreamBytes = 1e8;
 
 template <typename R, int TILE, bool STREAM>
@@ -659,7 +709,9 @@ template <typename R, int TILE>
 hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
   constexpr Fp8Tile t = kFp8Tiles[TILE];
   if constexpr (t.occ == 1) {  // the large tiles, which such results take
-    if ((double)a.m * a.n * sizeof(typename R::Type) > kStreamBytes)
+    constexpr size_t size = sizeof(typename R::Type);
+    if ((double)a.m * a.n * size > kStreamBytes && (uintptr_t)a.c % 64 == 0 &&
+        a.ldc * size % 64 == 0)
       return launch_tile_kernel<R, TILE, true>(s, a);
   }
   return launch_tile_kernel<R, TILE, false>(s, a);

@@ -51,6 +51,16 @@ MEASURED = [
     (0, 16, 28672, 4096, {2: 28.6, 3: 27.2, 4: 26.6, 5: 35.6}),
     (0, 128, 28672, 4096, {2: 41.2, 3: 46.6, 4: 57.8}),
     (0, 24, 2048, 2048, {3: 7.2, 4: 7.0, 6: 5.1}),
+    (0, 64, 768, 6272, {2: 22.0, 3: 16.2, 4: 15.2, 6: 11.8}),
+    (1, 64, 768, 6272, {2: 36.0, 3: 24.5, 4: 22.9, 6: 12.3}),
+    (0, 64, 2048, 4096, {2: 15.3, 3: 11.5, 4: 10.9, 6: 8.4}),
+    (1, 64, 2048, 4096, {2: 24.9, 3: 17.3, 4: 16.2, 6: 8.8}),
+    (0, 48, 1536, 14336, {2: 57.4, 3: 40.1, 4: 32.2, 6: 23.3}),
+    (0, 48, 4096, 4096, {2: 18.7, 3: 13.4, 4: 11.6, 6: 14.3}),
+    (1, 48, 4096, 4096, {2: 26.0, 3: 17.8, 4: 16.8, 6: 14.6}),
+    (0, 128, 768, 4096, {2: 15.3, 3: 11.5, 4: 10.9, 6: 8.3}),
+    (1, 128, 768, 4096, {2: 24.9, 3: 17.3, 4: 16.2, 6: 8.7}),
+    (0, 128, 2048, 2048, {2: 9.1, 3: 7.2, 4: 7.0, 6: 8.3}),
     (0, 512, 4096, 4096, {0: 60.1, 1: 35.5, 2: 19.4, 3: 21.2}),
     (1, 256, 4096, 4096, {1: 53.4, 2: 26.6, 3: 18.4, 4: 24.0}),
     (1, 512, 4096, 4096, {1: 54.2, 2: 27.4, 3: 27.3, 4: 43.9}),
