@@ -443,7 +443,7 @@ typedef struct {
                            the next multiple of 16 are read and have no effect */
   int64_t ldas, ldbs;   /* >= ceil(k / 128); ldas at most 2^21 */
   int64_t ldadd, ldc;   /* >= n */
-  int32_t m, n, k;      /* k = 0: C = add, or zero */
+  int32_t m, n, k;      /* m and n at most 2^30; k = 0: C = add, or zero */
   int32_t dtype;        /* LMOP_F16, LMOP_BF16 or LMOP_F32 */
   int32_t fast;         /* 1: products cut in fp32 results too, at up to twice the rate; else 0 */
 } lmop_matmul_args;

@@ -31,19 +31,23 @@ constexpr int kNumFp8Kernels = kNumFp8Tiles + 2;
 // Estimated us.  Tiles: rounds over the 256 CUs, at least the time in which
 // the weight comes from memory (4.4 TB/s), and 3 us around them.  Few tokens:
 // 4 us and a time per group, a fixed one or one per tile that grows with the
-// tokens (their codes are read again for every 16 columns).  Measured, us, few against the best tile:
-//   1 token:   n 6144 k 4096: 8.5 / 12.4, n 4096 k 14336: 12.9 / 33, n 28672 k 4096: 22.7 / 26.8
+// tokens (their codes are read again for every 16 columns).  Measured, us, few
+// against the best tile (whole products in brackets):
+//   1 token:   n 6144 k 4096 8.5 / 12.4, n 4096 k 14336 12.9 / 33, n 28672 k 4096 22.7 / 26.8
 //   16 tokens: 11.7 / 11.8, 18.6 / 32.3, 35.6 / 26.6
-//   24 tokens: 14.6 / 12.1, 23.8 / 32.6, 44.2 / 27.9;  n 2048 k 2048: 5.1 / 7.1
-//   more tokens, in parts of 32: 64, n 6144 k 4096 22.3 / 12.3, n 4096 k 14336 46.6 / 32.8, n 768 k 6272
-//   11.8 / 15.2 (whole products 12.3 / 22.9), n 2048 k 4096 8.4 / 10.9 (8.8 / 16.2); 48, n 4096
-//   k 4096 14.3 / 11.6 (14.6 / 16.8); 128, n 768 k 4096 8.3 / 10.9, n 2048 k 2048 8.3 / 7.0
-// and of the tiles, 16-bit results (fp32): 256 x 4096, k 4096: 32 x 64 17.1 (24.0), 64 x 64
-// 14.5 (18.4), 64 x 128 19.2 (26.6); 512 x 4096, k 4096: 32 x 64 31.7 (43.9), 64 x 64 20.8
-// (27.3), 64 x 128 19.6 (27.4), 128 x 256 35.4 (54.2), 256 x 256 60.0; 2047 x 4096, k 4096: 64 x 64
-// 71.9 (95.8), 64 x 128 57.0 (81.0), 128 x 256 40.8 (62.5), 256 x 256 62.3; 16384 x 4096, k 14336:
-// 64 x 128 1266 (1926), 128 x 256 902 (1526), 256 x 256 772; 16384 x 28672, k 4096: 128 x 256
-// 1868, 256 x 256 1645.
+//   24 tokens: 14.6 / 12.1, 23.8 / 32.6, 44.2 / 27.9; n 2048 k 2048 5.1 / 7.1
+//   48 tokens: n 4096 k 4096 14.3 / 11.6 (14.6 / 16.8), n 1536 k 14336 23.3 / 32.2
+//   64 tokens: n 6144 k 4096 22.3 / 12.3, n 4096 k 14336 46.6 / 32.8, n 768 k 6272 11.8 / 15.2
+//              (12.3 / 22.9), n 2048 k 4096 8.4 / 10.9 (8.8 / 16.2)
+//   128:       n 768 k 4096 8.3 / 10.9 (8.7 / 16.2), n 2048 k 2048 8.3 / 7.0
+// and of the tiles:
+//   256 x 4096, k 4096: 32 x 64 17.1 (24.0), 64 x 64 14.5 (18.4), 64 x 128 19.2 (26.6)
+//   512 x 4096, k 4096: 32 x 64 31.7 (43.9), 64 x 64 20.8 (27.3), 64 x 128 19.6 (27.4),
+//     128 x 256 35.4 (54.2), 256 x 256 60.0
+//   2047 x 4096, k 4096: 64 x 64 71.9 (95.8), 64 x 128 57.0 (81.0), 128 x 256 40.8 (62.5),
+//     256 x 256 62.3
+//   16384 x 4096, k 14336: 64 x 128 1266 (1926), 128 x 256 902 (1526), 256 x 256 772
+//   16384 x 28672, k 4096: 128 x 256 1868, 256 x 256 1645
 inline float fp8_cost(int kernel, bool whole, int m, int n, int k) {
   const float groups = (k + 127) / 128;
   if (kernel >= kNumFp8Tiles) {

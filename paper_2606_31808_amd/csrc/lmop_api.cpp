@@ -2846,7 +2846,8 @@ lmop_status lmop_matmul(lmop_ctx* ctx, const lmop_matmul_args* a) {
   if (a->fast != 0 && a->fast != 1)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "fast is %d (0 or 1)", a->fast);
   if (a->m == 0 || a->n == 0) return LMOP_OK;
-  if ((uint64_t)((a->m + 15ll) / 16) * ((a->n + 15ll) / 16) > kMaxTasks)
+  if ((uint64_t)a->m > kMaxTasks || (uint64_t)a->n > kMaxTasks ||
+      (uint64_t)((a->m + 15ll) / 16) * ((a->n + 15ll) / 16) > kMaxTasks)
     return fail(ctx, LMOP_ERR_UNSUPPORTED, "%d x %d is too large for one call", a->m, a->n);
   if (a->k > 0) {
     LMOP_TRY(check_codes(ctx, "a", a->a, a->k, a->lda));

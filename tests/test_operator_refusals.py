@@ -108,6 +108,15 @@ def test_qk_norm_rope(ctx, change, status):
     assert _call(ctx, "lmop_qk_norm_rope", _args(L.lmop_qk_norm_rope_args, QK, **change)) == status
 
 
+@pytest.mark.parametrize("m,n,refused", [(2 ** 30, 16, False), (2 ** 30 + 1, 1, True), (2 ** 31 - 1, 1, True),
+                                         (1, 2 ** 31 - 1, True), (16, 2 ** 30, False),
+                                         (2 ** 30, 256, False), (2 ** 30, 257, True)])
+def test_matmul_size_limits(ctx, m, n, refused):
+    a = _args(L.lmop_matmul_args, MM, m=m, n=n, ldc=n)
+    assert _call(ctx, "lmop_matmul", a) == UNS
+    assert ("too large" in L._lib.lmop_last_error(ctx.ctx).decode()) == refused
+
+
 @pytest.mark.parametrize("name", ["lmop_quantize", "lmop_matmul", "lmop_qk_norm_rope"])
 def test_null(ctx, name):
     assert _call(ctx, name, None) == INV
