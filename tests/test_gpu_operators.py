@@ -638,3 +638,34 @@ def test_other_users_keep_their_results(L):
     b, _ = ctx.eval_rows(wl.tokens, wl.offsets, wl.kind, wl.allowed, prefix=pre)
     assert a.tobytes() == b.tobytes()
     assert torch.equal(c, ctx.matmul(q, s, _codes(300, 256, 1), _scales(3, 2, 2), dtype=torch.float32))
+
+
+# ---------------------------------------------------------------- the gate at any size
+def test_quantize_gate_is_as_exact_at_any_size(ctx):
+    """A row of one feature has |y| / 448 as its scale.  x * silu(gate) is known there within
+    12 roundings of 2^-24: the exponential (the instruction's 2, its correction 1, what is left
+    of the exponent 1), the sum (1), the reciprocal (2), two products (2), the scale's division
+    and the product that undoes it here (2), and one more of the last bits of log2 e."""
+    x = 2.0 ** 70 * (1 + torch.rand(8001, 1, generator=_gen(1)))
+    gate = torch.linspace(-84, 84, 8001).view(-1, 1)
+    _, s = ctx.quantize(x.cuda(), gate=gate.cuda())
+    z = gate.double()
+    y = (x.double() * z * torch.sigmoid(z)).abs().clamp(min=2.0 ** -40)
+    off = (s.double().cpu() * 448 / y - 1).abs()
+    assert off.max() <= 12 * 2.0 ** -24, off.max() / 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_gate_extremes(ctx, dtype):
+    """Gates whose silu is zero in the type, the largest gates, infinities and NaN."""
+    dt = DT[dtype]
+    x = torch.tensor([1.0, 2.0 ** 20, 1.0, 2.0 ** -60, 2.0 ** -60, 0.0, 1.0, 1.0, 1.0])
+    z = torch.tensor([-100.0, -250.0, -3e38, 1e9, 3e38, 3e38, float("inf"), float("-inf"), float("nan")])
+    x, z = x.to(dt).view(-1, 1), z.to(dt).view(-1, 1)
+    q, s = ctx.quantize(x.cuda(), gate=z.cuda())
+    q, s = q.float().cpu().view(-1), s.double().cpu().view(-1)
+    y = (x.double() * z.double() / (1 + (-z.double()).exp())).view(-1)[:6]
+    want = y.abs().clamp(min=2.0 ** -40) / 448
+    assert torch.all((s[:6] / want - 1).abs() <= 12 * 2.0 ** -24)
+    assert torch.equal(q[:6], torch.where(y.abs() >= 2.0 ** -40, 448 * y.sign(), torch.zeros(6).double()).float())
+    assert torch.isnan(q[6:]).all() and torch.isnan(s[6:]).all()
