@@ -186,7 +186,9 @@ hipError_t launch_head_finalize(hipStream_t s, const float2* part, int n_chunks,
 
 // ---------------------------------------------------------------- block-scaled FP8 maps
 // The operators of include/lmop.h, with its argument structs: sizes above
-// zero, pointers and strides checked by the caller.
+// zero, pointers and strides checked by the caller.  A call of more threads than
+// HIP launches at a time (fewer than 2^32) is several launches.
+constexpr size_t kMaxLaunchThreads = ((size_t)1 << 32) - 1;
 hipError_t launch_quantize(hipStream_t s, const lmop_quantize_args& a);
 hipError_t launch_matmul_fp8(hipStream_t s, const lmop_matmul_args& a);
 struct QkArgs {

@@ -11,7 +11,7 @@
 #include "common.h"
 #include "kernels.h"
 
-#include <type_traits>
+#include <algorithm>
 
 namespace lmop {
 
@@ -111,12 +111,23 @@ __global__ __launch_bounds__(256) void quantize_kernel(const lmop_quantize_args 
 template <typename T>
 hipError_t launch(hipStream_t s, const lmop_quantize_args& a) {
   const size_t groups = ((size_t)a.cols + LMOP_FP8_GROUP - 1) / LMOP_FP8_GROUP;
-  const size_t tasks = a.rows * groups;
-  if (tasks > 0xFFFFFFE0u) return hipErrorInvalidValue;
   auto* k = a.gate ? quantize_kernel<T, true> : quantize_kernel<T, false>;
-  hipLaunchKernelGGL(k, dim3((unsigned)((tasks + 31) / 32)), dim3(256), 0, s, a, (uint32_t)groups,
-                     (uint32_t)tasks);
-  return hipGetLastError();
+  const int most = (int)std::min<size_t>(kMaxLaunchThreads / 256 * 32 / groups, a.rows);
+  if (most == 0) return hipErrorInvalidValue;
+  for (int done = 0, rows; done < a.rows; done += rows) {
+    rows = std::min(most, a.rows - done);
+    lmop_quantize_args p = a;
+    p.x = (const T*)a.x + (size_t)done * a.ldx;
+    if (a.gate) p.gate = (const T*)a.gate + (size_t)done * a.ldg;
+    p.q = a.q + (size_t)done * a.ldq;
+    p.scale = a.scale + (size_t)done * a.lds;
+    const size_t tasks = rows * groups;
+    hipLaunchKernelGGL(k, dim3((unsigned)((tasks + 31) / 32)), dim3(256), 0, s, p, (uint32_t)groups,
+                       (uint32_t)tasks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

@@ -669,3 +669,13 @@ def test_quantize_gate_extremes(ctx, dtype):
     assert torch.all((s[:6] / want - 1).abs() <= 12 * 2.0 ** -24)
     assert torch.equal(q[:6], torch.where(y.abs() >= 2.0 ** -40, 448 * y.sign(), torch.zeros(6).double()).float())
     assert torch.isnan(q[6:]).all() and torch.isnan(s[6:]).all()
+
+
+# ---------------------------------------------------------------- more threads than one launch has
+def test_quantize_more_groups_than_a_launch(ctx):
+    """2^29 groups and some (8 threads each: 2^32), which HIP does not launch at a time."""
+    n, base = 2 ** 29 + 77, torch.randn(4099, 1, generator=_gen(3)).half().cuda()
+    few_q, few_s = ctx.quantize(base)
+    q, s = ctx.quantize(base.repeat(n // 4099 + 1, 1)[:n])
+    assert torch.equal(s, few_s.repeat(n // 4099 + 1, 1)[:n])
+    assert torch.equal(q.view(torch.uint8), few_q.view(torch.uint8).repeat(n // 4099 + 1, 1)[:n])
