@@ -689,7 +689,6 @@ hipError_t launch_tile_kernel(hipStream_t s, const lmop_matmul_args& a) {
   constexpr Fp8Tile t = kFp8Tiles[TILE];
   using C = Tile<t.mt, t.nt, t.wm, t.wn, t.occ>;
   const size_t tiles = (size_t)((a.m + C::BM - 1) / C::BM) * ((a.n + C::BN - 1) / C::BN);
-  if (tiles > 0x3fffffffu) return hipErrorInvalidValue;
   auto* k = matmul_tile_kernel<R, t.mt, t.nt, t.wm, t.wn, t.occ, STREAM>;
   // more than 64 KB of LDS: asked for once on each device
   static std::atomic<uint64_t> raised{0};
@@ -720,21 +719,13 @@ hipError_t launch_tile(hipStream_t s, const lmop_matmul_args& a) {
 template <typename R, int MT, int U>
 hipError_t launch_few(hipStream_t s, const lmop_matmul_args& a) {
   const size_t tiles = (size_t)((a.m + 16 * MT - 1) / (16 * MT)) * ((a.n + 15) / 16);
-  if (tiles > 0x7fffffffu) return hipErrorInvalidValue;
   hipLaunchKernelGGL((matmul_few_kernel<R, MT, U>), dim3((unsigned)tiles), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename R>
-hipError_t launch(hipStream_t s, const lmop_matmul_args& a) {
-  if (a.k == 0) {
-    const size_t blocks = ((size_t)a.m * a.n + 255) / 256;
-    if (blocks > 0x7fffffffu) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(matmul_empty_kernel<typename R::Type>, dim3((unsigned)blocks), dim3(256), 0,
-                       s, a);
-    return hipGetLastError();
-  }
-  switch (pick_fp8_kernel(R::WHOLE, a.m, a.n, a.k)) {
+hipError_t launch_part(hipStream_t s, int kernel, const lmop_matmul_args& a) {
+  switch (kernel) {
     case 0:
       if constexpr (!R::WHOLE) return launch_tile<R, 0>(s, a);
       return hipErrorInvalidValue;  // not offered
@@ -745,6 +736,37 @@ hipError_t launch(hipStream_t s, const lmop_matmul_args& a) {
     case kFp8Few16: return launch_few<R, 1, 2>(s, a);
     default: return launch_few<R, 2, 1>(s, a);
   }
+}
+
+template <typename R>
+hipError_t launch_empty(hipStream_t s, const lmop_matmul_args& a) {
+  const size_t blocks = ((size_t)a.m * a.n + 255) / 256;
+  hipLaunchKernelGGL(matmul_empty_kernel<typename R::Type>, dim3((unsigned)blocks), dim3(256), 0,
+                     s, a);
+  return hipGetLastError();
+}
+
+template <typename R>
+hipError_t launch(hipStream_t s, const lmop_matmul_args& a) {
+  using T = typename R::Type;
+  const int kernel = a.k > 0 ? pick_fp8_kernel(R::WHOLE, a.m, a.n, a.k) : -1;
+  const int most = kernel < 0
+                       ? (int)std::min<size_t>(a.m, kMaxLaunchThreads / 256 * 256 / a.n)
+                       : fp8_rows(kernel, a.m, a.n);
+  if (most == 0) return hipErrorInvalidValue;
+  for (int done = 0; done < a.m; done += most) {
+    lmop_matmul_args p = a;
+    p.m = std::min(most, a.m - done);
+    p.c = (T*)a.c + (size_t)done * a.ldc;
+    if (a.add) p.add = a.add + (size_t)done * a.ldadd;
+    if (a.k > 0) {
+      p.a = a.a + (size_t)done * a.lda;
+      p.a_scale = a.a_scale + (size_t)done * a.ldas;
+    }
+    const hipError_t e = kernel < 0 ? launch_empty<R>(s, p) : launch_part<R>(s, kernel, p);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

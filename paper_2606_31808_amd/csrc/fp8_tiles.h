@@ -2,6 +2,7 @@
 // C++, so that the host can check which call takes which.
 #pragma once
 #include <algorithm>
+#include <cstdint>
 
 namespace lmop {
 
@@ -28,6 +29,25 @@ constexpr int kNumFp8Tiles = sizeof(kFp8Tiles) / sizeof(kFp8Tiles[0]);
 constexpr int kFp8Few16 = kNumFp8Tiles, kFp8Few32 = kNumFp8Tiles + 1;
 constexpr int kNumFp8Kernels = kNumFp8Tiles + 2;
 
+// tokens, columns and threads of a kernel's workgroup
+struct Fp8Group {
+  int bm, bn, threads;
+};
+constexpr Fp8Group fp8_group(int kernel) {
+  if (kernel >= kNumFp8Tiles) return {kernel == kFp8Few32 ? 32 : 16, 16, 512};
+  const Fp8Tile& t = kFp8Tiles[kernel];
+  return {t.bm(), t.bn(), 64 * t.wm * t.wn};
+}
+
+// The most tokens of one launch, whole tiles of them: HIP launches fewer than
+// 2^32 threads at a time.  Zero where one row of tiles is too many: the kernel
+// is then not picked (one of 128 columns and 256 threads serves 2^30 columns).
+inline int fp8_rows(int kernel, int m, int n) {
+  const Fp8Group g = fp8_group(kernel);
+  const int64_t most = ((int64_t(1) << 32) - 1) / g.threads, across = (n + g.bn - 1) / g.bn;
+  return (int)std::min<int64_t>(m, most / across * g.bm);
+}
+
 // Estimated us.  Tiles: rounds over the 256 CUs, at least the time in which
 // the weight comes from memory (4.4 TB/s), and 3 us around them.  Few tokens:
 // 4 us and a time per group, a fixed one or one per tile that grows with the
@@ -50,6 +70,7 @@ constexpr int kNumFp8Kernels = kNumFp8Tiles + 2;
 //   16384 x 28672, k 4096: 128 x 256 1868, 256 x 256 1645
 inline float fp8_cost(int kernel, bool whole, int m, int n, int k) {
   const float groups = (k + 127) / 128;
+  if (n >= 1 << 26 && fp8_rows(kernel, m, n) == 0) return 1e30f;
   if (kernel >= kNumFp8Tiles) {
     const bool wide = kernel == kFp8Few32;
     if (!wide && m > 16) return 1e30f;

@@ -46,8 +46,8 @@ constexpr int kMaxBatchBudget = 1 << 21;
 // longest row of FP8 codes: a tile's row offsets fit 32 bits
 constexpr int64_t kMaxCodeRow = int64_t(1) << 23;
 constexpr int64_t kMaxScaleRow = int64_t(1) << 21;  // and of the tokens' scales
-// the most 16 x 16 tiles, groups or heads of one operator call: grid and index
-// arithmetic stay within 31 bits
+// the most 16 x 16 tiles, groups or heads of one operator call: index
+// arithmetic stays within 31 bits
 constexpr uint64_t kMaxTasks = uint64_t(1) << 30;
 
 int round_up(int x, int m) { return (x + m - 1) / m * m; }

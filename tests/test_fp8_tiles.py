@@ -102,3 +102,46 @@ def test_helpers_keep_the_wait_state(tmp_path):
     at = next(i for i, l in enumerate(lines) if l.startswith("global_load_lds_dword "))
     assert re.match(r"s_\w+ m0,", lines[at - 2]) and not re.match(r"s_\w+ m0,", lines[at - 1])
     assert lines[at + 1].startswith("s_mov_b64 exec, -1")
+
+
+LIMITS = """
+#include "fp8_tiles.h"
+extern "C" int pick(int f32, int m, int n, int k) { return lmop::pick_fp8_kernel(f32, m, n, k); }
+extern "C" int rows(int kernel, int m, int n) { return lmop::fp8_rows(kernel, m, n); }
+extern "C" void group(int kernel, int* out) {
+  const lmop::Fp8Group g = lmop::fp8_group(kernel);
+  out[0] = g.bm, out[1] = g.bn, out[2] = g.threads;
+}
+"""
+
+
+def test_every_launch_is_one_that_hip_makes(tmp_path):
+    """The launches of a call have fewer than 2^32 threads each and whole tiles, for the kernel
+    that the rule picks, at sizes up to the accepted limits (2^30 tiles of 16 x 16)."""
+    if not shutil.which("g++"):
+        pytest.skip("no g++")
+    (tmp_path / "l.cpp").write_text(LIMITS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{build.CSRC}",
+                    str(tmp_path / "l.cpp"), "-o", str(tmp_path / "l.so")], check=True)
+    lib, out = C.CDLL(str(tmp_path / "l.so")), (C.c_int * 3)()
+    ends = [2 ** i + d for i in range(30) for d in (-1, 0, 1)] + [2 ** 30 - 1, 2 ** 30]
+    ends = sorted({x for x in ends if x > 0})
+    several = 0
+    for f32 in (0, 1):
+        for k in (1, 128, 4096, 14336, 2 ** 23):
+            for n in ends:
+                # every order of magnitude of tokens that is accepted beside n columns
+                most = min(2 ** 30, (2 ** 30 // -(-n // 16)) * 16)
+                for m in {1, 16, 17, 32, 33, 64, 300, 2000, most // 3, most - 1, most}:
+                    if not 0 < m <= most:
+                        continue
+                    kernel = lib.pick(f32, m, n, k)
+                    lib.group(kernel, out)
+                    bm, bn, threads = out
+                    rows = lib.rows(kernel, m, n)
+                    assert 0 < rows <= m and (rows == m or rows % bm == 0), (m, n, k, kernel)
+                    assert -(-rows // bm) * -(-n // bn) * threads < 2 ** 32, (m, n, k, kernel)
+                    # what fits is one launch
+                    assert rows == m or -(-m // bm) * -(-n // bn) * threads >= 2 ** 32
+                    several += rows != m
+    assert several

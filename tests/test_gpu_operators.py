@@ -679,3 +679,27 @@ def test_quantize_more_groups_than_a_launch(ctx):
     q, s = ctx.quantize(base.repeat(n // 4099 + 1, 1)[:n])
     assert torch.equal(s, few_s.repeat(n // 4099 + 1, 1)[:n])
     assert torch.equal(q.view(torch.uint8), few_q.view(torch.uint8).repeat(n // 4099 + 1, 1)[:n])
+
+
+@pytest.mark.parametrize("m,n,dtype", [(2 ** 30, 16, "f16"), (2 ** 30 - 5, 1, "f32")])
+def test_matmul_more_tiles_than_a_launch(ctx, m, n, dtype):
+    """2^24 tiles of 256 threads."""
+    print("large", m, n, dtype, flush=True)
+    k, few = 16, 4099
+    a, b = _codes(few, k, 1, pad=0), _codes(n, k, 2, pad=0)
+    sa, sb = _scales(few, 1, 3, pad=0), _scales(1, 1, 4, pad=0)
+    want = ctx.matmul(a, sa, b, sb, dtype=DT[dtype])
+    times = -(-m // few)
+    c = ctx.matmul(a.view(torch.uint8).repeat(times, 1)[:m].view(F8), sa.repeat(times, 1)[:m], b, sb,
+                   dtype=DT[dtype])
+    assert torch.equal(c, want.repeat(times, 1)[:m])
+
+
+def test_matmul_more_values_than_a_launch(ctx):
+    """No features: more than 2^32 results."""
+    m, n = 65541, 65536
+    a, sa = torch.empty(m, 0, dtype=F8, device="cuda"), torch.empty(m, 0, device="cuda")
+    b, sb = torch.empty(n, 0, dtype=F8, device="cuda"), torch.empty(n // G, 0, device="cuda")
+    c = torch.full((m, n), 9.0, dtype=torch.float16, device="cuda")
+    ctx.matmul(a, sa, b, sb, out=c)
+    assert not c.any()
