@@ -396,7 +396,7 @@ lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t 
  * lies between rows is not written.  An output may not overlap an input
  * unless said.  A size of zero is a no-op.  Results do not depend on which
  * other rows are in the call, bit for bit.  A call is limited to 2^30 tiles of
- * 16 x 16 results, groups, or heads. */
+ * 16 x 16 results, groups, or heads (of tokens counted in 64s). */
 typedef enum { LMOP_F16 = 0, LMOP_BF16 = 1, LMOP_F32 = 2 } lmop_dtype;
 
 /* Features that share one scale. */

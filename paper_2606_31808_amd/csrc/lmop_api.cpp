@@ -2881,7 +2881,9 @@ lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* a) {
   if (a->v_layout != LMOP_V_ROWS && a->v_layout != LMOP_V_COLUMNS)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown v_layout %d", a->v_layout);
   if (a->n_tokens == 0 || (!a->q && !a->k && !a->v)) return LMOP_OK;
-  if ((uint64_t)a->n_tokens * (ctx->cfg.n_heads + 2ll * ctx->cfg.n_kv_heads) > kMaxTasks)
+  // tokens in 64s: the workgroups that transpose values take that many
+  if (((uint64_t)a->n_tokens + 63) / 64 * 64 * (ctx->cfg.n_heads + 2ll * ctx->cfg.n_kv_heads) >
+      kMaxTasks)
     return fail(ctx, LMOP_ERR_UNSUPPORTED, "%d tokens are too many for one call", a->n_tokens);
   if ((a->k || a->v) && !a->slot && a->n_slots < a->n_tokens)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "%d tokens without slots, %d slots", a->n_tokens,

@@ -190,7 +190,7 @@ hipError_t launch(hipStream_t s, const QkArgs& a) {
   const int chunks = (long)p.n_tokens * all <= 10240 ? 1 : all, splits = all / chunks;
   const long want = ((long)p.n_tokens * splits + kWaves - 1) / kWaves;
   const long blocks = (!p.q && !p.k && (columns || !p.v)) ? 0 : want < 65536 ? want : 65536;
-  if (value_blocks + blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if ((size_t)(value_blocks + blocks) * 64 * kWaves > kMaxLaunchThreads) return hipErrorInvalidValue;
   hipLaunchKernelGGL((qk_norm_rope_kernel<T, HD>), dim3((unsigned)(value_blocks + blocks)),
                      dim3(64 * kWaves), 0, s, a, (int)value_blocks, chunks, splits);
   return hipGetLastError();

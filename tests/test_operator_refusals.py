@@ -164,3 +164,16 @@ def test_binding_refuses(ctx):
     with pytest.raises(ValueError):  # a tensor of another device
         L.Context(dataclasses.replace(SHAPES["tiny"]), device=-1).quantize(
             torch.empty(3, 200, dtype=torch.float16, device="meta"))
+
+
+@pytest.mark.parametrize("tokens,heads,refused", [(1, 2 ** 23, True), (64, 2 ** 23, True), (64, 2 ** 22, False),
+                                                  (1, 2 ** 22, False), (2 ** 22, 64, False)])
+def test_qk_norm_rope_heads_fit_a_launch(tokens, heads, refused):
+    """Values written as columns take heads * head_dim / 64 workgroups of 256 threads for each 64
+    tokens: 2^24 of them are more threads than HIP launches at a time."""
+    c = L.Context(dataclasses.replace(SHAPES["tiny"], n_heads=heads, n_kv_heads=heads, head_dim=128), device=-1)
+    row = heads * 128
+    a = _args(L.lmop_qk_norm_rope_args, QK, n_tokens=tokens, n_slots=tokens, v_layout=L.LMOP_V_COLUMNS, ldvo=tokens,
+              **{f: row for f in ("ldq", "ldk", "ldv", "ldqo", "ldko")})
+    assert _call(c, "lmop_qk_norm_rope", a) == UNS
+    assert ("too many" in L._lib.lmop_last_error(c.ctx).decode()) == refused
