@@ -148,10 +148,13 @@ struct lmop_ctx {
   std::vector<LayerW> layers;
   std::vector<void*> weight_allocs;
   float2* rope_tab = nullptr;
-  // lmop_load_qk_norms: the layers' gains, and a rotation by nothing for the
-  // QKV epilogue of the packed formats (the norms come before the rotation)
+  // the layers' query and key gains of lmop_load_qk_norms (allocated with the
+  // weights), whether they are in use, and behind them a rotation by nothing for
+  // the QKV epilogue of the packed formats (the norms come before the rotation):
+  // one position's row, which every token reads
   float* qk_gain = nullptr;
-  float2* no_rope = nullptr;
+  bool normed = false;
+  const float2* no_rope = nullptr;
 
   // library-allocated scratch: named grow-only buffers
   std::map<std::string, std::pair<void*, size_t>> ws;
@@ -632,9 +635,9 @@ void free_weights(lmop_ctx* c) {
   c->emb = c->head = nullptr;
   c->final_norm = nullptr;
   (void)dev_free(c, c->qk_gain);
-  (void)dev_free(c, c->no_rope);
   c->qk_gain = nullptr;
   c->no_rope = nullptr;
+  c->normed = false;
 }
 
 bool block_format(const lmop_ctx* c) { return c->wfmt == LMOP_W_FP8_BLOCK; }
@@ -884,6 +887,7 @@ std::vector<std::pair<const char*, size_t>> scratch_items(const lmop_ctx* c, con
     add("wide", T * std::max(qkv_width(c), gu_width(c)) * 2);
   } else {
     add("act", T * c->f64 * 2);
+    if (c->normed) add("no_pos", T * 4);
   }
   add("xlast", n.last * d * 4);
   add("own_kv", n.own_kv);
@@ -1116,6 +1120,11 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
   } else {
     LMOP_TRY(ws_get(c, "act", (size_t)T * c->f64, &act));
   }
+  int32_t* no_pos = nullptr;
+  if (!blocks && c->normed) {
+    LMOP_TRY(ws_get(c, "no_pos", (size_t)T, &no_pos));
+    HIP_OK(c, launch_fill_u32(c->stream, no_pos, (size_t)T, 0u));
+  }
   // Block-scaled maps: rows of fp16 (or silu(gate) * x of them) to codes, and
   // codes through a map, the result fp16 in `wide` or added to the fp32 rows `x32`.
   auto quantize = [&](const uint16_t* in, int64_t ld, const uint16_t* gate, int rows, int cols) {
@@ -1209,10 +1218,10 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
       ga.M = rows;
       ga.N = round_up(c1, 256) - c0;
       ga.K = L.qkv.kp;
-      ga.pos = pos;
-      ga.slot = b.slot;
       // query and key norms come before the rotation, in a pass of their own
-      ga.rope = L.q_gain ? c->no_rope : c->rope_tab;
+      ga.pos = no_pos ? no_pos : pos;
+      ga.slot = b.slot;
+      ga.rope = no_pos ? c->no_rope : c->rope_tab;
       ga.qout = q;
       ga.kc = kc;
       ga.vt = vt;
@@ -1259,7 +1268,7 @@ lmop_status forward(lmop_ctx* c, const Batch& b) {
     } else {
       LMOP_TRY(qkv(h, T, b.pos, 0, L.qkv.n));
     }
-    if (!blocks && L.q_gain) {
+    if (no_pos) {
       // in place: the queries that were computed, every token's key in its slot
       QkArgs a{};
       a.t.q = a.t.q_out = q;
@@ -1812,6 +1821,7 @@ lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w) {
     release_all_prefixes(ctx);
     ctx->generation++;
     ctx->wfmt = (uint32_t)w->format;
+    ctx->normed = false;
     ctx->loaded = true;
     return LMOP_OK;
   }
@@ -1849,6 +1859,16 @@ lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w) {
   }
   LMOP_TRY(upload(ctx, w->final_norm, (size_t)d * 4, od, &p));
   ctx->final_norm = (float*)p;
+  {  // room for query and key norms: loading them cannot run out of memory
+    const size_t gains = 2 * (size_t)cf.n_layers * cf.head_dim;
+    const std::vector<float2> one(cf.head_dim / 2, make_float2(1.f, 0.f));
+    LMOP_TRY(dev_alloc(ctx, &p, gains * 4 + one.size() * sizeof(float2)));
+    ctx->qk_gain = (float*)p;
+    ctx->no_rope = (const float2*)(ctx->qk_gain + gains);
+    HIP_OK(ctx, hipMemcpyAsync(ctx->qk_gain + gains, one.data(), one.size() * sizeof(float2),
+                               hipMemcpyHostToDevice, ctx->stream));
+    HIP_OK(ctx, hipStreamSynchronize(ctx->stream));
+  }
   ctx->layers.resize(cf.n_layers);
   for (int l = 0; l < cf.n_layers; ++l) {
     const lmop_layer& L = w->layers[l];
@@ -1923,23 +1943,11 @@ lmop_status lmop_load_qk_norms(lmop_ctx* ctx, const float* q_gain, const float* 
   if (!ctx->host_only) HIP_OK(ctx, hipStreamSynchronize(ctx->stream));
   release_all_prefixes(ctx);
   ctx->generation++;
+  ctx->normed = q_gain && cf.n_layers > 0;
   if (ctx->host_only) return LMOP_OK;
   for (LayerW& L : ctx->layers) L.q_gain = L.k_gain = nullptr;
-  if (!q_gain || cf.n_layers == 0) return LMOP_OK;
+  if (!ctx->normed) return LMOP_OK;
   const size_t n = (size_t)cf.n_layers * cf.head_dim;
-  void* p = nullptr;
-  if (!ctx->qk_gain) {
-    LMOP_TRY(dev_alloc(ctx, &p, 2 * n * 4));
-    ctx->qk_gain = (float*)p;
-  }
-  if (!ctx->no_rope && !block_format(ctx)) {
-    const std::vector<float2> one((size_t)cf.max_seq * (cf.head_dim / 2), make_float2(1.f, 0.f));
-    LMOP_TRY(dev_alloc(ctx, &p, one.size() * sizeof(float2)));
-    ctx->no_rope = (float2*)p;
-    HIP_OK(ctx, hipMemcpyAsync(p, one.data(), one.size() * sizeof(float2), hipMemcpyHostToDevice,
-                               ctx->stream));
-    HIP_OK(ctx, hipStreamSynchronize(ctx->stream));
-  }
   const hipMemcpyKind kind = on_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice;
   HIP_OK(ctx, hipMemcpyAsync(ctx->qk_gain, q_gain, n * 4, kind, ctx->stream));
   HIP_OK(ctx, hipMemcpyAsync(ctx->qk_gain + n, k_gain, n * 4, kind, ctx->stream));

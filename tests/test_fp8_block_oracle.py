@@ -142,3 +142,20 @@ def test_plan_covers_block_scaled_passes(rows, dec):
     need = T * (TINY.d_model * 6 + TINY.n_heads * TINY.head_dim * 4 + 2 * wide + 688 + 4 * 6)
     assert pl["scratch_bytes"] >= need
     assert 0 < pl["min_workspace_bytes"] <= pl["scratch_bytes"]
+
+
+def test_plan_covers_norms_of_the_packed_formats():
+    """Their passes read one position for every token: 4 bytes each."""
+    ctx = L.Context(TINY, device=-1)
+    ctx.load_weights(make_weights(TINY, seed=5))
+    args = (np.arange(800) % TINY.vocab, np.arange(41) * 20, L.LMOP_BOOL, [3, 4])
+    g = torch.ones(TINY.n_layers, TINY.head_dim)
+    plain = ctx.plan_rows(*args, no_dedup=True)
+    ctx.load_qk_norms(g, g)
+    pl = ctx.plan_rows(*args, no_dedup=True)
+    assert pl["scratch_bytes"] == plain["scratch_bytes"] + -(-4 * 800 // 256) * 256
+    ctx.load_qk_norms()
+    assert ctx.plan_rows(*args, no_dedup=True)["scratch_bytes"] == plain["scratch_bytes"]
+    ctx.load_qk_norms(g, g)
+    ctx.load_weights(make_weights(TINY, seed=5))
+    assert ctx.plan_rows(*args, no_dedup=True)["scratch_bytes"] == plain["scratch_bytes"]

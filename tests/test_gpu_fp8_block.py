@@ -297,3 +297,28 @@ def test_1b_widths(L):
     assert few.tobytes() == out.tobytes() and np.array_equal(dbg, d2)
     _near(w, shape, lambda o, **k: o.eval_rows(prefix, rows[:6], 1, allowed, **k), out[:6], dbg[:6],
           "1b widths", dtype=np.float32)
+
+
+@pytest.mark.parametrize("fmt", ["int4_g32", "fp8_e4m3", "fp8_block"])
+def test_norms_take_no_memory_of_their_own(L, fmt):
+    """Their room comes with the weights, so loading them cannot fail for want of memory and
+    leave a model without its norms; a planned smallest workspace holds a pass with norms."""
+    ctx = L.Context(TINY, device=0, stream=torch.cuda.current_stream().cuda_stream, max_seq=1 << 17)
+    w = make_weights(TINY, seed=9, fmt=fmt, qk_norm=True)
+    gains = [torch.stack([getattr(l, n) for l in w.layers]) for n in ("q_norm", "k_norm")]
+    for l in w.layers:
+        l.q_norm = l.k_norm = None
+    ctx.load_weights(w)
+    held = ctx.memory()["device_bytes"]
+    ctx.load_qk_norms(*gains)
+    assert ctx.memory()["device_bytes"] == held
+    wl = make_workload("filter_tiny", n_rows=30)
+    pre = ctx.set_prefix(wl.prefix)
+    out, _ = _run(ctx, wl, pre)
+    need = ctx.plan_rows(wl.tokens, wl.offsets, wl.kind, wl.type_spec, prefix=pre,
+                         debug_logits=True)["min_workspace_bytes"]
+    buf = torch.full((need + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    at = -buf.data_ptr() % 256
+    ctx.set_workspace(buf.data_ptr() + at, need)
+    assert _run(ctx, wl, pre)[0].tobytes() == out.tobytes()
+    ctx.set_workspace(0, 0)
