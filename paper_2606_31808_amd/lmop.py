@@ -211,10 +211,16 @@ def _ptr(a: np.ndarray, ct):
 
 
 # ---------------------------------------------------------------- C-named calls
+class _Ctx(C.c_void_p):
+    """A ctx, and the shape of its query and key norms (n_layers, head_dim)."""
+    norms = None
+
+
 def lmop_create(cfg: lmop_config, device: int = 0, stream: Optional[int] = None):
-    out = C.c_void_p()
+    out = _Ctx()
     st = _lib.lmop_create(C.byref(cfg), device, C.c_void_p(stream or 0), C.byref(out))
     _check(st, None)
+    out.norms = cfg.n_layers, cfg.head_dim
     return out
 
 
@@ -233,7 +239,7 @@ def _tensor_ptr(t, keep):
     return a.ctypes.data, False
 
 
-def _qk_norms(weights, head_dim: Optional[int] = None):
+def _qk_norms(weights, ctx):
     """The layers' query and key norms, [n_layers, head_dim] each; None without."""
     norms = [(getattr(l, "q_norm", None), getattr(l, "k_norm", None)) for l in weights.layers]
     if all(n is None for pair in norms for n in pair):
@@ -242,8 +248,8 @@ def _qk_norms(weights, head_dim: Optional[int] = None):
         raise ValueError("query and key norms: in every layer, or in none")
     norms = [[torch.as_tensor(n).detach().cpu().float() for n in pair] for pair in norms]
     for n in (n for pair in norms for n in pair):
-        if tuple(n.shape) != (head_dim or norms[0][0].numel(),):
-            raise ValueError(f"a query or key norm of shape {tuple(n.shape)}")
+        if tuple(n.shape) != (ctx.norms[1],):
+            raise ValueError(f"a query or key norm of shape {tuple(n.shape)}, expected ({ctx.norms[1]},)")
     return [torch.stack([pair[i] for pair in norms]) for i in (0, 1)]
 
 
@@ -252,7 +258,7 @@ def lmop_load_weights(ctx, weights) -> None:
     (attn_norm, mlp_norm, wq .. w_down each with qweight/scales/n/k and a format name
     `fmt`, "int4_g32" (default), "fp8_e4m3" or "fp8_block"), all on one device.  Layers
     with q_norm and k_norm (fp32 [head_dim]) have these loaded too."""
-    norms = _qk_norms(weights)
+    norms = _qk_norms(weights, ctx)  # refused before anything is loaded
     keep = []
     where = set()
 
@@ -285,11 +291,15 @@ def lmop_load_weights(ctx, weights) -> None:
 
 
 def lmop_load_qk_norms(ctx, q_gain=None, k_gain=None) -> None:
-    """Query and key norms, [n_layers, head_dim] (both None: no norms)."""
+    """Query and key norms, [n_layers, head_dim] (both None: no norms); ctx is one of
+    lmop_create."""
     # few values, from the host: a copy or conversion on torch's current stream is
     # not ordered with the ctx's
     keep = [None if g is None else torch.as_tensor(g).detach().cpu().float().contiguous()
             for g in (q_gain, k_gain)]
+    for g in keep:
+        if g is not None and tuple(g.shape) != ctx.norms:
+            raise ValueError(f"norms of shape {tuple(g.shape)}, expected {ctx.norms}")
     _check(_lib.lmop_load_qk_norms(ctx, *(None if g is None else g.data_ptr() for g in keep), 0),
            ctx)
 
@@ -639,14 +649,9 @@ class Context:
             pass
 
     def load_weights(self, weights):
-        _qk_norms(weights, self.heads[2])  # refused before anything is loaded
         lmop_load_weights(self.ctx, weights)
 
     def load_qk_norms(self, q_gain=None, k_gain=None):
-        for g in (q_gain, k_gain):
-            if g is not None and tuple(g.shape) != (self.n_layers, self.heads[2]):
-                raise ValueError(f"a norm of shape {tuple(g.shape)}, expected "
-                                 f"({self.n_layers}, {self.heads[2]})")
         lmop_load_qk_norms(self.ctx, q_gain, k_gain)
 
     def set_prefix(self, tokens, parent=None):

@@ -159,3 +159,21 @@ def test_plan_covers_norms_of_the_packed_formats():
     ctx.load_qk_norms(g, g)
     ctx.load_weights(make_weights(TINY, seed=5))
     assert ctx.plan_rows(*args, no_dedup=True)["scratch_bytes"] == plain["scratch_bytes"]
+
+
+def test_c_named_calls_check_the_norms_shape():
+    """The library copies n_layers * head_dim values from each pointer."""
+    ctx = L.Context(TINY, device=-1)
+    w = make_weights(TINY, seed=5, qk_norm=True)
+    for l in w.layers:
+        l.q_norm = l.k_norm = torch.ones(TINY.head_dim // 2)
+    with pytest.raises(ValueError):
+        L.lmop_load_weights(ctx.ctx, w)
+    _expect(L.LMOP_ERR_STATE, L.lmop_load_qk_norms, ctx.ctx)  # nothing was loaded
+    L.lmop_load_weights(ctx.ctx, make_weights(TINY, seed=5, qk_norm=True))
+    g = torch.ones(TINY.n_layers, TINY.head_dim)
+    for bad in (g[:1], g[:, :1], g[0], g.view(-1), torch.ones(0, TINY.head_dim)):
+        for pair in ((bad, g), (g, bad)):
+            with pytest.raises(ValueError):
+                L.lmop_load_qk_norms(ctx.ctx, *pair)
+    L.lmop_load_qk_norms(ctx.ctx, g.numpy(), g.double())
