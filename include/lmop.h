@@ -388,15 +388,17 @@ lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t 
  * stream (the null stream for a ctx made without one) and returns: the
  * tensors must stay alive until the stream has passed it, work that writes
  * them must be ordered before it, and a caller may capture it into a HIP
- * graph (a ctx with a stream, profiling off).  It allocates nothing,
- * uses no workspace and no state of the ctx other than what is said at each
- * one, and leaves the calling thread's current device as it was.  The ctx
- * needs no weights.  Tensors are device memory of the ctx's device; strides
- * are in elements between rows; the elements of a row are adjacent; what
- * lies between rows is not written.  An output may not overlap an input
- * unless said.  A size of zero is a no-op.  Results do not depend on which
- * other rows are in the call, bit for bit.  A call is limited to 2^30 tiles of
- * 16 x 16 results, groups, or heads (of tokens counted in 64s). */
+ * graph (a ctx with a stream, profiling off).  It allocates nothing (with
+ * profiling on, two HIP events for each of up to 1024 timed launches that have
+ * not ended; past those an operator is counted, not timed), uses no workspace
+ * and no state of the ctx other than what is said at each one, and leaves the
+ * calling thread's current device as it was.  The ctx needs no weights.
+ * Tensors are device memory of the ctx's device; strides are in elements
+ * between rows; the elements of a row are adjacent; what lies between rows is
+ * not written.  An output may not overlap an input unless said.  A size of
+ * zero is a no-op.  Results do not depend on which other rows are in the call,
+ * bit for bit.  A call is limited to 2^30 tiles of 16 x 16 results, groups, or
+ * heads (of tokens counted in 64s). */
 typedef enum { LMOP_F16 = 0, LMOP_BF16 = 1, LMOP_F32 = 2 } lmop_dtype;
 
 /* Features that share one scale. */

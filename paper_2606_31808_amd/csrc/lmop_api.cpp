@@ -50,6 +50,9 @@ constexpr int64_t kMaxScaleRow = int64_t(1) << 21;  // and of the tokens' scales
 // arithmetic stays within 31 bits
 constexpr uint64_t kMaxTasks = uint64_t(1) << 30;
 
+// timed operator launches that a ctx keeps events for at a time
+constexpr size_t kMaxTimedOperators = 1024;
+
 int round_up(int x, int m) { return (x + m - 1) / m * m; }
 int64_t round_up64(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -404,9 +407,9 @@ hipEvent_t take_event(lmop_ctx* c) {
 
 template <typename F>
 lmop_status timed_on(lmop_ctx* c, hipStream_t stream, const char* name, double flops, double bytes,
-                     F&& launch) {
+                     F&& launch, bool may_time = true) {
   hipEvent_t a = nullptr, b = nullptr;
-  if (c->prof > 0 && c->stats[name].launches++ % c->prof == 0) {
+  if (c->prof > 0 && c->stats[name].launches++ % c->prof == 0 && may_time) {
     a = take_event(c);
     b = take_event(c);
     if (a && b) {
@@ -434,9 +437,17 @@ lmop_status timed(lmop_ctx* c, const char* name, double flops, double bytes, F&&
   return timed_on(c, c->stream, name, flops, bytes, launch);
 }
 
-lmop_status resolve_spans(lmop_ctx* c) {
+// Adds up the timed launches in order, up to the first that has not ended where
+// `wait` is not set, and takes their events back.
+lmop_status resolve_spans(lmop_ctx* c, bool wait = true) {
+  size_t done = 0;
   for (auto& s : c->spans) {
-    HIP_OK(c, hipEventSynchronize(s.b));
+    const hipError_t e = wait ? hipEventSynchronize(s.b) : hipEventQuery(s.b);
+    if (e == hipErrorNotReady) {
+      (void)hipGetLastError();
+      break;
+    }
+    HIP_OK(c, e);
     float ms = 0.f;
     HIP_OK(c, hipEventElapsedTime(&ms, s.a, s.b));
     Stat& st = c->stats[s.name];
@@ -446,8 +457,9 @@ lmop_status resolve_spans(lmop_ctx* c) {
     st.bytes += s.bytes;
     c->ev_free.push_back(s.a);
     c->ev_free.push_back(s.b);
+    ++done;
   }
-  c->spans.clear();
+  c->spans.erase(c->spans.begin(), c->spans.begin() + done);
   return LMOP_OK;
 }
 
@@ -1563,11 +1575,18 @@ lmop_status queue_operator(lmop_ctx* ctx, const char* name, double flops, double
     if (cap != hipStreamCaptureStatusNone)
       return fail(ctx, LMOP_ERR_STATE, "%s cannot be captured while profiling is on", name);
   }
+  // nothing waits for an operator, so the events of those that have ended are
+  // taken back here; while kMaxTimedOperators are under way the next are counted only
+  bool may_time = true;
+  if (ctx->prof > 0 && ctx->spans.size() >= kMaxTimedOperators) {
+    LMOP_TRY(resolve_spans(ctx, false));
+    may_time = ctx->spans.size() < kMaxTimedOperators;
+  }
   int before = -1;
   HIP_OK(ctx, hipGetDevice(&before));
   if (before != ctx->device) HIP_OK(ctx, hipSetDevice(ctx->device));
   const lmop_status st =
-      timed_on(ctx, stream, name, flops, bytes, [&] { return launch(stream); });
+      timed_on(ctx, stream, name, flops, bytes, [&] { return launch(stream); }, may_time);
   if (before != ctx->device) HIP_OK(ctx, hipSetDevice(before));
   return st;
 }

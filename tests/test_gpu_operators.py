@@ -703,3 +703,26 @@ def test_matmul_more_values_than_a_launch(ctx):
     c = torch.full((m, n), 9.0, dtype=torch.float16, device="cuda")
     ctx.matmul(a, sa, b, sb, out=c)
     assert not c.any()
+
+
+def test_profiled_operators_hold_a_bounded_number_of_events(ctx):
+    """Nothing waits for operators: 1024 timed launches are under way at most, later ones counted
+    only, and timing goes on when those have ended."""
+    m, n, k = 4096, 16384, 4096  # 0.2 ms
+    a, b = _codes(m, k, 1, pad=0), _codes(n, k, 2, pad=0)
+    sa, sb = _scales(m, k // G, 3), _scales(n // G, k // G, 4)
+    c, x = torch.empty(m, n, dtype=torch.float16, device="cuda"), torch.zeros(1, 128, device="cuda")
+    out = ctx.quantize(x)
+    ctx.set_profiling(1)
+    for _ in range(1000):
+        ctx.matmul(a, sa, b, sb, out=c)
+    for _ in range(600):
+        ctx.quantize(x, out=out)
+    st = ctx.kernel_stats()
+    assert st["matmul_fp8"]["launches"] == 1000 and st["quantize"]["launches"] == 600
+    timed = st["matmul_fp8"]["timed"] + st["quantize"]["timed"]
+    assert 1024 <= timed < 1600
+    for _ in range(5):
+        ctx.quantize(x, out=out)
+    assert ctx.kernel_stats()["quantize"]["timed"] == st["quantize"]["timed"] + 5
+    ctx.set_profiling(0)
