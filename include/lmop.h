@@ -388,17 +388,19 @@ lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t 
  * stream (the null stream for a ctx made without one) and returns: the
  * tensors must stay alive until the stream has passed it, work that writes
  * them must be ordered before it, and a caller may capture it into a HIP
- * graph (a ctx with a stream, profiling off).  It allocates nothing (with
- * profiling on, two HIP events for each of up to 1024 timed launches that have
- * not ended; past those an operator is counted, not timed), uses no workspace
- * and no state of the ctx other than what is said at each one, and leaves the
- * calling thread's current device as it was.  The ctx needs no weights.
- * Tensors are device memory of the ctx's device; strides are in elements
- * between rows; the elements of a row are adjacent; what lies between rows is
- * not written.  An output may not overlap an input unless said.  A size of
- * zero is a no-op.  Results do not depend on which other rows are in the call,
- * bit for bit.  A call is limited to 2^30 tiles of 16 x 16 results, groups, or
- * heads (of tokens counted in 64s). */
+ * graph (a ctx with a stream, profiling off).  The ctx must outlive every
+ * replay of such a graph: lmop_destroy frees the rotary table that
+ * lmop_qk_norm_rope reads.  An operator allocates nothing (with profiling on,
+ * two HIP events for each of up to 1024 timed launches that have not ended;
+ * past those it is counted, not timed), uses no workspace and no state of the
+ * ctx other than what is said at each one, and leaves the calling thread's
+ * current device as it was.  The ctx needs no weights.  Tensors are device
+ * memory of the ctx's device; strides are in elements between rows; the
+ * elements of a row are adjacent; what lies between rows is not written.  An
+ * output may not overlap an input unless said.  A size of zero is a no-op.
+ * Results do not depend on which other rows are in the call, bit for bit.  A
+ * call is limited to 2^30 tiles of 16 x 16 results, groups, or heads (of
+ * tokens counted in 64s). */
 typedef enum { LMOP_F16 = 0, LMOP_BF16 = 1, LMOP_F32 = 2 } lmop_dtype;
 
 /* Features that share one scale. */
@@ -429,9 +431,14 @@ lmop_status lmop_quantize(lmop_ctx* ctx, const lmop_quantize_args* args);
  *             * (sum over the features f of g of a[i][f] * b[j][f])
  * The sums are held in fp32 and rounded to dtype once; the groups are added
  * in order of g.  For fp16 and bf16 results the inner sum runs on the 8-bit
- * matrix instruction, which cuts a product's bits below 2^-13 of the largest
- * of its 8 neighbours (2e-5 of a result's usual size, less than a tenth of its
- * rounding); for fp32 results every product is whole, unless `fast` asks for
+ * matrix instruction, which cuts each product towards zero at 2^-13 of the
+ * leading bit (2 to the sum of the two exponents) of the largest of eight
+ * neighbouring products.  A sum of eight is off by less than 7 * 2^-13 of its
+ * largest product: where large products cancel, more than the rounding of the
+ * result.  On unit-normal tokens and weights it is 1.5e-5 of the result's
+ * norm, and 2.0e-5 to 2.5e-5 with a feature in a hundred ten times as large,
+ * beside 2.1e-4 of the rounding to fp16: a twelfth of the fp16 values become
+ * the next one.  For fp32 results every product is whole, unless `fast` asks for
  * the 8-bit instruction there too.  NaN codes give NaN. */
 typedef struct {
   const uint8_t* a;     /* [m][k] codes (tokens), 16-byte aligned */
@@ -473,8 +480,8 @@ typedef struct {
   const float* k_gain;   /* NULL or fp32 [head_dim] */
   const int32_t* pos;    /* [n_tokens] */
   const int32_t* slot;   /* NULL (token i's slot is i), or [n_tokens]: the slot of its key and
-                            value; outside [0, n_slots): neither is written.  Two tokens with
-                            one slot: either's key and value may stay */
+                            value; outside [0, n_slots): neither is written.  Of two tokens
+                            with one slot, any mix of their values may stay there */
   void* q_out;           /* [n_tokens][n_heads * head_dim]; may be q itself */
   void* k_out;           /* [n_slots][n_kv_heads * head_dim]; may be k itself without slots */
   void* v_out;           /* LMOP_V_ROWS: [n_slots][n_kv_heads * head_dim];

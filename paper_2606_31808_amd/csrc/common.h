@@ -9,8 +9,6 @@ typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16;
-typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 #define LMOP_DEVICE __device__ __forceinline__
@@ -25,10 +23,10 @@ LMOP_DEVICE f32x4 mfma16x16x32(f16x8 a, f16x8 b, f32x4 c) {
 // v_mfma_f32_16x16x128_f8f6f4 of two E4M3 operands, accumulator zero: lane
 // 16g + c holds 32 features of row c of each operand (any 32 of the 128, the
 // same ones in both, a different set for each g); D as above.  Of the eight
-// products of a lane's 8 adjacent codes the instruction keeps the bits down
-// to 2^-13 of the largest one's leading bit (2^(sum of its two exponents))
-// and cuts the rest off; the sums of eights are added in fp32.  (Measured;
-// v_mfma_f32_16x16x32_fp8_fp8 does the same.)
+// products of a lane's 8 adjacent codes the instruction cuts each, towards
+// zero, at 2^-13 of the leading bit of the largest one: 2^(sum of its two
+// exponents, -6 for subnormal codes).  The sums of eights are added in fp32.
+// (Measured, to the bit; v_mfma_f32_16x16x32_fp8_fp8 does the same.)
 LMOP_DEVICE f32x4 mfma16x16x128_e4m3(i32x8 a, i32x8 b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0,
                                                           0, 0, 0);

@@ -7,6 +7,7 @@ import shutil
 import subprocess
 
 import pytest
+import torch
 
 from paper_2606_31808_amd import build
 from tests import test_gpu_operators as gpu
@@ -145,3 +146,30 @@ def test_every_launch_is_one_that_hip_makes(tmp_path):
                     assert rows == m or -(-m // bm) * -(-n // bn) * threads >= 2 ** 32
                     several += rows != m
     assert several
+
+
+@pytest.mark.parametrize("big", [False, True])
+def test_what_the_cut_of_products_costs(big):
+    """The 8-bit instruction's cut (which a GPU test pins to the bit) on unit-normal tokens and
+    weights, and with a feature in a hundred ten times as large.  Of eight products seven lose
+    up to u = 2^-13 of the largest p, of either sign: 7 u off at most, and u / sqrt(3) each in
+    the root mean square if what is cut off is spread evenly."""
+    g, (m, n, k) = torch.Generator().manual_seed(7), (48, 128, 1024)
+    x = torch.randn(m, k, generator=g)
+    if big:
+        x *= torch.where(torch.rand(k, generator=g) < 0.01, 10.0, 1.0)
+    groups = x.view(m, -1, gpu.G)
+    sa = groups.abs().amax(-1) / 448
+    a = (groups / sa[..., None]).view(m, k).to(gpu.F8)
+    w = torch.randn(n, k, generator=g).view(n, -1, gpu.G)
+    sb = (w.abs().amax((0, 2)) / 448)[None]
+    b = (w / sb[..., None]).view(n, k).to(gpu.F8)
+    off = gpu._cut_product(a, sa, b, sb)[0].double()
+    whole, _, largest = gpu._ref_matmul(a, sa, b, sb)
+    off -= whole
+    assert torch.all(off.abs() <= 7 * 2.0 ** -13 * largest)
+    p = [t.float().double().abs().view(t.shape[0], -1, 8).amax(-1) * s.double().repeat_interleave(16, 1)
+         for t, s in ((a, sa), (b, sb))]
+    rms = (7 / 3) ** 0.5 * 2.0 ** -13 * ((p[0] ** 2) @ (p[1] ** 2).t()).sum() ** 0.5
+    print(f"off by {off.norm() / whole.norm():.2e} of the norm, bound {rms / whole.norm():.2e}")
+    assert 1e-5 * whole.norm() < off.norm() <= rms
