@@ -104,7 +104,7 @@ const char* lmop_status_string(lmop_status s);
  * Every map's input, fp16 per token, is quantised as lmop_quantize does (one
  * scale per 128 features; w_down's is silu(gate) * up of the fp16 gate and
  * up) and multiplied as lmop_matmul does (fp16 results, and fast fp32 ones
- * added to the residual). */
+ * added to the residual).  A map has at most 2^23 input features. */
 typedef struct {
   const uint8_t* qweight;
   const void* scales;

@@ -1824,6 +1824,9 @@ lmop_status lmop_load_weights(lmop_ctx* ctx, const lmop_weights* w) {
       w->format != (int32_t)LMOP_W_FP8_BLOCK)
     return fail(ctx, LMOP_ERR_INVALID_ARG, "unknown weight format %d", w->format);
   const int d = cf.d_model, nq = ctx->nq_dim, nkv = ctx->nkv_dim, F = cf.d_ff;
+  if (w->format == (int32_t)LMOP_W_FP8_BLOCK && std::max({d, nq, F}) > kMaxCodeRow)
+    return fail(ctx, LMOP_ERR_UNSUPPORTED, "block-scaled maps of %d features (at most %lld)",
+                std::max({d, nq, F}), (long long)kMaxCodeRow);
   for (int l = 0; l < cf.n_layers; ++l) {
     const lmop_layer& L = w->layers[l];
     if (!L.attn_norm || !L.mlp_norm)

@@ -177,3 +177,22 @@ def test_c_named_calls_check_the_norms_shape():
             with pytest.raises(ValueError):
                 L.lmop_load_qk_norms(ctx.ctx, *pair)
     L.lmop_load_qk_norms(ctx.ctx, g.numpy(), g.double())
+
+
+@pytest.mark.parametrize("d_ff,d,heads,fmt,status", [
+    (2 ** 23, 64, 1, L.LMOP_W_FP8_BLOCK, L.LMOP_OK), (2 ** 23 + 16, 64, 1, L.LMOP_W_FP8_BLOCK, L.LMOP_ERR_UNSUPPORTED),
+    (64, 2 ** 23 + 64, 1, L.LMOP_W_FP8_BLOCK, L.LMOP_ERR_UNSUPPORTED),
+    (64, 64, 2 ** 17 + 1, L.LMOP_W_FP8_BLOCK, L.LMOP_ERR_UNSUPPORTED), (2 ** 24, 64, 1, L.LMOP_W_INT4_G32, L.LMOP_OK)])
+def test_rows_of_codes_that_a_tile_cannot_address(d_ff, d, heads, fmt, status):
+    """A tile's row offsets are 32 bits: 256 rows of 2^24 bytes would pass them (addresses that
+    are not read: a host-only ctx checks the shapes)."""
+    shape = dataclasses.replace(TINY, n_layers=1, d_model=d, n_heads=heads, n_kv_heads=1, head_dim=64, d_ff=d_ff)
+    ctx = L.Context(shape, device=-1)
+
+    def m(n, k):
+        return L.lmop_qmat(4096, 4096, n, k)
+
+    nq, layer = heads * 64, (L.lmop_layer * 1)()
+    layer[0] = L.lmop_layer(4096, 4096, m(nq, d), m(64, d), m(64, d), m(d, nq), m(d_ff, d), m(d_ff, d), m(d, d_ff))
+    w = L.lmop_weights(4096, 4096, 4096, layer, 1, 0, fmt)
+    assert L._lib.lmop_load_weights(ctx.ctx, L.C.byref(w)) == status
