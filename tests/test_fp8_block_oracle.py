@@ -10,6 +10,7 @@ from oracle import OracleLM
 from oracle.lmop_oracle import (KIND_ENUM, dequant_fp8_block, quantize_rows, rms_norm, round_e4m3)
 from paper_2606_31808_amd import lmop as L
 from synth import SHAPES, ModelShape, make_weights, quantize_fp8_block
+from tests import test_gpu_fp8_block as gpu
 
 TINY = SHAPES["tiny"]
 MICRO = ModelShape("micro", 2, 64, 4, 2, 16, 96, 64, 1e4)
@@ -196,3 +197,43 @@ def test_rows_of_codes_that_a_tile_cannot_address(d_ff, d, heads, fmt, status):
     layer[0] = L.lmop_layer(4096, 4096, m(nq, d), m(64, d), m(64, d), m(d, nq), m(d_ff, d), m(d_ff, d), m(d, d_ff))
     w = L.lmop_weights(4096, 4096, 4096, layer, 1, 0, fmt)
     assert L._lib.lmop_load_weights(ctx.ctx, L.C.byref(w)) == status
+
+
+class _Wrong(OracleLM):
+    """The oracle with one mistake in its queries, keys or values."""
+
+    def __init__(self, what, *a, **k):
+        super().__init__(*a, **k)
+        self.what, own = what, self.qk_norms
+        if what == "gains swapped":
+            self.qk_norms = [[b, a] for a, b in own]
+        if what == "no key gain":
+            self.qk_norms = [[a, np.ones_like(b)] for a, b in own]
+        if what == "first layer's gains":
+            self.qk_norms = [own[0]] * len(own)
+        if what == "no norms":
+            self.qk_norms = [[None, None] for _ in own]
+
+    def _qkv(self, l, h, w, pos):
+        q, k, v = super()._qkv(l, h, w, pos * 0 if self.what == "no rotation" else pos)
+        if self.what == "queries one position on":
+            q = super()._qkv(l, h, w, pos + 1)[0]
+        if self.what == "keys one slot on":
+            k = np.roll(k, 1, 0)
+        if self.what == "values one slot on":
+            v = np.roll(v, 1, 0)
+        return q, k, v
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("sizes", gpu.TELLING, ids=["hd64", "hd128", "tiny"])
+def test_mistakes_in_queries_and_keys_are_seen(sizes, norm):
+    """What the GPU test of queries and keys allows, each of these mistakes exceeds by half."""
+    t = gpu.Telling(sizes, norm)
+    wrong = ["no rotation", "queries one position on", "keys one slot on", "values one slot on"]
+    if norm:
+        wrong += ["gains swapped", "no key gain", "first layer's gains", "no norms"]
+    for what in wrong:
+        off = t.off(t.logits(_Wrong(what, t.w, t.shape)))
+        print(what, f"{off:.3f}, bound {t.bound:.3f}")
+        assert off > 1.5 * t.bound, what

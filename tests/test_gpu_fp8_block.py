@@ -322,3 +322,56 @@ def test_norms_take_no_memory_of_their_own(L, fmt):
     ctx.set_workspace(buf.data_ptr() + at, need)
     assert _run(ctx, wl, pre)[0].tobytes() == out.tobytes()
     ctx.set_workspace(0, 0)
+
+
+# ---------------------------------------------------------------- queries and keys that matter
+# Rows of three tokens behind a prefix of three, so that attention weighs six keys; query and
+# key projections (gains, with norms) scaled up, so that it weighs them unevenly; a first layer
+# that adds nothing to the residual, so that the second one's drift is a single layer's.  The
+# measure is the median row: its largest difference, which a drifted code moves by some 0.01 to
+# 0.1 sigma, while what queries and keys are taken wrongly for moves every row.
+TELLING = [dict(d_model=64, n_heads=2, n_kv_heads=1, head_dim=64, d_ff=64),
+           dict(d_model=64, n_heads=2, n_kv_heads=1, head_dim=128, d_ff=64),
+           dict(d_model=256, n_heads=4, n_kv_heads=4, head_dim=64, d_ff=688)]
+
+
+class Telling:
+    """A model, its rows, and how far from the oracle the median row may be (in sigma)."""
+
+    def __init__(self, sizes, norm):
+        self.shape = dataclasses.replace(TINY, n_layers=2, vocab=512, **sizes)
+        self.w = make_weights(self.shape, seed=3, fmt="fp8_block", qk_norm=norm)
+        for m in (self.w.layers[0].wo, self.w.layers[0].w_down):
+            m.qweight.zero_()
+        for l in self.w.layers:
+            if norm:
+                l.q_norm *= 2
+            else:
+                l.wq.scales *= 8
+                l.wk.scales *= 8
+        rng = np.random.default_rng(1)
+        self.prefix = rng.integers(0, 512, 3)
+        self.rows = [rng.integers(0, 512, 3) for _ in range(60)]
+        self.allowed = np.array([3, 9], dtype=np.int32)
+        self.z = self.logits(OracleLM(self.w, self.shape))
+        drift = [self.off(self.logits(_Nudged(s, self.w, self.shape))) for s in (1, 2)]
+        self.bound = 2 * max(drift)
+
+    def logits(self, orc):
+        out = orc.eval_rows(self.prefix, self.rows, KIND_BOOL, self.allowed, keep_logits=True)
+        return np.stack([s[0] for s in out["logits"]])
+
+    def off(self, z):
+        return float(np.median(np.abs(z - self.z).max(1)) / self.z.std())
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("sizes", TELLING, ids=["hd64", "hd128", "tiny"])
+def test_queries_and_keys(L, sizes, norm):
+    t = Telling(sizes, norm)
+    ctx = _ctx(L, t.w, t.shape)
+    _, dbg = ctx.eval_rows(np.concatenate(t.rows), np.arange(61) * 3, KIND_BOOL, t.allowed,
+                           prefix=ctx.set_prefix(t.prefix), debug_logits=True)
+    off = t.off(dbg[:, 0])
+    _log("queries and keys", sizes, norm, f"median row off by {off:.4f} sigma, bound {t.bound:.4f}")
+    assert off <= t.bound
