@@ -437,13 +437,13 @@ lmop_status timed(lmop_ctx* c, const char* name, double flops, double bytes, F&&
   return timed_on(c, c->stream, name, flops, bytes, launch);
 }
 
-// Adds up the timed launches in order, up to the first that has not ended where
-// `wait` is not set, and takes their events back.
+// Adds up the timed launches in order and takes their events back; where `wait` is
+// not set, up to the first that cannot be asked or has not ended.
 lmop_status resolve_spans(lmop_ctx* c, bool wait = true) {
   size_t done = 0;
   for (auto& s : c->spans) {
     const hipError_t e = wait ? hipEventSynchronize(s.b) : hipEventQuery(s.b);
-    if (e == hipErrorNotReady) {
+    if (!wait && e != hipSuccess) {
       (void)hipGetLastError();
       break;
     }
