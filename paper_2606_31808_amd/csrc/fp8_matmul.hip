@@ -556,9 +556,10 @@ __global__ __launch_bounds__((64 * WM * WN), ((OCC * WM * WN + 3) / 4)) void mat
 // add them in the order of the groups.  A weight of few rows is then spread
 // over the chip along K.  The operands of two rounds are in flight or in
 // registers (4 * U * (1 + MT) KB a wave).  Bound by memory for one token (n 28672, k 4096: 117 MB
-// in 22.6 us, 5.2 TB/s; n 4096, k 14336: 13.9, 4.2), for more by L2, from which every 16
-// columns read the tokens' codes again (16 tokens 19.0, 24 tokens 24.2); twice the loads
-// in flight, or 16 waves, take as long.
+// in 22.6 us, 5.2 TB/s; n 4096, k 14336: 13.9, 4.2).  What bounds more tokens, whose codes every
+// 16 columns read again, is not established (16 tokens 19.0, 24 tokens 24.2 with weights from
+// memory, 21.0 with weights in the last cache); twice the loads in flight, or 16 waves, take as
+// long.
 template <typename R, int MT, int U>
 __global__ __launch_bounds__(512, 2) void matmul_few_kernel(const lmop_matmul_args p) {
   using T = typename R::Type;

@@ -2,7 +2,8 @@
 // and values into a cache, in one pass over a batch of tokens.
 //
 // Bound by memory: each element is read and written once (16,384 tokens of 32 + 8
-// heads of 128 and their values: 411 MB in 77 us, 5.4 TB/s; 9 tokens: 3 us).  A head is held by
+// heads of 128 and their values: 411 MB in 80 us where row evaluation wrote them
+// just before, 92 from memory, 4.5 to 5.1 TB/s; 9 tokens: 3 us).  A head is held by
 // hd / 16 lanes, lane j with dimensions 8j .. 8j+7 and the same of the upper
 // half, so that both members of every rotation pair are in one lane and the
 // sum of squares takes two or three exchanges between lanes, without LDS.  A

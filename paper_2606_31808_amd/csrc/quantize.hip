@@ -2,9 +2,9 @@
 // of silu(gate) * x (the operand of the block-scaled FP8 products).
 //
 // Bound by memory: every input is read once, held in registers between the
-// maximum and the codes, and every code written once (16384 x 4096 of fp16: 203 MB in 32
-// to 36 us, 5.6 to 6.3 TB/s, by the card; 4099 x 14336 of bf16 with a gate: 296 MB in 62.5 us,
-// 4.7 TB/s; a copy does 4.8, or 7.2 from the last cache).  Eight lanes hold a
+// maximum and the codes, and every code written once (16384 x 4096 of fp16: 203 MB in 36.4
+// us, 5.6 TB/s; 4099 x 14336 of bf16 with a gate: 296 MB in 62.5, 4.7 TB/s, the vector
+// units beside it; a copy does 4.8, or 7.2 from the last cache).  Eight lanes hold a
 // group, two runs of 8 features each (64 features apart, so that the lanes'
 // 16-byte loads lie side by side); the maximum takes three exchanges between
 // lanes, without LDS.
