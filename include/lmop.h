@@ -77,7 +77,9 @@ typedef struct {
  * GPU return LMOP_ERR_UNSUPPORTED after validation.  On failure *out is NULL
  * and lmop_last_error(NULL) describes the cause (per host thread). */
 lmop_status lmop_create(const lmop_config* cfg, int32_t device, void* hip_stream, lmop_ctx** out);
-void lmop_destroy(lmop_ctx* ctx); /* frees everything, including live prefixes; NULL is a no-op */
+/* Frees everything, including live prefixes; NULL is a no-op.  It waits and frees
+ * device memory, so not while the thread captures a stream: HIP ends the capture. */
+void lmop_destroy(lmop_ctx* ctx);
 const char* lmop_last_error(const lmop_ctx* ctx);
 const char* lmop_status_string(lmop_status s);
 

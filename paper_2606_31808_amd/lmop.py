@@ -620,8 +620,19 @@ def config_from_shape(shape, max_seq: int = 0) -> lmop_config:
                        shape.rms_eps, shape.rope_theta, max_seq)
 
 
+# ctxs that nothing referred to any more while a stream was being captured, where
+# freeing one would end the capture: freed with the next ctx made or closed
+_dropped = []
+
+
+def _free_dropped():
+    while _dropped:
+        lmop_destroy(_dropped.pop())
+
+
 class Context:
-    """One lmop ctx on a HIP device (device=-1: host-only, validation only)."""
+    """One lmop ctx on a HIP device (device=-1: host-only, validation only).  It has to outlive
+    the graphs that captured its operators."""
 
     def __init__(self, shape, device: int = 0, stream: Optional[int] = None, max_seq: int = 0,
                  n_layers: Optional[int] = None):
@@ -635,16 +646,23 @@ class Context:
         # they are ordered on
         self.device = max(int(device), -1)
         self.stream = int(stream or 0)
+        _free_dropped()
         self.ctx = lmop_create(cfg, device, stream)
 
     def close(self):
+        _free_dropped()
         if self.ctx:
             lmop_destroy(self.ctx)
             self.ctx = None
 
     def __del__(self):
         try:
-            self.close()
+            # a garbage collection may come in the middle of a capture
+            if self.device >= 0 and torch.cuda.is_current_stream_capturing():
+                _dropped.append(self.ctx)
+                self.ctx = None
+            else:
+                self.close()
         except Exception:
             pass
 

@@ -324,6 +324,26 @@ def test_norms_take_no_memory_of_their_own(L, fmt):
     ctx.set_workspace(0, 0)
 
 
+@pytest.mark.parametrize("fmt", ["int4_g32", "fp8_block"])
+def test_prefixes_and_decoding_with_norms_in_a_workspace(L, fmt):
+    """Every pass of a ctx with norms finds its scratch in the caller's workspace."""
+    ctx = _ctx(L, make_weights(TINY, seed=9, fmt=fmt, qk_norm=True))
+    wl = make_workload("options_tiny", n_rows=12)
+
+    def all_passes():
+        pre = ctx.set_prefix(wl.prefix)
+        kids = ctx.set_prefixes([wl.suffix(0)[:5], wl.suffix(1)[:3]], parent=pre)
+        out = _run(ctx, wl, pre)[0].tobytes()
+        child = ctx.eval_rows(wl.suffix(2), [0, len(wl.suffix(2))], KIND_BOOL, [3, 9], row_prefix=[kids[1]])[0]
+        return out, child.tobytes()
+
+    want = all_passes()
+    buf = torch.full((64 << 20,), 0x7F, dtype=torch.uint8, device="cuda")
+    ctx.set_workspace(buf.data_ptr(), buf.numel())
+    assert all_passes() == want
+    ctx.set_workspace(0, 0)
+
+
 # ---------------------------------------------------------------- queries and keys that matter
 # Rows of three tokens behind a prefix of three, so that attention weighs six keys; query and
 # key projections (gains, with norms) scaled up, so that it weighs them unevenly; a first layer

@@ -560,6 +560,26 @@ def test_captured(L, T):
         assert torch.equal(ctx.matmul(eager[3][0], eager[3][1], args[2], args[3]), eager[0])
 
 
+def test_ctx_dropped_in_a_capture(L):
+    """A ctx that goes while another's operators are captured leaves the capture whole."""
+    stream = torch.cuda.Stream()
+    ctx, other = (L.Context(Shape(), device=0, stream=stream.cuda_stream) for _ in range(2))
+    with torch.cuda.stream(stream):
+        x = torch.randn(9, 300, device="cuda")
+        want = [t.clone() for t in ctx.quantize(x)]
+        stream.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            got = ctx.quantize(x)
+            del other
+        for _ in range(3):
+            got[0].view(torch.uint8).zero_(), got[1].zero_()
+            g.replay()
+            stream.synchronize()
+            for t, w in zip(got, want):
+                assert torch.equal(t.contiguous().view(torch.uint8), w.contiguous().view(torch.uint8))
+
+
 def test_streams(L):
     """A ctx of another stream than torch's current one refuses; its own stream serves."""
     stream = torch.cuda.Stream()

@@ -177,3 +177,24 @@ def test_qk_norm_rope_heads_fit_a_launch(tokens, heads, refused):
               **{f: row for f in ("ldq", "ldk", "ldv", "ldqo", "ldko")})
     assert _call(c, "lmop_qk_norm_rope", a) == UNS
     assert ("too many" in L._lib.lmop_last_error(c.ctx).decode()) == refused
+
+
+def test_a_ctx_dropped_in_a_capture_is_freed_later(monkeypatch):
+    """Freeing one waits and frees memory, which ends the capture; a garbage collection may come
+    at any time."""
+    freed = []
+    monkeypatch.setattr(L, "lmop_destroy", lambda h: freed.append(h.value))
+    capturing = [True]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    ctx = L.Context(SHAPES["tiny"], device=-1)
+    handle, ctx.device = ctx.ctx.value, 0
+    del ctx
+    assert freed == []
+    capturing[0] = False
+    other = L.Context(SHAPES["tiny"], device=-1)
+    assert freed == [handle]
+    other.device = 0
+    handle = other.ctx.value
+    del other
+    assert freed[1:] == [handle]
+    assert not L._dropped
