@@ -658,7 +658,7 @@ class Context:
     def __del__(self):
         try:
             # a garbage collection may come in the middle of a capture
-            if self.device >= 0 and torch.cuda.is_current_stream_capturing():
+            if self.ctx and self.device >= 0 and torch.cuda.is_current_stream_capturing():
                 _dropped.append(self.ctx)
                 self.ctx = None
             else:
