@@ -403,7 +403,12 @@ lmop_status lmop_get_kernel_stats(lmop_ctx* ctx, lmop_kernel_stat* out, int32_t 
  * Results do not depend on which other rows are in the call, bit for bit.  A
  * call is limited to 2^30 tiles of 16 x 16 results, groups, or heads (of
  * tokens counted in 64s). */
-typedef enum { LMOP_F16 = 0, LMOP_BF16 = 1, LMOP_F32 = 2 } lmop_dtype;
+typedef enum {
+  LMOP_F16 = 0,
+  LMOP_BF16 = 1,
+  LMOP_F32 = 2,
+  LMOP_E4M3 = 3 /* the pages of an lmop_cache only */
+} lmop_dtype;
 
 /* Features that share one scale. */
 #define LMOP_FP8_GROUP 128
@@ -495,6 +500,135 @@ typedef struct {
   int32_t dtype;         /* LMOP_F16 or LMOP_BF16, of all tensors */
 } lmop_qk_norm_rope_args;
 lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* args);
+
+/* ------------------------------------------- operators on a paged cache
+ * Keys and values of many sequences in pages of a few tokens, the attention
+ * that reads them, and the choice of the pages that are worth reading.  What is said
+ * of the operators above holds here too, but for three things: lmop_attend
+ * needs a workspace for some calls; how it divides a call's keys among workgroups, and
+ * with that the order of its sums, depends on the sizes in its arguments (not
+ * on what device memory holds: a call repeated gives the same bits); and what
+ * device memory names (pages, lengths, starts) cannot be checked on the host, so
+ * each call says what a wrong one does.  None makes a kernel read or write
+ * outside the tensors.
+ *
+ * A page holds page_size tokens of every kv head: [n_kv_heads][page_size][head_dim].
+ * LMOP_E4M3 pages hold E4M3 codes, and for each token and head a power of two
+ * as its exponent + 127: value = e4m3(code) * 2^(exp - 127).  A power of two because
+ * codes are floating-point: any other scale would round no less, and this
+ * one is undone exactly. */
+typedef struct {
+  void *k, *v;             /* [n_pages] pages of dtype, page_stride apart; 16-byte aligned */
+  uint8_t *k_exp, *v_exp;  /* LMOP_E4M3: [n_pages][n_kv_heads][page_size], 16-byte aligned; else NULL */
+  void* k_mean;            /* NULL, or [n_pages][n_kv_heads][head_dim] of the tokens' dtype: the mean
+                              key of each full page; 16-byte aligned */
+  int64_t page_stride;     /* elements from a page to the next, in k and in v: at least
+                              n_kv_heads * page_size * head_dim, a multiple of 16 */
+  int32_t n_pages;
+  int32_t page_size;       /* 16, 32, 64, 128 or 256 tokens */
+  int32_t dtype;           /* LMOP_F16 or LMOP_BF16, the tokens' own, or LMOP_E4M3 */
+} lmop_cache;
+
+/* The tokens of a call: those of sequence s are start[s] .. start[s+1]-1, in
+ * order; tokens before start[0] and from start[n_seqs] on belong to none, and their
+ * rows are left as they are.  Key i of a sequence is in page table[s][i / page_size],
+ * at i % page_size.  The call's tokens are the last of a sequence's
+ * length[s] keys: token j of n is key length[s] - n + j. */
+typedef struct {
+  const int32_t* table;  /* [n_seqs][max_pages] page numbers; those past a sequence's keys are not
+                            read or not used, whatever they are */
+  const int32_t* length; /* [n_seqs] */
+  const int32_t* start;  /* [n_seqs + 1], ascending; NULL: one token each (n_tokens == n_seqs) */
+  int64_t ld_table;      /* >= max_pages */
+  int32_t max_pages, n_seqs, n_tokens;
+} lmop_batch;
+
+/* Appends tokens to the cache: rotates keys (rotate-half, by the angles
+ * pos * rope_theta^(-2 i / head_dim), pos = first + the key's index; in fp32,
+ * rounded once) and writes keys and values into their pages; queries, if given, are
+ * rotated likewise into q_out.  Into LMOP_E4M3 pages a head is written with the least
+ * power of two 2^e, e >= -126, for which its largest magnitude is at most 448 * 2^e, and
+ * codes e4m3(x * 2^-e) to nearest even; fp16 heads are cut at +-61440 first, the most that
+ * both types hold; a head with an infinity or a NaN gets NaN codes.
+ * With k_mean, each page whose last key is among the call's tokens gets its
+ * mean: the sum of its keys as they are kept, in fp64, over page_size, rounded
+ * once.
+ * A position outside [0, max_seq) gives NaN queries and keys.  A token whose
+ * index is negative or past the table, or whose table entry names no page, is
+ * not written (its query is rotated by its position all the same).  Of two tokens
+ * in one place, any mix of their values may stay. */
+typedef struct {
+  lmop_cache cache;
+  lmop_batch batch;
+  const void *q, *k, *v; /* [n_tokens][n_heads * head_dim], [n_tokens][n_kv_heads * head_dim] twice;
+                            q may be NULL */
+  void* q_out;           /* [n_tokens][n_heads * head_dim]; may be q itself */
+  int64_t ldq, ldk, ldv, ldqo;
+  int32_t first;         /* position of key 0 (the length of a shared prefix), >= 0 */
+  int32_t rotate;        /* 1; 0: keys and queries are copied as they are */
+  int32_t dtype;         /* LMOP_F16 or LMOP_BF16, of q, k, v and q_out */
+} lmop_append_args;
+lmop_status lmop_cache_append(lmop_ctx* ctx, const lmop_append_args* args);
+
+/* Attention of a batch's tokens over its sequences' keys and over a prefix
+ * that all share, whose keys every token sees:
+ *   out = sum over the keys seen of softmax(scale * q . key) * value
+ *   lse = ln(sum over the keys seen of exp(scale * q . key))
+ * for every query head, which reads kv head h / (n_heads / n_kv_heads).  Token j of
+ * n sees its sequence's keys up to its own, index length - n + j; with
+ * `blocks`, of those only the ones in the blocks listed for it and the kv
+ * head (block b is keys b * page_size and on; an entry outside the table, -1 for
+ * instance, stands for none; one listed twice counts twice).  A key that
+ * a token does not see has no effect on its result, whatever it or its value holds.  A token
+ * that sees no key, or only scores of minus infinity, gets zeros and lse = -inf.
+ * Scores, sums and outputs are held in fp32; the weights are rounded to dtype for the
+ * product with the values, and the sum that divides is that of the rounded
+ * ones.
+ * NaN results: for every token of a sequence of more than max_tokens tokens, or whose length is
+ * below 0 or above max_length; for a token that sees a key whose page does not
+ * exist. */
+typedef struct {
+  lmop_cache cache;
+  lmop_batch batch;
+  const void* q;         /* [n_tokens][n_heads * head_dim] */
+  void* out;             /* [n_tokens][n_heads * head_dim]; may not be q */
+  float* lse;            /* NULL or [n_tokens][n_heads] */
+  const int32_t* prefix; /* the prefix's ceil(prefix_length / page_size) pages */
+  const int32_t* blocks; /* [n_tokens][n_kv_heads][n_blocks], or NULL with n_blocks 0; not with a prefix */
+  void* workspace;       /* 256-byte aligned; NULL if lmop_attend_workspace says 0.  Only this call's
+                            kernels use it, and nothing in it matters before or after them */
+  uint64_t workspace_bytes;
+  int64_t ldq, ldo;
+  int32_t prefix_length; /* >= 0 */
+  int32_t n_blocks;
+  int32_t max_tokens;    /* at least the most tokens of a sequence in the call; 1 without starts */
+  int32_t max_length;    /* at least the longest length, at most max_pages * page_size: with
+                            max_tokens what the call's shape is chosen by */
+  float scale;           /* 0: 1 / sqrt(head_dim); else 1e-30 to 1e30 */
+  int32_t dtype;         /* LMOP_F16 or LMOP_BF16, of q and out */
+} lmop_attend_args;
+lmop_status lmop_attend(lmop_ctx* ctx, const lmop_attend_args* args);
+/* The workspace such a call needs (of its pointers it matters only whether batch.start is NULL). */
+lmop_status lmop_attend_workspace(lmop_ctx* ctx, const lmop_attend_args* args, uint64_t* bytes);
+
+/* Chooses for every token and kv head the n_blocks blocks (pages) to attend to: the token's
+ * own (index / page_size), and of those before it the n_blocks - 1 with the largest
+ *   score = (sum of the queries of the kv head's group) . k_mean of the page
+ * in fp64 (exact for ordinary values); of equal ones the first, NaN as the
+ * least.  blocks holds them in ascending order and -1 after them; all -1 for a token
+ * whose index is negative or past the table, or a sequence whose length is above max_length.  A table entry that
+ * names no page scores as the least. */
+typedef struct {
+  lmop_cache cache;      /* k_mean, n_pages and page_size; the rest is not looked at */
+  lmop_batch batch;
+  const void* q;         /* [n_tokens][n_heads * head_dim] */
+  int32_t* blocks;       /* [n_tokens][n_kv_heads][n_blocks] */
+  int64_t ldq;
+  int32_t n_blocks;      /* 1 .. 1024 */
+  int32_t max_length;    /* at least the longest length; at most 16384 pages' */
+  int32_t dtype;         /* LMOP_F16 or LMOP_BF16, of q and k_mean */
+} lmop_select_args;
+lmop_status lmop_select_blocks(lmop_ctx* ctx, const lmop_select_args* args);
 
 #ifdef __cplusplus
 }

@@ -16,7 +16,8 @@ OBJ = os.path.join(PKG, "_build")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "liblmop.so")
 SOURCES = ["gemm.hip", "attention.hip", "elementwise.hip", "fp8_matmul.hip", "quantize.hip",
-           "qk_norm_rope.hip", "lmop_api.cpp"]
+           "qk_norm_rope.hip", "paged_cache.hip", "paged_attention.hip", "select_blocks.hip",
+           "lmop_api.cpp"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

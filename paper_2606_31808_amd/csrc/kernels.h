@@ -201,4 +201,22 @@ struct QkArgs {
 };
 hipError_t launch_qk_norm_rope(hipStream_t s, const QkArgs& a);
 
+// ---------------------------------------------------------------- paged cache
+// The operators of include/lmop.h, checked by the caller: sizes above zero, with the
+// model's head counts.
+struct Heads {
+  int nq, nkv, hd;
+};
+struct AppendArgs {
+  lmop_append_args t;
+  Heads n;
+  const float2* rope;  // [max_seq][hd/2] (cos, sin)
+  int max_seq;
+};
+hipError_t launch_cache_append(hipStream_t s, const AppendArgs& a);
+hipError_t launch_select_blocks(hipStream_t s, const lmop_select_args& a, const Heads& n);
+struct AttendPlan;
+// queues the plan's one to three kernels
+hipError_t launch_attend(hipStream_t s, const lmop_attend_args& a, const Heads& n, const AttendPlan& plan);
+
 }  // namespace lmop

@@ -22,6 +22,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "attend_plan.h"
 #include "kernels.h"
 
 using namespace lmop;
@@ -1620,6 +1621,124 @@ lmop_status check_codes(lmop_ctx* c, const char* what, const void* p, int64_t le
   return LMOP_OK;
 }
 
+// ---- a paged cache and its batch
+constexpr int64_t kMaxPageStride = int64_t(1) << 32;
+constexpr int kMaxSelected = 1024;
+constexpr int64_t kMaxSelectPages = 16384;
+
+lmop_status check_ptr(lmop_ctx* c, const char* what, const void* p, size_t align) {
+  if (!p) return fail(c, LMOP_ERR_INVALID_ARG, "%s is NULL", what);
+  if ((uintptr_t)p % align != 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "%s is not aligned to %zu bytes", what, align);
+  return LMOP_OK;
+}
+
+lmop_status check_token_dtype(lmop_ctx* c, int32_t dtype) {
+  if (dtype != LMOP_F16 && dtype != LMOP_BF16)
+    return fail(c, LMOP_ERR_INVALID_ARG, "dtype %d (F16 or BF16)", dtype);
+  return LMOP_OK;
+}
+
+lmop_status check_page_size(lmop_ctx* c, const lmop_cache& k) {
+  if (k.page_size < 16 || k.page_size > 256 || (k.page_size & (k.page_size - 1)) != 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "page_size %d (16, 32, 64, 128 or 256)", k.page_size);
+  if (k.n_pages < 1) return fail(c, LMOP_ERR_INVALID_ARG, "n_pages %d", k.n_pages);
+  return LMOP_OK;
+}
+
+lmop_status check_cache(lmop_ctx* c, const lmop_cache& k, int32_t dtype) {
+  LMOP_TRY(check_page_size(c, k));
+  if (k.dtype != LMOP_E4M3 && k.dtype != dtype)
+    return fail(c, LMOP_ERR_INVALID_ARG, "pages of dtype %d for tokens of %d (the same, or E4M3)", k.dtype, dtype);
+  LMOP_TRY(check_ptr(c, "cache.k", k.k, 16));
+  LMOP_TRY(check_ptr(c, "cache.v", k.v, 16));
+  if (k.dtype == LMOP_E4M3) {
+    LMOP_TRY(check_ptr(c, "cache.k_exp", k.k_exp, 16));
+    LMOP_TRY(check_ptr(c, "cache.v_exp", k.v_exp, 16));
+  } else if (k.k_exp || k.v_exp) {
+    return fail(c, LMOP_ERR_INVALID_ARG, "exponents with 16-bit pages");
+  }
+  if ((uintptr_t)k.k_mean % 16 != 0) return fail(c, LMOP_ERR_INVALID_ARG, "cache.k_mean is not aligned to 16 bytes");
+  if (k.page_stride < (int64_t)c->nkv_dim * k.page_size || k.page_stride % 16 != 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "pages of %lld elements are %lld apart (a multiple of 16)",
+                (long long)c->nkv_dim * k.page_size, (long long)k.page_stride);
+  if (k.page_stride > kMaxPageStride)
+    return fail(c, LMOP_ERR_UNSUPPORTED, "pages %lld elements apart", (long long)k.page_stride);
+  return LMOP_OK;
+}
+
+// sizes first: a batch of none is a no-op, whatever its pointers
+lmop_status check_batch_sizes(lmop_ctx* c, const lmop_batch& b) {
+  if (b.n_seqs < 0 || b.n_tokens < 0 || b.max_pages < 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "n_seqs %d, n_tokens %d, max_pages %d", b.n_seqs, b.n_tokens, b.max_pages);
+  return LMOP_OK;
+}
+lmop_status check_batch(lmop_ctx* c, const lmop_batch& b, int page_size) {
+  if (!b.start && b.n_tokens != b.n_seqs)
+    return fail(c, LMOP_ERR_INVALID_ARG, "%d tokens of %d sequences without starts", b.n_tokens, b.n_seqs);
+  if (b.max_pages > 0) LMOP_TRY(check_rows(c, "batch.table", b.table, b.max_pages, b.ld_table, 4, 4));
+  LMOP_TRY(check_ptr(c, "batch.length", b.length, 4));
+  if ((uintptr_t)b.start % 4 != 0) return fail(c, LMOP_ERR_INVALID_ARG, "batch.start is not aligned to 4 bytes");
+  if ((int64_t)b.max_pages * page_size > (int64_t(1) << 30))
+    return fail(c, LMOP_ERR_UNSUPPORTED, "%d pages of %d tokens for a sequence", b.max_pages, page_size);
+  // HIP launches fewer than 2^32 threads at a time: 16 million workgroups of 256
+  if (((uint64_t)b.n_tokens + 2 * (uint64_t)b.n_seqs) * (uint64_t)(c->cfg.n_heads + 2 * c->cfg.n_kv_heads) >
+      kMaxTasks / 64)
+    return fail(c, LMOP_ERR_UNSUPPORTED, "%d tokens of %d sequences are too many for one call", b.n_tokens, b.n_seqs);
+  return LMOP_OK;
+}
+
+AttendSizes attend_sizes(const lmop_ctx* c, const lmop_attend_args& a) {
+  AttendSizes s{};
+  s.n_seqs = a.batch.n_seqs;
+  s.n_tokens = a.batch.n_tokens;
+  s.max_tokens = a.max_tokens;
+  s.max_length = a.max_length;
+  s.prefix_length = a.prefix_length;
+  s.n_blocks = a.n_blocks;
+  s.page_size = a.cache.page_size;
+  s.nq = c->cfg.n_heads;
+  s.nkv = c->cfg.n_kv_heads;
+  s.hd = c->cfg.head_dim;
+  s.starts = a.batch.start != nullptr;
+  return s;
+}
+
+// the sizes that a plan is made from; *empty: nothing to do
+lmop_status check_attend_sizes(lmop_ctx* c, const lmop_attend_args& a, bool* empty) {
+  LMOP_TRY(check_token_dtype(c, a.dtype));
+  LMOP_TRY(check_batch_sizes(c, a.batch));
+  if (a.prefix_length < 0 || a.n_blocks < 0 || a.max_tokens < 0 || a.max_length < 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "prefix_length %d, n_blocks %d, max_tokens %d, max_length %d",
+                a.prefix_length, a.n_blocks, a.max_tokens, a.max_length);
+  *empty = a.batch.n_tokens == 0 || a.batch.n_seqs == 0;
+  if (*empty) return LMOP_OK;
+  LMOP_TRY(check_page_size(c, a.cache));
+  if (!a.batch.start && (a.batch.n_tokens != a.batch.n_seqs || a.max_tokens != 1))
+    return fail(c, LMOP_ERR_INVALID_ARG, "%d tokens of %d sequences (at most %d of one) without starts",
+                a.batch.n_tokens, a.batch.n_seqs, a.max_tokens);
+  if (a.max_tokens < 1 || a.max_tokens > a.batch.n_tokens)
+    return fail(c, LMOP_ERR_INVALID_ARG, "max_tokens %d of %d tokens", a.max_tokens, a.batch.n_tokens);
+  if (a.max_length > (int64_t)a.batch.max_pages * a.cache.page_size)
+    return fail(c, LMOP_ERR_INVALID_ARG, "max_length %d: %d pages of %d", a.max_length, a.batch.max_pages,
+                a.cache.page_size);
+  if (a.prefix_length > (1 << 29))
+    return fail(c, LMOP_ERR_UNSUPPORTED, "a prefix of %d keys", a.prefix_length);
+  if (a.n_blocks > 0 && a.prefix_length > 0)
+    return fail(c, LMOP_ERR_INVALID_ARG, "blocks and a prefix of %d keys", a.prefix_length);
+  if (a.n_blocks > (1 << 16)) return fail(c, LMOP_ERR_UNSUPPORTED, "%d blocks", a.n_blocks);
+  const AttendSizes s = attend_sizes(c, a);
+  if (((uint64_t)s.n_tokens + s.n_seqs) * s.nq > kMaxTasks / 64)
+    return fail(c, LMOP_ERR_UNSUPPORTED, "%d tokens of %d sequences are too many for one call", s.n_tokens, s.n_seqs);
+  // fewer than 2^32 threads a launch, at most 65535 splits
+  const AttendPlan p = plan_attend(s);
+  for (const AttendLaunch& l : {p.own, p.prefix})
+    if (l.splits > 65535 || (uint64_t)l.tiles * s.nkv * l.splits >= kMaxTasks / 64)
+      return fail(c, LMOP_ERR_UNSUPPORTED, "%d tokens over %d keys (%d blocks) behind %d are too many for one call",
+                  s.n_tokens, s.max_length, s.n_blocks, s.prefix_length);
+  return LMOP_OK;
+}
+
 int64_t fp8_groups(int64_t features) {
   return (features + LMOP_FP8_GROUP - 1) / LMOP_FP8_GROUP;
 }
@@ -2951,6 +3070,114 @@ lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* a) {
   qa.max_seq = ctx->cfg.max_seq;
   return queue_operator(ctx, "qk_norm_rope", 7 * e, 4 * e,
                         [&](hipStream_t s) { return launch_qk_norm_rope(s, qa); });
+}
+
+lmop_status lmop_cache_append(lmop_ctx* ctx, const lmop_append_args* a) {
+  LMOP_TRY(enter_operator(ctx, a));
+  const int64_t nqd = ctx->nq_dim, nkvd = ctx->nkv_dim;
+  LMOP_TRY(check_token_dtype(ctx, a->dtype));
+  LMOP_TRY(check_batch_sizes(ctx, a->batch));
+  if (a->first < 0 || (a->rotate != 0 && a->rotate != 1))
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "first %d, rotate %d (0 or 1)", a->first, a->rotate);
+  if (a->batch.n_tokens == 0 || a->batch.n_seqs == 0) return LMOP_OK;
+  LMOP_TRY(check_cache(ctx, a->cache, a->dtype));
+  LMOP_TRY(check_batch(ctx, a->batch, a->cache.page_size));
+  LMOP_TRY(check_rows(ctx, "k", a->k, nkvd, a->ldk, 2, 2));
+  LMOP_TRY(check_rows(ctx, "v", a->v, nkvd, a->ldv, 2, 2));
+  if (a->q) {
+    LMOP_TRY(check_rows(ctx, "q", a->q, nqd, a->ldq, 2, 2));
+    LMOP_TRY(check_rows(ctx, "q_out", a->q_out, nqd, a->ldqo, 2, 2));
+    if (a->q_out == a->q && a->ldqo != a->ldq)
+      return fail(ctx, LMOP_ERR_INVALID_ARG, "q_out is q, with another stride");
+  }
+  AppendArgs k{};
+  k.t = *a;
+  k.n = Heads{ctx->cfg.n_heads, ctx->cfg.n_kv_heads, ctx->cfg.head_dim};
+  k.rope = ctx->rope_tab;
+  k.max_seq = ctx->cfg.max_seq;
+  const double n = a->batch.n_tokens, kept = a->cache.dtype == LMOP_E4M3 ? 1 : 2;
+  return queue_operator(ctx, "cache_append", n * 3 * ((a->q ? nqd : 0) + nkvd),
+                        n * ((a->q ? 4.0 * nqd : 0) + 2 * nkvd * (2 + kept)),
+                        [&](hipStream_t s) { return launch_cache_append(s, k); });
+}
+
+lmop_status lmop_attend_workspace(lmop_ctx* ctx, const lmop_attend_args* a, uint64_t* bytes) {
+  LMOP_TRY(enter_operator(ctx, a));
+  if (!bytes) return fail(ctx, LMOP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = 0;
+  bool empty;
+  LMOP_TRY(check_attend_sizes(ctx, *a, &empty));
+  if (empty) return LMOP_OK;
+  const AttendSizes s = attend_sizes(ctx, *a);
+  *bytes = attend_workspace(plan_attend(s), s);
+  return LMOP_OK;
+}
+
+lmop_status lmop_attend(lmop_ctx* ctx, const lmop_attend_args* a) {
+  LMOP_TRY(enter_operator(ctx, a));
+  const int64_t nqd = ctx->nq_dim, nkvd = ctx->nkv_dim;
+  bool empty;
+  LMOP_TRY(check_attend_sizes(ctx, *a, &empty));
+  if (empty) return LMOP_OK;
+  LMOP_TRY(check_cache(ctx, a->cache, a->dtype));
+  LMOP_TRY(check_batch(ctx, a->batch, a->cache.page_size));
+  LMOP_TRY(check_rows(ctx, "q", a->q, nqd, a->ldq, 2, 2));
+  LMOP_TRY(check_rows(ctx, "out", a->out, nqd, a->ldo, 2, 2));
+  if (a->out == a->q) return fail(ctx, LMOP_ERR_INVALID_ARG, "out is q");
+  if ((uintptr_t)a->lse % 4 != 0) return fail(ctx, LMOP_ERR_INVALID_ARG, "lse is misaligned");
+  if (a->n_blocks > 0) {
+    LMOP_TRY(check_ptr(ctx, "blocks", a->blocks, 4));
+  } else if (a->blocks) {
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "blocks with n_blocks 0");
+  }
+  if (a->prefix_length > 0) LMOP_TRY(check_ptr(ctx, "prefix", a->prefix, 4));
+  if (a->scale != 0.f && !(a->scale >= 1e-30f && a->scale <= 1e30f))
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "scale %g (0, or 1e-30 to 1e30)", a->scale);
+  const AttendSizes s = attend_sizes(ctx, *a);
+  const AttendPlan plan = plan_attend(s);
+  const uint64_t need = attend_workspace(plan, s);
+  if (need > 0) {
+    if (a->workspace_bytes < need)
+      return fail(ctx, LMOP_ERR_INVALID_ARG, "a workspace of %llu bytes, %llu needed",
+                  (unsigned long long)a->workspace_bytes, (unsigned long long)need);
+    LMOP_TRY(check_ptr(ctx, "workspace", a->workspace, 256));
+  }
+  const int64_t own = a->n_blocks > 0 ? (int64_t)a->n_blocks * a->cache.page_size : a->max_length;
+  // as if every sequence were the longest: the lengths are in device memory
+  const double keys = (double)own + a->prefix_length, n = s.n_tokens;
+  const double one = nkvd * (a->cache.dtype == LMOP_E4M3 ? 2.0 : 4.0);
+  return queue_operator(ctx, a->n_blocks > 0 ? "attend_blocks" : "attend", 4 * n * nqd * keys,
+                        4 * n * nqd + one * ((a->n_blocks > 0 ? n : (double)s.n_seqs) * own + a->prefix_length),
+                        [&](hipStream_t st) {
+                          return launch_attend(st, *a, Heads{s.nq, s.nkv, s.hd}, plan);
+                        });
+}
+
+lmop_status lmop_select_blocks(lmop_ctx* ctx, const lmop_select_args* a) {
+  LMOP_TRY(enter_operator(ctx, a));
+  LMOP_TRY(check_token_dtype(ctx, a->dtype));
+  LMOP_TRY(check_batch_sizes(ctx, a->batch));
+  if (a->n_blocks < 0 || a->max_length < 0)
+    return fail(ctx, LMOP_ERR_INVALID_ARG, "n_blocks %d, max_length %d", a->n_blocks, a->max_length);
+  if (a->batch.n_tokens == 0 || a->batch.n_seqs == 0 || a->n_blocks == 0) return LMOP_OK;
+  if (a->n_blocks > kMaxSelected)
+    return fail(ctx, LMOP_ERR_UNSUPPORTED, "%d blocks (at most %d)", a->n_blocks, kMaxSelected);
+  LMOP_TRY(check_page_size(ctx, a->cache));
+  LMOP_TRY(check_ptr(ctx, "cache.k_mean", a->cache.k_mean, 16));
+  LMOP_TRY(check_batch(ctx, a->batch, a->cache.page_size));
+  if (a->max_length > kMaxSelectPages * a->cache.page_size)
+    return fail(ctx, LMOP_ERR_UNSUPPORTED, "max_length %d: at most %lld pages of %d", a->max_length,
+                (long long)kMaxSelectPages, a->cache.page_size);
+  LMOP_TRY(check_rows(ctx, "q", a->q, ctx->nq_dim, a->ldq, 2, 2));
+  LMOP_TRY(check_ptr(ctx, "blocks", a->blocks, 4));
+  const double n = a->batch.n_tokens, pages = (double)a->max_length / a->cache.page_size;
+  return queue_operator(ctx, "select_blocks", 2 * n * ctx->nkv_dim * pages,
+                        n * 2 * ctx->nq_dim + 2.0 * a->batch.n_seqs * pages * ctx->nkv_dim +
+                            4 * n * ctx->cfg.n_kv_heads * a->n_blocks,
+                        [&](hipStream_t s) {
+                          return launch_select_blocks(
+                              s, *a, Heads{ctx->cfg.n_heads, ctx->cfg.n_kv_heads, ctx->cfg.head_dim});
+                        });
 }
 
 lmop_status lmop_set_profiling(lmop_ctx* ctx, int32_t period) {

@@ -1,0 +1,86 @@
+// Device side of a paged cache: batches, pages, and the types that pages hold.
+#pragma once
+#include "common.h"
+#include "lmop.h"
+
+namespace lmop {
+
+typedef f16 f16x8u __attribute__((ext_vector_type(8), aligned(2)));
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// 16-bit types: vectors, the matrix instruction (operands as mfma16x16x32's), E4M3 codes times a
+// power of two (two codes of a word; exact, but for what lies past the type's range)
+template <typename T>
+struct Half;
+template <>
+struct Half<f16> {
+  typedef f16x2 x2;
+  typedef f16x4 x4;
+  typedef f16x8 x8;
+  static LMOP_DEVICE f32x4 mfma(x8 a, x8 b, f32x4 c) { return mfma16x16x32(a, b, c); }
+  template <bool HI>
+  static LMOP_DEVICE x2 decode(uint32_t w, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, HI);
+  }
+};
+template <>
+struct Half<bf16> {
+  typedef bf16x2 x2;
+  typedef bf16x4 x4;
+  typedef bf16x8 x8;
+  static LMOP_DEVICE f32x4 mfma(x8 a, x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  template <bool HI>
+  static LMOP_DEVICE x2 decode(uint32_t w, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI);
+  }
+};
+
+// 2^(e - 127) of an exponent byte 1 .. 254
+LMOP_DEVICE float exp_scale(uint32_t e) { return __uint_as_float(e << 23); }
+
+// eight codes of two words
+template <typename T>
+LMOP_DEVICE typename Half<T>::x8 decode8(uint32_t lo, uint32_t hi, float scale) {
+  const auto a = Half<T>::template decode<false>(lo, scale), b = Half<T>::template decode<true>(lo, scale);
+  const auto c = Half<T>::template decode<false>(hi, scale), d = Half<T>::template decode<true>(hi, scale);
+  return typename Half<T>::x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The tokens of sequence s: [x, y)
+LMOP_DEVICE int2 seq_tokens(const lmop_batch& b, int s) {
+  if (!b.start) return int2{s, s + 1};
+  int x = b.start[s], y = b.start[s + 1];
+  x = x < 0 ? 0 : x > b.n_tokens ? b.n_tokens : x;
+  y = y < x ? x : y > b.n_tokens ? b.n_tokens : y;
+  return int2{x, y};
+}
+
+// The last s in [0, n) with base(s) <= i (base ascending, base(0) <= i), by a whole
+// wave: 64 probes a step, so two dependent loads for up to 4096 sequences.
+template <typename F>
+LMOP_DEVICE int find_seq(int n, int i, F&& base) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64;
+    const int at = lo + (lane + 1) * step;
+    const bool below = at < hi && base(at) <= i;
+    const int count = __builtin_popcountll(__ballot(below));
+    lo += count * step;
+    hi = hi < lo + step ? hi : lo + step;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// The page of a sequence's keys b * page_size and on, or -1
+LMOP_DEVICE int page_of(const lmop_batch& b, int n_pages, int s, int block) {
+  if (block < 0 || block >= b.max_pages) return -1;
+  const int p = b.table[(int64_t)s * b.ld_table + block];
+  return p >= 0 && p < n_pages ? p : -1;
+}
+
+}  // namespace lmop

@@ -1,0 +1,873 @@
+// Attention of a batch's tokens over a paged cache, and over a prefix that the
+// batch shares.
+//
+// Per query vector (a token and a head; the G heads of a kv head lie side by side)
+//   out = sum_i exp(z_i - m) v_i / sum_i exp(z_i - m),   z_i = scale * q . k_i,
+// in one pass over the keys: m is a reference that follows the largest score, and
+// when it moves, the sums so far are multiplied by exp(m_old - m_new).  Sums over
+// disjoint sets of keys join the same way, so a long axis is split among
+// workgroups and the prefix is walked once for all sequences' tokens;
+// combine_kernel joins the parts.
+//
+// Two kernels:
+//  * few vectors (a decode step: G vectors against a sequence's keys).  Bound by
+//    reading the cache once.  Keys and values go from memory straight to the registers of
+//    the wave that uses them: nothing is shared between waves, so LDS would only
+//    add a copy and a barrier.
+//  * tiles (prompts, rows, the shared prefix): 128 vectors against blocks of 64 keys
+//    in LDS.  Bound by the matrix and vector units.
+//
+// Both compute S^T = K Q^T and O^T = V^T P^T with the 16x16x32 instruction, so
+// that scores, maxima and outputs of a query vector stay in one column of lanes
+// (lane 16 g + c: vector c) and P^T leaves the first product in the layout that
+// the second one reads, if key rows are taken in score_key's order.  Row sums of
+// P come from the same instruction, with ones for V^T: they are then the sums of the rounded
+// weights, and cost the vector units nothing.
+#include <math.h>
+
+#include "attend_plan.h"
+#include "kernels.h"
+#include "paged.h"
+
+namespace lmop {
+
+namespace {
+
+// The tile of 32 keys: score tile hf (0, 1) row m holds key 8 (m / 4) + 4 hf + m % 4, so
+// lane group g has scores of keys 8g + 4 hf + r, r = 0..3: 8g .. 8g+7 in order
+LMOP_DEVICE int score_key(int hf, int m) { return 8 * (m >> 2) + 4 * hf + (m & 3); }
+
+// over the lanes 16 and 32 apart: the four lanes of a query vector
+LMOP_DEVICE float max4(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+struct Args {
+  lmop_attend_args t;
+  Heads n;
+  AttendLaunch l;
+  float c;      // scale * log2(e): weights are 2^(c z' - c m) of the unscaled scores z'
+  int flat;     // the launch over the prefix: vectors of all tokens
+  int fused;    // own launch that walks the prefix first
+  int parts;    // 0: writes the output
+  int part0;    // the launch's first part
+};
+
+// partial results in the workspace: o [part][token][head][hd], then (m, l) [part][token][head]
+LMOP_DEVICE float* part_o(const Args& a, int part, int t, int h) {
+  return (float*)a.t.workspace + (((size_t)part * a.t.batch.n_tokens + t) * a.n.nq + h) * a.n.hd;
+}
+LMOP_DEVICE float2* part_ml(const Args& a, int part, int t, int h) {
+  return (float2*)((float*)a.t.workspace + (size_t)a.parts * a.t.batch.n_tokens * a.n.nq * a.n.hd) +
+         ((size_t)part * a.t.batch.n_tokens + t) * a.n.nq + h;
+}
+
+// The running state of a vector: reference m of the unscaled scores (-inf: none seen yet).  It moves
+// only where a score exceeds it by more than 2^8 in weight, so that the sums are seldom rescaled.
+LMOP_DEVICE float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// exp2 of a difference of references, 0 where there was none
+LMOP_DEVICE float rescale(float m_old, float m_new, float c) {
+  return m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - m_new) * c);
+}
+
+// What a workgroup works on: vectors v0 .. of tokens [tok.x, tok.y); a vector is token
+// tok.x + v / G, head kv * G + v % G
+struct Tile {
+  int2 tok;
+  int v0;
+  int seq;
+  int len;   // keys of the sequence
+  bool bad;  // the sequence gets NaN
+};
+
+LMOP_DEVICE Tile find_tile(const Args& a, int tile, int vectors) {
+  const lmop_batch& b = a.t.batch;
+  Tile w{};
+  if (a.flat) {
+    w.tok = int2{0, b.n_tokens};
+    w.v0 = tile * vectors;
+    return w;
+  }
+  const int G = a.n.nq / a.n.nkv;
+  if (a.l.per_seq) {
+    w.seq = tile / a.l.per_seq;
+    w.tok = seq_tokens(b, w.seq);
+    w.v0 = tile % a.l.per_seq * vectors;
+  } else {
+    // sequence s has the tiles from base(s) on, at least as many as it needs
+    auto base = [&](int i) { return (int)((int64_t)seq_tokens(b, i).x * G / vectors) + i; };
+    w.seq = find_seq(b.n_seqs, tile, base);
+    w.tok = seq_tokens(b, w.seq);
+    const int nth = tile - base(w.seq);
+    w.v0 = nth < 0 ? (w.tok.y - w.tok.x) * G : nth * vectors;
+  }
+  w.len = b.length[w.seq];
+  w.bad = w.len < 0 || w.len > a.t.max_length || w.tok.y - w.tok.x > a.t.max_tokens;
+  return w;
+}
+
+template <typename T>
+LMOP_DEVICE void write_bad(const Args& a, int t, int h, int part, int lane, int lanes) {
+  if (a.parts) {
+    if (lane == 0) *part_ml(a, part, t, h) = float2{0.f, NAN};
+    return;
+  }
+  for (int d = lane; d < a.n.hd; d += lanes) ((T*)a.t.out)[t * a.t.ldo + h * a.n.hd + d] = (T)NAN;
+  if (lane == 0 && a.t.lse) a.t.lse[(size_t)t * a.n.nq + h] = NAN;
+}
+
+LMOP_DEVICE float lse_of(const Args& a, float m, float l) {
+  // l > 0 means that some score was finite
+  return l == 0.f ? -INFINITY : (m * a.c + __log2f(l)) * 0.6931471805599453f;
+}
+
+// ---------------------------------------------------------------- few vectors
+constexpr int kFewWaves = 4;
+
+// One workgroup: 16 vectors x a kv head x a split.  Its pages are looked up once, into LDS; wave
+// w takes the 32-key chunks w, w + 4, ...; the four waves' states are joined through LDS at the
+// end.
+//
+// A lane's share of a chunk: the key rows that score_key names for its column, hd / 4 dimensions of each (its group's), as the
+// first product reads them; and 8 value rows (its group's keys), 16 lanes side by side along
+// hd.  The second product needs 8 keys of a dimension in a lane, so the rows are transposed
+// in registers, half a v_perm an element.
+template <typename T, bool E8, int HD, bool BLOCKS>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
+  typedef typename Half<T>::x8 x8;
+  constexpr int NS = HD / 32;   // k-steps of the score product
+  constexpr int NT = HD / 16;   // output tiles; lane column c has dimensions NT c .. of a value row
+  constexpr int ORow = HD + 4;  // of the joined outputs in LDS
+  __shared__ int e_page[kMaxEntries + 16], e_first[kMaxEntries + 16], e_cap[kMaxEntries + 16];
+  __shared__ float s_ml[kFewWaves][2][16];
+  __shared__ __attribute__((aligned(16))) float s_o[kFewWaves][16][ORow];
+
+  const lmop_attend_args& p = a.t;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  const int tile = blockIdx.x / a.n.nkv, h = blockIdx.x % a.n.nkv, split = blockIdx.y;
+  const int G = a.n.nq / a.n.nkv;
+  const int ps = p.cache.page_size, lps = __builtin_ctz(ps);
+  const int part = a.part0 + split;
+
+  Tile w;
+  if constexpr (BLOCKS) {
+    const int t = tile / a.l.per_seq;
+    w = Tile{};
+    w.seq = t;
+    if (p.batch.start) {
+      if (t < p.batch.start[0] || t >= p.batch.start[p.batch.n_seqs]) return;
+      w.seq = find_seq(p.batch.n_seqs, t, [&](int i) { return p.batch.start[i]; });
+    }
+    const int2 all = seq_tokens(p.batch, w.seq);
+    // the sequence as it was at this token
+    w.tok = int2{t, t + 1};
+    const int len = p.batch.length[w.seq];
+    w.bad = len < 0 || len > p.max_length || all.y - all.x > p.max_tokens;
+    w.len = w.bad ? 0 : len - (all.y - t) + 1;
+    w.v0 = tile % a.l.per_seq * kFewVectors;
+  } else {
+    w = find_tile(a, tile, kFewVectors);
+  }
+  const int nv = (w.tok.y - w.tok.x) * G;  // vectors
+  if (w.bad) {
+    // a workgroup of the sequence's first tile does all of its tokens: there may be more than max_tokens
+    if (w.v0 == 0)
+      for (int v = wave; v < nv; v += kFewWaves)
+        write_bad<T>(a, w.tok.x + v / G, h * G + v % G, part, lane, 64);
+    return;
+  }
+  if (w.v0 >= nv) return;
+
+  // the keys that the tile's vectors see, and the pages that hold them
+  const int n_tok = w.tok.y - w.tok.x;
+  const int t_first = w.v0 / G;
+  const int t_last = (w.v0 + kFewVectors - 1) / G < n_tok ? (w.v0 + kFewVectors - 1) / G : n_tok - 1;
+  // index of the last key that a token of the sequence sees
+  const int lim_max = w.len - n_tok + t_last;
+  const bool shared = a.flat || a.fused;
+  const int n_pre = shared ? (int)((p.prefix_length + (int64_t)ps - 1) >> lps) : 0;
+  const int n_own = a.flat ? 0 : BLOCKS ? p.n_blocks : lim_max < 0 ? 0 : (lim_max >> lps) + 1;
+  const int64_t from = (int64_t)split * a.l.chunk;
+  const int64_t left = (int64_t)n_pre + n_own - from;
+  const int ne = (int)(left < 0 ? 0 : left < a.l.chunk ? left : a.l.chunk);
+  for (int i = tid; i < kMaxEntries + 16; i += 64 * kFewWaves) {
+    int page = 0, first = 0, cap = 0;
+    if (i < ne) {
+      const int e = (int)from + i;
+      if (e < n_pre) {
+        const int q = p.prefix[e];
+        page = q >= 0 && q < p.cache.n_pages ? q : -1;
+        first = -(1 << 30);  // every token sees it
+        cap = p.prefix_length - (e << lps) < ps ? p.prefix_length - (e << lps) : ps;
+      } else {
+        int b = e - n_pre;
+        if constexpr (BLOCKS) b = p.blocks[((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks + b];
+        // (a block past what the token sees is left out here, so its page does not matter)
+        if (b >= 0 && b < p.batch.max_pages && b <= (lim_max >> lps)) {
+          page = page_of(p.batch, p.cache.n_pages, w.seq, b);
+          first = b << lps;
+          cap = ps;
+        }
+      }
+    }
+    if (i < ((ne + 15) & ~15) + 1) e_page[i] = page, e_first[i] = first, e_cap[i] = cap;
+  }
+
+  // this lane's query vector
+  const int v = w.v0 + c;
+  const bool valid = v < nv;
+  const int tok = valid ? v / G : t_last;
+  const int hq = h * G + (valid ? v - tok * G : 0);
+  const int lim = a.flat ? 0 : w.len - n_tok + tok;
+  const bool one = t_first == t_last || a.flat;  // all vectors see the same keys
+  x8 qf[NS];
+  {
+    const T* q = (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + hq * HD;
+    typedef T xu __attribute__((ext_vector_type(8), aligned(2)));
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      // dimensions of step s: 32 s + 8 g; of 8-bit rows, read 16 at a time, 64 (s / 2) + 16 g + 8 (s % 2)
+      const int d = E8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+      const xu x = valid ? *(const xu*)(q + d) : xu{};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qf[s][i] = x[i];
+    }
+  }
+  __syncthreads();
+
+  f32x4 o[NT], l4 = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < NT; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY;
+  const float thr = 8.0f / a.c;
+  const int n_keys = ne << lps;
+  const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
+
+  for (int kb = wave * 32; kb < n_keys; kb += 32 * kFewWaves) {
+    // halves of 16 keys lie in one page each: this lane's key rows in half c / 8, its values in half g / 2
+    const int at_k = kb + 16 * (c >> 3), at_v = kb + 16 * (g >> 1);
+    const int ek = at_k >> lps, ev = at_v >> lps;
+    const int page_k = e_page[ek], page_v = e_page[ev];
+    const size_t row_k = (size_t)h * ps + (at_k & (ps - 1)) + 8 * ((c >> 2) & 1) + (c & 3);
+    const int slot_v = (at_v & (ps - 1)) + 8 * (g & 1);
+    const size_t row_v = (size_t)h * ps + slot_v;
+    const int64_t pk = page_k < 0 ? 0 : page_k, pv = page_v < 0 ? 0 : page_v;
+
+    x8 kf[2][NS];
+    uint32_t vw[8][NT / 2];  // 8 value rows, 2 values a word
+    if constexpr (!E8) {
+      const T* k = (const T*)p.cache.k + pk * p.cache.page_stride + row_k * HD + 8 * g;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) kf[hf][s] = *(const x8*)(k + 4 * hf * HD + 32 * s);
+      const T* vp = (const T*)p.cache.v + pv * p.cache.page_stride + row_v * HD + NT * c;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (NT == 8) {
+          const uint4 x = *(const uint4*)(vp + j * HD);
+          vw[j][0] = x.x, vw[j][1] = x.y, vw[j][2] = x.z, vw[j][3] = x.w;
+        } else {
+          const uint2 x = *(const uint2*)(vp + j * HD);
+          vw[j][0] = x.x, vw[j][1] = x.y;
+        }
+      }
+    } else {
+      const uint8_t* k = (const uint8_t*)p.cache.k + pk * p.cache.page_stride + row_k * HD + 16 * g;
+      const uint8_t* ke = p.cache.k_exp + pk * a.n.nkv * ps + row_k;
+      uint4 kw[2][NS / 2];
+      uint32_t kx[2];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        kx[hf] = ke[4 * hf];
+#pragma unroll
+        for (int u = 0; u < NS / 2; ++u) kw[hf][u] = *(const uint4*)(k + 4 * hf * HD + 64 * u);
+      }
+      const uint8_t* vp = (const uint8_t*)p.cache.v + pv * p.cache.page_stride + row_v * HD + NT * c;
+      const uint2 vx = *(const uint2*)(p.cache.v_exp + pv * a.n.nkv * ps + row_v);
+      uint32_t raw[8][NT / 4];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (NT == 8) {
+          const uint2 x = *(const uint2*)(vp + j * HD);
+          raw[j][0] = x.x, raw[j][1] = x.y;
+        } else {
+          raw[j][0] = *(const uint32_t*)(vp + j * HD);
+        }
+      }
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const float sc = exp_scale(kx[hf]);
+#pragma unroll
+        for (int u = 0; u < NS / 2; ++u) {
+          kf[hf][2 * u] = decode8<T>(kw[hf][u].x, kw[hf][u].y, sc);
+          kf[hf][2 * u + 1] = decode8<T>(kw[hf][u].z, kw[hf][u].w, sc);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float sc = exp_scale(((j < 4 ? vx.x : vx.y) >> (8 * (j & 3))) & 255u);
+#pragma unroll
+        for (int i = 0; i < NT / 4; ++i) {
+          vw[j][2 * i] = __builtin_bit_cast(uint32_t, Half<T>::template decode<false>(raw[j][i], sc));
+          vw[j][2 * i + 1] = __builtin_bit_cast(uint32_t, Half<T>::template decode<true>(raw[j][i], sc));
+        }
+      }
+    }
+
+    f32x4 st[2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      st[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) st[hf] = Half<T>::mfma(kf[hf][s], qf[s], st[hf]);
+    }
+    // of the lane's 8 keys (4 hf + r), its vector sees the first `seen`; any vector the first `any`
+    const int room = e_cap[ev] - slot_v, first = e_first[ev] + slot_v;
+    const int seen = room < lim - first + 1 ? room : lim - first + 1;
+    const bool whole = __all(seen >= 8 && page_v >= 0);
+    bool apart = false;
+    if (!whole) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          st[hf][r] = 4 * hf + r < seen ? (page_v < 0 ? NAN : st[hf][r]) : -INFINITY;
+      // what no vector sees may hold anything: zeros instead
+      const int any = room < (a.flat ? 0 : lim_max) - first + 1 ? room : (a.flat ? 0 : lim_max) - first + 1;
+      uint32_t odd = 0;  // infinities and NaN (exponent bits all ones)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < NT / 2; ++i) {
+          if (j >= any || page_v < 0) vw[j][i] = 0;
+          constexpr uint32_t E = __is_same(T, f16) ? 0x7C00u : 0x7F80u;
+          odd |= ((vw[j][i] & E) == E) | ((vw[j][i] >> 16 & E) == E);
+        }
+      apart = !one && __any(odd != 0);
+    }
+
+    float mb = -INFINITY;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mb = fmaxf(mb, st[hf][r]);
+    mb = max4(mb);
+    if (__any(mb > m + thr)) {
+      const float m_new = mb > m + thr ? mb : m;
+      const float alpha = rescale(m, m_new, a.c);
+      l4 *= alpha;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[i] *= alpha;
+      m = m_new;
+    }
+    const float nmc = -ref_of(m) * a.c;
+    x8 pb;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        pb[4 * hf + r] = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(st[hf][r], a.c, nmc));
+    l4 = Half<T>::mfma(ones, pb, l4);
+
+    // output tile i: dimension NT c + i of the lane group's 8 keys
+    auto values = [&](int i) {
+      const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
+      uint32_t x[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = __builtin_amdgcn_perm(vw[2 * q + 1][i >> 1], vw[2 * q][i >> 1], sel);
+      return __builtin_bit_cast(x8, uint4{x[0], x[1], x[2], x[3]});
+    };
+    if (!apart) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[i] = Half<T>::mfma(values(i), pb, o[i]);
+    } else {
+      // values that some vectors may not see are infinite or NaN: one token at a time, with zeros
+      // for what it does not see
+      for (int t = t_first; t <= t_last; ++t) {
+        const int lim_t = w.len - n_tok + t;
+        const int seen_t = room < lim_t - first + 1 ? room : lim_t - first + 1;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          x8 x = values(i);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = j < seen_t ? x[j] : (T)0.f;
+          const f32x4 y = Half<T>::mfma(x, pb, o[i]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[i][r] = tok == t ? y[r] : o[i][r];
+        }
+      }
+    }
+  }
+
+  // join the waves
+  if (g == 0) s_ml[wave][0][c] = m, s_ml[wave][1][c] = l4[0];
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kFewWaves; ++i) top = fmaxf(top, s_ml[i][0][c]);
+  const float f = rescale(m, top, a.c);
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int i = 0; i < NT; i += 4) {
+      const f32x4 y = {o[i][r] * f, o[i + 1][r] * f, o[i + 2][r] * f, o[i + 3][r] * f};
+      *(f32x4*)&s_o[wave][c][NT * (4 * g + r) + i] = y;
+    }
+  __syncthreads();
+  // thread: vector tid / 16, NT dimensions
+  const int vo = tid >> 4, d = (tid & 15) * NT;
+  if (w.v0 + vo >= nv) return;
+  const int to = (w.v0 + vo) / G, ho = h * G + (w.v0 + vo) % G;
+  float mt = -INFINITY, lt = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFewWaves; ++i) mt = fmaxf(mt, s_ml[i][0][vo]);
+  float y[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) y[i] = 0.f;
+#pragma unroll
+  for (int q = 0; q < kFewWaves; ++q) {
+    const float lq = s_ml[q][1][vo];
+    lt += lq != lq ? lq : lq * rescale(s_ml[q][0][vo], mt, a.c);
+#pragma unroll
+    for (int i = 0; i < NT; i += 4) {
+      const f32x4 x = *(const f32x4*)&s_o[q][vo][d + i];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[i + r] += x[r];
+    }
+  }
+  const int t = w.tok.x + to;
+  if (a.parts) {
+    float* dst = part_o(a, part, t, ho) + d;
+#pragma unroll
+    for (int i = 0; i < NT; i += 4) *(f32x4*)(dst + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+    if (d == 0) *part_ml(a, part, t, ho) = float2{mt, lt};
+    return;
+  }
+  const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+  typedef T xo __attribute__((ext_vector_type(NT), aligned(2)));
+  xo r;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) r[i] = (T)(lt == 0.f ? 0.f : y[i] * inv);
+  *(xo*)((T*)p.out + t * p.ldo + ho * HD + d) = r;
+  if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + ho] = lse_of(a, mt, lt);
+}
+
+// ---------------------------------------------------------------- tiles
+constexpr int kTileWaves = 4;
+constexpr int KB = kTileKeys;
+
+// 16-byte chunk c of LDS row `key` lies at chunk c ^ kswz: score fragments (score_key's rows, one
+// chunk column) then meet every bank
+template <int HD>
+LMOP_DEVICE int kswz(int key) {
+  const int s = ((key >> 1) & 12) | (key & 3);  // = m of score_key within a tile
+  return HD == 128 ? s : (s & 7);
+}
+// values: 32-byte units, by the keys that one transposing read takes together (4 of one lane
+// group, and the next group's)
+template <int HD>
+LMOP_DEVICE int vswz(int key) {
+  return HD == 128 ? (key & 3) | (key >> 1 & 4) : (key >> 1 & 1) | (key >> 2 & 2);
+}
+
+// 4 keys of a dimension: within 16 lanes, lane 4 j + i gives the address of 4 dimensions (i) of key
+// j, and lane n gets dimension n of keys 0..3
+template <typename T>
+LMOP_DEVICE typename Half<T>::x4 read_transposed(const char* lds) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  const s16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) s16x4*)lds);
+  return __builtin_bit_cast(typename Half<T>::x4, r);
+}
+
+// One workgroup: 128 vectors x a kv head x a split, 32 vectors a wave.  Blocks of 64 keys go through
+// registers (page lookup, codes to 16 bits) into one of two LDS stages while the
+// block before them is worked on.
+template <typename T, bool E8, int HD>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) {
+  typedef typename Half<T>::x8 x8;
+  typedef typename Half<T>::x4 x4;
+  constexpr int NS = HD / 32, NT = HD / 16, QS = 2;
+  constexpr int ROW = HD * 2;                    // bytes of an LDS row
+  constexpr int STAGE = 2 * KB * ROW;            // K, then V
+  constexpr int LANES = E8 ? HD / 16 : HD / 8;   // 16-byte loads of a key row
+  constexpr int ROWS = 64 * kTileWaves / LANES;  // key rows of a pass
+  constexpr int LOADS = KB / ROWS;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+
+  const lmop_attend_args& p = a.t;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  const int h = blockIdx.x % a.n.nkv, split = blockIdx.y;
+  const int G = a.n.nq / a.n.nkv;
+  const int ps = p.cache.page_size, lps = __builtin_ctz(ps);
+  const int part = a.part0 + split;
+  // later tiles of a prompt see more keys: they go first
+  const Tile w = find_tile(a, a.l.tiles - 1 - (int)blockIdx.x / a.n.nkv, kTileVectors);
+  const int n_tok = w.tok.y - w.tok.x, nv = n_tok * G;
+  if (w.v0 >= nv) return;
+  if (w.bad) {
+    // its tiles cover all of its tokens, but where per_seq was reckoned from max_tokens
+    const int end = a.l.per_seq && w.v0 + kTileVectors >= a.l.per_seq * kTileVectors ? nv : w.v0 + kTileVectors;
+    for (int v = w.v0 + wave; v < end && v < nv; v += kTileWaves)
+      write_bad<T>(a, w.tok.x + v / G, h * G + v % G, part, lane, 64);
+    return;
+  }
+
+  const int t_first = w.v0 / G;
+  const int t_last = (w.v0 + kTileVectors - 1) / G < n_tok ? (w.v0 + kTileVectors - 1) / G : n_tok - 1;
+  const int lim_max = a.flat ? -1 : w.len - n_tok + t_last, lim_min = a.flat ? -1 : w.len - n_tok + t_first;
+  const int n_pre = a.flat || a.fused ? p.prefix_length : 0;
+  const int n_own = lim_max + 1 > 0 ? lim_max + 1 : 0;
+  const int nb_pre = (n_pre + KB - 1) / KB;
+  const int nb = nb_pre + (n_own + KB - 1) / KB;
+  const int64_t b_from = (int64_t)split * a.l.chunk;
+  const int b0 = b_from < nb ? (int)b_from : nb;
+  const int b1 = nb - b0 < a.l.chunk ? nb : b0 + a.l.chunk;
+
+  // the block that the staging registers hold
+  uint4 kr[LOADS], vr[LOADS];
+  uint32_t kx[LOADS], vx[LOADS];
+  const int lrow = tid / LANES, lch = tid % LANES;
+  uint32_t load_bad = 0;  // 16-key groups whose page does not exist
+  auto page_at = [&](int b, int grp) {  // of 16 keys, wave-uniform; -1: missing, 0: past the end
+    const bool pre = b < nb_pre;
+    const int key = (pre ? b : b - nb_pre) * KB + 16 * grp;
+    if (key >= (pre ? n_pre : n_own)) return 0;
+    if (!pre) return __builtin_amdgcn_readfirstlane(page_of(p.batch, p.cache.n_pages, w.seq, key >> lps));
+    const int q = __builtin_amdgcn_readfirstlane(p.prefix[key >> lps]);
+    return q >= 0 && q < p.cache.n_pages ? q : -1;
+  };
+  auto load = [&](int b) {
+    const bool pre = b < nb_pre;
+    const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
+    load_bad = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_bad |= page_at(b, i) < 0 ? 1u << i : 0u;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = lrow + i * ROWS;
+      int pg = page_at(b, __builtin_amdgcn_readfirstlane(r >> 4));
+      pg = pg < 0 ? 0 : pg;
+      const size_t row = (size_t)h * ps + ((kb + r) & (ps - 1));
+      const size_t at = (pg * p.cache.page_stride + row * HD) * (E8 ? 1 : 2) + lch * 16;
+      kr[i] = *(const uint4*)((const char*)p.cache.k + at);
+      vr[i] = *(const uint4*)((const char*)p.cache.v + at);
+      if (kb + r >= n) vr[i] = uint4{0, 0, 0, 0};
+      if constexpr (E8) {
+        kx[i] = p.cache.k_exp[(size_t)pg * a.n.nkv * ps + row];
+        vx[i] = p.cache.v_exp[(size_t)pg * a.n.nkv * ps + row];
+      }
+    }
+  };
+  auto store = [&](int st) {
+    char* sk = smem + st * STAGE;
+    char* sv = sk + KB * ROW;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = lrow + i * ROWS;
+      // chunk ch of a row: keys by 16-byte chunks, values by 32-byte units
+      auto put = [&](int ch, const uint4& k, const uint4& v) {
+        *(uint4*)(sk + r * ROW + ((ch ^ kswz<HD>(r)) * 16)) = k;
+        *(uint4*)(sv + r * ROW + (((ch >> 1) ^ vswz<HD>(r)) * 32) + (ch & 1) * 16) = v;
+      };
+      if constexpr (!E8) {
+        put(lch, kr[i], vr[i]);
+      } else {
+        const float ks = exp_scale(kx[i]), vs = exp_scale(vx[i]);
+        put(2 * lch, __builtin_bit_cast(uint4, decode8<T>(kr[i].x, kr[i].y, ks)),
+            __builtin_bit_cast(uint4, decode8<T>(vr[i].x, vr[i].y, vs)));
+        put(2 * lch + 1, __builtin_bit_cast(uint4, decode8<T>(kr[i].z, kr[i].w, ks)),
+            __builtin_bit_cast(uint4, decode8<T>(vr[i].z, vr[i].w, vs)));
+      }
+    }
+  };
+
+  // this lane's vectors: 32 of the wave, column c of two
+  x8 qf[QS][NS];
+  int lim[QS], tok[QS], hq[QS];
+  bool valid[QS];
+#pragma unroll
+  for (int qs = 0; qs < QS; ++qs) {
+    const int v = w.v0 + wave * 16 * QS + 16 * qs + c;
+    valid[qs] = v < nv;
+    tok[qs] = valid[qs] ? v / G : t_last;
+    hq[qs] = h * G + (valid[qs] ? v - tok[qs] * G : 0);
+    lim[qs] = a.flat ? -1 : w.len - n_tok + tok[qs];
+    const T* q = (const T*)p.q + (int64_t)(w.tok.x + tok[qs]) * p.ldq + hq[qs] * HD;
+    typedef T xu __attribute__((ext_vector_type(8), aligned(2)));
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const xu x = valid[qs] ? *(const xu*)(q + 32 * s + 8 * g) : xu{};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qf[qs][s][i] = x[i];
+    }
+  }
+  // a wave whose vectors all lie past the end only helps to load
+  const bool active = w.v0 + wave * 16 * QS < nv;
+
+  f32x4 o[QS][NT], l4[QS];
+  float m[QS];
+#pragma unroll
+  for (int qs = 0; qs < QS; ++qs) {
+    m[qs] = -INFINITY;
+    l4[qs] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NT; ++i) o[qs][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float thr = 8.0f / a.c;
+  const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
+
+  uint32_t bad = 0;
+  if (b0 < b1) {
+    load(b0);
+    store(b0 & 1);
+    bad = load_bad;
+  }
+  __syncthreads();
+  for (int b = b0; b < b1; ++b) {
+    if (b + 1 < b1) load(b + 1);
+    const char* sk = smem + (b & 1) * STAGE;
+    const char* sv = sk + KB * ROW;
+    const bool pre = b < nb_pre;
+    const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
+    if (active) {
+      f32x4 st[QS][4];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const int key = 32 * (kt >> 1) + score_key(kt & 1, c);
+        x8 kf[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) kf[s] = *(const x8*)(sk + key * ROW + (((4 * s + g) ^ kswz<HD>(key)) * 16));
+#pragma unroll
+        for (int qs = 0; qs < QS; ++qs) {
+          st[qs][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < NS; ++s) st[qs][kt] = Half<T>::mfma(kf[s], qf[qs][s], st[qs][kt]);
+        }
+      }
+      const bool ragged = kb + KB > n || bad != 0 || (!pre && kb + KB - 1 > lim_min);
+      bool apart = false;
+      if (ragged) {
+#pragma unroll
+        for (int qs = 0; qs < QS; ++qs) {
+          // key kb + 32 (kt / 2) + 8 g + 4 (kt % 2) + r is seen if below `end`
+          const int end = pre ? n : n < lim[qs] + 1 ? n : lim[qs] + 1;
+          const int dl = end - kb - 8 * g;
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt) {
+            const bool gone = (bad >> (2 * (kt >> 1) + (g >> 1))) & 1;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              st[qs][kt][r] = 32 * (kt >> 1) + 4 * (kt & 1) + r < dl ? (gone ? NAN : st[qs][kt][r]) : -INFINITY;
+          }
+        }
+        if (!pre) {
+          // infinities and NaN among values that not every vector sees
+          uint32_t odd = 0;
+          for (int i = lane; i < KB * HD / 8; i += 64) {
+            const uint4 x = *(const uint4*)(sv + i * 16);
+            const uint32_t ws[4] = {x.x, x.y, x.z, x.w};
+            constexpr uint32_t E = __is_same(T, f16) ? 0x7C00u : 0x7F80u;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) odd |= ((ws[q] & E) == E) | ((ws[q] >> 16 & E) == E);
+          }
+          apart = __any(odd != 0);
+        }
+      }
+      x8 pb[QS][2];
+#pragma unroll
+      for (int qs = 0; qs < QS; ++qs) {
+        float mb = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mb = fmaxf(mb, st[qs][kt][r]);
+        mb = max4(mb);
+        if (__any(mb > m[qs] + thr)) {
+          const float m_new = mb > m[qs] + thr ? mb : m[qs];
+          const float alpha = rescale(m[qs], m_new, a.c);
+          l4[qs] *= alpha;
+#pragma unroll
+          for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
+          m[qs] = m_new;
+        }
+        const float nmc = -ref_of(m[qs]) * a.c;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            pb[qs][kt >> 1][4 * (kt & 1) + r] =
+                (T)__builtin_amdgcn_exp2f(__builtin_fmaf(st[qs][kt][r], a.c, nmc));
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) l4[qs] = Half<T>::mfma(ones, pb[qs][kc], l4[qs]);
+      }
+      // tile i: dimensions 16 i .. +15; lane (g, c) gets dimension 16 i + c of keys 32 kc + 8 g .. +7
+      auto values = [&](int kc, int i) {
+        const int key = 32 * kc + 8 * g + (c >> 2);
+        const x4 lo = read_transposed<T>(sv + key * ROW + ((i ^ vswz<HD>(key)) * 32) + (c & 3) * 8);
+        const x4 hi = read_transposed<T>(sv + (key + 4) * ROW + ((i ^ vswz<HD>(key + 4)) * 32) + (c & 3) * 8);
+        return x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      };
+#pragma unroll
+      for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          const x8 x = values(kc, i);
+          if (!apart) {
+#pragma unroll
+            for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
+          } else {
+            // one token at a time, with zeros for the values it does not see
+            for (int t = t_first; t <= t_last; ++t) {
+              const int seen = w.len - n_tok + t + 1 - (kb + 32 * kc + 8 * g);
+              x8 y;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) y[j] = j < seen ? x[j] : (T)0.f;
+#pragma unroll
+              for (int qs = 0; qs < QS; ++qs) {
+                const f32x4 z = Half<T>::mfma(y, pb[qs][kc], o[qs][i]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[qs][i][r] = tok[qs] == t ? z[r] : o[qs][i][r];
+              }
+            }
+          }
+        }
+    }
+    if (b + 1 < b1) {
+      store((b + 1) & 1);
+      bad = load_bad;
+    }
+    __syncthreads();
+  }
+
+  if (!active) return;
+#pragma unroll
+  for (int qs = 0; qs < QS; ++qs) {
+    if (!valid[qs]) continue;
+    const float l = l4[qs][0];
+    const int t = w.tok.x + tok[qs];
+    if (a.parts) {
+      float* dst = part_o(a, part, t, hq[qs]);
+#pragma unroll
+      for (int i = 0; i < NT; ++i) *(f32x4*)(dst + 16 * i + 4 * g) = o[qs][i];
+      if (g == 0) *part_ml(a, part, t, hq[qs]) = float2{m[qs], l};
+      continue;
+    }
+    const float inv = 1.0f / l;
+    T* dst = (T*)p.out + t * p.ldo + hq[qs] * HD;
+    typedef T xo __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      xo y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = (T)(l == 0.f ? 0.f : o[qs][i][r] * inv);
+      *(xo*)(dst + 16 * i + 4 * g) = y;
+    }
+    if (p.lse && g == 0) p.lse[(size_t)t * a.n.nq + hq[qs]] = lse_of(a, m[qs], l);
+  }
+}
+
+// ---------------------------------------------------------------- joining the parts
+// A group of hd / 4 lanes a (token, head): out = sum_i f_i o_i / sum_i f_i l_i with
+// f_i = 2^(c (m_i - max m)), parts in order.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void combine_kernel(const Args a) {
+  constexpr int LANES = HD / 4;
+  const lmop_attend_args& p = a.t;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+  const int d = threadIdx.x % LANES * 4;
+  if (i >= (int64_t)p.batch.n_tokens * a.n.nq) return;
+  const int t = (int)(i / a.n.nq), h = (int)(i % a.n.nq);
+  if (p.batch.start && (t < p.batch.start[0] || t >= p.batch.start[p.batch.n_seqs])) return;
+  float m = -INFINITY;
+  for (int q = 0; q < a.parts; ++q) m = fmaxf(m, part_ml(a, q, t, h)->x);
+  f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int q = 0; q < a.parts; ++q) {
+    const float2 ml = *part_ml(a, q, t, h);
+    if (ml.y != ml.y) {
+      l = ml.y;
+      continue;
+    }
+    // (a part that saw nothing may not have written its outputs)
+    if (ml.y == 0.f) continue;
+    const float f = rescale(ml.x, m, a.c);
+    l += ml.y * f;
+    const f32x4 x = *(const f32x4*)(part_o(a, q, t, h) + d);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] += x[r] * f;
+  }
+  const float inv = 1.0f / l;
+  typedef T xo __attribute__((ext_vector_type(4), aligned(2)));
+  xo r;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) r[k] = (T)(l == 0.f ? 0.f : y[k] * inv);
+  *(xo*)((T*)p.out + t * p.ldo + h * HD + d) = r;
+  if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + h] = lse_of(a, m, l);
+}
+
+template <typename T, bool E8, int HD>
+hipError_t launch_one(hipStream_t s, const Args& a) {
+  const dim3 grid(a.n.nkv * a.l.tiles, a.l.splits);
+  if (a.l.few) {
+    if (a.t.blocks)
+      hipLaunchKernelGGL((few_kernel<T, E8, HD, true>), grid, dim3(64 * kFewWaves), 0, s, a);
+    else
+      hipLaunchKernelGGL((few_kernel<T, E8, HD, false>), grid, dim3(64 * kFewWaves), 0, s, a);
+  } else {
+    constexpr int lds = 2 * 2 * KB * HD * 2;
+    hipLaunchKernelGGL((tile_kernel<T, E8, HD>), grid, dim3(64 * kTileWaves), lds, s, a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, bool E8, int HD>
+hipError_t launch(hipStream_t s, const lmop_attend_args& t, const Heads& n, const AttendPlan& plan) {
+  Args a{};
+  a.t = t;
+  a.n = n;
+  a.c = (t.scale == 0.f ? 1.0f / sqrtf((float)HD) : t.scale) * 1.4426950408889634f;
+  a.parts = plan.parts;
+  a.l = plan.own;
+  a.fused = plan.prefix.tiles == 0 && t.prefix_length > 0;
+  hipError_t e = launch_one<T, E8, HD>(s, a);
+  if (e != hipSuccess) return e;
+  if (plan.prefix.tiles > 0) {
+    Args q = a;
+    q.l = plan.prefix;
+    q.flat = 1;
+    q.fused = 0;
+    q.part0 = plan.own.splits;
+    e = launch_one<T, E8, HD>(s, q);
+    if (e != hipSuccess) return e;
+  }
+  if (plan.parts == 0) return hipSuccess;
+  const int64_t groups = (int64_t)t.batch.n_tokens * n.nq, per = 256 / (HD / 4);
+  hipLaunchKernelGGL((combine_kernel<T, HD>), dim3((unsigned)((groups + per - 1) / per)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_t(hipStream_t s, const lmop_attend_args& t, const Heads& n, const AttendPlan& plan) {
+  const bool e8 = t.cache.dtype == LMOP_E4M3;
+  if (n.hd == 128) return e8 ? launch<T, true, 128>(s, t, n, plan) : launch<T, false, 128>(s, t, n, plan);
+  if (n.hd == 64) return e8 ? launch<T, true, 64>(s, t, n, plan) : launch<T, false, 64>(s, t, n, plan);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_attend(hipStream_t s, const lmop_attend_args& a, const Heads& n, const AttendPlan& plan) {
+  return a.dtype == LMOP_F16 ? launch_t<f16>(s, a, n, plan) : launch_t<bf16>(s, a, n, plan);
+}
+
+}  // namespace lmop

@@ -33,9 +33,10 @@ EXPORTED = (
     "lmop_set_prefix", "lmop_set_prefixes", "lmop_release_prefix", "lmop_prefix_length", "lmop_eval_rows",
     "lmop_dedup_rows", "lmop_set_profiling", "lmop_get_kernel_stats", "lmop_set_workspace",
     "lmop_get_memory", "lmop_eval_rows_noalloc", "lmop_plan_rows", "lmop_quantize", "lmop_matmul",
-    "lmop_qk_norm_rope", "lmop_load_qk_norms",
+    "lmop_qk_norm_rope", "lmop_load_qk_norms", "lmop_cache_append", "lmop_attend",
+    "lmop_attend_workspace", "lmop_select_blocks",
 )
-LMOP_F16, LMOP_BF16, LMOP_F32 = 0, 1, 2
+LMOP_F16, LMOP_BF16, LMOP_F32, LMOP_E4M3 = 0, 1, 2, 3
 LMOP_FP8_GROUP = 128
 LMOP_V_ROWS, LMOP_V_COLUMNS = 0, 1
 # size of the static device array lmop_eval_rows_noalloc carves its scratch from
@@ -129,6 +130,40 @@ class lmop_qk_norm_rope_args(C.Structure):
                 ("n_slots", C.c_int32), ("v_layout", C.c_int32), ("dtype", C.c_int32)]
 
 
+class lmop_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("k_mean", C.c_void_p), ("page_stride", C.c_int64), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("dtype", C.c_int32)]
+
+
+class lmop_batch(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("length", C.c_void_p), ("start", C.c_void_p),
+                ("ld_table", C.c_int64), ("max_pages", C.c_int32), ("n_seqs", C.c_int32),
+                ("n_tokens", C.c_int32)]
+
+
+class lmop_append_args(C.Structure):
+    _fields_ = [("cache", lmop_cache), ("batch", lmop_batch), ("q", C.c_void_p), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("q_out", C.c_void_p), ("ldq", C.c_int64), ("ldk", C.c_int64),
+                ("ldv", C.c_int64), ("ldqo", C.c_int64), ("first", C.c_int32), ("rotate", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+class lmop_attend_args(C.Structure):
+    _fields_ = [("cache", lmop_cache), ("batch", lmop_batch), ("q", C.c_void_p), ("out", C.c_void_p),
+                ("lse", C.c_void_p), ("prefix", C.c_void_p), ("blocks", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("ldq", C.c_int64),
+                ("ldo", C.c_int64), ("prefix_length", C.c_int32), ("n_blocks", C.c_int32),
+                ("max_tokens", C.c_int32), ("max_length", C.c_int32), ("scale", C.c_float),
+                ("dtype", C.c_int32)]
+
+
+class lmop_select_args(C.Structure):
+    _fields_ = [("cache", lmop_cache), ("batch", lmop_batch), ("q", C.c_void_p),
+                ("blocks", C.c_void_p), ("ldq", C.c_int64), ("n_blocks", C.c_int32),
+                ("max_length", C.c_int32), ("dtype", C.c_int32)]
+
+
 RESULT_DTYPE = np.dtype([("value", "<i8"), ("logprob", "<f4"), ("logprob_full", "<f4"),
                          ("n_tokens", "<i4"), ("tokens", "<i4", (8,)), ("_pad", "<i4")])
 assert C.sizeof(lmop_result) == RESULT_DTYPE.itemsize
@@ -175,6 +210,10 @@ def _load():
         "lmop_quantize": (st, [vp, vp]),
         "lmop_matmul": (st, [vp, vp]),
         "lmop_qk_norm_rope": (st, [vp, vp]),
+        "lmop_cache_append": (st, [vp, vp]),
+        "lmop_attend": (st, [vp, vp]),
+        "lmop_attend_workspace": (st, [vp, vp, C.POINTER(C.c_uint64)]),
+        "lmop_select_blocks": (st, [vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -476,10 +515,17 @@ def lmop_get_kernel_stats(ctx):
 _DTYPES = {torch.float16: LMOP_F16, torch.bfloat16: LMOP_BF16, torch.float32: LMOP_F32}
 _CODES = {torch.float8_e4m3fn: 0, torch.uint8: 0}
 _F32 = {torch.float32: LMOP_F32}
+_I32 = {torch.int32: 0}
+_TOKENS = {torch.float16, torch.bfloat16}
+_PAGES = {torch.float16: LMOP_F16, torch.bfloat16: LMOP_BF16, torch.float8_e4m3fn: LMOP_E4M3}
 _PACK = {}
 for _name, _fmt, _struct in (("quantize", "4P4q3i4x", lmop_quantize_args),
                              ("matmul", "6P6q5i4x", lmop_matmul_args),
-                             ("qk_norm_rope", "10P6q4i", lmop_qk_norm_rope_args)):
+                             ("qk_norm_rope", "10P6q4i", lmop_qk_norm_rope_args),
+                             ("cache", "5Pq3i4x", lmop_cache), ("batch", "3Pq3i4x", lmop_batch),
+                             ("append", "64s48s4P4q3i4x", lmop_append_args),
+                             ("attend", "64s48s6PQ2q4ifi", lmop_attend_args),
+                             ("select", "64s48s2Pq3i4x", lmop_select_args)):
     assert struct.calcsize(_fmt) == C.sizeof(_struct)
     _PACK[_name] = struct.Struct(_fmt).pack
 
@@ -609,6 +655,142 @@ def lmop_qk_norm_rope(ctx, heads, n_tokens, q=None, k=None, v=None, pos=None, q_
         _vec(k_gain, "k_gain", hd, torch.float32, dev), _vec(pos, "pos", n_tokens, torch.int32, dev),
         _vec(slot, "slot", n_tokens, torch.int32, dev), pqo, pko, pvo, ldq, ldk, ldv, ldqo, ldko,
         ldvo, n_tokens, n_slots, LMOP_V_COLUMNS if v_columns else LMOP_V_ROWS, _DTYPES[dt]))
+    if st:
+        _check(st, ctx)
+
+
+class PagedCache:
+    """Keys and values in pages, on the caller's tensors: k and v [n_pages, n_kv_heads, page_size,
+    head_dim] (float16, bfloat16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages, n_kv_heads,
+    page_size]); pages may lie apart, what is in one may not.  k_mean, for select_blocks:
+    [n_pages, n_kv_heads, head_dim] of the tokens' dtype.  Its tensors have to keep their
+    memory."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None, k_mean=None):
+        if k.dim() != 4 or k.dtype not in _PAGES:
+            raise ValueError(f"k: {k.dtype} of shape {tuple(k.shape)}, expected [n_pages, n_kv_heads, page_size, "
+                             "head_dim] of float16, bfloat16 or float8_e4m3fn")
+        pages, heads, size, dim = k.shape
+        dev = k.get_device()
+        stride = k.stride(0) if pages > 1 else heads * size * dim
+        for t, what in ((k, "k"), (v, "v")):
+            if t.get_device() != dev or t.dtype != k.dtype or t.shape != k.shape:
+                raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)} on {t.device}, unlike k")
+            if pages > 0 and not t[0].is_contiguous() or pages > 1 and t.stride(0) != stride:
+                raise ValueError(f"{what}: a page is not contiguous, or its pages lie otherwise than k's")
+        e8 = k.dtype is torch.float8_e4m3fn
+        for t, what in ((k_exp, "k_exp"), (v_exp, "v_exp")):
+            if (t is not None) != e8:
+                raise ValueError(f"{what} is for float8_e4m3fn pages, which need it")
+            if e8 and (t.get_device() != dev or t.dtype != torch.uint8 or t.shape != (pages, heads, size) or
+                       not t.is_contiguous()):
+                raise ValueError(f"{what}: expected contiguous uint8 {(pages, heads, size)} on device {dev}")
+        if k_mean is not None and (k_mean.get_device() != dev or k_mean.shape != (pages, heads, dim) or
+                                   k_mean.dtype not in (torch.float16, torch.bfloat16) or
+                                   not e8 and k_mean.dtype != k.dtype or not k_mean.is_contiguous()):
+            raise ValueError(f"k_mean: expected contiguous {(pages, heads, dim)} of the tokens' dtype on device {dev}")
+        self.k, self.v, self.k_exp, self.v_exp, self.k_mean = k, v, k_exp, v_exp, k_mean
+        self.page_size, self.heads, self.device = size, (heads, dim), dev
+        self.token_dtype = (k_mean.dtype if k_mean is not None else None) if e8 else k.dtype
+        self.packed = _PACK["cache"](k.data_ptr(), v.data_ptr(), *(0 if t is None else t.data_ptr()
+                                                                  for t in (k_exp, v_exp, k_mean)),
+                                     stride, pages, size, _PAGES[k.dtype])
+
+
+def _batch(ctx_heads, cache, table, length, start, n_tokens, dtype, dev):
+    """A packed lmop_batch."""
+    if cache.device != dev or cache.heads != ctx_heads[1:]:
+        raise ValueError(f"a cache of {cache.heads} (kv heads, head_dim) on device {cache.device}, the ctx has "
+                         f"{ctx_heads[1:]} on {dev}")
+    if cache.token_dtype is not None and dtype is not cache.token_dtype:
+        raise ValueError(f"tokens of {dtype}, the cache is for {cache.token_dtype}")
+    n_seqs, pages = table.shape
+    ld = _ld(table, "table", n_seqs, pages, _I32, dev)
+    if start is None and n_tokens != n_seqs:
+        raise ValueError(f"{n_tokens} tokens of {n_seqs} sequences need start")
+    return _PACK["batch"](table.data_ptr(), _vec(length, "length", n_seqs, torch.int32, dev),
+                          _vec(start, "start", n_seqs + 1, torch.int32, dev), ld, pages, n_seqs, n_tokens)
+
+
+def lmop_cache_append(ctx, heads, cache, k, v, table, length, start=None, first: int = 0, rotate: bool = True,
+                      q=None, q_out=None) -> None:
+    """Rotates and appends keys and values to the sequences' pages; rotates queries into q_out."""
+    nq, nkv, hd = heads
+    n, dt, dev = k.shape[0], k.dtype, k.get_device()
+    if dt not in _TOKENS:
+        raise ValueError(f"dtype {dt}: float16 or bfloat16")
+    own = (dt,)
+    pq = pqo = ldq = ldqo = 0
+    if q is not None:
+        ldq, ldqo = _ld(q, "q", n, nq * hd, own, dev), _ld(q_out, "q_out", n, nq * hd, own, dev)
+        pq, pqo = q.data_ptr(), q_out.data_ptr()
+    st = _lib.lmop_cache_append(ctx, _PACK["append"](
+        cache.packed, _batch(heads, cache, table, length, start, n, dt, dev), pq, k.data_ptr(), v.data_ptr(), pqo,
+        ldq, _ld(k, "k", n, nkv * hd, own, dev), _ld(v, "v", n, nkv * hd, own, dev), ldqo, first, rotate,
+        _DTYPES[dt]))
+    if st:
+        _check(st, ctx)
+
+
+def lmop_attend(ctx, heads, cache, q, out, table, length, start=None, max_tokens: int = 1, max_length: int = 0,
+                prefix=None, prefix_length: int = 0, blocks=None, scale: float = 0.0, lse=None) -> None:
+    """Attention of the tokens over their sequences' keys and a prefix; its workspace comes from torch."""
+    nq, nkv, hd = heads
+    n, dt, dev = q.shape[0], q.dtype, q.get_device()
+    if dt not in _TOKENS:
+        raise ValueError(f"dtype {dt}: float16 or bfloat16")
+    own = (dt,)
+    n_blocks = pb = 0
+    if blocks is not None:
+        n_blocks = blocks.shape[-1]
+        if (blocks.get_device() != dev or blocks.dtype != torch.int32 or blocks.shape != (n, nkv, n_blocks) or
+                not blocks.is_contiguous()):
+            raise ValueError(f"blocks: expected contiguous int32 [{n}, {nkv}, n_blocks] on device {dev}")
+        pb = blocks.data_ptr()
+    pl = 0
+    if lse is not None:
+        if _ld(lse, "lse", n, nq, _F32, dev) != nq:
+            raise ValueError("lse: rows are not adjacent")
+        pl = lse.data_ptr()
+    pp = 0
+    if prefix_length > 0:
+        if prefix is None or prefix.dim() != 1 or prefix.shape[0] * cache.page_size < prefix_length:
+            raise ValueError(f"a prefix of {prefix_length} keys needs its pages")
+        pp = _vec(prefix, "prefix", prefix.shape[0], torch.int32, dev)
+    batch = _batch(heads, cache, table, length, start, n, dt, dev)
+    ldq, ldo = _ld(q, "q", n, nq * hd, own, dev), _ld(out, "out", n, nq * hd, own, dev)
+    pack = _PACK["attend"]
+
+    def args(ws, size):
+        return pack(cache.packed, batch, q.data_ptr(), out.data_ptr(), pl, pp, pb, ws, size, ldq, ldo, prefix_length,
+                    n_blocks, max_tokens, max_length, scale, _DTYPES[dt])
+
+    a = args(0, 0)
+    size = C.c_uint64()
+    st = _lib.lmop_attend_workspace(ctx, a, size)
+    if st:
+        _check(st, ctx)
+    if size.value:
+        ws = torch.empty(size.value, dtype=torch.uint8, device=q.device)
+        a = args(ws.data_ptr(), size.value)
+    st = _lib.lmop_attend(ctx, a)
+    if st:
+        _check(st, ctx)
+
+
+def lmop_select_blocks(ctx, heads, cache, q, blocks, table, length, start=None, max_length: int = 0) -> None:
+    """The blocks for each token and kv head, by the pages' mean keys."""
+    nq, nkv, hd = heads
+    n, dt, dev = q.shape[0], q.dtype, q.get_device()
+    if cache.k_mean is None:
+        raise ValueError("the cache has no k_mean")
+    n_blocks = blocks.shape[-1]
+    if (blocks.get_device() != dev or blocks.dtype != torch.int32 or blocks.shape != (n, nkv, n_blocks) or
+            not blocks.is_contiguous()):
+        raise ValueError(f"blocks: expected contiguous int32 [{n}, {nkv}, n_blocks] on device {dev}")
+    st = _lib.lmop_select_blocks(ctx, _PACK["select"](
+        cache.packed, _batch(heads, cache, table, length, start, n, dt, dev), q.data_ptr(), blocks.data_ptr(),
+        _ld(q, "q", n, nq * hd, (dt,), dev), n_blocks, max_length, _DTYPES[dt]))
     if st:
         _check(st, ctx)
 
@@ -758,3 +940,45 @@ class Context:
         lmop_qk_norm_rope(self.ctx, self.heads, pos.shape[0], q, k, v, pos, q_gain, k_gain, slot,
                           q_out, k_out, v_out, v_columns)
         return q_out
+
+    def cache_append(self, cache, k, v, *, table, length, start=None, first=0, rotate=True, q=None, q_out=None):
+        """Appends tokens to the pages of a PagedCache: keys rotated by their positions (first + their
+        index in the sequence), values as they are, the mean key of each page filled.  table
+        [n_seqs, pages], length [n_seqs] (with the call's tokens) and start [n_seqs + 1]
+        (None: a token each) are int32 on the device.  Returns the rotated queries
+        (q_out, or a new tensor; None without q)."""
+        self._here(k)
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lmop_cache_append(self.ctx, self.heads, cache, k, v, table, length, start, first, rotate, q, q_out)
+        return q_out
+
+    def attend(self, cache, q, *, table, length, start=None, max_tokens=None, max_length=None, prefix=None,
+               prefix_length=0, blocks=None, scale=0.0, out=None, lse=None):
+        """Attention of tokens [n, n_heads * head_dim] over their sequences' keys in a PagedCache, up to
+        each token's own, and over a prefix that all share (int32 page numbers, and its length in
+        keys); with blocks (of select_blocks) over the listed blocks only.  max_tokens and
+        max_length: at least the most tokens and keys of a sequence; what they are closer to, the
+        better the call is divided (default: all of them, the table's room).  lse: float32
+        [n, n_heads] to write the logarithm of the sum of exponentials into."""
+        self._here(q)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if max_tokens is None:
+            max_tokens = 1 if start is None else q.shape[0]
+        if max_length is None:
+            max_length = table.shape[1] * cache.page_size
+        lmop_attend(self.ctx, self.heads, cache, q, out, table, length, start, max_tokens, max_length, prefix,
+                    prefix_length, blocks, scale, lse)
+        return out
+
+    def select_blocks(self, cache, q, n_blocks, *, table, length, start=None, max_length=None, out=None):
+        """int32 [n, n_kv_heads, n_blocks]: the blocks (pages) that each token attends to, its own and
+        those before it whose mean key scores highest, ascending, then -1."""
+        self._here(q)
+        if out is None:
+            out = torch.empty((q.shape[0], self.heads[1], n_blocks), dtype=torch.int32, device=q.device)
+        if max_length is None:
+            max_length = table.shape[1] * cache.page_size
+        lmop_select_blocks(self.ctx, self.heads, cache, q, out, table, length, start, max_length)
+        return out
