@@ -27,6 +27,7 @@
 
 #include "attend_plan.h"
 #include "kernels.h"
+#include "lds_dma.h"
 #include "paged.h"
 
 namespace lmop {
@@ -37,12 +38,16 @@ namespace {
 // lane group g has scores of keys 8g + 4 hf + r, r = 0..3: 8g .. 8g+7 in order
 LMOP_DEVICE int score_key(int hf, int m) { return 8 * (m >> 2) + 4 * hf + (m & 3); }
 
+// (of fmaxf the compiler makes an instruction more for every operand, against signalling NaN)
+LMOP_DEVICE float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+LMOP_DEVICE float max3(float a, float b, float c) { return max2(max2(a, b), c); }
+
 // over the lanes 16 and 32 apart: the four lanes of a query vector
 LMOP_DEVICE float max4(float x) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  x = max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
   r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 struct Args {
@@ -123,6 +128,33 @@ LMOP_DEVICE void write_bad(const Args& a, int t, int h, int part, int lane, int 
 LMOP_DEVICE float lse_of(const Args& a, float m, float l) {
   // l > 0 means that some score was finite
   return l == 0.f ? -INFINITY : (m * a.c + __log2f(l)) * 0.6931471805599453f;
+}
+
+// A value that one vector of a workgroup sees and another does not must not reach the second one, but
+// 0 * inf and 0 * NaN in its column would.  So where vectors see different keys, infinities and
+// NaN among the values become zeros in the product, and are added to the vectors that see
+// them: the weight, being positive, does not matter.
+template <typename T>
+LMOP_DEVICE bool unbounded(uint32_t w) {  // either of two values
+  constexpr uint32_t E = __is_same(T, f16) ? 0x7C00u : 0x7F80u;
+  return (w & E) == E || (w >> 16 & E) == E;
+}
+
+// four values of the cache, as the product would read them
+template <typename T, bool E8>
+LMOP_DEVICE f32x4 value4(const lmop_cache& k, const Heads& n, int page, int h, int slot, int d) {
+  const size_t row = (size_t)h * k.page_size + slot, at = page * k.page_stride + row * n.hd + d;
+  f32x4 r;
+  if constexpr (E8) {
+    const uint32_t w = *(const uint32_t*)((const uint8_t*)k.v + at);
+    const float s = exp_scale(k.v_exp[(size_t)page * n.nkv * k.page_size + row]);
+    const auto x = Half<T>::template decode<false>(w, s), y = Half<T>::template decode<true>(w, s);
+    r = f32x4{(float)x[0], (float)x[1], (float)y[0], (float)y[1]};
+  } else {
+    const typename Half<T>::x4 x = *(const typename Half<T>::x4*)((const T*)k.v + at);
+    r = f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+  }
+  return r;
 }
 
 // ---------------------------------------------------------------- few vectors
@@ -226,6 +258,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   const int hq = h * G + (valid ? v - tok * G : 0);
   const int lim = a.flat ? 0 : w.len - n_tok + tok;
   const bool one = t_first == t_last || a.flat;  // all vectors see the same keys
+  const int lim_any = a.flat ? 0 : lim_max;
   x8 qf[NS];
   {
     const T* q = (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + hq * HD;
@@ -332,7 +365,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
     const int room = e_cap[ev] - slot_v, first = e_first[ev] + slot_v;
     const int seen = room < lim - first + 1 ? room : lim - first + 1;
     const bool whole = __all(seen >= 8 && page_v >= 0);
-    bool apart = false;
+    uint32_t odd = 0;  // the lane's value rows that hold infinities or NaN which not every vector sees
     if (!whole) {
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
@@ -340,25 +373,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
         for (int r = 0; r < 4; ++r)
           st[hf][r] = 4 * hf + r < seen ? (page_v < 0 ? NAN : st[hf][r]) : -INFINITY;
       // what no vector sees may hold anything: zeros instead
-      const int any = room < (a.flat ? 0 : lim_max) - first + 1 ? room : (a.flat ? 0 : lim_max) - first + 1;
-      uint32_t odd = 0;  // infinities and NaN (exponent bits all ones)
+      const int any = room < lim_any - first + 1 ? room : lim_any - first + 1;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int i = 0; i < NT / 2; ++i) {
           if (j >= any || page_v < 0) vw[j][i] = 0;
-          constexpr uint32_t E = __is_same(T, f16) ? 0x7C00u : 0x7F80u;
-          odd |= ((vw[j][i] & E) == E) | ((vw[j][i] >> 16 & E) == E);
+          if (!one && unbounded<T>(vw[j][i])) odd |= 1u << j, vw[j][i] = 0;
         }
-      apart = !one && __any(odd != 0);
     }
 
-    float mb = -INFINITY;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mb = fmaxf(mb, st[hf][r]);
-    mb = max4(mb);
+    float mb = max3(st[0][0], st[0][1], st[0][2]);
+    mb = max3(mb, st[0][3], st[1][0]);
+    mb = max3(mb, st[1][1], st[1][2]);
+    mb = max4(max2(mb, st[1][3]));
     if (__any(mb > m + thr)) {
       const float m_new = mb > m + thr ? mb : m;
       const float alpha = rescale(m, m_new, a.c);
@@ -384,24 +412,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
       for (int q = 0; q < 4; ++q) x[q] = __builtin_amdgcn_perm(vw[2 * q + 1][i >> 1], vw[2 * q][i >> 1], sel);
       return __builtin_bit_cast(x8, uint4{x[0], x[1], x[2], x[3]});
     };
-    if (!apart) {
 #pragma unroll
-      for (int i = 0; i < NT; ++i) o[i] = Half<T>::mfma(values(i), pb, o[i]);
-    } else {
-      // values that some vectors may not see are infinite or NaN: one token at a time, with zeros
-      // for what it does not see
-      for (int t = t_first; t <= t_last; ++t) {
-        const int lim_t = w.len - n_tok + t;
-        const int seen_t = room < lim_t - first + 1 ? room : lim_t - first + 1;
+    for (int i = 0; i < NT; ++i) o[i] = Half<T>::mfma(values(i), pb, o[i]);
+    if (__any(odd != 0)) {
+      for (int j = 0; j < 32; ++j) {
+        // key j of the chunk, its rows held by the lanes of group j / 8
+        if (!((__ballot((odd >> (j & 7)) & 1) >> (16 * (j >> 3))) & 0xFFFF)) continue;
+        const int at = kb + j, e = at >> lps;
+        if (e_first[e] + (at & (ps - 1)) > lim) continue;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          x8 x = values(i);
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = j < seen_t ? x[j] : (T)0.f;
-          const f32x4 y = Half<T>::mfma(x, pb, o[i]);
+          for (int i = 0; i < NT; i += 4) {
+            const f32x4 x = value4<T, E8>(p.cache, a.n, e_page[e], h, at & (ps - 1), NT * (4 * g + r) + i);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[i][r] = tok == t ? y[r] : o[i][r];
-        }
+            for (int q = 0; q < 4; ++q)
+              if (!(fabsf(x[q]) < INFINITY)) o[i + q][r] += x[q];
+          }
       }
     }
   }
@@ -487,20 +514,25 @@ LMOP_DEVICE typename Half<T>::x4 read_transposed(const char* lds) {
   return __builtin_bit_cast(typename Half<T>::x4, r);
 }
 
-// One workgroup: 128 vectors x a kv head x a split, 32 vectors a wave.  Blocks of 64 keys go through
-// registers (page lookup, codes to 16 bits) into one of two LDS stages while the
-// block before them is worked on.
+// One workgroup: 128 vectors x a kv head x a split, 32 vectors a wave.  Blocks of 64 keys
+// come into one of two LDS stages while the block before them is worked on: 16-bit pages by
+// direct loads (a row's chunks permuted on the way), 8-bit ones through registers,
+// where they become 16 bits.
 template <typename T, bool E8, int HD>
 __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) {
   typedef typename Half<T>::x8 x8;
   typedef typename Half<T>::x4 x4;
+  typedef typename Half<T>::x2 x2;
   constexpr int NS = HD / 32, NT = HD / 16, QS = 2;
-  constexpr int ROW = HD * 2;                    // bytes of an LDS row
-  constexpr int STAGE = 2 * KB * ROW;            // K, then V
-  constexpr int LANES = E8 ? HD / 16 : HD / 8;   // 16-byte loads of a key row
-  constexpr int ROWS = 64 * kTileWaves / LANES;  // key rows of a pass
-  constexpr int LOADS = KB / ROWS;
+  constexpr int ROW = HD * 2;                             // bytes of an LDS row
+  constexpr int STAGE = 2 * KB * ROW;                     // K, then V
+  constexpr int RPL = 1024 / ROW;                         // rows of a wave's direct load
+  constexpr int DMA = KB / RPL / kTileWaves;              // direct loads of a wave, of K or V
+  constexpr int LANES = HD / 16;                          // 16-byte loads of an 8-bit row
+  constexpr int ROWS = 64 * kTileWaves / LANES;           // 8-bit rows of a pass
+  constexpr int LOADS = E8 ? KB / ROWS : 1;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ uint32_t s_odd[2][2];  // by block parity: keys with infinities or NaN among their values
 
   const lmop_attend_args& p = a.t;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -533,80 +565,100 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
   const int b0 = b_from < nb ? (int)b_from : nb;
   const int b1 = nb - b0 < a.l.chunk ? nb : b0 + a.l.chunk;
 
-  // the block that the staging registers hold
-  uint4 kr[LOADS], vr[LOADS];
-  uint32_t kx[LOADS], vx[LOADS];
-  const int lrow = tid / LANES, lch = tid % LANES;
-  uint32_t load_bad = 0;  // 16-key groups whose page does not exist
-  auto page_at = [&](int b, int grp) {  // of 16 keys, wave-uniform; -1: missing, 0: past the end
-    const bool pre = b < nb_pre;
-    const int key = (pre ? b : b - nb_pre) * KB + 16 * grp;
-    if (key >= (pre ? n_pre : n_own)) return 0;
-    if (!pre) return __builtin_amdgcn_readfirstlane(page_of(p.batch, p.cache.n_pages, w.seq, key >> lps));
-    const int q = __builtin_amdgcn_readfirstlane(p.prefix[key >> lps]);
-    return q >= 0 && q < p.cache.n_pages ? q : -1;
+  // ---- loads.  The pages of a block's four groups of 16 keys are looked up a block ahead.
+  struct Pages {
+    int page[4];
+    uint32_t bad;  // groups whose page does not exist
   };
-  auto load = [&](int b) {
+  const int32_t* own_table = p.batch.table + (int64_t)w.seq * p.batch.ld_table;
+  auto look_up = [&](int b) {
+    Pages r;
+    r.bad = 0;
     const bool pre = b < nb_pre;
     const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
-    load_bad = 0;
+    const int32_t* table = pre ? p.prefix : own_table;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_bad |= page_at(b, i) < 0 ? 1u << i : 0u;
+    for (int i = 0; i < 4; ++i) {
+      const int key = kb + 16 * i;
+      int q = 0;
+      if (b < b1 && key < n) {
+        q = __builtin_amdgcn_readfirstlane(table[key >> lps]);
+        if (q < 0 || q >= p.cache.n_pages) q = 0, r.bad |= 1u << i;
+      }
+      r.page[i] = q;
+    }
+    return r;
+  };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + (uint32_t)wave * 1024u;
+  // this lane's share of a direct load i: row `lrow` of a group, its chunk permuted
+  const int lrow = ((wave * RPL) & 15) + lane / (HD / 8);
+  uint32_t koff[DMA];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int r = lrow + i * ROWS;
-      int pg = page_at(b, __builtin_amdgcn_readfirstlane(r >> 4));
-      pg = pg < 0 ? 0 : pg;
-      const size_t row = (size_t)h * ps + ((kb + r) & (ps - 1));
-      const size_t at = (pg * p.cache.page_stride + row * HD) * (E8 ? 1 : 2) + lch * 16;
-      kr[i] = *(const uint4*)((const char*)p.cache.k + at);
-      vr[i] = *(const uint4*)((const char*)p.cache.v + at);
-      if (kb + r >= n) vr[i] = uint4{0, 0, 0, 0};
-      if constexpr (E8) {
-        kx[i] = p.cache.k_exp[(size_t)pg * a.n.nkv * ps + row];
-        vx[i] = p.cache.v_exp[(size_t)pg * a.n.nkv * ps + row];
+  for (int i = 0; i < DMA; ++i) {
+    const int r = (wave + kTileWaves * i) * RPL + lane / (HD / 8);
+    koff[i] = (uint32_t)((h * ps + lrow) * HD + ((lane % (HD / 8)) ^ kswz<HD>(r)) * 8) * 2u;
+  }
+  const int vch = lane % (HD / 8);
+  const uint32_t voff = (uint32_t)((h * ps + lrow) * HD + ((((vch >> 1) ^ vswz<HD>(lrow)) << 1) | (vch & 1)) * 8) * 2u;
+  uint4 kr[LOADS], vr[LOADS];
+  uint32_t kx[LOADS], vx[LOADS];
+  auto load = [&](int b, const Pages& pg, int st) {
+    const int kb = (b < nb_pre ? b : b - nb_pre) * KB;
+    if constexpr (!E8) {
+#pragma unroll
+      for (int i = 0; i < DMA; ++i) {
+        const int grp = DMA == 4 ? i : 2 * i + (wave >> 1);
+        const int page = DMA == 4 ? pg.page[i] : (wave >> 1) ? pg.page[2 * i + 1] : pg.page[2 * i];
+        const int64_t at = (page * p.cache.page_stride + ((kb + 16 * grp) & (ps - 1)) * HD) * 2;
+        const uint32_t dst = lds0 + (uint32_t)(st * STAGE + kTileWaves * 1024 * i);
+        g2l16_m0((const char*)p.cache.k + at, koff[i], dst);
+        g2l16_m0((const char*)p.cache.v + at, voff, dst + KB * ROW);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = tid / LANES + i * ROWS;
+        const int grp = __builtin_amdgcn_readfirstlane(r >> 4);
+        const int page = grp == 0 ? pg.page[0] : grp == 1 ? pg.page[1] : grp == 2 ? pg.page[2] : pg.page[3];
+        const size_t row = (size_t)h * ps + ((kb + r) & (ps - 1));
+        const size_t at = page * p.cache.page_stride + row * HD + tid % LANES * 16;
+        kr[i] = *(const uint4*)((const char*)p.cache.k + at);
+        vr[i] = *(const uint4*)((const char*)p.cache.v + at);
+        kx[i] = p.cache.k_exp[(size_t)page * a.n.nkv * ps + row];
+        vx[i] = p.cache.v_exp[(size_t)page * a.n.nkv * ps + row];
       }
     }
   };
+  // 16-byte chunk ch of a value row
+  auto vchunk = [&](int r, int ch) { return r * ROW + (((ch >> 1) ^ vswz<HD>(r)) * 32) + (ch & 1) * 16; };
   auto store = [&](int st) {
     char* sk = smem + st * STAGE;
     char* sv = sk + KB * ROW;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int r = lrow + i * ROWS;
-      // chunk ch of a row: keys by 16-byte chunks, values by 32-byte units
-      auto put = [&](int ch, const uint4& k, const uint4& v) {
-        *(uint4*)(sk + r * ROW + ((ch ^ kswz<HD>(r)) * 16)) = k;
-        *(uint4*)(sv + r * ROW + (((ch >> 1) ^ vswz<HD>(r)) * 32) + (ch & 1) * 16) = v;
-      };
-      if constexpr (!E8) {
-        put(lch, kr[i], vr[i]);
-      } else {
-        const float ks = exp_scale(kx[i]), vs = exp_scale(vx[i]);
-        put(2 * lch, __builtin_bit_cast(uint4, decode8<T>(kr[i].x, kr[i].y, ks)),
-            __builtin_bit_cast(uint4, decode8<T>(vr[i].x, vr[i].y, vs)));
-        put(2 * lch + 1, __builtin_bit_cast(uint4, decode8<T>(kr[i].z, kr[i].w, ks)),
-            __builtin_bit_cast(uint4, decode8<T>(vr[i].z, vr[i].w, vs)));
-      }
+      const int r = tid / LANES + i * ROWS, ch = tid % LANES * 2;
+      const float ks = exp_scale(kx[i]), vs = exp_scale(vx[i]);
+      *(x8*)(sk + r * ROW + ((ch ^ kswz<HD>(r)) * 16)) = decode8<T>(kr[i].x, kr[i].y, ks);
+      *(x8*)(sk + r * ROW + (((ch + 1) ^ kswz<HD>(r)) * 16)) = decode8<T>(kr[i].z, kr[i].w, ks);
+      *(x8*)(sv + vchunk(r, ch)) = decode8<T>(vr[i].x, vr[i].y, vs);
+      *(x8*)(sv + vchunk(r, ch + 1)) = decode8<T>(vr[i].z, vr[i].w, vs);
     }
   };
 
   // this lane's vectors: 32 of the wave, column c of two
   x8 qf[QS][NS];
-  int lim[QS], tok[QS], hq[QS];
-  bool valid[QS];
+  int lim[QS];
 #pragma unroll
   for (int qs = 0; qs < QS; ++qs) {
     const int v = w.v0 + wave * 16 * QS + 16 * qs + c;
-    valid[qs] = v < nv;
-    tok[qs] = valid[qs] ? v / G : t_last;
-    hq[qs] = h * G + (valid[qs] ? v - tok[qs] * G : 0);
-    lim[qs] = a.flat ? -1 : w.len - n_tok + tok[qs];
-    const T* q = (const T*)p.q + (int64_t)(w.tok.x + tok[qs]) * p.ldq + hq[qs] * HD;
+    const bool valid = v < nv;
+    const int tok = valid ? v / G : t_last;
+    lim[qs] = a.flat ? -1 : w.len - n_tok + tok;
+    const T* q = (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + (valid ? v - tok * G : 0)) * HD;
     typedef T xu __attribute__((ext_vector_type(8), aligned(2)));
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      const xu x = valid[qs] ? *(const xu*)(q + 32 * s + 8 * g) : xu{};
+      const xu x = valid ? *(const xu*)(q + 32 * s + 8 * g) : xu{};
 #pragma unroll
       for (int i = 0; i < 8; ++i) qf[qs][s][i] = x[i];
     }
@@ -626,19 +678,57 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
   const float thr = 8.0f / a.c;
   const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
 
+  if (tid < 4) s_odd[tid >> 1][tid & 1] = 0;
   uint32_t bad = 0;
+  Pages next{};
   if (b0 < b1) {
-    load(b0);
-    store(b0 & 1);
-    bad = load_bad;
+    const Pages pg = look_up(b0);
+    load(b0, pg, b0 & 1);
+    bad = pg.bad;
+    next = look_up(b0 + 1);
+    if constexpr (E8) store(b0 & 1);
   }
-  __syncthreads();
   for (int b = b0; b < b1; ++b) {
-    if (b + 1 < b1) load(b + 1);
-    const char* sk = smem + (b & 1) * STAGE;
-    const char* sv = sk + KB * ROW;
+    // the block is in LDS for every wave, and every wave is done with the one before it, whose
+    // stage the next one takes
+    if constexpr (!E8) wait_vmcnt<0>();
+    __syncthreads();
+    const uint32_t next_bad = next.bad;
+    if (b + 1 < b1) {
+      load(b + 1, next, (b + 1) & 1);
+      next = look_up(b + 2);
+    }
+    char* sk = smem + (b & 1) * STAGE;
+    char* sv = sk + KB * ROW;
     const bool pre = b < nb_pre;
     const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
+    const bool mixed = !pre && kb + KB - 1 > lim_min;  // not every vector sees every key
+    uint64_t odd = 0;
+    if (mixed || kb + KB > n) {
+      // values that no vector sees may be anything, and unbounded ones are left out of the product
+      if (tid < 2) s_odd[(b + 1) & 1][tid] = 0;
+#pragma unroll
+      for (int i = 0; i < KB * HD / 8 / (64 * kTileWaves); ++i) {
+        const int at = tid + i * 64 * kTileWaves, r = at / (HD / 8);
+        uint4* x = (uint4*)(sv + vchunk(r, at % (HD / 8)));
+        if (kb + r >= n) {
+          *x = uint4{0, 0, 0, 0};
+        } else if (mixed) {
+          uint4 y = *x;
+          bool any = false;
+          uint32_t* ys = (uint32_t*)&y;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (unbounded<T>(ys[q])) ys[q] = 0, any = true;
+          if (any) {
+            *x = y;
+            atomicOr(&s_odd[b & 1][r >> 5], 1u << (r & 31));
+          }
+        }
+      }
+      __syncthreads();
+      odd = s_odd[b & 1][0] | (uint64_t)s_odd[b & 1][1] << 32;
+    }
     if (active) {
       f32x4 st[QS][4];
 #pragma unroll
@@ -654,9 +744,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
           for (int s = 0; s < NS; ++s) st[qs][kt] = Half<T>::mfma(kf[s], qf[qs][s], st[qs][kt]);
         }
       }
-      const bool ragged = kb + KB > n || bad != 0 || (!pre && kb + KB - 1 > lim_min);
-      bool apart = false;
-      if (ragged) {
+      if (mixed || kb + KB > n || bad != 0) {
 #pragma unroll
         for (int qs = 0; qs < QS; ++qs) {
           // key kb + 32 (kt / 2) + 8 g + 4 (kt % 2) + r is seen if below `end`
@@ -670,28 +758,18 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
               st[qs][kt][r] = 32 * (kt >> 1) + 4 * (kt & 1) + r < dl ? (gone ? NAN : st[qs][kt][r]) : -INFINITY;
           }
         }
-        if (!pre) {
-          // infinities and NaN among values that not every vector sees
-          uint32_t odd = 0;
-          for (int i = lane; i < KB * HD / 8; i += 64) {
-            const uint4 x = *(const uint4*)(sv + i * 16);
-            const uint32_t ws[4] = {x.x, x.y, x.z, x.w};
-            constexpr uint32_t E = __is_same(T, f16) ? 0x7C00u : 0x7F80u;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) odd |= ((ws[q] & E) == E) | ((ws[q] >> 16 & E) == E);
-          }
-          apart = __any(odd != 0);
-        }
       }
       x8 pb[QS][2];
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) {
-        float mb = -INFINITY;
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) mb = fmaxf(mb, st[qs][kt][r]);
-        mb = max4(mb);
+        float mb = max3(st[qs][0][0], st[qs][0][1], st[qs][0][2]);
+        mb = max3(mb, st[qs][0][3], st[qs][1][0]);
+        mb = max3(mb, st[qs][1][1], st[qs][1][2]);
+        mb = max3(mb, st[qs][1][3], st[qs][2][0]);
+        mb = max3(mb, st[qs][2][1], st[qs][2][2]);
+        mb = max3(mb, st[qs][2][3], st[qs][3][0]);
+        mb = max3(mb, st[qs][3][1], st[qs][3][2]);
+        mb = max4(max2(mb, st[qs][3][3]));
         if (__any(mb > m[qs] + thr)) {
           const float m_new = mb > m[qs] + thr ? mb : m[qs];
           const float alpha = rescale(m[qs], m_new, a.c);
@@ -704,66 +782,67 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            pb[qs][kt >> 1][4 * (kt & 1) + r] =
-                (T)__builtin_amdgcn_exp2f(__builtin_fmaf(st[qs][kt][r], a.c, nmc));
+          for (int r = 0; r < 4; r += 2) {
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(st[qs][kt][r], a.c, nmc)),
+                             __builtin_amdgcn_exp2f(__builtin_fmaf(st[qs][kt][r + 1], a.c, nmc))};
+            const x2 y = __builtin_convertvector(e, x2);
+            pb[qs][kt >> 1][4 * (kt & 1) + r] = y[0];
+            pb[qs][kt >> 1][4 * (kt & 1) + r + 1] = y[1];
+          }
 #pragma unroll
         for (int kc = 0; kc < 2; ++kc) l4[qs] = Half<T>::mfma(ones, pb[qs][kc], l4[qs]);
       }
       // tile i: dimensions 16 i .. +15; lane (g, c) gets dimension 16 i + c of keys 32 kc + 8 g .. +7
-      auto values = [&](int kc, int i) {
-        const int key = 32 * kc + 8 * g + (c >> 2);
-        const x4 lo = read_transposed<T>(sv + key * ROW + ((i ^ vswz<HD>(key)) * 32) + (c & 3) * 8);
-        const x4 hi = read_transposed<T>(sv + (key + 4) * ROW + ((i ^ vswz<HD>(key + 4)) * 32) + (c & 3) * 8);
-        return x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      };
 #pragma unroll
       for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          const x8 x = values(kc, i);
-          if (!apart) {
+          const int key = 32 * kc + 8 * g + (c >> 2);
+          const x4 lo = read_transposed<T>(sv + key * ROW + ((i ^ vswz<HD>(key)) * 32) + (c & 3) * 8);
+          const x4 hi = read_transposed<T>(sv + (key + 4) * ROW + ((i ^ vswz<HD>(key + 4)) * 32) + (c & 3) * 8);
+          const x8 x = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 #pragma unroll
-            for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
-          } else {
-            // one token at a time, with zeros for the values it does not see
-            for (int t = t_first; t <= t_last; ++t) {
-              const int seen = w.len - n_tok + t + 1 - (kb + 32 * kc + 8 * g);
-              x8 y;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = j < seen ? x[j] : (T)0.f;
-#pragma unroll
-              for (int qs = 0; qs < QS; ++qs) {
-                const f32x4 z = Half<T>::mfma(y, pb[qs][kc], o[qs][i]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[qs][i][r] = tok[qs] == t ? z[r] : o[qs][i][r];
-              }
-            }
-          }
+          for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
         }
+      while (odd) {
+        const int key = kb + __builtin_ctzll(odd);
+        odd &= odd - 1;
+        const int page = own_table[key >> lps];
+        if (page < 0 || page >= p.cache.n_pages) continue;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          const f32x4 x = value4<T, E8>(p.cache, a.n, page, h, key & (ps - 1), 16 * i + 4 * g);
+#pragma unroll
+          for (int qs = 0; qs < QS; ++qs)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (key <= lim[qs] && !(fabsf(x[r]) < INFINITY)) o[qs][i][r] += x[r];
+        }
+      }
     }
-    if (b + 1 < b1) {
-      store((b + 1) & 1);
-      bad = load_bad;
+    bad = next_bad;
+    if constexpr (E8) {
+      if (b + 1 < b1) store((b + 1) & 1);
     }
-    __syncthreads();
   }
 
   if (!active) return;
 #pragma unroll
   for (int qs = 0; qs < QS; ++qs) {
-    if (!valid[qs]) continue;
+    const int v = w.v0 + wave * 16 * QS + 16 * qs + c;
+    if (v >= nv) continue;
     const float l = l4[qs][0];
-    const int t = w.tok.x + tok[qs];
+    const int t = w.tok.x + v / G, hq = h * G + v % G;
     if (a.parts) {
-      float* dst = part_o(a, part, t, hq[qs]);
+      float* dst = part_o(a, part, t, hq);
 #pragma unroll
       for (int i = 0; i < NT; ++i) *(f32x4*)(dst + 16 * i + 4 * g) = o[qs][i];
-      if (g == 0) *part_ml(a, part, t, hq[qs]) = float2{m[qs], l};
+      if (g == 0) *part_ml(a, part, t, hq) = float2{m[qs], l};
       continue;
     }
     const float inv = 1.0f / l;
-    T* dst = (T*)p.out + t * p.ldo + hq[qs] * HD;
+    T* dst = (T*)p.out + t * p.ldo + hq * HD;
     typedef T xo __attribute__((ext_vector_type(4), aligned(2)));
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -772,7 +851,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
       for (int r = 0; r < 4; ++r) y[r] = (T)(l == 0.f ? 0.f : o[qs][i][r] * inv);
       *(xo*)(dst + 16 * i + 4 * g) = y;
     }
-    if (p.lse && g == 0) p.lse[(size_t)t * a.n.nq + hq[qs]] = lse_of(a, m[qs], l);
+    if (p.lse && g == 0) p.lse[(size_t)t * a.n.nq + hq] = lse_of(a, m[qs], l);
   }
 }
 
