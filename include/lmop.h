@@ -578,7 +578,7 @@ lmop_status lmop_cache_append(lmop_ctx* ctx, const lmop_append_args* args);
  * n sees its sequence's keys up to its own, index length - n + j; with
  * `blocks`, of those only the ones in the blocks listed for it and the kv
  * head (block b is keys b * page_size and on; an entry outside the table, -1 for
- * instance, stands for none; one listed twice counts twice).  A key that
+ * instance, stands for none; one listed twice counts once).  A key that
  * a token does not see has no effect on its result, whatever it or its value holds.  A token
  * that sees no key, or only scores of minus infinity, gets zeros and lse = -inf.
  * Scores, sums and outputs are held in fp32; the weights are rounded to dtype for the

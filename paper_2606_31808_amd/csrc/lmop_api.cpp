@@ -1726,7 +1726,8 @@ lmop_status check_attend_sizes(lmop_ctx* c, const lmop_attend_args& a, bool* emp
     return fail(c, LMOP_ERR_UNSUPPORTED, "a prefix of %d keys", a.prefix_length);
   if (a.n_blocks > 0 && a.prefix_length > 0)
     return fail(c, LMOP_ERR_INVALID_ARG, "blocks and a prefix of %d keys", a.prefix_length);
-  if (a.n_blocks > (1 << 16)) return fail(c, LMOP_ERR_UNSUPPORTED, "%d blocks", a.n_blocks);
+  if (a.n_blocks > kMaxSelected)
+    return fail(c, LMOP_ERR_UNSUPPORTED, "%d blocks (at most %d)", a.n_blocks, kMaxSelected);
   const AttendSizes s = attend_sizes(c, a);
   if (((uint64_t)s.n_tokens + s.n_seqs) * s.nq > kMaxTasks / 64)
     return fail(c, LMOP_ERR_UNSUPPORTED, "%d tokens of %d sequences are too many for one call", s.n_tokens, s.n_seqs);

@@ -228,6 +228,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   const int64_t from = (int64_t)split * a.l.chunk;
   const int64_t left = (int64_t)n_pre + n_own - from;
   const int ne = (int)(left < 0 ? 0 : left < a.l.chunk ? left : a.l.chunk);
+  bool ascending = true;
+  if constexpr (BLOCKS) {
+    const int32_t* list = p.blocks + ((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks;
+    for (int i = tid + 1; i < p.n_blocks; i += 64 * kFewWaves) ascending = ascending && (list[i] < 0 || (list[i - 1] >= 0 && list[i] > list[i - 1]));
+    ascending = !__syncthreads_or(!ascending);
+  }
   for (int i = tid; i < kMaxEntries + 16; i += 64 * kFewWaves) {
     int page = 0, first = 0, cap = 0;
     if (i < ne) {
@@ -239,7 +245,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
         cap = p.prefix_length - (e << lps) < ps ? p.prefix_length - (e << lps) : ps;
       } else {
         int b = e - n_pre;
-        if constexpr (BLOCKS) b = p.blocks[((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks + b];
+        if constexpr (BLOCKS) {
+          // one listed twice counts once; lists of select_blocks ascend, which rules that out at a glance
+          const int32_t* list = p.blocks + ((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks;
+          const int at = b;
+          b = list[at];
+          bool twice = false;
+          for (int j = ascending ? at : 0; j < at; ++j) twice = twice || list[j] == b;
+          if (twice) b = -1;
+        }
         // (a block past what the token sees is left out here, so its page does not matter)
         if (b >= 0 && b < p.batch.max_pages && b <= (lim_max >> lps)) {
           page = page_of(p.batch, p.cache.n_pages, w.seq, b);
@@ -489,6 +503,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
 // ---------------------------------------------------------------- tiles
 constexpr int kTileWaves = 4;
 constexpr int KB = kTileKeys;
+constexpr int kWindow = kTileWindow;
 
 // 16-byte chunk c of LDS row `key` lies at chunk c ^ kswz: score fragments (score_key's rows, one
 // chunk column) then meet every bank
@@ -514,49 +529,298 @@ LMOP_DEVICE typename Half<T>::x4 read_transposed(const char* lds) {
   return __builtin_bit_cast(typename Half<T>::x4, r);
 }
 
-// One workgroup: 128 vectors x a kv head x a split, 32 vectors a wave.  Blocks of 64 keys
-// come into one of two LDS stages while the block before them is worked on: 16-bit pages by
-// direct loads (a row's chunks permuted on the way), 8-bit ones through registers,
-// where they become 16 bits.
+// A block's four groups of 16 keys, which lie in one page each
+struct Groups {
+  int page[4], slot[4];  // 0 for a page that does not exist, or keys past the end
+  uint32_t bad;          // groups whose page does not exist
+};
+
+// What both tile kernels share.  A workgroup: 128 vectors x a kv head, 32 vectors a wave.  Blocks of 64
+// keys come into one of two LDS stages while the block before them is worked on:
+// 16-bit pages by direct loads (a row's chunks permuted on the way), 8-bit ones through
+// registers, where they become 16 bits.
 template <typename T, bool E8, int HD>
-__global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) {
+struct TileCore {
   typedef typename Half<T>::x8 x8;
   typedef typename Half<T>::x4 x4;
   typedef typename Half<T>::x2 x2;
-  constexpr int NS = HD / 32, NT = HD / 16, QS = 2;
-  constexpr int ROW = HD * 2;                             // bytes of an LDS row
-  constexpr int STAGE = 2 * KB * ROW;                     // K, then V
-  constexpr int RPL = 1024 / ROW;                         // rows of a wave's direct load
-  constexpr int DMA = KB / RPL / kTileWaves;              // direct loads of a wave, of K or V
-  constexpr int LANES = HD / 16;                          // 16-byte loads of an 8-bit row
-  constexpr int ROWS = 64 * kTileWaves / LANES;           // 8-bit rows of a pass
-  constexpr int LOADS = E8 ? KB / ROWS : 1;
+  static constexpr int NS = HD / 32, NT = HD / 16, QS = 2;
+  static constexpr int ROW = HD * 2;                    // bytes of an LDS row
+  static constexpr int STAGE = 2 * KB * ROW;            // K, then V
+  static constexpr int RPL = 1024 / ROW;                // rows of a wave's direct load
+  static constexpr int DMA = KB / RPL / kTileWaves;     // direct loads of a wave, of K or V
+  static constexpr int LANES = HD / 16;                 // 16-byte loads of an 8-bit row
+  static constexpr int ROWS = 64 * kTileWaves / LANES;  // 8-bit rows of a pass
+  static constexpr int LOADS = E8 ? KB / ROWS : 1;
+  static_assert(E8 || DMA == 4 || DMA == 2, "which group a direct load belongs to");
+
+  const lmop_cache& cache;
+  const Heads& n;
+  char* smem;
+  int tid, lane, wave, g, c, h, ps;
+  uint32_t lds0, koff[DMA], voff;
+  uint4 kr[LOADS], vr[LOADS];
+  uint32_t kx[LOADS], vx[LOADS];
+  x8 qf[QS][NS];
+  f32x4 o[QS][NT], l4[QS];
+  float m[QS];
+
+  LMOP_DEVICE TileCore(const Args& a, char* smem_, int h_) : cache(a.t.cache), n(a.n), smem(smem_), h(h_) {
+    tid = threadIdx.x, lane = tid & 63;
+    wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    g = lane >> 4, c = lane & 15;
+    ps = cache.page_size;
+    lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + (uint32_t)wave * 1024u;
+    // this lane's share of a direct load: row `lrow` of a group, its chunk permuted
+    const int lrow = ((wave * RPL) & 15) + lane / (HD / 8), ch = lane % (HD / 8);
+#pragma unroll
+    for (int i = 0; i < DMA; ++i) {
+      const int r = (wave + kTileWaves * i) * RPL + lane / (HD / 8);
+      koff[i] = (uint32_t)((h * ps + lrow) * HD + (ch ^ kswz<HD>(r)) * 8) * 2u;
+    }
+    voff = (uint32_t)((h * ps + lrow) * HD + ((((ch >> 1) ^ vswz<HD>(lrow)) << 1) | (ch & 1)) * 8) * 2u;
+    clear();
+  }
+
+  LMOP_DEVICE void clear() {
+#pragma unroll
+    for (int qs = 0; qs < QS; ++qs) {
+      m[qs] = -INFINITY;
+      l4[qs] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[qs][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // q: the vector's first element, NULL past the end
+  LMOP_DEVICE void load_query(int qs, const T* q) {
+    typedef T xu __attribute__((ext_vector_type(8), aligned(2)));
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const xu x = q ? *(const xu*)(q + 32 * s + 8 * g) : xu{};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qf[qs][s][i] = x[i];
+    }
+  }
+
+  // A block on its way: 16-bit pages to the stage, 8-bit ones to registers (store() follows)
+  LMOP_DEVICE void load(const Groups& b, int st) {
+    if constexpr (!E8) {
+#pragma unroll
+      for (int i = 0; i < DMA; ++i) {
+        const int page = DMA == 4 ? b.page[i] : (wave >> 1) ? b.page[2 * i + 1] : b.page[2 * i];
+        const int slot = DMA == 4 ? b.slot[i] : (wave >> 1) ? b.slot[2 * i + 1] : b.slot[2 * i];
+        const int64_t at = (page * cache.page_stride + slot * HD) * 2;
+        const uint32_t dst = lds0 + (uint32_t)(st * STAGE + kTileWaves * 1024 * i);
+        g2l16_m0((const char*)cache.k + at, koff[i], dst);
+        g2l16_m0((const char*)cache.v + at, voff, dst + KB * ROW);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = tid / LANES + i * ROWS;
+        const int grp = __builtin_amdgcn_readfirstlane(r >> 4);
+        const int page = grp == 0 ? b.page[0] : grp == 1 ? b.page[1] : grp == 2 ? b.page[2] : b.page[3];
+        const int slot = grp == 0 ? b.slot[0] : grp == 1 ? b.slot[1] : grp == 2 ? b.slot[2] : b.slot[3];
+        const size_t row = (size_t)h * ps + slot + (r & 15);
+        const size_t at = page * cache.page_stride + row * HD + tid % LANES * 16;
+        kr[i] = *(const uint4*)((const char*)cache.k + at);
+        vr[i] = *(const uint4*)((const char*)cache.v + at);
+        kx[i] = cache.k_exp[(size_t)page * n.nkv * ps + row];
+        vx[i] = cache.v_exp[(size_t)page * n.nkv * ps + row];
+      }
+    }
+  }
+  // 16-byte chunk ch of a value row
+  static LMOP_DEVICE int vchunk(int r, int ch) { return r * ROW + (((ch >> 1) ^ vswz<HD>(r)) * 32) + (ch & 1) * 16; }
+  LMOP_DEVICE void store(int st) {
+    char* sk = smem + st * STAGE;
+    char* sv = sk + KB * ROW;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = tid / LANES + i * ROWS, ch = tid % LANES * 2;
+      const float ks = exp_scale(kx[i]), vs = exp_scale(vx[i]);
+      *(x8*)(sk + r * ROW + ((ch ^ kswz<HD>(r)) * 16)) = decode8<T>(kr[i].x, kr[i].y, ks);
+      *(x8*)(sk + r * ROW + (((ch + 1) ^ kswz<HD>(r)) * 16)) = decode8<T>(kr[i].z, kr[i].w, ks);
+      *(x8*)(sv + vchunk(r, ch)) = decode8<T>(vr[i].x, vr[i].y, vs);
+      *(x8*)(sv + vchunk(r, ch + 1)) = decode8<T>(vr[i].z, vr[i].w, vs);
+    }
+  }
+
+  // Value rows that no vector sees (gone(row)) become zeros: they may hold anything.  With `bounded`
+  // infinities and NaN in the others do too, and their rows are marked in odd[2].
+  template <typename F>
+  LMOP_DEVICE void mend(int st, F&& gone, bool bounded, uint32_t* odd) {
+    char* sv = smem + st * STAGE + KB * ROW;
+#pragma unroll
+    for (int i = 0; i < KB * HD / 8 / (64 * kTileWaves); ++i) {
+      const int at = tid + i * 64 * kTileWaves, r = at / (HD / 8);
+      uint4* x = (uint4*)(sv + vchunk(r, at % (HD / 8)));
+      if (gone(r)) {
+        *x = uint4{0, 0, 0, 0};
+      } else if (bounded) {
+        uint4 y = *x;
+        bool any = false;
+        uint32_t* ys = (uint32_t*)&y;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (unbounded<T>(ys[q])) ys[q] = 0, any = true;
+        if (any) {
+          *x = y;
+          atomicOr(&odd[r >> 5], 1u << (r & 31));
+        }
+      }
+    }
+  }
+
+  // Scores of the vectors qs with live[qs].  st[qs][kt]: register r of lane group g is key
+  // 32 (kt / 2) + 8 g + 4 (kt % 2) + r
+  LMOP_DEVICE void scores(int stage, const bool* live, f32x4 (&st)[QS][4]) {
+    const char* sk = smem + stage * STAGE;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      const int key = 32 * (kt >> 1) + score_key(kt & 1, c);
+      x8 kf[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) kf[s] = *(const x8*)(sk + key * ROW + (((4 * s + g) ^ kswz<HD>(key)) * 16));
+#pragma unroll
+      for (int qs = 0; qs < QS; ++qs) {
+        if (!live[qs]) continue;
+        st[qs][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) st[qs][kt] = Half<T>::mfma(kf[s], qf[qs][s], st[qs][kt]);
+      }
+    }
+  }
+
+  // The vectors' weights of the block and their sums; the states move to a new reference where needed
+  LMOP_DEVICE void weights(int qs, const f32x4 (&st)[4], float cs, float thr, x8 (&pb)[2]) {
+    const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
+    float mb = max3(st[0][0], st[0][1], st[0][2]);
+    mb = max3(mb, st[0][3], st[1][0]);
+    mb = max3(mb, st[1][1], st[1][2]);
+    mb = max3(mb, st[1][3], st[2][0]);
+    mb = max3(mb, st[2][1], st[2][2]);
+    mb = max3(mb, st[2][3], st[3][0]);
+    mb = max3(mb, st[3][1], st[3][2]);
+    mb = max4(max2(mb, st[3][3]));
+    if (__any(mb > m[qs] + thr)) {
+      const float m_new = mb > m[qs] + thr ? mb : m[qs];
+      const float alpha = rescale(m[qs], m_new, cs);
+      l4[qs] *= alpha;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
+      m[qs] = m_new;
+    }
+    const float nmc = -ref_of(m[qs]) * cs;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][r], cs, nmc)),
+                         __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][r + 1], cs, nmc))};
+        const x2 y = __builtin_convertvector(e, x2);
+        pb[kt >> 1][4 * (kt & 1) + r] = y[0];
+        pb[kt >> 1][4 * (kt & 1) + r + 1] = y[1];
+      }
+#pragma unroll
+    for (int kc = 0; kc < 2; ++kc) l4[qs] = Half<T>::mfma(ones, pb[kc], l4[qs]);
+  }
+
+  // O^T += V^T P^T.  Tile i: dimensions 16 i .. +15; lane (g, c) gets dimension 16 i + c of keys
+  // 32 kc + 8 g .. +7
+  LMOP_DEVICE void product(int stage, const bool* live, const x8 (&pb)[QS][2]) {
+    const char* sv = smem + stage * STAGE + KB * ROW;
+#pragma unroll
+    for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const int key = 32 * kc + 8 * g + (c >> 2);
+        const x4 lo = read_transposed<T>(sv + key * ROW + ((i ^ vswz<HD>(key)) * 32) + (c & 3) * 8);
+        const x4 hi = read_transposed<T>(sv + (key + 4) * ROW + ((i ^ vswz<HD>(key + 4)) * 32) + (c & 3) * 8);
+        const x8 x = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+        for (int qs = 0; qs < QS; ++qs)
+          if (live[qs]) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
+      }
+  }
+
+  // The infinities and NaN of a value row that were left out, for the vectors that see it
+  LMOP_DEVICE void add_unbounded(int page, int slot, const bool* sees) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const f32x4 x = value4<T, E8>(cache, n, page, h, slot, 16 * i + 4 * g);
+#pragma unroll
+      for (int qs = 0; qs < QS; ++qs)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (sees[qs] && !(fabsf(x[r]) < INFINITY)) o[qs][i][r] += x[r];
+    }
+  }
+
+  // The wave's results: vector qs of lane column c is (token t, head hq)
+  LMOP_DEVICE void write(const Args& a, int qs, int t, int hq, int part) {
+    const float l = l4[qs][0];
+    if (a.parts) {
+      float* dst = part_o(a, part, t, hq);
+#pragma unroll
+      for (int i = 0; i < NT; ++i) *(f32x4*)(dst + 16 * i + 4 * g) = o[qs][i];
+      if (g == 0) *part_ml(a, part, t, hq) = float2{m[qs], l};
+      return;
+    }
+    const float inv = 1.0f / l;
+    T* dst = (T*)a.t.out + t * a.t.ldo + hq * HD;
+    typedef T xo __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      xo y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = (T)(l == 0.f ? 0.f : o[qs][i][r] * inv);
+      *(xo*)(dst + 16 * i + 4 * g) = y;
+    }
+    if (a.t.lse && g == 0) a.t.lse[(size_t)t * a.n.nq + hq] = lse_of(a, m[qs], l);
+  }
+};
+
+// What a tile's vectors see of their sequence
+struct Span {
+  int n_tok, nv, t_first, t_last;
+  LMOP_DEVICE Span(const Tile& w, int G) {
+    n_tok = w.tok.y - w.tok.x, nv = n_tok * G;
+    t_first = w.v0 / G;
+    t_last = (w.v0 + kTileVectors - 1) / G < n_tok ? (w.v0 + kTileVectors - 1) / G : n_tok - 1;
+  }
+};
+
+template <typename T>
+LMOP_DEVICE void write_bad_tile(const Args& a, const Tile& w, int nv, int h, int part) {
+  // its tiles cover all of its tokens, but where per_seq was reckoned from max_tokens
+  const int end = a.l.per_seq && w.v0 + kTileVectors >= a.l.per_seq * kTileVectors ? nv : w.v0 + kTileVectors;
+  const int G = a.n.nq / a.n.nkv;
+  for (int v = w.v0 + (threadIdx.x >> 6); v < end && v < nv; v += kTileWaves)
+    write_bad<T>(a, w.tok.x + v / G, h * G + v % G, part, threadIdx.x & 63, 64);
+}
+
+// A split of the keys: the prefix's, then the sequence's own up to the tile's last token
+template <typename T, bool E8, int HD>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) {
+  typedef TileCore<T, E8, HD> Core;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   __shared__ uint32_t s_odd[2][2];  // by block parity: keys with infinities or NaN among their values
 
   const lmop_attend_args& p = a.t;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
   const int h = blockIdx.x % a.n.nkv, split = blockIdx.y;
   const int G = a.n.nq / a.n.nkv;
   const int ps = p.cache.page_size, lps = __builtin_ctz(ps);
   const int part = a.part0 + split;
   // later tiles of a prompt see more keys: they go first
   const Tile w = find_tile(a, a.l.tiles - 1 - (int)blockIdx.x / a.n.nkv, kTileVectors);
-  const int n_tok = w.tok.y - w.tok.x, nv = n_tok * G;
-  if (w.v0 >= nv) return;
-  if (w.bad) {
-    // its tiles cover all of its tokens, but where per_seq was reckoned from max_tokens
-    const int end = a.l.per_seq && w.v0 + kTileVectors >= a.l.per_seq * kTileVectors ? nv : w.v0 + kTileVectors;
-    for (int v = w.v0 + wave; v < end && v < nv; v += kTileWaves)
-      write_bad<T>(a, w.tok.x + v / G, h * G + v % G, part, lane, 64);
-    return;
-  }
+  const Span sp(w, G);
+  if (w.v0 >= sp.nv) return;
+  if (w.bad) return write_bad_tile<T>(a, w, sp.nv, h, part);
 
-  const int t_first = w.v0 / G;
-  const int t_last = (w.v0 + kTileVectors - 1) / G < n_tok ? (w.v0 + kTileVectors - 1) / G : n_tok - 1;
-  const int lim_max = a.flat ? -1 : w.len - n_tok + t_last, lim_min = a.flat ? -1 : w.len - n_tok + t_first;
+  const int lim_max = a.flat ? -1 : w.len - sp.n_tok + sp.t_last, lim_min = a.flat ? -1 : w.len - sp.n_tok + sp.t_first;
   const int n_pre = a.flat || a.fused ? p.prefix_length : 0;
   const int n_own = lim_max + 1 > 0 ? lim_max + 1 : 0;
   const int nb_pre = (n_pre + KB - 1) / KB;
@@ -565,14 +829,10 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
   const int b0 = b_from < nb ? (int)b_from : nb;
   const int b1 = nb - b0 < a.l.chunk ? nb : b0 + a.l.chunk;
 
-  // ---- loads.  The pages of a block's four groups of 16 keys are looked up a block ahead.
-  struct Pages {
-    int page[4];
-    uint32_t bad;  // groups whose page does not exist
-  };
+  // pages are looked up a block before they are loaded
   const int32_t* own_table = p.batch.table + (int64_t)w.seq * p.batch.ld_table;
   auto look_up = [&](int b) {
-    Pages r;
+    Groups r;
     r.bad = 0;
     const bool pre = b < nb_pre;
     const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
@@ -586,107 +846,34 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
         if (q < 0 || q >= p.cache.n_pages) q = 0, r.bad |= 1u << i;
       }
       r.page[i] = q;
+      r.slot[i] = key & (ps - 1);
     }
     return r;
   };
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + (uint32_t)wave * 1024u;
-  // this lane's share of a direct load i: row `lrow` of a group, its chunk permuted
-  const int lrow = ((wave * RPL) & 15) + lane / (HD / 8);
-  uint32_t koff[DMA];
-#pragma unroll
-  for (int i = 0; i < DMA; ++i) {
-    const int r = (wave + kTileWaves * i) * RPL + lane / (HD / 8);
-    koff[i] = (uint32_t)((h * ps + lrow) * HD + ((lane % (HD / 8)) ^ kswz<HD>(r)) * 8) * 2u;
-  }
-  const int vch = lane % (HD / 8);
-  const uint32_t voff = (uint32_t)((h * ps + lrow) * HD + ((((vch >> 1) ^ vswz<HD>(lrow)) << 1) | (vch & 1)) * 8) * 2u;
-  uint4 kr[LOADS], vr[LOADS];
-  uint32_t kx[LOADS], vx[LOADS];
-  auto load = [&](int b, const Pages& pg, int st) {
-    const int kb = (b < nb_pre ? b : b - nb_pre) * KB;
-    if constexpr (!E8) {
-#pragma unroll
-      for (int i = 0; i < DMA; ++i) {
-        const int grp = DMA == 4 ? i : 2 * i + (wave >> 1);
-        const int page = DMA == 4 ? pg.page[i] : (wave >> 1) ? pg.page[2 * i + 1] : pg.page[2 * i];
-        const int64_t at = (page * p.cache.page_stride + ((kb + 16 * grp) & (ps - 1)) * HD) * 2;
-        const uint32_t dst = lds0 + (uint32_t)(st * STAGE + kTileWaves * 1024 * i);
-        g2l16_m0((const char*)p.cache.k + at, koff[i], dst);
-        g2l16_m0((const char*)p.cache.v + at, voff, dst + KB * ROW);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int r = tid / LANES + i * ROWS;
-        const int grp = __builtin_amdgcn_readfirstlane(r >> 4);
-        const int page = grp == 0 ? pg.page[0] : grp == 1 ? pg.page[1] : grp == 2 ? pg.page[2] : pg.page[3];
-        const size_t row = (size_t)h * ps + ((kb + r) & (ps - 1));
-        const size_t at = page * p.cache.page_stride + row * HD + tid % LANES * 16;
-        kr[i] = *(const uint4*)((const char*)p.cache.k + at);
-        vr[i] = *(const uint4*)((const char*)p.cache.v + at);
-        kx[i] = p.cache.k_exp[(size_t)page * a.n.nkv * ps + row];
-        vx[i] = p.cache.v_exp[(size_t)page * a.n.nkv * ps + row];
-      }
-    }
-  };
-  // 16-byte chunk ch of a value row
-  auto vchunk = [&](int r, int ch) { return r * ROW + (((ch >> 1) ^ vswz<HD>(r)) * 32) + (ch & 1) * 16; };
-  auto store = [&](int st) {
-    char* sk = smem + st * STAGE;
-    char* sv = sk + KB * ROW;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int r = tid / LANES + i * ROWS, ch = tid % LANES * 2;
-      const float ks = exp_scale(kx[i]), vs = exp_scale(vx[i]);
-      *(x8*)(sk + r * ROW + ((ch ^ kswz<HD>(r)) * 16)) = decode8<T>(kr[i].x, kr[i].y, ks);
-      *(x8*)(sk + r * ROW + (((ch + 1) ^ kswz<HD>(r)) * 16)) = decode8<T>(kr[i].z, kr[i].w, ks);
-      *(x8*)(sv + vchunk(r, ch)) = decode8<T>(vr[i].x, vr[i].y, vs);
-      *(x8*)(sv + vchunk(r, ch + 1)) = decode8<T>(vr[i].z, vr[i].w, vs);
-    }
-  };
 
-  // this lane's vectors: 32 of the wave, column c of two
-  x8 qf[QS][NS];
-  int lim[QS];
+  Core k(a, smem, h);
+  int lim[Core::QS];
 #pragma unroll
-  for (int qs = 0; qs < QS; ++qs) {
-    const int v = w.v0 + wave * 16 * QS + 16 * qs + c;
-    const bool valid = v < nv;
-    const int tok = valid ? v / G : t_last;
-    lim[qs] = a.flat ? -1 : w.len - n_tok + tok;
-    const T* q = (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + (valid ? v - tok * G : 0)) * HD;
-    typedef T xu __attribute__((ext_vector_type(8), aligned(2)));
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const xu x = valid ? *(const xu*)(q + 32 * s + 8 * g) : xu{};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) qf[qs][s][i] = x[i];
-    }
+  for (int qs = 0; qs < Core::QS; ++qs) {
+    const int v = w.v0 + k.wave * 16 * Core::QS + 16 * qs + k.c;
+    const int tok = v < sp.nv ? v / G : sp.t_last;
+    lim[qs] = a.flat ? -1 : w.len - sp.n_tok + tok;
+    k.load_query(qs, v < sp.nv ? (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + v - tok * G) * HD : nullptr);
   }
   // a wave whose vectors all lie past the end only helps to load
-  const bool active = w.v0 + wave * 16 * QS < nv;
-
-  f32x4 o[QS][NT], l4[QS];
-  float m[QS];
-#pragma unroll
-  for (int qs = 0; qs < QS; ++qs) {
-    m[qs] = -INFINITY;
-    l4[qs] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < NT; ++i) o[qs][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  const bool active = w.v0 + k.wave * 16 * Core::QS < sp.nv;
+  const bool both[2] = {true, true};
   const float thr = 8.0f / a.c;
-  const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
 
-  if (tid < 4) s_odd[tid >> 1][tid & 1] = 0;
+  if (k.tid < 4) s_odd[k.tid >> 1][k.tid & 1] = 0;
   uint32_t bad = 0;
-  Pages next{};
+  Groups next{};
   if (b0 < b1) {
-    const Pages pg = look_up(b0);
-    load(b0, pg, b0 & 1);
-    bad = pg.bad;
+    const Groups first = look_up(b0);
+    k.load(first, b0 & 1);
+    bad = first.bad;
     next = look_up(b0 + 1);
-    if constexpr (E8) store(b0 & 1);
+    if constexpr (E8) k.store(b0 & 1);
   }
   for (int b = b0; b < b1; ++b) {
     // the block is in LDS for every wave, and every wave is done with the one before it, whose
@@ -695,163 +882,251 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
     __syncthreads();
     const uint32_t next_bad = next.bad;
     if (b + 1 < b1) {
-      load(b + 1, next, (b + 1) & 1);
+      k.load(next, (b + 1) & 1);
       next = look_up(b + 2);
     }
-    char* sk = smem + (b & 1) * STAGE;
-    char* sv = sk + KB * ROW;
     const bool pre = b < nb_pre;
     const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
     const bool mixed = !pre && kb + KB - 1 > lim_min;  // not every vector sees every key
     uint64_t odd = 0;
     if (mixed || kb + KB > n) {
-      // values that no vector sees may be anything, and unbounded ones are left out of the product
-      if (tid < 2) s_odd[(b + 1) & 1][tid] = 0;
-#pragma unroll
-      for (int i = 0; i < KB * HD / 8 / (64 * kTileWaves); ++i) {
-        const int at = tid + i * 64 * kTileWaves, r = at / (HD / 8);
-        uint4* x = (uint4*)(sv + vchunk(r, at % (HD / 8)));
-        if (kb + r >= n) {
-          *x = uint4{0, 0, 0, 0};
-        } else if (mixed) {
-          uint4 y = *x;
-          bool any = false;
-          uint32_t* ys = (uint32_t*)&y;
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (unbounded<T>(ys[q])) ys[q] = 0, any = true;
-          if (any) {
-            *x = y;
-            atomicOr(&s_odd[b & 1][r >> 5], 1u << (r & 31));
-          }
-        }
-      }
+      if (k.tid < 2) s_odd[(b + 1) & 1][k.tid] = 0;
+      k.mend(b & 1, [&](int r) { return kb + r >= n; }, mixed, s_odd[b & 1]);
       __syncthreads();
       odd = s_odd[b & 1][0] | (uint64_t)s_odd[b & 1][1] << 32;
     }
     if (active) {
-      f32x4 st[QS][4];
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const int key = 32 * (kt >> 1) + score_key(kt & 1, c);
-        x8 kf[NS];
-#pragma unroll
-        for (int s = 0; s < NS; ++s) kf[s] = *(const x8*)(sk + key * ROW + (((4 * s + g) ^ kswz<HD>(key)) * 16));
-#pragma unroll
-        for (int qs = 0; qs < QS; ++qs) {
-          st[qs][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int s = 0; s < NS; ++s) st[qs][kt] = Half<T>::mfma(kf[s], qf[qs][s], st[qs][kt]);
-        }
-      }
+      f32x4 st[Core::QS][4];
+      k.scores(b & 1, both, st);
       if (mixed || kb + KB > n || bad != 0) {
 #pragma unroll
-        for (int qs = 0; qs < QS; ++qs) {
+        for (int qs = 0; qs < Core::QS; ++qs) {
           // key kb + 32 (kt / 2) + 8 g + 4 (kt % 2) + r is seen if below `end`
           const int end = pre ? n : n < lim[qs] + 1 ? n : lim[qs] + 1;
-          const int dl = end - kb - 8 * g;
+          const int dl = end - kb - 8 * k.g;
 #pragma unroll
           for (int kt = 0; kt < 4; ++kt) {
-            const bool gone = (bad >> (2 * (kt >> 1) + (g >> 1))) & 1;
+            const bool gone = (bad >> (2 * (kt >> 1) + (k.g >> 1))) & 1;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
               st[qs][kt][r] = 32 * (kt >> 1) + 4 * (kt & 1) + r < dl ? (gone ? NAN : st[qs][kt][r]) : -INFINITY;
           }
         }
       }
-      x8 pb[QS][2];
+      typename Core::x8 pb[Core::QS][2];
 #pragma unroll
-      for (int qs = 0; qs < QS; ++qs) {
-        float mb = max3(st[qs][0][0], st[qs][0][1], st[qs][0][2]);
-        mb = max3(mb, st[qs][0][3], st[qs][1][0]);
-        mb = max3(mb, st[qs][1][1], st[qs][1][2]);
-        mb = max3(mb, st[qs][1][3], st[qs][2][0]);
-        mb = max3(mb, st[qs][2][1], st[qs][2][2]);
-        mb = max3(mb, st[qs][2][3], st[qs][3][0]);
-        mb = max3(mb, st[qs][3][1], st[qs][3][2]);
-        mb = max4(max2(mb, st[qs][3][3]));
-        if (__any(mb > m[qs] + thr)) {
-          const float m_new = mb > m[qs] + thr ? mb : m[qs];
-          const float alpha = rescale(m[qs], m_new, a.c);
-          l4[qs] *= alpha;
-#pragma unroll
-          for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
-          m[qs] = m_new;
-        }
-        const float nmc = -ref_of(m[qs]) * a.c;
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; r += 2) {
-            typedef float f32x2 __attribute__((ext_vector_type(2)));
-            const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(st[qs][kt][r], a.c, nmc)),
-                             __builtin_amdgcn_exp2f(__builtin_fmaf(st[qs][kt][r + 1], a.c, nmc))};
-            const x2 y = __builtin_convertvector(e, x2);
-            pb[qs][kt >> 1][4 * (kt & 1) + r] = y[0];
-            pb[qs][kt >> 1][4 * (kt & 1) + r + 1] = y[1];
-          }
-#pragma unroll
-        for (int kc = 0; kc < 2; ++kc) l4[qs] = Half<T>::mfma(ones, pb[qs][kc], l4[qs]);
-      }
-      // tile i: dimensions 16 i .. +15; lane (g, c) gets dimension 16 i + c of keys 32 kc + 8 g .. +7
-#pragma unroll
-      for (int kc = 0; kc < 2; ++kc)
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const int key = 32 * kc + 8 * g + (c >> 2);
-          const x4 lo = read_transposed<T>(sv + key * ROW + ((i ^ vswz<HD>(key)) * 32) + (c & 3) * 8);
-          const x4 hi = read_transposed<T>(sv + (key + 4) * ROW + ((i ^ vswz<HD>(key + 4)) * 32) + (c & 3) * 8);
-          const x8 x = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-#pragma unroll
-          for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
-        }
+      for (int qs = 0; qs < Core::QS; ++qs) k.weights(qs, st[qs], a.c, thr, pb[qs]);
+      k.product(b & 1, both, pb);
       while (odd) {
         const int key = kb + __builtin_ctzll(odd);
         odd &= odd - 1;
         const int page = own_table[key >> lps];
-        if (page < 0 || page >= p.cache.n_pages) continue;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const f32x4 x = value4<T, E8>(p.cache, a.n, page, h, key & (ps - 1), 16 * i + 4 * g);
-#pragma unroll
-          for (int qs = 0; qs < QS; ++qs)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (key <= lim[qs] && !(fabsf(x[r]) < INFINITY)) o[qs][i][r] += x[r];
-        }
+        const bool sees[2] = {key <= lim[0], key <= lim[1]};
+        if (page >= 0 && page < p.cache.n_pages) k.add_unbounded(page, key & (ps - 1), sees);
       }
     }
     bad = next_bad;
     if constexpr (E8) {
-      if (b + 1 < b1) store((b + 1) & 1);
+      if (b + 1 < b1) k.store((b + 1) & 1);
     }
   }
 
   if (!active) return;
 #pragma unroll
-  for (int qs = 0; qs < QS; ++qs) {
-    const int v = w.v0 + wave * 16 * QS + 16 * qs + c;
-    if (v >= nv) continue;
-    const float l = l4[qs][0];
-    const int t = w.tok.x + v / G, hq = h * G + v % G;
-    if (a.parts) {
-      float* dst = part_o(a, part, t, hq);
+  for (int qs = 0; qs < Core::QS; ++qs) {
+    const int v = w.v0 + k.wave * 16 * Core::QS + 16 * qs + k.c;
+    if (v < sp.nv) k.write(a, qs, w.tok.x + v / G, h * G + v % G, part);
+  }
+}
+
+// Over chosen blocks: a tile walks the blocks that any of its tokens chose, in ascending order, a window
+// of kWindow at a time, and a wave works on those that one of its vectors sees.  Neighbours choose
+// many blocks in common, and workgroups that walk the same way find them in their L2.
+template <typename T, bool E8, int HD>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void tile_blocks_kernel(const Args a) {
+  typedef TileCore<T, E8, HD> Core;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ uint32_t s_odd[2][2];
+  __shared__ uint32_t s_mask[kWindow][kTileVectors / 32];  // the window's blocks: which of the tile's tokens chose it
+  __shared__ int s_id[kWindow], s_page[kWindow];           // the chosen ones
+  __shared__ int s_n;
+
+  const lmop_attend_args& p = a.t;
+  const int h = blockIdx.x % a.n.nkv, split = blockIdx.y;
+  const int G = a.n.nq / a.n.nkv;
+  const int ps = p.cache.page_size, lps = __builtin_ctz(ps);
+  const int part = a.part0 + split;
+  const Tile w = find_tile(a, (int)blockIdx.x / a.n.nkv, kTileVectors);
+  const Span sp(w, G);
+  if (w.v0 >= sp.nv) return;
+  if (w.bad) return write_bad_tile<T>(a, w, sp.nv, h, part);
+  const int lim0 = w.len - sp.n_tok, lim_max = lim0 + sp.t_last;
+  const int n_tile = sp.t_last - sp.t_first + 1;
+
+  Core k(a, smem, h);
+  int lim[Core::QS], word[Core::QS], bit[Core::QS];
 #pragma unroll
-      for (int i = 0; i < NT; ++i) *(f32x4*)(dst + 16 * i + 4 * g) = o[qs][i];
-      if (g == 0) *part_ml(a, part, t, hq) = float2{m[qs], l};
-      continue;
+  for (int qs = 0; qs < Core::QS; ++qs) {
+    const int v = w.v0 + k.wave * 16 * Core::QS + 16 * qs + k.c;
+    const int tok = v < sp.nv ? v / G : sp.t_last;
+    lim[qs] = v < sp.nv ? lim0 + tok : -1;
+    word[qs] = (tok - sp.t_first) >> 5, bit[qs] = (tok - sp.t_first) & 31;
+    k.load_query(qs, v < sp.nv ? (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + v - tok * G) * HD : nullptr);
+  }
+  const float thr = 8.0f / a.c;
+  const int32_t* lists = p.blocks + ((size_t)(w.tok.x + sp.t_first) * a.n.nkv + h) * p.n_blocks;
+  const int blocks = lim_max < 0 ? 0 : (lim_max >> lps) + 1;
+  const int64_t w_from = (int64_t)split * a.l.chunk * kWindow;
+  const int first_block = w_from < blocks ? (int)w_from : blocks;
+  const int last_block = blocks - first_block < a.l.chunk * (int64_t)kWindow ? blocks : first_block + a.l.chunk * kWindow;
+
+  // Infinities and NaN among the values reach vectors that do not see them (0 * inf).  They are rare, so the
+  // walk looks for them only when it has to go again: careful.
+  for (int careful = 0; careful < 2; ++careful) {
+    for (int wb = first_block; wb < last_block; wb += kWindow) {
+      const int wn = last_block - wb < kWindow ? last_block - wb : kWindow;
+      __syncthreads();
+      for (int i = k.tid; i < kWindow * (kTileVectors / 32); i += 64 * kTileWaves) (&s_mask[0][0])[i] = 0;
+      if (k.tid < 4) s_odd[k.tid >> 1][k.tid & 1] = 0;
+      __syncthreads();
+      for (int i = k.tid; i < n_tile * p.n_blocks; i += 64 * kTileWaves) {
+        const int t = i / p.n_blocks, b = lists[(size_t)t * a.n.nkv * p.n_blocks + (i - t * p.n_blocks)];
+        if (b >= wb && b - wb < wn && b <= ((lim0 + sp.t_first + t) >> lps)) atomicOr(&s_mask[b - wb][t >> 5], 1u << (t & 31));
+      }
+      __syncthreads();
+      if (k.tid < 64) {
+        int placed = 0;
+#pragma unroll
+        for (int i = 0; i < kWindow; i += 64) {
+          const int b = i + k.lane;
+          uint32_t any = 0;
+#pragma unroll
+          for (int q = 0; q < kTileVectors / 32; ++q) any |= s_mask[b][q];
+          const uint64_t set = __ballot(any != 0);
+          if (any) {
+            const int at = placed + __builtin_popcountll(set & ((1ull << k.lane) - 1));
+            s_id[at] = wb + b;
+            s_page[at] = page_of(p.batch, p.cache.n_pages, w.seq, wb + b);
+          }
+          placed += __builtin_popcountll(set);
+        }
+        if (k.lane == 0) s_n = placed;
+      }
+      __syncthreads();
+      const int n_keys = __builtin_amdgcn_readfirstlane(s_n) << lps;
+      const int nb = (n_keys + KB - 1) / KB;
+      auto look_up = [&](int b) {
+        Groups r;
+        r.bad = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = b * KB + 16 * i;
+          int q = 0;
+          if (key < n_keys) {
+            q = __builtin_amdgcn_readfirstlane(s_page[key >> lps]);
+            if (q < 0) q = 0, r.bad |= 1u << i;
+          }
+          r.page[i] = q;
+          r.slot[i] = key & (ps - 1);
+        }
+        return r;
+      };
+      uint32_t bad = 0;
+      Groups next{};
+      if (nb > 0) {
+        const Groups first = look_up(0);
+        k.load(first, 0);
+        bad = first.bad;
+        next = look_up(1);
+        if constexpr (E8) k.store(0);
+      }
+      for (int b = 0; b < nb; ++b) {
+        if constexpr (!E8) wait_vmcnt<0>();
+        __syncthreads();
+        const uint32_t next_bad = next.bad;
+        if (b + 1 < nb) {
+          k.load(next, (b + 1) & 1);
+          next = look_up(b + 2);
+        }
+        // index of the key in row r of the block
+        const int e_last = ((b + 1) * KB < n_keys ? (b + 1) * KB : n_keys) - 1;
+        auto index = [&](int r) {
+          const int key = b * KB + r;
+          return key < n_keys ? (s_id[key >> lps] << lps) + (key & (ps - 1)) : 0x7FFFFFFF;
+        };
+        // (ids ascend, so the block's last key has the largest index)
+        uint64_t odd = 0;
+        if (careful || bad != 0 || (b + 1) * KB > n_keys || index(e_last - b * KB) > lim_max) {
+          if (k.tid < 2) s_odd[(b + 1) & 1][k.tid] = 0;
+          k.mend(b & 1, [&](int r) { return index(r) > lim_max || ((bad >> (r >> 4)) & 1); }, careful != 0, s_odd[b & 1]);
+          __syncthreads();
+          odd = s_odd[b & 1][0] | (uint64_t)s_odd[b & 1][1] << 32;
+        }
+        // of the lane's 8 keys of each 32-key chunk, vector qs sees the first seen[qs][kc]
+        int seen[Core::QS][2];
+        bool live[Core::QS];
+#pragma unroll
+        for (int qs = 0; qs < Core::QS; ++qs) {
+#pragma unroll
+          for (int kc = 0; kc < 2; ++kc) {
+            const int r = 32 * kc + 8 * k.g, key = b * KB + r;
+            seen[qs][kc] = 0;
+            if (key < n_keys) {
+              const int id = s_id[key >> lps];
+              if ((s_mask[id - wb][word[qs]] >> bit[qs]) & 1) seen[qs][kc] = lim[qs] + 1 - index(r);
+            }
+          }
+          live[qs] = __any(seen[qs][0] > 0 || seen[qs][1] > 0);
+        }
+        if (live[0] || live[1]) {
+          f32x4 st[Core::QS][4];
+          k.scores(b & 1, live, st);
+          typename Core::x8 pb[Core::QS][2];
+#pragma unroll
+          for (int qs = 0; qs < Core::QS; ++qs) {
+            if (!live[qs]) continue;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+              const bool gone = (bad >> (2 * (kt >> 1) + (k.g >> 1))) & 1;
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                st[qs][kt][r] = 4 * (kt & 1) + r < seen[qs][kt >> 1] ? (gone ? NAN : st[qs][kt][r]) : -INFINITY;
+            }
+            k.weights(qs, st[qs], a.c, thr, pb[qs]);
+          }
+          k.product(b & 1, live, pb);
+          while (odd) {
+            const int r = __builtin_ctzll(odd);
+            odd &= odd - 1;
+            const int key = b * KB + r, id = s_id[key >> lps], at = index(r);
+            bool sees[Core::QS];
+#pragma unroll
+            for (int qs = 0; qs < Core::QS; ++qs)
+              sees[qs] = at <= lim[qs] && ((s_mask[id - wb][word[qs]] >> bit[qs]) & 1);
+            k.add_unbounded(s_page[key >> lps], key & (ps - 1), sees);
+          }
+        }
+        bad = next_bad;
+        if constexpr (E8) {
+          if (b + 1 < nb) k.store((b + 1) & 1);
+        }
+      }
     }
-    const float inv = 1.0f / l;
-    T* dst = (T*)p.out + t * p.ldo + hq * HD;
-    typedef T xo __attribute__((ext_vector_type(4), aligned(2)));
+    bool finite = true;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      xo y;
+    for (int qs = 0; qs < Core::QS; ++qs)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = (T)(l == 0.f ? 0.f : o[qs][i][r] * inv);
-      *(xo*)(dst + 16 * i + 4 * g) = y;
-    }
-    if (p.lse && g == 0) p.lse[(size_t)t * a.n.nq + hq] = lse_of(a, m[qs], l);
+      for (int i = 0; i < Core::NT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) finite = finite && fabsf(k.o[qs][i][r]) < INFINITY;
+    if (careful || !__syncthreads_or(!finite)) break;
+    k.clear();
+  }
+
+#pragma unroll
+  for (int qs = 0; qs < Core::QS; ++qs) {
+    const int v = w.v0 + k.wave * 16 * Core::QS + 16 * qs + k.c;
+    if (v < sp.nv) k.write(a, qs, w.tok.x + v / G, h * G + v % G, part);
   }
 }
 
@@ -903,8 +1178,13 @@ hipError_t launch_one(hipStream_t s, const Args& a) {
     else
       hipLaunchKernelGGL((few_kernel<T, E8, HD, false>), grid, dim3(64 * kFewWaves), 0, s, a);
   } else {
-    constexpr int lds = 2 * 2 * KB * HD * 2;
-    hipLaunchKernelGGL((tile_kernel<T, E8, HD>), grid, dim3(64 * kTileWaves), lds, s, a);
+    constexpr int lds = 2 * TileCore<T, E8, HD>::STAGE;
+    const auto kernel = a.t.blocks ? tile_blocks_kernel<T, E8, HD> : tile_kernel<T, E8, HD>;
+    if constexpr (lds > 32768) {  // more than HIP allows unasked, with what the kernels have of their own
+      const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * kTileWaves), lds, s, a);
   }
   return hipGetLastError();
 }

@@ -146,12 +146,8 @@ def _reference(b, blocks=None, scale=None):
             kh, vh, qh = k[:, h * nkv // nq], v[:, h * nkv // nq], q[here:here + n, h]
             for j in range(n):
                 seen = index <= m - n + j
-                times = torch.ones(int(seen.sum()), dtype=torch.float64)
                 if blocks is not None:
-                    mine = [int(x) for x in blocks[here + j, h * nkv // nq]]
-                    count = torch.tensor([mine.count(int(x) // b.page) for x in index])
-                    seen = seen & (count > 0)
-                    times = count[seen].double()
+                    seen = seen & torch.isin(index // b.page, blocks[here + j, h * nkv // nq])
                 out[here + j, h] = 0
                 lse[here + j, h] = -math.inf
                 if not seen.any():
@@ -159,7 +155,7 @@ def _reference(b, blocks=None, scale=None):
                 ks, vs = kh[seen], vh[seen]
                 prod = ks * qh[j]
                 z = prod.sum(-1) * scale
-                w = torch.exp(z - z.max()) * times
+                w = torch.exp(z - z.max())
                 total = w.sum()
                 out[here + j, h] = (w[:, None] * vs).sum(0) / total
                 lse[here + j, h] = z.max() + total.log()
@@ -507,8 +503,9 @@ def _choose(b, mean, n_blocks):
                 continue
             mine = idx // b.page
             for h in range(nkv):
-                z = [float((q[t, h] * mean[int(b.table[i, x]), h].double()).sum()) for x in range(mine)]
-                z = [-math.inf if x != x else x for x in z]
+                # (sums of exact products, exact in any order but for infinities and NaN)
+                z = (q[t, h] * mean[b.table[i, :mine].long(), h].double()).sum(-1)
+                z = [-math.inf if x != x else x for x in z.tolist()]
                 best = sorted(range(mine), key=lambda x: (-z[x], x))[:n_blocks - 1]
                 ids = sorted(best) + [mine]
                 out[t, h, :len(ids)] = torch.tensor(ids, dtype=torch.int32)
@@ -519,7 +516,8 @@ def _choose(b, mean, n_blocks):
 @pytest.mark.parametrize("nq,nkv,page,new,length,n_blocks", [
     (4, 2, 16, [1, 1, 1], [5, 100, 700], 4), (8, 1, 64, [1], [4000], 16), (3, 3, 16, [5, 0, 20], [5, 30, 400], 3),
     (2, 2, 16, [2], [2100], 1), (4, 2, 32, [3], [500], 1000), (4, 1, 16, [4, 3], [2, 64], 2),
-    (14, 2, 16, [1], [9000], 33)])
+    (14, 2, 16, [1], [9000], 33), (4, 2, 16, [40, 17], [600, 333], 8), (6, 2, 16, [9], [24000], 5),
+    (2, 1, 16, [5], [70000], 3)])
 def test_select(L, dtype, hd, nq, nkv, page, new, length, n_blocks):
     print("select", dtype, hd, nq, nkv, page, new, length, n_blocks, flush=True)
     b = Batch(nq, nkv, hd, dtype, dtype, page, new, length, seed=n_blocks)
@@ -543,7 +541,9 @@ def test_select(L, dtype, hd, nq, nkv, page, new, length, n_blocks):
 @pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
 @pytest.mark.parametrize("nq,nkv,page,new,length,n_blocks", [
     (4, 2, 16, [1, 1], [300, 20], 5), (8, 1, 64, [1], [1000], 9), (3, 3, 16, [5, 3], [5, 200], 4),
-    (2, 2, 128, [2], [600], 3), (4, 2, 16, [3], [90], 200), (20, 1, 32, [2], [200], 4), (4, 2, 16, [1], [5000], 256)])
+    (2, 2, 128, [2], [600], 3), (4, 2, 16, [3], [90], 200), (20, 1, 32, [2], [200], 4), (4, 2, 16, [1], [5000], 256),
+    (4, 2, 16, [40, 33], [300, 40], 5), (8, 1, 64, [50], [1500], 7), (3, 1, 128, [43], [700], 3),
+    (4, 4, 32, [130], [2000], 6), (8, 2, 16, [70], [3000], 9), (2, 1, 256, [70], [1000], 2)])
 def test_attend_blocks(L, dtype, cache, hd, nq, nkv, page, new, length, n_blocks):
     print("blocks", dtype, cache, hd, nq, nkv, page, new, length, n_blocks, flush=True)
     b = Batch(nq, nkv, hd, dtype, cache, page, new, length, seed=n_blocks, lead=1, tail=2)
