@@ -8,7 +8,8 @@ namespace lmop {
 constexpr int kFewVectors = 16;    // query vectors (token, head of the group) of a few-vector workgroup
 constexpr int kTileVectors = 128;  // of a tile workgroup
 constexpr int kTileKeys = 64;      // keys of a tile workgroup's step
-constexpr int kTileWindow = 128;   // blocks that a tile workgroup over chosen blocks gathers at a time
+constexpr int kWalkVectors = 32;   // of a wave that walks the blocks its tokens chose
+constexpr int kWalkWindow = 128;   // blocks that it gathers at a time
 constexpr int kMaxEntries = 512;   // pages a few-vector workgroup walks at most
 
 struct AttendSizes {
@@ -47,10 +48,10 @@ inline void split_steps(AttendLaunch& l, int64_t steps, int64_t want, int64_t le
 }
 
 // workgroups that fill the chip
-constexpr int kFewFill = 1024, kTileFill = 512;
+constexpr int kFewFill = 1024, kTileFill = 512, kWalkFill = 2048;
 
-// chosen blocks: vectors of a sequence from which tiles of its tokens walk the blocks of all
-constexpr int kBlocksTileVectors = 64;
+// chosen blocks: vectors of a sequence from which waves walk the blocks of several tokens
+constexpr int kWalkLeast = 64;
 
 inline AttendPlan plan_attend(const AttendSizes& s) {
   AttendPlan p;
@@ -59,16 +60,16 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
   const int64_t pages = ceil_div(s.max_length, s.page_size);
   const int64_t prefix_pages = ceil_div(s.prefix_length, s.page_size);
   const int64_t few_least = ceil_div(256, s.page_size);
-  // tiles: as many as the sequences need, found from the starts, or max_tokens' for each
-  auto tiles = [&](AttendLaunch& l) {
-    const int64_t each = ceil_div(vectors, kTileVectors);
-    const int64_t ragged = (int64_t)s.n_tokens * group / kTileVectors + s.n_seqs;
+  // tiles of `of` vectors: as many as the sequences need, found from the starts, or max_tokens' for each
+  auto tiles = [&](AttendLaunch& l, int of) {
+    const int64_t each = ceil_div(vectors, of);
+    const int64_t ragged = (int64_t)s.n_tokens * group / of + s.n_seqs;
     l.per_seq = s.n_seqs * each <= ragged ? (int)each : 0;
     l.tiles = (int)(l.per_seq ? s.n_seqs * each : ragged);
   };
-  if (s.n_blocks > 0 && s.starts && (int64_t)s.n_tokens * group >= (int64_t)kBlocksTileVectors * s.n_seqs) {
-    tiles(p.own);
-    split_steps(p.own, ceil_div(pages, kTileWindow), kTileFill / ((int64_t)p.own.tiles * s.nkv), 1, 1 << 20);
+  if (s.n_blocks > 0 && s.starts && (int64_t)s.n_tokens * group >= (int64_t)kWalkLeast * s.n_seqs) {
+    tiles(p.own, kWalkVectors);
+    split_steps(p.own, ceil_div(pages, kWalkWindow), kWalkFill / ((int64_t)p.own.tiles * s.nkv), 1, 1 << 20);
     p.parts = p.own.splits > 1 ? p.own.splits : 0;
     return p;
   }
@@ -88,7 +89,7 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     split_steps(p.own, pages + (separate ? 0 : prefix_pages),
                 kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries);
   } else {
-    tiles(p.own);
+    tiles(p.own, kTileVectors);
     split_steps(p.own, ceil_div(s.max_length, kTileKeys) + ceil_div(s.prefix_length, kTileKeys),
                 kTileFill / ((int64_t)p.own.tiles * s.nkv), 8, 1 << 30);
   }

@@ -160,19 +160,226 @@ LMOP_DEVICE f32x4 value4(const lmop_cache& k, const Heads& n, int page, int h, i
 // ---------------------------------------------------------------- few vectors
 constexpr int kFewWaves = 4;
 
+// A wave that takes 16 QS vectors against 32 keys at a time, which come from memory straight to its
+// registers.  Its share of such a chunk: the key rows that score_key names for its lane
+// column, hd / 4 dimensions of each (its group's), as the first product reads them; and 8
+// value rows (its group's keys), 16 lanes side by side along hd.  The second product needs 8
+// keys of a dimension in a lane, so the rows are transposed in registers, half a v_perm an
+// element.  The next chunk's keys are on their way once this one's scores are made, its
+// values once they are used.
+template <typename T, bool E8, int HD, int QS>
+struct WaveCore {
+  typedef typename Half<T>::x8 x8;
+  typedef typename Half<T>::x2 x2;
+  static constexpr int NS = HD / 32;  // k-steps of the score product
+  static constexpr int NT = HD / 16;  // output tiles; lane column c has dimensions NT c .. of a value row
+
+  const lmop_cache& cache;
+  const Heads& n;
+  int g, c, h, ps, lps;
+  x8 qf[QS][NS];
+  f32x4 o[QS][NT], l4[QS];
+  float m[QS];
+  x8 kf[E8 ? 1 : 2][NS];
+  uint4 kw[E8 ? 2 : 1][NS / 2];
+  uint32_t kx[2];
+  uint32_t vw[8][E8 ? NT / 4 : NT / 2];  // 8 value rows, as they are in the page
+  uint2 vx;
+
+  LMOP_DEVICE WaveCore(const Args& a, int h_) : cache(a.t.cache), n(a.n), h(h_) {
+    const int lane = threadIdx.x & 63;
+    g = lane >> 4, c = lane & 15;
+    ps = cache.page_size, lps = __builtin_ctz(ps);
+    clear();
+  }
+  LMOP_DEVICE void clear() {
+#pragma unroll
+    for (int qs = 0; qs < QS; ++qs) {
+      m[qs] = -INFINITY;
+      l4[qs] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[qs][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  // q: the vector's first element, NULL past the end
+  LMOP_DEVICE void load_query(int qs, const T* q) {
+    typedef T xu __attribute__((ext_vector_type(8), aligned(2)));
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      // dimensions of step s: 32 s + 8 g; of 8-bit rows, read 16 at a time, 64 (s / 2) + 16 g + 8 (s % 2)
+      const int d = E8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+      const xu x = q ? *(const xu*)(q + d) : xu{};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qf[qs][s][i] = x[i];
+    }
+  }
+
+  // A chunk's two halves of 16 keys lie in one page each; lanes have key rows of half c / 8 and
+  // values of half g / 2.  page (at least 0) and slot: this lane's half's
+  LMOP_DEVICE int key_half() const { return c >> 3; }
+  LMOP_DEVICE int value_half() const { return g >> 1; }
+  LMOP_DEVICE void load_keys(int64_t page, int slot) {
+    const size_t row = (size_t)h * ps + slot + 8 * ((c >> 2) & 1) + (c & 3);
+    if constexpr (!E8) {
+      const T* k = (const T*)cache.k + page * cache.page_stride + row * HD + 8 * g;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) kf[hf][s] = *(const x8*)(k + 4 * hf * HD + 32 * s);
+    } else {
+      const uint8_t* k = (const uint8_t*)cache.k + page * cache.page_stride + row * HD + 16 * g;
+      const uint8_t* ke = cache.k_exp + page * n.nkv * ps + row;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        kx[hf] = ke[4 * hf];
+#pragma unroll
+        for (int u = 0; u < NS / 2; ++u) kw[hf][u] = *(const uint4*)(k + 4 * hf * HD + 64 * u);
+      }
+    }
+  }
+  LMOP_DEVICE void load_values(int64_t page, int slot) {
+    const size_t row = (size_t)h * ps + slot + 8 * (g & 1);
+    constexpr int W = E8 ? NT / 4 : NT / 2;  // words of a lane's part of a row
+    typedef uint32_t words __attribute__((ext_vector_type(W)));
+    const char* v = (const char*)cache.v + (page * cache.page_stride + row * HD) * (E8 ? 1 : 2) + 4 * W * c;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (W == 1) {
+        vw[j][0] = *(const uint32_t*)(v + j * HD);
+      } else {
+        const words x = *(const words*)(v + j * HD * (E8 ? 1 : 2));
+#pragma unroll
+        for (int i = 0; i < W; ++i) vw[j][i] = x[i];
+      }
+    }
+    if constexpr (E8) vx = *(const uint2*)(cache.v_exp + page * n.nkv * ps + row);
+  }
+
+  // st[qs][hf]: register r of lane group g is the score of key 8 g + 4 hf + r
+  LMOP_DEVICE void scores(f32x4 (&st)[QS][2]) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      x8 k[NS];
+      if constexpr (E8) {
+        const float sc = exp_scale(kx[hf]);
+#pragma unroll
+        for (int u = 0; u < NS / 2; ++u) {
+          k[2 * u] = decode8<T>(kw[hf][u].x, kw[hf][u].y, sc);
+          k[2 * u + 1] = decode8<T>(kw[hf][u].z, kw[hf][u].w, sc);
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) k[s] = kf[hf][s];
+      }
+#pragma unroll
+      for (int qs = 0; qs < QS; ++qs) {
+        st[qs][hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) st[qs][hf] = Half<T>::mfma(k[s], qf[qs][s], st[qs][hf]);
+      }
+    }
+  }
+
+  // the vectors' weights of the chunk and their sums; the states move to a new reference where needed
+  LMOP_DEVICE x8 weights(int qs, const f32x4 (&st)[2], float cs, float thr) {
+    const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
+    float mb = max3(st[0][0], st[0][1], st[0][2]);
+    mb = max3(mb, st[0][3], st[1][0]);
+    mb = max3(mb, st[1][1], st[1][2]);
+    mb = max4(max2(mb, st[1][3]));
+    if (__any(mb > m[qs] + thr)) {
+      const float m_new = mb > m[qs] + thr ? mb : m[qs];
+      const float alpha = rescale(m[qs], m_new, cs);
+      l4[qs] *= alpha;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
+      m[qs] = m_new;
+    }
+    const float nmc = -ref_of(m[qs]) * cs;
+    x8 pb;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(st[hf][r], cs, nmc)),
+                         __builtin_amdgcn_exp2f(__builtin_fmaf(st[hf][r + 1], cs, nmc))};
+        const x2 y = __builtin_convertvector(e, x2);
+        pb[4 * hf + r] = y[0];
+        pb[4 * hf + r + 1] = y[1];
+      }
+    l4[qs] = Half<T>::mfma(ones, pb, l4[qs]);
+    return pb;
+  }
+
+  // The lane's value rows as 16-bit words.  Those from `any` on, which no vector sees, become zeros: they
+  // may hold anything.  With `bounded` infinities and NaN in the others do too; returns the rows that have some.
+  LMOP_DEVICE uint32_t values(uint32_t (&w)[8][NT / 2], bool mend, int any, bool bounded) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (E8) {
+        const float sc = exp_scale(((j < 4 ? vx.x : vx.y) >> (8 * (j & 3))) & 255u);
+#pragma unroll
+        for (int i = 0; i < NT / 4; ++i) {
+          w[j][2 * i] = __builtin_bit_cast(uint32_t, Half<T>::template decode<false>(vw[j][i], sc));
+          w[j][2 * i + 1] = __builtin_bit_cast(uint32_t, Half<T>::template decode<true>(vw[j][i], sc));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NT / 2; ++i) w[j][i] = vw[j][i];
+      }
+    }
+    uint32_t odd = 0;
+    if (mend) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < NT / 2; ++i) {
+          if (j >= any) w[j][i] = 0;
+          if (bounded && unbounded<T>(w[j][i])) odd |= 1u << j, w[j][i] = 0;
+        }
+    }
+    return odd;
+  }
+
+  // O^T += V^T P^T.  Tile i: dimension NT c + i of the lane group's 8 keys
+  LMOP_DEVICE void product(const uint32_t (&w)[8][NT / 2], const x8 (&pb)[QS]) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
+      uint32_t x[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = __builtin_amdgcn_perm(w[2 * q + 1][i >> 1], w[2 * q][i >> 1], sel);
+      const x8 v = __builtin_bit_cast(x8, uint4{x[0], x[1], x[2], x[3]});
+#pragma unroll
+      for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(v, pb[qs], o[qs][i]);
+    }
+  }
+
+  // the infinities and NaN of a value row that were left out, for the vectors that see it
+  LMOP_DEVICE void add_unbounded(int page, int slot, const bool (&sees)[QS]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int i = 0; i < NT; i += 4) {
+        const f32x4 x = value4<T, E8>(cache, n, page, h, slot, NT * (4 * g + r) + i);
+#pragma unroll
+        for (int qs = 0; qs < QS; ++qs)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (sees[qs] && !(fabsf(x[q]) < INFINITY)) o[qs][i + q][r] += x[q];
+      }
+  }
+};
+
 // One workgroup: 16 vectors x a kv head x a split.  Its pages are looked up once, into LDS; wave
 // w takes the 32-key chunks w, w + 4, ...; the four waves' states are joined through LDS at the
 // end.
-//
-// A lane's share of a chunk: the key rows that score_key names for its column, hd / 4 dimensions of each (its group's), as the
-// first product reads them; and 8 value rows (its group's keys), 16 lanes side by side along
-// hd.  The second product needs 8 keys of a dimension in a lane, so the rows are transposed
-// in registers, half a v_perm an element.
 template <typename T, bool E8, int HD, bool BLOCKS>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
-  typedef typename Half<T>::x8 x8;
-  constexpr int NS = HD / 32;   // k-steps of the score product
-  constexpr int NT = HD / 16;   // output tiles; lane column c has dimensions NT c .. of a value row
+  typedef WaveCore<T, E8, HD, 1> Core;
+  typedef typename Core::x8 x8;
+  constexpr int NT = Core::NT;
   constexpr int ORow = HD + 4;  // of the joined outputs in LDS
   __shared__ int e_page[kMaxEntries + 16], e_first[kMaxEntries + 16], e_cap[kMaxEntries + 16];
   __shared__ float s_ml[kFewWaves][2][16];
@@ -181,10 +388,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   const lmop_attend_args& p = a.t;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
   const int tile = blockIdx.x / a.n.nkv, h = blockIdx.x % a.n.nkv, split = blockIdx.y;
   const int G = a.n.nq / a.n.nkv;
-  const int ps = p.cache.page_size, lps = __builtin_ctz(ps);
   const int part = a.part0 + split;
 
   Tile w;
@@ -217,6 +422,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   if (w.v0 >= nv) return;
 
   // the keys that the tile's vectors see, and the pages that hold them
+  Core k(a, h);
+  const int ps = k.ps, lps = k.lps;
   const int n_tok = w.tok.y - w.tok.x;
   const int t_first = w.v0 / G;
   const int t_last = (w.v0 + kFewVectors - 1) / G < n_tok ? (w.v0 + kFewVectors - 1) / G : n_tok - 1;
@@ -228,13 +435,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   const int64_t from = (int64_t)split * a.l.chunk;
   const int64_t left = (int64_t)n_pre + n_own - from;
   const int ne = (int)(left < 0 ? 0 : left < a.l.chunk ? left : a.l.chunk);
+  const int32_t* list = BLOCKS ? p.blocks + ((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks : nullptr;
   bool ascending = true;
   if constexpr (BLOCKS) {
-    const int32_t* list = p.blocks + ((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks;
-    for (int i = tid + 1; i < p.n_blocks; i += 64 * kFewWaves) ascending = ascending && (list[i] < 0 || (list[i - 1] >= 0 && list[i] > list[i - 1]));
+    for (int i = tid + 1; i < p.n_blocks; i += 64 * kFewWaves)
+      ascending = ascending && (list[i] < 0 || (list[i - 1] >= 0 && list[i] > list[i - 1]));
     ascending = !__syncthreads_or(!ascending);
   }
-  for (int i = tid; i < kMaxEntries + 16; i += 64 * kFewWaves) {
+  // (one entry more: of 16-token pages, an odd number of them ends inside a chunk)
+  for (int i = tid; i <= ne; i += 64 * kFewWaves) {
     int page = 0, first = 0, cap = 0;
     if (i < ne) {
       const int e = (int)from + i;
@@ -247,7 +456,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
         int b = e - n_pre;
         if constexpr (BLOCKS) {
           // one listed twice counts once; lists of select_blocks ascend, which rules that out at a glance
-          const int32_t* list = p.blocks + ((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks;
           const int at = b;
           b = list[at];
           bool twice = false;
@@ -262,203 +470,79 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
         }
       }
     }
-    if (i < ((ne + 15) & ~15) + 1) e_page[i] = page, e_first[i] = first, e_cap[i] = cap;
+    e_page[i] = page, e_first[i] = first, e_cap[i] = cap;
   }
 
   // this lane's query vector
-  const int v = w.v0 + c;
-  const bool valid = v < nv;
-  const int tok = valid ? v / G : t_last;
-  const int hq = h * G + (valid ? v - tok * G : 0);
-  const int lim = a.flat ? 0 : w.len - n_tok + tok;
+  const int v = w.v0 + k.c;
+  const int tok = v < nv ? v / G : t_last;
+  const int lim = a.flat ? 0 : w.len - n_tok + tok, lim_any = a.flat ? 0 : lim_max;
   const bool one = t_first == t_last || a.flat;  // all vectors see the same keys
-  const int lim_any = a.flat ? 0 : lim_max;
-  x8 qf[NS];
-  {
-    const T* q = (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + hq * HD;
-    typedef T xu __attribute__((ext_vector_type(8), aligned(2)));
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      // dimensions of step s: 32 s + 8 g; of 8-bit rows, read 16 at a time, 64 (s / 2) + 16 g + 8 (s % 2)
-      const int d = E8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-      const xu x = valid ? *(const xu*)(q + d) : xu{};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) qf[s][i] = x[i];
-    }
-  }
+  k.load_query(0, v < nv ? (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + v - tok * G) * HD : nullptr);
   __syncthreads();
 
-  f32x4 o[NT], l4 = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < NT; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY;
   const float thr = 8.0f / a.c;
   const int n_keys = ne << lps;
-  const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
-
-  for (int kb = wave * 32; kb < n_keys; kb += 32 * kFewWaves) {
-    // halves of 16 keys lie in one page each: this lane's key rows in half c / 8, its values in half g / 2
-    const int at_k = kb + 16 * (c >> 3), at_v = kb + 16 * (g >> 1);
-    const int ek = at_k >> lps, ev = at_v >> lps;
-    const int page_k = e_page[ek], page_v = e_page[ev];
-    const size_t row_k = (size_t)h * ps + (at_k & (ps - 1)) + 8 * ((c >> 2) & 1) + (c & 3);
-    const int slot_v = (at_v & (ps - 1)) + 8 * (g & 1);
-    const size_t row_v = (size_t)h * ps + slot_v;
-    const int64_t pk = page_k < 0 ? 0 : page_k, pv = page_v < 0 ? 0 : page_v;
-
-    x8 kf[2][NS];
-    uint32_t vw[8][NT / 2];  // 8 value rows, 2 values a word
-    if constexpr (!E8) {
-      const T* k = (const T*)p.cache.k + pk * p.cache.page_stride + row_k * HD + 8 * g;
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-        for (int s = 0; s < NS; ++s) kf[hf][s] = *(const x8*)(k + 4 * hf * HD + 32 * s);
-      const T* vp = (const T*)p.cache.v + pv * p.cache.page_stride + row_v * HD + NT * c;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (NT == 8) {
-          const uint4 x = *(const uint4*)(vp + j * HD);
-          vw[j][0] = x.x, vw[j][1] = x.y, vw[j][2] = x.z, vw[j][3] = x.w;
-        } else {
-          const uint2 x = *(const uint2*)(vp + j * HD);
-          vw[j][0] = x.x, vw[j][1] = x.y;
-        }
-      }
-    } else {
-      const uint8_t* k = (const uint8_t*)p.cache.k + pk * p.cache.page_stride + row_k * HD + 16 * g;
-      const uint8_t* ke = p.cache.k_exp + pk * a.n.nkv * ps + row_k;
-      uint4 kw[2][NS / 2];
-      uint32_t kx[2];
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        kx[hf] = ke[4 * hf];
-#pragma unroll
-        for (int u = 0; u < NS / 2; ++u) kw[hf][u] = *(const uint4*)(k + 4 * hf * HD + 64 * u);
-      }
-      const uint8_t* vp = (const uint8_t*)p.cache.v + pv * p.cache.page_stride + row_v * HD + NT * c;
-      const uint2 vx = *(const uint2*)(p.cache.v_exp + pv * a.n.nkv * ps + row_v);
-      uint32_t raw[8][NT / 4];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (NT == 8) {
-          const uint2 x = *(const uint2*)(vp + j * HD);
-          raw[j][0] = x.x, raw[j][1] = x.y;
-        } else {
-          raw[j][0] = *(const uint32_t*)(vp + j * HD);
-        }
-      }
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const float sc = exp_scale(kx[hf]);
-#pragma unroll
-        for (int u = 0; u < NS / 2; ++u) {
-          kf[hf][2 * u] = decode8<T>(kw[hf][u].x, kw[hf][u].y, sc);
-          kf[hf][2 * u + 1] = decode8<T>(kw[hf][u].z, kw[hf][u].w, sc);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float sc = exp_scale(((j < 4 ? vx.x : vx.y) >> (8 * (j & 3))) & 255u);
-#pragma unroll
-        for (int i = 0; i < NT / 4; ++i) {
-          vw[j][2 * i] = __builtin_bit_cast(uint32_t, Half<T>::template decode<false>(raw[j][i], sc));
-          vw[j][2 * i + 1] = __builtin_bit_cast(uint32_t, Half<T>::template decode<true>(raw[j][i], sc));
-        }
-      }
-    }
-
-    f32x4 st[2];
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      st[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < NS; ++s) st[hf] = Half<T>::mfma(kf[hf][s], qf[s], st[hf]);
-    }
+  auto load_keys = [&](int kb) {
+    const int at = kb + 16 * k.key_half(), page = e_page[at >> lps];
+    k.load_keys(page < 0 ? 0 : page, at & (ps - 1));
+  };
+  auto load_values = [&](int kb) {
+    const int at = kb + 16 * k.value_half(), page = e_page[at >> lps];
+    k.load_values(page < 0 ? 0 : page, at & (ps - 1));
+  };
+  constexpr int STEP = 32 * kFewWaves;
+  if (wave * 32 < n_keys) {
+    load_keys(wave * 32);
+    load_values(wave * 32);
+  }
+  for (int kb = wave * 32; kb < n_keys; kb += STEP) {
+    f32x4 st[1][2];
+    k.scores(st);
+    if (kb + STEP < n_keys) load_keys(kb + STEP);
     // of the lane's 8 keys (4 hf + r), its vector sees the first `seen`; any vector the first `any`
-    const int room = e_cap[ev] - slot_v, first = e_first[ev] + slot_v;
+    const int at = kb + 16 * k.value_half(), e = at >> lps, slot = (at & (ps - 1)) + 8 * (k.g & 1);
+    const bool gone = e_page[e] < 0;
+    const int room = e_cap[e] - slot, first = e_first[e] + slot;
     const int seen = room < lim - first + 1 ? room : lim - first + 1;
-    const bool whole = __all(seen >= 8 && page_v >= 0);
-    uint32_t odd = 0;  // the lane's value rows that hold infinities or NaN which not every vector sees
+    const int any = gone ? 0 : room < lim_any - first + 1 ? room : lim_any - first + 1;
+    const bool whole = __all(seen >= 8 && !gone);
     if (!whole) {
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          st[hf][r] = 4 * hf + r < seen ? (page_v < 0 ? NAN : st[hf][r]) : -INFINITY;
-      // what no vector sees may hold anything: zeros instead
-      const int any = room < lim_any - first + 1 ? room : lim_any - first + 1;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int i = 0; i < NT / 2; ++i) {
-          if (j >= any || page_v < 0) vw[j][i] = 0;
-          if (!one && unbounded<T>(vw[j][i])) odd |= 1u << j, vw[j][i] = 0;
-        }
+          st[0][hf][r] = 4 * hf + r < seen ? (gone ? NAN : st[0][hf][r]) : -INFINITY;
     }
-
-    float mb = max3(st[0][0], st[0][1], st[0][2]);
-    mb = max3(mb, st[0][3], st[1][0]);
-    mb = max3(mb, st[1][1], st[1][2]);
-    mb = max4(max2(mb, st[1][3]));
-    if (__any(mb > m + thr)) {
-      const float m_new = mb > m + thr ? mb : m;
-      const float alpha = rescale(m, m_new, a.c);
-      l4 *= alpha;
-#pragma unroll
-      for (int i = 0; i < NT; ++i) o[i] *= alpha;
-      m = m_new;
-    }
-    const float nmc = -ref_of(m) * a.c;
-    x8 pb;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        pb[4 * hf + r] = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(st[hf][r], a.c, nmc));
-    l4 = Half<T>::mfma(ones, pb, l4);
-
-    // output tile i: dimension NT c + i of the lane group's 8 keys
-    auto values = [&](int i) {
-      const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
-      uint32_t x[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) x[q] = __builtin_amdgcn_perm(vw[2 * q + 1][i >> 1], vw[2 * q][i >> 1], sel);
-      return __builtin_bit_cast(x8, uint4{x[0], x[1], x[2], x[3]});
-    };
-#pragma unroll
-    for (int i = 0; i < NT; ++i) o[i] = Half<T>::mfma(values(i), pb, o[i]);
+    const x8 pb[1] = {k.weights(0, st[0], a.c, thr)};
+    uint32_t vals[8][NT / 2];
+    const uint32_t odd = k.values(vals, !whole, any, !one);
+    k.product(vals, pb);
+    if (kb + STEP < n_keys) load_values(kb + STEP);
     if (__any(odd != 0)) {
       for (int j = 0; j < 32; ++j) {
         // key j of the chunk, its rows held by the lanes of group j / 8
         if (!((__ballot((odd >> (j & 7)) & 1) >> (16 * (j >> 3))) & 0xFFFF)) continue;
-        const int at = kb + j, e = at >> lps;
-        if (e_first[e] + (at & (ps - 1)) > lim) continue;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int i = 0; i < NT; i += 4) {
-            const f32x4 x = value4<T, E8>(p.cache, a.n, e_page[e], h, at & (ps - 1), NT * (4 * g + r) + i);
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (!(fabsf(x[q]) < INFINITY)) o[i + q][r] += x[q];
-          }
+        const int key = kb + j;
+        const bool sees[1] = {e_first[key >> lps] + (key & (ps - 1)) <= lim};
+        k.add_unbounded(e_page[key >> lps], key & (ps - 1), sees);
       }
     }
   }
 
   // join the waves
-  if (g == 0) s_ml[wave][0][c] = m, s_ml[wave][1][c] = l4[0];
+  const int g = k.g, c = k.c;
+  if (g == 0) s_ml[wave][0][c] = k.m[0], s_ml[wave][1][c] = k.l4[0][0];
   __syncthreads();
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kFewWaves; ++i) top = fmaxf(top, s_ml[i][0][c]);
-  const float f = rescale(m, top, a.c);
+  const float f = rescale(k.m[0], top, a.c);
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int i = 0; i < NT; i += 4) {
-      const f32x4 y = {o[i][r] * f, o[i + 1][r] * f, o[i + 2][r] * f, o[i + 3][r] * f};
+      const f32x4 y = {k.o[0][i][r] * f, k.o[0][i + 1][r] * f, k.o[0][i + 2][r] * f, k.o[0][i + 3][r] * f};
       *(f32x4*)&s_o[wave][c][NT * (4 * g + r) + i] = y;
     }
   __syncthreads();
@@ -500,10 +584,187 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + ho] = lse_of(a, mt, lt);
 }
 
+// Chosen blocks of neighbouring tokens: a wave, alone, takes 32 vectors (8 tokens of 4 heads) and walks
+// the blocks that any of its tokens chose, in ascending order, a window of kWindow
+// at a time.  Neighbours choose many blocks in common, and waves that walk the same way
+// find them in their L2, if the waves of a kv head are on one XCD (consecutive workgroups are dealt
+// to the eight XCDs in turn).
+constexpr int kWindow = kWalkWindow;
+constexpr int kWalkTokens = kWalkVectors;  // at most, with one head a group
+
+template <typename T, bool E8, int HD>
+__global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
+  constexpr int QS = kWalkVectors / 16;
+  typedef WaveCore<T, E8, HD, QS> Core;
+  typedef typename Core::x8 x8;
+  constexpr int NT = Core::NT;
+  static_assert(kWalkTokens <= 32, "a word of tokens");
+  __shared__ uint32_t s_mask[kWindow];                           // the window's blocks: which tokens chose them
+  __shared__ int s_id[kWindow + 2], s_page[kWindow + 2];         // the chosen ones
+  __shared__ uint32_t s_who[kWindow + 2];
+
+  const lmop_attend_args& p = a.t;
+  const int lane = threadIdx.x;
+  const int h = blockIdx.x % a.n.nkv, split = blockIdx.y, part = a.part0 + split;
+  const int G = a.n.nq / a.n.nkv;
+  const Tile w = find_tile(a, (int)blockIdx.x / a.n.nkv, kWalkVectors);
+  const int n_tok = w.tok.y - w.tok.x, nv = n_tok * G;
+  if (w.v0 >= nv) return;
+  if (w.bad) {
+    const int end = a.l.per_seq && w.v0 + kWalkVectors >= a.l.per_seq * kWalkVectors ? nv : w.v0 + kWalkVectors;
+    for (int v = w.v0; v < end && v < nv; ++v) write_bad<T>(a, w.tok.x + v / G, h * G + v % G, part, lane, 64);
+    return;
+  }
+  const int t_first = w.v0 / G;
+  const int t_last = (w.v0 + kWalkVectors - 1) / G < n_tok ? (w.v0 + kWalkVectors - 1) / G : n_tok - 1;
+  const int lim0 = w.len - n_tok, lim_max = lim0 + t_last;
+
+  Core k(a, h);
+  const int ps = k.ps, lps = k.lps;
+  int lim[QS];
+  uint32_t bit[QS];
+#pragma unroll
+  for (int qs = 0; qs < QS; ++qs) {
+    const int v = w.v0 + 16 * qs + k.c;
+    const int tok = v < nv ? v / G : t_last;
+    lim[qs] = v < nv ? lim0 + tok : -1;
+    bit[qs] = 1u << (tok - t_first);
+    k.load_query(qs, v < nv ? (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + v - tok * G) * HD : nullptr);
+  }
+  const float thr = 8.0f / a.c;
+  const int32_t* lists = p.blocks + ((size_t)(w.tok.x + t_first) * a.n.nkv + h) * p.n_blocks;
+  const int n_list = (t_last - t_first + 1) * p.n_blocks;
+  const int blocks = lim_max < 0 ? 0 : (lim_max >> lps) + 1;
+  const int64_t w_from = (int64_t)split * a.l.chunk * kWindow;
+  const int first_block = w_from < blocks ? (int)w_from : blocks;
+  const int last_block =
+      blocks - first_block < (int64_t)a.l.chunk * kWindow ? blocks : first_block + a.l.chunk * kWindow;
+
+  // Infinities and NaN among the values reach vectors that do not see them (0 * inf).  They are rare, so the
+  // walk looks for them only when it has to go again: careful.
+  for (int careful = 0; careful < 2; ++careful) {
+    for (int wb = first_block; wb < last_block; wb += kWindow) {
+      const int wn = last_block - wb < kWindow ? last_block - wb : kWindow;
+      __syncthreads();
+      for (int i = lane; i < kWindow; i += 64) s_mask[i] = 0;
+      __syncthreads();
+      for (int i = lane; i < n_list; i += 64) {
+        const int t = i / p.n_blocks, b = lists[(size_t)t * a.n.nkv * p.n_blocks + (i - t * p.n_blocks)];
+        if (b >= wb && b - wb < wn && b <= ((lim0 + t_first + t) >> lps)) atomicOr(&s_mask[b - wb], 1u << t);
+      }
+      __syncthreads();
+      int ne = 0;
+      for (int i = 0; i < kWindow; i += 64) {
+        const uint32_t who = s_mask[i + lane];
+        const uint64_t set = __ballot(who != 0);
+        if (who) {
+          const int at = ne + __builtin_popcountll(set & ((1ull << lane) - 1));
+          s_id[at] = wb + i + lane;
+          s_who[at] = who;
+          s_page[at] = page_of(p.batch, p.cache.n_pages, w.seq, wb + i + lane);
+        }
+        ne += __builtin_popcountll(set);
+      }
+      // (of 16-token pages, an odd number of them ends inside a chunk)
+      if (lane == 0) s_id[ne] = 0, s_page[ne] = 0, s_who[ne] = 0;
+      __syncthreads();
+
+      const int n_keys = ne << lps;
+      auto load_keys = [&](int kb) {
+        const int at = kb + 16 * k.key_half(), page = s_page[at >> lps];
+        k.load_keys(page < 0 ? 0 : page, at & (ps - 1));
+      };
+      auto load_values = [&](int kb) {
+        const int at = kb + 16 * k.value_half(), page = s_page[at >> lps];
+        k.load_values(page < 0 ? 0 : page, at & (ps - 1));
+      };
+      if (n_keys > 0) {
+        load_keys(0);
+        load_values(0);
+      }
+      for (int kb = 0; kb < n_keys; kb += 32) {
+        f32x4 st[QS][2];
+        k.scores(st);
+        if (kb + 32 < n_keys) load_keys(kb + 32);
+        const int at = kb + 16 * k.value_half(), e = at >> lps, slot = (at & (ps - 1)) + 8 * (k.g & 1);
+        const bool gone = s_page[e] < 0;
+        const uint32_t who = s_who[e];
+        const int index = (s_id[e] << lps) + slot;
+        x8 pb[QS];
+#pragma unroll
+        for (int qs = 0; qs < QS; ++qs) {
+          // of the lane's 8 keys, its vector sees the first `seen`
+          const int seen = who & bit[qs] ? lim[qs] + 1 - index : 0;
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              st[qs][hf][r] = 4 * hf + r < seen ? (gone ? NAN : st[qs][hf][r]) : -INFINITY;
+          pb[qs] = k.weights(qs, st[qs], a.c, thr);
+        }
+        const int any = gone || who == 0 ? 0 : lim_max + 1 - index;
+        uint32_t vals[8][NT / 2];
+        const uint32_t odd = k.values(vals, careful || !__all(any >= 8), any, careful);
+        k.product(vals, pb);
+        if (kb + 32 < n_keys) load_values(kb + 32);
+        if (careful && __any(odd != 0)) {
+          for (int j = 0; j < 32; ++j) {
+            if (!((__ballot((odd >> (j & 7)) & 1) >> (16 * (j >> 3))) & 0xFFFF)) continue;
+            const int key = kb + j, en = key >> lps;
+            bool sees[QS];
+#pragma unroll
+            for (int qs = 0; qs < QS; ++qs)
+              sees[qs] = (s_who[en] & bit[qs]) && (s_id[en] << lps) + (key & (ps - 1)) <= lim[qs];
+            k.add_unbounded(s_page[en], key & (ps - 1), sees);
+          }
+        }
+      }
+    }
+    bool finite = true;
+#pragma unroll
+    for (int qs = 0; qs < QS; ++qs)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) finite = finite && fabsf(k.o[qs][i][r]) < INFINITY;
+    if (careful || __all(finite)) break;
+    k.clear();
+  }
+
+#pragma unroll
+  for (int qs = 0; qs < QS; ++qs) {
+    const int v = w.v0 + 16 * qs + k.c;
+    if (v >= nv) continue;
+    const int t = w.tok.x + v / G, hq = h * G + v % G;
+    const float l = k.l4[qs][0];
+    if (a.parts) {
+      float* dst = part_o(a, part, t, hq);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < NT; i += 4)
+          *(f32x4*)(dst + NT * (4 * k.g + r) + i) =
+              f32x4{k.o[qs][i][r], k.o[qs][i + 1][r], k.o[qs][i + 2][r], k.o[qs][i + 3][r]};
+      if (k.g == 0) *part_ml(a, part, t, hq) = float2{k.m[qs], l};
+      continue;
+    }
+    const float inv = 1.0f / l;
+    T* dst = (T*)p.out + t * p.ldo + hq * HD;
+    typedef T xo __attribute__((ext_vector_type(NT), aligned(2)));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      xo y;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) y[i] = (T)(l == 0.f ? 0.f : k.o[qs][i][r] * inv);
+      *(xo*)(dst + NT * (4 * k.g + r)) = y;
+    }
+    if (p.lse && k.g == 0) p.lse[(size_t)t * a.n.nq + hq] = lse_of(a, k.m[qs], l);
+  }
+}
+
 // ---------------------------------------------------------------- tiles
 constexpr int kTileWaves = 4;
 constexpr int KB = kTileKeys;
-constexpr int kWindow = kTileWindow;
 
 // 16-byte chunk c of LDS row `key` lies at chunk c ^ kswz: score fragments (score_key's rows, one
 // chunk column) then meet every bank
@@ -535,7 +796,7 @@ struct Groups {
   uint32_t bad;          // groups whose page does not exist
 };
 
-// What both tile kernels share.  A workgroup: 128 vectors x a kv head, 32 vectors a wave.  Blocks of 64
+// A workgroup: 128 vectors x a kv head, 32 vectors a wave.  Blocks of 64
 // keys come into one of two LDS stages while the block before them is worked on:
 // 16-bit pages by direct loads (a row's chunks permuted on the way), 8-bit ones through
 // registers, where they become 16 bits.
@@ -673,9 +934,8 @@ struct TileCore {
     }
   }
 
-  // Scores of the vectors qs with live[qs].  st[qs][kt]: register r of lane group g is key
-  // 32 (kt / 2) + 8 g + 4 (kt % 2) + r
-  LMOP_DEVICE void scores(int stage, const bool* live, f32x4 (&st)[QS][4]) {
+  // st[qs][kt]: register r of lane group g is the score of key 32 (kt / 2) + 8 g + 4 (kt % 2) + r
+  LMOP_DEVICE void scores(int stage, f32x4 (&st)[QS][4]) {
     const char* sk = smem + stage * STAGE;
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
@@ -685,7 +945,6 @@ struct TileCore {
       for (int s = 0; s < NS; ++s) kf[s] = *(const x8*)(sk + key * ROW + (((4 * s + g) ^ kswz<HD>(key)) * 16));
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) {
-        if (!live[qs]) continue;
         st[qs][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NS; ++s) st[qs][kt] = Half<T>::mfma(kf[s], qf[qs][s], st[qs][kt]);
@@ -730,7 +989,7 @@ struct TileCore {
 
   // O^T += V^T P^T.  Tile i: dimensions 16 i .. +15; lane (g, c) gets dimension 16 i + c of keys
   // 32 kc + 8 g .. +7
-  LMOP_DEVICE void product(int stage, const bool* live, const x8 (&pb)[QS][2]) {
+  LMOP_DEVICE void product(int stage, const x8 (&pb)[QS][2]) {
     const char* sv = smem + stage * STAGE + KB * ROW;
 #pragma unroll
     for (int kc = 0; kc < 2; ++kc)
@@ -741,8 +1000,7 @@ struct TileCore {
         const x4 hi = read_transposed<T>(sv + (key + 4) * ROW + ((i ^ vswz<HD>(key + 4)) * 32) + (c & 3) * 8);
         const x8 x = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 #pragma unroll
-        for (int qs = 0; qs < QS; ++qs)
-          if (live[qs]) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
+        for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
       }
   }
 
@@ -862,7 +1120,6 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
   }
   // a wave whose vectors all lie past the end only helps to load
   const bool active = w.v0 + k.wave * 16 * Core::QS < sp.nv;
-  const bool both[2] = {true, true};
   const float thr = 8.0f / a.c;
 
   if (k.tid < 4) s_odd[k.tid >> 1][k.tid & 1] = 0;
@@ -897,7 +1154,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
     }
     if (active) {
       f32x4 st[Core::QS][4];
-      k.scores(b & 1, both, st);
+      k.scores(b & 1, st);
       if (mixed || kb + KB > n || bad != 0) {
 #pragma unroll
         for (int qs = 0; qs < Core::QS; ++qs) {
@@ -916,7 +1173,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
       typename Core::x8 pb[Core::QS][2];
 #pragma unroll
       for (int qs = 0; qs < Core::QS; ++qs) k.weights(qs, st[qs], a.c, thr, pb[qs]);
-      k.product(b & 1, both, pb);
+      k.product(b & 1, pb);
       while (odd) {
         const int key = kb + __builtin_ctzll(odd);
         odd &= odd - 1;
@@ -932,197 +1189,6 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) 
   }
 
   if (!active) return;
-#pragma unroll
-  for (int qs = 0; qs < Core::QS; ++qs) {
-    const int v = w.v0 + k.wave * 16 * Core::QS + 16 * qs + k.c;
-    if (v < sp.nv) k.write(a, qs, w.tok.x + v / G, h * G + v % G, part);
-  }
-}
-
-// Over chosen blocks: a tile walks the blocks that any of its tokens chose, in ascending order, a window
-// of kWindow at a time, and a wave works on those that one of its vectors sees.  Neighbours choose
-// many blocks in common, and workgroups that walk the same way find them in their L2.
-template <typename T, bool E8, int HD>
-__global__ __launch_bounds__(64 * kTileWaves, 2) void tile_blocks_kernel(const Args a) {
-  typedef TileCore<T, E8, HD> Core;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  __shared__ uint32_t s_odd[2][2];
-  __shared__ uint32_t s_mask[kWindow][kTileVectors / 32];  // the window's blocks: which of the tile's tokens chose it
-  __shared__ int s_id[kWindow], s_page[kWindow];           // the chosen ones
-  __shared__ int s_n;
-
-  const lmop_attend_args& p = a.t;
-  const int h = blockIdx.x % a.n.nkv, split = blockIdx.y;
-  const int G = a.n.nq / a.n.nkv;
-  const int ps = p.cache.page_size, lps = __builtin_ctz(ps);
-  const int part = a.part0 + split;
-  const Tile w = find_tile(a, (int)blockIdx.x / a.n.nkv, kTileVectors);
-  const Span sp(w, G);
-  if (w.v0 >= sp.nv) return;
-  if (w.bad) return write_bad_tile<T>(a, w, sp.nv, h, part);
-  const int lim0 = w.len - sp.n_tok, lim_max = lim0 + sp.t_last;
-  const int n_tile = sp.t_last - sp.t_first + 1;
-
-  Core k(a, smem, h);
-  int lim[Core::QS], word[Core::QS], bit[Core::QS];
-#pragma unroll
-  for (int qs = 0; qs < Core::QS; ++qs) {
-    const int v = w.v0 + k.wave * 16 * Core::QS + 16 * qs + k.c;
-    const int tok = v < sp.nv ? v / G : sp.t_last;
-    lim[qs] = v < sp.nv ? lim0 + tok : -1;
-    word[qs] = (tok - sp.t_first) >> 5, bit[qs] = (tok - sp.t_first) & 31;
-    k.load_query(qs, v < sp.nv ? (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + v - tok * G) * HD : nullptr);
-  }
-  const float thr = 8.0f / a.c;
-  const int32_t* lists = p.blocks + ((size_t)(w.tok.x + sp.t_first) * a.n.nkv + h) * p.n_blocks;
-  const int blocks = lim_max < 0 ? 0 : (lim_max >> lps) + 1;
-  const int64_t w_from = (int64_t)split * a.l.chunk * kWindow;
-  const int first_block = w_from < blocks ? (int)w_from : blocks;
-  const int last_block = blocks - first_block < a.l.chunk * (int64_t)kWindow ? blocks : first_block + a.l.chunk * kWindow;
-
-  // Infinities and NaN among the values reach vectors that do not see them (0 * inf).  They are rare, so the
-  // walk looks for them only when it has to go again: careful.
-  for (int careful = 0; careful < 2; ++careful) {
-    for (int wb = first_block; wb < last_block; wb += kWindow) {
-      const int wn = last_block - wb < kWindow ? last_block - wb : kWindow;
-      __syncthreads();
-      for (int i = k.tid; i < kWindow * (kTileVectors / 32); i += 64 * kTileWaves) (&s_mask[0][0])[i] = 0;
-      if (k.tid < 4) s_odd[k.tid >> 1][k.tid & 1] = 0;
-      __syncthreads();
-      for (int i = k.tid; i < n_tile * p.n_blocks; i += 64 * kTileWaves) {
-        const int t = i / p.n_blocks, b = lists[(size_t)t * a.n.nkv * p.n_blocks + (i - t * p.n_blocks)];
-        if (b >= wb && b - wb < wn && b <= ((lim0 + sp.t_first + t) >> lps)) atomicOr(&s_mask[b - wb][t >> 5], 1u << (t & 31));
-      }
-      __syncthreads();
-      if (k.tid < 64) {
-        int placed = 0;
-#pragma unroll
-        for (int i = 0; i < kWindow; i += 64) {
-          const int b = i + k.lane;
-          uint32_t any = 0;
-#pragma unroll
-          for (int q = 0; q < kTileVectors / 32; ++q) any |= s_mask[b][q];
-          const uint64_t set = __ballot(any != 0);
-          if (any) {
-            const int at = placed + __builtin_popcountll(set & ((1ull << k.lane) - 1));
-            s_id[at] = wb + b;
-            s_page[at] = page_of(p.batch, p.cache.n_pages, w.seq, wb + b);
-          }
-          placed += __builtin_popcountll(set);
-        }
-        if (k.lane == 0) s_n = placed;
-      }
-      __syncthreads();
-      const int n_keys = __builtin_amdgcn_readfirstlane(s_n) << lps;
-      const int nb = (n_keys + KB - 1) / KB;
-      auto look_up = [&](int b) {
-        Groups r;
-        r.bad = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = b * KB + 16 * i;
-          int q = 0;
-          if (key < n_keys) {
-            q = __builtin_amdgcn_readfirstlane(s_page[key >> lps]);
-            if (q < 0) q = 0, r.bad |= 1u << i;
-          }
-          r.page[i] = q;
-          r.slot[i] = key & (ps - 1);
-        }
-        return r;
-      };
-      uint32_t bad = 0;
-      Groups next{};
-      if (nb > 0) {
-        const Groups first = look_up(0);
-        k.load(first, 0);
-        bad = first.bad;
-        next = look_up(1);
-        if constexpr (E8) k.store(0);
-      }
-      for (int b = 0; b < nb; ++b) {
-        if constexpr (!E8) wait_vmcnt<0>();
-        __syncthreads();
-        const uint32_t next_bad = next.bad;
-        if (b + 1 < nb) {
-          k.load(next, (b + 1) & 1);
-          next = look_up(b + 2);
-        }
-        // index of the key in row r of the block
-        const int e_last = ((b + 1) * KB < n_keys ? (b + 1) * KB : n_keys) - 1;
-        auto index = [&](int r) {
-          const int key = b * KB + r;
-          return key < n_keys ? (s_id[key >> lps] << lps) + (key & (ps - 1)) : 0x7FFFFFFF;
-        };
-        // (ids ascend, so the block's last key has the largest index)
-        uint64_t odd = 0;
-        if (careful || bad != 0 || (b + 1) * KB > n_keys || index(e_last - b * KB) > lim_max) {
-          if (k.tid < 2) s_odd[(b + 1) & 1][k.tid] = 0;
-          k.mend(b & 1, [&](int r) { return index(r) > lim_max || ((bad >> (r >> 4)) & 1); }, careful != 0, s_odd[b & 1]);
-          __syncthreads();
-          odd = s_odd[b & 1][0] | (uint64_t)s_odd[b & 1][1] << 32;
-        }
-        // of the lane's 8 keys of each 32-key chunk, vector qs sees the first seen[qs][kc]
-        int seen[Core::QS][2];
-        bool live[Core::QS];
-#pragma unroll
-        for (int qs = 0; qs < Core::QS; ++qs) {
-#pragma unroll
-          for (int kc = 0; kc < 2; ++kc) {
-            const int r = 32 * kc + 8 * k.g, key = b * KB + r;
-            seen[qs][kc] = 0;
-            if (key < n_keys) {
-              const int id = s_id[key >> lps];
-              if ((s_mask[id - wb][word[qs]] >> bit[qs]) & 1) seen[qs][kc] = lim[qs] + 1 - index(r);
-            }
-          }
-          live[qs] = __any(seen[qs][0] > 0 || seen[qs][1] > 0);
-        }
-        if (live[0] || live[1]) {
-          f32x4 st[Core::QS][4];
-          k.scores(b & 1, live, st);
-          typename Core::x8 pb[Core::QS][2];
-#pragma unroll
-          for (int qs = 0; qs < Core::QS; ++qs) {
-            if (!live[qs]) continue;
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
-              const bool gone = (bad >> (2 * (kt >> 1) + (k.g >> 1))) & 1;
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                st[qs][kt][r] = 4 * (kt & 1) + r < seen[qs][kt >> 1] ? (gone ? NAN : st[qs][kt][r]) : -INFINITY;
-            }
-            k.weights(qs, st[qs], a.c, thr, pb[qs]);
-          }
-          k.product(b & 1, live, pb);
-          while (odd) {
-            const int r = __builtin_ctzll(odd);
-            odd &= odd - 1;
-            const int key = b * KB + r, id = s_id[key >> lps], at = index(r);
-            bool sees[Core::QS];
-#pragma unroll
-            for (int qs = 0; qs < Core::QS; ++qs)
-              sees[qs] = at <= lim[qs] && ((s_mask[id - wb][word[qs]] >> bit[qs]) & 1);
-            k.add_unbounded(s_page[key >> lps], key & (ps - 1), sees);
-          }
-        }
-        bad = next_bad;
-        if constexpr (E8) {
-          if (b + 1 < nb) k.store((b + 1) & 1);
-        }
-      }
-    }
-    bool finite = true;
-#pragma unroll
-    for (int qs = 0; qs < Core::QS; ++qs)
-#pragma unroll
-      for (int i = 0; i < Core::NT; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) finite = finite && fabsf(k.o[qs][i][r]) < INFINITY;
-    if (careful || !__syncthreads_or(!finite)) break;
-    k.clear();
-  }
-
 #pragma unroll
   for (int qs = 0; qs < Core::QS; ++qs) {
     const int v = w.v0 + k.wave * 16 * Core::QS + 16 * qs + k.c;
@@ -1172,14 +1238,16 @@ __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
 template <typename T, bool E8, int HD>
 hipError_t launch_one(hipStream_t s, const Args& a) {
   const dim3 grid(a.n.nkv * a.l.tiles, a.l.splits);
-  if (a.l.few) {
+  if (a.t.blocks && !a.l.few) {
+    hipLaunchKernelGGL((walk_kernel<T, E8, HD>), grid, dim3(64), 0, s, a);
+  } else if (a.l.few) {
     if (a.t.blocks)
       hipLaunchKernelGGL((few_kernel<T, E8, HD, true>), grid, dim3(64 * kFewWaves), 0, s, a);
     else
       hipLaunchKernelGGL((few_kernel<T, E8, HD, false>), grid, dim3(64 * kFewWaves), 0, s, a);
   } else {
     constexpr int lds = 2 * TileCore<T, E8, HD>::STAGE;
-    const auto kernel = a.t.blocks ? tile_blocks_kernel<T, E8, HD> : tile_kernel<T, E8, HD>;
+    const auto kernel = tile_kernel<T, E8, HD>;
     if constexpr (lds > 32768) {  // more than HIP allows unasked, with what the kernels have of their own
       const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       if (e != hipSuccess) return e;
