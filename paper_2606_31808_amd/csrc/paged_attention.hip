@@ -160,13 +160,13 @@ LMOP_DEVICE f32x4 value4(const lmop_cache& k, const Heads& n, int page, int h, i
 // ---------------------------------------------------------------- few vectors
 constexpr int kFewWaves = 4;
 
-// A wave that takes 16 QS vectors against 32 keys at a time, which come from memory straight to its
-// registers.  Its share of such a chunk: the key rows that score_key names for its lane
-// column, hd / 4 dimensions of each (its group's), as the first product reads them; and 8
-// value rows (its group's keys), 16 lanes side by side along hd.  The second product needs 8
-// keys of a dimension in a lane, so the rows are transposed in registers, half a v_perm an
-// element.  The next chunk's keys are on their way once this one's scores are made, its
-// values once they are used.
+// A wave that takes 16 QS vectors against 32 keys at a time, which come from memory to its
+// registers, the next chunk's while this one is worked on.  Lanes side by side read a row:
+// the caches take four lanes' 64 bytes at a time if they adjoin (a row to each lane, as the first product
+// has them, took four times the accesses, and bound the walk over chosen blocks: 403 us).  So
+// keys change lanes, through LDS of the wave's own, without a barrier.  Of the values a lane has
+// 8 rows (its group's keys), 16 lanes side by side along hd; the second product needs 8 keys of a
+// dimension in a lane, so the rows are transposed in registers, half a v_perm an element.
 template <typename T, bool E8, int HD, int QS>
 struct WaveCore {
   typedef typename Half<T>::x8 x8;
@@ -176,18 +176,21 @@ struct WaveCore {
 
   const lmop_cache& cache;
   const Heads& n;
-  int g, c, h, ps, lps;
+  int lane, g, c, h, ps, lps;
   x8 qf[QS][NS];
   f32x4 o[QS][NT], l4[QS];
   float m[QS];
-  x8 kf[E8 ? 1 : 2][NS];
-  uint4 kw[E8 ? 2 : 1][NS / 2];
-  uint32_t kx[2];
+  static constexpr int ROW = HD * (E8 ? 1 : 2);  // bytes of a row
+  static constexpr int CH = ROW / 16;            // its 16-byte chunks
+  static constexpr int KL = 32 * ROW / 1024;     // loads of a chunk's keys
+  char* lds;                                     // 32 rows of keys
+  uint4 kr[KL];
+  uint2 kx;                                      // the exponents of keys 8 (c / 4) .. +7
   uint32_t vw[8][E8 ? NT / 4 : NT / 2];  // 8 value rows, as they are in the page
   uint2 vx;
 
-  LMOP_DEVICE WaveCore(const Args& a, int h_) : cache(a.t.cache), n(a.n), h(h_) {
-    const int lane = threadIdx.x & 63;
+  LMOP_DEVICE WaveCore(const Args& a, int h_, char* lds_) : cache(a.t.cache), n(a.n), h(h_), lds(lds_) {
+    lane = threadIdx.x & 63;
     g = lane >> 4, c = lane & 15;
     ps = cache.page_size, lps = __builtin_ctz(ps);
     clear();
@@ -214,29 +217,39 @@ struct WaveCore {
     }
   }
 
-  // A chunk's two halves of 16 keys lie in one page each; lanes have key rows of half c / 8 and
-  // values of half g / 2.  page (at least 0) and slot: this lane's half's
-  LMOP_DEVICE int key_half() const { return c >> 3; }
-  LMOP_DEVICE int value_half() const { return g >> 1; }
-  LMOP_DEVICE void load_keys(int64_t page, int slot) {
-    const size_t row = (size_t)h * ps + slot + 8 * ((c >> 2) & 1) + (c & 3);
-    if constexpr (!E8) {
-      const T* k = (const T*)cache.k + page * cache.page_stride + row * HD + 8 * g;
+  // chunk ch of key row r in LDS: the rows that a fragment takes meet every bank
+  static LMOP_DEVICE int key_at(int r, int ch) {
+    const int m = ((r >> 1) & 12) | (r & 3);  // row r is row m of a score tile
+    return r * ROW + (ch ^ (m & (CH - 1))) * 16;
+  }
+  // A chunk's two halves of 16 keys lie in one page each (at least 0); page and slot are the same for the
+  // whole wave
+  LMOP_DEVICE void load_keys(const int (&page)[2], const int (&slot)[2]) {
+    constexpr int RPL = 64 / CH;  // rows of a load
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-        for (int s = 0; s < NS; ++s) kf[hf][s] = *(const x8*)(k + 4 * hf * HD + 32 * s);
-    } else {
-      const uint8_t* k = (const uint8_t*)cache.k + page * cache.page_stride + row * HD + 16 * g;
-      const uint8_t* ke = cache.k_exp + page * n.nkv * ps + row;
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        kx[hf] = ke[4 * hf];
-#pragma unroll
-        for (int u = 0; u < NS / 2; ++u) kw[hf][u] = *(const uint4*)(k + 4 * hf * HD + 64 * u);
-      }
+    for (int i = 0; i < KL; ++i) {
+      const int half = i * RPL / 16;
+      const char* base = (const char*)cache.k + (page[half] * cache.page_stride + ((int64_t)h * ps + slot[half]) * HD) * (E8 ? 1 : 2);
+      kr[i] = *(const uint4*)(base + (i * RPL % 16 + lane / CH) * ROW + lane % CH * 16);
+    }
+    if constexpr (E8) {
+      const int half = c >> 3;
+      kx = *(const uint2*)(cache.k_exp + ((int64_t)(half ? page[1] : page[0]) * n.nkv + h) * ps +
+                           (half ? slot[1] : slot[0]) + 8 * ((c >> 2) & 1));
     }
   }
+  uint32_t key_exp[2];
+  LMOP_DEVICE void stash_keys() {
+    constexpr int RPL = 64 / CH;
+#pragma unroll
+    for (int i = 0; i < KL; ++i) *(uint4*)(lds + key_at(i * RPL + lane / CH, lane % CH)) = kr[i];
+    if constexpr (E8) {
+      key_exp[0] = (kx.x >> (8 * (c & 3))) & 255u;
+      key_exp[1] = (kx.y >> (8 * (c & 3))) & 255u;
+    }
+  }
+  // values of half g / 2 are this lane's
+  LMOP_DEVICE int value_half() const { return g >> 1; }
   LMOP_DEVICE void load_values(int64_t page, int slot) {
     const size_t row = (size_t)h * ps + slot + 8 * (g & 1);
     constexpr int W = E8 ? NT / 4 : NT / 2;  // words of a lane's part of a row
@@ -260,16 +273,18 @@ struct WaveCore {
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       x8 k[NS];
+      const int row = score_key(hf, c);
       if constexpr (E8) {
-        const float sc = exp_scale(kx[hf]);
+        const float sc = exp_scale(key_exp[hf]);
 #pragma unroll
         for (int u = 0; u < NS / 2; ++u) {
-          k[2 * u] = decode8<T>(kw[hf][u].x, kw[hf][u].y, sc);
-          k[2 * u + 1] = decode8<T>(kw[hf][u].z, kw[hf][u].w, sc);
+          const uint4 w = *(const uint4*)(lds + key_at(row, 4 * u + g));
+          k[2 * u] = decode8<T>(w.x, w.y, sc);
+          k[2 * u + 1] = decode8<T>(w.z, w.w, sc);
         }
       } else {
 #pragma unroll
-        for (int s = 0; s < NS; ++s) k[s] = kf[hf][s];
+        for (int s = 0; s < NS; ++s) k[s] = *(const x8*)(lds + key_at(row, 4 * s + g));
       }
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) {
@@ -381,9 +396,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   typedef typename Core::x8 x8;
   constexpr int NT = Core::NT;
   constexpr int ORow = HD + 4;  // of the joined outputs in LDS
+  // the waves' keys, and in their place at the end their outputs
+  constexpr int KEYS = 32 * Core::ROW, OUTS = 16 * ORow * 4;
+  __shared__ __attribute__((aligned(16))) char s_mem[kFewWaves * (KEYS > OUTS ? KEYS : OUTS)];
+  float(*s_o)[16][ORow] = (float(*)[16][ORow])s_mem;
   __shared__ int e_page[kMaxEntries + 16], e_first[kMaxEntries + 16], e_cap[kMaxEntries + 16];
   __shared__ float s_ml[kFewWaves][2][16];
-  __shared__ __attribute__((aligned(16))) float s_o[kFewWaves][16][ORow];
 
   const lmop_attend_args& p = a.t;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -422,7 +440,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   if (w.v0 >= nv) return;
 
   // the keys that the tile's vectors see, and the pages that hold them
-  Core k(a, h);
+  Core k(a, h, s_mem + wave * KEYS);
   const int ps = k.ps, lps = k.lps;
   const int n_tok = w.tok.y - w.tok.x;
   const int t_first = w.v0 / G;
@@ -484,8 +502,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   const float thr = 8.0f / a.c;
   const int n_keys = ne << lps;
   auto load_keys = [&](int kb) {
-    const int at = kb + 16 * k.key_half(), page = e_page[at >> lps];
-    k.load_keys(page < 0 ? 0 : page, at & (ps - 1));
+    int page[2], slot[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = kb + 16 * i, q = __builtin_amdgcn_readfirstlane(e_page[at >> lps]);
+      page[i] = q < 0 ? 0 : q, slot[i] = at & (ps - 1);
+    }
+    k.load_keys(page, slot);
   };
   auto load_values = [&](int kb) {
     const int at = kb + 16 * k.value_half(), page = e_page[at >> lps];
@@ -498,8 +521,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   }
   for (int kb = wave * 32; kb < n_keys; kb += STEP) {
     f32x4 st[1][2];
-    k.scores(st);
+    k.stash_keys();
     if (kb + STEP < n_keys) load_keys(kb + STEP);
+    k.scores(st);
     // of the lane's 8 keys (4 hf + r), its vector sees the first `seen`; any vector the first `any`
     const int at = kb + 16 * k.value_half(), e = at >> lps, slot = (at & (ps - 1)) + 8 * (k.g & 1);
     const bool gone = e_page[e] < 0;
@@ -602,6 +626,7 @@ __global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
   __shared__ uint32_t s_mask[kWindow];                           // the window's blocks: which tokens chose them
   __shared__ int s_id[kWindow + 2], s_page[kWindow + 2];         // the chosen ones
   __shared__ uint32_t s_who[kWindow + 2];
+  __shared__ __attribute__((aligned(16))) char s_keys[32 * Core::ROW];
 
   const lmop_attend_args& p = a.t;
   const int lane = threadIdx.x;
@@ -619,7 +644,7 @@ __global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
   const int t_last = (w.v0 + kWalkVectors - 1) / G < n_tok ? (w.v0 + kWalkVectors - 1) / G : n_tok - 1;
   const int lim0 = w.len - n_tok, lim_max = lim0 + t_last;
 
-  Core k(a, h);
+  Core k(a, h, s_keys);
   const int ps = k.ps, lps = k.lps;
   int lim[QS];
   uint32_t bit[QS];
@@ -671,8 +696,13 @@ __global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
 
       const int n_keys = ne << lps;
       auto load_keys = [&](int kb) {
-        const int at = kb + 16 * k.key_half(), page = s_page[at >> lps];
-        k.load_keys(page < 0 ? 0 : page, at & (ps - 1));
+        int page[2], slot[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = kb + 16 * i, q = __builtin_amdgcn_readfirstlane(s_page[at >> lps]);
+          page[i] = q < 0 ? 0 : q, slot[i] = at & (ps - 1);
+        }
+        k.load_keys(page, slot);
       };
       auto load_values = [&](int kb) {
         const int at = kb + 16 * k.value_half(), page = s_page[at >> lps];
@@ -684,8 +714,9 @@ __global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
       }
       for (int kb = 0; kb < n_keys; kb += 32) {
         f32x4 st[QS][2];
-        k.scores(st);
+        k.stash_keys();
         if (kb + 32 < n_keys) load_keys(kb + 32);
+        k.scores(st);
         const int at = kb + 16 * k.value_half(), e = at >> lps, slot = (at & (ps - 1)) + 8 * (k.g & 1);
         const bool gone = s_page[e] < 0;
         const uint32_t who = s_who[e];
