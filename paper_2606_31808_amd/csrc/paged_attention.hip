@@ -726,6 +726,10 @@ __global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
         for (int qs = 0; qs < QS; ++qs) {
           // of the lane's 8 keys, its vector sees the first `seen`
           const int seen = who & bit[qs] ? lim[qs] + 1 - index : 0;
+          if (!__any(seen > 0)) {  // a block that only the other 16 vectors chose
+            pb[qs] = x8{};
+            continue;
+          }
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf)
 #pragma unroll

@@ -5,10 +5,7 @@
 //
 // in fp64: products of 16-bit values and sums of a few hundred of them fit its 53 bits for ordinary
 // values, so scores are exact, and which blocks are chosen depends neither on the order
-// of a sum nor on what else is in the call.  A score becomes a 64-bit whole number with the
-// same order and stays in LDS; a wave finds the least one of the chosen eight bits at a time from
-// the counts of the values that remain, until those are as many as are wanted, and one pass in order
-// writes the chosen ones.
+// of a sum nor on what else is in the call.  Scores stay in LDS, and a wave picks the largest.
 //
 // Single tokens read each mean once, 16 bytes a lane, and are bound by that; tokens of one sequence are
 // taken 16 at a time, with the fp64 matrix instruction, and share the means.
@@ -19,19 +16,14 @@ namespace lmop {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
+constexpr int kTileWaves = 8;
 constexpr int kTileTokens = 16;
 constexpr int kScores = 16384;  // a workgroup holds at most (128 KB)
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
-// whole numbers in the order of the scores; NaN below all
-LMOP_DEVICE uint64_t order_of(double x) {
-  if (x != x) return 0;
-  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);  // (-0 is 0)
-  return (u >> 63) ? ~u : u | (1ull << 63);
-}
+// a score as it is ranked: NaN, and that of a page that does not exist, as the least
+LMOP_DEVICE double ranked(double x, int page) { return page < 0 || x != x ? -INFINITY : x; }
 
 // a wave's own LDS accesses happen in order; the compiler has to keep them so
 LMOP_DEVICE void wave_order() {
@@ -39,60 +31,163 @@ LMOP_DEVICE void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// By a whole wave: writes to out the `need` largest of key[0 .. n), 0 < need < n, of equal ones
-// the first, in ascending order of their index.  count: 256 words of LDS of the wave.
-LMOP_DEVICE void pick(const uint64_t* key, int n, int need, int* count, int32_t* out) {
+// The sum over a lane and those below it; the largest of all lanes.  (Lanes that a step does not reach add
+// `old`, or keep their own.)
+template <int CTRL, int ROWS>
+LMOP_DEVICE int dpp_rows(int old, int x) {
+  return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xF, false);
+}
+LMOP_DEVICE int scan(int x) {
+  x += dpp_rows<0x111, 0xF>(0, x);
+  x += dpp_rows<0x112, 0xF>(0, x);
+  x += dpp_rows<0x114, 0xF>(0, x);
+  x += dpp_rows<0x118, 0xF>(0, x);
+  x += dpp_rows<0x142, 0xA>(0, x);
+  x += dpp_rows<0x143, 0xC>(0, x);
+  return x;
+}
+LMOP_DEVICE float wave_max(float x) {
+  auto step = [&](int y) { x = fmaxf(x, __int_as_float(y)); };
+  step(dpp_rows<0x111, 0xF>(__float_as_int(x), __float_as_int(x)));
+  step(dpp_rows<0x112, 0xF>(__float_as_int(x), __float_as_int(x)));
+  step(dpp_rows<0x114, 0xF>(__float_as_int(x), __float_as_int(x)));
+  step(dpp_rows<0x118, 0xF>(__float_as_int(x), __float_as_int(x)));
+  step(dpp_rows<0x142, 0xA>(__float_as_int(x), __float_as_int(x)));
+  step(dpp_rows<0x143, 0xC>(__float_as_int(x), __float_as_int(x)));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
+// Of 256 counts, the value where those from above reach `want`, by the whole wave: the value, how many
+// are above it, its own count
+struct Cut {
+  int value, above, share;
+};
+LMOP_DEVICE Cut cut_at(const int* count, int want) {
   const int lane = threadIdx.x & 63;
+  // lane i: values 255 - 4 i and the three below
+  const int4 c4 = *(const int4*)(count + 252 - 4 * lane);
+  const int c[4] = {c4.w, c4.z, c4.y, c4.x};
+  int before = scan(c[0] + c[1] + c[2] + c[3]) - (c[0] + c[1] + c[2] + c[3]);
+  Cut r{-1, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (r.value < 0 && before < want && before + c[i] >= want) r = Cut{255 - 4 * lane - i, before, c[i]};
+    before += c[i];
+  }
+  const int who = __builtin_ctzll(__ballot(r.value >= 0));
+  return Cut{__builtin_amdgcn_readlane(r.value, who), __builtin_amdgcn_readlane(r.above, who),
+             __builtin_amdgcn_readlane(r.share, who)};
+}
+
+// whole numbers in the order of the scores
+LMOP_DEVICE uint64_t order_of(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);  // (-0 is 0)
+  return (u >> 63) ? ~u : u | (1ull << 63);
+}
+
+// By a whole wave: writes to out the `need` largest of score[0 .. n) (no NaN), 0 < need < n, of equal ones
+// the first, in ascending order of their index.  count: 256 words of LDS of the wave, 16-byte aligned.
+//
+// Scores are counted in 256 intervals between the least and the largest.  All above the one where the count
+// reaches `need` are chosen, and of those in it, if 64 or fewer, the ones with the lowest rank.  Else the
+// least of the chosen is found eight bits at a time.
+LMOP_DEVICE void pick(const double* score, int n, int need, int* count, int32_t* out) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = (1ull << lane) - 1;
+  // f(first index of 64, this lane's score, whether it is one) in ascending order; eight reads at a time
+  auto each = [&](auto&& f) {
+    for (int b0 = 0; b0 < n; b0 += 512) {
+      double x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int b = b0 + 64 * i + lane;
+        x[i] = score[b < n ? b : n - 1];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (b0 + 64 * i < n) f(b0 + 64 * i, x[i], b0 + 64 * i + lane < n);
+    }
+  };
+  auto clear = [&]() {
+    wave_order();
+    *(int4*)(count + 4 * lane) = int4{0, 0, 0, 0};
+    wave_order();
+  };
+  // classes of scores: above the cut, in it (of which the first `want` are chosen, or those in `marked`), below
+  int placed = 0, in_cut = 0;
+  auto write = [&](int b0, bool above, bool cut, int want, uint64_t marked) {
+    const uint64_t cuts = __ballot(cut);
+    const int nth = in_cut + __builtin_popcountll(cuts & below);
+    const bool take = above || (cut && nth < want && (nth >= 64 || (marked >> nth & 1)));
+    const uint64_t takes = __ballot(take);
+    if (take) out[placed + __builtin_popcountll(takes & below)] = b0 + lane;
+    placed += __builtin_popcountll(takes);
+    in_cut += __builtin_popcountll(cuts);
+  };
+
+  float hi = -INFINITY, lo = -INFINITY;  // lo: of the negated scores
+  each([&](int, double x, bool) { hi = fmaxf(hi, (float)x), lo = fmaxf(lo, -(float)x); });
+  hi = wave_max(hi), lo = -wave_max(lo);
+  const float per = 255.0f / (hi - lo);
+  if (hi - lo > 0.f && hi - lo < INFINITY && per < INFINITY) {
+    auto interval = [&](double x) {  // ascends with x
+      const int i = (int)(((float)x - lo) * per);
+      return i < 255 ? i : 255;
+    };
+    clear();
+    each([&](int, double x, bool is) {
+      if (is) atomicAdd(&count[interval(x)], 1);
+    });
+    wave_order();
+    const Cut cut = cut_at(count, need);
+    const int want = need - cut.above;
+    if (cut.share <= 64) {
+      uint64_t marked = ~0ull;
+      if (cut.share > want) {
+        // ranks of those in the interval, in the place of the counts
+        wave_order();
+        double* s = (double*)count;
+        int found = 0;
+        each([&](int, double x, bool is) {
+          const bool in = is && interval(x) == cut.value;
+          const uint64_t ins = __ballot(in);
+          if (in) s[found + __builtin_popcountll(ins & below)] = x;
+          found += __builtin_popcountll(ins);
+        });
+        wave_order();
+        const double mine = s[lane < cut.share ? lane : 0];
+        int rank = 0;
+        for (int i = 0; i < cut.share; ++i) rank += s[i] > mine || (s[i] == mine && i < lane);
+        marked = __ballot(lane < cut.share && rank < want);
+      }
+      each([&](int b0, double x, bool is) {
+        const int i = is ? interval(x) : -1;
+        write(b0, i > cut.value, i == cut.value, 64, marked);
+      });
+      return;
+    }
+  }
   // `at`: the leading bits (mask) that the least of the chosen has; `want`: how many are chosen of those that
   // share them
   uint64_t at = 0, mask = 0;
   int want = need;
   for (int shift = 56; shift >= 0; shift -= 8) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) count[64 * i + lane] = 0;
+    clear();
+    each([&](int, double x, bool is) {
+      const uint64_t k = order_of(x);
+      if (is && (k & mask) == at) atomicAdd(&count[(k >> shift) & 255], 1);
+    });
     wave_order();
-    for (int b = lane; b < n; b += 64) {
-      const uint64_t k = key[b];
-      if ((k & mask) == at) atomicAdd(&count[(k >> shift) & 255], 1);
-    }
-    wave_order();
-    // lane i: values 255 - 4 i and the three below
-    int c[4], sum = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = count[255 - 4 * lane - i], sum += c[i];
-    int before = sum;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-      const int o = __shfl_up(before, m, 64);
-      if (lane >= m) before += o;
-    }
-    before -= sum;
-    // the value where the counts from above reach `want`: in one lane
-    int value = -1, above = 0, share = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (value < 0 && before < want && before + c[i] >= want) value = 255 - 4 * lane - i, above = before, share = c[i];
-      before += c[i];
-    }
-    const int who = __builtin_ctzll(__ballot(value >= 0));
-    at |= (uint64_t)(uint32_t)__shfl(value, who, 64) << shift;
+    const Cut cut = cut_at(count, want);
+    at |= (uint64_t)(uint32_t)cut.value << shift;
     mask |= 255ull << shift;
-    want -= __shfl(above, who, 64);
-    if (__shfl(share, who, 64) == want) break;  // all that share the leading bits
+    want -= cut.above;
+    if (cut.share == want) break;  // all that share the leading bits
   }
-  // above `at`: chosen; sharing its bits: the first `want`
-  int placed = 0, equal = 0;
-  for (int b0 = 0; b0 < n && placed < need; b0 += 64) {
-    const int b = b0 + lane;
-    const uint64_t k = b < n ? key[b] & mask : 0;
-    const bool eq = b < n && k == at;
-    const uint64_t eqs = __ballot(eq), below = (1ull << lane) - 1;
-    const bool take = b < n && (k > at || (eq && equal + __builtin_popcountll(eqs & below) < want));
-    const uint64_t takes = __ballot(take);
-    if (take) out[placed + __builtin_popcountll(takes & below)] = b;
-    placed += __builtin_popcountll(takes);
-    equal += __builtin_popcountll(eqs);
-  }
+  each([&](int b0, double x, bool is) {
+    const uint64_t k = is ? order_of(x) & mask : 0;
+    write(b0, is && k > at, is && k == at, want, ~0ull);
+  });
 }
 
 // What is chosen without scores: *done, or `mine` blocks before the token's own of which `need` are
@@ -118,14 +213,15 @@ LMOP_DEVICE Choice settle(const lmop_select_args& p, int64_t index, int len, int
 }
 
 // One workgroup: a token and a kv head.
-template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void select_one_kernel(const lmop_select_args p, const Heads n) {
+template <typename T, int HD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void select_one_kernel(const lmop_select_args p, const Heads n) {
+  constexpr int kThreads = 64 * WAVES;
   constexpr int LANES = HD / 8;             // of a mean
   constexpr int PAGES = kThreads / LANES;   // of a pass
   constexpr int UNROLL = 8;                 // passes whose loads are under way together
   __shared__ double s_q[HD];
-  __shared__ int s_count[256];
-  extern __shared__ __attribute__((aligned(16))) uint64_t s_key[];
+  __shared__ __attribute__((aligned(16))) int s_count[256];
+  extern __shared__ __attribute__((aligned(16))) double s_score[];
   const lmop_batch& bt = p.batch;
   const int tid = threadIdx.x;
   const int t = blockIdx.x / n.nkv, h = blockIdx.x % n.nkv;
@@ -146,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void select_one_kernel(const lmop_select_
     s_q[tid] = sum;
   }
   // the pages, in place of the scores that they become
-  for (int b = tid; b < c.mine; b += kThreads) s_key[b] = (uint64_t)(int64_t)page_of(bt, p.cache.n_pages, s, b);
+  for (int b = tid; b < c.mine; b += kThreads) s_score[b] = page_of(bt, p.cache.n_pages, s, b);
   __syncthreads();
   const int d = tid % LANES * 8;
   double q[8];
@@ -159,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void select_one_kernel(const lmop_select_
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
       const int b = b0 + u * PAGES;
-      page[u] = b < c.mine ? (int)s_key[b] : -1;
+      page[u] = b < c.mine ? (int)s_score[b] : -1;
       x[u] = *(const typename Half<T>::x8*)(mean + (size_t)(page[u] < 0 ? 0 : page[u]) * n.nkv * HD);
     }
 #pragma unroll
@@ -170,22 +266,22 @@ __global__ __launch_bounds__(kThreads) void select_one_kernel(const lmop_select_
 #pragma unroll
       for (int m = 1; m < LANES; m *= 2) z += __shfl_xor(z, m, 64);
       const int b = b0 + u * PAGES;
-      if (d == 0 && b < c.mine) s_key[b] = page[u] >= 0 ? order_of(z) : 0;
+      if (d == 0 && b < c.mine) s_score[b] = ranked(z, page[u]);
     }
   }
   __syncthreads();
-  if (tid < 64) pick(s_key, c.mine, c.need, s_count, out);
+  if (tid < 64) pick(s_score, c.mine, c.need, s_count, out);
 }
 
 // One workgroup: up to 16 tokens of a sequence (a.tile) and a kv head.  Scores are a product of the
 // tokens' queries and 16 means at a time: lane 16 g + c has token c's dimensions g * HD / 4 .. as the
 // one operand and page c's as the other, and gets tokens 4 r + g of page c.
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void select_tile_kernel(const lmop_select_args p, const Heads n, int tile,
+__global__ __launch_bounds__(64 * kTileWaves) void select_tile_kernel(const lmop_select_args p, const Heads n, int tile,
                                                                int pages) {
   constexpr int DIMS = HD / 4;
-  __shared__ int s_count[kWaves][256];
-  extern __shared__ __attribute__((aligned(16))) uint64_t s_key[];  // [tile][pages]
+  __shared__ __attribute__((aligned(16))) int s_count[kTileWaves][256];
+  extern __shared__ __attribute__((aligned(16))) double s_score[];  // [tile][pages]
   const lmop_batch& bt = p.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15;
@@ -224,13 +320,24 @@ __global__ __launch_bounds__(kThreads) void select_tile_kernel(const lmop_select
     for (int i = 0; i < DIMS; ++i) q[i] = sum[i];
   }
   const T* mean = (const T*)p.cache.k_mean + h * HD + g * DIMS;
-  for (int b0 = wave * 16; b0 < most; b0 += 16 * kWaves) {
-    const int b = b0 + c;
-    const int page = b < most ? page_of(bt, p.cache.n_pages, s, b) : -1;
+  typedef typename Half<T>::x8 x8;
+  // the next 16 means are on their way while these are multiplied, and their pages before that
+  auto look_up = [&](int b0) { return b0 + c < most ? page_of(bt, p.cache.n_pages, s, b0 + c) : -1; };
+  auto load = [&](int page, x8 (&x)[DIMS / 8]) {
     const T* src = mean + (size_t)(page < 0 ? 0 : page) * n.nkv * HD;
-    typename Half<T>::x8 x[DIMS / 8];
 #pragma unroll
-    for (int i = 0; i < DIMS / 8; ++i) x[i] = *(const typename Half<T>::x8*)(src + 8 * i);
+    for (int i = 0; i < DIMS / 8; ++i) x[i] = *(const x8*)(src + 8 * i);
+  };
+  constexpr int STEP = 16 * kTileWaves;
+  x8 next[DIMS / 8];
+  int page = look_up(wave * 16), next_page = look_up(wave * 16 + STEP);
+  load(page, next);
+  for (int b0 = wave * 16; b0 < most; b0 += STEP) {
+    x8 x[DIMS / 8];
+#pragma unroll
+    for (int i = 0; i < DIMS / 8; ++i) x[i] = next[i];
+    load(next_page, next);
+    const int after = look_up(b0 + 2 * STEP);
     f64x4 z = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < DIMS; ++i)
@@ -238,14 +345,15 @@ __global__ __launch_bounds__(kThreads) void select_tile_kernel(const lmop_select
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int t = 4 * r + g;
-      if (t < nt && b < most) s_key[(size_t)t * pages + b] = page >= 0 ? order_of(z[r]) : 0;
+      if (t < nt && b0 + c < most) s_score[(size_t)t * pages + b0 + c] = ranked(z[r], page);
     }
+    page = next_page, next_page = after;
   }
   __syncthreads();
-  for (int t = wave; t < nt; t += kWaves) {
+  for (int t = wave; t < nt; t += kTileWaves) {
     int32_t* out = p.blocks + ((size_t)(t0 + t) * n.nkv + h) * p.n_blocks;
     const Choice ch = settle(p, index0 + t, len, out);
-    if (!ch.done) pick(s_key + (size_t)t * pages, ch.mine, ch.need, s_count[wave], out);
+    if (!ch.done) pick(s_score + (size_t)t * pages, ch.mine, ch.need, s_count[wave], out);
   }
 }
 
@@ -267,14 +375,16 @@ hipError_t launch(hipStream_t s, const lmop_select_args& a, const Heads& n) {
     const int lds = (int)(tile * pages * 8);
     const hipError_t e = allow_lds(select_tile_kernel<T, HD>, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((select_tile_kernel<T, HD>), dim3((unsigned)(items * n.nkv)), dim3(kThreads), lds, s, a, n,
+    hipLaunchKernelGGL((select_tile_kernel<T, HD>), dim3((unsigned)(items * n.nkv)), dim3(64 * kTileWaves), lds, s, a, n,
                        tile, (int)pages);
   } else {
     const int lds = (int)(pages * 8);
-    const hipError_t e = allow_lds(select_one_kernel<T, HD>, lds);
+    // enough waves for all means to be on their way at once
+    const bool many = pages > 4 * 64 / (HD / 8) * 8;
+    const auto kernel = many ? select_one_kernel<T, HD, 16> : select_one_kernel<T, HD, 4>;
+    const hipError_t e = allow_lds(kernel, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((select_one_kernel<T, HD>), dim3((unsigned)((int64_t)b.n_tokens * n.nkv)), dim3(kThreads),
-                       lds, s, a, n);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)b.n_tokens * n.nkv)), dim3(64 * (many ? 16 : 4)), lds, s, a, n);
   }
   return hipGetLastError();
 }
