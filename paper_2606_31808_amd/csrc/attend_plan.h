@@ -35,10 +35,11 @@ struct AttendPlan {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Divides `steps` among at most `want` splits of at least `least` steps and at most `most`.
-inline void split_steps(AttendLaunch& l, int64_t steps, int64_t want, int64_t least, int64_t most) {
+// Divides `steps` among at most `want` splits of at least `least` steps and at most `most`; up to `whole`
+// steps stay together if `most` allows it.
+inline void split_steps(AttendLaunch& l, int64_t steps, int64_t want, int64_t least, int64_t most, int64_t whole = 0) {
   if (steps < 1) steps = 1;
-  int64_t n = steps / least;
+  int64_t n = steps <= whole ? 1 : steps / least;
   if (n > want) n = want;
   if (n < 1) n = 1;
   int64_t chunk = ceil_div(steps, n);
@@ -59,7 +60,9 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
   const int64_t vectors = (int64_t)s.max_tokens * group;
   const int64_t pages = ceil_div(s.max_length, s.page_size);
   const int64_t prefix_pages = ceil_div(s.prefix_length, s.page_size);
-  const int64_t few_least = ceil_div(256, s.page_size);
+  // Joining parts takes a second launch and some 4 us, in which a few-vector workgroup walks 512 keys (1024
+  // keys for each of 256 workgroups: 42 us whole, 50 in two parts, with the choice of blocks before it)
+  const int64_t few_least = ceil_div(512, s.page_size), few_whole = ceil_div(1024, s.page_size);
   // tiles of `of` vectors: as many as the sequences need, found from the starts, or max_tokens' for each
   auto tiles = [&](AttendLaunch& l, int of) {
     const int64_t each = ceil_div(vectors, of);
@@ -77,7 +80,7 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     p.own.few = true;
     p.own.per_seq = (int)ceil_div(group, kFewVectors);  // of a token here
     p.own.tiles = s.n_tokens * p.own.per_seq;
-    split_steps(p.own, s.n_blocks, kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries);
+    split_steps(p.own, s.n_blocks, kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries, few_whole);
     p.parts = p.own.splits > 1 ? p.own.splits : 0;
     return p;
   }
@@ -87,7 +90,7 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     p.own.per_seq = (int)ceil_div(vectors, kFewVectors);
     p.own.tiles = s.n_seqs * p.own.per_seq;
     split_steps(p.own, pages + (separate ? 0 : prefix_pages),
-                kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries);
+                kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries, few_whole);
   } else {
     tiles(p.own, kTileVectors);
     split_steps(p.own, ceil_div(s.max_length, kTileKeys) + ceil_div(s.prefix_length, kTileKeys),
@@ -98,7 +101,7 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     p.prefix.few = all <= 2 * kFewVectors;
     p.prefix.tiles = (int)ceil_div(all, p.prefix.few ? kFewVectors : kTileVectors);
     if (p.prefix.few)
-      split_steps(p.prefix, prefix_pages, kFewFill / ((int64_t)p.prefix.tiles * s.nkv), few_least, kMaxEntries);
+      split_steps(p.prefix, prefix_pages, kFewFill / ((int64_t)p.prefix.tiles * s.nkv), few_least, kMaxEntries, few_whole);
     else
       split_steps(p.prefix, ceil_div(s.prefix_length, kTileKeys), kTileFill / ((int64_t)p.prefix.tiles * s.nkv),
                   4, 1 << 30);

@@ -659,6 +659,9 @@ def lmop_qk_norm_rope(ctx, heads, n_tokens, q=None, k=None, v=None, pos=None, q_
         _check(st, ctx)
 
 
+_PACK_BATCH = _PACK["batch"]
+
+
 class PagedCache:
     """Keys and values in pages, on the caller's tensors: k and v [n_pages, n_kv_heads, page_size,
     head_dim] (float16, bfloat16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages, n_kv_heads,
@@ -706,10 +709,14 @@ def _batch(ctx_heads, cache, table, length, start, n_tokens, dtype, dev):
         raise ValueError(f"tokens of {dtype}, the cache is for {cache.token_dtype}")
     n_seqs, pages = table.shape
     ld = _ld(table, "table", n_seqs, pages, _I32, dev)
-    if start is None and n_tokens != n_seqs:
+    if start is not None:
+        ps = _vec(start, "start", n_seqs + 1, torch.int32, dev)
+    elif n_tokens == n_seqs:
+        ps = 0
+    else:
         raise ValueError(f"{n_tokens} tokens of {n_seqs} sequences need start")
-    return _PACK["batch"](table.data_ptr(), _vec(length, "length", n_seqs, torch.int32, dev),
-                          _vec(start, "start", n_seqs + 1, torch.int32, dev), ld, pages, n_seqs, n_tokens)
+    return _PACK_BATCH(table.data_ptr(), _vec(length, "length", n_seqs, torch.int32, dev), ps, ld, pages, n_seqs,
+                       n_tokens)
 
 
 def lmop_cache_append(ctx, heads, cache, k, v, table, length, start=None, first: int = 0, rotate: bool = True,
@@ -949,7 +956,7 @@ class Context:
         (q_out, or a new tensor; None without q)."""
         self._here(k)
         if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         lmop_cache_append(self.ctx, self.heads, cache, k, v, table, length, start, first, rotate, q, q_out)
         return q_out
 
@@ -963,7 +970,7 @@ class Context:
         [n, n_heads] to write the logarithm of the sum of exponentials into."""
         self._here(q)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if max_tokens is None:
             max_tokens = 1 if start is None else q.shape[0]
         if max_length is None:
@@ -977,7 +984,7 @@ class Context:
         those before it whose mean key scores highest, ascending, then -1."""
         self._here(q)
         if out is None:
-            out = torch.empty((q.shape[0], self.heads[1], n_blocks), dtype=torch.int32, device=q.device)
+            out = q.new_empty((q.shape[0], self.heads[1], n_blocks), dtype=torch.int32)
         if max_length is None:
             max_length = table.shape[1] * cache.page_size
         lmop_select_blocks(self.ctx, self.heads, cache, q, out, table, length, start, max_length)
