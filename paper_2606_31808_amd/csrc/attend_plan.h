@@ -23,6 +23,7 @@ struct AttendSizes {
 // steps (few-vector kernel: pages; tile kernel: kTileKeys keys) from z * chunk on.
 struct AttendLaunch {
   bool few = false;
+  int waves = 4;      // few-vector kernel: 1, 4 or 8 of a workgroup
   int tiles = 0, splits = 1, chunk = 1;
   int per_seq = 0;  // tiles of a sequence, or 0: as many as it needs, found from the starts
 };
@@ -50,6 +51,15 @@ inline void split_steps(AttendLaunch& l, int64_t steps, int64_t want, int64_t le
 
 // workgroups that fill the chip
 constexpr int kFewFill = 1024, kTileFill = 512, kWalkFill = 2048;
+
+// Waves of a few-vector workgroup.  Where there are workgroups for less than half the CUs, eight: more of
+// their keys are on their way at once (573 keys of one row 8.8 -> 7.9 us).  Where there are two waves for
+// every SIMD without a second one in a workgroup, and few keys each, one: nothing is joined (256 rows
+// of up to 112 keys 22 -> 9 us).  The other part of a launch has four.
+inline void pick_waves(AttendLaunch& l, const AttendSizes& s, bool pair) {
+  const int64_t workgroups = (int64_t)l.tiles * s.nkv * l.splits, keys = (int64_t)l.chunk * s.page_size;
+  l.waves = workgroups >= 2048 && keys <= 512 ? 1 : workgroups <= 128 && !pair ? 8 : 4;
+}
 
 // chosen blocks: vectors of a sequence from which waves walk the blocks of several tokens
 constexpr int kWalkLeast = 64;
@@ -81,6 +91,7 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     p.own.per_seq = (int)ceil_div(group, kFewVectors);  // of a token here
     p.own.tiles = s.n_tokens * p.own.per_seq;
     split_steps(p.own, s.n_blocks, kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries, few_whole);
+    pick_waves(p.own, s, false);
     p.parts = p.own.splits > 1 ? p.own.splits : 0;
     return p;
   }
@@ -91,6 +102,7 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     p.own.tiles = s.n_seqs * p.own.per_seq;
     split_steps(p.own, pages + (separate ? 0 : prefix_pages),
                 kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries, few_whole);
+    pick_waves(p.own, s, separate);
   } else {
     tiles(p.own, kTileVectors);
     split_steps(p.own, ceil_div(s.max_length, kTileKeys) + ceil_div(s.prefix_length, kTileKeys),

@@ -1731,12 +1731,13 @@ lmop_status check_attend_sizes(lmop_ctx* c, const lmop_attend_args& a, bool* emp
   const AttendSizes s = attend_sizes(c, a);
   if (((uint64_t)s.n_tokens + s.n_seqs) * s.nq > kMaxTasks / 64)
     return fail(c, LMOP_ERR_UNSUPPORTED, "%d tokens of %d sequences are too many for one call", s.n_tokens, s.n_seqs);
-  // fewer than 2^32 threads a launch, at most 65535 splits
+  // fewer than 2^32 threads a launch (that of both parts, too), at most 65535 splits
   const AttendPlan p = plan_attend(s);
-  for (const AttendLaunch& l : {p.own, p.prefix})
-    if (l.splits > 65535 || (uint64_t)l.tiles * s.nkv * l.splits >= kMaxTasks / 64)
-      return fail(c, LMOP_ERR_UNSUPPORTED, "%d tokens over %d keys (%d blocks) behind %d are too many for one call",
-                  s.n_tokens, s.max_length, s.n_blocks, s.prefix_length);
+  uint64_t workgroups = 0;
+  for (const AttendLaunch& l : {p.own, p.prefix}) workgroups += (uint64_t)l.tiles * s.nkv * l.splits;
+  if (p.own.splits > 65535 || workgroups >= kMaxTasks / 64)
+    return fail(c, LMOP_ERR_UNSUPPORTED, "%d tokens over %d keys (%d blocks) behind %d are too many for one call",
+                s.n_tokens, s.max_length, s.n_blocks, s.prefix_length);
   return LMOP_OK;
 }
 

@@ -388,25 +388,42 @@ struct WaveCore {
 };
 
 // One workgroup: 16 vectors x a kv head x a split.  Its pages are looked up once, into LDS; wave
-// w takes the 32-key chunks w, w + 4, ...; the four waves' states are joined through LDS at the
+// w takes the 32-key chunks w, w + WAVES, ...; the waves' states are joined through LDS at the
 // end.
-template <typename T, bool E8, int HD, bool BLOCKS>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
+template <typename T, bool E8, int HD, int WAVES>
+struct FewLds {
+  typedef WaveCore<T, E8, HD, 1> Core;
+  static constexpr int ORow = HD + 4;  // of the joined outputs
+  static constexpr int KEYS = 32 * Core::ROW, OUTS = 16 * ORow * 4;
+  union {  // the waves' keys, and in their place at the end their outputs
+    char keys[WAVES][KEYS];
+    float o[WAVES][16][ORow];
+  };
+  float ml[WAVES][2][16];
+  int page[kMaxEntries + 4], first[kMaxEntries + 4], cap[kMaxEntries + 4];
+};
+
+template <typename T, bool E8, int HD, bool BLOCKS, int WAVES>
+LMOP_DEVICE void few_vectors(const Args& a, int block, int split, FewLds<T, E8, HD, WAVES>& lds) {
   typedef WaveCore<T, E8, HD, 1> Core;
   typedef typename Core::x8 x8;
   constexpr int NT = Core::NT;
-  constexpr int ORow = HD + 4;  // of the joined outputs in LDS
-  // the waves' keys, and in their place at the end their outputs
-  constexpr int KEYS = 32 * Core::ROW, OUTS = 16 * ORow * 4;
-  __shared__ __attribute__((aligned(16))) char s_mem[kFewWaves * (KEYS > OUTS ? KEYS : OUTS)];
-  float(*s_o)[16][ORow] = (float(*)[16][ORow])s_mem;
-  __shared__ int e_page[kMaxEntries + 16], e_first[kMaxEntries + 16], e_cap[kMaxEntries + 16];
-  __shared__ float s_ml[kFewWaves][2][16];
-
+  auto& s_o = lds.o;
+  auto& s_ml = lds.ml;
+  int *e_page = lds.page, *e_first = lds.first, *e_cap = lds.cap;
   const lmop_attend_args& p = a.t;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tile = blockIdx.x / a.n.nkv, h = blockIdx.x % a.n.nkv, split = blockIdx.y;
+  const int lane = threadIdx.x & 63, tid = WAVES == 1 ? lane : threadIdx.x;
+  const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  // what the waves have written is there for all of them
+  auto meet = [&]() {
+    if constexpr (WAVES == 1) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    } else {
+      __syncthreads();
+    }
+  };
+  const int tile = block / a.n.nkv, h = block % a.n.nkv;
   const int G = a.n.nq / a.n.nkv;
   const int part = a.part0 + split;
 
@@ -433,14 +450,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   if (w.bad) {
     // a workgroup of the sequence's first tile does all of its tokens: there may be more than max_tokens
     if (w.v0 == 0)
-      for (int v = wave; v < nv; v += kFewWaves)
+      for (int v = wave; v < nv; v += WAVES)
         write_bad<T>(a, w.tok.x + v / G, h * G + v % G, part, lane, 64);
     return;
   }
   if (w.v0 >= nv) return;
 
   // the keys that the tile's vectors see, and the pages that hold them
-  Core k(a, h, s_mem + wave * KEYS);
+  Core k(a, h, lds.keys[wave]);
   const int ps = k.ps, lps = k.lps;
   const int n_tok = w.tok.y - w.tok.x;
   const int t_first = w.v0 / G;
@@ -456,12 +473,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   const int32_t* list = BLOCKS ? p.blocks + ((size_t)w.tok.x * a.n.nkv + h) * p.n_blocks : nullptr;
   bool ascending = true;
   if constexpr (BLOCKS) {
-    for (int i = tid + 1; i < p.n_blocks; i += 64 * kFewWaves)
+    for (int i = tid + 1; i < p.n_blocks; i += 64 * WAVES)
       ascending = ascending && (list[i] < 0 || (list[i - 1] >= 0 && list[i] > list[i - 1]));
-    ascending = !__syncthreads_or(!ascending);
+    if constexpr (WAVES == 1)
+      ascending = __all(ascending);
+    else
+      ascending = !__syncthreads_or(!ascending);
   }
   // (one entry more: of 16-token pages, an odd number of them ends inside a chunk)
-  for (int i = tid; i <= ne; i += 64 * kFewWaves) {
+  for (int i = tid; i <= ne; i += 64 * WAVES) {
     int page = 0, first = 0, cap = 0;
     if (i < ne) {
       const int e = (int)from + i;
@@ -497,7 +517,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   const int lim = a.flat ? 0 : w.len - n_tok + tok, lim_any = a.flat ? 0 : lim_max;
   const bool one = t_first == t_last || a.flat;  // all vectors see the same keys
   k.load_query(0, v < nv ? (const T*)p.q + (int64_t)(w.tok.x + tok) * p.ldq + (h * G + v - tok * G) * HD : nullptr);
-  __syncthreads();
+  meet();
 
   const float thr = 8.0f / a.c;
   const int n_keys = ne << lps;
@@ -514,7 +534,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
     const int at = kb + 16 * k.value_half(), page = e_page[at >> lps];
     k.load_values(page < 0 ? 0 : page, at & (ps - 1));
   };
-  constexpr int STEP = 32 * kFewWaves;
+  constexpr int STEP = 32 * WAVES;
   if (wave * 32 < n_keys) {
     load_keys(wave * 32);
     load_values(wave * 32);
@@ -557,10 +577,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
   // join the waves
   const int g = k.g, c = k.c;
   if (g == 0) s_ml[wave][0][c] = k.m[0], s_ml[wave][1][c] = k.l4[0][0];
-  __syncthreads();
+  meet();
   float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kFewWaves; ++i) top = fmaxf(top, s_ml[i][0][c]);
+  for (int i = 0; i < WAVES; ++i) top = fmaxf(top, s_ml[i][0][c]);
   const float f = rescale(k.m[0], top, a.c);
 #pragma unroll
   for (int r = 0; r < 4; ++r)
@@ -569,43 +589,43 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_kernel(const Args a) {
       const f32x4 y = {k.o[0][i][r] * f, k.o[0][i + 1][r] * f, k.o[0][i + 2][r] * f, k.o[0][i + 3][r] * f};
       *(f32x4*)&s_o[wave][c][NT * (4 * g + r) + i] = y;
     }
-  __syncthreads();
-  // thread: vector tid / 16, NT dimensions
-  const int vo = tid >> 4, d = (tid & 15) * NT;
-  if (w.v0 + vo >= nv) return;
-  const int to = (w.v0 + vo) / G, ho = h * G + (w.v0 + vo) % G;
-  float mt = -INFINITY, lt = 0.f;
+  meet();
+  // 16 lanes a vector, NT dimensions each
+  for (int vo = tid >> 4; vo < kFewVectors && w.v0 + vo < nv; vo += 4 * WAVES) {
+    const int d = (tid & 15) * NT;
+    const int t = w.tok.x + (w.v0 + vo) / G, ho = h * G + (w.v0 + vo) % G;
+    float mt = -INFINITY, lt = 0.f;
 #pragma unroll
-  for (int i = 0; i < kFewWaves; ++i) mt = fmaxf(mt, s_ml[i][0][vo]);
-  float y[NT];
+    for (int i = 0; i < WAVES; ++i) mt = fmaxf(mt, s_ml[i][0][vo]);
+    float y[NT];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) y[i] = 0.f;
+    for (int i = 0; i < NT; ++i) y[i] = 0.f;
 #pragma unroll
-  for (int q = 0; q < kFewWaves; ++q) {
-    const float lq = s_ml[q][1][vo];
-    lt += lq != lq ? lq : lq * rescale(s_ml[q][0][vo], mt, a.c);
+    for (int q = 0; q < WAVES; ++q) {
+      const float lq = s_ml[q][1][vo];
+      lt += lq != lq ? lq : lq * rescale(s_ml[q][0][vo], mt, a.c);
 #pragma unroll
-    for (int i = 0; i < NT; i += 4) {
-      const f32x4 x = *(const f32x4*)&s_o[q][vo][d + i];
+      for (int i = 0; i < NT; i += 4) {
+        const f32x4 x = *(const f32x4*)&s_o[q][vo][d + i];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[i + r] += x[r];
+        for (int r = 0; r < 4; ++r) y[i + r] += x[r];
+      }
     }
-  }
-  const int t = w.tok.x + to;
-  if (a.parts) {
-    float* dst = part_o(a, part, t, ho) + d;
+    if (a.parts) {
+      float* dst = part_o(a, part, t, ho) + d;
 #pragma unroll
-    for (int i = 0; i < NT; i += 4) *(f32x4*)(dst + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
-    if (d == 0) *part_ml(a, part, t, ho) = float2{mt, lt};
-    return;
-  }
-  const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-  typedef T xo __attribute__((ext_vector_type(NT), aligned(2)));
-  xo r;
+      for (int i = 0; i < NT; i += 4) *(f32x4*)(dst + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+      if (d == 0) *part_ml(a, part, t, ho) = float2{mt, lt};
+      continue;
+    }
+    const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+    typedef T xo __attribute__((ext_vector_type(NT), aligned(2)));
+    xo r;
 #pragma unroll
-  for (int i = 0; i < NT; ++i) r[i] = (T)(lt == 0.f ? 0.f : y[i] * inv);
-  *(xo*)((T*)p.out + t * p.ldo + ho * HD + d) = r;
-  if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + ho] = lse_of(a, mt, lt);
+    for (int i = 0; i < NT; ++i) r[i] = (T)(lt == 0.f ? 0.f : y[i] * inv);
+    *(xo*)((T*)p.out + t * p.ldo + ho * HD + d) = r;
+    if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + ho] = lse_of(a, mt, lt);
+  }
 }
 
 // Chosen blocks of neighbouring tokens: a wave, alone, takes 32 vectors (8 tokens of 4 heads) and walks
@@ -1097,18 +1117,17 @@ LMOP_DEVICE void write_bad_tile(const Args& a, const Tile& w, int nv, int h, int
 
 // A split of the keys: the prefix's, then the sequence's own up to the tile's last token
 template <typename T, bool E8, int HD>
-__global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) {
+LMOP_DEVICE void tile_vectors(const Args& a, int block, int split, char* smem) {
   typedef TileCore<T, E8, HD> Core;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
   __shared__ uint32_t s_odd[2][2];  // by block parity: keys with infinities or NaN among their values
 
   const lmop_attend_args& p = a.t;
-  const int h = blockIdx.x % a.n.nkv, split = blockIdx.y;
+  const int h = block % a.n.nkv;
   const int G = a.n.nq / a.n.nkv;
   const int ps = p.cache.page_size, lps = __builtin_ctz(ps);
   const int part = a.part0 + split;
   // later tiles of a prompt see more keys: they go first
-  const Tile w = find_tile(a, a.l.tiles - 1 - (int)blockIdx.x / a.n.nkv, kTileVectors);
+  const Tile w = find_tile(a, a.l.tiles - 1 - block / a.n.nkv, kTileVectors);
   const Span sp(w, G);
   if (w.v0 >= sp.nv) return;
   if (w.bad) return write_bad_tile<T>(a, w, sp.nv, h, part);
@@ -1270,30 +1289,63 @@ __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
   if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + h] = lse_of(a, m, l);
 }
 
+// ---------------------------------------------------------------- kernels
+// (with 8-bit pages three waves fit a SIMD, which reads faster: 32 contexts of up to 32,000 tokens 222 us,
+// of two 262)
+template <typename T, bool E8, int HD, bool BLOCKS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, E8 && WAVES == 4 ? 3 : 2) void few_kernel(const Args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  few_vectors<T, E8, HD, BLOCKS, WAVES>(a, blockIdx.x, blockIdx.y, *(FewLds<T, E8, HD, WAVES>*)smem);
+}
+
 template <typename T, bool E8, int HD>
-hipError_t launch_one(hipStream_t s, const Args& a) {
-  const dim3 grid(a.n.nkv * a.l.tiles, a.l.splits);
-  if (a.t.blocks && !a.l.few) {
-    hipLaunchKernelGGL((walk_kernel<T, E8, HD>), grid, dim3(64), 0, s, a);
-  } else if (a.l.few) {
-    if (a.t.blocks)
-      hipLaunchKernelGGL((few_kernel<T, E8, HD, true>), grid, dim3(64 * kFewWaves), 0, s, a);
+__global__ __launch_bounds__(64 * kTileWaves, 2) void tile_kernel(const Args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  tile_vectors<T, E8, HD>(a, blockIdx.x, blockIdx.y, smem);
+}
+
+// Both launches of a batch behind a prefix at once: the prefix's workgroups, which take longer, first.  With
+// SINGLE the own part's waves have sequences of their own.
+template <typename T, bool E8, int HD, bool FEW, bool SINGLE>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void pair_kernel(const Args prefix, const Args own) {
+  static_assert(kTileWaves == kFewWaves, "one size of workgroup");
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int each = prefix.l.tiles * prefix.n.nkv, first = each * prefix.l.splits;
+  const int block = blockIdx.x;
+  if (block < first) {
+    if constexpr (FEW)
+      few_vectors<T, E8, HD, false, kFewWaves>(prefix, block % each, block / each,
+                                               *(FewLds<T, E8, HD, kFewWaves>*)smem);
     else
-      hipLaunchKernelGGL((few_kernel<T, E8, HD, false>), grid, dim3(64 * kFewWaves), 0, s, a);
+      tile_vectors<T, E8, HD>(prefix, block % each, block / each, smem);
   } else {
-    constexpr int lds = 2 * TileCore<T, E8, HD>::STAGE;
-    const auto kernel = tile_kernel<T, E8, HD>;
-    if constexpr (lds > 32768) {  // more than HIP allows unasked, with what the kernels have of their own
-      const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (e != hipSuccess) return e;
+    const int per = own.l.tiles * own.n.nkv;
+    if constexpr (SINGLE) {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const int b = (block - first) * kFewWaves + wave;
+      if (b < per * own.l.splits)
+        few_vectors<T, E8, HD, false, 1>(own, b % per, b / per, ((FewLds<T, E8, HD, 1>*)smem)[wave]);
+    } else {
+      few_vectors<T, E8, HD, false, kFewWaves>(own, (block - first) % per, (block - first) / per,
+                                               *(FewLds<T, E8, HD, kFewWaves>*)smem);
     }
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * kTileWaves), lds, s, a);
   }
-  return hipGetLastError();
+}
+
+template <typename K>
+hipError_t allow_lds(K kernel, int lds) {
+  if (lds <= 32768) return hipSuccess;  // else more than HIP allows unasked, with what a kernel has of its own
+  return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
 }
 
 template <typename T, bool E8, int HD>
 hipError_t launch(hipStream_t s, const lmop_attend_args& t, const Heads& n, const AttendPlan& plan) {
+  constexpr int tile_lds = 2 * TileCore<T, E8, HD>::STAGE;
+  constexpr auto few_lds = [](int waves) {
+    return (int)(waves == 1   ? sizeof(FewLds<T, E8, HD, 1>)
+                 : waves == 4 ? sizeof(FewLds<T, E8, HD, 4>)
+                              : sizeof(FewLds<T, E8, HD, 8>));
+  };
   Args a{};
   a.t = t;
   a.n = n;
@@ -1301,18 +1353,46 @@ hipError_t launch(hipStream_t s, const lmop_attend_args& t, const Heads& n, cons
   a.parts = plan.parts;
   a.l = plan.own;
   a.fused = plan.prefix.tiles == 0 && t.prefix_length > 0;
-  hipError_t e = launch_one<T, E8, HD>(s, a);
-  if (e != hipSuccess) return e;
+  const dim3 grid(n.nkv * a.l.tiles, a.l.splits);
+  auto queue = [&](auto kernel, int threads, int lds) {
+    const hipError_t e = allow_lds(kernel, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, a);
+    return hipGetLastError();
+  };
+  hipError_t e;
   if (plan.prefix.tiles > 0) {
     Args q = a;
     q.l = plan.prefix;
     q.flat = 1;
-    q.fused = 0;
     q.part0 = plan.own.splits;
-    e = launch_one<T, E8, HD>(s, q);
+    const bool single = a.l.waves == 1;
+    const auto kernel = q.l.few ? (single ? pair_kernel<T, E8, HD, true, true> : pair_kernel<T, E8, HD, true, false>)
+                                : (single ? pair_kernel<T, E8, HD, false, true> : pair_kernel<T, E8, HD, false, false>);
+    int lds = single ? kFewWaves * few_lds(1) : few_lds(kFewWaves);
+    const int other = q.l.few ? few_lds(kFewWaves) : tile_lds;
+    lds = lds > other ? lds : other;
+    e = allow_lds(kernel, lds);
     if (e != hipSuccess) return e;
+    const unsigned own = (unsigned)n.nkv * a.l.tiles * a.l.splits;
+    const unsigned blocks = (unsigned)n.nkv * q.l.tiles * q.l.splits + (single ? (own + kFewWaves - 1) / kFewWaves : own);
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * kTileWaves), lds, s, q, a);
+    e = hipGetLastError();
+  } else if (t.blocks && !a.l.few) {
+    e = queue(walk_kernel<T, E8, HD>, 64, 0);
+  } else if (!a.l.few) {
+    e = queue(tile_kernel<T, E8, HD>, 64 * kTileWaves, tile_lds);
+  } else if (a.l.waves == 1) {
+    e = t.blocks ? queue(few_kernel<T, E8, HD, true, 1>, 64, few_lds(1))
+                 : queue(few_kernel<T, E8, HD, false, 1>, 64, few_lds(1));
+  } else if (a.l.waves == 4) {
+    e = t.blocks ? queue(few_kernel<T, E8, HD, true, 4>, 256, few_lds(4))
+                 : queue(few_kernel<T, E8, HD, false, 4>, 256, few_lds(4));
+  } else {
+    e = t.blocks ? queue(few_kernel<T, E8, HD, true, 8>, 512, few_lds(8))
+                 : queue(few_kernel<T, E8, HD, false, 8>, 512, few_lds(8));
   }
-  if (plan.parts == 0) return hipSuccess;
+  if (e != hipSuccess || plan.parts == 0) return e;
   const int64_t groups = (int64_t)t.batch.n_tokens * n.nq, per = 256 / (HD / 4);
   hipLaunchKernelGGL((combine_kernel<T, HD>), dim3((unsigned)((groups + per - 1) / per)), dim3(256), 0, s, a);
   return hipGetLastError();
