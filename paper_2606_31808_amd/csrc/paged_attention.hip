@@ -847,8 +847,9 @@ LMOP_DEVICE typename Half<T>::x4 read_transposed(const char* lds) {
 
 // A block's four groups of 16 keys, which lie in one page each
 struct Groups {
-  int page[4], slot[4];  // 0 for a page that does not exist, or keys past the end
-  uint32_t bad;          // groups whose page does not exist
+  int page[4];   // 0 for a page that does not exist, or keys past the end
+  int slot;      // of the block's first key; group i's is (slot + 16 i) % page_size
+  uint32_t bad;  // groups whose page does not exist
 };
 
 // A workgroup: 128 vectors x a kv head, 32 vectors a wave.  Blocks of 64
@@ -922,11 +923,16 @@ struct TileCore {
   // A block on its way: 16-bit pages to the stage, 8-bit ones to registers (store() follows)
   LMOP_DEVICE void load(const Groups& b, int st) {
     if constexpr (!E8) {
+      // (scalar instructions: those of four pages' addresses a block are worth a branch)
+      const int64_t whole = (b.page[0] * cache.page_stride + b.slot * HD) * 2;
 #pragma unroll
       for (int i = 0; i < DMA; ++i) {
-        const int page = DMA == 4 ? b.page[i] : (wave >> 1) ? b.page[2 * i + 1] : b.page[2 * i];
-        const int slot = DMA == 4 ? b.slot[i] : (wave >> 1) ? b.slot[2 * i + 1] : b.slot[2 * i];
-        const int64_t at = (page * cache.page_stride + slot * HD) * 2;
+        const int grp = DMA == 4 ? i : 2 * i + (wave >> 1);
+        int64_t at = whole + grp * (16 * HD * 2);
+        if (ps < KB) {
+          const int page = DMA == 4 ? b.page[i] : (wave >> 1) ? b.page[2 * i + 1] : b.page[2 * i];
+          at = (page * cache.page_stride + ((b.slot + 16 * grp) & (ps - 1)) * HD) * 2;
+        }
         const uint32_t dst = lds0 + (uint32_t)(st * STAGE + kTileWaves * 1024 * i);
         g2l16_m0((const char*)cache.k + at, koff[i], dst);
         g2l16_m0((const char*)cache.v + at, voff, dst + KB * ROW);
@@ -937,8 +943,7 @@ struct TileCore {
         const int r = tid / LANES + i * ROWS;
         const int grp = __builtin_amdgcn_readfirstlane(r >> 4);
         const int page = grp == 0 ? b.page[0] : grp == 1 ? b.page[1] : grp == 2 ? b.page[2] : b.page[3];
-        const int slot = grp == 0 ? b.slot[0] : grp == 1 ? b.slot[1] : grp == 2 ? b.slot[2] : b.slot[3];
-        const size_t row = (size_t)h * ps + slot + (r & 15);
+        const size_t row = (size_t)h * ps + ((b.slot + r) & (ps - 1));
         const size_t at = page * cache.page_stride + row * HD + tid % LANES * 16;
         kr[i] = *(const uint4*)((const char*)cache.k + at);
         vr[i] = *(const uint4*)((const char*)cache.v + at);
@@ -1141,24 +1146,23 @@ LMOP_DEVICE void tile_vectors(const Args& a, int block, int split, char* smem) {
   const int b0 = b_from < nb ? (int)b_from : nb;
   const int b1 = nb - b0 < a.l.chunk ? nb : b0 + a.l.chunk;
 
-  // pages are looked up a block before they are loaded
+  // Pages are looked up a block before they are loaded: lane i fetches group i's, and the wave takes them when
+  // the block before has come, for which it waits anyway (a wait at the look-up would be one for the
+  // loads before it, too).
   const int32_t* own_table = p.batch.table + (int64_t)w.seq * p.batch.ld_table;
-  auto look_up = [&](int b) {
+  auto fetch = [&](int b) {
+    const bool pre = b < nb_pre;
+    const int key = (pre ? b : b - nb_pre) * KB + 16 * (threadIdx.x & 3);
+    return b < b1 && key < (pre ? n_pre : n_own) ? (pre ? p.prefix : own_table)[key >> lps] : 0;
+  };
+  auto resolve = [&](int b, int fetched) {
     Groups r;
     r.bad = 0;
-    const bool pre = b < nb_pre;
-    const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
-    const int32_t* table = pre ? p.prefix : own_table;
+    r.slot = (b < nb_pre ? b : b - nb_pre) * KB & (ps - 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int key = kb + 16 * i;
-      int q = 0;
-      if (b < b1 && key < n) {
-        q = __builtin_amdgcn_readfirstlane(table[key >> lps]);
-        if (q < 0 || q >= p.cache.n_pages) q = 0, r.bad |= 1u << i;
-      }
-      r.page[i] = q;
-      r.slot[i] = key & (ps - 1);
+      r.page[i] = __builtin_amdgcn_readlane(fetched, i);
+      if (r.page[i] < 0 || r.page[i] >= p.cache.n_pages) r.page[i] = 0, r.bad |= 1u << i;
     }
     return r;
   };
@@ -1178,12 +1182,12 @@ LMOP_DEVICE void tile_vectors(const Args& a, int block, int split, char* smem) {
 
   if (k.tid < 4) s_odd[k.tid >> 1][k.tid & 1] = 0;
   uint32_t bad = 0;
-  Groups next{};
+  int fetched = 0;
   if (b0 < b1) {
-    const Groups first = look_up(b0);
+    const Groups first = resolve(b0, fetch(b0));
     k.load(first, b0 & 1);
     bad = first.bad;
-    next = look_up(b0 + 1);
+    fetched = fetch(b0 + 1);
     if constexpr (E8) k.store(b0 & 1);
   }
   for (int b = b0; b < b1; ++b) {
@@ -1191,10 +1195,12 @@ LMOP_DEVICE void tile_vectors(const Args& a, int block, int split, char* smem) {
     // stage the next one takes
     if constexpr (!E8) wait_vmcnt<0>();
     __syncthreads();
-    const uint32_t next_bad = next.bad;
+    uint32_t next_bad = 0;
     if (b + 1 < b1) {
+      const Groups next = resolve(b + 1, fetched);
+      next_bad = next.bad;
       k.load(next, (b + 1) & 1);
-      next = look_up(b + 2);
+      fetched = fetch(b + 2);
     }
     const bool pre = b < nb_pre;
     const int kb = (pre ? b : b - nb_pre) * KB, n = pre ? n_pre : n_own;
