@@ -514,7 +514,7 @@ lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* args)
  *
  * A page holds page_size tokens of every kv head: [n_kv_heads][page_size][head_dim].
  * LMOP_E4M3 pages hold E4M3 codes, and for each token and head a power of two
- * as its exponent + 127: value = e4m3(code) * 2^(exp - 127).  A power of two because
+ * as its exponent + 127, 1 to 254: value = e4m3(code) * 2^(exp - 127).  A power of two because
  * codes are floating-point: any other scale would round no less, and this
  * one is undone exactly. */
 typedef struct {
@@ -538,7 +538,8 @@ typedef struct {
   const int32_t* table;  /* [n_seqs][max_pages] page numbers; those past a sequence's keys are not
                             read or not used, whatever they are */
   const int32_t* length; /* [n_seqs] */
-  const int32_t* start;  /* [n_seqs + 1], ascending; NULL: one token each (n_tokens == n_seqs) */
+  const int32_t* start;  /* [n_seqs + 1], ascending (tokens between starts that are not are left out, or
+                            counted to either); NULL: one token each (n_tokens == n_seqs) */
   int64_t ld_table;      /* >= max_pages */
   int32_t max_pages, n_seqs, n_tokens;
 } lmop_batch;

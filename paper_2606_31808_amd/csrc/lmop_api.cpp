@@ -1662,8 +1662,9 @@ lmop_status check_cache(lmop_ctx* c, const lmop_cache& k, int32_t dtype) {
   if (k.page_stride < (int64_t)c->nkv_dim * k.page_size || k.page_stride % 16 != 0)
     return fail(c, LMOP_ERR_INVALID_ARG, "pages of %lld elements are %lld apart (a multiple of 16)",
                 (long long)c->nkv_dim * k.page_size, (long long)k.page_stride);
-  if (k.page_stride > kMaxPageStride)
-    return fail(c, LMOP_ERR_UNSUPPORTED, "pages %lld elements apart", (long long)k.page_stride);
+  if (k.page_stride > kMaxPageStride || (int64_t)c->nkv_dim * k.page_size > (int64_t(1) << 29))
+    return fail(c, LMOP_ERR_UNSUPPORTED, "pages of %lld elements, %lld apart", (long long)c->nkv_dim * k.page_size,
+                (long long)k.page_stride);
   return LMOP_OK;
 }
 

@@ -437,6 +437,7 @@ LMOP_DEVICE void few_vectors(const Args& a, int block, int split, FewLds<T, E8, 
       w.seq = find_seq(p.batch.n_seqs, t, [&](int i) { return p.batch.start[i]; });
     }
     const int2 all = seq_tokens(p.batch, w.seq);
+    if (t < all.x || t >= all.y) return;  // (starts that do not ascend)
     // the sequence as it was at this token
     w.tok = int2{t, t + 1};
     const int len = p.batch.length[w.seq];
@@ -488,7 +489,7 @@ LMOP_DEVICE void few_vectors(const Args& a, int block, int split, FewLds<T, E8, 
       if (e < n_pre) {
         const int q = p.prefix[e];
         page = q >= 0 && q < p.cache.n_pages ? q : -1;
-        first = -(1 << 30);  // every token sees it
+        first = -(1 << 28);  // every token sees it: indexes are above -2^24 and below 2^30
         cap = p.prefix_length - (e << lps) < ps ? p.prefix_length - (e << lps) : ps;
       } else {
         int b = e - n_pre;

@@ -157,7 +157,9 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
         if (t < bt.start[0] || t >= bt.start[bt.n_seqs]) continue;
         s = find_seq(bt.n_seqs, t, [&](int i) { return bt.start[i]; });
       }
-      const int64_t index = (int64_t)bt.length[s] - (seq_tokens(bt, s).y - t);
+      const int2 tok = seq_tokens(bt, s);
+      if (t < tok.x || t >= tok.y) continue;  // (starts that do not ascend)
+      const int64_t index = (int64_t)bt.length[s] - (tok.y - t);
       Angles w;
       if (p.rotate) w = load_angles(a, p.first + index, HD / 2, d);
       for (int c = c0; c < c0 + chunks; ++c) {

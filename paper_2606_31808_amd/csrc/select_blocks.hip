@@ -231,9 +231,11 @@ __global__ __launch_bounds__(64 * WAVES) void select_one_kernel(const lmop_selec
     if (t < bt.start[0] || t >= bt.start[bt.n_seqs]) return;
     s = find_seq(bt.n_seqs, t, [&](int i) { return bt.start[i]; });
   }
+  const int2 tok = seq_tokens(bt, s);
+  if (t < tok.x || t >= tok.y) return;  // (starts that do not ascend)
   const int len = bt.length[s];
   int32_t* out = p.blocks + ((size_t)t * n.nkv + h) * p.n_blocks;
-  const Choice c = settle(p, (int64_t)len - (seq_tokens(bt, s).y - t), len, out);
+  const Choice c = settle(p, (int64_t)len - (tok.y - t), len, out);
   if (c.done) return;
   if (tid < HD) {
     const T* q = (const T*)p.q + t * p.ldq + h * G * HD + tid;

@@ -603,3 +603,247 @@ def test_append_choose_attend(L, cache):
     step(new0, new0)
     for i in range(1, steps + 1):
         step([1] * 3, [n + i for n in new0])
+
+
+# ---------------------------------------------------------------- appending: places and values that do not fit
+@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS[:6])
+def test_append_places_that_do_not_exist(L, dtype, cache, hd):
+    """Tokens before the sequence, past the table, in a page that is none, at a position past max_seq."""
+    print("places", dtype, cache, hd, flush=True)
+    nq, nkv, page = 4, 2, 16
+    b = Batch(nq, nkv, hd, dtype, cache, page, [6, 40, 30], [6, 70, 30], spare=0)
+    c = b.cache(L)
+    old = [t.view(torch.uint8).clone() for t in (c.k, c.v)]
+    qkv = torch.randn(b.tokens, (nq + 2 * nkv) * hd, generator=_gen(1)).to(b.dt).cuda()
+    q, k, v = qkv.split((nq * hd, nkv * hd, nkv * hd), 1)
+    a = b.args(L)
+    a["length"] = torch.tensor([3, 10 ** 6, 30], dtype=torch.int32).cuda()
+    a["table"] = a["table"].clone()
+    a["table"][2, 1] = 2 ** 31 - 1
+    ctx = _ctx(L, nq, nkv, hd, max_seq=20)
+    out = ctx.cache_append(c, k, v, q=q, first=5, **a).view(b.tokens, -1)
+    torch.cuda.synchronize()
+    written = torch.zeros(b.live.shape, dtype=torch.bool)
+    written[int(b.table[0, 0]), :3] = True
+    written[int(b.table[2, 0]), :16] = True
+    for now, was in zip((c.k, c.v), old):
+        w = written[:, None, :].expand(now.shape[:3]).cuda()
+        assert torch.equal(now.view(torch.uint8)[~w], was[~w])
+    # keys of index 15 and on, at position 20 and on, are NaN, and so are queries; values are as they are
+    bits = c.k.view(torch.uint8) if cache == "e4m3" else c.k
+    p2 = bits[int(b.table[2, 0])]
+    assert ((p2[:, 15] & 0x7F) == 0x7F).all() if cache == "e4m3" else torch.isnan(p2[:, 15]).all()
+    assert not (((p2[:, 14] & 0x7F) == 0x7F).any() if cache == "e4m3" else torch.isnan(p2[:, 14]).any())
+    pos = [5 - 3 + i for i in range(6)] + [10 ** 6] * 40 + [5 + i for i in range(30)]
+    nan = torch.tensor([not 0 <= x < 20 for x in pos])
+    assert torch.equal(torch.isnan(out).all(1).cpu(), nan) and torch.isfinite(out[~nan.cuda()]).all()
+
+
+def test_append_codes_of_odd_heads(L):
+    """Zeros, the least and the largest values, borders of the scale, infinities and NaN."""
+    nkv, hd = 2, 64
+    for dtype in ("f16", "bf16"):
+        rows = [0.0, 448.0, 449.0, 448.0 * 2 ** -20, 1e-7, 61440.0, 65504.0, float("inf"), NAN, 3e38 if dtype == "bf16" else 1.0,
+                1e-38 if dtype == "bf16" else 6e-8]
+        b = Batch(2, nkv, hd, dtype, "e4m3", 16, [len(rows)], [len(rows)])
+        x = torch.randn(len(rows), nkv * hd, generator=_gen(2)) * 1e-3
+        top = torch.tensor(rows).to(b.dt)
+        x = (x.clamp(-1, 1) * top.float().nan_to_num(1, 1)[:, None]).to(b.dt)
+        x[:, 5] = top
+        x[:, hd + 7] = -top
+        c = b.cache(L)
+        ctx = _ctx(L, 2, nkv, hd)
+        ctx.cache_append(c, x.cuda(), x.cuda(), rotate=False, **b.args(L, starts=True))
+        page = int(b.table[0, 0])
+        for code, exp in ((c.k, c.k_exp), (c.v, c.v_exp)):
+            code, exp = code[page].double().cpu(), exp[page].double().cpu()
+            for i, r in enumerate(rows):
+                y = x[i].double().view(nkv, hd)
+                if not math.isfinite(r):
+                    assert torch.isnan(code[:, i]).all()
+                    continue
+                if dtype == "f16":
+                    y = y.clamp(-61440, 61440)
+                # the definition: the least exponent that fits
+                amax = y.abs().amax(-1)
+                for h in range(nkv):
+                    e = -126
+                    while amax[h] > 448 * 2.0 ** e:
+                        e += 1
+                    assert exp[h, i] == e + 127, (dtype, r)
+                    v = y[h] * 2.0 ** -e
+                    step = torch.pow(2.0, torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6))) - 3)
+                    assert torch.equal(code[h, i], torch.round(v / step) * step), (dtype, r)
+
+
+@pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("bf16", "e4m3")])
+def test_append_strides_and_in_place(L, dtype, cache):
+    nq, nkv, hd = 4, 2, 64
+    b = Batch(nq, nkv, hd, dtype, cache, 16, [20, 3], [30, 3])
+    x = torch.randn(b.tokens, (nq + 2 * nkv) * hd + 5, generator=_gen(3)).to(b.dt).cuda()
+    cols = (nq * hd, nkv * hd, nkv * hd)
+    q, k, v = x[:, 3:-2].split(cols, 1)
+    ctx = _ctx(L, nq, nkv, hd)
+    caches = [b.cache(L) for _ in range(2)]
+    want = ctx.cache_append(caches[0], k.contiguous(), v.contiguous(), q=q.contiguous(), **b.args(L))
+    before = x.clone()
+    got = ctx.cache_append(caches[1], k, v, q=q, q_out=q, **b.args(L))
+    assert got.data_ptr() == q.data_ptr() and torch.equal(q, want)
+    before[:, 3:3 + nq * hd] = want
+    assert torch.equal(x, before)
+    for n in ("k", "v"):
+        assert torch.equal(getattr(caches[0], n).view(torch.uint8), getattr(caches[1], n).view(torch.uint8))
+
+
+# ---------------------------------------------------------------- sizes
+@pytest.mark.parametrize("cache", ["f16", "e4m3"])
+def test_offsets_past_32_bits(L, cache):
+    """Pages more than 4 GiB (and 2^32 elements) into the cache."""
+    nq, nkv, hd, page = 8, 8, 128, 64
+    pool = 70000 if cache == "e4m3" else 36000
+    dt = E4M3 if cache == "e4m3" else torch.float16
+    print("far", cache, flush=True)
+    k, v = (torch.zeros(pool, nkv, page, hd, dtype=torch.uint8 if cache == "e4m3" else dt, device="cuda").view(dt)
+            for _ in range(2))
+    exps = [torch.full((pool, nkv, page), 127, dtype=torch.uint8, device="cuda") for _ in range(2)] if cache == "e4m3" else []
+    mean = torch.zeros(pool, nkv, hd, dtype=torch.float16, device="cuda")
+    far = L.PagedCache(k, v, *exps, k_mean=mean) if exps else L.PagedCache(k, v, k_mean=mean)
+    small = Batch(nq, nkv, hd, "f16", cache, page, [150], [150], spare=0)
+    near_mean = torch.zeros(len(small.live), nkv, hd, dtype=torch.float16, device="cuda")
+    near = small.cache(L, near_mean)
+    ctx = _ctx(L, nq, nkv, hd)
+    q, kk, vv = (torch.randn(150, n * hd, generator=_gen(i)).half().cuda() for i, n in enumerate((nq, nkv, nkv)))
+    a = small.args(L)
+    b = {**a, "table": torch.tensor([[pool - 1, pool - 3, pool - 2]], dtype=torch.int32).cuda()}
+    res = []
+    for c, args in ((near, a), (far, b)):
+        x = ctx.cache_append(c, kk, vv, q=q, **args)
+        blocks = ctx.select_blocks(c, x, 2, **args)
+        last = dict(table=args["table"], length=args["length"])
+        res.append((x, blocks, ctx.attend(c, x, **args), ctx.attend(c, x, blocks=blocks, **args),
+                    ctx.attend(c, x[-1:], **last), ctx.attend(c, x[-1:], prefix=args["table"][0], prefix_length=150,
+                                                             **{**last, "length": last["length"] * 0})))
+    for x, y in zip(*res):
+        assert torch.equal(x, y)
+
+
+def test_sizes_of_nothing(L):
+    ctx = _ctx(L, 4, 2, 64)
+    b = Batch(4, 2, 64, "f16", "f16", 16, [1], [5])
+    c = b.cache(L, torch.zeros(len(b.live), 2, 64, dtype=torch.float16, device="cuda"))
+    none = dict(table=torch.zeros(0, 3, dtype=torch.int32, device="cuda"),
+                length=torch.zeros(0, dtype=torch.int32, device="cuda"))
+    q, kv = (torch.zeros(0, n, dtype=torch.float16, device="cuda") for n in (256, 128))
+    assert ctx.attend(c, q, **none).shape == (0, 256)
+    assert ctx.select_blocks(c, q, 4, **none).shape == (0, 2, 4)
+    assert ctx.cache_append(c, kv, kv, q=q, **none).shape == (0, 256)
+    # a table without columns: only the prefix is there to see
+    one = dict(table=torch.zeros(1, 0, dtype=torch.int32, device="cuda"),
+               length=torch.zeros(1, dtype=torch.int32, device="cuda"))
+    want = ctx.attend(c, b.q.cuda(), prefix=b.table[0, :1].cuda(), prefix_length=5, **one)
+    assert torch.equal(want, b.attend(ctx, L))
+
+
+# ---------------------------------------------------------------- graphs, streams, contexts
+def _step(ctx, c, x, args, prefix, n):
+    q = ctx.cache_append(c, x[1], x[2], q=x[0], first=40, **args)
+    blocks = ctx.select_blocks(c, q, 3, max_length=700, **args)
+    return (q, blocks, ctx.attend(c, q, max_tokens=n, max_length=700, prefix=prefix, prefix_length=40, **args),
+            ctx.attend(c, q, max_tokens=n, max_length=700, blocks=blocks, **args),
+            ctx.attend(c, q, max_tokens=n, max_length=700, **args))
+
+
+@pytest.mark.parametrize("cache", ["f16", "e4m3"])
+@pytest.mark.parametrize("new", [[1, 1, 1], [30, 7, 44]])
+def test_captured(L, cache, new):
+    """Two graphs of a whole step, replayed in turn with eager calls between, follow what the tables,
+    lengths and tokens hold then."""
+    nq, nkv, hd = 8, 2, 64
+    stream = torch.cuda.Stream()
+    ctx = L.Context(Shape(nq, nkv, hd), device=0, stream=stream.cuda_stream, max_seq=4096)
+    b = Batch(nq, nkv, hd, "f16", cache, 16, new, [700, 650, 690], prefix=40, seed=5)
+    with torch.cuda.stream(stream):
+        mean = torch.zeros(len(b.live), nkv, hd, dtype=torch.float16, device="cuda")
+        c = b.cache(L, mean)
+        kept = [t for t in (c.k, c.v, c.k_exp, c.v_exp, c.k_mean) if t is not None]
+        args = b.args(L, starts=max(new) > 1)
+        prefix = b.prefix_pages.cuda()
+        x = [torch.randn(b.tokens, h * hd, device="cuda").half() for h in (nq, nkv, nkv)]
+
+        def eager():
+            return [t.clone() for t in _step(ctx, c, x, args, prefix, max(new))]
+
+        eager()
+        stream.synchronize()
+        graphs = []
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                out = _step(ctx, c, x, args, prefix, max(new))
+            graphs.append((g, out))
+        for i in range(6):
+            for t in x:
+                t.normal_()
+            args["length"].copy_(torch.tensor([n - 16 * i for n in b.len], dtype=torch.int32))
+            state = [t.clone() for t in kept]
+            want = eager()
+            after = [t.clone() for t in kept]
+            for t, s in zip(kept, state):
+                t.copy_(s)
+            g, out = graphs[i % 2]
+            g.replay()
+            stream.synchronize()
+            for got, w in zip(out, want):
+                assert torch.equal(got, w)
+            for t, w in zip(kept, after):
+                assert torch.equal(t.view(torch.uint8), w.view(torch.uint8))
+
+
+def test_two_contexts_at_once(L):
+    """Calls on two streams, interleaved: each as if alone."""
+    nq, nkv, hd = 8, 2, 64
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ctxs = [L.Context(Shape(nq, nkv, hd), device=0, stream=s.cuda_stream) for s in streams]
+    batches = [Batch(nq, nkv, hd, "f16", "f16", 16, n, [900, 300], prefix=100, seed=i)
+               for i, n in enumerate(([1, 1], [40, 9]))]
+    alone = [b.attend(_ctx(L, nq, nkv, hd), L) for b in batches]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(batches[i].attend(ctxs[i], L))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for x in got[i]:
+            assert torch.equal(x, alone[i])
+    with pytest.raises(ValueError):  # another stream than the ctx's
+        batches[0].attend(ctxs[0], L)
+
+
+def test_profiled(L):
+    ctx = _ctx(L, 4, 2, 64)
+    b = Batch(4, 2, 64, "f16", "f16", 16, [1, 1], [90, 40], prefix=20)
+    mean = torch.zeros(len(b.live), 2, 64, dtype=torch.float16, device="cuda")
+    c = b.cache(L, mean)
+    ctx.set_profiling(1)
+    kv = torch.zeros(2, 128, dtype=torch.float16, device="cuda")
+    ctx.cache_append(c, kv, kv, **b.args(L))
+    b.attend(ctx, L, cache=c)
+    blocks = ctx.select_blocks(c, b.q.cuda(), 2, **b.args(L))
+    ctx.attend(c, b.q.cuda(), blocks=blocks, **b.args(L))
+    st = ctx.kernel_stats()
+    for name in ("cache_append", "attend", "select_blocks", "attend_blocks"):
+        assert st[name]["launches"] == 1 and st[name]["ms"] > 0
+    ctx.set_profiling(0)
+
+
+def test_results_are_repeated(L):
+    """The same call gives the same bits."""
+    for new, prefix in (([1] * 40, 3000), ([20, 50], 100), ([1], 0)):
+        b = Batch(8, 2, 128, "f16", "e4m3", 32, new, [2000 + i for i in range(len(new))], prefix, seed=4)
+        ctx = _ctx(L, 8, 2, 128)
+        c = b.cache(L)
+        want = b.attend(ctx, L, cache=c)
+        for _ in range(3):
+            assert torch.equal(b.attend(ctx, L, cache=c), want)
