@@ -596,7 +596,7 @@ typedef struct {
   float* lse;            /* NULL or [n_tokens][n_heads] */
   const int32_t* prefix; /* the prefix's ceil(prefix_length / page_size) pages */
   const int32_t* blocks; /* [n_tokens][n_kv_heads][n_blocks], or NULL with n_blocks 0; not with a prefix */
-  void* workspace;       /* 256-byte aligned; NULL if lmop_attend_workspace says 0.  Only this call's
+  void* workspace;       /* 16-byte aligned; NULL if lmop_attend_workspace says 0.  Only this call's
                             kernels use it, and nothing in it matters before or after them */
   uint64_t workspace_bytes;
   int64_t ldq, ldo;

@@ -3143,7 +3143,7 @@ lmop_status lmop_attend(lmop_ctx* ctx, const lmop_attend_args* a) {
     if (a->workspace_bytes < need)
       return fail(ctx, LMOP_ERR_INVALID_ARG, "a workspace of %llu bytes, %llu needed",
                   (unsigned long long)a->workspace_bytes, (unsigned long long)need);
-    LMOP_TRY(check_ptr(ctx, "workspace", a->workspace, 256));
+    LMOP_TRY(check_ptr(ctx, "workspace", a->workspace, 16));
   }
   const int64_t own = a->n_blocks > 0 ? (int64_t)a->n_blocks * a->cache.page_size : a->max_length;
   // as if every sequence were the longest: the lengths are in device memory

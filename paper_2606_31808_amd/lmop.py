@@ -676,8 +676,13 @@ class PagedCache:
         pages, heads, size, dim = k.shape
         dev = k.get_device()
         stride = k.stride(0) if pages > 1 else heads * size * dim
+        if dev < 0 and not k.is_cpu:
+            raise ValueError(f"k is on {k.device}")
+        for t, what in ((k, "k"), (v, "v"), (k_exp, "k_exp"), (v_exp, "v_exp"), (k_mean, "k_mean")):
+            if t is not None and t.device != k.device:
+                raise ValueError(f"{what} is on {t.device}, k on {k.device}")
         for t, what in ((k, "k"), (v, "v")):
-            if t.get_device() != dev or t.dtype != k.dtype or t.shape != k.shape:
+            if t.dtype != k.dtype or t.shape != k.shape:
                 raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)} on {t.device}, unlike k")
             if pages > 0 and not t[0].is_contiguous() or pages > 1 and t.stride(0) != stride:
                 raise ValueError(f"{what}: a page is not contiguous, or its pages lie otherwise than k's")
@@ -685,10 +690,10 @@ class PagedCache:
         for t, what in ((k_exp, "k_exp"), (v_exp, "v_exp")):
             if (t is not None) != e8:
                 raise ValueError(f"{what} is for float8_e4m3fn pages, which need it")
-            if e8 and (t.get_device() != dev or t.dtype != torch.uint8 or t.shape != (pages, heads, size) or
+            if e8 and (t.dtype != torch.uint8 or t.shape != (pages, heads, size) or
                        not t.is_contiguous()):
                 raise ValueError(f"{what}: expected contiguous uint8 {(pages, heads, size)} on device {dev}")
-        if k_mean is not None and (k_mean.get_device() != dev or k_mean.shape != (pages, heads, dim) or
+        if k_mean is not None and (k_mean.shape != (pages, heads, dim) or
                                    k_mean.dtype not in (torch.float16, torch.bfloat16) or
                                    not e8 and k_mean.dtype != k.dtype or not k_mean.is_contiguous()):
             raise ValueError(f"k_mean: expected contiguous {(pages, heads, dim)} of the tokens' dtype on device {dev}")

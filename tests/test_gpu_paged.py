@@ -206,27 +206,42 @@ LAYOUTS = [("f16", "f16", 64), ("bf16", "bf16", 128), ("f16", "f16", 128), ("bf1
 
 
 # ---------------------------------------------------------------- attention: single tokens
-@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
-@pytest.mark.parametrize("nq,nkv,page,length,prefix", [
+SINGLE = [
     (4, 2, 16, [1], 0), (4, 2, 16, [15, 16, 17, 0, 1, 33], 0), (8, 2, 64, [63, 64, 65, 200], 0),
     (3, 1, 32, [5, 100, 31], 45), (8, 1, 16, [300, 1, 77], 1), (7, 1, 128, [129, 500], 130),
-    (2, 2, 256, [256, 257, 2], 255), (4, 4, 16, [40, 7], 64), (17, 1, 16, [50, 9], 20), (40, 2, 32, [70], 0)])
+    (2, 2, 256, [256, 257, 2], 255), (4, 4, 16, [40, 7], 64), (17, 1, 16, [50, 9], 20), (40, 2, 32, [70], 0)]
+
+
+@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
+@pytest.mark.parametrize("nq,nkv,page,length,prefix", SINGLE)
 def test_attend_single_tokens(L, dtype, cache, hd, nq, nkv, page, length, prefix):
     print("single", dtype, cache, hd, nq, nkv, page, length, prefix, flush=True)
     _run(L, Batch(nq, nkv, hd, dtype, cache, page, [1] * len(length), length, prefix, seed=len(length)))
 
 
+LONG = [(4, 1, 16, [9001, 700], 0), (8, 2, 64, [5000], 0), (4, 2, 32, [3], 4100), (2, 1, 64, [30] * 3, 3001)]
+# many sequences: a wave each, or four
+MANY = [(8, 8, 16, [i % 70 for i in range(300)], 0), (16, 8, 32, [i % 90 for i in range(260)], 50),
+        (4, 2, 16, [6 * i for i in range(100)], 0), (4, 2, 16, [3 * i for i in range(100)], 70),
+        (128, 128, 16, [i for i in range(16)], 20)]
+
+
+@pytest.mark.parametrize("dtype,cache,hd", [("f16", "f16", 128), ("bf16", "bf16", 64), ("bf16", "e4m3", 128)])
+@pytest.mark.parametrize("nq,nkv,page,length,prefix", MANY)
+def test_attend_many_sequences(L, dtype, cache, hd, nq, nkv, page, length, prefix):
+    print("many", dtype, cache, hd, nq, nkv, page, len(length), prefix, flush=True)
+    _run(L, Batch(nq, nkv, hd, dtype, cache, page, [1] * len(length), length, prefix, seed=len(length)))
+
+
 @pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
-@pytest.mark.parametrize("nq,nkv,page,length,prefix", [
-    (4, 1, 16, [9001, 700], 0), (8, 2, 64, [5000], 0), (4, 2, 32, [3], 4100), (2, 1, 64, [30] * 3, 3001)])
+@pytest.mark.parametrize("nq,nkv,page,length,prefix", LONG)
 def test_attend_long_axis_is_split_and_joined(L, dtype, cache, hd, nq, nkv, page, length, prefix):
     print("split", dtype, cache, hd, nq, nkv, page, length, prefix, flush=True)
     _run(L, Batch(nq, nkv, hd, dtype, cache, page, [1] * len(length), length, prefix, seed=3))
 
 
 # ---------------------------------------------------------------- attention: several tokens
-@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
-@pytest.mark.parametrize("nq,nkv,page,new,length,prefix", [
+SEVERAL = [
     (4, 2, 16, [2, 1, 3], [2, 17, 40], 0),        # few vectors, causal
     (4, 1, 32, [4, 2, 0, 1], [4, 33, 9, 1], 37),  # few vectors behind a prefix; a sequence without tokens
     (2, 2, 64, [16], [90], 0),
@@ -235,7 +250,12 @@ def test_attend_long_axis_is_split_and_joined(L, dtype, cache, hd, nq, nkv, page
     (3, 1, 128, [43], [170], 5),
     (4, 4, 32, [129, 127], [129, 300], 64),
     (16, 1, 16, [9, 20], [12, 20], 0),
-    (40, 2, 64, [7], [66], 10)])
+    (40, 2, 64, [7], [66], 10),
+    (2, 1, 32, [70], [3000], 0)]                  # tiles, their keys split
+
+
+@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
+@pytest.mark.parametrize("nq,nkv,page,new,length,prefix", SEVERAL)
 def test_attend_several_tokens(L, dtype, cache, hd, nq, nkv, page, new, length, prefix):
     print("several", dtype, cache, hd, nq, nkv, page, new, length, prefix, flush=True)
     _run(L, Batch(nq, nkv, hd, dtype, cache, page, new, length, prefix, seed=sum(new)))
@@ -538,12 +558,16 @@ def test_select(L, dtype, hd, nq, nkv, page, new, length, n_blocks):
 
 
 # ---------------------------------------------------------------- attention over blocks
-@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
-@pytest.mark.parametrize("nq,nkv,page,new,length,n_blocks", [
+BLOCKS = [
     (4, 2, 16, [1, 1], [300, 20], 5), (8, 1, 64, [1], [1000], 9), (3, 3, 16, [5, 3], [5, 200], 4),
     (2, 2, 128, [2], [600], 3), (4, 2, 16, [3], [90], 200), (20, 1, 32, [2], [200], 4), (4, 2, 16, [1], [5000], 256),
     (4, 2, 16, [40, 33], [300, 40], 5), (8, 1, 64, [50], [1500], 7), (3, 1, 128, [43], [700], 3),
-    (4, 4, 32, [130], [2000], 6), (8, 2, 16, [70], [3000], 9), (2, 1, 256, [70], [1000], 2)])
+    (4, 4, 32, [130], [2000], 6), (8, 2, 16, [70], [3000], 9), (2, 1, 256, [70], [1000], 2),
+    (4, 2, 16, [1] * 90, [11 * i for i in range(90)], 40), (8, 8, 16, [1] * 270, [i % 100 for i in range(270)], 3)]
+
+
+@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
+@pytest.mark.parametrize("nq,nkv,page,new,length,n_blocks", BLOCKS)
 def test_attend_blocks(L, dtype, cache, hd, nq, nkv, page, new, length, n_blocks):
     print("blocks", dtype, cache, hd, nq, nkv, page, new, length, n_blocks, flush=True)
     b = Batch(nq, nkv, hd, dtype, cache, page, new, length, seed=n_blocks, lead=1, tail=2)
@@ -561,6 +585,33 @@ def test_attend_blocks(L, dtype, cache, hd, nq, nkv, page, new, length, n_blocks
         blocks[:, :, 3] = -2 ** 31
         blocks[b.lead] = -1
         _run(L, b, blocks)
+
+
+@pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
+@pytest.mark.parametrize("nq,nkv,new", [(8, 2, [40]), (2, 2, [3]), (1, 1, [70])])
+def test_attend_blocks_unseen_keys_may_hold_anything(L, dtype, cache, hd, nq, nkv, new):
+    """A block with infinities and NaN reaches the tokens that chose it only."""
+    print("blocks unseen", dtype, cache, hd, nq, nkv, new, flush=True)
+    b = Batch(nq, nkv, hd, dtype, cache, 16, new, [400], seed=2)
+    g = _gen(3)
+    n = new[0]
+    blocks = torch.stack([torch.stack([torch.randperm(24, generator=g)[:5].sort()[0] for _ in range(nkv)])
+                          for _ in range(n)]).to(torch.int32)
+    ctx = _ctx(L, nq, nkv, hd)
+    clean = b.attend(ctx, L, blocks=blocks.cuda()).view(n, nkv, -1)
+    page = int(b.table[0, 7])
+    if cache == "e4m3":
+        b.k8[page, :, 3], b.v8[page, :, 9] = 0x7F, 0x7F
+    else:
+        b.k16[page, :, 3], b.v16[page, :, 9] = NAN, float("-inf")
+    got = b.attend(ctx, L, blocks=blocks.cuda()).view(n, nkv, -1)
+    sees = (blocks == 7).any(-1).cuda()
+    assert 0 < sees.sum() < sees.numel()
+    assert torch.isnan(got[sees]).all() and torch.equal(got[~sees], clean[~sees])
+    if cache != "e4m3":  # a value alone
+        b.k16[page, :, 3] = 0.5
+        got = b.attend(ctx, L, blocks=blocks.cuda()).view(n, nkv, -1)
+        assert not torch.isfinite(got[sees]).any() and torch.equal(got[~sees], clean[~sees])
 
 
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])

@@ -198,3 +198,197 @@ def test_a_ctx_dropped_in_a_capture_is_freed_later(monkeypatch):
     del other
     assert freed[1:] == [handle]
     assert not L._dropped
+
+
+# ---------------------------------------------------------------- the paged cache and its attention
+CACHE = dict(k=P, v=P, page_stride=4096, n_pages=10, page_size=16, dtype=L.LMOP_F16)
+BATCH = dict(table=P, length=P, start=P, ld_table=8, max_pages=8, n_seqs=3, n_tokens=7)
+APPEND = dict(q=P, k=P, v=P, q_out=2 * P, ldq=256, ldk=256, ldv=256, ldqo=256, first=5, rotate=1, dtype=L.LMOP_F16)
+ATTEND = dict(q=P, out=2 * P, ldq=256, ldo=256, max_tokens=5, max_length=100, dtype=L.LMOP_F16, workspace=P,
+              workspace_bytes=1 << 30)
+SELECT = dict(q=P, blocks=P, ldq=256, n_blocks=4, max_length=100, dtype=L.LMOP_F16)
+PAGED = {"lmop_cache_append": (L.lmop_append_args, APPEND), "lmop_attend": (L.lmop_attend_args, ATTEND),
+         "lmop_select_blocks": (L.lmop_select_args, SELECT)}
+E8 = dict(cache_dtype=L.LMOP_E4M3, cache_k_exp=P, cache_v_exp=P)
+
+
+def _paged(ctx, name, **change):
+    struct, base = PAGED[name]
+    parts = {"cache": dict(CACHE), "batch": dict(BATCH), "": dict(base)}
+    if name == "lmop_select_blocks":
+        parts["cache"]["k_mean"] = P
+    for k, v in change.items():
+        head, _, rest = k.partition("_")
+        at, key = (head, rest) if head in ("cache", "batch") else ("", k)
+        parts[at][key] = v
+    a = _args(struct, parts[""])
+    for n, t in (("cache", L.lmop_cache), ("batch", L.lmop_batch)):
+        for f, v in parts[n].items():
+            setattr(getattr(a, n), f, v)
+    return a
+
+
+@pytest.mark.parametrize("name", PAGED)
+@pytest.mark.parametrize("change,status", [
+    ({}, UNS), (dict(batch_n_tokens=0), OK), (dict(batch_n_seqs=0), OK), (dict(batch_n_tokens=-1), INV),
+    (dict(batch_n_seqs=-1), INV), (dict(batch_max_pages=-1), INV), (dict(dtype=L.LMOP_F32), INV), (dict(dtype=-1), INV),
+    (dict(dtype=L.LMOP_E4M3), INV), (dict(cache_page_size=0), INV), (dict(cache_page_size=8), INV),
+    (dict(cache_page_size=48), INV), (dict(cache_page_size=512), INV), (dict(cache_n_pages=0), INV),
+    (dict(cache_n_pages=-3), INV), (dict(batch_table=None), INV), (dict(batch_table=P + 2), INV),
+    (dict(batch_ld_table=7), INV), (dict(batch_length=None), INV), (dict(batch_length=P + 1), INV),
+    (dict(batch_start=P + 2), INV), (dict(batch_start=None), INV), (dict(q=P + 1), INV), (dict(ldq=255), INV),
+    (dict(batch_n_tokens=2 ** 31 - 1, batch_n_seqs=2 ** 31 - 1), UNS),
+    (dict(batch_max_pages=2 ** 31 - 1, batch_ld_table=2 ** 31), UNS),
+])
+def test_paged(ctx, name, change, status):
+    if name == "lmop_attend" and change.get("batch_n_tokens", 1) > 2 ** 20:
+        change = {**change, "max_tokens": 1, "batch_start": None}
+    assert _call(ctx, name, _paged(ctx, name, **change)) == status
+
+
+@pytest.mark.parametrize("name", ["lmop_cache_append", "lmop_attend"])
+@pytest.mark.parametrize("change,status", [
+    (E8, UNS), (dict(E8, dtype=L.LMOP_BF16), UNS), (dict(cache_dtype=L.LMOP_BF16), INV), (dict(cache_dtype=L.LMOP_F32), INV),
+    (dict(cache_dtype=9), INV), (dict(cache_dtype=L.LMOP_BF16, dtype=L.LMOP_BF16), UNS), (dict(E8, cache_k_exp=None), INV),
+    (dict(E8, cache_v_exp=P + 8), INV), (dict(cache_k_exp=P), INV), (dict(cache_k=None), INV), (dict(cache_v=P + 8), INV),
+    (dict(cache_k_mean=P + 8), INV), (dict(cache_page_stride=4095), INV), (dict(cache_page_stride=4104), INV),
+    (dict(cache_page_stride=4112), UNS), (dict(cache_page_stride=1 << 40), UNS),
+])
+def test_paged_cache(ctx, name, change, status):
+    assert _call(ctx, name, _paged(ctx, name, **change)) == status
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(first=-1), INV), (dict(rotate=2), INV), (dict(rotate=0), UNS), (dict(k=None), INV), (dict(v=None), INV),
+    (dict(ldk=255), INV), (dict(ldv=255), INV), (dict(q_out=None), INV), (dict(q=None, q_out=None), UNS),
+    (dict(q_out=P), UNS), (dict(q_out=P, ldqo=300), INV), (dict(ldqo=255), INV),
+    (dict(batch_start=None, batch_n_tokens=3), UNS),
+])
+def test_cache_append(ctx, change, status):
+    assert _call(ctx, "lmop_cache_append", _paged(ctx, "lmop_cache_append", **change)) == status
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(out=None), INV), (dict(out=P), INV), (dict(ldo=255), INV), (dict(lse=P), UNS), (dict(lse=P + 2), INV),
+    (dict(max_tokens=0), INV), (dict(max_tokens=8), INV), (dict(max_tokens=-1), INV), (dict(max_length=-1), INV),
+    (dict(max_length=128), UNS), (dict(max_length=129), INV), (dict(max_length=0), UNS),
+    (dict(prefix_length=-1), INV), (dict(prefix_length=3), INV), (dict(prefix_length=3, prefix=P), UNS),
+    (dict(prefix_length=3, prefix=P + 1), INV), (dict(prefix_length=2 ** 30, prefix=P), UNS),
+    (dict(n_blocks=-1), INV), (dict(n_blocks=3), INV), (dict(n_blocks=3, blocks=P), UNS), (dict(blocks=P), INV),
+    (dict(n_blocks=3, blocks=P + 2), INV), (dict(n_blocks=3, blocks=P, prefix_length=3, prefix=P), INV),
+    (dict(n_blocks=1025, blocks=P), UNS), (dict(scale=-1.0), INV), (dict(scale=float("nan")), INV),
+    (dict(scale=float("inf")), INV), (dict(scale=1e-35), INV), (dict(scale=0.5), UNS),
+    (dict(batch_start=None, batch_n_tokens=3), INV), (dict(batch_start=None, batch_n_tokens=3, max_tokens=1), UNS),
+    (dict(batch_n_seqs=1, batch_n_tokens=1, max_tokens=1, batch_max_pages=2 ** 20, batch_ld_table=2 ** 20,
+          max_length=2 ** 20, workspace_bytes=0), INV),
+    (dict(batch_n_seqs=1, batch_n_tokens=1, max_tokens=1, batch_max_pages=2 ** 20, batch_ld_table=2 ** 20,
+          max_length=2 ** 20, workspace=None), INV),
+    (dict(batch_n_seqs=1, batch_n_tokens=1, max_tokens=1, batch_max_pages=2 ** 20, batch_ld_table=2 ** 20,
+          max_length=2 ** 20, workspace=P + 8), INV),
+    (dict(batch_n_seqs=1, batch_n_tokens=1, max_tokens=1, batch_max_pages=2 ** 20, batch_ld_table=2 ** 20,
+          max_length=2 ** 20), UNS),
+])
+def test_attend(ctx, change, status):
+    assert _call(ctx, "lmop_attend", _paged(ctx, "lmop_attend", **change)) == status
+
+
+def test_attend_workspace(ctx):
+    def size(**change):
+        n = C.c_uint64(99)
+        st = L._lib.lmop_attend_workspace(ctx.ctx, C.byref(_paged(ctx, "lmop_attend", **change)), C.byref(n))
+        return st, n.value
+
+    assert size(workspace=None, q=None, out=None, cache_k=None) == (OK, 0)
+    assert size(batch_n_tokens=0) == (OK, 0)
+    assert size(max_length=129)[0] == INV
+    long = dict(batch_n_seqs=1, batch_n_tokens=1, max_tokens=1, batch_max_pages=2 ** 16, batch_ld_table=2 ** 16,
+                max_length=2 ** 20)
+    st, n = size(**long)
+    assert st == OK and n > 0 and n % (4 * 66 * 4) == 0
+    assert _call(ctx, "lmop_attend", _paged(ctx, "lmop_attend", **long, workspace_bytes=n - 1)) == INV
+    assert _call(ctx, "lmop_attend", _paged(ctx, "lmop_attend", **long, workspace_bytes=n)) == UNS
+    assert L._lib.lmop_attend_workspace(ctx.ctx, C.byref(_paged(ctx, "lmop_attend")), None) == INV
+    assert L._lib.lmop_attend_workspace(ctx.ctx, None, C.byref(C.c_uint64())) == INV
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(blocks=None), INV), (dict(blocks=P + 2), INV), (dict(cache_k_mean=None), INV), (dict(cache_k_mean=P + 2), INV),
+    (dict(n_blocks=0), OK), (dict(n_blocks=-1), INV), (dict(n_blocks=1024), UNS), (dict(n_blocks=1025), UNS),
+    (dict(max_length=-1), INV), (dict(max_length=16384 * 16), UNS), (dict(max_length=16384 * 16 + 1), UNS),
+    (dict(cache_k=None, cache_v=None, cache_dtype=77, cache_page_stride=0), UNS),
+])
+def test_select_blocks(ctx, change, status):
+    assert _call(ctx, "lmop_select_blocks", _paged(ctx, "lmop_select_blocks", **change)) == status
+
+
+@pytest.mark.parametrize("name", list(PAGED) + ["lmop_attend_workspace"])
+def test_paged_null(ctx, name):
+    extra = (None,) if name.endswith("workspace") else ()
+    assert getattr(L._lib, name)(ctx.ctx, None, *extra) == INV
+    assert getattr(L._lib, name)(None, None, *extra) == INV
+
+
+def _host_cache(dt=torch.float16, mean=None, pages=6, **kw):
+    k, v = (torch.zeros(pages, 4, 16, 64, dtype=dt) for _ in range(2))
+    if dt is F8:
+        kw.setdefault("k_exp", torch.zeros(pages, 4, 16, dtype=torch.uint8))
+        kw.setdefault("v_exp", torch.zeros(pages, 4, 16, dtype=torch.uint8))
+    return L.PagedCache(k, v, k_mean=mean, **kw)
+
+
+def test_binding_paged_valid_calls_reach_the_library(ctx):
+    x = torch.zeros(3, 256, dtype=torch.float16)
+    one = dict(table=torch.zeros(3, 2, dtype=torch.int32), length=torch.ones(3, dtype=torch.int32))
+    two = dict(one, start=torch.tensor([0, 1, 2, 3], dtype=torch.int32))
+    c = _host_cache(mean=torch.zeros(6, 4, 64, dtype=torch.float16))
+    for a in (one, two):
+        assert _status(ctx.cache_append, c, x, x, q=x, **a) == UNS
+        assert _status(ctx.attend, c, x, **a) == UNS
+        assert _status(ctx.attend, c, x, prefix=torch.zeros(2, dtype=torch.int32), prefix_length=30, **a) == UNS
+        assert _status(ctx.attend, c, x, blocks=torch.zeros(3, 4, 2, dtype=torch.int32), lse=torch.zeros(3, 4), **a) == UNS
+        assert _status(ctx.select_blocks, c, x, 2, **a) == UNS
+    assert _status(ctx.attend, _host_cache(F8), x.bfloat16(), **one) == UNS
+    assert _status(ctx.attend, c, x, max_length=33, **one) == INV
+
+
+def test_binding_paged_refuses(ctx):
+    x = torch.zeros(3, 256, dtype=torch.float16)
+    tab, ln, st = torch.zeros(3, 2, dtype=torch.int32), torch.ones(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    a = dict(table=tab, length=ln)
+    mean = torch.zeros(6, 4, 64, dtype=torch.float16)
+    c = _host_cache(mean=mean)
+    k = torch.zeros(6, 4, 16, 64, dtype=torch.float16)
+    for bad in (lambda: L.PagedCache(k[0], k[0]), lambda: L.PagedCache(k.float(), k.float()), lambda: L.PagedCache(k, k[:5]),
+                lambda: L.PagedCache(k, k.bfloat16()), lambda: L.PagedCache(k.transpose(1, 2), k.transpose(1, 2)),
+                lambda: L.PagedCache(k, torch.zeros(12, 4, 16, 64, dtype=torch.float16)[::2]),
+                lambda: L.PagedCache(k, k, k_exp=torch.zeros(6, 4, 16, dtype=torch.uint8)),
+                lambda: L.PagedCache(k.to(F8), k.to(F8)), lambda: _host_cache(F8, k_exp=torch.zeros(6, 4, 8, dtype=torch.uint8)),
+                lambda: _host_cache(F8, v_exp=torch.zeros(6, 4, 16)), lambda: _host_cache(mean=mean.bfloat16()),
+                lambda: _host_cache(mean=mean[:, :2]), lambda: _host_cache(F8, mean=mean.float()),
+                lambda: L.PagedCache(k, k.to("meta"))):
+        with pytest.raises(ValueError):
+            bad()
+    other = L.PagedCache(*(torch.zeros(6, 2, 16, 64, dtype=torch.float16) for _ in range(2)))
+    for f in (lambda **kw: ctx.attend(**{**dict(cache=c, q=x), **a, **kw}),
+              lambda **kw: ctx.select_blocks(**{**dict(cache=c, q=x, n_blocks=2), **a, **kw}),
+              lambda **kw: ctx.cache_append(**{**dict(cache=c, k=kw.get("q", x), v=x), **a, **kw})):
+        for kw in (dict(cache=other), dict(table=tab.long()), dict(table=tab.t()), dict(table=tab[:2]), dict(length=ln[:2]),
+                   dict(length=ln.float()), dict(start=st[:3]), dict(start=st.long()), dict(q=x.float()), dict(q=x[:, :128]),
+                   dict(q=x.bfloat16()), dict(q=x[:2])):
+            with pytest.raises(ValueError):
+                f(**kw)
+    for kw in (dict(out=x[:2]), dict(out=x.float()), dict(lse=torch.zeros(3, 3)), dict(lse=torch.zeros(3, 8)[:, :4]),
+               dict(lse=torch.zeros(3, 4, dtype=torch.float64)), dict(blocks=torch.zeros(3, 4, 2)),
+               dict(blocks=torch.zeros(3, 2, 2, dtype=torch.int32)), dict(blocks=torch.zeros(4, 3, 2, dtype=torch.int32).transpose(0, 1)),
+               dict(prefix_length=3), dict(prefix=tab[0], prefix_length=33), dict(prefix=tab[0].long(), prefix_length=3)):
+        with pytest.raises(ValueError):
+            ctx.attend(c, x, **a, **kw)
+    for kw in (dict(v=x[:2]), dict(v=x.bfloat16()), dict(q=x, q_out=x[:2])):
+        with pytest.raises(ValueError):
+            ctx.cache_append(c, x, **{"v": x, **a, **kw})
+    with pytest.raises(ValueError):
+        ctx.select_blocks(_host_cache(), x, 2, **a)
+    with pytest.raises(ValueError):
+        ctx.select_blocks(c, x, 2, out=torch.zeros(3, 4, 2), **a)
+    with pytest.raises(ValueError):  # a tensor of another device
+        ctx.attend(c, x.to("meta"), **a)
