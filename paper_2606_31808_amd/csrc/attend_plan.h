@@ -36,33 +36,53 @@ struct AttendPlan {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Divides `steps` among at most `want` splits of at least `least` steps and at most `most`; up to `whole`
-// steps stay together if `most` allows it.
-inline void split_steps(AttendLaunch& l, int64_t steps, int64_t want, int64_t least, int64_t most, int64_t whole = 0) {
+// Divides `steps` into n splits of equal chunks, of at most `most` steps
+inline void split_steps(AttendLaunch& l, int64_t steps, int64_t n, int64_t most) {
   if (steps < 1) steps = 1;
-  int64_t n = steps <= whole ? 1 : steps / least;
-  if (n > want) n = want;
   if (n < 1) n = 1;
   int64_t chunk = ceil_div(steps, n);
   if (chunk > most) chunk = most;
   l.chunk = (int)chunk;
   l.splits = (int)ceil_div(steps, chunk);
 }
+inline int64_t least_of(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// workgroups that fill the chip
-constexpr int kFewFill = 1024, kTileFill = 512, kWalkFill = 2048;
+// Splits of a few-vector launch of `workgroups` before it is split, over `keys` keys at most.  Joining parts takes a
+// second launch and some 4 us, in which a workgroup walks 512 keys, so up to 1024 stay together (16 blocks
+// of 64 for each of 256 workgroups: 42 us whole, 50 in four parts).  Two workgroups fit a CU: where the sequences
+// are alike, 512 of them are the fastest (us, with 1024 of them in brackets; 32 + 8 heads of 128: 16 sequences of
+// 8000 keys 100.6 (104.8), 64 of 2000 96.4 (101.0), 8-bit 4 of 32,000 48.7 (55.6) and 16 of 8000 48.5
+// (57.0)).  Where they are not, only some have keys in each split, and up to 1024 of long chunks balance
+// better: 32 of 1000 to 32,000, 8-bit, 244 us, of 512 workgroups 301.  Parts of at least 512 keys: one sequence of 4000
+// takes 15.8 us, in parts of 2048 24.8.
+inline int64_t few_splits(int64_t workgroups, int64_t keys) {
+  if (keys <= 1024) return 1;
+  const int64_t even = least_of(512 / workgroups, keys / 512), ragged = least_of(1024 / workgroups, keys / 4096);
+  return even > ragged ? even : ragged;
+}
+// Tile workgroups and waves that fill the chip
+constexpr int kTileFill = 512, kWalkFill = 2048;
 
 // Waves of a few-vector workgroup.  Where there are workgroups for less than half the CUs, eight: more of
 // their keys are on their way at once (573 keys of one row 8.8 -> 7.9 us).  Where there are two waves for
-// every SIMD without a second one in a workgroup, and few keys each, one: nothing is joined (256 rows
-// of up to 112 keys 22 -> 9 us).  The other part of a launch has four.
+// every SIMD without a second one in a workgroup, and few keys each, one: nothing is joined (256 rows of
+// up to 112 keys behind a prefix of 3900: 77 -> 73 us).  Beside a prefix's workgroups never eight.
 inline void pick_waves(AttendLaunch& l, const AttendSizes& s, bool pair) {
   const int64_t workgroups = (int64_t)l.tiles * s.nkv * l.splits, keys = (int64_t)l.chunk * s.page_size;
   l.waves = workgroups >= 2048 && keys <= 512 ? 1 : workgroups <= 128 && !pair ? 8 : 4;
 }
 
-// chosen blocks: vectors of a sequence from which waves walk the blocks of several tokens
-constexpr int kWalkLeast = 64;
+// Chosen blocks: from so many waves on, and vectors of a sequence, waves walk the blocks of several tokens.
+// us, walked against a workgroup a token (32 + 8 heads of 128, 16 of 500 blocks): one sequence of 256
+// tokens 94 / 73, 512 (512 waves) 121 / 147, 1000 199 / 274, 2000 327 / 521; eight of 64 167 / 140, of 128
+// 196 / 267; heads of 64: 256 tokens 70 / 39, 1000 133 / 144.
+constexpr int kWalkWaves = 640, kWalkLeast = 128;
+
+// Keys of the prefix that the sequences' workgroups would read, from which it is walked on its own, for
+// all sequences together: that takes another launch.  us, alone against with each (32 + 8 heads of 128):
+// 512 keys and 64 sequences (262144) 18 / 13, 128 of them 21 / 25, 256 26 / 45; 1024 and 32 19 / 16, 64 21 / 26;
+// 4096 and 8 (262144) 17 / 20, 16 26 / 30.
+constexpr int64_t kSharedKeys = 400000;
 
 inline AttendPlan plan_attend(const AttendSizes& s) {
   AttendPlan p;
@@ -70,9 +90,6 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
   const int64_t vectors = (int64_t)s.max_tokens * group;
   const int64_t pages = ceil_div(s.max_length, s.page_size);
   const int64_t prefix_pages = ceil_div(s.prefix_length, s.page_size);
-  // Joining parts takes a second launch and some 4 us, in which a few-vector workgroup walks 512 keys (1024
-  // keys for each of 256 workgroups: 42 us whole, 50 in two parts, with the choice of blocks before it)
-  const int64_t few_least = ceil_div(512, s.page_size), few_whole = ceil_div(1024, s.page_size);
   // tiles of `of` vectors: as many as the sequences need, found from the starts, or max_tokens' for each
   auto tiles = [&](AttendLaunch& l, int of) {
     const int64_t each = ceil_div(vectors, of);
@@ -80,9 +97,11 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     l.per_seq = s.n_seqs * each <= ragged ? (int)each : 0;
     l.tiles = (int)(l.per_seq ? s.n_seqs * each : ragged);
   };
-  if (s.n_blocks > 0 && s.starts && (int64_t)s.n_tokens * group >= (int64_t)kWalkLeast * s.n_seqs) {
+  if (s.n_blocks > 0 && s.starts && (int64_t)s.n_tokens * group >= (int64_t)kWalkLeast * s.n_seqs &&
+      (int64_t)s.n_tokens * group / kWalkVectors * s.nkv >= kWalkWaves) {
     tiles(p.own, kWalkVectors);
-    split_steps(p.own, ceil_div(pages, kWalkWindow), kWalkFill / ((int64_t)p.own.tiles * s.nkv), 1, 1 << 20);
+    const int64_t windows = ceil_div(pages, kWalkWindow);
+    split_steps(p.own, windows, least_of(kWalkFill / ((int64_t)p.own.tiles * s.nkv), windows), 1 << 20);
     p.parts = p.own.splits > 1 ? p.own.splits : 0;
     return p;
   }
@@ -90,33 +109,33 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     p.own.few = true;
     p.own.per_seq = (int)ceil_div(group, kFewVectors);  // of a token here
     p.own.tiles = s.n_tokens * p.own.per_seq;
-    split_steps(p.own, s.n_blocks, kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries, few_whole);
+    split_steps(p.own, s.n_blocks, few_splits((int64_t)p.own.tiles * s.nkv, (int64_t)s.n_blocks * s.page_size), kMaxEntries);
     pick_waves(p.own, s, false);
     p.parts = p.own.splits > 1 ? p.own.splits : 0;
     return p;
   }
   p.own.few = vectors <= kFewVectors || !s.starts;
-  const bool separate = s.prefix_length > 0 && p.own.few && s.n_seqs > 1;
+  const bool separate = p.own.few && (int64_t)s.n_seqs * s.nkv * s.prefix_length >= kSharedKeys;
   if (p.own.few) {
     p.own.per_seq = (int)ceil_div(vectors, kFewVectors);
     p.own.tiles = s.n_seqs * p.own.per_seq;
-    split_steps(p.own, pages + (separate ? 0 : prefix_pages),
-                kFewFill / ((int64_t)p.own.tiles * s.nkv), few_least, kMaxEntries, few_whole);
+    const int64_t walked = pages + (separate ? 0 : prefix_pages);
+    split_steps(p.own, walked, few_splits((int64_t)p.own.tiles * s.nkv, walked * s.page_size), kMaxEntries);
     pick_waves(p.own, s, separate);
   } else {
     tiles(p.own, kTileVectors);
-    split_steps(p.own, ceil_div(s.max_length, kTileKeys) + ceil_div(s.prefix_length, kTileKeys),
-                kTileFill / ((int64_t)p.own.tiles * s.nkv), 8, 1 << 30);
+    const int64_t blocks = ceil_div(s.max_length, kTileKeys) + ceil_div(s.prefix_length, kTileKeys);
+    split_steps(p.own, blocks, least_of(kTileFill / ((int64_t)p.own.tiles * s.nkv), blocks / 8), 1 << 30);
   }
   if (separate) {
     const int64_t all = (int64_t)s.n_tokens * group;
     p.prefix.few = all <= 2 * kFewVectors;
     p.prefix.tiles = (int)ceil_div(all, p.prefix.few ? kFewVectors : kTileVectors);
+    const int64_t workgroups = (int64_t)p.prefix.tiles * s.nkv, blocks = ceil_div(s.prefix_length, kTileKeys);
     if (p.prefix.few)
-      split_steps(p.prefix, prefix_pages, kFewFill / ((int64_t)p.prefix.tiles * s.nkv), few_least, kMaxEntries, few_whole);
+      split_steps(p.prefix, prefix_pages, few_splits(workgroups, s.prefix_length), kMaxEntries);
     else
-      split_steps(p.prefix, ceil_div(s.prefix_length, kTileKeys), kTileFill / ((int64_t)p.prefix.tiles * s.nkv),
-                  4, 1 << 30);
+      split_steps(p.prefix, blocks, least_of(kTileFill / workgroups, blocks / 4), 1 << 30);
   }
   p.parts = p.own.splits + (separate ? p.prefix.splits : 0);
   if (p.parts == 1) p.parts = 0;

@@ -1854,9 +1854,11 @@ lmop_status lmop_create(const lmop_config* cfg, int32_t device, void* hip_stream
   // rotary table: cos/sin of pos * theta^(-2i/hd) in double, stored fp32
   const int half = cf.head_dim / 2;
   std::vector<float2> tab((size_t)cf.max_seq * half);
+  std::vector<double> freq(half);
+  for (int i = 0; i < half; ++i) freq[i] = std::pow((double)cf.rope_theta, -2.0 * i / cf.head_dim);
   for (int p = 0; p < cf.max_seq; ++p)
     for (int i = 0; i < half; ++i) {
-      const double ang = (double)p * std::pow((double)cf.rope_theta, -2.0 * i / cf.head_dim);
+      const double ang = (double)p * freq[i];
       tab[(size_t)p * half + i] = make_float2((float)std::cos(ang), (float)std::sin(ang));
     }
   void* rt = nullptr;

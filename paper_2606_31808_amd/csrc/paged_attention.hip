@@ -1258,42 +1258,58 @@ LMOP_DEVICE void tile_vectors(const Args& a, int block, int split, char* smem) {
 }
 
 // ---------------------------------------------------------------- joining the parts
-// A group of hd / 4 lanes a (token, head): out = sum_i f_i o_i / sum_i f_i l_i with
-// f_i = 2^(c (m_i - max m)), parts in order.
-template <typename T, int HD>
+// out = sum_i f_i o_i / sum_i f_i l_i with f_i = 2^(c (m_i - max m)), in a fixed order.  A group of hd / 4 lanes
+// takes a (token, head); of more than 8 parts a workgroup does, whose groups share them, as each part
+// costs a group two dependent loads (one sequence of 32,000 keys in 62 parts: 63 -> 31 us).
+struct Sum {
+  f32x4 o;
+  float m, l;
+};
+LMOP_DEVICE void add_part(Sum& s, float m, float l, const f32x4& o, float c) {
+  if (l != l) {
+    s.l = l;
+    return;
+  }
+  if (l == 0.f) return;  // it saw nothing, and may not have written its outputs
+  const float m_new = m > s.m ? m : s.m, f = rescale(m, m_new, c), g = rescale(s.m, m_new, c);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) s.o[r] = s.o[r] * g + o[r] * f;
+  s.l = s.l * g + l * f;
+  s.m = m_new;
+}
+
+template <typename T, int HD, bool WIDE>
 __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
-  constexpr int LANES = HD / 4;
+  constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
   const lmop_attend_args& p = a.t;
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
-  const int d = threadIdx.x % LANES * 4;
+  const int group = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
+  const int64_t i = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * GROUPS + group;
   if (i >= (int64_t)p.batch.n_tokens * a.n.nq) return;
   const int t = (int)(i / a.n.nq), h = (int)(i % a.n.nq);
   if (p.batch.start && (t < p.batch.start[0] || t >= p.batch.start[p.batch.n_seqs])) return;
-  float m = -INFINITY;
-  for (int q = 0; q < a.parts; ++q) m = fmaxf(m, part_ml(a, q, t, h)->x);
-  f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (int q = 0; q < a.parts; ++q) {
+  Sum s{f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
+  for (int q = WIDE ? group : 0; q < a.parts; q += WIDE ? GROUPS : 1) {
     const float2 ml = *part_ml(a, q, t, h);
-    if (ml.y != ml.y) {
-      l = ml.y;
-      continue;
-    }
-    // (a part that saw nothing may not have written its outputs)
-    if (ml.y == 0.f) continue;
-    const float f = rescale(ml.x, m, a.c);
-    l += ml.y * f;
-    const f32x4 x = *(const f32x4*)(part_o(a, q, t, h) + d);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] += x[r] * f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (ml.y > 0.f) o = *(const f32x4*)(part_o(a, q, t, h) + d);
+    add_part(s, ml.x, ml.y, o, a.c);
   }
-  const float inv = 1.0f / l;
+  if constexpr (WIDE) {
+    __shared__ f32x4 s_o[GROUPS][LANES];
+    __shared__ float s_m[GROUPS], s_l[GROUPS];
+    s_o[group][threadIdx.x % LANES] = s.o;
+    if (d == 0) s_m[group] = s.m, s_l[group] = s.l;
+    __syncthreads();
+    if (group > 0) return;
+    for (int q = 1; q < GROUPS; ++q) add_part(s, s_m[q], s_l[q], s_o[q][threadIdx.x % LANES], a.c);
+  }
+  const float inv = 1.0f / s.l;
   typedef T xo __attribute__((ext_vector_type(4), aligned(2)));
   xo r;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) r[k] = (T)(l == 0.f ? 0.f : y[k] * inv);
+  for (int k = 0; k < 4; ++k) r[k] = (T)(s.l == 0.f ? 0.f : s.o[k] * inv);
   *(xo*)((T*)p.out + t * p.ldo + h * HD + d) = r;
-  if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + h] = lse_of(a, m, l);
+  if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + h] = lse_of(a, s.m, s.l);
 }
 
 // ---------------------------------------------------------------- kernels
@@ -1401,7 +1417,10 @@ hipError_t launch(hipStream_t s, const lmop_attend_args& t, const Heads& n, cons
   }
   if (e != hipSuccess || plan.parts == 0) return e;
   const int64_t groups = (int64_t)t.batch.n_tokens * n.nq, per = 256 / (HD / 4);
-  hipLaunchKernelGGL((combine_kernel<T, HD>), dim3((unsigned)((groups + per - 1) / per)), dim3(256), 0, s, a);
+  if (plan.parts > 8)
+    hipLaunchKernelGGL((combine_kernel<T, HD, true>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((combine_kernel<T, HD, false>), dim3((unsigned)((groups + per - 1) / per)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -142,33 +142,36 @@ def _reference(b, blocks=None, scale=None):
         k, v = (torch.cat((pre[j], b.keys_of(s, i, pool))) for j, (s, pool) in enumerate((("k", kp), ("v", vp))))
         here = b.lead + sum(b.new[:i])
         index = torch.arange(k.shape[0]) - b.prefix  # of an own key
-        for h in range(nq):
-            kh, vh, qh = k[:, h * nkv // nq], v[:, h * nkv // nq], q[here:here + n, h]
-            for j in range(n):
-                seen = index <= m - n + j
-                if blocks is not None:
-                    seen = seen & torch.isin(index // b.page, blocks[here + j, h * nkv // nq])
-                out[here + j, h] = 0
-                lse[here + j, h] = -math.inf
-                if not seen.any():
-                    continue
-                ks, vs = kh[seen], vh[seen]
-                prod = ks * qh[j]
-                z = prod.sum(-1) * scale
-                w = torch.exp(z - z.max())
-                total = w.sum()
-                out[here + j, h] = (w[:, None] * vs).sum(0) / total
-                lse[here + j, h] = z.max() + total.log()
-                most = float(z.abs().max())
-                e_score = hd * 2.0 ** -23 * float(prod.abs().sum(-1).max()) * scale + 4 * most * 2.0 ** -23 + 2.0 ** -21
-                size = (w[:, None] * vs.abs()).sum(0) / total
-                N = len(ks)
-                tol[here + j, h] = size * (2 * (eps / 2 + e_score) + 2 * (N + 64) * 2.0 ** -23)
-                if b.dt == torch.float16:
-                    tol[here + j, h] += 2 * 2.0 ** -25 * (vs.abs().sum(0) + N * size) + 2.0 ** -25
-                tol_lse[here + j, h] = e_score + eps / 2 + (N + 64) * 2.0 ** -23 + float(lse[here + j, h].abs()) * 2.0 ** -22
-                if b.dt == torch.float16:
-                    tol_lse[here + j, h] += N * 2.0 ** -25
+        kh, vh = k.transpose(0, 1).contiguous(), v.transpose(0, 1).contiguous()  # [nkv][keys][hd]
+        for j in range(n):
+            t = here + j
+            seen = (index <= m - n + j).expand(nkv, -1)
+            if blocks is not None:
+                seen = seen & (index[None, :, None] // b.page == blocks[t][:, None]).any(-1)
+            seen = seen[:, None]
+            # what is not seen may hold anything
+            ks = torch.where(seen[..., None], kh[:, None], 0.0)[:, 0]
+            vs = torch.where(seen[..., None], vh[:, None], 0.0)[:, 0]
+            qh = q[t].view(nkv, -1, hd)
+            z = torch.where(seen, torch.matmul(qh, ks.transpose(1, 2)) * scale, -math.inf)
+            mag = torch.matmul(qh.abs(), ks.abs().transpose(1, 2)).amax(-1) if k.shape[0] else torch.zeros(nkv, nq // nkv)
+            top = z.amax(-1, keepdim=True) if k.shape[0] else torch.full((nkv, nq // nkv, 1), -math.inf)
+            none = torch.isinf(top)
+            w = torch.where(none, 0.0, torch.exp(z - torch.where(none, 0.0, top)))
+            total = w.sum(-1, keepdim=True)
+            total = torch.where(none, 1.0, total)
+            out[t] = (torch.matmul(w, vs) / total).view(nq, hd)
+            lse[t] = torch.where(none, -math.inf, top + total.log()).view(nq)
+            most = torch.where(seen, z.abs(), 0.0).amax(-1, keepdim=True) if k.shape[0] else torch.zeros_like(top)
+            e_score = hd * 2.0 ** -23 * mag[..., None] * scale + 4 * most * 2.0 ** -23 + 2.0 ** -21
+            size = torch.matmul(w, vs.abs()) / total
+            N = seen.sum(-1, keepdim=True).double()
+            tt = size * (2 * (eps / 2 + e_score) + 2 * (N + 64) * 2.0 ** -23)
+            tl = e_score + eps / 2 + (N + 64) * 2.0 ** -23 + lse[t].view(nkv, -1, 1).abs() * 2.0 ** -22
+            if b.dt == torch.float16:
+                tt = tt + 2 * 2.0 ** -25 * (vs.abs().sum(1, keepdim=True) + N * size) + 2.0 ** -25
+                tl = tl + N * 2.0 ** -25
+            tol[t], tol_lse[t] = tt.reshape(nq, hd), tl.reshape(nq)
     tol = tol + eps / 2 * (out.abs() + tol)
     return out.view(b.tokens, -1), lse, tol.view(b.tokens, -1), tol_lse
 
@@ -221,9 +224,9 @@ def test_attend_single_tokens(L, dtype, cache, hd, nq, nkv, page, length, prefix
 
 LONG = [(4, 1, 16, [9001, 700], 0), (8, 2, 64, [5000], 0), (4, 2, 32, [3], 4100), (2, 1, 64, [30] * 3, 3001)]
 # many sequences: a wave each, or four
-MANY = [(8, 8, 16, [i % 70 for i in range(300)], 0), (16, 8, 32, [i % 90 for i in range(260)], 50),
-        (4, 2, 16, [6 * i for i in range(100)], 0), (4, 2, 16, [3 * i for i in range(100)], 70),
-        (128, 128, 16, [i for i in range(16)], 20)]
+MANY = [(8, 8, 16, [i % 70 for i in range(300)], 0), (16, 8, 32, [i % 90 for i in range(260)], 200),
+        (4, 2, 16, [6 * i for i in range(100)], 0), (4, 2, 16, [3 * i for i in range(100)], 2100),
+        (128, 128, 16, [i for i in range(16)], 200), (4, 2, 64, [5 * i for i in range(16)], 12600)]
 
 
 @pytest.mark.parametrize("dtype,cache,hd", [("f16", "f16", 128), ("bf16", "bf16", 64), ("bf16", "e4m3", 128)])
@@ -561,8 +564,10 @@ def test_select(L, dtype, hd, nq, nkv, page, new, length, n_blocks):
 BLOCKS = [
     (4, 2, 16, [1, 1], [300, 20], 5), (8, 1, 64, [1], [1000], 9), (3, 3, 16, [5, 3], [5, 200], 4),
     (2, 2, 128, [2], [600], 3), (4, 2, 16, [3], [90], 200), (20, 1, 32, [2], [200], 4), (4, 2, 16, [1], [5000], 256),
-    (4, 2, 16, [40, 33], [300, 40], 5), (8, 1, 64, [50], [1500], 7), (3, 1, 128, [43], [700], 3),
-    (4, 4, 32, [130], [2000], 6), (8, 2, 16, [70], [3000], 9), (2, 1, 256, [70], [1000], 2),
+    (4, 2, 16, [40, 33], [300, 40], 5),
+    # many tokens of a sequence: waves walk the blocks of several
+    (64, 16, 16, [170, 165], [700, 600], 5), (64, 64, 32, [330], [900], 4), (48, 16, 64, [450], [1500], 7),
+    (64, 8, 128, [330], [2000], 6), (40, 1, 256, [520], [1000], 2), (64, 16, 16, [340], [5000], 9),
     (4, 2, 16, [1] * 90, [11 * i for i in range(90)], 40), (8, 8, 16, [1] * 270, [i % 100 for i in range(270)], 3)]
 
 
@@ -588,11 +593,11 @@ def test_attend_blocks(L, dtype, cache, hd, nq, nkv, page, new, length, n_blocks
 
 
 @pytest.mark.parametrize("dtype,cache,hd", LAYOUTS)
-@pytest.mark.parametrize("nq,nkv,new", [(8, 2, [40]), (2, 2, [3]), (1, 1, [70])])
+@pytest.mark.parametrize("nq,nkv,new", [(8, 2, [40]), (2, 2, [3]), (64, 16, [340]), (40, 1, [530])])
 def test_attend_blocks_unseen_keys_may_hold_anything(L, dtype, cache, hd, nq, nkv, new):
     """A block with infinities and NaN reaches the tokens that chose it only."""
     print("blocks unseen", dtype, cache, hd, nq, nkv, new, flush=True)
-    b = Batch(nq, nkv, hd, dtype, cache, 16, new, [400], seed=2)
+    b = Batch(nq, nkv, hd, dtype, cache, 16, new, [new[0] + 400], seed=2)
     g = _gen(3)
     n = new[0]
     blocks = torch.stack([torch.stack([torch.randperm(24, generator=g)[:5].sort()[0] for _ in range(nkv)])
