@@ -1259,8 +1259,9 @@ LMOP_DEVICE void tile_vectors(const Args& a, int block, int split, char* smem) {
 
 // ---------------------------------------------------------------- joining the parts
 // out = sum_i f_i o_i / sum_i f_i l_i with f_i = 2^(c (m_i - max m)), in a fixed order.  A group of hd / 4 lanes
-// takes a (token, head); of more than 8 parts a workgroup does, whose groups share them, as each part
-// costs a group two dependent loads (one sequence of 32,000 keys in 62 parts: 63 -> 31 us).
+// takes a (token, head), or, of at most 4096 of them, a workgroup, whose groups share the parts: each part
+// costs a group two dependent loads.  us, groups against workgroups: 32 of 62 parts 63 / 31, 128 of 7 21.2 / 18.8, 2048 of
+// a prefix of 4096 keys 30.9 / 24.5, but 8192 54.0 / 58.7 and 32,000 95.6 / 113.9.
 struct Sum {
   f32x4 o;
   float m, l;
@@ -1417,7 +1418,7 @@ hipError_t launch(hipStream_t s, const lmop_attend_args& t, const Heads& n, cons
   }
   if (e != hipSuccess || plan.parts == 0) return e;
   const int64_t groups = (int64_t)t.batch.n_tokens * n.nq, per = 256 / (HD / 4);
-  if (plan.parts > 8)
+  if (groups <= 4096)
     hipLaunchKernelGGL((combine_kernel<T, HD, true>), dim3((unsigned)groups), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((combine_kernel<T, HD, false>), dim3((unsigned)((groups + per - 1) / per)), dim3(256), 0, s, a);

@@ -745,8 +745,10 @@ def lmop_cache_append(ctx, heads, cache, k, v, table, length, start=None, first:
 
 
 def lmop_attend(ctx, heads, cache, q, out, table, length, start=None, max_tokens: int = 1, max_length: int = 0,
-                prefix=None, prefix_length: int = 0, blocks=None, scale: float = 0.0, lse=None) -> None:
-    """Attention of the tokens over their sequences' keys and a prefix; its workspace comes from torch."""
+                prefix=None, prefix_length: int = 0, blocks=None, scale: float = 0.0, lse=None,
+                workspace=None) -> None:
+    """Attention of the tokens over their sequences' keys and a prefix.  workspace(n), called if the call
+    needs one: a uint8 tensor of n bytes that stays as long as the ctx's stream may use it."""
     nq, nkv, hd = heads
     n, dt, dev = q.shape[0], q.dtype, q.get_device()
     if dt not in _TOKENS:
@@ -782,9 +784,11 @@ def lmop_attend(ctx, heads, cache, q, out, table, length, start=None, max_tokens
     st = _lib.lmop_attend_workspace(ctx, a, size)
     if st:
         _check(st, ctx)
-    if size.value:
-        ws = torch.empty(size.value, dtype=torch.uint8, device=q.device)
-        a = args(ws.data_ptr(), size.value)
+    if size.value and workspace is not None:
+        ws = workspace(size.value)
+        if ws.dtype is not torch.uint8 or ws.device != q.device or not ws.is_contiguous():
+            raise ValueError(f"workspace: expected contiguous uint8 on {q.device}")
+        a = args(ws.data_ptr(), ws.numel())
     st = _lib.lmop_attend(ctx, a)
     if st:
         _check(st, ctx)
@@ -981,7 +985,9 @@ class Context:
         if max_length is None:
             max_length = table.shape[1] * cache.page_size
         lmop_attend(self.ctx, self.heads, cache, q, out, table, length, start, max_tokens, max_length, prefix,
-                    prefix_length, blocks, scale, lse)
+                    prefix_length, blocks, scale, lse,
+                    # (freed with the call: the stream is torch's current one, which orders its next use)
+                    lambda size: torch.empty(size, dtype=torch.uint8, device=q.device))
         return out
 
     def select_blocks(self, cache, q, n_blocks, *, table, length, start=None, max_length=None, out=None):

@@ -303,7 +303,7 @@ def test_attend_tokens_that_see_nothing(L, dtype, cache, hd, new, length):
 
 
 @pytest.mark.parametrize("cache", ["f16", "e4m3"])
-@pytest.mark.parametrize("new,prefix", [([1, 1, 1], 0), ([1, 1, 1], 70), ([5, 3, 4], 70), ([40, 50, 60], 0),
+@pytest.mark.parametrize("new,prefix", [([1, 1, 1], 0), ([1, 1, 1], 70), ([1, 1, 1], 70000), ([5, 3, 4], 70), ([40, 50, 60], 0),
                                         ([40, 50, 60], 70)])
 def test_attend_pages_and_lengths_that_do_not_fit(L, cache, new, prefix):
     """Each makes its own tokens' results NaN and leaves the others'."""
@@ -365,7 +365,7 @@ def test_attend_a_dominant_key_is_its_value(L):
 @pytest.mark.parametrize("dtype,cache,hd", LAYOUTS[:6])
 def test_attend_strides_and_rows_of_no_sequence(L, dtype, cache, hd):
     print("strides", dtype, cache, hd, flush=True)
-    for new, prefix in (([1, 2, 1], 0), ([1, 2, 1], 33), ([30, 50], 33)):
+    for new, prefix in (([1, 2, 1], 0), ([1, 2, 1], 33), ([1, 2, 1], 70000), ([30, 50], 33)):
         b = Batch(4, 2, hd, dtype, cache, 16, new, [60, 70, 80][:len(new)], prefix, seed=6, lead=3, tail=5)
         _run(L, b)
         ctx = _ctx(L, 4, 2, hd)

@@ -392,3 +392,16 @@ def test_binding_paged_refuses(ctx):
         ctx.select_blocks(c, x, 2, out=torch.zeros(3, 4, 2), **a)
     with pytest.raises(ValueError):  # a tensor of another device
         ctx.attend(c, x.to("meta"), **a)
+
+
+def test_binding_attend_takes_its_workspace_from_the_caller(ctx):
+    """Below Context nothing says which stream torch's allocations would be ordered with."""
+    q, c = torch.zeros(1, 256, dtype=torch.float16), _host_cache()
+    a = (ctx.ctx, ctx.heads, c, q, torch.empty_like(q), torch.zeros(1, 2 ** 16, dtype=torch.int32), torch.ones(1, dtype=torch.int32))
+    assert _status(L.lmop_attend, *a, max_length=2 ** 20) == INV
+    for bad in (lambda n: torch.zeros(n), lambda n: torch.zeros(2 * n, dtype=torch.uint8)[::2],
+                lambda n: torch.zeros(n, dtype=torch.uint8, device="meta")):
+        with pytest.raises(ValueError):
+            L.lmop_attend(*a, max_length=2 ** 20, workspace=bad)
+    assert _status(L.lmop_attend, *a, max_length=2 ** 20, workspace=lambda n: torch.zeros(n - 1, dtype=torch.uint8)) == INV
+    assert _status(L.lmop_attend, *a, max_length=2 ** 20, workspace=lambda n: torch.zeros(n, dtype=torch.uint8)) == UNS
