@@ -60,8 +60,19 @@ inline int64_t few_splits(int64_t workgroups, int64_t keys) {
   const int64_t even = least_of(512 / workgroups, keys / 512), ragged = least_of(1024 / workgroups, keys / 4096);
   return even > ragged ? even : ragged;
 }
-// Tile workgroups and waves that fill the chip
-constexpr int kTileFill = 512, kWalkFill = 2048;
+// Splits of a tile launch of `workgroups` over `blocks` steps, with `outputs` = tokens x heads.  Up to two
+// workgroups a CU (up to four: 64 tokens over 32,000 keys 80 -> 109 us; one: 256 tokens 193 -> 230).  A step takes
+// some 1.2 us; each part more costs outputs / 2048 * 0.5 us, written and read once more, so that their sum is
+// least at sqrt(4800 blocks / outputs) parts.  us, at that many and at twice or half of them: 64 tokens over
+// 1000 keys 18 (25); prefixes of 8192 keys, 16 tokens 21 (24), of 4096, 32 tokens 23 (26), of 8192,
+// 64 tokens 31 (35), of 2048, 256 tokens 33 (44).
+inline int64_t tile_splits(int64_t workgroups, int64_t blocks, int64_t outputs) {
+  int64_t n = least_of(512 / workgroups, blocks / 2);
+  while (n > 1 && n * n * outputs > 4800 * blocks) --n;
+  return n;
+}
+// Waves of a walk that fill the chip
+constexpr int kWalkFill = 2048;
 
 // Waves of a few-vector workgroup.  Where there are workgroups for less than half the CUs, eight: more of
 // their keys are on their way at once (573 keys of one row 8.8 -> 7.9 us).  Where there are two waves for
@@ -114,6 +125,8 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     p.parts = p.own.splits > 1 ? p.own.splits : 0;
     return p;
   }
+  // (us, of sequences of up to 64 vectors with few-vector workgroups in brackets: 4 of 8 tokens of 4 heads over 2000 keys
+  // 23.4 (16.6), but 64 of 16 tokens 105 (173), whose keys each tile reads once)
   p.own.few = vectors <= kFewVectors || !s.starts;
   const bool separate = p.own.few && (int64_t)s.n_seqs * s.nkv * s.prefix_length >= kSharedKeys;
   if (p.own.few) {
@@ -125,17 +138,19 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
   } else {
     tiles(p.own, kTileVectors);
     const int64_t blocks = ceil_div(s.max_length, kTileKeys) + ceil_div(s.prefix_length, kTileKeys);
-    split_steps(p.own, blocks, least_of(kTileFill / ((int64_t)p.own.tiles * s.nkv), blocks / 8), 1 << 30);
+    split_steps(p.own, blocks, tile_splits((int64_t)p.own.tiles * s.nkv, blocks, (int64_t)s.n_tokens * s.nq), 1 << 30);
   }
   if (separate) {
     const int64_t all = (int64_t)s.n_tokens * group;
+    // (us, as tiles in brackets: 16 vectors over 8192 keys 16.3 (18.1), 32 of them 16.2 (19.1), but 64
+    // 21.9 (20.9))
     p.prefix.few = all <= 2 * kFewVectors;
     p.prefix.tiles = (int)ceil_div(all, p.prefix.few ? kFewVectors : kTileVectors);
     const int64_t workgroups = (int64_t)p.prefix.tiles * s.nkv, blocks = ceil_div(s.prefix_length, kTileKeys);
     if (p.prefix.few)
       split_steps(p.prefix, prefix_pages, few_splits(workgroups, s.prefix_length), kMaxEntries);
     else
-      split_steps(p.prefix, blocks, least_of(kTileFill / workgroups, blocks / 4), 1 << 30);
+      split_steps(p.prefix, blocks, tile_splits(workgroups, blocks, (int64_t)s.n_tokens * s.nq), 1 << 30);
   }
   p.parts = p.own.splits + (separate ? p.prefix.splits : 0);
   if (p.parts == 1) p.parts = 0;

@@ -1,7 +1,8 @@
 // Keys and values of a batch of tokens into the pages of a cache, with the
 // rotation on the way, the codes of 8-bit pages, and the mean key of every page that fills.
 //
-// Bound by memory: each element is read and written once.  A workgroup takes a page
+// Bound by memory: each element is read and written once (16,346 tokens of 32 + 8 heads of 128 into 8-bit
+// pages: 377 MB in 81 to 86 us, 4.4 to 4.7 TB/s; 8448 of heads of 64, with means, 106 MB in 24 to 28).  A workgroup takes a page
 // that the call touches, for one or all kv heads; a head of a token is held by hd / 16
 // lanes, lane j with dimensions 8j .. 8j+7 and the same of the upper half, so
 // that rotation pairs are in one lane, and a head's largest magnitude takes two or
@@ -134,12 +135,11 @@ LMOP_DEVICE void decode_codes(const uint2& w, float scale, float* y) {
   }
 }
 
-// Blocks below kv_blocks: (touched page, group of `heads` kv heads).  The others: a
-// wave takes `chunks` head chunks of a token's query, and goes on with every `waves`-th
-// (token, chunk range).
+// Blocks below kv_blocks: (touched page, group of `heads` kv heads).  The others: a wave takes a token's
+// query heads, whose angles are the same, and goes on with every `waves`-th token (272 rows of 60
+// tokens of 32 heads of 128 81 us; a wave for every four heads 108).
 template <typename T, bool E8, int HD>
-__global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a, int kv_blocks, int heads,
-                                                             int chunks, int splits) {
+__global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a, int kv_blocks, int heads) {
   constexpr int LPH = HD / 16, HPW = 64 / LPH;
   constexpr int KEYS = kWaves * HPW;  // of a pass
   const lmop_append_args& p = a.t;
@@ -149,9 +149,7 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
 
   if ((int)blockIdx.x >= kv_blocks) {
     const int waves = (int)(gridDim.x - kv_blocks) * kWaves;
-    const int64_t tasks = (int64_t)bt.n_tokens * splits;
-    for (int64_t task = ((int)blockIdx.x - kv_blocks) * kWaves + wave; task < tasks; task += waves) {
-      const int t = (int)(task / splits), c0 = (int)(task % splits) * chunks;
+    for (int t = ((int)blockIdx.x - kv_blocks) * kWaves + wave; t < bt.n_tokens; t += waves) {
       int s = t;
       if (bt.start) {
         if (t < bt.start[0] || t >= bt.start[bt.n_seqs]) continue;
@@ -162,9 +160,7 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
       const int64_t index = (int64_t)bt.length[s] - (tok.y - t);
       Angles w;
       if (p.rotate) w = load_angles(a, p.first + index, HD / 2, d);
-      for (int c = c0; c < c0 + chunks; ++c) {
-        const int h = c * HPW + lane / LPH;
-        if (h >= a.n.nq) continue;
+      for (int h = lane / LPH; h < a.n.nq; h += HPW) {
         Dims x = load_dims((const T*)p.q + t * p.ldq + h * HD + d, HD / 2);
         if (p.rotate) turn(x, w);
         store_dims((T*)p.q_out + t * p.ldqo + h * HD + d, HD / 2, x);
@@ -300,18 +296,17 @@ hipError_t launch(hipStream_t s, const AppendArgs& a) {
   const lmop_append_args& p = a.t;
   const int64_t items = p.batch.start ? p.batch.n_tokens / p.cache.page_size + 2ll * p.batch.n_seqs
                                       : p.batch.n_seqs;
-  // All kv heads in a workgroup take a page's angles once; one each spreads few pages over the chip.  us, all
-  // against one (8 + 32 heads of 128): 1000 tokens 15.2 / 11.4, 100 rows of 60 30.1 / 26.0, 272 rows of 60
-  // 81 / 86, 8448 tokens 34.7 / 38.4.
-  const int heads = p.batch.n_tokens >= 8192 ? a.n.nkv : 1;
+  // All kv heads in a workgroup take a page's angles once; one each spreads few pages over the chip, and does not
+  // make means one after the other.  us, all against one (8 + 32 heads, pages of 64): 1000 tokens 15.5 / 11.4,
+  // 4000 23.8 / 20.3, 8448 35.0 / 38.1, 16,384 79.9 / 82.1 (pages of 16 78 / 91); with means, heads of 64, 8448
+  // 30.5 / 23.6, 16,384 35.0 / 39.9.
+  const int heads = p.batch.n_tokens >= (p.cache.k_mean ? 16384 : 8192) ? a.n.nkv : 1;
   const int64_t kv_blocks = items * ((a.n.nkv + heads - 1) / heads);
-  const int per_wave = 64 / (HD / 16), all = (a.n.nq + per_wave - 1) / per_wave;
-  const int chunks = (int64_t)p.batch.n_tokens * all <= 10240 ? 1 : all, splits = all / chunks;
-  const int64_t want = ((int64_t)p.batch.n_tokens * splits + kWaves - 1) / kWaves;
+  const int64_t want = ((int64_t)p.batch.n_tokens + kWaves - 1) / kWaves;
   const int64_t q_blocks = !p.q ? 0 : want < 65536 ? want : 65536;
   if ((size_t)(kv_blocks + q_blocks) * 64 * kWaves > kMaxLaunchThreads) return hipErrorInvalidValue;
   hipLaunchKernelGGL((append_kernel<T, E8, HD>), dim3((unsigned)(kv_blocks + q_blocks)), dim3(64 * kWaves), 0, s,
-                     a, (int)kv_blocks, heads, chunks, splits);
+                     a, (int)kv_blocks, heads);
   return hipGetLastError();
 }
 

@@ -8,7 +8,9 @@
 // of a sum nor on what else is in the call.  Scores stay in LDS, and a wave picks the largest.
 //
 // Single tokens read each mean once, 16 bytes a lane, and are bound by that; tokens of one sequence are
-// taken 16 at a time, with the fp64 matrix instruction, and share the means.
+// taken 16 at a time, with the fp64 matrix instruction, and share the means.  32 contexts of 500 pages (8 kv
+// heads of 128: 31 MB): 12 us, of which some 8 are the launch and a workgroup's chain of page look-up,
+// means, choice; 2048 tokens of such a context: 73 us, of which 25 are the fp64 matrix instructions.
 #include "kernels.h"
 #include "paged.h"
 
@@ -370,9 +372,12 @@ hipError_t launch(hipStream_t s, const lmop_select_args& a, const Heads& n) {
   const lmop_batch& b = a.batch;
   int64_t pages = (a.max_length + (int64_t)a.cache.page_size - 1) / a.cache.page_size;
   if (pages < 1) pages = 1;
-  // Sequences of four tokens or more share their means, as long as four tokens' scores fit.
+  // Sequences of four tokens or more share their means, as long as four tokens' scores fit.  A workgroup of 16 tokens
+  // takes longer than one of a single token, so only where those would be more than run at once.  us, shared against
+  // single (8 kv heads of 128): 16 tokens of 469 pages 24.5 / 10.9, 64 20.3 / 18.1, 200 25.3 / 48.6; 256 of 63 or
+  // 125 pages 13.6 / 14.6, 14.9 / 15.9; 32 of 469 pages in sequences of two 22.1 / 11.4.
   const int tile = (int)(kScores / pages < kTileTokens ? kScores / pages : kTileTokens);
-  if (b.start && b.n_tokens / 4 >= b.n_seqs && tile >= 4) {
+  if (b.start && b.n_tokens / 4 >= b.n_seqs && tile >= 4 && (int64_t)b.n_tokens * n.nkv >= 1024) {
     const int64_t items = b.n_tokens / tile + b.n_seqs;
     const int lds = (int)(tile * pages * 8);
     const hipError_t e = allow_lds(select_tile_kernel<T, HD>, lds);
@@ -381,7 +386,7 @@ hipError_t launch(hipStream_t s, const lmop_select_args& a, const Heads& n) {
                        tile, (int)pages);
   } else {
     const int lds = (int)(pages * 8);
-    // enough waves for all means to be on their way at once
+    // enough waves for all means to be on their way at once (32 contexts of 500 pages: 11 us, with four waves 16)
     const bool many = pages > 4 * 64 / (HD / 8) * 8;
     const auto kernel = many ? select_one_kernel<T, HD, 16> : select_one_kernel<T, HD, 4>;
     const hipError_t e = allow_lds(kernel, lds);

@@ -528,8 +528,8 @@ def _choose(b, mean, n_blocks):
             for h in range(nkv):
                 # (sums of exact products, exact in any order but for infinities and NaN)
                 z = (q[t, h] * mean[b.table[i, :mine].long(), h].double()).sum(-1)
-                z = [-math.inf if x != x else x for x in z.tolist()]
-                best = sorted(range(mine), key=lambda x: (-z[x], x))[:n_blocks - 1]
+                z = torch.where(z.isnan(), -math.inf, z)
+                best = torch.argsort(-z, stable=True)[:n_blocks - 1].tolist()  # of equal ones the first
                 ids = sorted(best) + [mine]
                 out[t, h, :len(ids)] = torch.tensor(ids, dtype=torch.int32)
     return out
@@ -540,7 +540,10 @@ def _choose(b, mean, n_blocks):
     (4, 2, 16, [1, 1, 1], [5, 100, 700], 4), (8, 1, 64, [1], [4000], 16), (3, 3, 16, [5, 0, 20], [5, 30, 400], 3),
     (2, 2, 16, [2], [2100], 1), (4, 2, 32, [3], [500], 1000), (4, 1, 16, [4, 3], [2, 64], 2),
     (14, 2, 16, [1], [9000], 33), (4, 2, 16, [40, 17], [600, 333], 8), (6, 2, 16, [9], [24000], 5),
-    (2, 1, 16, [5], [70000], 3)])
+    (2, 1, 16, [5], [70000], 3),
+    # many tokens of a sequence share their means
+    (32, 32, 16, [40, 17], [600, 333], 8), (64, 16, 16, [70, 5, 0, 41], [800, 1, 3, 500], 5),
+    (16, 16, 16, [70], [17000], 6), (8, 8, 16, [133], [33700], 40)])
 def test_select(L, dtype, hd, nq, nkv, page, new, length, n_blocks):
     print("select", dtype, hd, nq, nkv, page, new, length, n_blocks, flush=True)
     b = Batch(nq, nkv, hd, dtype, dtype, page, new, length, seed=n_blocks)
