@@ -126,7 +126,7 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     return p;
   }
   // (us, of sequences of up to 64 vectors with few-vector workgroups in brackets: 4 of 8 tokens of 4 heads over 2000 keys
-  // 23.4 (16.6), but 64 of 16 tokens 105 (173), whose keys each tile reads once)
+  // 18.1 (16.6), but 64 of 16 tokens 109 (173), whose keys a tile reads once)
   p.own.few = vectors <= kFewVectors || !s.starts;
   const bool separate = p.own.few && (int64_t)s.n_seqs * s.nkv * s.prefix_length >= kSharedKeys;
   if (p.own.few) {
