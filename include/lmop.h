@@ -616,8 +616,8 @@ lmop_status lmop_attend_workspace(lmop_ctx* ctx, const lmop_attend_args* args, u
  * own (index / page_size), and of those before it the n_blocks - 1 with the largest
  *   score = (sum of the queries of the kv head's group) . k_mean of the page
  * in fp64 (exact for ordinary values); of equal ones the first.  A score that is NaN, or of a table
- * entry that names no page, counts as minus infinity.  blocks holds them in ascending order and -1 after them; all -1 for a token
- * whose index is negative or past the table, or a sequence whose length is above max_length. */
+ * entry that names no page, counts as minus infinity.  blocks holds them in
+ * ascending order and -1 after them; all -1 for a token whose index is negative or past the table, or a sequence whose length is above max_length. */
 typedef struct {
   lmop_cache cache;      /* k_mean, n_pages and page_size; the rest is not looked at */
   lmop_batch batch;

@@ -2,8 +2,8 @@
 // rotation on the way, the codes of 8-bit pages, and the mean key of every page that fills.
 //
 // Bound by memory: each element is read and written once (16,346 tokens of 32 + 8 heads of 128 into 8-bit
-// pages: 377 MB in 81 to 86 us, 4.4 to 4.7 TB/s; 8448 of heads of 64, with means, 106 MB in 24 to 28).  A workgroup takes a page
-// that the call touches, for one or all kv heads; a head of a token is held by hd / 16
+// pages: 377 MB in 81 to 86 us, 4.4 to 4.7 TB/s; 8448 of heads of 64, with means, 106 MB in 24 to 28).  A workgroup takes a
+// page that the call touches, for one or all kv heads; a head of a token is held by hd / 16
 // lanes, lane j with dimensions 8j .. 8j+7 and the same of the upper half, so
 // that rotation pairs are in one lane, and a head's largest magnitude takes two or
 // three exchanges between lanes.  Pages rather than tokens, because then the workgroup that
