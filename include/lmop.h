@@ -624,7 +624,8 @@ typedef struct {
   const void* q;         /* [n_tokens][n_heads * head_dim] */
   int32_t* blocks;       /* [n_tokens][n_kv_heads][n_blocks] */
   int64_t ldq;
-  int32_t n_blocks;      /* 1 .. 1024 */
+  int32_t n_blocks;      /* 0 .. 1024; 0: nothing is written (and lmop_attend takes n_blocks 0 for a call
+                            without lists) */
   int32_t max_length;    /* at least the longest length; at most 16384 pages' */
   int32_t dtype;         /* LMOP_F16 or LMOP_BF16, of q and k_mean */
 } lmop_select_args;

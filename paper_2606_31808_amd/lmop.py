@@ -724,6 +724,16 @@ def _batch(ctx_heads, cache, table, length, start, n_tokens, dtype, dev):
                        n_tokens)
 
 
+def _listed(blocks, n: int, nkv: int, dev: int) -> int:
+    """How many blocks are listed for each token and kv head.  None is refused: to the library n_blocks 0
+    is a call without lists, which attends to all keys."""
+    n_blocks = blocks.shape[-1] if blocks.dim() else 0
+    if (blocks.get_device() != dev or blocks.dtype != torch.int32 or blocks.shape != (n, nkv, n_blocks) or
+            n_blocks < 1 or not blocks.is_contiguous()):
+        raise ValueError(f"blocks: expected contiguous int32 [{n}, {nkv}, n_blocks], n_blocks at least 1, on device {dev}")
+    return n_blocks
+
+
 def lmop_cache_append(ctx, heads, cache, k, v, table, length, start=None, first: int = 0, rotate: bool = True,
                       q=None, q_out=None) -> None:
     """Rotates and appends keys and values to the sequences' pages; rotates queries into q_out."""
@@ -756,10 +766,7 @@ def lmop_attend(ctx, heads, cache, q, out, table, length, start=None, max_tokens
     own = (dt,)
     n_blocks = pb = 0
     if blocks is not None:
-        n_blocks = blocks.shape[-1]
-        if (blocks.get_device() != dev or blocks.dtype != torch.int32 or blocks.shape != (n, nkv, n_blocks) or
-                not blocks.is_contiguous()):
-            raise ValueError(f"blocks: expected contiguous int32 [{n}, {nkv}, n_blocks] on device {dev}")
+        n_blocks = _listed(blocks, n, nkv, dev)
         pb = blocks.data_ptr()
     pl = 0
     if lse is not None:
@@ -800,10 +807,7 @@ def lmop_select_blocks(ctx, heads, cache, q, blocks, table, length, start=None, 
     n, dt, dev = q.shape[0], q.dtype, q.get_device()
     if cache.k_mean is None:
         raise ValueError("the cache has no k_mean")
-    n_blocks = blocks.shape[-1]
-    if (blocks.get_device() != dev or blocks.dtype != torch.int32 or blocks.shape != (n, nkv, n_blocks) or
-            not blocks.is_contiguous()):
-        raise ValueError(f"blocks: expected contiguous int32 [{n}, {nkv}, n_blocks] on device {dev}")
+    n_blocks = _listed(blocks, n, nkv, dev)
     st = _lib.lmop_select_blocks(ctx, _PACK["select"](
         cache.packed, _batch(heads, cache, table, length, start, n, dt, dev), q.data_ptr(), blocks.data_ptr(),
         _ld(q, "q", n, nq * hd, (dt,), dev), n_blocks, max_length, _DTYPES[dt]))

@@ -405,3 +405,21 @@ def test_binding_attend_takes_its_workspace_from_the_caller(ctx):
             L.lmop_attend(*a, max_length=2 ** 20, workspace=bad)
     assert _status(L.lmop_attend, *a, max_length=2 ** 20, workspace=lambda n: torch.zeros(n - 1, dtype=torch.uint8)) == INV
     assert _status(L.lmop_attend, *a, max_length=2 ** 20, workspace=lambda n: torch.zeros(n, dtype=torch.uint8)) == UNS
+
+
+def test_binding_refuses_lists_of_no_blocks(ctx):
+    """They would reach the library as a call without lists, whose tokens attend to all their keys."""
+    x = torch.zeros(3, 256, dtype=torch.float16)
+    a = dict(table=torch.zeros(3, 2, dtype=torch.int32), length=torch.ones(3, dtype=torch.int32))
+    c = _host_cache(mean=torch.zeros(6, 4, 64, dtype=torch.float16))
+    none = torch.zeros(3, 4, 0, dtype=torch.int32)
+    with pytest.raises(ValueError, match="n_blocks at least 1"):
+        ctx.attend(c, x, blocks=none, **a)
+    with pytest.raises(ValueError, match="n_blocks at least 1"):
+        ctx.attend(c, x, blocks=none, prefix=torch.zeros(2, dtype=torch.int32), prefix_length=30, **a)
+    with pytest.raises(ValueError, match="n_blocks at least 1"):
+        ctx.attend(c, x, blocks=torch.tensor(0, dtype=torch.int32), **a)
+    with pytest.raises(ValueError, match="n_blocks at least 1"):
+        ctx.select_blocks(c, x, 0, **a)
+    with pytest.raises(ValueError, match="n_blocks at least 1"):
+        ctx.select_blocks(c, x, 2, out=none, **a)
