@@ -76,6 +76,13 @@ LMOP_DEVICE int find_seq(int n, int i, F&& base) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Between LDS accesses of a wave's lanes to the same place: the hardware does them in order, the compiler has
+// to keep them so.
+LMOP_DEVICE void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // The page of a sequence's keys b * page_size and on, or -1
 LMOP_DEVICE int page_of(const lmop_batch& b, int n_pages, int s, int block) {
   if (block < 0 || block >= b.max_pages) return -1;

@@ -245,10 +245,13 @@ struct WaveCore {
     }
   }
   uint32_t key_exp[2];
+  // (other lanes' rows are read in scores(): of the chunk before until here, of this one from here on)
   LMOP_DEVICE void stash_keys() {
     constexpr int RPL = 64 / CH;
+    wave_order();
 #pragma unroll
     for (int i = 0; i < KL; ++i) *(uint4*)(lds + key_at(i * RPL + lane / CH, lane % CH)) = kr[i];
+    wave_order();
     if constexpr (E8) {
       key_exp[0] = (kx.x >> (8 * (c & 3))) & 255u;
       key_exp[1] = (kx.y >> (8 * (c & 3))) & 255u;
@@ -422,12 +425,10 @@ LMOP_DEVICE void few_vectors(const Args& a, int block, int split, FewLds<T, E8, 
   const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
   // what the waves have written is there for all of them
   auto meet = [&]() {
-    if constexpr (WAVES == 1) {
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    } else {
+    if constexpr (WAVES == 1)
+      wave_order();
+    else
       __syncthreads();
-    }
   };
   const int tile = block / a.n.nkv, h = block % a.n.nkv;
   const int G = a.n.nq / a.n.nkv;

@@ -27,12 +27,6 @@ typedef double f64x4 __attribute__((ext_vector_type(4)));
 // a score as it is ranked: NaN, and that of a page that does not exist, as the least
 LMOP_DEVICE double ranked(double x, int page) { return page < 0 || x != x ? -INFINITY : x; }
 
-// a wave's own LDS accesses happen in order; the compiler has to keep them so
-LMOP_DEVICE void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // The sum over a lane and those below it; the largest of all lanes.  (Lanes that a step does not reach add
 // `old`, or keep their own.)
 template <int CTRL, int ROWS>
