@@ -13,14 +13,13 @@
 // means, choice; 2048 tokens of such a context: 73 us, of which 25 are the fp64 matrix instructions.
 #include "kernels.h"
 #include "paged.h"
+#include "select_plan.h"
 
 namespace lmop {
 
 namespace {
 
-constexpr int kTileWaves = 8;
-constexpr int kTileTokens = 16;
-constexpr int kScores = 16384;  // a workgroup holds at most (128 KB)
+constexpr int kTileWaves = kSelectTileWaves;
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
@@ -208,9 +207,9 @@ LMOP_DEVICE Choice settle(const lmop_select_args& p, int64_t index, int len, int
   return Choice{(int)mine, need, need == 0};
 }
 
-// One workgroup: a token and a kv head.
+// One workgroup: a token (from `first` on) and a kv head.
 template <typename T, int HD, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void select_one_kernel(const lmop_select_args p, const Heads n) {
+__global__ __launch_bounds__(64 * WAVES) void select_one_kernel(const lmop_select_args p, const Heads n, int first) {
   constexpr int kThreads = 64 * WAVES;
   constexpr int LANES = HD / 8;             // of a mean
   constexpr int PAGES = kThreads / LANES;   // of a pass
@@ -220,7 +219,7 @@ __global__ __launch_bounds__(64 * WAVES) void select_one_kernel(const lmop_selec
   extern __shared__ __attribute__((aligned(16))) double s_score[];
   const lmop_batch& bt = p.batch;
   const int tid = threadIdx.x;
-  const int t = blockIdx.x / n.nkv, h = blockIdx.x % n.nkv;
+  const int t = first + blockIdx.x / n.nkv, h = blockIdx.x % n.nkv;
   const int G = n.nq / n.nkv;
   int s = t;
   if (bt.start) {
@@ -271,19 +270,19 @@ __global__ __launch_bounds__(64 * WAVES) void select_one_kernel(const lmop_selec
   if (tid < 64) pick(s_score, c.mine, c.need, s_count, out);
 }
 
-// One workgroup: up to 16 tokens of a sequence (a.tile) and a kv head.  Scores are a product of the
+// One workgroup: up to 16 tokens of a sequence (tile number `first` and on) and a kv head.  Scores are a product of the
 // tokens' queries and 16 means at a time: lane 16 g + c has token c's dimensions g * HD / 4 .. as the
 // one operand and page c's as the other, and gets tokens 4 r + g of page c.
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kTileWaves) void select_tile_kernel(const lmop_select_args p, const Heads n, int tile,
-                                                               int pages) {
+__global__ __launch_bounds__(64 * kTileWaves) void select_tile_kernel(const lmop_select_args p, const Heads n, int first,
+                                                               int tile, int pages) {
   constexpr int DIMS = HD / 4;
   __shared__ __attribute__((aligned(16))) int s_count[kTileWaves][256];
   extern __shared__ __attribute__((aligned(16))) double s_score[];  // [tile][pages]
   const lmop_batch& bt = p.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15;
-  const int item = blockIdx.x / n.nkv, h = blockIdx.x % n.nkv;
+  const int item = first + blockIdx.x / n.nkv, h = blockIdx.x % n.nkv;
   const int G = n.nq / n.nkv;
   auto base = [&](int i) { return seq_tokens(bt, i).x / tile + i; };
   const int s = find_seq(bt.n_seqs, item, base);
@@ -364,30 +363,23 @@ hipError_t allow_lds(K kernel, int lds) {
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const lmop_select_args& a, const Heads& n) {
   const lmop_batch& b = a.batch;
-  int64_t pages = (a.max_length + (int64_t)a.cache.page_size - 1) / a.cache.page_size;
-  if (pages < 1) pages = 1;
-  // Sequences of four tokens or more share their means, as long as four tokens' scores fit.  A workgroup of 16 tokens
-  // takes longer than one of a single token, so only where those would be more than run at once.  us, shared against
-  // single (8 kv heads of 128): 16 tokens of 469 pages 24.5 / 10.9, 64 20.3 / 18.1, 200 25.3 / 48.6; 256 of 63 or
-  // 125 pages 13.6 / 14.6, 14.9 / 15.9; 32 of 469 pages in sequences of two 22.1 / 11.4.
-  const int tile = (int)(kScores / pages < kTileTokens ? kScores / pages : kTileTokens);
-  if (b.start && b.n_tokens / 4 >= b.n_seqs && tile >= 4 && (int64_t)b.n_tokens * n.nkv >= 1024) {
-    const int64_t items = b.n_tokens / tile + b.n_seqs;
-    const int lds = (int)(tile * pages * 8);
-    const hipError_t e = allow_lds(select_tile_kernel<T, HD>, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((select_tile_kernel<T, HD>), dim3((unsigned)(items * n.nkv)), dim3(64 * kTileWaves), lds, s, a, n,
-                       tile, (int)pages);
-  } else {
-    const int lds = (int)(pages * 8);
-    // enough waves for all means to be on their way at once (32 contexts of 500 pages: 11 us, with four waves 16)
-    const bool many = pages > 4 * 64 / (HD / 8) * 8;
-    const auto kernel = many ? select_one_kernel<T, HD, 16> : select_one_kernel<T, HD, 4>;
+  const SelectPlan plan =
+      plan_select(SelectSizes{b.n_seqs, b.n_tokens, a.max_length, a.cache.page_size, n.nkv, n.hd, b.start != nullptr});
+  const int lds = (plan.tile ? plan.tile : 1) * plan.pages * 8;
+  const dim3 threads(64 * plan.waves);
+  auto queue = [&](auto kernel, auto... more) {
     const hipError_t e = allow_lds(kernel, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)b.n_tokens * n.nkv)), dim3(64 * (many ? 16 : 4)), lds, s, a, n);
-  }
-  return hipGetLastError();
+    for (int64_t first = 0; first < plan.items; first += plan.each) {
+      const int64_t items = plan.items - first < plan.each ? plan.items - first : plan.each;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(items * n.nkv)), threads, lds, s, a, n, (int)first, more...);
+      const hipError_t l = hipGetLastError();
+      if (l != hipSuccess) return l;
+    }
+    return hipSuccess;
+  };
+  if (plan.tile) return queue(select_tile_kernel<T, HD>, plan.tile, plan.pages);
+  return plan.waves == 16 ? queue(select_one_kernel<T, HD, 16>) : queue(select_one_kernel<T, HD, 4>);
 }
 
 }  // namespace
