@@ -80,6 +80,23 @@ LMOP_DEVICE float2* part_ml(const Args& a, int part, int t, int h) {
 // only where a score exceeds it by more than 2^8 in weight, so that the sums are seldom rescaled.
 LMOP_DEVICE float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
 
+// Weights are 2^(c z - c m) in one multiply-add of c m, rounded: off by half a step of c m, one factor for all of a
+// vector's weights, which its division takes away.  From 2^20 on, where that factor leaves 2^(1/32) (at 2^30 it is up to
+// 2^64, past either end of the weights' types), scores are taken from the reference before the scale: exact next to it.
+// Vectors apart, so that one's large scores leave another's bits.
+template <int N>
+LMOP_DEVICE float from_reference(f32x4 (&st)[N], float m, float c) {
+  const float ref = ref_of(m), nmc = -ref * c;
+  const bool far = fabsf(nmc) > 0x1p20f;
+  if (!__any(far)) return nmc;
+  const float off = far ? ref : 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) st[i][r] -= off;
+  return far ? 0.f : nmc;
+}
+
 // exp2 of a difference of references, 0 where there was none
 LMOP_DEVICE float rescale(float m_old, float m_new, float c) {
   return m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - m_new) * c);
@@ -305,7 +322,7 @@ struct WaveCore {
   }
 
   // the vectors' weights of the chunk and their sums; the states move to a new reference where needed
-  LMOP_DEVICE x8 weights(int qs, const f32x4 (&st)[2], float cs, float thr) {
+  LMOP_DEVICE x8 weights(int qs, f32x4 (&st)[2], float cs, float thr) {
     const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
     float mb = max3(st[0][0], st[0][1], st[0][2]);
     mb = max3(mb, st[0][3], st[1][0]);
@@ -319,7 +336,7 @@ struct WaveCore {
       for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
       m[qs] = m_new;
     }
-    const float nmc = -ref_of(m[qs]) * cs;
+    const float nmc = from_reference(st, m[qs], cs);
     x8 pb;
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
@@ -1021,7 +1038,7 @@ struct TileCore {
   }
 
   // The vectors' weights of the block and their sums; the states move to a new reference where needed
-  LMOP_DEVICE void weights(int qs, const f32x4 (&st)[4], float cs, float thr, x8 (&pb)[2]) {
+  LMOP_DEVICE void weights(int qs, f32x4 (&st)[4], float cs, float thr, x8 (&pb)[2]) {
     const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
     float mb = max3(st[0][0], st[0][1], st[0][2]);
     mb = max3(mb, st[0][3], st[1][0]);
@@ -1039,7 +1056,7 @@ struct TileCore {
       for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
       m[qs] = m_new;
     }
-    const float nmc = -ref_of(m[qs]) * cs;
+    const float nmc = from_reference(st, m[qs], cs);
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
