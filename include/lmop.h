@@ -582,9 +582,8 @@ lmop_status lmop_cache_append(lmop_ctx* ctx, const lmop_append_args* args);
  * instance, stands for none; one listed twice counts once).  A key that
  * a token does not see has no effect on its result, whatever it or its value holds.  A token
  * that sees no key, or only scores of minus infinity, gets zeros and lse = -inf.
- * Scores, sums and outputs are held in fp32; the weights are rounded to dtype for the
- * product with the values, and the sum that divides is that of the rounded
- * ones.
+ * Scores, weights, sums and outputs are held in fp32; for the product with the values a weight is two terms
+ * of dtype, 2^-16 of it off (LMOP_F16: 2^-22, or 2^-32 of the largest).
  * NaN results: for every token of a sequence of more than max_tokens tokens, or whose length is
  * below 0 or above max_length; for a token that sees a key whose page does not
  * exist. */

@@ -26,9 +26,10 @@
 // All compute S^T = K Q^T and O^T = V^T P^T with the 16x16x32 instruction, so
 // that scores, maxima and outputs of a query vector stay in one column of lanes
 // (lane 16 g + c: vector c) and P^T leaves the first product in the layout that
-// the second one reads, if key rows are taken in score_key's order.  Row sums of
-// P come from the same instruction, with ones for V^T: they are then the sums of the rounded
-// weights, and cost the vector units nothing.
+// the second one reads, if key rows are taken in score_key's order.  P is held in two terms of the type
+// (Weights), each with a product of its own: to 16 bits and more, as the fp32 around it.  Row sums of
+// P come from the same instruction, with ones for V^T: they are then the sums of the weights as multiplied,
+// and cost the vector units nothing.
 #include <math.h>
 
 #include "attend_plan.h"
@@ -85,16 +86,16 @@ LMOP_DEVICE float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
 // 2^64, past either end of the weights' types), scores are taken from the reference before the scale: exact next to it.
 // Vectors apart, so that one's large scores leave another's bits.
 template <int N>
-LMOP_DEVICE float from_reference(f32x4 (&st)[N], float m, float c) {
+LMOP_DEVICE float from_reference(f32x4 (&st)[N], float m, float c, float lift) {
   const float ref = ref_of(m), nmc = -ref * c;
   const bool far = fabsf(nmc) > 0x1p20f;
-  if (!__any(far)) return nmc;
+  if (!__any(far)) return nmc + lift;
   const float off = far ? ref : 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) st[i][r] -= off;
-  return far ? 0.f : nmc;
+  return far ? lift : nmc + lift;
 }
 
 // exp2 of a difference of references, 0 where there was none
@@ -148,9 +149,11 @@ LMOP_DEVICE void write_bad(const Args& a, int t, int h, int part, int lane, int 
   if (lane == 0 && a.t.lse) a.t.lse[(size_t)t * a.n.nq + h] = NAN;
 }
 
+template <typename T>
 LMOP_DEVICE float lse_of(const Args& a, float m, float l) {
-  // l > 0 means that some score was finite
-  return l == 0.f ? -INFINITY : (m * a.c + __log2f(l)) * 0.6931471805599453f;
+  // l > 0 means that some score was finite (the lift taken off before the logarithm, where that is exact)
+  constexpr float kDown = 1.f / (1 << (int)Weights<T>::kLift);
+  return l == 0.f ? -INFINITY : (m * a.c + __log2f(l * kDown)) * 0.6931471805599453f;
 }
 
 // A value that one vector of a workgroup sees and another does not must not reach the second one, but
@@ -322,7 +325,7 @@ struct WaveCore {
   }
 
   // the vectors' weights of the chunk and their sums; the states move to a new reference where needed
-  LMOP_DEVICE x8 weights(int qs, f32x4 (&st)[2], float cs, float thr) {
+  LMOP_DEVICE Weights<T> weights(int qs, f32x4 (&st)[2], float cs, float thr) {
     const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
     float mb = max3(st[0][0], st[0][1], st[0][2]);
     mb = max3(mb, st[0][3], st[1][0]);
@@ -336,20 +339,15 @@ struct WaveCore {
       for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
       m[qs] = m_new;
     }
-    const float nmc = from_reference(st, m[qs], cs);
-    x8 pb;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(st[hf][r], cs, nmc)),
-                         __builtin_amdgcn_exp2f(__builtin_fmaf(st[hf][r + 1], cs, nmc))};
-        const x2 y = __builtin_convertvector(e, x2);
-        pb[4 * hf + r] = y[0];
-        pb[4 * hf + r + 1] = y[1];
-      }
-    l4[qs] = Half<T>::mfma(ones, pb, l4[qs]);
+    const float nmc = from_reference(st, m[qs], cs, Weights<T>::kLift);
+    Weights<T> pb;
+    auto weight = [&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, cs, nmc)); };
+    pb.template set<0>(weight(st[0][0]), weight(st[0][1]));
+    pb.template set<2>(weight(st[0][2]), weight(st[0][3]));
+    pb.template set<4>(weight(st[1][0]), weight(st[1][1]));
+    pb.template set<6>(weight(st[1][2]), weight(st[1][3]));
+    l4[qs] = Half<T>::mfma(ones, pb.hi, l4[qs]);
+    l4[qs] = Half<T>::mfma(ones, pb.lo, l4[qs]);
     return pb;
   }
 
@@ -384,7 +382,7 @@ struct WaveCore {
   }
 
   // O^T += V^T P^T.  Tile i: dimension NT c + i of the lane group's 8 keys
-  LMOP_DEVICE void product(const uint32_t (&w)[8][NT / 2], const x8 (&pb)[QS]) {
+  LMOP_DEVICE void product(const uint32_t (&w)[8][NT / 2], const Weights<T> (&pb)[QS]) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
@@ -393,7 +391,9 @@ struct WaveCore {
       for (int q = 0; q < 4; ++q) x[q] = __builtin_amdgcn_perm(w[2 * q + 1][i >> 1], w[2 * q][i >> 1], sel);
       const x8 v = __builtin_bit_cast(x8, uint4{x[0], x[1], x[2], x[3]});
 #pragma unroll
-      for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(v, pb[qs], o[qs][i]);
+      for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(v, pb[qs].hi, o[qs][i]);
+#pragma unroll
+      for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(v, pb[qs].lo, o[qs][i]);
     }
   }
 
@@ -583,7 +583,7 @@ LMOP_DEVICE void few_vectors(const Args& a, int block, int split, FewLds<T, E8, 
         for (int r = 0; r < 4; ++r)
           st[0][hf][r] = 4 * hf + r < seen ? (gone ? NAN : st[0][hf][r]) : -INFINITY;
     }
-    const x8 pb[1] = {k.weights(0, st[0], a.c, thr)};
+    const Weights<T> pb[1] = {k.weights(0, st[0], a.c, thr)};
     uint32_t vals[8][NT / 2];
     const uint32_t odd = k.values(vals, !whole, any, !one);
     k.product(vals, pb);
@@ -649,7 +649,7 @@ LMOP_DEVICE void few_vectors(const Args& a, int block, int split, FewLds<T, E8, 
 #pragma unroll
     for (int i = 0; i < NT; ++i) r[i] = (T)(lt == 0.f ? 0.f : y[i] * inv);
     *(xo*)((T*)p.out + t * p.ldo + ho * HD + d) = r;
-    if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + ho] = lse_of(a, mt, lt);
+    if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + ho] = lse_of<T>(a, mt, lt);
   }
 }
 
@@ -766,13 +766,13 @@ __global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
         const bool gone = s_page[e] < 0;
         const uint32_t who = s_who[e];
         const int index = (s_id[e] << lps) + slot;
-        x8 pb[QS];
+        Weights<T> pb[QS];
 #pragma unroll
         for (int qs = 0; qs < QS; ++qs) {
           // of the lane's 8 keys, its vector sees the first `seen`
           const int seen = who & bit[qs] ? lim[qs] + 1 - index : 0;
           if (!__any(seen > 0)) {  // a block that only the other 16 vectors chose
-            pb[qs] = x8{};
+            pb[qs] = Weights<T>{};
             continue;
           }
 #pragma unroll
@@ -838,7 +838,7 @@ __global__ __launch_bounds__(64, 2) void walk_kernel(const Args a) {
       for (int i = 0; i < NT; ++i) y[i] = (T)(l == 0.f ? 0.f : k.o[qs][i][r] * inv);
       *(xo*)(dst + NT * (4 * k.g + r)) = y;
     }
-    if (p.lse && k.g == 0) p.lse[(size_t)t * a.n.nq + hq] = lse_of(a, k.m[qs], l);
+    if (p.lse && k.g == 0) p.lse[(size_t)t * a.n.nq + hq] = lse_of<T>(a, k.m[qs], l);
   }
 }
 
@@ -1038,7 +1038,7 @@ struct TileCore {
   }
 
   // The vectors' weights of the block and their sums; the states move to a new reference where needed
-  LMOP_DEVICE void weights(int qs, f32x4 (&st)[4], float cs, float thr, x8 (&pb)[2]) {
+  LMOP_DEVICE void weights(int qs, f32x4 (&st)[4], float cs, float thr, Weights<T> (&pb)[2]) {
     const x8 ones = {(T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f, (T)1.f};
     float mb = max3(st[0][0], st[0][1], st[0][2]);
     mb = max3(mb, st[0][3], st[1][0]);
@@ -1056,25 +1056,26 @@ struct TileCore {
       for (int i = 0; i < NT; ++i) o[qs][i] *= alpha;
       m[qs] = m_new;
     }
-    const float nmc = from_reference(st, m[qs], cs);
+    const float nmc = from_reference(st, m[qs], cs, Weights<T>::kLift);
+    auto weight = [&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, cs, nmc)); };
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
+    for (int kc = 0; kc < 2; ++kc) {
+      const f32x4 &x = st[2 * kc], &y = st[2 * kc + 1];
+      pb[kc].template set<0>(weight(x[0]), weight(x[1]));
+      pb[kc].template set<2>(weight(x[2]), weight(x[3]));
+      pb[kc].template set<4>(weight(y[0]), weight(y[1]));
+      pb[kc].template set<6>(weight(y[2]), weight(y[3]));
+    }
 #pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][r], cs, nmc)),
-                         __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][r + 1], cs, nmc))};
-        const x2 y = __builtin_convertvector(e, x2);
-        pb[kt >> 1][4 * (kt & 1) + r] = y[0];
-        pb[kt >> 1][4 * (kt & 1) + r + 1] = y[1];
-      }
-#pragma unroll
-    for (int kc = 0; kc < 2; ++kc) l4[qs] = Half<T>::mfma(ones, pb[kc], l4[qs]);
+    for (int kc = 0; kc < 2; ++kc) {
+      l4[qs] = Half<T>::mfma(ones, pb[kc].hi, l4[qs]);
+      l4[qs] = Half<T>::mfma(ones, pb[kc].lo, l4[qs]);
+    }
   }
 
   // O^T += V^T P^T.  Tile i: dimensions 16 i .. +15; lane (g, c) gets dimension 16 i + c of keys
   // 32 kc + 8 g .. +7
-  LMOP_DEVICE void product(int stage, const x8 (&pb)[QS][2]) {
+  LMOP_DEVICE void product(int stage, const Weights<T> (&pb)[QS][2]) {
     const char* sv = smem + stage * STAGE + KB * ROW;
 #pragma unroll
     for (int kc = 0; kc < 2; ++kc)
@@ -1085,7 +1086,9 @@ struct TileCore {
         const x4 hi = read_transposed<T>(sv + (key + 4) * ROW + ((i ^ vswz<HD>(key + 4)) * 32) + (c & 3) * 8);
         const x8 x = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 #pragma unroll
-        for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc], o[qs][i]);
+        for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc].hi, o[qs][i]);
+#pragma unroll
+        for (int qs = 0; qs < QS; ++qs) o[qs][i] = Half<T>::mfma(x, pb[qs][kc].lo, o[qs][i]);
       }
   }
 
@@ -1122,7 +1125,7 @@ struct TileCore {
       for (int r = 0; r < 4; ++r) y[r] = (T)(l == 0.f ? 0.f : o[qs][i][r] * inv);
       *(xo*)(dst + 16 * i + 4 * g) = y;
     }
-    if (a.t.lse && g == 0) a.t.lse[(size_t)t * a.n.nq + hq] = lse_of(a, m[qs], l);
+    if (a.t.lse && g == 0) a.t.lse[(size_t)t * a.n.nq + hq] = lse_of<T>(a, m[qs], l);
   }
 };
 
@@ -1255,7 +1258,7 @@ LMOP_DEVICE void tile_vectors(const Args& a, int block, int split, char* smem) {
           }
         }
       }
-      typename Core::x8 pb[Core::QS][2];
+      Weights<T> pb[Core::QS][2];
 #pragma unroll
       for (int qs = 0; qs < Core::QS; ++qs) k.weights(qs, st[qs], a.c, thr, pb[qs]);
       k.product(b & 1, pb);
@@ -1334,7 +1337,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) r[k] = (T)(s.l == 0.f ? 0.f : s.o[k] * inv);
   *(xo*)((T*)p.out + t * p.ldo + h * HD + d) = r;
-  if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + h] = lse_of(a, s.m, s.l);
+  if (p.lse && d == 0) p.lse[(size_t)t * a.n.nq + h] = lse_of<T>(a, s.m, s.l);
 }
 
 // ---------------------------------------------------------------- kernels

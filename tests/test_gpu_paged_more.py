@@ -3,7 +3,7 @@
 import pytest
 import torch
 
-from tests.test_gpu_paged import Batch, L, _ctx, _gen  # noqa: F401
+from tests.test_gpu_paged import Batch, L, _ctx, _gen, _reference  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +82,66 @@ def test_attend_scores_far_from_zero(L, dtype, new, length, prefix, n_blocks):  
             if not ok:
                 wrong.append((bits * sign, out[:, 0, 0].isnan().sum().item(), (out != want).sum().item()))
     assert not wrong, wrong
+
+
+# ---------------------------------------------------------------- attention: weights in fp32's precision
+# (nq, nkv, hd, page, new, length, prefix, blocks): every kernel, and parts that are joined
+EVERY = [(8, 2, 128, 64, [1], [500], 0, 0), (8, 2, 64, 16, [1] * 40, [200 + i for i in range(40)], 0, 0),
+         (8, 2, 128, 32, [1, 1], [5000, 300], 0, 0), (8, 2, 64, 16, [1] * 64, [20] * 64, 3300, 0),
+         (4, 2, 128, 64, [60, 41], [300, 200], 30, 0), (2, 1, 64, 32, [70], [3000], 0, 0),
+         (8, 2, 64, 16, [1, 1], [400, 300], 0, 6), (64, 16, 64, 16, [340], [900], 0, 8)]
+
+
+@pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("bf16", "bf16"), ("f16", "e4m3"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("nq,nkv,hd,page,new,length,prefix,n_blocks", EVERY)
+def test_attend_is_as_exact_as_its_type(L, dtype, cache, nq, nkv, hd, page, new, length, prefix, n_blocks):  # noqa: F811
+    """The error is that of rounding the result once.  Errors of independent steps add as squares: what is held in
+    fp32 (2^-23 of a score of up to 40, some tens of them), and weights to 2^-16, are at most 1/20 of the root mean
+    square of the result's rounding (2^-12 and 2^-9 / sqrt(3)), 1.00125 times together; weights of the type's own
+    precision make it 1.25 times."""
+    print("exact", dtype, cache, nq, nkv, hd, page, new, length, prefix, n_blocks, flush=True)
+    b = Batch(nq, nkv, hd, dtype, cache, page, new, length, prefix, seed=7, q_size=1.0)
+    blocks = None
+    if n_blocks:
+        g = _gen(3)
+        blocks = torch.stack([torch.randperm(min(length) // page, generator=g)[:n_blocks].sort()[0]
+                              for _ in range(b.tokens * nkv)]).view(b.tokens, nkv, n_blocks).to(torch.int32)
+    want = _reference(b, blocks)[0]
+    got = b.attend(_ctx(L, nq, nkv, hd), L, blocks=None if blocks is None else blocks.cuda()).double().cpu()
+    off = lambda x: (x - want).square().mean().sqrt().item()
+    assert off(got) <= 1.02 * off(want.to(b.dt).double())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new,length,prefix,n_blocks,nq,nkv", [
+    ([1], [30000], 0, 0, 4, 1), ([1] * 3, [30000] * 3, 0, 0, 4, 1), ([40], [30000], 0, 0, 4, 1), ([1] * 64, [0] * 64, 30000, 0, 8, 2),
+    ([1], [16384], 0, 1024, 4, 1), ([340], [16384], 0, 1024, 64, 16)])
+def test_attend_many_keys_of_little_weight(L, dtype, new, length, prefix, n_blocks, nq, nkv):  # noqa: F811
+    """One key of weight 1 whose value is zero, and thousands of weight 2^-26 with a value of one: all that the
+    result has comes from these."""
+    import math
+    print("tail", dtype, new, length, prefix, n_blocks, flush=True)
+    hd, page = 64, 16
+    b = Batch(nq, nkv, hd, dtype, dtype, page, new, length, prefix, seed=1)
+    b.q[:] = 1.0
+    live = b.live[:, None, :].expand(b.k16.shape[:3])
+    drop = 26 * math.log(2)
+    low = torch.tensor(-drop / hd / hd ** -0.5).to(b.dt)
+    b.k16[live], b.v16[live] = low, 1.0
+    pages = b.prefix_pages[:1].long() if prefix else b.table[:, 0].long()
+    b.k16[pages, :, 0], b.v16[pages, :, 0] = 0.0, 0.0
+    blocks = None
+    if n_blocks:
+        blocks = torch.arange(n_blocks, dtype=torch.int32).expand(b.tokens, nkv, n_blocks).contiguous().cuda()
+    lse = torch.full((b.tokens, nq), 7.0, device="cuda")
+    out = b.attend(_ctx(L, nq, nkv, hd), L, lse=lse, blocks=blocks).double().cpu().view(b.tokens, nq, hd)
+    w = math.exp(low.double().item() * hd * hd ** -0.5)
+    for t, (i, j) in enumerate((i, j) for i, n in enumerate(new) for j in range(n)):
+        tail = (prefix or length[i] - new[i] + j + 1) - 1
+        want = tail * w / (1 + tail * w)
+        # a score of 18: 64 exact products of 0.28, four roundings, the exponential; the weights; sums of equal terms
+        tol = 64 * 18 * 2.0 ** -23 + 4 * 18 * 2.0 ** -23 + 2.0 ** -21 + 2.0 ** -16 + 2 * (tail + 64) * 2.0 ** -23
+        eps = torch.finfo(b.dt).eps / 2
+        assert ((out[t] - want).abs() <= want * tol + eps * want * (1 + tol)).all()
+        # (the sum of the weights is 1 and more, and as a sum of fp32 terms known to N 2^-23 of that)
+        assert ((lse[t].double().cpu() - math.log1p(tail * w)).abs() <= tail * w * tol + (tail + 64) * 2.0 ** -23).all()
