@@ -31,6 +31,17 @@ __global__ __launch_bounds__(256) void index_tokens_kernel(const int32_t* __rest
   if (i < n) index[tok[i]] = i;
 }
 
+// --------------------------------------------------------------- rotary table
+// tab[p][i] = (cos, sin) of p * freq[i], in fp64, rounded once.  Made here and not on the host: 65,536 positions of 64
+// angles, 34 MB, took a CPU thread 60 to 116 ms, to which the copy to the device came.
+__global__ __launch_bounds__(256) void rotary_kernel(float2* __restrict__ tab, int n, int half, const RotaryFreqs f) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  double s, c;
+  sincos((double)(i / half) * f.freq[i % half], &s, &c);
+  tab[i] = make_float2((float)c, (float)s);
+}
+
 // --------------------------------------------------------------- embedding
 // x[t][:] = fp32(E[tok[t]][:]); one workgroup per token, 8 halves per thread-iteration
 __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ tok,
@@ -366,6 +377,12 @@ hipError_t launch_fill_u32(hipStream_t s, void* p, size_t n_words, uint32_t valu
   const size_t groups = (n_words + 1023) / 1024;
   const int blocks = (int)(groups < 8192 ? groups : 8192);
   hipLaunchKernelGGL(fill_u32_kernel, dim3(blocks), dim3(256), 0, s, (uint32_t*)p, n_words, value);
+  return hipGetLastError();
+}
+
+hipError_t launch_rotary(hipStream_t s, float2* tab, int positions, int half, const RotaryFreqs& f) {
+  const int n = positions * half;
+  hipLaunchKernelGGL(rotary_kernel, dim3((n + 255) / 256), dim3(256), 0, s, tab, n, half, f);
   return hipGetLastError();
 }
 

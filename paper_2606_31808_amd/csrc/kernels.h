@@ -116,6 +116,11 @@ hipError_t launch_repack_w8(hipStream_t s, const RepackSrc& src, const int32_t* 
 // ---------------------------------------------------------------- elementwise
 // p[i] = value for n_words 32-bit words (p 16-byte aligned)
 hipError_t launch_fill_u32(hipStream_t s, void* p, size_t n_words, uint32_t value);
+// tab[positions][half] = (cos, sin) of position * freq; positions * half below 2^31 - 256
+struct RotaryFreqs {
+  double freq[64];  // half of head_dim, at most
+};
+hipError_t launch_rotary(hipStream_t s, float2* tab, int positions, int half, const RotaryFreqs& f);
 // index[tok[i]] = i for n distinct tokens (other entries stay)
 hipError_t launch_index_tokens(hipStream_t s, const int32_t* tok, int n, int32_t* index);
 hipError_t launch_embed(hipStream_t s, const int32_t* tok, int T, const half_bits* emb, int d,

@@ -1851,22 +1851,18 @@ lmop_status lmop_create(const lmop_config* cfg, int32_t device, void* hip_stream
   for (auto& stg : c->stage)
     if (hipEventCreateWithFlags(&stg.done, hipEventDisableTiming) != hipSuccess)
       return bail(fail(cp, LMOP_ERR_DEVICE, "hipEventCreate failed"));
-  // rotary table: cos/sin of pos * theta^(-2i/hd) in double, stored fp32
+  // rotary table: cos/sin of pos * theta^(-2i/hd) in double, stored fp32.  On the null stream, and waited for: the
+  // ctx's stream may be one that a caller captures later, or another than its operators'
   const int half = cf.head_dim / 2;
-  std::vector<float2> tab((size_t)cf.max_seq * half);
-  std::vector<double> freq(half);
-  for (int i = 0; i < half; ++i) freq[i] = std::pow((double)cf.rope_theta, -2.0 * i / cf.head_dim);
-  for (int p = 0; p < cf.max_seq; ++p)
-    for (int i = 0; i < half; ++i) {
-      const double ang = (double)p * freq[i];
-      tab[(size_t)p * half + i] = make_float2((float)std::cos(ang), (float)std::sin(ang));
-    }
+  RotaryFreqs freqs{};
+  for (int i = 0; i < half; ++i) freqs.freq[i] = std::pow((double)cf.rope_theta, -2.0 * i / cf.head_dim);
   void* rt = nullptr;
-  st = dev_alloc(cp, &rt, tab.size() * sizeof(float2));
+  st = dev_alloc(cp, &rt, (size_t)cf.max_seq * half * sizeof(float2));
   if (st != LMOP_OK) return bail(st);
   c->rope_tab = (float2*)rt;
-  if (hipMemcpy(rt, tab.data(), tab.size() * sizeof(float2), hipMemcpyHostToDevice) != hipSuccess)
-    return bail(fail(cp, LMOP_ERR_DEVICE, "upload of the rotary table failed"));
+  if (launch_rotary(nullptr, c->rope_tab, cf.max_seq, half, freqs) != hipSuccess ||
+      hipStreamSynchronize(nullptr) != hipSuccess)
+    return bail(fail(cp, LMOP_ERR_DEVICE, "the rotary table was not made"));
   *out = c.release();
   return LMOP_OK;
 }
