@@ -3,7 +3,7 @@
 import pytest
 import torch
 
-from tests.test_gpu_paged import Batch, L, _ctx, _gen, _reference  # noqa: F401
+from tests.test_gpu_paged import Batch, L, Shape, _ctx, _gen, _reference  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -145,3 +145,104 @@ def test_attend_many_keys_of_little_weight(L, dtype, new, length, prefix, n_bloc
         assert ((out[t] - want).abs() <= want * tol + eps * want * (1 + tol)).all()
         # (the sum of the weights is 1 and more, and as a sum of fp32 terms known to N 2^-23 of that)
         assert ((lse[t].double().cpu() - math.log1p(tail * w)).abs() <= tail * w * tol + (tail + 64) * 2.0 ** -23).all()
+
+
+# ---------------------------------------------------------------- attention: tokens without keys
+@pytest.mark.parametrize("dtype,cache,hd", [("f16", "f16", 64), ("bf16", "bf16", 128), ("f16", "e4m3", 128), ("bf16", "e4m3", 64)])
+@pytest.mark.parametrize("new,length,prefix", [([1, 1, 1], [0, 20, 0], 0), ([3, 5], [1, 0], 0), ([40, 60, 2], [10, 0, 2], 0),
+                                               ([2, 1, 4], [5000, 0, 1], 0), ([70, 9], [3000, 4], 0), ([3, 1], [1, 0], 5)])
+def test_attend_tokens_before_their_sequence(L, dtype, cache, hd, new, length, prefix):  # noqa: F811
+    """Each that sees no key gets zeros and minus infinity, and no other does."""
+    print("before", dtype, cache, hd, new, length, prefix, flush=True)
+    b = Batch(4, 2, hd, dtype, cache, 16, new, length, prefix, seed=5)
+    lse = torch.full((b.tokens, 4), 7.0, device="cuda")
+    out = b.attend(_ctx(L, 4, 2, hd), L, lse=lse)
+    none = torch.tensor([prefix == 0 and m - n + j < 0 for n, m in zip(new, length) for j in range(n)]).cuda()
+    assert none.any() == (prefix == 0)
+    assert torch.all(out[none] == 0) and torch.all(lse[none] == -float("inf"))
+    assert torch.all(out[~none].abs().sum(1) > 0) and torch.isfinite(lse[~none]).all()
+
+
+# ---------------------------------------------------------------- calls with a workspace
+# (nq, nkv, hd, page, new, length, prefix, blocks): splits of few vectors; a prefix on its own, few vectors and
+# tiles; splits of tiles; splits of a walk; splits of chosen blocks
+WITH_PARTS = [(8, 2, 64, 16, [1, 1], [9000, 3000], 0, 0), (4, 2, 128, 64, [1] * 8, [40] * 8, 26000, 0),
+              (8, 2, 64, 16, [1] * 40, [20 + i for i in range(40)], 5300, 0), (2, 1, 64, 32, [70], [3000], 0, 0),
+              (64, 16, 64, 16, [340], [5000], 0, 9), (4, 2, 64, 16, [1], [5000], 0, 256)]
+
+
+class Call:
+    """One attention call with every tensor on the device."""
+
+    def __init__(self, L, ctx, nq, nkv, hd, page, new, length, prefix, n_blocks, seed):  # noqa: F811
+        b = Batch(nq, nkv, hd, "f16", "f16", page, new, length, prefix, seed=seed)
+        self.ctx, self.cache, self.q = ctx, b.cache(L), b.q.cuda()
+        self.args = b.args(L, max_tokens=max(new), max_length=max(length))
+        if prefix:
+            self.args.update(prefix=b.prefix_pages.cuda(), prefix_length=prefix)
+        if n_blocks:
+            g = _gen(seed)
+            self.args["blocks"] = torch.stack([torch.randperm(max(length) // page, generator=g)[:n_blocks].sort()[0]
+                                               for _ in range(b.tokens * nkv)]).view(b.tokens, nkv, n_blocks).to(torch.int32).cuda()
+        sizes = []
+
+        def workspace(n):
+            sizes.append(n)
+            return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+        a = self.args
+        L.lmop_attend(ctx.ctx, ctx.heads, self.cache, self.q, torch.empty_like(self.q), a["table"], a["length"], a["start"],
+                      a["max_tokens"], a["max_length"], a.get("prefix"), prefix, a.get("blocks"), workspace=workspace)
+        assert len(sizes) == 1 and sizes[0] > 0
+
+    def __call__(self):
+        return self.ctx.attend(self.cache, self.q, **self.args)
+
+
+@pytest.mark.parametrize("nq,nkv,hd,page,new,length,prefix,n_blocks", WITH_PARTS)
+def test_two_streams_with_workspaces(L, nq, nkv, hd, page, new, length, prefix, n_blocks):  # noqa: F811
+    """Calls of two contexts under way at once, each with its parts in a workspace of its own."""
+    print("streams", nq, nkv, hd, page, new[:3], length[:3], prefix, n_blocks, flush=True)
+    calls, want = [], []
+    for i in range(2):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            calls.append((stream, Call(L, L.Context(Shape(nq, nkv, hd), device=0, stream=stream.cuda_stream, max_seq=64),
+                                       nq, nkv, hd, page, new, length, prefix, n_blocks, seed=i)))
+            want.append(calls[i][1]())
+        torch.cuda.synchronize()
+    assert not torch.equal(*want)
+    got = [[], []]
+    for _ in range(30):
+        for i, (stream, call) in enumerate(calls):
+            with torch.cuda.stream(stream):
+                got[i].append(call())
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i])
+
+
+@pytest.mark.parametrize("nq,nkv,hd,page,new,length,prefix,n_blocks", WITH_PARTS)
+def test_captured_with_workspaces(L, nq, nkv, hd, page, new, length, prefix, n_blocks):  # noqa: F811
+    """Two graphs of a call and its joining launch, replayed in turn with eager calls between."""
+    print("graphs", nq, nkv, hd, page, new[:3], length[:3], prefix, n_blocks, flush=True)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        call = Call(L, L.Context(Shape(nq, nkv, hd), device=0, stream=stream.cuda_stream, max_seq=64), nq, nkv, hd, page,
+                    new, length, prefix, n_blocks, seed=3)
+        stream.synchronize()
+        graphs = []
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                out = call()
+            graphs.append((g, out))
+        for i in range(6):
+            call.q.normal_()
+            want = call().clone()
+            g, out = graphs[i % 2]
+            out.zero_()
+            g.replay()
+            again = call()
+            stream.synchronize()
+            assert torch.equal(out, want) and torch.equal(again, want)
