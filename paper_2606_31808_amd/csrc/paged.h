@@ -40,17 +40,21 @@ struct Half<bf16> {
 };
 
 // Positive weights in two terms: the nearest of the type, and the nearest of what is left.  Together off by 2^-16 of a
-// bf16 weight, 2^-22 of an fp16 one of 2^-3 and more, and 2^-25 of a smaller one: lifted by 2^kLift, so that the
-// largest of a softmax, which may pass its reference by 2^8, is 2^7 to 2^15, that is 2^-32 of it.  In one term the
-// results were 1.25 to 1.3 times as far from the formula as their own rounding takes them, and fp16 weights below 2^-25
-// were lost however many.  The second term costs the matrix units half as much again as before: a prompt of 8448 tokens 583 ->
-// 777 us, 272 rows behind 512 keys 280 -> 340, 256 tokens behind 8192 keys 76 -> 87, walks 285 -> 328, single tokens 1 to 2%.
+// bf16 weight, 2^-22 of an fp16 one of 2^-3 and more, and 2^-25 of a smaller one.  All are taken times 2^kLift, of which
+// the division rids them: the largest of a softmax may pass its reference by 2^8.  fp16 ones are then 2^7 to 2^15 at the
+// top, and what is lost is 2^-32 of that; bf16 ones 2^-8 to 1, so that values up to the type's end stay within fp32.
+//
+// In one term results were 1.25 to 1.3 times as far from the formula as their own rounding takes them, and fp16 weights
+// below 2^-25 were lost however many.  The second term is a second product with the values, half as much again for the
+// matrix units: a prompt of 8448 tokens 583 -> 784 us (1.1 PFLOP/s with it, what a large library product reaches), 272 rows
+// behind 512 keys 280 -> 338, 256 tokens behind 8192 keys 76 -> 87, the walk over chosen blocks 285 -> 325; single tokens,
+// whose matrix units wait for memory, 1 to 2%.
 template <typename T>
 struct Weights {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   typedef typename Half<T>::x2 x2;
   typename Half<T>::x8 hi, lo;
-  static constexpr float kLift = __is_same(T, f16) ? 7.f : 0.f;
+  static constexpr float kLift = __is_same(T, f16) ? 7.f : -8.f;
   template <int I>
   LMOP_DEVICE void set(float x, float y) {  // weights I and I + 1
     const x2 h = __builtin_convertvector((f32x2{x, y}), x2);

@@ -152,7 +152,7 @@ LMOP_DEVICE void write_bad(const Args& a, int t, int h, int part, int lane, int 
 template <typename T>
 LMOP_DEVICE float lse_of(const Args& a, float m, float l) {
   // l > 0 means that some score was finite (the lift taken off before the logarithm, where that is exact)
-  constexpr float kDown = 1.f / (1 << (int)Weights<T>::kLift);
+  constexpr float kLift = Weights<T>::kLift, kDown = kLift > 0 ? 1.f / (1 << (int)kLift) : (float)(1 << (int)-kLift);
   return l == 0.f ? -INFINITY : (m * a.c + __log2f(l * kDown)) * 0.6931471805599453f;
 }
 

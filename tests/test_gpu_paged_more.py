@@ -246,3 +246,31 @@ def test_captured_with_workspaces(L, nq, nkv, hd, page, new, length, prefix, n_b
             again = call()
             stream.synchronize()
             assert torch.equal(out, want) and torch.equal(again, want)
+
+
+# ---------------------------------------------------------------- attention: values near the type's end
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new,length,prefix,n_blocks,nq,nkv", [
+    ([1], [600], 0, 0, 8, 2), ([1] * 70, [600] * 70, 0, 0, 8, 8), ([60, 41], [700, 690], 0, 0, 4, 2), ([1] * 64, [0] * 64, 3300, 0, 8, 2),
+    ([1], [640], 0, 40, 8, 2), ([340], [980], 0, 40, 64, 16)])
+def test_attend_large_values(L, dtype, new, length, prefix, n_blocks, nq, nkv):  # noqa: F811
+    """Values of 2^127 (fp16: 65504) of two keys, the second of 2^7.9 times the first one's weight and 256 keys on, so
+    that the wave that holds both does not move its reference: the result is that value, as it is with weights of at
+    most one."""
+    print("large", dtype, new[:3], length[:3], prefix, n_blocks, flush=True)
+    hd = 128
+    b = Batch(nq, nkv, hd, dtype, dtype, 16, new, length, prefix, seed=1)
+    top = 65504.0 if dtype == "f16" else 2.0 ** 127
+    b.q[:] = 1.0
+    live = b.live[:, None, :].expand(b.k16.shape[:3])
+    unit = 0.6931471805599453 / hd * hd ** 0.5  # a key of so much: a power of two in weight
+    b.k16[live], b.v16[live] = -300 * unit, top
+    for i in range(len(new)):
+        pages = b.prefix_pages.long() if prefix else b.table[i].long()
+        for key, size in ((10, 0.0), (266, 7.9)):
+            b.k16[pages[key // 16], :, key % 16] = size * unit
+    blocks = None
+    if n_blocks:
+        blocks = torch.arange(n_blocks, dtype=torch.int32).expand(b.tokens, nkv, n_blocks).contiguous().cuda()
+    out = b.attend(_ctx(L, nq, nkv, hd), L, blocks=blocks)
+    assert torch.all(out.float() == torch.tensor(top).to(b.dt).float())
