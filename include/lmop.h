@@ -515,8 +515,10 @@ lmop_status lmop_qk_norm_rope(lmop_ctx* ctx, const lmop_qk_norm_rope_args* args)
  * A page holds page_size tokens of every kv head: [n_kv_heads][page_size][head_dim].
  * LMOP_E4M3 pages hold E4M3 codes, and for each token and head a power of two
  * as its exponent + 127, 1 to 254: value = e4m3(code) * 2^(exp - 127).  A power of two because
- * codes are floating-point: any other scale would round no less, and this
- * one is undone exactly. */
+ * codes are floating-point: any other scale would round no less.  lmop_attend takes a value as the
+ * nearest of the tokens' dtype, which is the value itself in LMOP_BF16 from 2^-126 on and in LMOP_F16 from 2^-14 to 61440;
+ * smaller ones become multiples of 2^-24 there (of what lmop_cache_append writes this touches
+ * rotated keys alone, by 2^-25 at most) and larger ones infinite. */
 typedef struct {
   void *k, *v;             /* [n_pages] pages of dtype, page_stride apart; 16-byte aligned */
   uint8_t *k_exp, *v_exp;  /* LMOP_E4M3: [n_pages][n_kv_heads][page_size], 16-byte aligned; else NULL */
@@ -601,7 +603,11 @@ typedef struct {
   int64_t ldq, ldo;
   int32_t prefix_length; /* >= 0 */
   int32_t n_blocks;
-  int32_t max_tokens;    /* at least the most tokens of a sequence in the call; 1 without starts */
+  int32_t max_tokens;    /* at least the most tokens of a sequence in the call; 1 without starts.  The whole call
+                            is divided for a sequence of so many, and a long prefix walked once for all
+                            sequences only where max_tokens * n_heads / n_kv_heads is at most 16, else
+                            once for each: prompts and single tokens are better two calls, each with
+                            its rows */
   int32_t max_length;    /* at least the longest length, at most max_pages * page_size: with
                             max_tokens what the call's shape is chosen by */
   float scale;           /* 0: 1 / sqrt(head_dim); else 1e-30 to 1e30 */

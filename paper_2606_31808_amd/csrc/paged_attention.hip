@@ -161,9 +161,9 @@ LMOP_DEVICE float lse_of(const Args& a, float m, float l) {
 // NaN among the values become zeros in the product, and are added to the vectors that see
 // them: the weight, being positive, does not matter.
 template <typename T>
-LMOP_DEVICE bool unbounded(uint32_t w) {  // either of two values
+LMOP_DEVICE uint32_t unbounded(uint32_t w) {  // a mask of those of two values that are
   constexpr uint32_t E = __is_same(T, f16) ? 0x7C00u : 0x7F80u;
-  return (w & E) == E || (w >> 16 & E) == E;
+  return ((w & E) == E ? 0xFFFFu : 0) | ((w >> 16 & E) == E ? 0xFFFF0000u : 0);
 }
 
 // four values of the cache, as the product would read them
@@ -375,7 +375,9 @@ struct WaveCore {
 #pragma unroll
         for (int i = 0; i < NT / 2; ++i) {
           if (j >= any) w[j][i] = 0;
-          if (bounded && unbounded<T>(w[j][i])) odd |= 1u << j, w[j][i] = 0;
+          if (!bounded) continue;
+          const uint32_t out = unbounded<T>(w[j][i]);
+          if (out) odd |= 1u << j, w[j][i] &= ~out;
         }
     }
     return odd;
@@ -1009,8 +1011,11 @@ struct TileCore {
         bool any = false;
         uint32_t* ys = (uint32_t*)&y;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (unbounded<T>(ys[q])) ys[q] = 0, any = true;
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t out = unbounded<T>(ys[q]);
+          ys[q] &= ~out;
+          any = any || out != 0;
+        }
         if (any) {
           *x = y;
           atomicOr(&odd[r >> 5], 1u << (r & 31));

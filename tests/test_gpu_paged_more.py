@@ -3,7 +3,7 @@
 import pytest
 import torch
 
-from tests.test_gpu_paged import Batch, L, Shape, _ctx, _gen, _reference  # noqa: F401
+from tests.test_gpu_paged import E4M3, NAN, Batch, L, Shape, _ctx, _gen, _reference  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -274,3 +274,34 @@ def test_attend_large_values(L, dtype, new, length, prefix, n_blocks, nq, nkv): 
         blocks = torch.arange(n_blocks, dtype=torch.int32).expand(b.tokens, nkv, n_blocks).contiguous().cuda()
     out = b.attend(_ctx(L, nq, nkv, hd), L, blocks=blocks)
     assert torch.all(out.float() == torch.tensor(top).to(b.dt).float())
+
+
+# ---------------------------------------------------------------- infinities among values: their neighbours
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("nq,nkv,hd,page,new,length,n_blocks", [
+    (2, 2, 64, 16, [9, 3], [40, 20], 0), (4, 1, 128, 32, [4], [300], 0), (4, 2, 128, 16, [60, 41], [300, 90], 0),
+    (64, 16, 64, 16, [340], [900], 8)])
+def test_attend_neighbours_of_infinite_values(L, dtype, nq, nkv, hd, page, new, length, n_blocks):  # noqa: F811
+    """A value that is infinite or NaN, of a key that some tokens see and some do not, says nothing about the key's
+    other dimensions: their results stay as they are, to the bit, in every token."""
+    print("neighbours", dtype, nq, nkv, hd, page, new, length, n_blocks, flush=True)
+    b = Batch(nq, nkv, hd, dtype, dtype, page, new, length, seed=9)
+    key = length[0] - 2  # of the last two tokens
+    blocks = None
+    if n_blocks:
+        key = 5 * page + 3
+        g = _gen(3)
+        blocks = torch.stack([torch.randperm(min(length) // page, generator=g)[:n_blocks].sort()[0]
+                              for _ in range(b.tokens * nkv)]).view(b.tokens, nkv, n_blocks).to(torch.int32).cuda()
+    ctx = _ctx(L, nq, nkv, hd)
+    clean = b.attend(ctx, L, blocks=blocks).view(b.tokens, nq, hd)
+    odd = {2: float("inf"), 9: float("-inf"), hd - 1: NAN}
+    for d, x in odd.items():
+        b.v16[int(b.table[0, key // page]), :, key % page, d] = x
+    got = b.attend(ctx, L, blocks=blocks).view(b.tokens, nq, hd)
+    others = [d for d in range(hd) if d not in odd]
+    assert torch.isfinite(clean).all() and torch.equal(got[..., others], clean[..., others])
+    sees = (blocks == 5).any(-1).repeat_interleave(nq // nkv, 1) if n_blocks else \
+        (torch.arange(b.tokens, device="cuda") >= new[0] - 2)[:, None].expand(-1, nq) & \
+        (torch.arange(b.tokens, device="cuda") < new[0])[:, None]
+    assert torch.equal(torch.isfinite(got).all(-1), ~sees)
