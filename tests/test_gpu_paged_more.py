@@ -141,6 +141,8 @@ def test_attend_many_keys_of_little_weight(L, dtype, new, length, prefix, n_bloc
         want = tail * w / (1 + tail * w)
         # a score of 18: 64 exact products of 0.28, four roundings, the exponential; the weights; sums of equal terms
         tol = 64 * 18 * 2.0 ** -23 + 4 * 18 * 2.0 ** -23 + 2.0 ** -21 + 2.0 ** -16 + 2 * (tail + 64) * 2.0 ** -23
+        if dtype == "f16":  # a weight is the nearest in steps of 2^-24, the largest at least 2^7
+            tol += 2.0 ** -32 / 2.0 ** -26
         eps = torch.finfo(b.dt).eps / 2
         assert ((out[t] - want).abs() <= want * tol + eps * want * (1 + tol)).all()
         # (the sum of the weights is 1 and more, and as a sum of fp32 terms known to N 2^-23 of that)
@@ -305,3 +307,62 @@ def test_attend_neighbours_of_infinite_values(L, dtype, nq, nkv, hd, page, new, 
         (torch.arange(b.tokens, device="cuda") >= new[0] - 2)[:, None].expand(-1, nq) & \
         (torch.arange(b.tokens, device="cuda") < new[0])[:, None]
     assert torch.equal(torch.isfinite(got).all(-1), ~sees)
+
+
+# ---------------------------------------------------------------- values of 8-bit pages
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_every_code_and_exponent(L, dtype, tokens):  # noqa: F811
+    """A token that sees one key gets its value: the code times the power of two, as the nearest of the tokens' type."""
+    dt, nkv, hd, page = torch.float16 if dtype == "f16" else torch.bfloat16, 2, 128, 16
+    n = 254
+    codes = torch.arange(256, dtype=torch.uint8).view(1, nkv, 1, hd).expand(n, nkv, page, hd).contiguous()
+    exps = torch.arange(1, 255, dtype=torch.uint8).view(n, 1, 1).expand(n, nkv, page).contiguous()
+    k = torch.zeros(n, nkv, page, hd, dtype=torch.uint8)
+    cache = L.PagedCache(k.view(E4M3).cuda(), codes.view(E4M3).cuda(), torch.full_like(exps, 127).cuda(), exps.cuda())
+    ctx = _ctx(L, nkv, nkv, hd)
+    out = ctx.attend(cache, torch.ones(n * tokens, nkv * hd, dtype=dt, device="cuda"),
+                     table=torch.arange(n, dtype=torch.int32, device="cuda")[:, None], max_tokens=tokens, max_length=1,
+                     length=torch.ones(n, dtype=torch.int32, device="cuda"),
+                     start=torch.arange(n + 1, dtype=torch.int32, device="cuda") * tokens)
+    got = out.view(n, tokens, 256)[:, -1].cpu().double()
+    value = codes[:, :, 0].reshape(n, 256).view(E4M3).double() * torch.pow(2.0, exps[:, :1, 0].double() - 127)
+    want = value.to(dt).double()
+    # (bf16: fp32 sums of weights of 2^-8 keep values from 2^-118 on)
+    least = 0 if dtype == "f16" else 2.0 ** -118
+    same = (got == want) | (got.isnan() & (want.isnan() | want.isinf())) | (value.abs() < least) & (got.abs() <= least)
+    assert same.all(), [(i, hex(j), value[i, j].item(), got[i, j].item()) for i, j in (~same).nonzero()[:8].tolist()]
+    if tokens > 1:
+        assert torch.all(out.view(n, tokens, 256)[:, :-1] == 0)
+
+
+# ---------------------------------------------------------------- infinities among values that are seen
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("nq,nkv,hd,page,new,length,prefix,n_blocks", EVERY)
+def test_attend_infinite_values(L, dtype, nq, nkv, hd, page, new, length, prefix, n_blocks):  # noqa: F811
+    """A positive weight times infinity is infinity, of its sign: in that dimension, for the tokens that see the key, and
+    with both signs or a NaN it is NaN.  No other result changes by a bit."""
+    print("inf", dtype, nq, nkv, hd, page, new[:3], length[:3], prefix, n_blocks, flush=True)
+    b = Batch(nq, nkv, hd, dtype, dtype, page, new, length, prefix, seed=7, q_size=1.0)
+    blocks = None
+    if n_blocks:
+        blocks = torch.arange(n_blocks, dtype=torch.int32).expand(b.tokens, nkv, n_blocks).contiguous().cuda()
+    ctx = _ctx(L, nq, nkv, hd)
+    clean = b.attend(ctx, L, blocks=blocks).view(b.tokens, nkv, nq // nkv, hd)
+    assert torch.isfinite(clean).all()
+    inf = float("inf")
+    want = clean.clone()
+    seq = torch.repeat_interleave(torch.arange(len(new)), torch.tensor(new)).cuda()
+    for where, pages, n, sees in ([(0, b.prefix_pages, prefix, torch.ones_like(seq, dtype=torch.bool))] if prefix else []) + \
+            [(1, b.table[0], length[0] - new[0], seq == 0)]:
+        if n < 8:
+            continue
+        for key, d, x in ((1, 3 + where, inf), (4, 17 + where, -inf), (2, 40 + where, inf), (5, 40 + where, -inf), (3, 50 + where, NAN)):
+            b.v16[int(pages[key // page]), nkv - 1, key % page, d] = x
+            at = want[sees][:, -1, :, d]
+            want[:, -1, :, d] = torch.where(sees[:, None], want[:, -1, :, d] + x, want[:, -1, :, d])
+            assert at.numel()
+    got = b.attend(ctx, L, blocks=blocks).view(want.shape)
+    same = (got == want) | (got.isnan() & want.isnan())
+    assert not torch.isfinite(want).all()
+    assert same.all(), [(i, got[tuple(i)].item(), want[tuple(i)].item()) for i in (~same).nonzero()[:6].tolist()]
