@@ -49,23 +49,23 @@ inline int64_t least_of(int64_t a, int64_t b) { return a < b ? a : b; }
 
 // Splits of a few-vector launch of `workgroups` before it is split, over `keys` keys at most.  Joining parts takes a
 // second launch and some 4 us, in which a workgroup walks 512 keys, so up to 1024 stay together (16 blocks
-// of 64 for each of 256 workgroups: 42 us whole, 50 in four parts).  Two workgroups fit a CU: where the sequences
+// of 64 for each of 256 workgroups: 25 us whole, 32 in four parts).  Two workgroups fit a CU: where the sequences
 // are alike, 512 of them are the fastest (us, with 1024 of them in brackets; 32 + 8 heads of 128: 16 sequences of
-// 8000 keys 100.6 (104.8), 64 of 2000 96.4 (101.0), 8-bit 4 of 32,000 48.7 (55.6) and 16 of 8000 48.5
-// (57.0)).  Where they are not, only some have keys in each split, and up to 1024 of long chunks balance
-// better: 32 of 1000 to 32,000, 8-bit, 244 us, of 512 workgroups 301.  Parts of at least 512 keys: one sequence of 4000
-// takes 15.8 us, in parts of 2048 24.8.
+// 8000 keys 98.3 (100.0), 64 of 2000 95.5 (100.5), 8-bit 4 of 32,000 47.9 (56.4) and 16 of 8000 46.7
+// (54.6)).  Where they are not, only some have keys in each split, and up to 1024 of long chunks balance
+// better: 32 of 1000 to 32,000, 8-bit, 228 us, of 512 workgroups 312.  Parts of at least 512 keys: one sequence of 4000
+// takes 12.3 us, in parts of 2048 26.9 (of 32,000 keys 30.9 and 27.7).
 inline int64_t few_splits(int64_t workgroups, int64_t keys) {
   if (keys <= 1024) return 1;
   const int64_t even = least_of(512 / workgroups, keys / 512), ragged = least_of(1024 / workgroups, keys / 4096);
   return even > ragged ? even : ragged;
 }
 // Splits of a tile launch of `workgroups` over `blocks` steps, with `outputs` = tokens x heads.  Up to two
-// workgroups a CU (up to four: 64 tokens over 32,000 keys 80 -> 109 us; one: 256 tokens 193 -> 230).  A step takes
+// workgroups a CU (up to four: 64 tokens over 32,000 keys 70 -> 93 us; one: 256 tokens 209 -> 271).  A step takes
 // some 1.2 us; each part more costs outputs / 2048 * 0.5 us, written and read once more, so that their sum is
-// least at sqrt(4800 blocks / outputs) parts.  us, at that many and at twice or half of them: 64 tokens over
-// 1000 keys 18 (25); prefixes of 8192 keys, 16 tokens 21 (24), of 4096, 32 tokens 23 (26), of 8192,
-// 64 tokens 31 (35), of 2048, 256 tokens 33 (44).
+// least at sqrt(4800 blocks / outputs) parts.  us, at that many, at twice and at half of them: 64 tokens over
+// 1000 keys 19.0, 20.1, 22.9; prefixes of 8192 keys, 16 tokens 21.6, 26.0, 26.7, of 4096, 32 tokens 23.2, 22.0, 29.0, of
+// 8192, 64 tokens 33.0, 37.1, 46.3, of 2048, 256 tokens 33.9, 45.6, 46.6.
 inline int64_t tile_splits(int64_t workgroups, int64_t blocks, int64_t outputs) {
   int64_t n = least_of(512 / workgroups, blocks / 2);
   while (n > 1 && n * n * outputs > 4800 * blocks) --n;
@@ -75,9 +75,9 @@ inline int64_t tile_splits(int64_t workgroups, int64_t blocks, int64_t outputs) 
 constexpr int kWalkFill = 2048;
 
 // Waves of a few-vector workgroup.  Where there are workgroups for less than half the CUs, eight: more of
-// their keys are on their way at once (573 keys of one row 8.8 -> 7.9 us).  Where there are two waves for
+// their keys are on their way at once (573 keys of one row 9.7 -> 8.6 us).  Where there are two waves for
 // every SIMD without a second one in a workgroup, and few keys each, one: nothing is joined (256 rows of
-// up to 112 keys behind a prefix of 3900: 77 -> 73 us).  Beside a prefix's workgroups never eight.
+// up to 112 keys behind a prefix of 3900: 59 -> 52 us).  Beside a prefix's workgroups never eight.
 inline void pick_waves(AttendLaunch& l, const AttendSizes& s, bool pair) {
   const int64_t workgroups = (int64_t)l.tiles * s.nkv * l.splits, keys = (int64_t)l.chunk * s.page_size;
   l.waves = workgroups >= 2048 && keys <= 512 ? 1 : workgroups <= 128 && !pair ? 8 : 4;
@@ -85,14 +85,15 @@ inline void pick_waves(AttendLaunch& l, const AttendSizes& s, bool pair) {
 
 // Chosen blocks: from so many waves on, and vectors of a sequence, waves walk the blocks of several tokens.
 // us, walked against a workgroup a token (32 + 8 heads of 128, 16 of 500 blocks): one sequence of 256
-// tokens 94 / 73, 512 (512 waves) 121 / 147, 1000 199 / 274, 2000 327 / 521; eight of 64 167 / 140, of 128
-// 196 / 267; heads of 64: 256 tokens 70 / 39, 1000 133 / 144.
+// tokens 100 / 74, 512 (512 waves) 124 / 137, 1000 197 / 265, 2000 324 / 518; eight of 64 (512 waves) 182 / 131, of 128
+// 200 / 258; heads of 64: 256 tokens 76 / 37, 1000 145 / 129.  So the best border depends on the sequences and the heads
+// too: at 512 waves either side wins, and with heads of 64 the walk loses up to 1000 tokens.
 constexpr int kWalkWaves = 640, kWalkLeast = 128;
 
 // Keys of the prefix that the sequences' workgroups would read, from which it is walked on its own, for
 // all sequences together: that takes another launch.  us, alone against with each (32 + 8 heads of 128):
-// 512 keys and 64 sequences (262144) 18 / 13, 128 of them 21 / 25, 256 26 / 45; 1024 and 32 19 / 16, 64 21 / 26;
-// 4096 and 8 (262144) 17 / 20, 16 26 / 30.
+// 512 keys and 64 sequences (262144) 16.7 / 13.4, 128 of them 22.7 / 25.0, 256 24.3 / 44.1; 1024 and 32 16.8 / 15.7, 64
+// (524288) 20.1 / 18.3; 4096 and 8 (262144) 13.6 / 16.1, 16 18.6 / 21.7: a long prefix gains somewhat earlier, a short one later.
 constexpr int64_t kSharedKeys = 400000;
 
 inline AttendPlan plan_attend(const AttendSizes& s) {
@@ -126,7 +127,9 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
     return p;
   }
   // (us, of sequences of up to 64 vectors with few-vector workgroups in brackets: 4 of 8 tokens of 4 heads over 2000 keys
-  // 18.1 (16.6), but 64 of 16 tokens 109 (173), whose keys a tile reads once)
+  // 18.6 (15.9), but 64 of 16 tokens 111 (158), whose keys a tile reads once.  All sequences go by the longest: a call
+  // that mixes prompts and single tokens gives each of these a tile, most of it empty, and walks its keys in
+  // a few workgroups, and its prefix once a sequence.)
   p.own.few = vectors <= kFewVectors || !s.starts;
   const bool separate = p.own.few && (int64_t)s.n_seqs * s.nkv * s.prefix_length >= kSharedKeys;
   if (p.own.few) {
@@ -142,8 +145,8 @@ inline AttendPlan plan_attend(const AttendSizes& s) {
   }
   if (separate) {
     const int64_t all = (int64_t)s.n_tokens * group;
-    // (us, as tiles in brackets: 16 vectors over 8192 keys 16.3 (18.1), 32 of them 16.2 (19.1), but 64
-    // 21.9 (20.9))
+    // (us, as tiles in brackets: 16 vectors over 8192 keys 16.3 (22.1), 32 of them 17.2 (20.5), but 64
+    // 23.6 (22.5))
     p.prefix.few = all <= 2 * kFewVectors;
     p.prefix.tiles = (int)ceil_div(all, p.prefix.few ? kFewVectors : kTileVectors);
     const int64_t workgroups = (int64_t)p.prefix.tiles * s.nkv, blocks = ceil_div(s.prefix_length, kTileKeys);

@@ -13,14 +13,14 @@
 //  * few vectors (a decode step: G vectors against a sequence's keys).  Bound by
 //    reading the cache once.  Keys and values go from memory straight to the registers of
 //    the wave that uses them: nothing is shared between waves, so a stage in LDS would only
-//    add a copy and a barrier.  32 contexts of 1000 to 32,000 keys, 8-bit, 8 kv heads of 128: 1.16 GB in 221 us,
-//    5.3 TB/s; 4 of 32,000, fp16: 524 MB in 100 us.
+//    add a copy and a barrier.  32 contexts of 1000 to 32,000 keys, 8-bit, 8 kv heads of 128: 1.16 GB in 227 us,
+//    5.1 TB/s; 4 of 32,000, fp16: 524 MB in 99 us.
 //  * tiles (prompts, rows, the shared prefix): 128 vectors against blocks of 64 keys
-//    in LDS.  Bound by the matrix and vector units: a prompt of 8448 tokens, 32 + 8 heads of 128, 573 to 588 us,
-//    some 1000 TFLOP/s, matrix instructions 44% of the time.
+//    in LDS.  Bound by the matrix and vector units: a prompt of 8448 tokens, 32 + 8 heads of 128, 784 to 810 us,
+//    740 TFLOP/s and half as much again for the weights' second terms, matrix instructions 50% of the time.
 //  * both at once: single tokens behind a long prefix, whose keys tiles of all sequences' tokens read once
-//    (256 tokens behind 8192 keys 66 us and 10 to join).
-//  * a walk over the blocks that a sequence's tokens chose (2000 tokens, 16 of 500 blocks: 285 us).  Bound by the
+//    (256 tokens behind 8192 keys 79 us and 9 to join).
+//  * a walk over the blocks that a sequence's tokens chose (2000 tokens, 16 of 500 blocks: 324 us).  Bound by the
 //    latency of loads at two waves a SIMD.
 //
 // All compute S^T = K Q^T and O^T = V^T P^T with the 16x16x32 instruction, so
@@ -211,7 +211,7 @@ constexpr int kFewWaves = 4;
 // A wave that takes 16 QS vectors against 32 keys at a time, which come from memory to its
 // registers, the next chunk's while this one is worked on.  Lanes side by side read a row:
 // the caches take four lanes' 64 bytes at a time if they adjoin (a row to each lane, as the first product
-// has them, took four times the accesses, and bound the walk over chosen blocks: 403 us).  So
+// has them, took four times the accesses, and bound the walk over chosen blocks: 403 us, 350 with this).  So
 // keys change lanes, through LDS of the wave's own, without a barrier.  Of the values a lane has
 // 8 rows (its group's keys), 16 lanes side by side along hd; the second product needs 8 keys of a
 // dimension in a lane, so the rows are transposed in registers, half a v_perm an element.
@@ -1420,8 +1420,8 @@ __global__ __launch_bounds__(256) void combine_kernel(const Args a) {
 }
 
 // ---------------------------------------------------------------- kernels
-// (with 8-bit pages three waves fit a SIMD, which reads faster: 32 contexts of up to 32,000 tokens 222 us,
-// of two 262)
+// (with 8-bit pages three waves fit a SIMD, which reads faster: 32 contexts of up to 32,000 tokens 227 us,
+// of two 268)
 template <typename T, bool E8, int HD, bool BLOCKS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, E8 && WAVES == 4 ? 3 : 2) void few_kernel(const Args a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
