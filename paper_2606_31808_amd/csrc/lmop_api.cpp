@@ -1860,6 +1860,7 @@ lmop_status lmop_create(const lmop_config* cfg, int32_t device, void* hip_stream
   st = dev_alloc(cp, &rt, (size_t)cf.max_seq * half * sizeof(float2));
   if (st != LMOP_OK) return bail(st);
   c->rope_tab = (float2*)rt;
+  (void)hipGetLastError();  // what an earlier call of the program left
   if (launch_rotary(nullptr, c->rope_tab, cf.max_seq, half, freqs) != hipSuccess ||
       hipStreamSynchronize(nullptr) != hipSuccess)
     return bail(fail(cp, LMOP_ERR_DEVICE, "the rotary table was not made"));

@@ -1,9 +1,12 @@
 """The paged cache's operators where their sizes, values and uses are out of the ordinary; batches, the definition in
 64 bits and its tolerances are test_gpu_paged's."""
+import copy
+import math
+
 import pytest
 import torch
 
-from tests.test_gpu_paged import E4M3, NAN, Batch, L, Shape, _ctx, _gen, _reference  # noqa: F401
+from tests.test_gpu_paged import E4M3, NAN, Batch, L, Shape, _check, _ctx, _gen, _reference  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -119,7 +122,6 @@ def test_attend_is_as_exact_as_its_type(L, dtype, cache, nq, nkv, hd, page, new,
 def test_attend_many_keys_of_little_weight(L, dtype, new, length, prefix, n_blocks, nq, nkv):  # noqa: F811
     """One key of weight 1 whose value is zero, and thousands of weight 2^-26 with a value of one: all that the
     result has comes from these."""
-    import math
     print("tail", dtype, new, length, prefix, n_blocks, flush=True)
     hd, page = 64, 16
     b = Batch(nq, nkv, hd, dtype, dtype, page, new, length, prefix, seed=1)
@@ -366,3 +368,24 @@ def test_attend_infinite_values(L, dtype, nq, nkv, hd, page, new, length, prefix
     same = (got == want) | (got.isnan() & want.isnan())
     assert not torch.isfinite(want).all()
     assert same.all(), [(i, got[tuple(i)].item(), want[tuple(i)].item()) for i in (~same).nonzero()[:6].tolist()]
+
+
+@pytest.mark.parametrize("dtype,cache,hd", [("f16", "f16", 64), ("bf16", "bf16", 128), ("f16", "e4m3", 128), ("bf16", "e4m3", 64)])
+@pytest.mark.parametrize("nq,nkv,new,length,prefix", [
+    (4, 2, [3, 1], [1, 0], 37), (7, 1, [8], [5], 7), (4, 2, [40, 60, 2], [10, 0, 2], 100), (4, 4, [2, 3] * 30, [0, 9] * 30, 3000),
+    (8, 1, [38, 13], [35, 15], 5000), (16, 2, [2, 1, 2], [0, 5, 2], 130)])
+def test_attend_tokens_before_their_sequence_see_the_prefix(L, dtype, cache, hd, nq, nkv, new, length, prefix):  # noqa: F811
+    """All of it, whatever their index; every other token its own keys too."""
+    print("before, prefix", dtype, cache, hd, nq, nkv, new[:4], length[:4], prefix, flush=True)
+    b = Batch(nq, nkv, hd, dtype, cache, 16, new, length, prefix, seed=6)
+    index = torch.tensor([m - n + j for n, m in zip(new, length) for j in range(n)])
+    early = (index < 0).nonzero()[:, 0]
+    lse = torch.full((b.tokens, nq), 7.0, device="cuda")
+    out = b.attend(_ctx(L, nq, nkv, hd), L, lse=lse)
+    alone = copy.copy(b)  # the same cache, each such token a sequence without keys
+    alone.new, alone.len, alone.q, alone.tokens = [1] * len(early), [0] * len(early), b.q[early], len(early)
+    alone.table = b.table[:1].expand(len(early), -1)
+    _check(alone, out[early.cuda()], lse[early.cuda()], _reference(alone))
+    ref = [x.clone() for x in _reference(b)]
+    ref[1][early] = NAN  # (left out by _check)
+    _check(b, out, lse, ref)
