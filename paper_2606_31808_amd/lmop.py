@@ -1000,6 +1000,8 @@ class Context:
         self._here(q)
         if out is None:
             out = q.new_empty((q.shape[0], self.heads[1], n_blocks), dtype=torch.int32)
+        elif out.dim() != 3 or out.shape[2] != n_blocks:
+            raise ValueError(f"out of shape {tuple(out.shape)} for {n_blocks} blocks")
         if max_length is None:
             max_length = table.shape[1] * cache.page_size
         lmop_select_blocks(self.ctx, self.heads, cache, q, out, table, length, start, max_length)

@@ -423,3 +423,14 @@ def test_binding_refuses_lists_of_no_blocks(ctx):
         ctx.select_blocks(c, x, 0, **a)
     with pytest.raises(ValueError, match="n_blocks at least 1"):
         ctx.select_blocks(c, x, 2, out=none, **a)
+
+
+def test_binding_select_refuses_an_out_of_another_number_of_blocks(ctx):
+    """The number asked for is the number chosen."""
+    x = torch.zeros(3, 256, dtype=torch.float16)
+    a = dict(table=torch.zeros(3, 2, dtype=torch.int32), length=torch.ones(3, dtype=torch.int32))
+    c = _host_cache(mean=torch.zeros(6, 4, 64, dtype=torch.float16))
+    assert _status(ctx.select_blocks, c, x, 2, out=torch.zeros(3, 4, 2, dtype=torch.int32), **a) == UNS
+    for out in (torch.zeros(3, 4, 3, dtype=torch.int32), torch.zeros(3, 4, 1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="for 2 blocks"):
+            ctx.select_blocks(c, x, 2, out=out, **a)
