@@ -968,6 +968,8 @@ class Context:
         (None: a token each) are int32 on the device.  Returns the rotated queries
         (q_out, or a new tensor; None without q)."""
         self._here(k)
+        if q is None and q_out is not None:
+            raise ValueError("q_out without q")
         if q is not None and q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         lmop_cache_append(self.ctx, self.heads, cache, k, v, table, length, start, first, rotate, q, q_out)

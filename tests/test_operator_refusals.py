@@ -434,3 +434,12 @@ def test_binding_select_refuses_an_out_of_another_number_of_blocks(ctx):
     for out in (torch.zeros(3, 4, 3, dtype=torch.int32), torch.zeros(3, 4, 1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)):
         with pytest.raises(ValueError, match="for 2 blocks"):
             ctx.select_blocks(c, x, 2, out=out, **a)
+
+
+def test_binding_append_refuses_queries_to_write_without_any(ctx):
+    """They came back as they were, as if rotated."""
+    x = torch.zeros(3, 256, dtype=torch.float16)
+    a = dict(table=torch.zeros(3, 2, dtype=torch.int32), length=torch.ones(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="q_out without q"):
+        ctx.cache_append(_host_cache(), x, x, q_out=torch.zeros_like(x), **a)
+    assert _status(ctx.cache_append, _host_cache(), x, x, **a) == UNS
