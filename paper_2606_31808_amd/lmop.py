@@ -1003,7 +1003,7 @@ class Context:
         if out is None:
             out = q.new_empty((q.shape[0], self.heads[1], n_blocks), dtype=torch.int32)
         elif out.dim() != 3 or out.shape[2] != n_blocks:
-            raise ValueError(f"out of shape {tuple(out.shape)} for {n_blocks} blocks")
+            raise ValueError(f"out of shape {tuple(out.shape)} for {n_blocks} blocks (n_blocks at least 1)")
         if max_length is None:
             max_length = table.shape[1] * cache.page_size
         lmop_select_blocks(self.ctx, self.heads, cache, q, out, table, length, start, max_length)
