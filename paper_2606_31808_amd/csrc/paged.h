@@ -46,9 +46,9 @@ struct Half<bf16> {
 //
 // In one term results were 1.25 to 1.3 times as far from the formula as their own rounding takes them, and fp16 weights
 // below 2^-25 were lost however many.  The second term is a second product with the values, half as much again for the
-// matrix units: a prompt of 8448 tokens 583 -> 784 us (1.1 PFLOP/s with it, what a large library product reaches), 272 rows
-// behind 512 keys 280 -> 338, 256 tokens behind 8192 keys 76 -> 87, the walk over chosen blocks 285 -> 325; single tokens,
-// whose matrix units wait for memory, 1 to 2%.
+// matrix units: a prompt of 8448 tokens 583 -> 790 us (1.1 PFLOP/s with it, what a large library product reaches), 272 rows
+// behind 512 keys 280 -> 345, 256 tokens behind 8192 keys 76 -> 88, the walk over chosen blocks 285 -> 325; long single
+// tokens, whose matrix units wait for memory, 1 to 2%, one over 573 keys 8.3 -> 8.8.
 template <typename T>
 struct Weights {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
